@@ -258,6 +258,60 @@ ppow_status ppow_expected_acceptance(const ppow_params *params,
 ppow_status ppow_reference_logprob(const ppow_params *params, const void *ref_target_logits,
                                    const int32_t *valid_len, float *row_logp, float *ref_logp, void *cuda_stream);
 
+/*
+ * Log-probability of given tokens straight from hidden states and the head's weight (the token terms of the
+ * clipped objective, Sec. 4.1, and of the supervised loss, App. C.2), without keeping the logits:
+ *     z = hidden weight^T / temperature        lse = log sum_v exp(z_v)        logp = z_y - lse
+ * The cross entropy of a token is -logp.  Products are of the storage type with float32 sums; maximum, sum and
+ * logarithm are float32 per 256 vocabulary entries and float64 across them.
+ */
+typedef struct {
+    int32_t T;              /* tokens, 0 .. 2^20 */
+    int32_t V;              /* vocabulary size, 2 .. 2^22 */
+    int32_t D;              /* width of the hidden states, a multiple of 8, 8 .. 65536 */
+    int32_t dtype;          /* PPOW_BF16 or PPOW_F16: hidden, weight and their gradients */
+    int64_t hidden_stride;  /* elements from one row of hidden to the next, >= D */
+    int64_t weight_stride;  /* elements from one row of weight to the next, >= D, a multiple of 8 */
+    float temperature;      /* > 0 */
+} ppow_head_params;
+
+/* Bytes of device scratch for these parameters (0 on invalid ones); backward != 0: for the gradient.  The gradient
+ * works on pieces of the vocabulary; its scratch holds one piece of dz (at most 512 MiB, or 256 vocabulary entries),
+ * float32 sums of grad_hidden and a copy of the live rows. */
+size_t ppow_head_workspace_bytes(const ppow_head_params *params, int backward);
+
+/*
+ *   hidden      device, [T, D], rows hidden_stride apart, aligned to its element size
+ *   weight      device, [V, D], rows weight_stride apart, 16-byte aligned
+ *   tokens      device, [T] int32.  A negative token masks its row: the row's hidden state is not used (it may hold
+ *               anything) and logp = lse = 0.  A token >= V gets logp = -inf and sets PPOW_FLAG_TOKEN_RANGE.
+ *   logp, lse   device, [T] float32
+ *   workspace   device, >= ppow_head_workspace_bytes(params, 0), 256-byte aligned; ppow_read_error_flags works on it
+ * Rows that are not masked must hold finite values.  The error flag PPOW_FLAG_DEVICE_TIMEOUT as for ppow_score_windows.
+ */
+ppow_status ppow_head_logprob(const ppow_head_params *params, const void *hidden, const void *weight, const int32_t *tokens,
+                              float *logp, float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Gradient of sum_i grad_logp[i] * logp[i] with respect to hidden and weight:
+ *     dz_i = grad_logp[i] / temperature * (onehot(y_i) - softmax(z_i))     grad_hidden = dz weight     grad_weight = dz^T hidden
+ * dz is rounded to the storage type (a relative error of at most half a step per term, of the size of the operands' own
+ * rounding); for PPOW_F16 each row of it is brought near 2^15 by a power of two first, which is undone after the sums.
+ * The sums are float32 in a fixed order: equal inputs give equal results.
+ *   hidden, weight, tokens   as above.  Rows with a negative token, a token >= V (which sets PPOW_FLAG_TOKEN_RANGE) or
+ *                            grad_logp == 0 are masked: their gradient is 0 and they add nothing to grad_weight.
+ *   lse          device, [T] float32, as written by ppow_head_logprob (not read at masked rows)
+ *   grad_logp    device, [T] float32
+ *   grad_hidden  device, [T, D] of the storage type, contiguous, 16-byte aligned, or NULL
+ *   grad_weight  device, [V, D] of the storage type, contiguous, 16-byte aligned, or NULL (a frozen head).  At least one
+ *                of the two is required.  T == 0 sets grad_weight to 0.
+ *   workspace    device, >= ppow_head_workspace_bytes(params, 1), 256-byte aligned
+ */
+ppow_status ppow_head_logprob_backward(const ppow_head_params *params, const void *hidden, const void *weight,
+                                       const int32_t *tokens, const float *lse, const float *grad_logp,
+                                       void *grad_hidden, void *grad_weight,
+                                       void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 /* Copies the error word that the last ppow_score_windows call on `workspace` left behind into
  * *flags_host (PPOW_FLAG_* bits) and synchronises `cuda_stream` to do so.  Returns
  * PPOW_ERR_DEVICE_TIMEOUT if that bit is set, PPOW_ERR_CUDA on a CUDA failure, else PPOW_OK. */

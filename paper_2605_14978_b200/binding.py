@@ -6,6 +6,7 @@ PyTorch is used for device memory and streams only.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -32,6 +33,7 @@ EXPORTS = ("ppow_score_workspace_bytes", "ppow_score_windows", "ppow_score_windo
            "ppow_noalloc_read_error_flags",
            "ppow_group_advantage", "ppow_sequence_windows", "ppow_sequence_windows_mixed", "ppow_expected_acceptance",
            "ppow_reference_logprob", "ppow_selftest_wait_timeout", "ppow_stream_read_probe", "ppow_score_kernel_launches",
+           "ppow_head_workspace_bytes", "ppow_head_logprob", "ppow_head_logprob_backward",
            "ppow_checked_failures", "ppow_timeline_read", "ppow_status_string", "ppow_version")
 
 POSITION_OUTPUTS = {"accept_flag": torch.uint8, "kl": torch.float32, "conf": torch.float32, "crit": torch.float32,
@@ -58,6 +60,11 @@ class ppow_outputs(ctypes.Structure):
                 ("accept_flag", "accepted_len", "reward_speedup", "reward_dist", "reward", "delta", "score",
                  "kl", "conf", "crit", "logp_tok", "logq_tok", "target_argmax",
                  "kl_rev", "kl_rev_mean", "nabla", "lse_p", "lse_q")]
+
+
+class ppow_head_params(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("V", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("hidden_stride", ctypes.c_int64), ("weight_stride", ctypes.c_int64), ("temperature", ctypes.c_float)]
 
 
 class PpowError(RuntimeError):
@@ -120,6 +127,12 @@ def load_library():
     lib.ppow_stream_read_probe.argtypes = [vp, sz, vp, vp]
     lib.ppow_score_kernel_launches.restype = ctypes.c_int
     lib.ppow_score_kernel_launches.argtypes = [ctypes.POINTER(ppow_params)]
+    lib.ppow_head_workspace_bytes.restype = sz
+    lib.ppow_head_workspace_bytes.argtypes = [ctypes.POINTER(ppow_head_params), ctypes.c_int]
+    lib.ppow_head_logprob.restype = ctypes.c_int
+    lib.ppow_head_logprob.argtypes = [ctypes.POINTER(ppow_head_params), vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.ppow_head_logprob_backward.restype = ctypes.c_int
+    lib.ppow_head_logprob_backward.argtypes = [ctypes.POINTER(ppow_head_params), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ppow_checked_failures.restype = ctypes.c_int
     lib.ppow_checked_failures.argtypes = [ctypes.POINTER(ctypes.c_uint32), ctypes.POINTER(ctypes.c_uint32)]
     lib.ppow_timeline_read.restype = ctypes.c_int
@@ -436,6 +449,93 @@ def ppow_reference_logprob(params: ppow_params, ref_target_logits, valid_len, ro
         raise PpowError(st, "ppow_reference_logprob")
 
 
+def _rows_ptr(t: torch.Tensor, dtype, name):
+    """Pointer and row stride (elements) of a 2-D tensor whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError("%s must live on a CUDA device (no CPU path exists)" % name)
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("%s must be 2-D with contiguous rows" % name)
+    if t.dtype != dtype:
+        raise ValueError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _check_shape(t: Optional[torch.Tensor], shape, name):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+
+
+def _check_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError("%s must live on %s, got %s" % (name, dev, t.device))
+
+
+@contextlib.contextmanager
+def _on(dev, stream):
+    """Current device ``dev`` and, if given, current stream ``stream``: what is allocated inside belongs to that stream,
+    so that the allocator hands it on only behind the work enqueued there."""
+    with torch.cuda.device(dev):
+        if stream is None:
+            yield
+        else:
+            with torch.cuda.stream(stream):
+                yield
+
+
+def make_head_params(hidden, weight, temperature=1.0) -> ppow_head_params:
+    """Sizes, type and row strides of a head call, from its tensors ``hidden`` [T, D] and ``weight`` [V, D]."""
+    if hidden.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("hidden must be bfloat16 or float16, got %s" % hidden.dtype)
+    _, hs = _rows_ptr(hidden, hidden.dtype, "hidden")
+    _, ws = _rows_ptr(weight, hidden.dtype, "weight")
+    _check_shape(weight, (weight.shape[0], hidden.shape[1]), "weight")
+    return ppow_head_params(int(hidden.shape[0]), int(weight.shape[0]), int(hidden.shape[1]), DTYPE_CODES[hidden.dtype], int(hs),
+                            int(ws), float(temperature))
+
+
+def ppow_head_workspace_bytes(params: ppow_head_params, backward: bool) -> int:
+    return int(load_library().ppow_head_workspace_bytes(ctypes.byref(params), 1 if backward else 0))
+
+
+def _check_head(params, hidden, weight, **per_token):
+    _check_shape(hidden, (params.T, params.D), "hidden")
+    _check_shape(weight, (params.V, params.D), "weight")
+    for name, t in per_token.items():
+        _check_shape(t, (params.T,), name)
+    _check_device(hidden.device, weight=weight, **per_token)
+
+
+def ppow_head_logprob(params: ppow_head_params, hidden, weight, tokens, logp, lse, workspace, stream=None) -> None:
+    """Enqueue log-probabilities of ``tokens`` [T] from ``hidden`` [T, D] and ``weight`` [V, D] into ``logp`` and ``lse``."""
+    dt = LOGIT_DTYPES[params.dtype]
+    _check_head(params, hidden, weight, tokens=tokens, logp=logp, lse=lse)
+    st = load_library().ppow_head_logprob(
+        ctypes.byref(params), _rows_ptr(hidden, dt, "hidden")[0], _rows_ptr(weight, dt, "weight")[0],
+        _dev_ptr(tokens, torch.int32, "tokens"), _dev_ptr(logp, torch.float32, "logp"), _dev_ptr(lse, torch.float32, "lse"),
+        _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream_ptr(stream))
+    if st != PPOW_OK:
+        raise PpowError(st, "ppow_head_logprob")
+
+
+def ppow_head_logprob_backward(params: ppow_head_params, hidden, weight, tokens, lse, grad_logp, grad_hidden, grad_weight, workspace,
+                               stream=None) -> None:
+    """Enqueue the gradient of sum(grad_logp * logp); ``grad_hidden`` or ``grad_weight`` may be None."""
+    dt = LOGIT_DTYPES[params.dtype]
+    _check_head(params, hidden, weight, tokens=tokens, lse=lse, grad_logp=grad_logp)
+    _check_shape(grad_hidden, (params.T, params.D), "grad_hidden")
+    _check_shape(grad_weight, (params.V, params.D), "grad_weight")
+    _check_device(hidden.device, grad_hidden=grad_hidden, grad_weight=grad_weight, workspace=workspace)
+    st = load_library().ppow_head_logprob_backward(
+        ctypes.byref(params), _rows_ptr(hidden, dt, "hidden")[0], _rows_ptr(weight, dt, "weight")[0],
+        _dev_ptr(tokens, torch.int32, "tokens"), _dev_ptr(lse, torch.float32, "lse"),
+        _dev_ptr(grad_logp, torch.float32, "grad_logp"), _dev_ptr(grad_hidden, dt, "grad_hidden"),
+        _dev_ptr(grad_weight, dt, "grad_weight"), _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
+        _stream_ptr(stream))
+    if st != PPOW_OK:
+        raise PpowError(st, "ppow_head_logprob_backward")
+
+
 def _host_ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
     if t is None:
         return None
@@ -504,3 +604,27 @@ def select_windows(score, n_keep: int, want_mask: bool = False, stream=None):
         ws = alloc_workspace(ppow_select_workspace_bytes(N), dev)
         ppow_select_windows(score, n_keep, sel, mask, ws, stream)
     return (sel, mask) if want_mask else sel
+
+
+def head_logprob(hidden, weight, tokens, *, temperature=1.0, stream=None) -> dict:
+    """Allocate outputs and workspace, run ppow_head_logprob; returns logp and lse, both [T] float32."""
+    params = make_head_params(hidden, weight, temperature)
+    dev = hidden.device
+    with _on(dev, stream):
+        out = {"logp": torch.empty((params.T,), dtype=torch.float32, device=dev),
+               "lse": torch.empty((params.T,), dtype=torch.float32, device=dev)}
+        ws = alloc_workspace(ppow_head_workspace_bytes(params, False), dev)
+        ppow_head_logprob(params, hidden, weight, tokens, out["logp"], out["lse"], ws, stream)
+    return out
+
+
+def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature=1.0, want_hidden=True, want_weight=True, stream=None):
+    """Allocate gradients and workspace, run ppow_head_logprob_backward; returns (grad_hidden, grad_weight), None where not wanted."""
+    params = make_head_params(hidden, weight, temperature)
+    dev = hidden.device
+    with _on(dev, stream):
+        gh = torch.empty((params.T, params.D), dtype=hidden.dtype, device=dev) if want_hidden else None
+        gw = torch.empty((params.V, params.D), dtype=hidden.dtype, device=dev) if want_weight else None
+        ws = alloc_workspace(ppow_head_workspace_bytes(params, True), dev)
+        ppow_head_logprob_backward(params, hidden, weight, tokens, lse, grad_logp, gh, gw, ws, stream)
+    return gh, gw

@@ -39,4 +39,5 @@ static inline int read_check_counters(unsigned int *failures, unsigned int *firs
 #define PPOW_CHECK(cond, site, error_word) (true)
 #endif
 
-// Check sites (reported by ppow_checked_failures): 1xx row reduction, 2xx window scan, 3xx selection, 4xx training side.
+// Check sites (reported by ppow_checked_failures): 1xx row reduction, 2xx window scan, 3xx selection, 4xx training side,
+// 5xx head log-probability.

@@ -1,0 +1,887 @@
+// Log-probability of given tokens straight from hidden states and the head's weight, and its gradient, without keeping
+// the logits (the token terms of the objective of Sec. 4.1 and of the supervised loss of App. C.2):
+//   z = h W^T / T,   lse = log sum_v exp z_v,   logp = z_y - lse,
+//   dz_v = g/T ([v = y] - exp(z_v - lse)),   dh = dz W,   dW = dz^T h      (g: the gradient that arrives at logp).
+//
+// Steps of a call:
+//   gather    live rows of `hidden` are copied, in order, to the front of a workspace array (masked rows are skipped, so
+//             whatever they hold touches nothing and costs nothing; rows of any stride and alignment become tiles)
+//   forward   logits by tiles of 256 tokens x 256 vocabulary entries; each tile leaves a maximum and a sum of exponentials
+//             per row; `merge` joins them in float64
+//   backward  per piece of the vocabulary: logits again, dz rounded to the operands' 16-bit type; dW of the piece, and the
+//             piece's share of dh added to float32 sums; `finish` rounds dh once
+// All three products run in one kernel template on tcgen05 (ppow_mma.cuh).
+#include "../../include/ppow.h"
+#include "ppow_checked.cuh"
+#include "ppow_device.cuh"
+#include "ppow_mma.cuh"
+
+#include <cuda_bf16.h>
+#include <math.h>
+
+namespace ppow {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr int TILE = 256;            // rows and columns of an output tile (a pair of CTAs)
+constexpr int HALF_TILE = 128;       // rows of A and columns of B that one CTA holds
+constexpr int BK = 64;               // products' inner step per pipeline stage: one 128-byte swizzle row
+constexpr int STAGES = 6;
+constexpr uint32_t OPERAND_BYTES = HALF_TILE * BK * 2;     // 16 KB
+constexpr uint32_t STAGE_BYTES = 2 * OPERAND_BYTES;
+constexpr int MMA_THREADS = 192;     // producer warp, issuing warp, four epilogue warps
+constexpr size_t MMA_SMEM = 1024 + (size_t)STAGES * STAGE_BYTES + 256;
+
+constexpr int GATHER_THREADS = 256;
+constexpr int GATHER_ROWS_MAX = 1024, GATHER_CTAS = 1024;
+constexpr size_t HEADER_BYTES = 256;
+constexpr size_t DZ_BYTES = 512u << 20;      // a piece of dz holds at most this much
+constexpr int MAX_SPLIT = 16;
+constexpr int32_t MAX_TOKENS = 1 << 20, MAX_VOCAB = 1 << 22, MAX_WIDTH = 1 << 16;
+
+// First bytes of the workspace; error_flags sits where ppow_read_error_flags looks for it.
+struct HeadHeader {
+    unsigned int unused;
+    unsigned int error_flags;
+    int32_t live;          // live rows
+    float out_scale;       // factor of dW (f16: undoes the power of two that the rows were brought to)
+};
+
+// Arrays of the workspace, all indexed by live row.
+struct HeadRows {
+    HeadHeader *header;
+    int32_t *source;       // row of `hidden`
+    int32_t *token;
+    float *mult;           // dz = mult * (softmax - onehot)
+    float *lse2;           // normaliser in log2 units
+    float *row_scale;      // dh = row_scale * (dz W)
+    void *rows;            // [padded, D] hidden states
+    void *scaled;          // f16 backward: the same times a power of two per row
+};
+
+__device__ __forceinline__ void fault(HeadHeader *h, unsigned int bit) { atomicOr(&h->error_flags, bit); }
+
+// ---- gather -----------------------------------------------------------------------------------------
+struct GatherJob {
+    const uint16_t *hidden;
+    const int32_t *tokens;
+    const float *lse, *grad;
+    float *logp_out, *lse_out;      // forward: masked rows receive 0
+    uint16_t *grad_hidden;          // backward: masked rows receive 0 (may be null)
+    int64_t stride;
+    int32_t T, D, V, rows_per_cta;
+    float inv_temperature;
+    bool vec;                       // rows start on 16-byte boundaries
+};
+
+// mult of a row, and for f16 the split into a factor near 2^15 and a power of two: dz of a row whose gradient is small
+// would fall below f16's smallest values.
+__device__ __forceinline__ float row_mult(float g, float inv_temperature) { return -g * inv_temperature; }
+
+// Every CTA looks at all T tokens (4 bytes each, from L2) to learn where its rows go, instead of waiting for a scan kernel.
+template <bool BACKWARD, bool SCALED>
+__global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob job, HeadRows out)
+{
+    __shared__ int32_t part[4][GATHER_THREADS / 32];
+    __shared__ int32_t dest[GATHER_ROWS_MAX];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int32_t r0 = (int32_t)min((int64_t)blockIdx.x * job.rows_per_cta, (int64_t)job.T);
+    const int32_t n = min(job.rows_per_cta, job.T - r0);
+    auto live = [&](int32_t i) {
+        const int32_t y = job.tokens[i];
+        if (BACKWARD) return y >= 0 && y < job.V && !(job.grad[i] == 0.0f);
+        return y >= 0;
+    };
+    int32_t before = 0, total = 0, top = -1000, range = 0;
+    for (int32_t i = tid; i < job.T; i += GATHER_THREADS) {
+        const bool ok = live(i);
+        total += ok;
+        before += ok && i < r0;
+        range |= job.tokens[i] >= job.V;
+        if (SCALED && ok) {
+            const float m = row_mult(job.grad[i], job.inv_temperature);
+            int e;
+            if (isfinite(m) && m != 0.0f) {
+                frexpf(m, &e);
+                top = max(top, e);
+            }
+        }
+    }
+    before = __reduce_add_sync(0xffffffffu, before);
+    total = __reduce_add_sync(0xffffffffu, total);
+    top = __reduce_max_sync(0xffffffffu, top);
+    range = __reduce_or_sync(0xffffffffu, range);
+    if (lane == 0) {
+        part[0][warp] = before;
+        part[1][warp] = total;
+        part[2][warp] = top;
+        part[3][warp] = range;
+    }
+    __syncthreads();
+    before = total = range = 0;
+    top = -1000;
+#pragma unroll
+    for (int w = 0; w < GATHER_THREADS / 32; ++w) {
+        before += part[0][w];
+        total += part[1][w];
+        top = max(top, part[2][w]);
+        range |= part[3][w];
+    }
+    if (top == -1000) top = 0;
+    if (blockIdx.x == 0 && tid == 0) {
+        out.header->error_flags = range ? (unsigned)PPOW_FLAG_TOKEN_RANGE : 0u;
+        out.header->live = total;
+        out.header->out_scale = SCALED ? ldexpf(1.0f, top - 15) : 1.0f;
+    }
+    if (warp == 0) {
+        int32_t next = before;
+        for (int32_t k = 0; k < n; k += 32) {
+            const bool ok = k + lane < n && live(r0 + k + lane);
+            const unsigned m = __ballot_sync(0xffffffffu, ok);
+            if (k + lane < n) dest[k + lane] = ok ? next + __popc(m & ((1u << lane) - 1u)) : -1;
+            next += __popc(m);
+        }
+    }
+    __syncthreads();
+
+    const int32_t units = job.D / 8;     // 16-byte units of a row
+    for (int32_t k = warp; k < n; k += GATHER_THREADS / 32) {
+        const int32_t r = r0 + k, d = dest[k];
+        if (d < 0) {
+            if (!BACKWARD && lane == 0) {
+                job.logp_out[r] = 0.0f;
+                job.lse_out[r] = 0.0f;
+            }
+            if (BACKWARD && job.grad_hidden)
+                for (int32_t u = lane; u < units; u += 32)
+                    reinterpret_cast<uint4 *>(job.grad_hidden + (size_t)r * job.D)[u] = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        if (!PPOW_CHECK(d < total && d <= r, 501, nullptr)) continue;
+        int e = 0;
+        if (lane == 0) {
+            out.source[d] = r;
+            out.token[d] = job.tokens[r];
+        }
+        if (BACKWARD) {
+            float m = row_mult(job.grad[r], job.inv_temperature), scale = 1.0f;
+            if (SCALED) {
+                m = frexpf(m, &e);
+                if (!isfinite(m) || m == 0.0f) e = top;
+                m = ldexpf(m, 15);
+                scale = ldexpf(1.0f, e - 15);
+            }
+            if (lane == 0) {
+                out.mult[d] = m;
+                out.row_scale[d] = scale;
+                out.lse2[d] = job.lse[r] * LOG2E;
+            }
+        }
+        const uint16_t *src = job.hidden + (size_t)r * job.stride;
+        uint4 *to = reinterpret_cast<uint4 *>((uint16_t *)out.rows + (size_t)d * job.D);
+        uint4 *to_scaled = SCALED ? reinterpret_cast<uint4 *>((uint16_t *)out.scaled + (size_t)d * job.D) : nullptr;
+        const float down = SCALED ? ldexpf(1.0f, e - top) : 1.0f;
+        for (int32_t u = lane; u < units; u += 32) {
+            uint4 x;
+            if (job.vec) {
+                x = __ldg(reinterpret_cast<const uint4 *>(src) + u);
+            } else {
+                uint32_t w[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) w[q] = (uint32_t)src[u * 8 + 2 * q] | ((uint32_t)src[u * 8 + 2 * q + 1] << 16);
+                x = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            to[u] = x;
+            if (SCALED) {
+                uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const __half2 h = *reinterpret_cast<__half2 *>(&w[q]);
+                    const __half2 s = __floats2half2_rn(__low2float(h) * down, __high2float(h) * down);
+                    w[q] = *reinterpret_cast<const uint32_t *>(&s);
+                }
+                to_scaled[u] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    }
+    // the last tile's rows behind the live ones are zeros: they are products' operands too
+    const int32_t padded = max(TILE, (total + TILE - 1) / TILE * TILE);
+    for (int32_t p = total + blockIdx.x * (GATHER_THREADS / 32) + warp; p < padded; p += gridDim.x * (GATHER_THREADS / 32)) {
+        if (lane == 0) {
+            out.token[p] = -1;
+            out.mult[p] = 0.0f;
+            out.lse2[p] = 0.0f;
+        }
+        for (int32_t u = lane; u < units; u += 32) {
+            reinterpret_cast<uint4 *>((uint16_t *)out.rows + (size_t)p * job.D)[u] = make_uint4(0, 0, 0, 0);
+            if (SCALED) reinterpret_cast<uint4 *>((uint16_t *)out.scaled + (size_t)p * job.D)[u] = make_uint4(0, 0, 0, 0);
+        }
+    }
+}
+
+// ---- the products -----------------------------------------------------------------------------------
+enum Product {
+    LOGITS_SUM,   // rows x W^T: maximum and sum of exponentials per row and tile
+    LOGITS_GRAD,  // rows x W^T: dz of a piece of the vocabulary
+    GRAD_HIDDEN,  // dz x W: the piece's share of dh
+    GRAD_WEIGHT   // dz^T x rows: dW of the piece
+};
+
+struct ProductJob {
+    HeadRows rows;
+    float scale;            // log2(e) / temperature
+    int32_t D, V;
+    int32_t v0, columns;    // the piece: vocabulary entries v0 .. v0 + columns - 1
+    int32_t v_tiles, d_tiles, splits;
+    int32_t piece;          // row length of dz
+    bool add;               // GRAD_HIDDEN: add to what the pieces before left
+    float2 *partial;        // LOGITS_SUM: [live row][v_tiles] maximum, sum (log2 units)
+    float *at_token;        // LOGITS_SUM: the token's product, per live row
+    uint16_t *dz;           // [padded rows][piece]
+    float *grad_rows;       // GRAD_HIDDEN: [splits][padded rows][D]
+    size_t split_stride;
+    uint16_t *grad_weight;  // [V, D]
+};
+
+struct Tile {
+    int32_t row, col;       // first row and column, in elements of the product's own axes
+    int32_t k0, k1;         // inner steps of BK
+    int32_t index, split;   // column tile; share of the inner axis
+};
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if (BF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+template <int PRODUCT>
+__device__ __forceinline__ int64_t tile_count(const ProductJob &job, int32_t row_tiles)
+{
+    if (PRODUCT == GRAD_HIDDEN) return (int64_t)row_tiles * job.d_tiles * job.splits;
+    if (PRODUCT == GRAD_WEIGHT) return (int64_t)job.v_tiles * job.d_tiles;
+    return (int64_t)row_tiles * job.v_tiles;
+}
+
+// Logit tiles go through all rows for one strip of W, then the next strip: W comes from HBM once, the rows stay in L2.
+template <int PRODUCT>
+__device__ __forceinline__ Tile tile_at(const ProductJob &job, int32_t row_tiles, int32_t live, int64_t t)
+{
+    Tile x;
+    x.split = 0;
+    if (PRODUCT == LOGITS_SUM || PRODUCT == LOGITS_GRAD) {
+        x.index = (int32_t)(t / row_tiles);
+        x.row = (int32_t)(t % row_tiles) * TILE;
+        x.col = job.v0 + x.index * TILE;
+        x.k0 = 0;
+        x.k1 = (job.D + BK - 1) / BK;
+    } else if (PRODUCT == GRAD_HIDDEN) {
+        x.index = (int32_t)(t % job.d_tiles);
+        const int32_t u = (int32_t)(t / job.d_tiles);
+        x.row = (u % row_tiles) * TILE;
+        x.split = u / row_tiles;
+        x.col = x.index * TILE;
+        const int32_t steps = (job.columns + BK - 1) / BK;
+        x.k0 = (int32_t)((int64_t)steps * x.split / job.splits);
+        x.k1 = (int32_t)((int64_t)steps * (x.split + 1) / job.splits);
+    } else {
+        x.index = (int32_t)(t % job.d_tiles);
+        x.row = (int32_t)(t / job.d_tiles) * TILE;
+        x.col = x.index * TILE;
+        x.k0 = 0;
+        x.k1 = max(1, (live + BK - 1) / BK);    // no live row: one step over rows of zeros
+    }
+    return x;
+}
+
+// Persistent: one CTA per SM, pair p takes tiles p, p + pairs, ...  Warp 0 keeps the operand ring full, one thread of
+// the leader's warp 1 issues the products into one of two accumulators, warps 2..5 read the other one out.
+template <int PRODUCT, bool BF16>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
+    head_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductJob job)
+{
+    constexpr bool A_K = PRODUCT != GRAD_WEIGHT;                                // the inner axis is contiguous in A
+    constexpr bool B_K = PRODUCT == LOGITS_SUM || PRODUCT == LOGITS_GRAD;
+    constexpr uint32_t INSTRUCTION = mma_instruction(BF16, A_K, B_K, TILE, TILE);
+    constexpr uint32_t BLOCK_BYTES = BK * 128;                                  // 64 wide x BK rows
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const uint32_t bars = smem + STAGES * STAGE_BYTES;
+    auto full = [&](uint32_t s) { return bars + 8 * s; };                       // the leader's count, for both CTAs
+    auto empty = [&](uint32_t s) { return bars + 8 * (STAGES + s); };
+    auto acc_full = [&](uint32_t b) { return bars + 8 * (2 * STAGES + b); };
+    auto acc_empty = [&](uint32_t b) { return bars + 8 * (2 * STAGES + 2 + b); };   // the leader's count, for both CTAs
+    const uint32_t tmem_slot = bars + 8 * (2 * STAGES + 4);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    HeadHeader *header = job.rows.header;
+
+    if (threadIdx.x == 0) {
+        prefetch_tensor_map(&map_a);
+        prefetch_tensor_map(&map_b);
+        for (uint32_t s = 0; s < STAGES; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (uint32_t b = 0; b < 2; ++b) {
+            mbar_init(acc_full(b), 1);
+            mbar_init(acc_empty(b), 8);     // four epilogue warps of each CTA
+        }
+        mbar_init_fence();
+    }
+    if (warp == 1) tmem_alloc_pair(tmem_slot);
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    tcgen05_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
+
+    const int32_t live = header->live;
+    int32_t row_tiles = (live + TILE - 1) / TILE;
+    if (PRODUCT != LOGITS_SUM) row_tiles = max(1, row_tiles);
+    const int64_t tiles = tile_count<PRODUCT>(job, row_tiles);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int64_t t = pair; t < tiles && ok; t += pairs) {
+                const Tile x = tile_at<PRODUCT>(job, row_tiles, live, t);
+                for (int32_t k = x.k0; k < x.k1 && ok; ++k, ++it) {
+                    const uint32_t s = it % STAGES, phase = (it / STAGES) & 1u;
+                    ok = mbar_wait_ns(empty(s), phase ^ 1u);
+                    if (!ok) break;
+                    if (rank == 0) mbar_arrive_expect_tx(full(s), 2 * STAGE_BYTES);
+                    const uint32_t bar = peer_addr(full(s), 0);
+                    const uint32_t a = smem + s * STAGE_BYTES, b = a + OPERAND_BYTES;
+                    const int32_t m = x.row + (int32_t)rank * HALF_TILE, n = x.col + (int32_t)rank * HALF_TILE;
+                    if (A_K) {
+                        tma_load_pair(a, &map_a, k * BK, m, bar);
+                    } else {
+                        tma_load_pair(a, &map_a, m, k * BK, bar);
+                        tma_load_pair(a + BLOCK_BYTES, &map_a, m + 64, k * BK, bar);
+                    }
+                    if (B_K) {
+                        tma_load_pair(b, &map_b, k * BK, n, bar);
+                    } else {
+                        const int32_t y = k * BK + (PRODUCT == GRAD_HIDDEN ? job.v0 : 0);
+                        tma_load_pair(b, &map_b, n, y, bar);
+                        tma_load_pair(b + BLOCK_BYTES, &map_b, n + 64, y, bar);
+                    }
+                }
+            }
+            // the leader's last commits land on this CTA's barriers: stay until they have
+            for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it && ok; ++j) ok = mbar_wait_ns(empty(j % STAGES), (j / STAGES) & 1u);
+            if (!ok) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && lane == 0) {
+            uint32_t it = 0, acc = 0;
+            bool ok = true;
+            for (int64_t t = pair; t < tiles && ok; t += pairs, ++acc) {
+                const Tile x = tile_at<PRODUCT>(job, row_tiles, live, t);
+                const uint32_t b = acc & 1u, d = tmem + b * TILE;
+                ok = mbar_wait_ns(acc_empty(b), ((acc >> 1) & 1u) ^ 1u);
+                tcgen05_fence_after();
+                for (int32_t k = x.k0; k < x.k1 && ok; ++k, ++it) {
+                    const uint32_t s = it % STAGES;
+                    ok = mbar_wait_ns(full(s), (it / STAGES) & 1u);
+                    if (!ok) break;
+                    tcgen05_fence_after();
+                    const uint32_t a = smem + s * STAGE_BYTES;
+                    const uint64_t da = operand_descriptor(a, A_K, BLOCK_BYTES), db = operand_descriptor(a + OPERAND_BYTES, B_K, BLOCK_BYTES);
+#pragma unroll
+                    for (int q = 0; q < BK / 16; ++q)
+                        mma_pair(d, da + (uint64_t)(q * (A_K ? 32 : 2048) >> 4), db + (uint64_t)(q * (B_K ? 32 : 2048) >> 4), INSTRUCTION,
+                                 k > x.k0 || q > 0);
+                    mma_commit_pair(empty(s));
+                }
+                if (ok) mma_commit_pair(acc_full(b));
+            }
+            if (!ok) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
+        }
+    } else {
+        const uint32_t quarter = warp & 3;                       // the 32 Tensor Memory lanes that this warp may read
+        const int32_t in_tile = (int32_t)(rank * HALF_TILE + quarter * 32 + lane);
+        uint32_t acc = 0;
+        bool ok = true;
+        for (int64_t t = pair; t < tiles; t += pairs, ++acc) {
+            const Tile x = tile_at<PRODUCT>(job, row_tiles, live, t);
+            const uint32_t b = acc & 1u;
+            ok = __all_sync(0xffffffffu, mbar_wait_ns(acc_full(b), (acc >> 1) & 1u));
+            if (!ok) break;
+            tcgen05_fence_after();
+            const uint32_t src = tmem + b * TILE + (quarter * 32u << 16);
+            const int32_t row = x.row + in_tile;                 // a live row, or for GRAD_WEIGHT an entry of the piece
+            uint32_t w[32];
+            if (PRODUCT == LOGITS_SUM) {
+                const int32_t left = min(TILE, job.V - x.col);   // columns that exist
+                const int32_t at = job.rows.token[row] - x.col;  // padded rows hold -1
+                float top = -INFINITY, sum = 0.0f, mine = 0.0f;
+                for (int32_t c = 0; c < left; c += 32) {
+                    tmem_load32(src + c, w);
+                    tmem_wait_load32(w);
+                    if (c + 32 > left) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (c + j >= left) w[j] = 0xff800000u;
+                    }
+                    float hi = __uint_as_float(w[0]);
+#pragma unroll
+                    for (int j = 1; j < 32; ++j) hi = fmaxf(hi, __uint_as_float(w[j]));
+                    const float next = fmaxf(top, hi * job.scale);
+                    float add = 0.0f, add2 = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        add += ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -next));
+                        add2 += ex2_approx(fmaf(__uint_as_float(w[j + 1]), job.scale, -next));
+                    }
+                    sum = fmaf(sum, ex2_approx(top - next), add + add2);
+                    top = next;
+                    if (at >= c && at < c + 32) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (at == c + j) mine = __uint_as_float(w[j]);
+                    }
+                }
+                if (row < live && PPOW_CHECK(x.index < job.v_tiles, 502, &header->error_flags)) {
+                    job.partial[(size_t)row * job.v_tiles + x.index] = make_float2(top, sum);
+                    if (at >= 0 && at < left) job.at_token[row] = mine;
+                }
+            } else if (PRODUCT == LOGITS_GRAD) {
+                const int32_t left = min(TILE, job.V - x.col);
+                const int32_t at = job.rows.token[row] - x.col;
+                const float mult = job.rows.mult[row], lse2 = job.rows.lse2[row];
+                uint16_t *to = job.dz + (size_t)row * job.piece + x.index * TILE;
+                for (int32_t c = 0; c < TILE; c += 32) {
+                    tmem_load32(src + c, w);
+                    tmem_wait_load32(w);
+                    float p[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) p[j] = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -lse2));
+                    if (at >= c && at < c + 32) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (at == c + j) p[j] -= 1.0f;
+                    }
+                    if (row >= live || c + 32 > left) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            if (row >= live || c + j >= left) p[j] = 0.0f;
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t o[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) o[j] = pack2<BF16>(p[16 * h + 2 * j] * mult, p[16 * h + 2 * j + 1] * mult);
+                        if (PPOW_CHECK(x.index * TILE + c + 16 * h + 16 <= job.piece, 503, &header->error_flags)) store32(to + c + 16 * h, o);
+                    }
+                }
+            } else if (PRODUCT == GRAD_HIDDEN) {
+                float *to = job.grad_rows + x.split * job.split_stride + (size_t)row * job.D + x.col;
+                const int32_t left = min(TILE, job.D - x.col);   // a multiple of 8
+                const bool none = x.k0 == x.k1;                  // more shares than steps: nothing was multiplied
+                for (int32_t c = 0; c < left; c += 32) {
+                    tmem_load32(src + c, w);
+                    tmem_wait_load32(w);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        if (c + 8 * h < left && row < live && PPOW_CHECK(x.split < job.splits, 504, &header->error_flags)) {
+                            uint32_t o[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) o[j] = none ? 0u : w[8 * h + j];
+                            if (job.add) {
+                                const float4 *old = reinterpret_cast<const float4 *>(to + c + 8 * h);
+                                const float4 p = old[0], q = old[1];
+                                const float f[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) + f[j]);
+                            }
+                            store32(to + c + 8 * h, o);
+                        }
+                    }
+                }
+            } else {
+                const int32_t left = min(TILE, job.D - x.col);
+                const float out_scale = header->out_scale;
+                uint16_t *to = job.grad_weight + (size_t)(job.v0 + row) * job.D + x.col;
+                for (int32_t c = 0; c < left; c += 32) {
+                    tmem_load32(src + c, w);
+                    tmem_wait_load32(w);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        if (c + 8 * h < left && row < job.columns && PPOW_CHECK(job.v0 + row < job.V, 505, &header->error_flags)) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                o[j] = pack2<BF16>(__uint_as_float(w[8 * h + 2 * j]) * out_scale, __uint_as_float(w[8 * h + 2 * j + 1]) * out_scale);
+                            *reinterpret_cast<uint4 *>(to + c + 8 * h) = make_uint4(o[0], o[1], o[2], o[3]);
+                        }
+                    }
+                }
+            }
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(peer_addr(acc_empty(b), 0));
+        }
+        if (!ok && lane == 0) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
+    }
+    __syncwarp();
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    if (warp == 1) {
+        tcgen05_fence_after();
+        tmem_free_pair(tmem);
+    }
+}
+
+// ---- merge: one warp per live row -------------------------------------------------------------------
+constexpr int MERGE_THREADS = 128;
+__global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows, const float2 *__restrict__ partial,
+                                                                   const float *__restrict__ at_token, int32_t v_tiles, int32_t V,
+                                                                   float scale, float *__restrict__ logp, float *__restrict__ lse)
+{
+    const int lane = threadIdx.x & 31;
+    const int32_t row = (int32_t)((blockIdx.x * (unsigned)MERGE_THREADS + threadIdx.x) >> 5);
+    if (row >= rows.header->live) return;
+    const float2 *p = partial + (size_t)row * v_tiles;
+    float top = -INFINITY;
+    for (int32_t i = lane; i < v_tiles; i += 32) top = fmaxf(top, p[i].x);
+    top = warp_max(top);
+    double sum = 0.0;
+    for (int32_t i = lane; i < v_tiles; i += 32) sum += (double)p[i].y * (double)ex2_approx(p[i].x - top);
+    sum = warp_sum_f64(sum);
+    if (lane == 0) {
+        const double lse2 = (double)top + log2(sum);
+        const int32_t r = rows.source[row], y = rows.token[row];
+        const double ln2 = 0.69314718055994530942;
+        lse[r] = (float)(lse2 * ln2);
+        logp[r] = y < V ? (float)(((double)at_token[row] * (double)scale - lse2) * ln2) : -INFINITY;
+    }
+}
+
+// ---- finish: dh of the live rows, rounded once ------------------------------------------------------
+constexpr int FINISH_THREADS = 256;
+template <bool BF16>
+__global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows rows, const float *__restrict__ parts, int32_t splits,
+                                                                     size_t split_stride, int32_t D, uint16_t *__restrict__ grad_hidden)
+{
+    const int32_t units = D / 8;
+    const int64_t all = (int64_t)rows.header->live * units;
+    for (int64_t i = (int64_t)blockIdx.x * FINISH_THREADS + threadIdx.x; i < all; i += (int64_t)gridDim.x * FINISH_THREADS) {
+        const int32_t row = (int32_t)(i / units), u = (int32_t)(i % units);
+        float f[8] = {};
+        for (int32_t s = 0; s < splits; ++s) {
+            const float4 *p = reinterpret_cast<const float4 *>(parts + s * split_stride + (size_t)row * D) + 2 * u;
+            const float4 a = __ldcs(p), b = __ldcs(p + 1);
+            f[0] += a.x, f[1] += a.y, f[2] += a.z, f[3] += a.w, f[4] += b.x, f[5] += b.y, f[6] += b.z, f[7] += b.w;
+        }
+        const float k = rows.row_scale[row];
+        reinterpret_cast<uint4 *>(grad_hidden + (size_t)rows.source[row] * D)[u] =
+            make_uint4(pack2<BF16>(f[0] * k, f[1] * k), pack2<BF16>(f[2] * k, f[3] * k), pack2<BF16>(f[4] * k, f[5] * k),
+                       pack2<BF16>(f[6] * k, f[7] * k));
+    }
+}
+
+// ---- host side --------------------------------------------------------------------------------------
+namespace {
+
+bool params_ok(const ppow_head_params *p)
+{
+    if (!p || p->T < 0 || p->T > MAX_TOKENS || p->V < 2 || p->V > MAX_VOCAB || p->D < 8 || p->D > MAX_WIDTH || p->D % 8) return false;
+    if (p->dtype != PPOW_BF16 && p->dtype != PPOW_F16) return false;
+    if (!(p->temperature > 0.0f) || !isfinite(p->temperature)) return false;
+    if (p->hidden_stride < p->D || p->weight_stride < p->D || p->weight_stride % 8) return false;
+    if (p->hidden_stride > (int64_t)1 << 40 || p->weight_stride > (int64_t)1 << 32) return false;
+    return true;
+}
+
+struct Layout {
+    size_t source, token, mult, lse2, row_scale, rows, scaled, partial, at_token, dz, grad_rows, total;
+    size_t split_stride;
+    int32_t padded, v_tiles, d_tiles, piece, splits;
+};
+
+// Shares of the inner axis for dh: tiles x shares should fill whole rounds of `74` pairs.  The count is a function of the
+// sizes alone, so that the workspace is too.
+int32_t split_count(int64_t tiles, int32_t steps)
+{
+    constexpr int64_t PAIRS = 74;
+    int32_t best = 1;
+    double best_cost = 1e30;
+    for (int32_t s = 1; s <= MAX_SPLIT && s * 8 <= steps; ++s) {
+        const double cost = (double)((tiles * s + PAIRS - 1) / PAIRS) / s * (1.0 + 0.02 * s);
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+
+Layout layout_of(const ppow_head_params *p, bool backward)
+{
+    Layout L = {};
+    size_t off = HEADER_BYTES;
+    auto take = [&](size_t bytes) {
+        const size_t o = off;
+        off = (off + bytes + 255) & ~(size_t)255;
+        return o;
+    };
+    L.padded = (p->T + TILE - 1) / TILE * TILE;
+    if (L.padded < TILE) L.padded = TILE;
+    L.v_tiles = (p->V + TILE - 1) / TILE;
+    L.d_tiles = (p->D + TILE - 1) / TILE;
+    const size_t rows = (size_t)L.padded;
+    L.source = take(rows * 4);
+    L.token = take(rows * 4);
+    L.mult = take(rows * 4);
+    L.lse2 = take(rows * 4);
+    L.row_scale = take(rows * 4);
+    L.rows = take(rows * p->D * 2);
+    if (!backward) {
+        L.partial = take(rows * L.v_tiles * sizeof(float2));
+        L.at_token = take(rows * 4);
+    } else {
+        if (p->dtype == PPOW_F16) L.scaled = take(rows * p->D * 2);
+        const size_t strip = rows * TILE * 2;                      // one column tile of dz
+        int32_t fit = (int32_t)(DZ_BYTES / strip);
+        if (fit < 1) fit = 1;
+        const int32_t pieces = (L.v_tiles + fit - 1) / fit;
+        L.piece = (L.v_tiles + pieces - 1) / pieces * TILE;        // pieces of nearly the same length
+        L.dz = take(rows * L.piece * 2);
+        L.splits = split_count((int64_t)(L.padded / TILE) * L.d_tiles, L.piece / BK);
+        L.split_stride = rows * p->D;
+        L.grad_rows = take(L.splits * L.split_stride * 4);
+    }
+    L.total = off;
+    return L;
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled()
+{
+    static EncodeTiled fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return (EncodeTiled)p;
+    }();
+    return fn;
+}
+
+// [height, width] 16-bit elements, rows `stride` elements apart; boxes of 64 x `box_rows`, what lies outside reads as 0.
+bool make_map(CUtensorMap *map, const void *base, bool bf16, int64_t width, int64_t height, int64_t stride, uint32_t box_rows)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)height}, strides[1] = {(cuuint64_t)stride * 2};
+    const cuuint32_t box[2] = {BK, box_rows}, step[2] = {1, 1};
+    return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(base), dims,
+                  strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int pair_count()
+{
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return sms / 2;
+}
+
+template <int PRODUCT, bool BF16>
+bool launch_product(const CUtensorMap &a, const CUtensorMap &b, const ProductJob &job, int64_t most_tiles, int pairs, cudaStream_t stream)
+{
+    if (cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MMA_SMEM) != cudaSuccess)
+        return false;
+    const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
+    head_product_kernel<PRODUCT, BF16><<<2 * n, MMA_THREADS, MMA_SMEM, stream>>>(a, b, job);
+    return cudaGetLastError() == cudaSuccess;
+}
+
+HeadRows rows_of(char *ws, const Layout &L)
+{
+    HeadRows r = {};
+    r.header = (HeadHeader *)ws;
+    r.source = (int32_t *)(ws + L.source);
+    r.token = (int32_t *)(ws + L.token);
+    r.mult = (float *)(ws + L.mult);
+    r.lse2 = (float *)(ws + L.lse2);
+    r.row_scale = (float *)(ws + L.row_scale);
+    r.rows = ws + L.rows;
+    r.scaled = ws + L.scaled;
+    return r;
+}
+
+template <bool BACKWARD, bool SCALED>
+bool launch_gather(const ppow_head_params *p, const Layout &L, const GatherJob &base, const HeadRows &rows, const void *hidden,
+                   cudaStream_t stream)
+{
+    GatherJob job = base;
+    job.stride = p->hidden_stride;
+    job.T = p->T;
+    job.D = p->D;
+    job.V = p->V;
+    job.inv_temperature = (float)(1.0 / (double)p->temperature);
+    job.vec = (uintptr_t)hidden % 16 == 0 && p->hidden_stride % 8 == 0;
+    job.hidden = (const uint16_t *)hidden;
+    // few rows per CTA, but at most about a thousand CTAs: each of them looks at all tokens
+    job.rows_per_cta = (L.padded + GATHER_CTAS - 1) / GATHER_CTAS;
+    if (job.rows_per_cta < 8) job.rows_per_cta = 8;
+    const unsigned grid = (unsigned)((L.padded + job.rows_per_cta - 1) / job.rows_per_cta);
+    head_gather_kernel<BACKWARD, SCALED><<<grid, GATHER_THREADS, 0, stream>>>(job, rows);
+    return cudaGetLastError() == cudaSuccess;
+}
+
+template <bool BF16>
+ppow_status forward(const ppow_head_params *p, const void *hidden, const void *weight, const int32_t *tokens, float *logp, float *lse,
+                    char *ws, cudaStream_t stream)
+{
+    const Layout L = layout_of(p, false);
+    const HeadRows rows = rows_of(ws, L);
+    CUtensorMap map_rows, map_weight;
+    if (!make_map(&map_rows, rows.rows, BF16, p->D, L.padded, p->D, HALF_TILE) ||
+        !make_map(&map_weight, weight, BF16, p->D, p->V, p->weight_stride, HALF_TILE))
+        return PPOW_ERR_CUDA;
+    const int pairs = pair_count();
+    if (pairs < 1) return PPOW_ERR_CUDA;
+    GatherJob g = {};
+    g.tokens = tokens;
+    g.logp_out = logp;
+    g.lse_out = lse;
+    if (!launch_gather<false, false>(p, L, g, rows, hidden, stream)) return PPOW_ERR_CUDA;
+    ProductJob job = {};
+    job.rows = rows;
+    job.scale = (float)(1.4426950408889634074 / (double)p->temperature);
+    job.D = p->D;
+    job.V = job.columns = p->V;
+    job.v_tiles = L.v_tiles;
+    job.d_tiles = L.d_tiles;
+    job.partial = (float2 *)(ws + L.partial);
+    job.at_token = (float *)(ws + L.at_token);
+    const int64_t tiles = (int64_t)(L.padded / TILE) * L.v_tiles;
+    if (!launch_product<LOGITS_SUM, BF16>(map_rows, map_weight, job, tiles, pairs, stream)) return PPOW_ERR_CUDA;
+    head_merge_kernel<<<(unsigned)((p->T * 32ll + MERGE_THREADS - 1) / MERGE_THREADS), MERGE_THREADS, 0, stream>>>(
+        rows, job.partial, job.at_token, L.v_tiles, p->V, job.scale, logp, lse);
+    return cudaGetLastError() == cudaSuccess ? PPOW_OK : PPOW_ERR_CUDA;
+}
+
+template <bool BF16>
+ppow_status backward(const ppow_head_params *p, const void *hidden, const void *weight, const int32_t *tokens, const float *lse,
+                     const float *grad_logp, void *grad_hidden, void *grad_weight, char *ws, cudaStream_t stream)
+{
+    const Layout L = layout_of(p, true);
+    const HeadRows rows = rows_of(ws, L);
+    uint16_t *dz = (uint16_t *)(ws + L.dz);
+    CUtensorMap map_rows, map_rows_t, map_weight, map_weight_t, map_dz, map_dz_t;
+    if (!make_map(&map_rows, rows.rows, BF16, p->D, L.padded, p->D, HALF_TILE) ||
+        !make_map(&map_rows_t, BF16 ? rows.rows : rows.scaled, BF16, p->D, L.padded, p->D, BK) ||
+        !make_map(&map_weight, weight, BF16, p->D, p->V, p->weight_stride, HALF_TILE) ||
+        !make_map(&map_weight_t, weight, BF16, p->D, p->V, p->weight_stride, BK) ||
+        !make_map(&map_dz, dz, BF16, L.piece, L.padded, L.piece, HALF_TILE) || !make_map(&map_dz_t, dz, BF16, L.piece, L.padded, L.piece, BK))
+        return PPOW_ERR_CUDA;
+    const int pairs = pair_count();
+    if (pairs < 1) return PPOW_ERR_CUDA;
+    GatherJob g = {};
+    g.tokens = tokens;
+    g.lse = lse;
+    g.grad = grad_logp;
+    g.grad_hidden = (uint16_t *)grad_hidden;
+    if (!launch_gather<true, !BF16>(p, L, g, rows, hidden, stream)) return PPOW_ERR_CUDA;
+    ProductJob job = {};
+    job.rows = rows;
+    job.scale = (float)(1.4426950408889634074 / (double)p->temperature);
+    job.D = p->D;
+    job.V = p->V;
+    job.d_tiles = L.d_tiles;
+    job.splits = L.splits;
+    job.piece = L.piece;
+    job.dz = dz;
+    job.grad_rows = (float *)(ws + L.grad_rows);
+    job.split_stride = L.split_stride;
+    job.grad_weight = (uint16_t *)grad_weight;
+    const int64_t row_tiles = L.padded / TILE;
+    for (int64_t v0 = 0; v0 < p->V; v0 += L.piece) {
+        job.v0 = (int32_t)v0;
+        job.columns = (int32_t)(p->V - v0 < L.piece ? p->V - v0 : L.piece);
+        job.v_tiles = (job.columns + TILE - 1) / TILE;
+        job.add = v0 > 0;
+        if (!launch_product<LOGITS_GRAD, BF16>(map_rows, map_weight, job, row_tiles * job.v_tiles, pairs, stream)) return PPOW_ERR_CUDA;
+        if (grad_hidden &&
+            !launch_product<GRAD_HIDDEN, BF16>(map_dz, map_weight_t, job, row_tiles * L.d_tiles * L.splits, pairs, stream))
+            return PPOW_ERR_CUDA;
+        if (grad_weight &&
+            !launch_product<GRAD_WEIGHT, BF16>(map_dz_t, map_rows_t, job, (int64_t)job.v_tiles * L.d_tiles, pairs, stream))
+            return PPOW_ERR_CUDA;
+    }
+    if (grad_hidden) {
+        const int64_t blocks = ((int64_t)p->T * (p->D / 8) + FINISH_THREADS - 1) / FINISH_THREADS;
+        head_finish_kernel<BF16><<<(unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), FINISH_THREADS, 0, stream>>>(
+            rows, job.grad_rows, L.splits, L.split_stride, p->D, (uint16_t *)grad_hidden);
+        if (cudaGetLastError() != cudaSuccess) return PPOW_ERR_CUDA;
+    }
+    return PPOW_OK;
+}
+
+}  // namespace
+}  // namespace ppow
+
+#ifdef PPOW_CHECKED
+namespace ppow { int read_check_counters_head(unsigned int *f, unsigned int *s) { return read_check_counters(f, s); } }
+#endif
+
+using namespace ppow;
+
+extern "C" size_t ppow_head_workspace_bytes(const ppow_head_params *params, int backward)
+{
+    return params_ok(params) ? layout_of(params, backward != 0).total : 0;
+}
+
+extern "C" ppow_status ppow_head_logprob(const ppow_head_params *params, const void *hidden, const void *weight, const int32_t *tokens,
+                                         float *logp, float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    if (!params_ok(params)) return PPOW_ERR_INVALID_ARG;
+    if (params->T == 0) return PPOW_OK;
+    if (!hidden || !weight || !tokens || !logp || !lse) return PPOW_ERR_INVALID_ARG;
+    if ((uintptr_t)hidden % 2 || (uintptr_t)weight % 16 || (uintptr_t)tokens % 4 || (uintptr_t)logp % 4 || (uintptr_t)lse % 4)
+        return PPOW_ERR_INVALID_ARG;
+    if (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < layout_of(params, false).total) return PPOW_ERR_WORKSPACE;
+    return params->dtype == PPOW_BF16
+               ? forward<true>(params, hidden, weight, tokens, logp, lse, (char *)workspace, (cudaStream_t)cuda_stream)
+               : forward<false>(params, hidden, weight, tokens, logp, lse, (char *)workspace, (cudaStream_t)cuda_stream);
+}
+
+extern "C" ppow_status ppow_head_logprob_backward(const ppow_head_params *params, const void *hidden, const void *weight,
+                                                  const int32_t *tokens, const float *lse, const float *grad_logp, void *grad_hidden,
+                                                  void *grad_weight, void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    if (!params_ok(params)) return PPOW_ERR_INVALID_ARG;
+    if ((!grad_hidden && !grad_weight) || (uintptr_t)grad_hidden % 16 || (uintptr_t)grad_weight % 16) return PPOW_ERR_INVALID_ARG;
+    if (params->T == 0) {
+        if (grad_weight && cudaMemsetAsync(grad_weight, 0, (size_t)params->V * params->D * 2, (cudaStream_t)cuda_stream) != cudaSuccess)
+            return PPOW_ERR_CUDA;
+        return PPOW_OK;
+    }
+    if (!hidden || !weight || !tokens || !lse || !grad_logp) return PPOW_ERR_INVALID_ARG;
+    if ((uintptr_t)hidden % 2 || (uintptr_t)weight % 16 || (uintptr_t)tokens % 4 || (uintptr_t)lse % 4 || (uintptr_t)grad_logp % 4)
+        return PPOW_ERR_INVALID_ARG;
+    if (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < layout_of(params, true).total) return PPOW_ERR_WORKSPACE;
+    return params->dtype == PPOW_BF16 ? backward<true>(params, hidden, weight, tokens, lse, grad_logp, grad_hidden, grad_weight,
+                                                       (char *)workspace, (cudaStream_t)cuda_stream)
+                                      : backward<false>(params, hidden, weight, tokens, lse, grad_logp, grad_hidden, grad_weight,
+                                                        (char *)workspace, (cudaStream_t)cuda_stream);
+}

@@ -201,6 +201,7 @@ extern "C" ppow_status ppow_select_windows(const float *score, int32_t N, int32_
 namespace ppow {
 int read_check_counters_score(unsigned int *f, unsigned int *s);
 int read_check_counters_train(unsigned int *f, unsigned int *s);
+int read_check_counters_head(unsigned int *f, unsigned int *s);
 }
 #endif
 
@@ -210,7 +211,8 @@ extern "C" ppow_status ppow_checked_failures(uint32_t *failures_host, uint32_t *
 #ifdef PPOW_CHECKED
     unsigned int f = 0, s = 0;
     if (cudaDeviceSynchronize() != cudaSuccess) return PPOW_ERR_CUDA;
-    if (read_check_counters(&f, &s) || read_check_counters_score(&f, &s) || read_check_counters_train(&f, &s))
+    if (read_check_counters(&f, &s) || read_check_counters_score(&f, &s) || read_check_counters_train(&f, &s) ||
+        read_check_counters_head(&f, &s))
         return PPOW_ERR_CUDA;
     *failures_host = f;
     if (first_site_host) *first_site_host = s;
