@@ -312,6 +312,66 @@ ppow_status ppow_head_logprob_backward(const ppow_head_params *params, const voi
                                        void *grad_hidden, void *grad_weight,
                                        void *workspace, size_t workspace_bytes, void *cuda_stream);
 
+/*
+ * Layer normalisation of the drafter's hidden states in front of its head, and its gradient:
+ *     y = (x - mean) * rstd * weight + bias         rstd = 1 / sqrt(var + eps), var the population variance of the row
+ * and 8-bit checkpoints of activations, so that what the backward pass needs of the forward pass takes half the memory.
+ * Statistics and sums are float32; sums over rows are added up in a fixed order.
+ */
+typedef struct {
+    int32_t R;              /* rows, 0 .. 2^28 */
+    int32_t D;              /* width, >= 1; more than 16384 is PPOW_ERR_UNSUPPORTED */
+    int32_t dtype;          /* ppow_dtype of x, y and their gradients */
+    int32_t param_dtype;    /* ppow_dtype of weight, bias and their gradients: PPOW_F32 or the same as dtype */
+    float eps;              /* >= 0 */
+} ppow_norm_params;
+
+/*
+ * 8-bit form of an activation [R, D]: each block of 128 values along a row (the last one may be shorter) shares a factor
+ * 2^e, e the smallest integer >= -126 with max|x| <= 448 * 2^e over the block's finite values (-126 if all are 0), and a
+ * value is x / 2^e rounded to nearest even in e4m3 (1 sign, 4 exponent, 3 mantissa bits; no infinity).  A value that is
+ * not finite becomes NaN.
+ *   packed   device, [R, D] bytes, contiguous: the e4m3 codes
+ *   scale    device, [R, ceil(D / 128)] bytes, contiguous: e + 127
+ * Restored values are code * 2^e, rounded once to the storage type (exact in float32 and, but for subnormals, in bfloat16).
+ */
+
+/*
+ *   x            device, [R, D] of params->dtype, rows x_stride elements apart (>= D), aligned to its element size
+ *   weight       device, [D] of params->param_dtype         bias   the same, or NULL for none
+ *   y            device, [R, D], contiguous                 mean, rstd   device, [R] float32
+ *   packed, scale   the 8-bit form of x, written in the same pass; both or neither may be NULL
+ * Full speed needs rows of whole 16-byte units at 16-byte aligned addresses.  y must not overlap x.  No workspace.
+ */
+ppow_status ppow_layer_norm(const ppow_norm_params *params, const void *x, int64_t x_stride,
+                            const void *weight, const void *bias, void *y, float *mean, float *rstd,
+                            uint8_t *packed, uint8_t *scale, void *cuda_stream);
+
+/* Bytes of device scratch of the gradient (0 on parameters it refuses). */
+size_t ppow_layer_norm_workspace_bytes(const ppow_norm_params *params);
+
+/*
+ * Gradient, with a = grad_y * weight and xh = (x - mean) * rstd:
+ *     grad_x = rstd * (a - mean(a) - xh * mean(a * xh))    grad_weight = sum_rows grad_y * xh    grad_bias = sum_rows grad_y
+ *   grad_y          device, [R, D] of params->dtype, rows grad_y_stride elements apart
+ *   x, x_stride     the forward pass's input, or NULL: then packed and scale hold its 8-bit form (exactly one of the two)
+ *   mean, rstd      device, [R] float32, as written by ppow_layer_norm
+ *   grad_x          device, [R, D], contiguous
+ *   grad_weight, grad_bias   device, [D] of params->param_dtype; either may be NULL.  R == 0 sets them to 0.
+ *   workspace       device, >= ppow_layer_norm_workspace_bytes(params), 256-byte aligned
+ */
+ppow_status ppow_layer_norm_backward(const ppow_norm_params *params, const void *grad_y, int64_t grad_y_stride,
+                                     const void *x, int64_t x_stride, const uint8_t *packed, const uint8_t *scale,
+                                     const void *weight, const float *mean, const float *rstd,
+                                     void *grad_x, void *grad_weight, void *grad_bias,
+                                     void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* The 8-bit form of any activation x [R, D], rows x_stride elements apart, and back.  1 <= D <= 2^20.  No workspace. */
+ppow_status ppow_pack_activation(const void *x, int64_t x_stride, int32_t R, int32_t D, int32_t dtype,
+                                 uint8_t *packed, uint8_t *scale, void *cuda_stream);
+ppow_status ppow_unpack_activation(const uint8_t *packed, const uint8_t *scale, int32_t R, int32_t D, int32_t dtype,
+                                   void *x, void *cuda_stream);
+
 /* Copies the error word that the last ppow_score_windows call on `workspace` left behind into
  * *flags_host (PPOW_FLAG_* bits) and synchronises `cuda_stream` to do so.  Returns
  * PPOW_ERR_DEVICE_TIMEOUT if that bit is set, PPOW_ERR_CUDA on a CUDA failure, else PPOW_OK. */

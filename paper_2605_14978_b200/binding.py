@@ -34,6 +34,8 @@ EXPORTS = ("ppow_score_workspace_bytes", "ppow_score_windows", "ppow_score_windo
            "ppow_group_advantage", "ppow_sequence_windows", "ppow_sequence_windows_mixed", "ppow_expected_acceptance",
            "ppow_reference_logprob", "ppow_selftest_wait_timeout", "ppow_stream_read_probe", "ppow_score_kernel_launches",
            "ppow_head_workspace_bytes", "ppow_head_logprob", "ppow_head_logprob_backward",
+           "ppow_layer_norm", "ppow_layer_norm_workspace_bytes", "ppow_layer_norm_backward", "ppow_pack_activation",
+           "ppow_unpack_activation",
            "ppow_checked_failures", "ppow_timeline_read", "ppow_status_string", "ppow_version")
 
 POSITION_OUTPUTS = {"accept_flag": torch.uint8, "kl": torch.float32, "conf": torch.float32, "crit": torch.float32,
@@ -65,6 +67,11 @@ class ppow_outputs(ctypes.Structure):
 class ppow_head_params(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("V", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("hidden_stride", ctypes.c_int64), ("weight_stride", ctypes.c_int64), ("temperature", ctypes.c_float)]
+
+
+class ppow_norm_params(ctypes.Structure):
+    _fields_ = [("R", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
 
 
 class PpowError(RuntimeError):
@@ -133,6 +140,18 @@ def load_library():
     lib.ppow_head_logprob.argtypes = [ctypes.POINTER(ppow_head_params), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ppow_head_logprob_backward.restype = ctypes.c_int
     lib.ppow_head_logprob_backward.argtypes = [ctypes.POINTER(ppow_head_params), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.ppow_layer_norm.restype = ctypes.c_int
+    i64 = ctypes.c_int64
+    lib.ppow_layer_norm.argtypes = [ctypes.POINTER(ppow_norm_params), vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.ppow_layer_norm_workspace_bytes.restype = sz
+    lib.ppow_layer_norm_workspace_bytes.argtypes = [ctypes.POINTER(ppow_norm_params)]
+    lib.ppow_layer_norm_backward.restype = ctypes.c_int
+    lib.ppow_layer_norm_backward.argtypes = [ctypes.POINTER(ppow_norm_params), vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp,
+                                             vp, sz, vp]
+    lib.ppow_pack_activation.restype = ctypes.c_int
+    lib.ppow_pack_activation.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp]
+    lib.ppow_unpack_activation.restype = ctypes.c_int
+    lib.ppow_unpack_activation.argtypes = [vp, vp, i32, i32, i32, vp, vp]
     lib.ppow_checked_failures.restype = ctypes.c_int
     lib.ppow_checked_failures.argtypes = [ctypes.POINTER(ctypes.c_uint32), ctypes.POINTER(ctypes.c_uint32)]
     lib.ppow_timeline_read.restype = ctypes.c_int
@@ -536,6 +555,85 @@ def ppow_head_logprob_backward(params: ppow_head_params, hidden, weight, tokens,
         raise PpowError(st, "ppow_head_logprob_backward")
 
 
+CHECKPOINT_DTYPE = torch.float8_e4m3fn   # codes; scales are uint8, exponent + 127
+CHECKPOINT_BLOCK = 128                  # values along a row that share a scale
+
+
+def make_norm_params(R, D, dtype, param_dtype, eps=1e-5) -> ppow_norm_params:
+    return ppow_norm_params(int(R), int(D), DTYPE_CODES[dtype], DTYPE_CODES[param_dtype], float(eps))
+
+
+def _check_packed(packed, scale, R, D):
+    _check_shape(packed, (R, D), "packed")
+    _check_shape(scale, (R, -(-D // CHECKPOINT_BLOCK)), "scale")
+    return _dev_ptr(packed, CHECKPOINT_DTYPE, "packed"), _dev_ptr(scale, torch.uint8, "scale")
+
+
+def ppow_layer_norm(params: ppow_norm_params, x, weight, bias, y, mean, rstd, packed=None, scale=None, stream=None) -> None:
+    """Enqueue the forward pass on ``x`` [R, D]; with ``packed`` and ``scale`` it also writes the 8-bit form of ``x``."""
+    R, D, dt, pt = params.R, params.D, LOGIT_DTYPES[params.dtype], LOGIT_DTYPES[params.param_dtype]
+    for name, t, shape in (("x", x, (R, D)), ("weight", weight, (D,)), ("bias", bias, (D,)), ("y", y, (R, D)), ("mean", mean, (R,)),
+                           ("rstd", rstd, (R,))):
+        _check_shape(t, shape, name)
+    _check_device(x.device, weight=weight, bias=bias, y=y, mean=mean, rstd=rstd, packed=packed, scale=scale)
+    xp, xs = _rows_ptr(x, dt, "x")
+    st = load_library().ppow_layer_norm(
+        ctypes.byref(params), xp, xs, _dev_ptr(weight, pt, "weight"), _dev_ptr(bias, pt, "bias"), _dev_ptr(y, dt, "y"),
+        _dev_ptr(mean, torch.float32, "mean"), _dev_ptr(rstd, torch.float32, "rstd"), *_check_packed(packed, scale, R, D),
+        _stream_ptr(stream))
+    if st != PPOW_OK:
+        raise PpowError(st, "ppow_layer_norm")
+
+
+def ppow_layer_norm_workspace_bytes(params: ppow_norm_params) -> int:
+    return int(load_library().ppow_layer_norm_workspace_bytes(ctypes.byref(params)))
+
+
+def ppow_layer_norm_backward(params: ppow_norm_params, grad_y, x, packed, scale, weight, mean, rstd, grad_x, grad_weight, grad_bias,
+                             workspace, stream=None) -> None:
+    """Enqueue the gradient; the forward pass's input is either ``x`` or, where that is None, ``packed`` and ``scale``."""
+    R, D, dt, pt = params.R, params.D, LOGIT_DTYPES[params.dtype], LOGIT_DTYPES[params.param_dtype]
+    for name, t, shape in (("grad_y", grad_y, (R, D)), ("x", x, (R, D)), ("weight", weight, (D,)), ("mean", mean, (R,)), ("rstd", rstd, (R,)),
+                           ("grad_x", grad_x, (R, D)), ("grad_weight", grad_weight, (D,)), ("grad_bias", grad_bias, (D,))):
+        _check_shape(t, shape, name)
+    _check_device(grad_y.device, x=x, packed=packed, scale=scale, weight=weight, mean=mean, rstd=rstd, grad_x=grad_x,
+                  grad_weight=grad_weight, grad_bias=grad_bias, workspace=workspace)
+    gp, gs = _rows_ptr(grad_y, dt, "grad_y")
+    xp, xs = (None, D) if x is None else _rows_ptr(x, dt, "x")
+    st = load_library().ppow_layer_norm_backward(
+        ctypes.byref(params), gp, gs, xp, xs, *_check_packed(packed, scale, R, D), _dev_ptr(weight, pt, "weight"),
+        _dev_ptr(mean, torch.float32, "mean"), _dev_ptr(rstd, torch.float32, "rstd"), _dev_ptr(grad_x, dt, "grad_x"),
+        _dev_ptr(grad_weight, pt, "grad_weight"), _dev_ptr(grad_bias, pt, "grad_bias"), _dev_ptr(workspace, torch.uint8, "workspace"),
+        workspace.numel(), _stream_ptr(stream))
+    if st != PPOW_OK:
+        raise PpowError(st, "ppow_layer_norm_backward")
+
+
+def ppow_pack_activation(x, packed, scale, stream=None) -> None:
+    """Enqueue the 8-bit form of ``x`` [R, D]: codes into ``packed`` [R, D], exponents into ``scale`` [R, ceil(D/128)]."""
+    if x.dtype not in DTYPE_CODES:
+        raise ValueError("x must be float32, bfloat16 or float16, got %s" % x.dtype)
+    xp, xs = _rows_ptr(x, x.dtype, "x")
+    R, D = x.shape
+    _check_device(x.device, packed=packed, scale=scale)
+    st = load_library().ppow_pack_activation(xp, xs, R, D, DTYPE_CODES[x.dtype], *_check_packed(packed, scale, R, D), _stream_ptr(stream))
+    if st != PPOW_OK:
+        raise PpowError(st, "ppow_pack_activation")
+
+
+def ppow_unpack_activation(packed, scale, x, stream=None) -> None:
+    """Enqueue the way back: values of the 8-bit form into ``x`` [R, D], rounded to its type."""
+    if x.dtype not in DTYPE_CODES:
+        raise ValueError("x must be float32, bfloat16 or float16, got %s" % x.dtype)
+    R, D = packed.shape
+    _check_shape(x, (R, D), "x")
+    _check_device(packed.device, scale=scale, x=x)
+    st = load_library().ppow_unpack_activation(*_check_packed(packed, scale, R, D), R, D, DTYPE_CODES[x.dtype], _dev_ptr(x, x.dtype, "x"),
+                                               _stream_ptr(stream))
+    if st != PPOW_OK:
+        raise PpowError(st, "ppow_unpack_activation")
+
+
 def _host_ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
     if t is None:
         return None
@@ -628,3 +726,57 @@ def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature
         ws = alloc_workspace(ppow_head_workspace_bytes(params, True), dev)
         ppow_head_logprob_backward(params, hidden, weight, tokens, lse, grad_logp, gh, gw, ws, stream)
     return gh, gw
+
+
+def layer_norm(x, weight, bias=None, *, eps=1e-5, checkpoint=False, stream=None) -> dict:
+    """Allocate outputs and run ppow_layer_norm on ``x`` [R, D]; returns y, mean, rstd and, with ``checkpoint``, the 8-bit form of
+    ``x`` as packed and scale."""
+    R, D = x.shape
+    params = make_norm_params(R, D, x.dtype, weight.dtype, eps)
+    dev = x.device
+    with _on(dev, stream):
+        out = {"y": torch.empty((R, D), dtype=x.dtype, device=dev), "mean": torch.empty((R,), dtype=torch.float32, device=dev),
+               "rstd": torch.empty((R,), dtype=torch.float32, device=dev)}
+        if checkpoint:
+            out.update(_alloc_packed(R, D, dev))
+        ppow_layer_norm(params, x, weight, bias, out["y"], out["mean"], out["rstd"], out.get("packed"), out.get("scale"), stream)
+    return out
+
+
+def layer_norm_backward(grad_y, x, weight, mean, rstd, *, want_bias=True, stream=None):
+    """Allocate gradients and workspace, run ppow_layer_norm_backward; returns (grad_x, grad_weight, grad_bias or None).
+    ``x`` is the forward pass's input or the pair (packed, scale) that the forward pass left."""
+    R, D = grad_y.shape
+    params = make_norm_params(R, D, grad_y.dtype, weight.dtype)
+    dev = grad_y.device
+    x, packed, scale = (None, *x) if isinstance(x, (tuple, list)) else (x, None, None)
+    with _on(dev, stream):
+        gx = torch.empty((R, D), dtype=grad_y.dtype, device=dev)
+        gw = torch.empty((D,), dtype=weight.dtype, device=dev)
+        gb = torch.empty((D,), dtype=weight.dtype, device=dev) if want_bias else None
+        ws = alloc_workspace(ppow_layer_norm_workspace_bytes(params), dev)
+        ppow_layer_norm_backward(params, grad_y, x, packed, scale, weight, mean, rstd, gx, gw, gb, ws, stream)
+    return gx, gw, gb
+
+
+def _alloc_packed(R: int, D: int, dev) -> dict:
+    return {"packed": torch.empty((R, D), dtype=CHECKPOINT_DTYPE, device=dev),
+            "scale": torch.empty((R, -(-D // CHECKPOINT_BLOCK)), dtype=torch.uint8, device=dev)}
+
+
+def pack_activation(x, stream=None):
+    """Allocate and run ppow_pack_activation; returns (packed, scale)."""
+    dev = x.device
+    with _on(dev, stream):
+        out = _alloc_packed(x.shape[0], x.shape[1], dev)
+        ppow_pack_activation(x, out["packed"], out["scale"], stream)
+    return out["packed"], out["scale"]
+
+
+def unpack_activation(packed, scale, dtype=torch.bfloat16, stream=None):
+    """Allocate and run ppow_unpack_activation; returns the restored activation in ``dtype``."""
+    dev = packed.device
+    with _on(dev, stream):
+        x = torch.empty(tuple(packed.shape), dtype=dtype, device=dev)
+        ppow_unpack_activation(packed, scale, x, stream)
+    return x

@@ -40,4 +40,4 @@ static inline int read_check_counters(unsigned int *failures, unsigned int *firs
 #endif
 
 // Check sites (reported by ppow_checked_failures): 1xx row reduction, 2xx window scan, 3xx selection, 4xx training side,
-// 5xx head log-probability.
+// 5xx head log-probability, 6xx layer norm and checkpoints.
