@@ -6,7 +6,6 @@ PyTorch is used for device memory and streams only.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -468,91 +467,117 @@ def ppow_reference_logprob(params: ppow_params, ref_target_logits, valid_len, ro
         raise PpowError(st, "ppow_reference_logprob")
 
 
-def _rows_ptr(t: torch.Tensor, dtype, name):
-    """Pointer and row stride (elements) of a 2-D tensor whose rows are contiguous."""
-    if not t.is_cuda:
+# The calls below take a few microseconds on the device for one window of tokens, so their checks are one chain of cheap
+# comparisons per tensor, and pointers go to the library as plain integers.
+
+
+def _index_of(t: torch.Tensor, name) -> int:
+    """Index of the CUDA device that holds ``t``."""
+    i = t.get_device()
+    if i < 0:
         raise ValueError("%s must live on a CUDA device (no CPU path exists)" % name)
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError("%s must be 2-D with contiguous rows" % name)
-    if t.dtype != dtype:
-        raise ValueError("%s must have dtype %s, got %s" % (name, dtype, t.dtype))
-    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return i
 
 
-def _check_shape(t: Optional[torch.Tensor], shape, name):
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+def _arg(t: Optional[torch.Tensor], dtype, shape, dev: int, name):
+    """Address of a contiguous tensor of this type and shape on device ``dev`` (None for None)."""
+    if t is None:
+        return None
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        if not t.is_cuda:
+            raise ValueError("%s must live on a CUDA device (no CPU path exists)" % name)
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d, got %s, %s, strides %s on %s" % (
+            name, dtype, tuple(shape), dev, t.dtype, tuple(t.shape), t.stride(), t.device))
+    return t.data_ptr()
 
 
-def _check_device(dev, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != dev:
-            raise ValueError("%s must live on %s, got %s" % (name, dev, t.device))
+def _rows_arg(t: torch.Tensor, dtype, shape, dev: int, name):
+    """Address and row stride (elements) of a 2-D tensor whose rows are contiguous."""
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape or (shape[1] > 1 and t.stride(1) != 1):
+        if not t.is_cuda:
+            raise ValueError("%s must live on a CUDA device (no CPU path exists)" % name)
+        raise ValueError("%s must be a %s tensor of shape %s with contiguous rows on cuda:%d, got %s, %s, strides %s on %s" % (
+            name, dtype, tuple(shape), dev, t.dtype, tuple(t.shape), t.stride(), t.device))
+    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1])
 
 
-@contextlib.contextmanager
-def _on(dev, stream):
-    """Current device ``dev`` and, if given, current stream ``stream``: what is allocated inside belongs to that stream,
-    so that the allocator hands it on only behind the work enqueued there."""
-    with torch.cuda.device(dev):
-        if stream is None:
-            yield
-        else:
-            with torch.cuda.stream(stream):
-                yield
+def _workspace_arg(t: torch.Tensor, dev: int):
+    if t.dim() != 1:
+        raise ValueError("workspace must be one-dimensional")
+    return _arg(t, torch.uint8, t.shape, dev, "workspace"), t.shape[0]
+
+
+def _raw_stream(stream, dev: int) -> int:
+    """cudaStream_t of ``stream``, or of the stream that is current on device ``dev``."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError("stream must belong to cuda:%d" % dev)
+    return stream.cuda_stream
+
+
+def _call(fn, where, dev: int, *args) -> None:
+    """Calls the library with device ``dev`` current."""
+    if torch.cuda.current_device() == dev:
+        st = fn(*args)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args)
+    if st != PPOW_OK:
+        raise PpowError(st, where)
+
+
+class _On:
+    """Current stream ``stream`` if one is given: what is allocated inside belongs to it, so that the allocator hands it on
+    only behind the work enqueued there."""
+
+    def __init__(self, stream):
+        self.inner = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.inner is not None:
+            self.inner.__enter__()
+
+    def __exit__(self, *exc):
+        if self.inner is not None:
+            self.inner.__exit__(*exc)
 
 
 def make_head_params(hidden, weight, temperature=1.0) -> ppow_head_params:
     """Sizes, type and row strides of a head call, from its tensors ``hidden`` [T, D] and ``weight`` [V, D]."""
     if hidden.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError("hidden must be bfloat16 or float16, got %s" % hidden.dtype)
-    _, hs = _rows_ptr(hidden, hidden.dtype, "hidden")
-    _, ws = _rows_ptr(weight, hidden.dtype, "weight")
-    _check_shape(weight, (weight.shape[0], hidden.shape[1]), "weight")
-    return ppow_head_params(int(hidden.shape[0]), int(weight.shape[0]), int(hidden.shape[1]), DTYPE_CODES[hidden.dtype], int(hs),
-                            int(ws), float(temperature))
+    if hidden.dim() != 2 or weight.dim() != 2:
+        raise ValueError("hidden and weight must be 2-D")
+    (T, D), V = hidden.shape, weight.shape[0]
+    return ppow_head_params(T, V, D, DTYPE_CODES[hidden.dtype], hidden.stride(0) if T > 1 else D, weight.stride(0) if V > 1 else D,
+                            float(temperature))
 
 
 def ppow_head_workspace_bytes(params: ppow_head_params, backward: bool) -> int:
-    return int(load_library().ppow_head_workspace_bytes(ctypes.byref(params), 1 if backward else 0))
-
-
-def _check_head(params, hidden, weight, **per_token):
-    _check_shape(hidden, (params.T, params.D), "hidden")
-    _check_shape(weight, (params.V, params.D), "weight")
-    for name, t in per_token.items():
-        _check_shape(t, (params.T,), name)
-    _check_device(hidden.device, weight=weight, **per_token)
+    return load_library().ppow_head_workspace_bytes(ctypes.byref(params), 1 if backward else 0)
 
 
 def ppow_head_logprob(params: ppow_head_params, hidden, weight, tokens, logp, lse, workspace, stream=None) -> None:
     """Enqueue log-probabilities of ``tokens`` [T] from ``hidden`` [T, D] and ``weight`` [V, D] into ``logp`` and ``lse``."""
-    dt = LOGIT_DTYPES[params.dtype]
-    _check_head(params, hidden, weight, tokens=tokens, logp=logp, lse=lse)
-    st = load_library().ppow_head_logprob(
-        ctypes.byref(params), _rows_ptr(hidden, dt, "hidden")[0], _rows_ptr(weight, dt, "weight")[0],
-        _dev_ptr(tokens, torch.int32, "tokens"), _dev_ptr(logp, torch.float32, "logp"), _dev_ptr(lse, torch.float32, "lse"),
-        _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream_ptr(stream))
-    if st != PPOW_OK:
-        raise PpowError(st, "ppow_head_logprob")
+    T, V, D, dt, dev = params.T, params.V, params.D, LOGIT_DTYPES[params.dtype], _index_of(hidden, "hidden")
+    h, params.hidden_stride = _rows_arg(hidden, dt, (T, D), dev, "hidden")
+    w, params.weight_stride = _rows_arg(weight, dt, (V, D), dev, "weight")
+    _call(load_library().ppow_head_logprob, "ppow_head_logprob", dev, ctypes.byref(params), h, w,
+          _arg(tokens, torch.int32, (T,), dev, "tokens"), _arg(logp, torch.float32, (T,), dev, "logp"),
+          _arg(lse, torch.float32, (T,), dev, "lse"), *_workspace_arg(workspace, dev), _raw_stream(stream, dev))
 
 
 def ppow_head_logprob_backward(params: ppow_head_params, hidden, weight, tokens, lse, grad_logp, grad_hidden, grad_weight, workspace,
                                stream=None) -> None:
     """Enqueue the gradient of sum(grad_logp * logp); ``grad_hidden`` or ``grad_weight`` may be None."""
-    dt = LOGIT_DTYPES[params.dtype]
-    _check_head(params, hidden, weight, tokens=tokens, lse=lse, grad_logp=grad_logp)
-    _check_shape(grad_hidden, (params.T, params.D), "grad_hidden")
-    _check_shape(grad_weight, (params.V, params.D), "grad_weight")
-    _check_device(hidden.device, grad_hidden=grad_hidden, grad_weight=grad_weight, workspace=workspace)
-    st = load_library().ppow_head_logprob_backward(
-        ctypes.byref(params), _rows_ptr(hidden, dt, "hidden")[0], _rows_ptr(weight, dt, "weight")[0],
-        _dev_ptr(tokens, torch.int32, "tokens"), _dev_ptr(lse, torch.float32, "lse"),
-        _dev_ptr(grad_logp, torch.float32, "grad_logp"), _dev_ptr(grad_hidden, dt, "grad_hidden"),
-        _dev_ptr(grad_weight, dt, "grad_weight"), _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
-        _stream_ptr(stream))
-    if st != PPOW_OK:
-        raise PpowError(st, "ppow_head_logprob_backward")
+    T, V, D, dt, dev = params.T, params.V, params.D, LOGIT_DTYPES[params.dtype], _index_of(hidden, "hidden")
+    h, params.hidden_stride = _rows_arg(hidden, dt, (T, D), dev, "hidden")
+    w, params.weight_stride = _rows_arg(weight, dt, (V, D), dev, "weight")
+    _call(load_library().ppow_head_logprob_backward, "ppow_head_logprob_backward", dev, ctypes.byref(params), h, w,
+          _arg(tokens, torch.int32, (T,), dev, "tokens"), _arg(lse, torch.float32, (T,), dev, "lse"),
+          _arg(grad_logp, torch.float32, (T,), dev, "grad_logp"), _arg(grad_hidden, dt, (T, D), dev, "grad_hidden"),
+          _arg(grad_weight, dt, (V, D), dev, "grad_weight"), *_workspace_arg(workspace, dev), _raw_stream(stream, dev))
 
 
 CHECKPOINT_DTYPE = torch.float8_e4m3fn   # codes; scales are uint8, exponent + 127
@@ -560,78 +585,64 @@ CHECKPOINT_BLOCK = 128                  # values along a row that share a scale
 
 
 def make_norm_params(R, D, dtype, param_dtype, eps=1e-5) -> ppow_norm_params:
-    return ppow_norm_params(int(R), int(D), DTYPE_CODES[dtype], DTYPE_CODES[param_dtype], float(eps))
+    if dtype not in DTYPE_CODES or param_dtype not in DTYPE_CODES:
+        raise ValueError("types must be float32, bfloat16 or float16, got %s and %s" % (dtype, param_dtype))
+    return ppow_norm_params(R, D, DTYPE_CODES[dtype], DTYPE_CODES[param_dtype], eps)
 
 
-def _check_packed(packed, scale, R, D):
-    _check_shape(packed, (R, D), "packed")
-    _check_shape(scale, (R, -(-D // CHECKPOINT_BLOCK)), "scale")
-    return _dev_ptr(packed, CHECKPOINT_DTYPE, "packed"), _dev_ptr(scale, torch.uint8, "scale")
+def _packed_args(packed, scale, R, D, dev):
+    return (_arg(packed, CHECKPOINT_DTYPE, (R, D), dev, "packed"),
+            _arg(scale, torch.uint8, (R, (D + CHECKPOINT_BLOCK - 1) // CHECKPOINT_BLOCK), dev, "scale"))
 
 
 def ppow_layer_norm(params: ppow_norm_params, x, weight, bias, y, mean, rstd, packed=None, scale=None, stream=None) -> None:
     """Enqueue the forward pass on ``x`` [R, D]; with ``packed`` and ``scale`` it also writes the 8-bit form of ``x``."""
-    R, D, dt, pt = params.R, params.D, LOGIT_DTYPES[params.dtype], LOGIT_DTYPES[params.param_dtype]
-    for name, t, shape in (("x", x, (R, D)), ("weight", weight, (D,)), ("bias", bias, (D,)), ("y", y, (R, D)), ("mean", mean, (R,)),
-                           ("rstd", rstd, (R,))):
-        _check_shape(t, shape, name)
-    _check_device(x.device, weight=weight, bias=bias, y=y, mean=mean, rstd=rstd, packed=packed, scale=scale)
-    xp, xs = _rows_ptr(x, dt, "x")
-    st = load_library().ppow_layer_norm(
-        ctypes.byref(params), xp, xs, _dev_ptr(weight, pt, "weight"), _dev_ptr(bias, pt, "bias"), _dev_ptr(y, dt, "y"),
-        _dev_ptr(mean, torch.float32, "mean"), _dev_ptr(rstd, torch.float32, "rstd"), *_check_packed(packed, scale, R, D),
-        _stream_ptr(stream))
-    if st != PPOW_OK:
-        raise PpowError(st, "ppow_layer_norm")
+    R, D, dt, pt, dev = params.R, params.D, LOGIT_DTYPES[params.dtype], LOGIT_DTYPES[params.param_dtype], _index_of(x, "x")
+    f32 = torch.float32
+    _call(load_library().ppow_layer_norm, "ppow_layer_norm", dev, ctypes.byref(params), *_rows_arg(x, dt, (R, D), dev, "x"),
+          _arg(weight, pt, (D,), dev, "weight"), _arg(bias, pt, (D,), dev, "bias"), _arg(y, dt, (R, D), dev, "y"),
+          _arg(mean, f32, (R,), dev, "mean"), _arg(rstd, f32, (R,), dev, "rstd"), *_packed_args(packed, scale, R, D, dev),
+          _raw_stream(stream, dev))
 
 
 def ppow_layer_norm_workspace_bytes(params: ppow_norm_params) -> int:
-    return int(load_library().ppow_layer_norm_workspace_bytes(ctypes.byref(params)))
+    return load_library().ppow_layer_norm_workspace_bytes(ctypes.byref(params))
 
 
 def ppow_layer_norm_backward(params: ppow_norm_params, grad_y, x, packed, scale, weight, mean, rstd, grad_x, grad_weight, grad_bias,
                              workspace, stream=None) -> None:
     """Enqueue the gradient; the forward pass's input is either ``x`` or, where that is None, ``packed`` and ``scale``."""
-    R, D, dt, pt = params.R, params.D, LOGIT_DTYPES[params.dtype], LOGIT_DTYPES[params.param_dtype]
-    for name, t, shape in (("grad_y", grad_y, (R, D)), ("x", x, (R, D)), ("weight", weight, (D,)), ("mean", mean, (R,)), ("rstd", rstd, (R,)),
-                           ("grad_x", grad_x, (R, D)), ("grad_weight", grad_weight, (D,)), ("grad_bias", grad_bias, (D,))):
-        _check_shape(t, shape, name)
-    _check_device(grad_y.device, x=x, packed=packed, scale=scale, weight=weight, mean=mean, rstd=rstd, grad_x=grad_x,
-                  grad_weight=grad_weight, grad_bias=grad_bias, workspace=workspace)
-    gp, gs = _rows_ptr(grad_y, dt, "grad_y")
-    xp, xs = (None, D) if x is None else _rows_ptr(x, dt, "x")
-    st = load_library().ppow_layer_norm_backward(
-        ctypes.byref(params), gp, gs, xp, xs, *_check_packed(packed, scale, R, D), _dev_ptr(weight, pt, "weight"),
-        _dev_ptr(mean, torch.float32, "mean"), _dev_ptr(rstd, torch.float32, "rstd"), _dev_ptr(grad_x, dt, "grad_x"),
-        _dev_ptr(grad_weight, pt, "grad_weight"), _dev_ptr(grad_bias, pt, "grad_bias"), _dev_ptr(workspace, torch.uint8, "workspace"),
-        workspace.numel(), _stream_ptr(stream))
-    if st != PPOW_OK:
-        raise PpowError(st, "ppow_layer_norm_backward")
+    R, D, dt, pt, dev = params.R, params.D, LOGIT_DTYPES[params.dtype], LOGIT_DTYPES[params.param_dtype], _index_of(grad_y, "grad_y")
+    f32 = torch.float32
+    xp, xs = (None, D) if x is None else _rows_arg(x, dt, (R, D), dev, "x")
+    _call(load_library().ppow_layer_norm_backward, "ppow_layer_norm_backward", dev, ctypes.byref(params),
+          *_rows_arg(grad_y, dt, (R, D), dev, "grad_y"), xp, xs, *_packed_args(packed, scale, R, D, dev),
+          _arg(weight, pt, (D,), dev, "weight"), _arg(mean, f32, (R,), dev, "mean"), _arg(rstd, f32, (R,), dev, "rstd"),
+          _arg(grad_x, dt, (R, D), dev, "grad_x"), _arg(grad_weight, pt, (D,), dev, "grad_weight"),
+          _arg(grad_bias, pt, (D,), dev, "grad_bias"), *_workspace_arg(workspace, dev), _raw_stream(stream, dev))
+
+
+def _storage_code(dtype, name) -> int:
+    code = DTYPE_CODES.get(dtype)
+    if code is None:
+        raise ValueError("%s must be float32, bfloat16 or float16, got %s" % (name, dtype))
+    return code
 
 
 def ppow_pack_activation(x, packed, scale, stream=None) -> None:
     """Enqueue the 8-bit form of ``x`` [R, D]: codes into ``packed`` [R, D], exponents into ``scale`` [R, ceil(D/128)]."""
-    if x.dtype not in DTYPE_CODES:
-        raise ValueError("x must be float32, bfloat16 or float16, got %s" % x.dtype)
-    xp, xs = _rows_ptr(x, x.dtype, "x")
     R, D = x.shape
-    _check_device(x.device, packed=packed, scale=scale)
-    st = load_library().ppow_pack_activation(xp, xs, R, D, DTYPE_CODES[x.dtype], *_check_packed(packed, scale, R, D), _stream_ptr(stream))
-    if st != PPOW_OK:
-        raise PpowError(st, "ppow_pack_activation")
+    code, dev = _storage_code(x.dtype, "x"), _index_of(x, "x")
+    _call(load_library().ppow_pack_activation, "ppow_pack_activation", dev, *_rows_arg(x, x.dtype, (R, D), dev, "x"), R, D, code,
+          *_packed_args(packed, scale, R, D, dev), _raw_stream(stream, dev))
 
 
 def ppow_unpack_activation(packed, scale, x, stream=None) -> None:
     """Enqueue the way back: values of the 8-bit form into ``x`` [R, D], rounded to its type."""
-    if x.dtype not in DTYPE_CODES:
-        raise ValueError("x must be float32, bfloat16 or float16, got %s" % x.dtype)
     R, D = packed.shape
-    _check_shape(x, (R, D), "x")
-    _check_device(packed.device, scale=scale, x=x)
-    st = load_library().ppow_unpack_activation(*_check_packed(packed, scale, R, D), R, D, DTYPE_CODES[x.dtype], _dev_ptr(x, x.dtype, "x"),
-                                               _stream_ptr(stream))
-    if st != PPOW_OK:
-        raise PpowError(st, "ppow_unpack_activation")
+    code, dev = _storage_code(x.dtype, "x"), _index_of(packed, "packed")
+    _call(load_library().ppow_unpack_activation, "ppow_unpack_activation", dev, *_packed_args(packed, scale, R, D, dev), R, D, code,
+          _arg(x, x.dtype, (R, D), dev, "x"), _raw_stream(stream, dev))
 
 
 def _host_ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
@@ -708,7 +719,7 @@ def head_logprob(hidden, weight, tokens, *, temperature=1.0, stream=None) -> dic
     """Allocate outputs and workspace, run ppow_head_logprob; returns logp and lse, both [T] float32."""
     params = make_head_params(hidden, weight, temperature)
     dev = hidden.device
-    with _on(dev, stream):
+    with _On(stream):
         out = {"logp": torch.empty((params.T,), dtype=torch.float32, device=dev),
                "lse": torch.empty((params.T,), dtype=torch.float32, device=dev)}
         ws = alloc_workspace(ppow_head_workspace_bytes(params, False), dev)
@@ -720,7 +731,7 @@ def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature
     """Allocate gradients and workspace, run ppow_head_logprob_backward; returns (grad_hidden, grad_weight), None where not wanted."""
     params = make_head_params(hidden, weight, temperature)
     dev = hidden.device
-    with _on(dev, stream):
+    with _On(stream):
         gh = torch.empty((params.T, params.D), dtype=hidden.dtype, device=dev) if want_hidden else None
         gw = torch.empty((params.V, params.D), dtype=hidden.dtype, device=dev) if want_weight else None
         ws = alloc_workspace(ppow_head_workspace_bytes(params, True), dev)
@@ -734,7 +745,7 @@ def layer_norm(x, weight, bias=None, *, eps=1e-5, checkpoint=False, stream=None)
     R, D = x.shape
     params = make_norm_params(R, D, x.dtype, weight.dtype, eps)
     dev = x.device
-    with _on(dev, stream):
+    with _On(stream):
         out = {"y": torch.empty((R, D), dtype=x.dtype, device=dev), "mean": torch.empty((R,), dtype=torch.float32, device=dev),
                "rstd": torch.empty((R,), dtype=torch.float32, device=dev)}
         if checkpoint:
@@ -750,7 +761,7 @@ def layer_norm_backward(grad_y, x, weight, mean, rstd, *, want_bias=True, stream
     params = make_norm_params(R, D, grad_y.dtype, weight.dtype)
     dev = grad_y.device
     x, packed, scale = (None, *x) if isinstance(x, (tuple, list)) else (x, None, None)
-    with _on(dev, stream):
+    with _On(stream):
         gx = torch.empty((R, D), dtype=grad_y.dtype, device=dev)
         gw = torch.empty((D,), dtype=weight.dtype, device=dev)
         gb = torch.empty((D,), dtype=weight.dtype, device=dev) if want_bias else None
@@ -767,7 +778,7 @@ def _alloc_packed(R: int, D: int, dev) -> dict:
 def pack_activation(x, stream=None):
     """Allocate and run ppow_pack_activation; returns (packed, scale)."""
     dev = x.device
-    with _on(dev, stream):
+    with _On(stream):
         out = _alloc_packed(x.shape[0], x.shape[1], dev)
         ppow_pack_activation(x, out["packed"], out["scale"], stream)
     return out["packed"], out["scale"]
@@ -776,7 +787,7 @@ def pack_activation(x, stream=None):
 def unpack_activation(packed, scale, dtype=torch.bfloat16, stream=None):
     """Allocate and run ppow_unpack_activation; returns the restored activation in ``dtype``."""
     dev = packed.device
-    with _on(dev, stream):
+    with _On(stream):
         x = torch.empty(tuple(packed.shape), dtype=dtype, device=dev)
         ppow_unpack_activation(packed, scale, x, stream)
     return x

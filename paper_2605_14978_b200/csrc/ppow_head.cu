@@ -17,6 +17,8 @@
 #include "ppow_mma.cuh"
 
 #include <cuda_bf16.h>
+
+#include <atomic>
 #include <math.h>
 
 namespace ppow {
@@ -696,18 +698,30 @@ bool make_map(CUtensorMap *map, const void *base, bool bf16, int64_t width, int6
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int pair_count()
+// Pairs of SMs of the current device, asked once per device; the kernels' shared-memory limit is raised at the same time.
+constexpr int DEVICES = 64;
+template <int PRODUCT, bool BF16> bool allow_smem()
 {
+    return cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MMA_SMEM) == cudaSuccess;
+}
+template <bool BF16> int pair_count()
+{
+    static std::atomic<int> known[DEVICES];
     int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return sms / 2;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEVICES) return 0;
+    int n = known[dev].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    if (!allow_smem<LOGITS_SUM, BF16>() || !allow_smem<LOGITS_GRAD, BF16>() || !allow_smem<GRAD_HIDDEN, BF16>() ||
+        !allow_smem<GRAD_WEIGHT, BF16>() || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return 0;
+    n = sms / 2;
+    known[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 template <int PRODUCT, bool BF16>
 bool launch_product(const CUtensorMap &a, const CUtensorMap &b, const ProductJob &job, int64_t most_tiles, int pairs, cudaStream_t stream)
 {
-    if (cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MMA_SMEM) != cudaSuccess)
-        return false;
     const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
     head_product_kernel<PRODUCT, BF16><<<2 * n, MMA_THREADS, MMA_SMEM, stream>>>(a, b, job);
     return cudaGetLastError() == cudaSuccess;
@@ -757,7 +771,7 @@ ppow_status forward(const ppow_head_params *p, const void *hidden, const void *w
     if (!make_map(&map_rows, rows.rows, BF16, p->D, L.padded, p->D, HALF_TILE) ||
         !make_map(&map_weight, weight, BF16, p->D, p->V, p->weight_stride, HALF_TILE))
         return PPOW_ERR_CUDA;
-    const int pairs = pair_count();
+    const int pairs = pair_count<BF16>();
     if (pairs < 1) return PPOW_ERR_CUDA;
     GatherJob g = {};
     g.tokens = tokens;
@@ -794,7 +808,7 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
         !make_map(&map_weight_t, weight, BF16, p->D, p->V, p->weight_stride, BK) ||
         !make_map(&map_dz, dz, BF16, L.piece, L.padded, L.piece, HALF_TILE) || !make_map(&map_dz_t, dz, BF16, L.piece, L.padded, L.piece, BK))
         return PPOW_ERR_CUDA;
-    const int pairs = pair_count();
+    const int pairs = pair_count<BF16>();
     if (pairs < 1) return PPOW_ERR_CUDA;
     GatherJob g = {};
     g.tokens = tokens;

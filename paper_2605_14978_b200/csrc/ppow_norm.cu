@@ -18,6 +18,7 @@
 
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
+#include <atomic>
 #include <math.h>
 
 namespace ppow {
@@ -659,63 +660,77 @@ bool vec_ok(const void *p, int64_t stride, int32_t D, size_t es)
     return (uintptr_t)p % 16 == 0 && (size_t)D * es % 16 == 0 && (size_t)stride * es % 16 == 0;
 }
 
-int sm_count()
+// CTAs of a kernel that one launch keeps resident on the current device; asked once per device and kernel.
+constexpr int DEVICES = 64;
+struct Resident {
+    std::atomic<int> ctas[DEVICES];
+};
+template <typename Kernel>
+int resident_ctas(Resident &known, Kernel kernel, int threads, size_t smem)
 {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return sms;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEVICES) return 0;
+    int n = known.ctas[dev].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    int sms = 0, per_sm = 0;
+    if (smem > 0 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return 0;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess)
+        return 0;
+    n = sms * per_sm;
+    known.ctas[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 // CTAs of the backward pass: each leaves one share of the column sums.  148 SMs x 2 to 4; a function of the sizes alone.
 constexpr int32_t SHARES_MAX = 148 * 4;
 
 template <int DTYPE, bool VEC, int TPR, int U>
-bool forward_launch(const NormJob &job, int sms, cudaStream_t stream)
+bool forward_launch(const NormJob &job, cudaStream_t stream)
 {
     constexpr int THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR;
-    int resident = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, norm_forward_kernel<DTYPE, VEC, TPR, U>, THREADS, 0) != cudaSuccess || resident < 1)
-        return false;
-    const int64_t need = ((int64_t)job.R + ROWS - 1) / ROWS, most = (int64_t)sms * resident;
+    static Resident known;
+    const int64_t need = ((int64_t)job.R + ROWS - 1) / ROWS, most = resident_ctas(known, norm_forward_kernel<DTYPE, VEC, TPR, U>, THREADS, 0);
+    if (most < 1) return false;
     norm_forward_kernel<DTYPE, VEC, TPR, U><<<(unsigned)(need < most ? need : most), THREADS, 0, stream>>>(job);
     return cudaGetLastError() == cudaSuccess;
 }
 
 template <int DTYPE, bool VEC>
-bool forward_shape(const NormJob &job, int sms, cudaStream_t stream)
+bool forward_shape(const NormJob &job, cudaStream_t stream)
 {
     const int32_t units = VEC ? job.D / (16 / (int32_t)bytes_of(DTYPE)) : (job.D + CKPT_BLOCK - 1) / CKPT_BLOCK * 32;
-    if (units <= 32 * 4) return forward_launch<DTYPE, VEC, 32, 4>(job, sms, stream);
-    if (units <= 128 * 4) return forward_launch<DTYPE, VEC, 128, 4>(job, sms, stream);
-    if (units <= 256 * 4) return forward_launch<DTYPE, VEC, 256, 4>(job, sms, stream);
-    return forward_launch<DTYPE, VEC, 1024, 4>(job, sms, stream);
+    if (units <= 32 * 4) return forward_launch<DTYPE, VEC, 32, 4>(job, stream);
+    if (units <= 128 * 4) return forward_launch<DTYPE, VEC, 128, 4>(job, stream);
+    if (units <= 256 * 4) return forward_launch<DTYPE, VEC, 256, 4>(job, stream);
+    return forward_launch<DTYPE, VEC, 1024, 4>(job, stream);
 }
 
 template <int DTYPE, bool VEC, bool PACKED, int TPR, int U>
-bool backward_launch(const NormGradJob &job, int sms, int32_t *shares, cudaStream_t stream)
+bool backward_launch(const NormGradJob &job, int32_t *shares, cudaStream_t stream)
 {
     constexpr int THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR;
-    const size_t smem = TPR <= 256 ? 0 : (size_t)job.D * 8;
+    constexpr size_t SMEM = TPR <= 256 ? 0 : (size_t)NORM_MAX_WIDTH * 8;
     auto kernel = norm_backward_kernel<DTYPE, VEC, PACKED, TPR, U>;
-    if (smem > 0 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
-    int resident = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, THREADS, smem) != cudaSuccess || resident < 1) return false;
+    static Resident known;
+    const int64_t most = resident_ctas(known, kernel, THREADS, SMEM);
+    if (most < 1) return false;
     int64_t n = ((int64_t)job.R + ROWS - 1) / ROWS;
-    if (n > (int64_t)sms * resident) n = (int64_t)sms * resident;
+    if (n > most) n = most;
     if (n > SHARES_MAX) n = SHARES_MAX;
     *shares = (int32_t)n;
-    kernel<<<(unsigned)n, THREADS, smem, stream>>>(job);
+    kernel<<<(unsigned)n, THREADS, SMEM, stream>>>(job);
     return cudaGetLastError() == cudaSuccess;
 }
 
 template <int DTYPE, bool VEC, bool PACKED>
-bool backward_shape(const NormGradJob &job, int sms, int32_t *shares, cudaStream_t stream)
+bool backward_shape(const NormGradJob &job, int32_t *shares, cudaStream_t stream)
 {
     const int32_t units = VEC ? job.D / (16 / (int32_t)bytes_of(DTYPE)) : (job.D + CKPT_BLOCK - 1) / CKPT_BLOCK * 32;
-    if (units <= 32 * 4) return backward_launch<DTYPE, VEC, PACKED, 32, 4>(job, sms, shares, stream);
-    if (units <= 128 * 4) return backward_launch<DTYPE, VEC, PACKED, 128, 4>(job, sms, shares, stream);
-    if (units <= 256 * 4) return backward_launch<DTYPE, VEC, PACKED, 256, 4>(job, sms, shares, stream);
-    return backward_launch<DTYPE, VEC, PACKED, 1024, 4>(job, sms, shares, stream);
+    if (units <= 32 * 4) return backward_launch<DTYPE, VEC, PACKED, 32, 4>(job, shares, stream);
+    if (units <= 128 * 4) return backward_launch<DTYPE, VEC, PACKED, 128, 4>(job, shares, stream);
+    if (units <= 256 * 4) return backward_launch<DTYPE, VEC, PACKED, 256, 4>(job, shares, stream);
+    return backward_launch<DTYPE, VEC, PACKED, 1024, 4>(job, shares, stream);
 }
 
 template <int DTYPE, bool VEC>
@@ -756,12 +771,10 @@ extern "C" ppow_status ppow_layer_norm(const ppow_norm_params *params, const voi
     if (!x || !weight || !y || !mean || !rstd || !packed != !scale) return PPOW_ERR_INVALID_ARG;
     if ((uintptr_t)x % es || (uintptr_t)y % es || (uintptr_t)weight % ps || (uintptr_t)bias % ps || (uintptr_t)mean % 4 || (uintptr_t)rstd % 4)
         return PPOW_ERR_INVALID_ARG;
-    const int sms = sm_count();
-    if (sms < 1) return PPOW_ERR_CUDA;
     NormJob job = {x, x_stride, weight, bias, params->R, params->D, params->param_dtype, (params->D + CKPT_BLOCK - 1) / CKPT_BLOCK,
                    params->eps, y, mean, rstd, packed, scale};
     const bool vec = vec_ok(x, x_stride, params->D, es) && (uintptr_t)y % 16 == 0 && (uintptr_t)packed % 8 == 0;
-#define PPOW_CALL(DT, VEC) forward_shape<DT, VEC>(job, sms, (cudaStream_t)cuda_stream)
+#define PPOW_CALL(DT, VEC) forward_shape<DT, VEC>(job, (cudaStream_t)cuda_stream)
     return PPOW_BY_TYPE(params->dtype, vec, PPOW_CALL) ? PPOW_OK : PPOW_ERR_CUDA;
 #undef PPOW_CALL
 }
@@ -794,14 +807,12 @@ extern "C" ppow_status ppow_layer_norm_backward(const ppow_norm_params *params, 
         (uintptr_t)rstd % 4)
         return PPOW_ERR_INVALID_ARG;
     if (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < ppow_layer_norm_workspace_bytes(params)) return PPOW_ERR_WORKSPACE;
-    const int sms = sm_count();
-    if (sms < 1) return PPOW_ERR_CUDA;
     NormGradJob job = {grad_y, grad_y_stride, x, x_stride, packed, scale, weight, mean, rstd, params->R, params->D, params->param_dtype,
                        (params->D + CKPT_BLOCK - 1) / CKPT_BLOCK, grad_x, (float *)workspace};
     const bool vec = vec_ok(grad_y, grad_y_stride, params->D, es) && (uintptr_t)grad_x % 16 == 0 &&
                      (x ? vec_ok(x, x_stride, params->D, es) : (uintptr_t)packed % 8 == 0);
     int32_t shares = 0;
-#define PPOW_CALL(DT, VEC) (x ? backward_shape<DT, VEC, false>(job, sms, &shares, stream) : backward_shape<DT, VEC, true>(job, sms, &shares, stream))
+#define PPOW_CALL(DT, VEC) (x ? backward_shape<DT, VEC, false>(job, &shares, stream) : backward_shape<DT, VEC, true>(job, &shares, stream))
     if (!PPOW_BY_TYPE(params->dtype, vec, PPOW_CALL)) return PPOW_ERR_CUDA;
 #undef PPOW_CALL
     if (grad_weight || grad_bias) {
