@@ -25,19 +25,24 @@ namespace ppow {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int TILE = 256;            // rows and columns of an output tile (a pair of CTAs)
-constexpr int HALF_TILE = 128;       // rows of A and columns of B that one CTA holds
+constexpr int HALF_TILE = 128;       // rows of A that one CTA holds
 constexpr int BK = 64;               // products' inner step per pipeline stage: one 128-byte swizzle row
-constexpr int STAGES = 6;
-constexpr uint32_t OPERAND_BYTES = HALF_TILE * BK * 2;     // 16 KB
-constexpr uint32_t STAGE_BYTES = 2 * OPERAND_BYTES;
-constexpr int MMA_THREADS = 192;     // producer warp, issuing warp, four epilogue warps
-constexpr size_t MMA_SMEM = 1024 + (size_t)STAGES * STAGE_BYTES + 256;
+constexpr uint32_t A_BYTES = HALF_TILE * BK * 2;           // 16 KB
+constexpr int MMA_THREADS = 320;     // producer warp, issuing warp, eight epilogue warps
+constexpr int PAIRS = 74;            // pairs of SMs that the shares of an inner axis are planned for
+
+// Columns of a tile: 256, or for few tokens the tokens themselves (16, 32, 64 or 128), with W taking the 256 rows.
+template <int N> __host__ __device__ constexpr uint32_t stage_bytes() { return A_BYTES + N / 2 * BK * 2; }
+template <int N> __host__ __device__ constexpr int stage_count()
+{
+    return N == 256 ? 6 : N == 128 ? 8 : N == 64 ? 10 : N == 32 ? 11 : 12;    // 192 to 204 KB
+}
+template <int N> __host__ __device__ constexpr size_t mma_smem() { return 1024 + (size_t)stage_count<N>() * stage_bytes<N>() + 256; }
 
 constexpr int GATHER_THREADS = 256;
 constexpr int GATHER_ROWS_MAX = 1024, GATHER_CTAS = 1024;
 constexpr size_t HEADER_BYTES = 256;
 constexpr size_t DZ_BYTES = 512u << 20;      // a piece of dz holds at most this much
-constexpr int MAX_SPLIT = 16;
 constexpr int32_t MAX_TOKENS = 1 << 20, MAX_VOCAB = 1 << 22, MAX_WIDTH = 1 << 16;
 
 // First bytes of the workspace; error_flags sits where ppow_read_error_flags looks for it.
@@ -46,6 +51,7 @@ struct HeadHeader {
     unsigned int error_flags;
     int32_t live;          // live rows
     float out_scale;       // factor of dW (f16: undoes the power of two that the rows were brought to)
+    int32_t splits;        // shares of the inner axis of dh
 };
 
 // Arrays of the workspace, all indexed by live row.
@@ -71,13 +77,38 @@ struct GatherJob {
     uint16_t *grad_hidden;          // backward: masked rows receive 0 (may be null)
     int64_t stride;
     int32_t T, D, V, rows_per_cta;
+    int32_t few;                    // token columns of a call of few tokens, else 0
+    int32_t d_tiles, piece_steps;   // backward: what the shares of dh follow from
     float inv_temperature;
     bool vec;                       // rows start on 16-byte boundaries
 };
 
+// Shares of the inner axis of dh: `tiles` output tiles times the shares should fill whole rounds of the pairs.  A share is
+// at least eight steps long, and each one costs a pass over its sums (2 % of a round is about what that measures).
+constexpr int32_t SPLIT_TILES = 8 * PAIRS;      // tiles x shares where there is more than one share
+__device__ __forceinline__ int32_t split_count(int32_t tiles, int32_t steps)
+{
+    int32_t best = 1;
+    float best_cost = (float)((tiles + PAIRS - 1) / PAIRS);
+    for (int32_t s = 2; s <= PAIRS && s * 8 <= steps && s * tiles <= SPLIT_TILES; ++s) {
+        const float cost = (float)((tiles * s + PAIRS - 1) / PAIRS) / (float)s * (1.0f + 0.02f * (float)min(s, 10));
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+
 // mult of a row, and for f16 the split into a factor near 2^15 and a power of two: dz of a row whose gradient is small
 // would fall below f16's smallest values.
 __device__ __forceinline__ float row_mult(float g, float inv_temperature) { return -g * inv_temperature; }
+__device__ __forceinline__ int row_exponent(float mult, int top)
+{
+    int e = top;
+    if (isfinite(mult) && mult != 0.0f) frexpf(mult, &e);
+    return e;
+}
 
 // Every CTA looks at all T tokens (4 bytes each, from L2) to learn where its rows go, instead of waiting for a scan kernel.
 template <bool BACKWARD, bool SCALED>
@@ -86,6 +117,7 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
     __shared__ int32_t part[4][GATHER_THREADS / 32];
     __shared__ int32_t dest[GATHER_ROWS_MAX];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    allow_next_kernel();
     const int32_t r0 = (int32_t)min((int64_t)blockIdx.x * job.rows_per_cta, (int64_t)job.T);
     const int32_t n = min(job.rows_per_cta, job.T - r0);
     auto live = [&](int32_t i) {
@@ -101,11 +133,7 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
         range |= job.tokens[i] >= job.V;
         if (SCALED && ok) {
             const float m = row_mult(job.grad[i], job.inv_temperature);
-            int e;
-            if (isfinite(m) && m != 0.0f) {
-                frexpf(m, &e);
-                top = max(top, e);
-            }
+            if (isfinite(m) && m != 0.0f) top = max(top, row_exponent(m, 0));
         }
     }
     before = __reduce_add_sync(0xffffffffu, before);
@@ -133,6 +161,10 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
         out.header->error_flags = range ? (unsigned)PPOW_FLAG_TOKEN_RANGE : 0u;
         out.header->live = total;
         out.header->out_scale = SCALED ? ldexpf(1.0f, top - 15) : 1.0f;
+        if (BACKWARD) {
+            const int64_t tiles = (int64_t)(job.few ? 1 : max(1, (total + TILE - 1) / TILE)) * job.d_tiles;
+            out.header->splits = tiles > SPLIT_TILES ? 1 : split_count((int32_t)tiles, job.piece_steps);
+        }
     }
     if (warp == 0) {
         int32_t next = before;
@@ -145,75 +177,68 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
     }
     __syncthreads();
 
-    const int32_t units = job.D / 8;     // 16-byte units of a row
-    for (int32_t k = warp; k < n; k += GATHER_THREADS / 32) {
+    // per row: what the products need to know of it
+    for (int32_t k = tid; k < n; k += GATHER_THREADS) {
         const int32_t r = r0 + k, d = dest[k];
         if (d < 0) {
-            if (!BACKWARD && lane == 0) {
-                job.logp_out[r] = 0.0f;
-                job.lse_out[r] = 0.0f;
-            }
-            if (BACKWARD && job.grad_hidden)
-                for (int32_t u = lane; u < units; u += 32)
-                    reinterpret_cast<uint4 *>(job.grad_hidden + (size_t)r * job.D)[u] = make_uint4(0, 0, 0, 0);
+            if (!BACKWARD) job.logp_out[r] = job.lse_out[r] = 0.0f;
             continue;
         }
         if (!PPOW_CHECK(d < total && d <= r, 501, nullptr)) continue;
-        int e = 0;
-        if (lane == 0) {
-            out.source[d] = r;
-            out.token[d] = job.tokens[r];
-        }
+        out.source[d] = r;
+        out.token[d] = job.tokens[r];
         if (BACKWARD) {
             float m = row_mult(job.grad[r], job.inv_temperature), scale = 1.0f;
             if (SCALED) {
-                m = frexpf(m, &e);
-                if (!isfinite(m) || m == 0.0f) e = top;
-                m = ldexpf(m, 15);
+                const int e = row_exponent(m, top);
+                m = ldexpf(m, 15 - e);
                 scale = ldexpf(1.0f, e - 15);
             }
-            if (lane == 0) {
-                out.mult[d] = m;
-                out.row_scale[d] = scale;
-                out.lse2[d] = job.lse[r] * LOG2E;
-            }
+            out.mult[d] = m;
+            out.row_scale[d] = scale;
+            out.lse2[d] = job.lse[r] * LOG2E;
+        }
+    }
+    // the rows themselves, by 16-byte units
+    const int32_t units = job.D / 8;
+    for (int32_t i = tid; i < n * units; i += GATHER_THREADS) {
+        const int32_t k = i / units, u = i % units, r = r0 + k, d = dest[k];
+        if (d < 0) {
+            if (BACKWARD && job.grad_hidden) reinterpret_cast<uint4 *>(job.grad_hidden + (size_t)r * job.D)[u] = make_uint4(0, 0, 0, 0);
+            continue;
         }
         const uint16_t *src = job.hidden + (size_t)r * job.stride;
-        uint4 *to = reinterpret_cast<uint4 *>((uint16_t *)out.rows + (size_t)d * job.D);
-        uint4 *to_scaled = SCALED ? reinterpret_cast<uint4 *>((uint16_t *)out.scaled + (size_t)d * job.D) : nullptr;
-        const float down = SCALED ? ldexpf(1.0f, e - top) : 1.0f;
-        for (int32_t u = lane; u < units; u += 32) {
-            uint4 x;
-            if (job.vec) {
-                x = __ldg(reinterpret_cast<const uint4 *>(src) + u);
-            } else {
-                uint32_t w[4];
+        uint4 x;
+        if (job.vec) {
+            x = __ldg(reinterpret_cast<const uint4 *>(src) + u);
+        } else {
+            uint32_t w[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) w[q] = (uint32_t)src[u * 8 + 2 * q] | ((uint32_t)src[u * 8 + 2 * q + 1] << 16);
-                x = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-            to[u] = x;
-            if (SCALED) {
-                uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            for (int q = 0; q < 4; ++q) w[q] = (uint32_t)src[u * 8 + 2 * q] | ((uint32_t)src[u * 8 + 2 * q + 1] << 16);
+            x = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        reinterpret_cast<uint4 *>((uint16_t *)out.rows + (size_t)d * job.D)[u] = x;
+        if (SCALED) {
+            const float down = ldexpf(1.0f, row_exponent(row_mult(job.grad[r], job.inv_temperature), top) - top);
+            uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const __half2 h = *reinterpret_cast<__half2 *>(&w[q]);
-                    const __half2 s = __floats2half2_rn(__low2float(h) * down, __high2float(h) * down);
-                    w[q] = *reinterpret_cast<const uint32_t *>(&s);
-                }
-                to_scaled[u] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int q = 0; q < 4; ++q) {
+                const __half2 h = *reinterpret_cast<__half2 *>(&w[q]);
+                const __half2 s = __floats2half2_rn(__low2float(h) * down, __high2float(h) * down);
+                w[q] = *reinterpret_cast<const uint32_t *>(&s);
             }
+            reinterpret_cast<uint4 *>((uint16_t *)out.scaled + (size_t)d * job.D)[u] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
     // the last tile's rows behind the live ones are zeros: they are products' operands too
-    const int32_t padded = max(TILE, (total + TILE - 1) / TILE * TILE);
-    for (int32_t p = total + blockIdx.x * (GATHER_THREADS / 32) + warp; p < padded; p += gridDim.x * (GATHER_THREADS / 32)) {
-        if (lane == 0) {
+    const int32_t padded = job.few ? job.few : max(TILE, (total + TILE - 1) / TILE * TILE);
+    for (int32_t p = total + blockIdx.x; p < padded; p += gridDim.x) {
+        if (tid == 0) {
             out.token[p] = -1;
             out.mult[p] = 0.0f;
             out.lse2[p] = 0.0f;
         }
-        for (int32_t u = lane; u < units; u += 32) {
+        for (int32_t u = tid; u < units; u += GATHER_THREADS) {
             reinterpret_cast<uint4 *>((uint16_t *)out.rows + (size_t)p * job.D)[u] = make_uint4(0, 0, 0, 0);
             if (SCALED) reinterpret_cast<uint4 *>((uint16_t *)out.scaled + (size_t)p * job.D)[u] = make_uint4(0, 0, 0, 0);
         }
@@ -233,21 +258,22 @@ struct ProductJob {
     float scale;            // log2(e) / temperature
     int32_t D, V;
     int32_t v0, columns;    // the piece: vocabulary entries v0 .. v0 + columns - 1
-    int32_t v_tiles, d_tiles, splits;
+    int32_t v_tiles, d_tiles;
     int32_t piece;          // row length of dz
     bool add;               // GRAD_HIDDEN: add to what the pieces before left
-    float2 *partial;        // LOGITS_SUM: [live row][v_tiles] maximum, sum (log2 units)
+    bool wide_rows;         // grad_weight: rows in whole 32-byte units
+    int32_t parts;          // LOGITS_SUM: entries of `partial` per row
+    float2 *partial;        // LOGITS_SUM: [live row][parts] maximum, sum (log2 units)
     float *at_token;        // LOGITS_SUM: the token's product, per live row
     uint16_t *dz;           // [padded rows][piece]
-    float *grad_rows;       // GRAD_HIDDEN: [splits][padded rows][D]
-    size_t split_stride;
+    float *grad_rows;       // GRAD_HIDDEN: [splits][padded live rows][D]
     uint16_t *grad_weight;  // [V, D]
 };
 
 struct Tile {
-    int32_t row, col;       // first row and column, in elements of the product's own axes
+    int32_t row, col;       // first row of A and column of B, in elements of the product's own axes
     int32_t k0, k1;         // inner steps of BK
-    int32_t index, split;   // column tile; share of the inner axis
+    int32_t index, split;   // tile along the vocabulary or the width; share of the inner axis
 };
 
 template <bool BF16>
@@ -261,55 +287,260 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// What a launch works on: sizes that follow from the number of live rows.
+struct Extent {
+    int32_t live, row_tiles, splits;
+};
+
 template <int PRODUCT>
-__device__ __forceinline__ int64_t tile_count(const ProductJob &job, int32_t row_tiles)
+__device__ __forceinline__ int64_t tile_count(const ProductJob &job, const Extent &x)
 {
-    if (PRODUCT == GRAD_HIDDEN) return (int64_t)row_tiles * job.d_tiles * job.splits;
+    if (PRODUCT == GRAD_HIDDEN) return (int64_t)x.row_tiles * job.d_tiles * x.splits;
     if (PRODUCT == GRAD_WEIGHT) return (int64_t)job.v_tiles * job.d_tiles;
-    return (int64_t)row_tiles * job.v_tiles;
+    return (int64_t)x.row_tiles * job.v_tiles;
 }
 
 // Logit tiles go through all rows for one strip of W, then the next strip: W comes from HBM once, the rows stay in L2.
-template <int PRODUCT>
-__device__ __forceinline__ Tile tile_at(const ProductJob &job, int32_t row_tiles, int32_t live, int64_t t)
+// With few tokens there is one tile of them, the columns, and the rows are the vocabulary's or the width's.
+template <int PRODUCT, bool FEW>
+__device__ __forceinline__ Tile tile_at(const ProductJob &job, const Extent &e, int64_t t)
 {
     Tile x;
     x.split = 0;
     if (PRODUCT == LOGITS_SUM || PRODUCT == LOGITS_GRAD) {
-        x.index = (int32_t)(t / row_tiles);
-        x.row = (int32_t)(t % row_tiles) * TILE;
-        x.col = job.v0 + x.index * TILE;
+        x.index = (int32_t)(FEW ? t : t / e.row_tiles);
+        const int32_t rows = (int32_t)(FEW ? 0 : t % e.row_tiles) * TILE, vocab = job.v0 + x.index * TILE;
+        x.row = FEW ? vocab : rows;
+        x.col = FEW ? 0 : vocab;
         x.k0 = 0;
         x.k1 = (job.D + BK - 1) / BK;
     } else if (PRODUCT == GRAD_HIDDEN) {
         x.index = (int32_t)(t % job.d_tiles);
         const int32_t u = (int32_t)(t / job.d_tiles);
-        x.row = (u % row_tiles) * TILE;
-        x.split = u / row_tiles;
-        x.col = x.index * TILE;
+        x.split = u / e.row_tiles;
+        x.row = FEW ? x.index * TILE : (u % e.row_tiles) * TILE;
+        x.col = FEW ? 0 : x.index * TILE;
         const int32_t steps = (job.columns + BK - 1) / BK;
-        x.k0 = (int32_t)((int64_t)steps * x.split / job.splits);
-        x.k1 = (int32_t)((int64_t)steps * (x.split + 1) / job.splits);
+        x.k0 = (int32_t)((int64_t)steps * x.split / e.splits);
+        x.k1 = (int32_t)((int64_t)steps * (x.split + 1) / e.splits);
     } else {
         x.index = (int32_t)(t % job.d_tiles);
         x.row = (int32_t)(t / job.d_tiles) * TILE;
         x.col = x.index * TILE;
         x.k0 = 0;
-        x.k1 = max(1, (live + BK - 1) / BK);    // no live row: one step over rows of zeros
+        x.k1 = max(1, (e.live + BK - 1) / BK);    // no live row: one step over rows of zeros
     }
     return x;
 }
 
-// Persistent: one CTA per SM, pair p takes tiles p, p + pairs, ...  Warp 0 keeps the operand ring full, one thread of
-// the leader's warp 1 issues the products into one of two accumulators, warps 2..5 read the other one out.
+// ---- epilogues: one warp, 32 rows of the tile's accumulator (its Tensor Memory lanes), half of the columns --------
+// Loads run one step ahead of the arithmetic.
+template <int CHUNKS, int WIDTH, typename F>
+__device__ __forceinline__ void for_chunks(uint32_t src, F &&f)
+{
+    uint32_t w[2][WIDTH];
+    tmem_load(src, w[0]);
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+        tmem_wait(w[i & 1]);
+        if (i + 1 < CHUNKS) tmem_load(src + (i + 1) * WIDTH, w[(i + 1) & 1]);
+        f(i * WIDTH, w[i & 1]);
+    }
+}
+
+// rows: tokens, columns: vocabulary
 template <int PRODUCT, bool BF16>
+__device__ __forceinline__ void epilogue_many(const ProductJob &job, const Extent &e, const Tile &x, uint32_t src, int32_t in_tile, int half)
+{
+    constexpr int COLS = TILE / 2;
+    const int32_t row = x.row + in_tile;                     // a live row, or for GRAD_WEIGHT an entry of the piece
+    const int32_t first = half * COLS;                       // this warp's columns of the tile
+    src += first;
+    [[maybe_unused]] unsigned int *flags = &job.rows.header->error_flags;
+    if (PRODUCT == LOGITS_SUM) {
+        const int32_t left = min(TILE, job.V - x.col) - first;   // columns that exist
+        const int32_t at = job.rows.token[row] - x.col - first;  // padded rows hold a negative token
+        float top = -INFINITY, sum = 0.0f, mine = 0.0f;
+        for_chunks<COLS / 32, 32>(src, [&](int c, uint32_t (&w)[32]) {
+            if (c >= left) return;
+            if (c + 32 > left) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (c + j >= left) w[j] = 0xff800000u;
+            }
+            float hi = __uint_as_float(w[0]), hi2 = __uint_as_float(w[1]);
+#pragma unroll
+            for (int j = 2; j < 32; j += 2) {
+                hi = fmaxf(hi, __uint_as_float(w[j]));
+                hi2 = fmaxf(hi2, __uint_as_float(w[j + 1]));
+            }
+            const float next = fmaxf(top, fmaxf(hi, hi2) * job.scale);
+            float add = 0.0f, add2 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+                add += ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -next));
+                add2 += ex2_approx(fmaf(__uint_as_float(w[j + 1]), job.scale, -next));
+            }
+            sum = fmaf(sum, ex2_approx(top - next), add + add2);
+            top = next;
+            if (at >= c && at < c + 32) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (at == c + j) mine = __uint_as_float(w[j]);
+            }
+        });
+        if (row < e.live && PPOW_CHECK(2 * x.index + half < job.parts, 502, flags)) {
+            job.partial[(size_t)row * job.parts + 2 * x.index + half] = make_float2(top, sum);
+            if (at >= 0 && at < min(left, COLS)) job.at_token[row] = mine;
+        }
+    } else if (PRODUCT == LOGITS_GRAD) {
+        const int32_t left = min(TILE, job.V - x.col) - first;
+        const int32_t at = job.rows.token[row] - x.col - first;
+        const float mult = job.rows.mult[row], lse2 = job.rows.lse2[row];
+        uint16_t *to = job.dz + (size_t)row * job.piece + x.index * TILE + first;
+        for_chunks<COLS / 32, 32>(src, [&](int c, uint32_t (&w)[32]) {
+            float p[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) p[j] = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -lse2));
+            if (at >= c && at < c + 32) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (at == c + j) p[j] -= 1.0f;
+            }
+            if (row >= e.live || c + 32 > left) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (row >= e.live || c + j >= left) p[j] = 0.0f;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t o[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = pack2<BF16>(p[16 * h + 2 * j] * mult, p[16 * h + 2 * j + 1] * mult);
+                if (PPOW_CHECK(x.index * TILE + first + c + 16 * h + 16 <= job.piece, 503, flags)) store32(to + c + 16 * h, o);
+            }
+        });
+    } else if (PRODUCT == GRAD_HIDDEN) {
+        float *to = job.grad_rows + ((size_t)x.split * e.row_tiles * TILE + row) * job.D + x.col + first;
+        const int32_t left = min(TILE, job.D - x.col) - first;   // a multiple of 8
+        const bool none = x.k0 == x.k1;                          // more shares than steps: nothing was multiplied
+        for_chunks<COLS / 32, 32>(src, [&](int c, uint32_t (&w)[32]) {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                if (c + 8 * h < left && row < e.live && PPOW_CHECK(x.split < e.splits, 504, flags)) {
+                    uint32_t o[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) o[j] = none ? 0u : w[8 * h + j];
+                    if (job.add) {
+                        const float4 *old = reinterpret_cast<const float4 *>(to + c + 8 * h);
+                        const float4 p = old[0], q = old[1];
+                        const float f[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) + f[j]);
+                    }
+                    store32(to + c + 8 * h, o);
+                }
+            }
+        });
+    } else {
+        const int32_t left = min(TILE, job.D - x.col) - first;
+        const float out_scale = job.rows.header->out_scale;
+        uint16_t *to = job.grad_weight + (size_t)(job.v0 + row) * job.D + x.col + first;
+        const bool mine = row < job.columns && PPOW_CHECK(job.v0 + min(row, job.columns - 1) < job.V, 505, flags);
+        for_chunks<COLS / 32, 32>(src, [&](int c, uint32_t (&w)[32]) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t o[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    o[j] = pack2<BF16>(__uint_as_float(w[16 * h + 2 * j]) * out_scale, __uint_as_float(w[16 * h + 2 * j + 1]) * out_scale);
+                if (!mine) continue;
+                if (job.wide_rows) {
+                    if (c + 16 * h < left) store32(to + c + 16 * h, o);
+                } else {
+                    if (c + 16 * h < left) *reinterpret_cast<uint4 *>(to + c + 16 * h) = make_uint4(o[0], o[1], o[2], o[3]);
+                    if (c + 16 * h + 8 < left) *reinterpret_cast<uint4 *>(to + c + 16 * h + 8) = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+            }
+        });
+    }
+}
+
+// rows: the vocabulary's entries, for GRAD_HIDDEN the width's; columns: tokens.  Sums over the rows run across the lanes.
+template <int PRODUCT, bool BF16, int N>
+__device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent &e, const Tile &x, uint32_t src, int32_t in_tile, int half)
+{
+    constexpr int COLS = N / 2, WIDTH = COLS < 32 ? COLS : 32;
+    const int lane = threadIdx.x & 31;
+    const int32_t row = x.row + in_tile, first = half * COLS;
+    src += first;
+    [[maybe_unused]] unsigned int *flags = &job.rows.header->error_flags;
+    if (PRODUCT == LOGITS_SUM) {
+        const bool inside = row < job.V;
+        const int32_t part = x.index * 8 + in_tile / 32;
+        for_chunks<COLS / WIDTH, WIDTH>(src, [&](int c, uint32_t (&w)[WIDTH]) {
+            if (first + c >= e.live) return;
+            float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < WIDTH; ++j) {
+                const float v = inside ? __uint_as_float(w[j]) * job.scale : -INFINITY;
+                const float hi = warp_max(v);
+                float s = hi > -INFINITY ? ex2_approx(v - hi) : 0.0f;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                if (lane == j) top = hi, sum = s;
+                const int32_t token = first + c + j;
+                if (inside && token < e.live && job.rows.token[token] == row) job.at_token[token] = __uint_as_float(w[j]);
+            }
+            const int32_t token = first + c + lane;
+            if (lane < WIDTH && token < e.live && PPOW_CHECK(part < job.parts, 506, flags))
+                job.partial[(size_t)token * job.parts + part] = make_float2(top, sum);
+        });
+    } else if (PRODUCT == LOGITS_GRAD) {
+        const bool inside = row < job.V;
+        uint16_t *to = job.dz + x.index * TILE + in_tile;
+        for_chunks<COLS / WIDTH, WIDTH>(src, [&](int c, uint32_t (&w)[WIDTH]) {
+#pragma unroll
+            for (int j = 0; j < WIDTH; ++j) {
+                const int32_t token = first + c + j;
+                float d = 0.0f;
+                if (inside && token < e.live) {
+                    d = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -job.rows.lse2[token]));
+                    if (job.rows.token[token] == row) d -= 1.0f;
+                    d *= job.rows.mult[token];
+                }
+                if (PPOW_CHECK(x.index * TILE + in_tile < job.piece, 507, flags)) to[(size_t)token * job.piece] = (uint16_t)pack2<BF16>(d, 0.0f);
+            }
+        });
+    } else {
+        float *to = job.grad_rows + (size_t)x.split * N * job.D + row;
+        const bool inside = row < job.D, none = x.k0 == x.k1;
+        for_chunks<COLS / WIDTH, WIDTH>(src, [&](int c, uint32_t (&w)[WIDTH]) {
+#pragma unroll
+            for (int j = 0; j < WIDTH; ++j) {
+                const int32_t token = first + c + j;
+                if (inside && token < e.live && PPOW_CHECK(x.split < e.splits, 508, flags)) {
+                    float *p = to + (size_t)token * job.D;
+                    const float v = none ? 0.0f : __uint_as_float(w[j]);
+                    *p = job.add ? *p + v : v;
+                }
+            }
+        });
+    }
+}
+
+// Persistent: one CTA per SM, pair p takes tiles p, p + pairs, ...  Warp 0 keeps the operand ring full, one thread of
+// the leader's warp 1 issues the products into one of two accumulators, warps 2..9 read the other one out.
+template <int PRODUCT, bool BF16, int N>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     head_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductJob job)
 {
-    constexpr bool A_K = PRODUCT != GRAD_WEIGHT;                                // the inner axis is contiguous in A
-    constexpr bool B_K = PRODUCT == LOGITS_SUM || PRODUCT == LOGITS_GRAD;
-    constexpr uint32_t INSTRUCTION = mma_instruction(BF16, A_K, B_K, TILE, TILE);
-    constexpr uint32_t BLOCK_BYTES = BK * 128;                                  // 64 wide x BK rows
+    constexpr bool FEW = N < TILE;
+    constexpr bool A_K = FEW ? PRODUCT != GRAD_HIDDEN : PRODUCT != GRAD_WEIGHT;     // the inner axis is contiguous in A
+    constexpr bool B_K = FEW || PRODUCT == LOGITS_SUM || PRODUCT == LOGITS_GRAD;
+    constexpr uint32_t INSTRUCTION = mma_instruction(BF16, A_K, B_K, TILE, N);
+    constexpr uint32_t BLOCK_BYTES = BK * 128;                                      // 64 wide x BK rows
+    constexpr uint32_t STAGES = stage_count<N>(), STAGE_BYTES = stage_bytes<N>();
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -334,7 +565,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
         }
         for (uint32_t b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
-            mbar_init(acc_empty(b), 8);     // four epilogue warps of each CTA
+            mbar_init(acc_empty(b), 16);     // eight epilogue warps of each CTA
         }
         mbar_init_fence();
     }
@@ -345,38 +576,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     tcgen05_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
+    allow_next_kernel();
+    wait_for_previous_kernel();
 
-    const int32_t live = header->live;
-    int32_t row_tiles = (live + TILE - 1) / TILE;
-    if (PRODUCT != LOGITS_SUM) row_tiles = max(1, row_tiles);
-    const int64_t tiles = tile_count<PRODUCT>(job, row_tiles);
+    Extent e;
+    e.live = header->live;
+    e.row_tiles = (e.live + TILE - 1) / TILE;
+    if (FEW || PRODUCT != LOGITS_SUM) e.row_tiles = max(1, e.row_tiles);
+    e.splits = PRODUCT == GRAD_HIDDEN ? header->splits : 1;
+    const int64_t tiles = tile_count<PRODUCT>(job, e);
 
     if (warp == 0) {
         if (lane == 0) {
             uint32_t it = 0;
             bool ok = true;
             for (int64_t t = pair; t < tiles && ok; t += pairs) {
-                const Tile x = tile_at<PRODUCT>(job, row_tiles, live, t);
+                const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
                 for (int32_t k = x.k0; k < x.k1 && ok; ++k, ++it) {
                     const uint32_t s = it % STAGES, phase = (it / STAGES) & 1u;
                     ok = mbar_wait_ns(empty(s), phase ^ 1u);
                     if (!ok) break;
                     if (rank == 0) mbar_arrive_expect_tx(full(s), 2 * STAGE_BYTES);
                     const uint32_t bar = peer_addr(full(s), 0);
-                    const uint32_t a = smem + s * STAGE_BYTES, b = a + OPERAND_BYTES;
-                    const int32_t m = x.row + (int32_t)rank * HALF_TILE, n = x.col + (int32_t)rank * HALF_TILE;
+                    const uint32_t a = smem + s * STAGE_BYTES, b = a + A_BYTES;
+                    const int32_t m = x.row + (int32_t)rank * HALF_TILE, n = x.col + (int32_t)rank * (N / 2);
+                    // the vocabulary is the inner axis of dh: its coordinate in W starts at the piece
+                    const int32_t k_weight = k * BK + (PRODUCT == GRAD_HIDDEN ? job.v0 : 0);
                     if (A_K) {
                         tma_load_pair(a, &map_a, k * BK, m, bar);
                     } else {
-                        tma_load_pair(a, &map_a, m, k * BK, bar);
-                        tma_load_pair(a + BLOCK_BYTES, &map_a, m + 64, k * BK, bar);
+                        tma_load_pair(a, &map_a, m, k_weight, bar);
+                        tma_load_pair(a + BLOCK_BYTES, &map_a, m + 64, k_weight, bar);
                     }
                     if (B_K) {
                         tma_load_pair(b, &map_b, k * BK, n, bar);
                     } else {
-                        const int32_t y = k * BK + (PRODUCT == GRAD_HIDDEN ? job.v0 : 0);
-                        tma_load_pair(b, &map_b, n, y, bar);
-                        tma_load_pair(b + BLOCK_BYTES, &map_b, n + 64, y, bar);
+                        tma_load_pair(b, &map_b, n, k_weight, bar);
+                        tma_load_pair(b + BLOCK_BYTES, &map_b, n + 64, k_weight, bar);
                     }
                 }
             }
@@ -389,7 +625,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
             uint32_t it = 0, acc = 0;
             bool ok = true;
             for (int64_t t = pair; t < tiles && ok; t += pairs, ++acc) {
-                const Tile x = tile_at<PRODUCT>(job, row_tiles, live, t);
+                const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
                 const uint32_t b = acc & 1u, d = tmem + b * TILE;
                 ok = mbar_wait_ns(acc_empty(b), ((acc >> 1) & 1u) ^ 1u);
                 tcgen05_fence_after();
@@ -399,7 +635,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                     if (!ok) break;
                     tcgen05_fence_after();
                     const uint32_t a = smem + s * STAGE_BYTES;
-                    const uint64_t da = operand_descriptor(a, A_K, BLOCK_BYTES), db = operand_descriptor(a + OPERAND_BYTES, B_K, BLOCK_BYTES);
+                    const uint64_t da = operand_descriptor(a, A_K, BLOCK_BYTES), db = operand_descriptor(a + A_BYTES, B_K, BLOCK_BYTES);
 #pragma unroll
                     for (int q = 0; q < BK / 16; ++q)
                         mma_pair(d, da + (uint64_t)(q * (A_K ? 32 : 2048) >> 4), db + (uint64_t)(q * (B_K ? 32 : 2048) >> 4), INSTRUCTION,
@@ -412,124 +648,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
         }
     } else {
         const uint32_t quarter = warp & 3;                       // the 32 Tensor Memory lanes that this warp may read
+        const int half = (warp - 2) >> 2;
         const int32_t in_tile = (int32_t)(rank * HALF_TILE + quarter * 32 + lane);
         uint32_t acc = 0;
         bool ok = true;
         for (int64_t t = pair; t < tiles; t += pairs, ++acc) {
-            const Tile x = tile_at<PRODUCT>(job, row_tiles, live, t);
+            const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
             const uint32_t b = acc & 1u;
             ok = __all_sync(0xffffffffu, mbar_wait_ns(acc_full(b), (acc >> 1) & 1u));
             if (!ok) break;
             tcgen05_fence_after();
             const uint32_t src = tmem + b * TILE + (quarter * 32u << 16);
-            const int32_t row = x.row + in_tile;                 // a live row, or for GRAD_WEIGHT an entry of the piece
-            uint32_t w[32];
-            if (PRODUCT == LOGITS_SUM) {
-                const int32_t left = min(TILE, job.V - x.col);   // columns that exist
-                const int32_t at = job.rows.token[row] - x.col;  // padded rows hold -1
-                float top = -INFINITY, sum = 0.0f, mine = 0.0f;
-                for (int32_t c = 0; c < left; c += 32) {
-                    tmem_load32(src + c, w);
-                    tmem_wait_load32(w);
-                    if (c + 32 > left) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (c + j >= left) w[j] = 0xff800000u;
-                    }
-                    float hi = __uint_as_float(w[0]);
-#pragma unroll
-                    for (int j = 1; j < 32; ++j) hi = fmaxf(hi, __uint_as_float(w[j]));
-                    const float next = fmaxf(top, hi * job.scale);
-                    float add = 0.0f, add2 = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        add += ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -next));
-                        add2 += ex2_approx(fmaf(__uint_as_float(w[j + 1]), job.scale, -next));
-                    }
-                    sum = fmaf(sum, ex2_approx(top - next), add + add2);
-                    top = next;
-                    if (at >= c && at < c + 32) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (at == c + j) mine = __uint_as_float(w[j]);
-                    }
-                }
-                if (row < live && PPOW_CHECK(x.index < job.v_tiles, 502, &header->error_flags)) {
-                    job.partial[(size_t)row * job.v_tiles + x.index] = make_float2(top, sum);
-                    if (at >= 0 && at < left) job.at_token[row] = mine;
-                }
-            } else if (PRODUCT == LOGITS_GRAD) {
-                const int32_t left = min(TILE, job.V - x.col);
-                const int32_t at = job.rows.token[row] - x.col;
-                const float mult = job.rows.mult[row], lse2 = job.rows.lse2[row];
-                uint16_t *to = job.dz + (size_t)row * job.piece + x.index * TILE;
-                for (int32_t c = 0; c < TILE; c += 32) {
-                    tmem_load32(src + c, w);
-                    tmem_wait_load32(w);
-                    float p[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) p[j] = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -lse2));
-                    if (at >= c && at < c + 32) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (at == c + j) p[j] -= 1.0f;
-                    }
-                    if (row >= live || c + 32 > left) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (row >= live || c + j >= left) p[j] = 0.0f;
-                    }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t o[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) o[j] = pack2<BF16>(p[16 * h + 2 * j] * mult, p[16 * h + 2 * j + 1] * mult);
-                        if (PPOW_CHECK(x.index * TILE + c + 16 * h + 16 <= job.piece, 503, &header->error_flags)) store32(to + c + 16 * h, o);
-                    }
-                }
-            } else if (PRODUCT == GRAD_HIDDEN) {
-                float *to = job.grad_rows + x.split * job.split_stride + (size_t)row * job.D + x.col;
-                const int32_t left = min(TILE, job.D - x.col);   // a multiple of 8
-                const bool none = x.k0 == x.k1;                  // more shares than steps: nothing was multiplied
-                for (int32_t c = 0; c < left; c += 32) {
-                    tmem_load32(src + c, w);
-                    tmem_wait_load32(w);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        if (c + 8 * h < left && row < live && PPOW_CHECK(x.split < job.splits, 504, &header->error_flags)) {
-                            uint32_t o[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) o[j] = none ? 0u : w[8 * h + j];
-                            if (job.add) {
-                                const float4 *old = reinterpret_cast<const float4 *>(to + c + 8 * h);
-                                const float4 p = old[0], q = old[1];
-                                const float f[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) + f[j]);
-                            }
-                            store32(to + c + 8 * h, o);
-                        }
-                    }
-                }
-            } else {
-                const int32_t left = min(TILE, job.D - x.col);
-                const float out_scale = header->out_scale;
-                uint16_t *to = job.grad_weight + (size_t)(job.v0 + row) * job.D + x.col;
-                for (int32_t c = 0; c < left; c += 32) {
-                    tmem_load32(src + c, w);
-                    tmem_wait_load32(w);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        if (c + 8 * h < left && row < job.columns && PPOW_CHECK(job.v0 + row < job.V, 505, &header->error_flags)) {
-                            uint32_t o[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                o[j] = pack2<BF16>(__uint_as_float(w[8 * h + 2 * j]) * out_scale, __uint_as_float(w[8 * h + 2 * j + 1]) * out_scale);
-                            *reinterpret_cast<uint4 *>(to + c + 8 * h) = make_uint4(o[0], o[1], o[2], o[3]);
-                        }
-                    }
-                }
-            }
+            if constexpr (FEW)
+                epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half);
+            else
+                epilogue_many<PRODUCT, BF16>(job, e, x, src, in_tile, half);
             tcgen05_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(peer_addr(acc_empty(b), 0));
@@ -549,18 +682,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
 // ---- merge: one warp per live row -------------------------------------------------------------------
 constexpr int MERGE_THREADS = 128;
 __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows, const float2 *__restrict__ partial,
-                                                                   const float *__restrict__ at_token, int32_t v_tiles, int32_t V,
+                                                                   const float *__restrict__ at_token, int32_t parts, int32_t V,
                                                                    float scale, float *__restrict__ logp, float *__restrict__ lse)
 {
     const int lane = threadIdx.x & 31;
     const int32_t row = (int32_t)((blockIdx.x * (unsigned)MERGE_THREADS + threadIdx.x) >> 5);
+    wait_for_previous_kernel();
     if (row >= rows.header->live) return;
-    const float2 *p = partial + (size_t)row * v_tiles;
+    const float2 *p = partial + (size_t)row * parts;
     float top = -INFINITY;
-    for (int32_t i = lane; i < v_tiles; i += 32) top = fmaxf(top, p[i].x);
+    for (int32_t i = lane; i < parts; i += 32) top = fmaxf(top, p[i].x);
     top = warp_max(top);
     double sum = 0.0;
-    for (int32_t i = lane; i < v_tiles; i += 32) sum += (double)p[i].y * (double)ex2_approx(p[i].x - top);
+    for (int32_t i = lane; i < parts; i += 32) sum += (double)p[i].y * (double)ex2_approx(p[i].x - top);
     sum = warp_sum_f64(sum);
     if (lane == 0) {
         const double lse2 = (double)top + log2(sum);
@@ -574,10 +708,12 @@ __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows
 // ---- finish: dh of the live rows, rounded once ------------------------------------------------------
 constexpr int FINISH_THREADS = 256;
 template <bool BF16>
-__global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows rows, const float *__restrict__ parts, int32_t splits,
-                                                                     size_t split_stride, int32_t D, uint16_t *__restrict__ grad_hidden)
+__global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows rows, const float *__restrict__ parts, int32_t few,
+                                                                     int32_t D, uint16_t *__restrict__ grad_hidden)
 {
-    const int32_t units = D / 8;
+    wait_for_previous_kernel();
+    const int32_t units = D / 8, splits = rows.header->splits;
+    const size_t split_stride = (size_t)(few ? few : (rows.header->live + TILE - 1) / TILE * TILE) * D;
     const int64_t all = (int64_t)rows.header->live * units;
     for (int64_t i = (int64_t)blockIdx.x * FINISH_THREADS + threadIdx.x; i < all; i += (int64_t)gridDim.x * FINISH_THREADS) {
         const int32_t row = (int32_t)(i / units), u = (int32_t)(i % units);
@@ -607,28 +743,14 @@ bool params_ok(const ppow_head_params *p)
     return true;
 }
 
+// Columns of a tile for this many tokens.  Up to 128 the tokens are the columns and W the rows: 8 tokens x 4096 x 128256
+// would spend as much on loading and multiplying 256 rows, 248 of them zeros, as W takes to come from HBM.
+int32_t tile_columns(int32_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : TILE; }
+
 struct Layout {
     size_t source, token, mult, lse2, row_scale, rows, scaled, partial, at_token, dz, grad_rows, total;
-    size_t split_stride;
-    int32_t padded, v_tiles, d_tiles, piece, splits;
+    int32_t columns, few, padded, v_tiles, d_tiles, piece, parts;
 };
-
-// Shares of the inner axis for dh: tiles x shares should fill whole rounds of `74` pairs.  The count is a function of the
-// sizes alone, so that the workspace is too.
-int32_t split_count(int64_t tiles, int32_t steps)
-{
-    constexpr int64_t PAIRS = 74;
-    int32_t best = 1;
-    double best_cost = 1e30;
-    for (int32_t s = 1; s <= MAX_SPLIT && s * 8 <= steps; ++s) {
-        const double cost = (double)((tiles * s + PAIRS - 1) / PAIRS) / s * (1.0 + 0.02 * s);
-        if (cost < best_cost) {
-            best_cost = cost;
-            best = s;
-        }
-    }
-    return best;
-}
 
 Layout layout_of(const ppow_head_params *p, bool backward)
 {
@@ -639,8 +761,9 @@ Layout layout_of(const ppow_head_params *p, bool backward)
         off = (off + bytes + 255) & ~(size_t)255;
         return o;
     };
-    L.padded = (p->T + TILE - 1) / TILE * TILE;
-    if (L.padded < TILE) L.padded = TILE;
+    L.columns = tile_columns(p->T);
+    L.few = L.columns < TILE ? L.columns : 0;
+    L.padded = L.few ? L.few : (p->T + TILE - 1) / TILE * TILE;
     L.v_tiles = (p->V + TILE - 1) / TILE;
     L.d_tiles = (p->D + TILE - 1) / TILE;
     const size_t rows = (size_t)L.padded;
@@ -651,7 +774,8 @@ Layout layout_of(const ppow_head_params *p, bool backward)
     L.row_scale = take(rows * 4);
     L.rows = take(rows * p->D * 2);
     if (!backward) {
-        L.partial = take(rows * L.v_tiles * sizeof(float2));
+        L.parts = L.v_tiles * (L.few ? 8 : 2);
+        L.partial = take(rows * L.parts * sizeof(float2));
         L.at_token = take(rows * 4);
     } else {
         if (p->dtype == PPOW_F16) L.scaled = take(rows * p->D * 2);
@@ -661,9 +785,10 @@ Layout layout_of(const ppow_head_params *p, bool backward)
         const int32_t pieces = (L.v_tiles + fit - 1) / fit;
         L.piece = (L.v_tiles + pieces - 1) / pieces * TILE;        // pieces of nearly the same length
         L.dz = take(rows * L.piece * 2);
-        L.splits = split_count((int64_t)(L.padded / TILE) * L.d_tiles, L.piece / BK);
-        L.split_stride = rows * p->D;
-        L.grad_rows = take(L.splits * L.split_stride * 4);
+        // sums of dh: all rows once, or as many shares as SPLIT_TILES allows
+        size_t sums = rows, split = (size_t)(SPLIT_TILES / L.d_tiles) * (L.few ? L.few : TILE);
+        if (split > sums) sums = split;
+        L.grad_rows = take(sums * p->D * 4);
     }
     L.total = off;
     return L;
@@ -700,9 +825,15 @@ bool make_map(CUtensorMap *map, const void *base, bool bf16, int64_t width, int6
 
 // Pairs of SMs of the current device, asked once per device; the kernels' shared-memory limit is raised at the same time.
 constexpr int DEVICES = 64;
-template <int PRODUCT, bool BF16> bool allow_smem()
+template <int PRODUCT, bool BF16, int N> bool allow_smem()
 {
-    return cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MMA_SMEM) == cudaSuccess;
+    return cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)mma_smem<N>()) ==
+           cudaSuccess;
+}
+template <int PRODUCT, bool BF16> bool allow_smem_few()
+{
+    return allow_smem<PRODUCT, BF16, 16>() && allow_smem<PRODUCT, BF16, 32>() && allow_smem<PRODUCT, BF16, 64>() &&
+           allow_smem<PRODUCT, BF16, 128>() && allow_smem<PRODUCT, BF16, TILE>();
 }
 template <bool BF16> int pair_count()
 {
@@ -711,20 +842,33 @@ template <bool BF16> int pair_count()
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEVICES) return 0;
     int n = known[dev].load(std::memory_order_relaxed);
     if (n > 0) return n;
-    if (!allow_smem<LOGITS_SUM, BF16>() || !allow_smem<LOGITS_GRAD, BF16>() || !allow_smem<GRAD_HIDDEN, BF16>() ||
-        !allow_smem<GRAD_WEIGHT, BF16>() || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    if (!allow_smem_few<LOGITS_SUM, BF16>() || !allow_smem_few<LOGITS_GRAD, BF16>() || !allow_smem_few<GRAD_HIDDEN, BF16>() ||
+        !allow_smem<GRAD_WEIGHT, BF16, TILE>() || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return 0;
     n = sms / 2;
     known[dev].store(n, std::memory_order_relaxed);
     return n;
 }
 
-template <int PRODUCT, bool BF16>
-bool launch_product(const CUtensorMap &a, const CUtensorMap &b, const ProductJob &job, int64_t most_tiles, int pairs, cudaStream_t stream)
+template <int PRODUCT, bool BF16, int N>
+bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const ProductJob &job, int64_t most_tiles, int pairs, cudaStream_t stream)
 {
     const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
-    head_product_kernel<PRODUCT, BF16><<<2 * n, MMA_THREADS, MMA_SMEM, stream>>>(a, b, job);
-    return cudaGetLastError() == cudaSuccess;
+    return launch_after(head_product_kernel<PRODUCT, BF16, N>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, job);
+}
+
+// `rows` and `weight`: the operand maps of the token side and of W's side.  With few tokens the two change places.
+template <int PRODUCT, bool BF16>
+bool launch_product(const CUtensorMap &rows, const CUtensorMap &weight, const ProductJob &job, int32_t columns, int64_t most_tiles, int pairs,
+                    cudaStream_t stream)
+{
+    switch (columns) {
+    case 16: return launch_tiles<PRODUCT, BF16, 16>(weight, rows, job, most_tiles, pairs, stream);
+    case 32: return launch_tiles<PRODUCT, BF16, 32>(weight, rows, job, most_tiles, pairs, stream);
+    case 64: return launch_tiles<PRODUCT, BF16, 64>(weight, rows, job, most_tiles, pairs, stream);
+    case 128: return launch_tiles<PRODUCT, BF16, 128>(weight, rows, job, most_tiles, pairs, stream);
+    }
+    return launch_tiles<PRODUCT, BF16, TILE>(rows, weight, job, most_tiles, pairs, stream);
 }
 
 HeadRows rows_of(char *ws, const Layout &L)
@@ -750,12 +894,14 @@ bool launch_gather(const ppow_head_params *p, const Layout &L, const GatherJob &
     job.T = p->T;
     job.D = p->D;
     job.V = p->V;
+    job.few = L.few;
+    job.d_tiles = L.d_tiles;
+    job.piece_steps = L.piece / BK;
     job.inv_temperature = (float)(1.0 / (double)p->temperature);
     job.vec = (uintptr_t)hidden % 16 == 0 && p->hidden_stride % 8 == 0;
     job.hidden = (const uint16_t *)hidden;
-    // few rows per CTA, but at most about a thousand CTAs: each of them looks at all tokens
+    // a row per CTA, more where that would be over a thousand CTAs: each of them looks at all tokens
     job.rows_per_cta = (L.padded + GATHER_CTAS - 1) / GATHER_CTAS;
-    if (job.rows_per_cta < 8) job.rows_per_cta = 8;
     const unsigned grid = (unsigned)((L.padded + job.rows_per_cta - 1) / job.rows_per_cta);
     head_gather_kernel<BACKWARD, SCALED><<<grid, GATHER_THREADS, 0, stream>>>(job, rows);
     return cudaGetLastError() == cudaSuccess;
@@ -768,7 +914,7 @@ ppow_status forward(const ppow_head_params *p, const void *hidden, const void *w
     const Layout L = layout_of(p, false);
     const HeadRows rows = rows_of(ws, L);
     CUtensorMap map_rows, map_weight;
-    if (!make_map(&map_rows, rows.rows, BF16, p->D, L.padded, p->D, HALF_TILE) ||
+    if (!make_map(&map_rows, rows.rows, BF16, p->D, L.padded, p->D, L.columns / 2) ||
         !make_map(&map_weight, weight, BF16, p->D, p->V, p->weight_stride, HALF_TILE))
         return PPOW_ERR_CUDA;
     const int pairs = pair_count<BF16>();
@@ -785,13 +931,15 @@ ppow_status forward(const ppow_head_params *p, const void *hidden, const void *w
     job.V = job.columns = p->V;
     job.v_tiles = L.v_tiles;
     job.d_tiles = L.d_tiles;
+    job.parts = L.parts;
     job.partial = (float2 *)(ws + L.partial);
     job.at_token = (float *)(ws + L.at_token);
-    const int64_t tiles = (int64_t)(L.padded / TILE) * L.v_tiles;
-    if (!launch_product<LOGITS_SUM, BF16>(map_rows, map_weight, job, tiles, pairs, stream)) return PPOW_ERR_CUDA;
-    head_merge_kernel<<<(unsigned)((p->T * 32ll + MERGE_THREADS - 1) / MERGE_THREADS), MERGE_THREADS, 0, stream>>>(
-        rows, job.partial, job.at_token, L.v_tiles, p->V, job.scale, logp, lse);
-    return cudaGetLastError() == cudaSuccess ? PPOW_OK : PPOW_ERR_CUDA;
+    const int64_t tiles = (int64_t)((L.padded + TILE - 1) / TILE) * L.v_tiles;
+    if (!launch_product<LOGITS_SUM, BF16>(map_rows, map_weight, job, L.columns, tiles, pairs, stream)) return PPOW_ERR_CUDA;
+    const unsigned merge = (unsigned)((p->T * 32ll + MERGE_THREADS - 1) / MERGE_THREADS);
+    return launch_after(head_merge_kernel, merge, MERGE_THREADS, 0, stream, rows, job.partial, job.at_token, L.parts, p->V, job.scale, logp, lse)
+               ? PPOW_OK
+               : PPOW_ERR_CUDA;
 }
 
 template <bool BF16>
@@ -802,11 +950,11 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     const HeadRows rows = rows_of(ws, L);
     uint16_t *dz = (uint16_t *)(ws + L.dz);
     CUtensorMap map_rows, map_rows_t, map_weight, map_weight_t, map_dz, map_dz_t;
-    if (!make_map(&map_rows, rows.rows, BF16, p->D, L.padded, p->D, HALF_TILE) ||
+    if (!make_map(&map_rows, rows.rows, BF16, p->D, L.padded, p->D, L.columns / 2) ||
         !make_map(&map_rows_t, BF16 ? rows.rows : rows.scaled, BF16, p->D, L.padded, p->D, BK) ||
         !make_map(&map_weight, weight, BF16, p->D, p->V, p->weight_stride, HALF_TILE) ||
         !make_map(&map_weight_t, weight, BF16, p->D, p->V, p->weight_stride, BK) ||
-        !make_map(&map_dz, dz, BF16, L.piece, L.padded, L.piece, HALF_TILE) || !make_map(&map_dz_t, dz, BF16, L.piece, L.padded, L.piece, BK))
+        !make_map(&map_dz, dz, BF16, L.piece, L.padded, L.piece, L.columns / 2) || !make_map(&map_dz_t, dz, BF16, L.piece, L.padded, L.piece, BK))
         return PPOW_ERR_CUDA;
     const int pairs = pair_count<BF16>();
     if (pairs < 1) return PPOW_ERR_CUDA;
@@ -822,31 +970,28 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     job.D = p->D;
     job.V = p->V;
     job.d_tiles = L.d_tiles;
-    job.splits = L.splits;
     job.piece = L.piece;
+    job.wide_rows = p->D % 16 == 0 && (uintptr_t)grad_weight % 32 == 0;
     job.dz = dz;
     job.grad_rows = (float *)(ws + L.grad_rows);
-    job.split_stride = L.split_stride;
     job.grad_weight = (uint16_t *)grad_weight;
-    const int64_t row_tiles = L.padded / TILE;
+    const int64_t row_tiles = (L.padded + TILE - 1) / TILE;
     for (int64_t v0 = 0; v0 < p->V; v0 += L.piece) {
         job.v0 = (int32_t)v0;
         job.columns = (int32_t)(p->V - v0 < L.piece ? p->V - v0 : L.piece);
         job.v_tiles = (job.columns + TILE - 1) / TILE;
         job.add = v0 > 0;
-        if (!launch_product<LOGITS_GRAD, BF16>(map_rows, map_weight, job, row_tiles * job.v_tiles, pairs, stream)) return PPOW_ERR_CUDA;
-        if (grad_hidden &&
-            !launch_product<GRAD_HIDDEN, BF16>(map_dz, map_weight_t, job, row_tiles * L.d_tiles * L.splits, pairs, stream))
+        if (!launch_product<LOGITS_GRAD, BF16>(map_rows, map_weight, job, L.columns, row_tiles * job.v_tiles, pairs, stream))
             return PPOW_ERR_CUDA;
-        if (grad_weight &&
-            !launch_product<GRAD_WEIGHT, BF16>(map_dz_t, map_rows_t, job, (int64_t)job.v_tiles * L.d_tiles, pairs, stream))
+        if (grad_hidden && !launch_product<GRAD_HIDDEN, BF16>(map_dz, map_weight_t, job, L.columns, pairs, pairs, stream)) return PPOW_ERR_CUDA;
+        if (grad_weight && !launch_tiles<GRAD_WEIGHT, BF16, TILE>(map_dz_t, map_rows_t, job, (int64_t)job.v_tiles * L.d_tiles, pairs, stream))
             return PPOW_ERR_CUDA;
     }
     if (grad_hidden) {
         const int64_t blocks = ((int64_t)p->T * (p->D / 8) + FINISH_THREADS - 1) / FINISH_THREADS;
-        head_finish_kernel<BF16><<<(unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), FINISH_THREADS, 0, stream>>>(
-            rows, job.grad_rows, L.splits, L.split_stride, p->D, (uint16_t *)grad_hidden);
-        if (cudaGetLastError() != cudaSuccess) return PPOW_ERR_CUDA;
+        if (!launch_after(head_finish_kernel<BF16>, (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), FINISH_THREADS, 0, stream, rows,
+                          job.grad_rows, L.few, p->D, (uint16_t *)grad_hidden))
+            return PPOW_ERR_CUDA;
     }
     return PPOW_OK;
 }

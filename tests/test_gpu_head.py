@@ -121,7 +121,8 @@ def run(h, w, tok, grad, temperature=1.0):
 
 
 SHAPES = [(1, 2, 8), (1, 1000, 64), (7, 257, 72), (129, 256, 64), (255, 1001, 520), (256, 512, 64), (257, 300, 256),
-          (300, 4097, 136), (513, 1500, 1000), (31, 32000, 256)]
+          (300, 4097, 136), (513, 1500, 1000), (31, 32000, 256), (16, 777, 96), (17, 1001, 264), (64, 4099, 128), (65, 900, 1032),
+          (128, 2500, 328)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
