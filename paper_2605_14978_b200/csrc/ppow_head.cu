@@ -37,7 +37,12 @@ template <int N> __host__ __device__ constexpr int stage_count()
 {
     return N == 256 ? 6 : N == 128 ? 8 : N == 64 ? 10 : N == 32 ? 11 : 12;    // 192 to 204 KB
 }
-template <int N> __host__ __device__ constexpr size_t mma_smem() { return 1024 + (size_t)stage_count<N>() * stage_bytes<N>() + 256; }
+// Tiles of 16-bit results leave through shared memory: a box of 128 rows x 64 columns for each half of the columns.
+constexpr uint32_t BOX_BYTES = HALF_TILE * 128;
+template <int N> __host__ __device__ constexpr size_t mma_smem()
+{
+    return 1024 + (size_t)stage_count<N>() * stage_bytes<N>() + (N == 256 ? 2 * BOX_BYTES : 0) + 256;
+}
 
 constexpr int GATHER_THREADS = 256;
 constexpr int GATHER_ROWS_MAX = 1024, GATHER_CTAS = 1024;
@@ -118,6 +123,7 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
     __shared__ int32_t dest[GATHER_ROWS_MAX];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     allow_next_kernel();
+    wait_for_previous_kernel();
     const int32_t r0 = (int32_t)min((int64_t)blockIdx.x * job.rows_per_cta, (int64_t)job.T);
     const int32_t n = min(job.rows_per_cta, job.T - r0);
     auto live = [&](int32_t i) {
@@ -261,13 +267,11 @@ struct ProductJob {
     int32_t v_tiles, d_tiles;
     int32_t piece;          // row length of dz
     bool add;               // GRAD_HIDDEN: add to what the pieces before left
-    bool wide_rows;         // grad_weight: rows in whole 32-byte units
     int32_t parts;          // LOGITS_SUM: entries of `partial` per row
     float2 *partial;        // LOGITS_SUM: [live row][parts] maximum, sum (log2 units)
     float *at_token;        // LOGITS_SUM: the token's product, per live row
     uint16_t *dz;           // [padded rows][piece]
     float *grad_rows;       // GRAD_HIDDEN: [splits][padded live rows][D]
-    uint16_t *grad_weight;  // [V, D]
 };
 
 struct Tile {
@@ -334,23 +338,56 @@ __device__ __forceinline__ Tile tile_at(const ProductJob &job, const Extent &e, 
 }
 
 // ---- epilogues: one warp, 32 rows of the tile's accumulator (its Tensor Memory lanes), half of the columns --------
-// Loads run one step ahead of the arithmetic.
-template <int CHUNKS, int WIDTH, typename F>
-__device__ __forceinline__ void for_chunks(uint32_t src, F &&f)
+// Loads run one step ahead of the arithmetic; `release` hands the accumulator back as soon as the last one is in.
+template <int CHUNKS, int WIDTH, typename R, typename F>
+__device__ __forceinline__ void for_chunks(uint32_t src, R &&release, F &&f)
 {
     uint32_t w[2][WIDTH];
     tmem_load(src, w[0]);
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
         tmem_wait(w[i & 1]);
-        if (i + 1 < CHUNKS) tmem_load(src + (i + 1) * WIDTH, w[(i + 1) & 1]);
+        if (i + 1 < CHUNKS)
+            tmem_load(src + (i + 1) * WIDTH, w[(i + 1) & 1]);
+        else
+            release();
         f(i * WIDTH, w[i & 1]);
     }
 }
 
+// What a row's epilogue needs of its token, loaded before the tile is waited for.
+struct RowData {
+    int32_t token;
+    float mult, lse2;
+};
+
+// 32 columns (from column c of the half's 128) of the calling thread's row into the half's box, in the 128-byte swizzle: the
+// 16-byte unit i of row r sits at i ^ (r & 7), so that the 32 rows of a warp's store spread over all banks.  Every second
+// call the box is full and one thread hands it to the copy engine, at column x0 + 64 * (c / 64) and row y of `map`.
+__device__ __forceinline__ void put_box(uint32_t box, int32_t in_tile, int half, int c, const uint32_t (&o)[16], const CUtensorMap *map,
+                                        int32_t x0, int32_t y, bool inside)
+{
+    const uint32_t r = in_tile % HALF_TILE, threads = 128, id = 1 + half;
+    const bool first = r == 0;
+    const uint32_t row = box + half * BOX_BYTES + r * 128;
+    if (c % 64 == 0) {
+        if (first) tma_store_wait_read();
+        named_barrier(id, threads);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        store_shared16(row + ((((c % 64) / 8 + i) ^ (r & 7)) << 4), o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+    if (c % 64 == 32) {
+        fence_for_copy_engine();
+        named_barrier(id, threads);
+        if (first && inside) tma_store(map, box + half * BOX_BYTES, x0 + c / 64 * 64, y);
+    }
+}
+
 // rows: tokens, columns: vocabulary
-template <int PRODUCT, bool BF16>
-__device__ __forceinline__ void epilogue_many(const ProductJob &job, const Extent &e, const Tile &x, uint32_t src, int32_t in_tile, int half)
+template <int PRODUCT, bool BF16, typename R>
+__device__ __forceinline__ void epilogue_many(const ProductJob &job, const Extent &e, const Tile &x, const RowData &own, uint32_t src,
+                                              int32_t in_tile, int half, const CUtensorMap *map_out, uint32_t box, R &&release)
 {
     constexpr int COLS = TILE / 2;
     const int32_t row = x.row + in_tile;                     // a live row, or for GRAD_WEIGHT an entry of the piece
@@ -359,46 +396,51 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
     [[maybe_unused]] unsigned int *flags = &job.rows.header->error_flags;
     if (PRODUCT == LOGITS_SUM) {
         const int32_t left = min(TILE, job.V - x.col) - first;   // columns that exist
-        const int32_t at = job.rows.token[row] - x.col - first;  // padded rows hold a negative token
-        float top = -INFINITY, sum = 0.0f, mine = 0.0f;
-        for_chunks<COLS / 32, 32>(src, [&](int c, uint32_t (&w)[32]) {
-            if (c >= left) return;
-            if (c + 32 > left) {
+        const int32_t at = own.token - x.col - first;            // padded rows hold a negative token
+        // all 128 columns at once: one maximum, no rescaling, and the accumulator is free before the arithmetic starts
+        uint32_t w[COLS / 32][32];
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (c + j >= left) w[j] = 0xff800000u;
-            }
-            float hi = __uint_as_float(w[0]), hi2 = __uint_as_float(w[1]);
+        for (int i = 0; i < COLS / 32; ++i) tmem_load(src + 32 * i, w[i]);
 #pragma unroll
-            for (int j = 2; j < 32; j += 2) {
-                hi = fmaxf(hi, __uint_as_float(w[j]));
-                hi2 = fmaxf(hi2, __uint_as_float(w[j + 1]));
-            }
-            const float next = fmaxf(top, fmaxf(hi, hi2) * job.scale);
-            float add = 0.0f, add2 = 0.0f;
+        for (int i = 0; i < COLS / 32; ++i) tmem_wait(w[i]);
+        release();
+        if (left < COLS) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-                add += ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -next));
-                add2 += ex2_approx(fmaf(__uint_as_float(w[j + 1]), job.scale, -next));
-            }
-            sum = fmaf(sum, ex2_approx(top - next), add + add2);
-            top = next;
-            if (at >= c && at < c + 32) {
+            for (int j = 0; j < COLS; ++j)
+                if (j >= left) w[j / 32][j % 32] = 0xff800000u;
+        }
+        float hi[4];
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (at == c + j) mine = __uint_as_float(w[j]);
-            }
-        });
+        for (int j = 0; j < 4; ++j) hi[j] = __uint_as_float(w[0][j]);
+#pragma unroll
+        for (int j = 4; j < COLS; ++j) hi[j & 3] = fmaxf(hi[j & 3], __uint_as_float(w[j / 32][j % 32]));
+        const float most = fmaxf(fmaxf(hi[0], hi[1]), fmaxf(hi[2], hi[3]));
+        const float top = most * job.scale;
+        const float2 scale2 = make_float2(job.scale, job.scale), minus = make_float2(-top, -top);
+        float2 add[4] = {};
+#pragma unroll
+        for (int j = 0; j < COLS; j += 2) {
+            const float2 a = __ffma2_rn(make_float2(__uint_as_float(w[j / 32][j % 32]), __uint_as_float(w[j / 32][j % 32 + 1])), scale2, minus);
+            add[(j >> 1) & 3] = __fadd2_rn(add[(j >> 1) & 3], make_float2(ex2_approx(a.x), ex2_approx(a.y)));
+        }
+        const float2 s01 = __fadd2_rn(add[0], add[1]), s23 = __fadd2_rn(add[2], add[3]);
+        // a half that lies behind the vocabulary's end has no terms
+        const float sum = left > 0 ? (s01.x + s01.y) + (s23.x + s23.y) : 0.0f;
+        float mine = 0.0f;
+        if (at >= 0 && at < COLS) {
+#pragma unroll
+            for (int j = 0; j < COLS; ++j)
+                if (at == j) mine = __uint_as_float(w[j / 32][j % 32]);
+        }
         if (row < e.live && PPOW_CHECK(2 * x.index + half < job.parts, 502, flags)) {
             job.partial[(size_t)row * job.parts + 2 * x.index + half] = make_float2(top, sum);
             if (at >= 0 && at < min(left, COLS)) job.at_token[row] = mine;
         }
     } else if (PRODUCT == LOGITS_GRAD) {
         const int32_t left = min(TILE, job.V - x.col) - first;
-        const int32_t at = job.rows.token[row] - x.col - first;
-        const float mult = job.rows.mult[row], lse2 = job.rows.lse2[row];
-        uint16_t *to = job.dz + (size_t)row * job.piece + x.index * TILE + first;
-        for_chunks<COLS / 32, 32>(src, [&](int c, uint32_t (&w)[32]) {
+        const int32_t at = own.token - x.col - first;
+        const float mult = own.mult, lse2 = own.lse2;
+        for_chunks<COLS / 32, 32>(src, release, [&](int c, uint32_t (&w)[32]) {
             float p[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) p[j] = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -lse2));
@@ -412,19 +454,17 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
                 for (int j = 0; j < 32; ++j)
                     if (row >= e.live || c + j >= left) p[j] = 0.0f;
             }
+            uint32_t o[16];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t o[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = pack2<BF16>(p[16 * h + 2 * j] * mult, p[16 * h + 2 * j + 1] * mult);
-                if (PPOW_CHECK(x.index * TILE + first + c + 16 * h + 16 <= job.piece, 503, flags)) store32(to + c + 16 * h, o);
-            }
+            for (int j = 0; j < 16; ++j) o[j] = pack2<BF16>(p[2 * j] * mult, p[2 * j + 1] * mult);
+            put_box(box, in_tile, half, c, o, map_out, x.index * TILE + first, x.row + in_tile / HALF_TILE * HALF_TILE,
+                    PPOW_CHECK(x.index * TILE + first + c < job.piece, 503, flags));
         });
     } else if (PRODUCT == GRAD_HIDDEN) {
         float *to = job.grad_rows + ((size_t)x.split * e.row_tiles * TILE + row) * job.D + x.col + first;
         const int32_t left = min(TILE, job.D - x.col) - first;   // a multiple of 8
         const bool none = x.k0 == x.k1;                          // more shares than steps: nothing was multiplied
-        for_chunks<COLS / 32, 32>(src, [&](int c, uint32_t (&w)[32]) {
+        for_chunks<COLS / 32, 32>(src, release, [&](int c, uint32_t (&w)[32]) {
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 if (c + 8 * h < left && row < e.live && PPOW_CHECK(x.split < e.splits, 504, flags)) {
@@ -443,32 +483,43 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
             }
         });
     } else {
-        const int32_t left = min(TILE, job.D - x.col) - first;
         const float out_scale = job.rows.header->out_scale;
-        uint16_t *to = job.grad_weight + (size_t)(job.v0 + row) * job.D + x.col + first;
-        const bool mine = row < job.columns && PPOW_CHECK(job.v0 + min(row, job.columns - 1) < job.V, 505, flags);
-        for_chunks<COLS / 32, 32>(src, [&](int c, uint32_t (&w)[32]) {
+        const int32_t v = x.row + in_tile / HALF_TILE * HALF_TILE;       // the box's first row within the piece
+        for_chunks<COLS / 32, 32>(src, release, [&](int c, uint32_t (&w)[32]) {
+            uint32_t o[16];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t o[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    o[j] = pack2<BF16>(__uint_as_float(w[16 * h + 2 * j]) * out_scale, __uint_as_float(w[16 * h + 2 * j + 1]) * out_scale);
-                if (!mine) continue;
-                if (job.wide_rows) {
-                    if (c + 16 * h < left) store32(to + c + 16 * h, o);
-                } else {
-                    if (c + 16 * h < left) *reinterpret_cast<uint4 *>(to + c + 16 * h) = make_uint4(o[0], o[1], o[2], o[3]);
-                    if (c + 16 * h + 8 < left) *reinterpret_cast<uint4 *>(to + c + 16 * h + 8) = make_uint4(o[4], o[5], o[6], o[7]);
-                }
-            }
+            for (int j = 0; j < 16; ++j)
+                o[j] = pack2<BF16>(__uint_as_float(w[2 * j]) * out_scale, __uint_as_float(w[2 * j + 1]) * out_scale);
+            put_box(box, in_tile, half, c, o, map_out, x.col + first, job.v0 + v, x.col + first + (c & 64) < job.D && v < job.columns);
         });
     }
 }
 
+// Combines column j of the 32 lanes for every j: lane l ends with the result of column l % WIDTH in v[0].  Each step halves the
+// columns that a lane still carries (31 exchanges in all, not 5 for each column).
+template <int WIDTH, typename Op>
+__device__ __forceinline__ void across_lanes(float (&v)[WIDTH], Op op)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        if (o >= WIDTH) {
+#pragma unroll
+            for (int j = 0; j < WIDTH; ++j) v[j] = op(v[j], __shfl_xor_sync(0xffffffffu, v[j], o));
+        } else {
+#pragma unroll
+            for (int j = 0; j < o; ++j) {
+                const float give = lane & o ? v[j] : v[j + o], keep = lane & o ? v[j + o] : v[j];
+                v[j] = op(keep, __shfl_xor_sync(0xffffffffu, give, o));
+            }
+        }
+    }
+}
+
 // rows: the vocabulary's entries, for GRAD_HIDDEN the width's; columns: tokens.  Sums over the rows run across the lanes.
-template <int PRODUCT, bool BF16, int N>
-__device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent &e, const Tile &x, uint32_t src, int32_t in_tile, int half)
+template <int PRODUCT, bool BF16, int N, typename R>
+__device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent &e, const Tile &x, uint32_t src, int32_t in_tile, int half,
+                                             R &&release)
 {
     constexpr int COLS = N / 2, WIDTH = COLS < 32 ? COLS : 32;
     const int lane = threadIdx.x & 31;
@@ -478,17 +529,22 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
     if (PRODUCT == LOGITS_SUM) {
         const bool inside = row < job.V;
         const int32_t part = x.index * 8 + in_tile / 32;
-        for_chunks<COLS / WIDTH, WIDTH>(src, [&](int c, uint32_t (&w)[WIDTH]) {
+        for_chunks<COLS / WIDTH, WIDTH>(src, release, [&](int c, uint32_t (&w)[WIDTH]) {
             if (first + c >= e.live) return;
-            float top = -INFINITY, sum = 0.0f;
+            float v[WIDTH], r[WIDTH];
+#pragma unroll
+            for (int j = 0; j < WIDTH; ++j) r[j] = v[j] = inside ? __uint_as_float(w[j]) * job.scale : -INFINITY;
+            across_lanes<WIDTH>(r, [](float a, float b) { return fmaxf(a, b); });
+            const float top = r[0];                      // of column lane % WIDTH
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) {
-                const float v = inside ? __uint_as_float(w[j]) * job.scale : -INFINITY;
-                const float hi = warp_max(v);
-                float s = hi > -INFINITY ? ex2_approx(v - hi) : 0.0f;
+                const float hi = __shfl_sync(0xffffffffu, top, j);
+                r[j] = inside ? ex2_approx(v[j] - hi) : 0.0f;
+            }
+            across_lanes<WIDTH>(r, [](float a, float b) { return a + b; });
+            const float sum = r[0];
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (lane == j) top = hi, sum = s;
+            for (int j = 0; j < WIDTH; ++j) {
                 const int32_t token = first + c + j;
                 if (inside && token < e.live && job.rows.token[token] == row) job.at_token[token] = __uint_as_float(w[j]);
             }
@@ -499,7 +555,7 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
     } else if (PRODUCT == LOGITS_GRAD) {
         const bool inside = row < job.V;
         uint16_t *to = job.dz + x.index * TILE + in_tile;
-        for_chunks<COLS / WIDTH, WIDTH>(src, [&](int c, uint32_t (&w)[WIDTH]) {
+        for_chunks<COLS / WIDTH, WIDTH>(src, release, [&](int c, uint32_t (&w)[WIDTH]) {
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) {
                 const int32_t token = first + c + j;
@@ -515,7 +571,7 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
     } else {
         float *to = job.grad_rows + (size_t)x.split * N * job.D + row;
         const bool inside = row < job.D, none = x.k0 == x.k1;
-        for_chunks<COLS / WIDTH, WIDTH>(src, [&](int c, uint32_t (&w)[WIDTH]) {
+        for_chunks<COLS / WIDTH, WIDTH>(src, release, [&](int c, uint32_t (&w)[WIDTH]) {
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) {
                 const int32_t token = first + c + j;
@@ -533,7 +589,8 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
 // the leader's warp 1 issues the products into one of two accumulators, warps 2..9 read the other one out.
 template <int PRODUCT, bool BF16, int N>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
-    head_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ProductJob job)
+    head_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                        const __grid_constant__ CUtensorMap map_out, const ProductJob job)
 {
     constexpr bool FEW = N < TILE;
     constexpr bool A_K = FEW ? PRODUCT != GRAD_HIDDEN : PRODUCT != GRAD_WEIGHT;     // the inner axis is contiguous in A
@@ -544,7 +601,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
-    const uint32_t bars = smem + STAGES * STAGE_BYTES;
+    const uint32_t box = smem + STAGES * STAGE_BYTES, bars = box + (FEW ? 0 : 2 * BOX_BYTES);
     auto full = [&](uint32_t s) { return bars + 8 * s; };                       // the leader's count, for both CTAs
     auto empty = [&](uint32_t s) { return bars + 8 * (STAGES + s); };
     auto acc_full = [&](uint32_t b) { return bars + 8 * (2 * STAGES + b); };
@@ -655,18 +712,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
         for (int64_t t = pair; t < tiles; t += pairs, ++acc) {
             const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
             const uint32_t b = acc & 1u;
-            ok = __all_sync(0xffffffffu, mbar_wait_ns(acc_full(b), (acc >> 1) & 1u));
+            RowData own = {};
+            if (!FEW && (PRODUCT == LOGITS_SUM || PRODUCT == LOGITS_GRAD)) {
+                own.token = job.rows.token[x.row + in_tile];
+                if (PRODUCT == LOGITS_GRAD) {
+                    own.mult = job.rows.mult[x.row + in_tile];
+                    own.lse2 = job.rows.lse2[x.row + in_tile];
+                }
+            }
+            // all four warps of a half go on or none does: they meet at barriers further down
+            ok = named_barrier_all(1 + half, 128, mbar_wait_ns(acc_full(b), (acc >> 1) & 1u));
             if (!ok) break;
             tcgen05_fence_after();
             const uint32_t src = tmem + b * TILE + (quarter * 32u << 16);
+            auto release = [&] {
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(peer_addr(acc_empty(b), 0));
+            };
             if constexpr (FEW)
-                epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half);
+                epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half, release);
             else
-                epilogue_many<PRODUCT, BF16>(job, e, x, src, in_tile, half);
-            tcgen05_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(peer_addr(acc_empty(b), 0));
+                epilogue_many<PRODUCT, BF16>(job, e, x, own, src, in_tile, half, &map_out, box, release);
         }
+        if (!FEW && (PRODUCT == LOGITS_GRAD || PRODUCT == GRAD_WEIGHT) && in_tile % HALF_TILE == 0) tma_store_wait();
         if (!ok && lane == 0) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
     }
     __syncwarp();
@@ -679,24 +748,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     }
 }
 
-// ---- merge: one warp per live row -------------------------------------------------------------------
+// ---- merge: one CTA per live row ----------------------------------------------------------------------
 constexpr int MERGE_THREADS = 128;
 __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows, const float2 *__restrict__ partial,
                                                                    const float *__restrict__ at_token, int32_t parts, int32_t V,
                                                                    float scale, float *__restrict__ logp, float *__restrict__ lse)
 {
-    const int lane = threadIdx.x & 31;
-    const int32_t row = (int32_t)((blockIdx.x * (unsigned)MERGE_THREADS + threadIdx.x) >> 5);
+    constexpr int HELD = 16;                             // entries per thread that are read once; more are read twice
+    __shared__ float tops[MERGE_THREADS / 32];
+    __shared__ double sums[MERGE_THREADS / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int32_t row = blockIdx.x;
+    allow_next_kernel();
     wait_for_previous_kernel();
     if (row >= rows.header->live) return;
     const float2 *p = partial + (size_t)row * parts;
+    float2 held[HELD];
     float top = -INFINITY;
-    for (int32_t i = lane; i < parts; i += 32) top = fmaxf(top, p[i].x);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        const int32_t k = tid + i * MERGE_THREADS;
+        held[i] = k < parts ? p[k] : make_float2(-INFINITY, 0.0f);
+    }
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) top = fmaxf(top, held[i].x);
+#pragma unroll 8
+    for (int32_t k = tid + HELD * MERGE_THREADS; k < parts; k += MERGE_THREADS) top = fmaxf(top, p[k].x);
     top = warp_max(top);
+    if (lane == 0) tops[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MERGE_THREADS / 32; ++i) top = fmaxf(top, tops[i]);
     double sum = 0.0;
-    for (int32_t i = lane; i < parts; i += 32) sum += (double)p[i].y * (double)ex2_approx(p[i].x - top);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) sum += (double)(held[i].y * ex2_approx(held[i].x - top));
+#pragma unroll 8
+    for (int32_t k = tid + HELD * MERGE_THREADS; k < parts; k += MERGE_THREADS) sum += (double)(p[k].y * ex2_approx(p[k].x - top));
     sum = warp_sum_f64(sum);
-    if (lane == 0) {
+    if (lane == 0) sums[warp] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < MERGE_THREADS / 32; ++i) sum += sums[i];
         const double lse2 = (double)top + log2(sum);
         const int32_t r = rows.source[row], y = rows.token[row];
         const double ln2 = 0.69314718055994530942;
@@ -706,27 +800,35 @@ __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows
 }
 
 // ---- finish: dh of the live rows, rounded once ------------------------------------------------------
-constexpr int FINISH_THREADS = 256;
+constexpr int FINISH_THREADS = 128;
 template <bool BF16>
 __global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows rows, const float *__restrict__ parts, int32_t few,
                                                                      int32_t D, uint16_t *__restrict__ grad_hidden)
 {
+    allow_next_kernel();
     wait_for_previous_kernel();
-    const int32_t units = D / 8, splits = rows.header->splits;
-    const size_t split_stride = (size_t)(few ? few : (rows.header->live + TILE - 1) / TILE * TILE) * D;
-    const int64_t all = (int64_t)rows.header->live * units;
+    const int32_t units = D / 4, splits = rows.header->splits, live = rows.header->live;
+    const size_t split_units = (size_t)(few ? few : (live + TILE - 1) / TILE * TILE) * units;
+    const int64_t all = (int64_t)live * units;
     for (int64_t i = (int64_t)blockIdx.x * FINISH_THREADS + threadIdx.x; i < all; i += (int64_t)gridDim.x * FINISH_THREADS) {
         const int32_t row = (int32_t)(i / units), u = (int32_t)(i % units);
-        float f[8] = {};
-        for (int32_t s = 0; s < splits; ++s) {
-            const float4 *p = reinterpret_cast<const float4 *>(parts + s * split_stride + (size_t)row * D) + 2 * u;
-            const float4 a = __ldcs(p), b = __ldcs(p + 1);
-            f[0] += a.x, f[1] += a.y, f[2] += a.z, f[3] += a.w, f[4] += b.x, f[5] += b.y, f[6] += b.z, f[7] += b.w;
+        const float4 *p = reinterpret_cast<const float4 *>(parts) + i;
+        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        int32_t s = 0;
+        for (; s + 8 <= splits; s += 8) {
+            float4 a[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) a[j] = p[(s + j) * split_units];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f.x += a[j].x, f.y += a[j].y, f.z += a[j].z, f.w += a[j].w;
+        }
+        for (; s < splits; ++s) {
+            const float4 a = p[s * split_units];
+            f.x += a.x, f.y += a.y, f.z += a.z, f.w += a.w;
         }
         const float k = rows.row_scale[row];
-        reinterpret_cast<uint4 *>(grad_hidden + (size_t)rows.source[row] * D)[u] =
-            make_uint4(pack2<BF16>(f[0] * k, f[1] * k), pack2<BF16>(f[2] * k, f[3] * k), pack2<BF16>(f[4] * k, f[5] * k),
-                       pack2<BF16>(f[6] * k, f[7] * k));
+        reinterpret_cast<uint2 *>(grad_hidden + (size_t)rows.source[row] * D)[u] =
+            make_uint2(pack2<BF16>(f.x * k, f.y * k), pack2<BF16>(f.z * k, f.w * k));
     }
 }
 
@@ -851,24 +953,26 @@ template <bool BF16> int pair_count()
 }
 
 template <int PRODUCT, bool BF16, int N>
-bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const ProductJob &job, int64_t most_tiles, int pairs, cudaStream_t stream)
+bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const ProductJob &job, int64_t most_tiles, int pairs,
+                  cudaStream_t stream)
 {
     const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
-    return launch_after(head_product_kernel<PRODUCT, BF16, N>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, job);
+    return launch_after(head_product_kernel<PRODUCT, BF16, N>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, job);
 }
 
-// `rows` and `weight`: the operand maps of the token side and of W's side.  With few tokens the two change places.
+// `rows` and `weight`: the operand maps of the token side and of W's side.  With few tokens the two change places.  `out`: the
+// map of 16-bit results, where there are any.
 template <int PRODUCT, bool BF16>
-bool launch_product(const CUtensorMap &rows, const CUtensorMap &weight, const ProductJob &job, int32_t columns, int64_t most_tiles, int pairs,
-                    cudaStream_t stream)
+bool launch_product(const CUtensorMap &rows, const CUtensorMap &weight, const CUtensorMap &out, const ProductJob &job, int32_t columns,
+                    int64_t most_tiles, int pairs, cudaStream_t stream)
 {
     switch (columns) {
-    case 16: return launch_tiles<PRODUCT, BF16, 16>(weight, rows, job, most_tiles, pairs, stream);
-    case 32: return launch_tiles<PRODUCT, BF16, 32>(weight, rows, job, most_tiles, pairs, stream);
-    case 64: return launch_tiles<PRODUCT, BF16, 64>(weight, rows, job, most_tiles, pairs, stream);
-    case 128: return launch_tiles<PRODUCT, BF16, 128>(weight, rows, job, most_tiles, pairs, stream);
+    case 16: return launch_tiles<PRODUCT, BF16, 16>(weight, rows, out, job, most_tiles, pairs, stream);
+    case 32: return launch_tiles<PRODUCT, BF16, 32>(weight, rows, out, job, most_tiles, pairs, stream);
+    case 64: return launch_tiles<PRODUCT, BF16, 64>(weight, rows, out, job, most_tiles, pairs, stream);
+    case 128: return launch_tiles<PRODUCT, BF16, 128>(weight, rows, out, job, most_tiles, pairs, stream);
     }
-    return launch_tiles<PRODUCT, BF16, TILE>(rows, weight, job, most_tiles, pairs, stream);
+    return launch_tiles<PRODUCT, BF16, TILE>(rows, weight, out, job, most_tiles, pairs, stream);
 }
 
 HeadRows rows_of(char *ws, const Layout &L)
@@ -903,8 +1007,7 @@ bool launch_gather(const ppow_head_params *p, const Layout &L, const GatherJob &
     // a row per CTA, more where that would be over a thousand CTAs: each of them looks at all tokens
     job.rows_per_cta = (L.padded + GATHER_CTAS - 1) / GATHER_CTAS;
     const unsigned grid = (unsigned)((L.padded + job.rows_per_cta - 1) / job.rows_per_cta);
-    head_gather_kernel<BACKWARD, SCALED><<<grid, GATHER_THREADS, 0, stream>>>(job, rows);
-    return cudaGetLastError() == cudaSuccess;
+    return launch_after(head_gather_kernel<BACKWARD, SCALED>, grid, GATHER_THREADS, 0, stream, job, rows);
 }
 
 template <bool BF16>
@@ -935,9 +1038,8 @@ ppow_status forward(const ppow_head_params *p, const void *hidden, const void *w
     job.partial = (float2 *)(ws + L.partial);
     job.at_token = (float *)(ws + L.at_token);
     const int64_t tiles = (int64_t)((L.padded + TILE - 1) / TILE) * L.v_tiles;
-    if (!launch_product<LOGITS_SUM, BF16>(map_rows, map_weight, job, L.columns, tiles, pairs, stream)) return PPOW_ERR_CUDA;
-    const unsigned merge = (unsigned)((p->T * 32ll + MERGE_THREADS - 1) / MERGE_THREADS);
-    return launch_after(head_merge_kernel, merge, MERGE_THREADS, 0, stream, rows, job.partial, job.at_token, L.parts, p->V, job.scale, logp, lse)
+    if (!launch_product<LOGITS_SUM, BF16>(map_rows, map_weight, map_rows, job, L.columns, tiles, pairs, stream)) return PPOW_ERR_CUDA;
+    return launch_after(head_merge_kernel, (unsigned)p->T, MERGE_THREADS, 0, stream, rows, job.partial, job.at_token, L.parts, p->V, job.scale, logp, lse)
                ? PPOW_OK
                : PPOW_ERR_CUDA;
 }
@@ -949,12 +1051,13 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     const Layout L = layout_of(p, true);
     const HeadRows rows = rows_of(ws, L);
     uint16_t *dz = (uint16_t *)(ws + L.dz);
-    CUtensorMap map_rows, map_rows_t, map_weight, map_weight_t, map_dz, map_dz_t;
+    CUtensorMap map_rows, map_rows_t, map_weight, map_weight_t, map_dz, map_dz_t, map_grad;
     if (!make_map(&map_rows, rows.rows, BF16, p->D, L.padded, p->D, L.columns / 2) ||
         !make_map(&map_rows_t, BF16 ? rows.rows : rows.scaled, BF16, p->D, L.padded, p->D, BK) ||
         !make_map(&map_weight, weight, BF16, p->D, p->V, p->weight_stride, HALF_TILE) ||
         !make_map(&map_weight_t, weight, BF16, p->D, p->V, p->weight_stride, BK) ||
-        !make_map(&map_dz, dz, BF16, L.piece, L.padded, L.piece, L.columns / 2) || !make_map(&map_dz_t, dz, BF16, L.piece, L.padded, L.piece, BK))
+        !make_map(&map_dz, dz, BF16, L.piece, L.padded, L.piece, L.columns / 2) || !make_map(&map_dz_t, dz, BF16, L.piece, L.padded, L.piece, BK) ||
+        (grad_weight && !make_map(&map_grad, grad_weight, BF16, p->D, p->V, p->D, HALF_TILE)))
         return PPOW_ERR_CUDA;
     const int pairs = pair_count<BF16>();
     if (pairs < 1) return PPOW_ERR_CUDA;
@@ -971,24 +1074,22 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     job.V = p->V;
     job.d_tiles = L.d_tiles;
     job.piece = L.piece;
-    job.wide_rows = p->D % 16 == 0 && (uintptr_t)grad_weight % 32 == 0;
     job.dz = dz;
     job.grad_rows = (float *)(ws + L.grad_rows);
-    job.grad_weight = (uint16_t *)grad_weight;
     const int64_t row_tiles = (L.padded + TILE - 1) / TILE;
     for (int64_t v0 = 0; v0 < p->V; v0 += L.piece) {
         job.v0 = (int32_t)v0;
         job.columns = (int32_t)(p->V - v0 < L.piece ? p->V - v0 : L.piece);
         job.v_tiles = (job.columns + TILE - 1) / TILE;
         job.add = v0 > 0;
-        if (!launch_product<LOGITS_GRAD, BF16>(map_rows, map_weight, job, L.columns, row_tiles * job.v_tiles, pairs, stream))
+        if (!launch_product<LOGITS_GRAD, BF16>(map_rows, map_weight, map_dz, job, L.columns, row_tiles * job.v_tiles, pairs, stream))
             return PPOW_ERR_CUDA;
-        if (grad_hidden && !launch_product<GRAD_HIDDEN, BF16>(map_dz, map_weight_t, job, L.columns, pairs, pairs, stream)) return PPOW_ERR_CUDA;
-        if (grad_weight && !launch_tiles<GRAD_WEIGHT, BF16, TILE>(map_dz_t, map_rows_t, job, (int64_t)job.v_tiles * L.d_tiles, pairs, stream))
+        if (grad_hidden && !launch_product<GRAD_HIDDEN, BF16>(map_dz, map_weight_t, map_dz, job, L.columns, pairs, pairs, stream)) return PPOW_ERR_CUDA;
+        if (grad_weight && !launch_tiles<GRAD_WEIGHT, BF16, TILE>(map_dz_t, map_rows_t, map_grad, job, (int64_t)job.v_tiles * L.d_tiles, pairs, stream))
             return PPOW_ERR_CUDA;
     }
     if (grad_hidden) {
-        const int64_t blocks = ((int64_t)p->T * (p->D / 8) + FINISH_THREADS - 1) / FINISH_THREADS;
+        const int64_t blocks = ((int64_t)p->T * (p->D / 4) + FINISH_THREADS - 1) / FINISH_THREADS;
         if (!launch_after(head_finish_kernel<BF16>, (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), FINISH_THREADS, 0, stream, rows,
                           job.grad_rows, L.few, p->D, (uint16_t *)grad_hidden))
             return PPOW_ERR_CUDA;
