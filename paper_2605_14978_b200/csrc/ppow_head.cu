@@ -30,6 +30,7 @@ constexpr int BK = 64;               // products' inner step per pipeline stage:
 constexpr uint32_t A_BYTES = HALF_TILE * BK * 2;           // 16 KB
 constexpr int MMA_THREADS = 320;     // producer warp, issuing warp, eight epilogue warps
 constexpr int PAIRS = 74;            // pairs of SMs that the shares of an inner axis are planned for
+constexpr int MAX_PAIRS = 128;       // pairs that a launch uses at most
 
 // Columns of a tile: 256, or for few tokens the tokens themselves (16, 32, 64 or 128), with W taking the 256 rows.
 template <int N> __host__ __device__ constexpr uint32_t stage_bytes() { return A_BYTES + N / 2 * BK * 2; }
@@ -516,10 +517,15 @@ __device__ __forceinline__ void across_lanes(float (&v)[WIDTH], Op op)
     }
 }
 
+// Maximum and sum of exponentials, over the tiles that a warp has seen, of column lane % 32 of a chunk of 32.
+struct RunningSum {
+    float top, sum;
+};
+
 // rows: the vocabulary's entries, for GRAD_HIDDEN the width's; columns: tokens.  Sums over the rows run across the lanes.
 template <int PRODUCT, bool BF16, int N, typename R>
 __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent &e, const Tile &x, uint32_t src, int32_t in_tile, int half,
-                                             R &&release)
+                                             RunningSum (&run)[2], R &&release)
 {
     constexpr int COLS = N / 2, WIDTH = COLS < 32 ? COLS : 32;
     const int lane = threadIdx.x & 31;
@@ -528,44 +534,48 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
     [[maybe_unused]] unsigned int *flags = &job.rows.header->error_flags;
     if (PRODUCT == LOGITS_SUM) {
         const bool inside = row < job.V;
-        const int32_t part = x.index * 8 + in_tile / 32;
         for_chunks<COLS / WIDTH, WIDTH>(src, release, [&](int c, uint32_t (&w)[WIDTH]) {
             if (first + c >= e.live) return;
             float v[WIDTH], r[WIDTH];
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) r[j] = v[j] = inside ? __uint_as_float(w[j]) * job.scale : -INFINITY;
             across_lanes<WIDTH>(r, [](float a, float b) { return fmaxf(a, b); });
-            const float top = r[0];                      // of column lane % WIDTH
+            RunningSum &seen = run[c / 32];
+            const float top = fmaxf(seen.top, r[0]);         // of column lane % WIDTH
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) {
                 const float hi = __shfl_sync(0xffffffffu, top, j);
                 r[j] = inside ? ex2_approx(v[j] - hi) : 0.0f;
             }
             across_lanes<WIDTH>(r, [](float a, float b) { return a + b; });
-            const float sum = r[0];
+            seen.sum = top > -INFINITY ? fmaf(seen.sum, ex2_approx(seen.top - top), r[0]) : 0.0f;
+            seen.top = top;
+            // the product of a token that lies in this warp's 32 rows, if any does
+            const int32_t mine = first + c + lane, at = lane < WIDTH && mine < e.live ? job.rows.token[mine] - (row - lane) : -1;
+            const unsigned hits = __ballot_sync(0xffffffffu, at >= 0 && at < 32);
+            if (hits) {
 #pragma unroll
-            for (int j = 0; j < WIDTH; ++j) {
-                const int32_t token = first + c + j;
-                if (inside && token < e.live && job.rows.token[token] == row) job.at_token[token] = __uint_as_float(w[j]);
+                for (int j = 0; j < WIDTH; ++j)
+                    if ((hits >> j & 1u) && __shfl_sync(0xffffffffu, at, j) == lane) job.at_token[first + c + j] = __uint_as_float(w[j]);
             }
-            const int32_t token = first + c + lane;
-            if (lane < WIDTH && token < e.live && PPOW_CHECK(part < job.parts, 506, flags))
-                job.partial[(size_t)token * job.parts + part] = make_float2(top, sum);
         });
     } else if (PRODUCT == LOGITS_GRAD) {
         const bool inside = row < job.V;
         uint16_t *to = job.dz + x.index * TILE + in_tile;
         for_chunks<COLS / WIDTH, WIDTH>(src, release, [&](int c, uint32_t (&w)[WIDTH]) {
+            // lane j holds what column j needs of its token; columns behind the live ones get zeros
+            const int32_t mine = first + c + lane;
+            const bool live = lane < WIDTH && mine < e.live;
+            const float lse2 = live ? job.rows.lse2[mine] : 0.0f, mult = live ? job.rows.mult[mine] : 0.0f;
+            const int32_t token = live ? job.rows.token[mine] : -1;
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) {
-                const int32_t token = first + c + j;
-                float d = 0.0f;
-                if (inside && token < e.live) {
-                    d = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -job.rows.lse2[token]));
-                    if (job.rows.token[token] == row) d -= 1.0f;
-                    d *= job.rows.mult[token];
-                }
-                if (PPOW_CHECK(x.index * TILE + in_tile < job.piece, 507, flags)) to[(size_t)token * job.piece] = (uint16_t)pack2<BF16>(d, 0.0f);
+                const float l = __shfl_sync(0xffffffffu, lse2, j), m = __shfl_sync(0xffffffffu, mult, j);
+                float d = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -l));
+                if (__shfl_sync(0xffffffffu, token, j) == row) d -= 1.0f;
+                d = inside && first + c + j < e.live ? d * m : 0.0f;
+                if (PPOW_CHECK(x.index * TILE + in_tile < job.piece, 507, flags))
+                    to[(size_t)(first + c + j) * job.piece] = (uint16_t)pack2<BF16>(d, 0.0f);
             }
         });
     } else {
@@ -709,6 +719,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
         const int32_t in_tile = (int32_t)(rank * HALF_TILE + quarter * 32 + lane);
         uint32_t acc = 0;
         bool ok = true;
+        RunningSum run[2] = {{-INFINITY, 0.0f}, {-INFINITY, 0.0f}};
         for (int64_t t = pair; t < tiles; t += pairs, ++acc) {
             const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
             const uint32_t b = acc & 1u;
@@ -731,9 +742,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                 if (lane == 0) mbar_arrive_cluster(peer_addr(acc_empty(b), 0));
             };
             if constexpr (FEW)
-                epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half, release);
+                epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half, run, release);
             else
                 epilogue_many<PRODUCT, BF16>(job, e, x, own, src, in_tile, half, &map_out, box, release);
+        }
+        if (FEW && PRODUCT == LOGITS_SUM) {
+            constexpr int COLS = N / 2;
+            const int32_t part = (int32_t)blockIdx.x * 4 + (int32_t)quarter;
+#pragma unroll
+            for (int c = 0; c < COLS; c += 32) {
+                const int32_t token = half * COLS + c + lane;
+                if (c + lane < COLS && token < e.live && PPOW_CHECK(part < job.parts, 506, &header->error_flags))
+                    job.partial[(size_t)token * job.parts + part] = make_float2(run[c / 32].top, run[c / 32].sum);
+            }
         }
         if (!FEW && (PRODUCT == LOGITS_GRAD || PRODUCT == GRAD_WEIGHT) && in_tile % HALF_TILE == 0) tma_store_wait();
         if (!ok && lane == 0) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
@@ -876,7 +897,8 @@ Layout layout_of(const ppow_head_params *p, bool backward)
     L.row_scale = take(rows * 4);
     L.rows = take(rows * p->D * 2);
     if (!backward) {
-        L.parts = L.v_tiles * (L.few ? 8 : 2);
+        // few tokens: four warps of each CTA; there are at most as many pairs as tiles
+        L.parts = L.few ? 8 * (L.v_tiles < MAX_PAIRS ? L.v_tiles : MAX_PAIRS) : 2 * L.v_tiles;
         L.partial = take(rows * L.parts * sizeof(float2));
         L.at_token = take(rows * 4);
     } else {
@@ -947,7 +969,7 @@ template <bool BF16> int pair_count()
     if (!allow_smem_few<LOGITS_SUM, BF16>() || !allow_smem_few<LOGITS_GRAD, BF16>() || !allow_smem_few<GRAD_HIDDEN, BF16>() ||
         !allow_smem<GRAD_WEIGHT, BF16, TILE>() || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
         return 0;
-    n = sms / 2;
+    n = sms / 2 < MAX_PAIRS ? sms / 2 : MAX_PAIRS;
     known[dev].store(n, std::memory_order_relaxed);
     return n;
 }
@@ -1034,12 +1056,12 @@ ppow_status forward(const ppow_head_params *p, const void *hidden, const void *w
     job.V = job.columns = p->V;
     job.v_tiles = L.v_tiles;
     job.d_tiles = L.d_tiles;
-    job.parts = L.parts;
+    job.parts = L.few ? 8 * (L.v_tiles < pairs ? L.v_tiles : pairs) : L.parts;
     job.partial = (float2 *)(ws + L.partial);
     job.at_token = (float *)(ws + L.at_token);
     const int64_t tiles = (int64_t)((L.padded + TILE - 1) / TILE) * L.v_tiles;
     if (!launch_product<LOGITS_SUM, BF16>(map_rows, map_weight, map_rows, job, L.columns, tiles, pairs, stream)) return PPOW_ERR_CUDA;
-    return launch_after(head_merge_kernel, (unsigned)p->T, MERGE_THREADS, 0, stream, rows, job.partial, job.at_token, L.parts, p->V, job.scale, logp, lse)
+    return launch_after(head_merge_kernel, (unsigned)p->T, MERGE_THREADS, 0, stream, rows, job.partial, job.at_token, job.parts, p->V, job.scale, logp, lse)
                ? PPOW_OK
                : PPOW_ERR_CUDA;
 }
