@@ -715,14 +715,18 @@ def select_windows(score, n_keep: int, want_mask: bool = False, stream=None):
     return (sel, mask) if want_mask else sel
 
 
+def _workspace(nbytes: int, dev) -> torch.Tensor:
+    return torch.empty(nbytes or 256, dtype=torch.uint8, device=dev)      # (sizes as plain integers: a tuple takes 0.8 us more)
+
+
 def head_logprob(hidden, weight, tokens, *, temperature=1.0, stream=None) -> dict:
     """Allocate outputs and workspace, run ppow_head_logprob; returns logp and lse, both [T] float32."""
     params = make_head_params(hidden, weight, temperature)
     dev = hidden.device
     with _On(stream):
-        out = {"logp": torch.empty((params.T,), dtype=torch.float32, device=dev),
-               "lse": torch.empty((params.T,), dtype=torch.float32, device=dev)}
-        ws = alloc_workspace(ppow_head_workspace_bytes(params, False), dev)
+        out = {"logp": torch.empty(params.T, dtype=torch.float32, device=dev),
+               "lse": torch.empty(params.T, dtype=torch.float32, device=dev)}
+        ws = _workspace(ppow_head_workspace_bytes(params, False), dev)
         ppow_head_logprob(params, hidden, weight, tokens, out["logp"], out["lse"], ws, stream)
     return out
 
@@ -732,9 +736,9 @@ def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature
     params = make_head_params(hidden, weight, temperature)
     dev = hidden.device
     with _On(stream):
-        gh = torch.empty((params.T, params.D), dtype=hidden.dtype, device=dev) if want_hidden else None
-        gw = torch.empty((params.V, params.D), dtype=hidden.dtype, device=dev) if want_weight else None
-        ws = alloc_workspace(ppow_head_workspace_bytes(params, True), dev)
+        gh = torch.empty(params.T, params.D, dtype=hidden.dtype, device=dev) if want_hidden else None
+        gw = torch.empty(params.V, params.D, dtype=hidden.dtype, device=dev) if want_weight else None
+        ws = _workspace(ppow_head_workspace_bytes(params, True), dev)
         ppow_head_logprob_backward(params, hidden, weight, tokens, lse, grad_logp, gh, gw, ws, stream)
     return gh, gw
 
@@ -746,8 +750,8 @@ def layer_norm(x, weight, bias=None, *, eps=1e-5, checkpoint=False, stream=None)
     params = make_norm_params(R, D, x.dtype, weight.dtype, eps)
     dev = x.device
     with _On(stream):
-        out = {"y": torch.empty((R, D), dtype=x.dtype, device=dev), "mean": torch.empty((R,), dtype=torch.float32, device=dev),
-               "rstd": torch.empty((R,), dtype=torch.float32, device=dev)}
+        out = {"y": torch.empty(R, D, dtype=x.dtype, device=dev), "mean": torch.empty(R, dtype=torch.float32, device=dev),
+               "rstd": torch.empty(R, dtype=torch.float32, device=dev)}
         if checkpoint:
             out.update(_alloc_packed(R, D, dev))
         ppow_layer_norm(params, x, weight, bias, out["y"], out["mean"], out["rstd"], out.get("packed"), out.get("scale"), stream)
@@ -762,17 +766,17 @@ def layer_norm_backward(grad_y, x, weight, mean, rstd, *, want_bias=True, stream
     dev = grad_y.device
     x, packed, scale = (None, *x) if isinstance(x, (tuple, list)) else (x, None, None)
     with _On(stream):
-        gx = torch.empty((R, D), dtype=grad_y.dtype, device=dev)
-        gw = torch.empty((D,), dtype=weight.dtype, device=dev)
-        gb = torch.empty((D,), dtype=weight.dtype, device=dev) if want_bias else None
-        ws = alloc_workspace(ppow_layer_norm_workspace_bytes(params), dev)
+        gx = torch.empty(R, D, dtype=grad_y.dtype, device=dev)
+        gw = torch.empty(D, dtype=weight.dtype, device=dev)
+        gb = torch.empty(D, dtype=weight.dtype, device=dev) if want_bias else None
+        ws = _workspace(ppow_layer_norm_workspace_bytes(params), dev)
         ppow_layer_norm_backward(params, grad_y, x, packed, scale, weight, mean, rstd, gx, gw, gb, ws, stream)
     return gx, gw, gb
 
 
 def _alloc_packed(R: int, D: int, dev) -> dict:
-    return {"packed": torch.empty((R, D), dtype=CHECKPOINT_DTYPE, device=dev),
-            "scale": torch.empty((R, -(-D // CHECKPOINT_BLOCK)), dtype=torch.uint8, device=dev)}
+    return {"packed": torch.empty(R, D, dtype=CHECKPOINT_DTYPE, device=dev),
+            "scale": torch.empty(R, -(-D // CHECKPOINT_BLOCK), dtype=torch.uint8, device=dev)}
 
 
 def pack_activation(x, stream=None):
@@ -788,6 +792,6 @@ def unpack_activation(packed, scale, dtype=torch.bfloat16, stream=None):
     """Allocate and run ppow_unpack_activation; returns the restored activation in ``dtype``."""
     dev = packed.device
     with _On(stream):
-        x = torch.empty(tuple(packed.shape), dtype=dtype, device=dev)
+        x = torch.empty(*packed.shape, dtype=dtype, device=dev)
         ppow_unpack_activation(packed, scale, x, stream)
     return x

@@ -20,6 +20,7 @@
 #include <cuda_fp8.h>
 #include <atomic>
 #include <math.h>
+#include <type_traits>
 
 namespace ppow {
 
@@ -211,19 +212,6 @@ __device__ __forceinline__ void pack_unit(const float (&f)[DealT::E], bool valid
     if (u % DealT::BLOCK_LANES == 0) scales[u / DealT::BLOCK_LANES] = (uint8_t)code;
 }
 
-template <typename DealT>
-__device__ __forceinline__ void unpack_unit(const uint8_t *codes, const uint8_t *scales, int32_t u, int32_t D, float (&f)[DealT::E])
-{
-    uint32_t q[DealT::E / 2];
-    DealT::load_codes(codes, u, D, q);
-    const float down = scale_down(scales[u / DealT::BLOCK_LANES]);
-#pragma unroll
-    for (int e = 0; e < DealT::E / 2; ++e) {
-        const float2 v = values_of(q[e], down);
-        f[2 * e] = v.x, f[2 * e + 1] = v.y;
-    }
-}
-
 __device__ __forceinline__ float load_param(const void *p, int32_t dtype, int32_t i)
 {
     if (dtype == PPOW_F32) return static_cast<const float *>(p)[i];
@@ -238,6 +226,126 @@ __device__ __forceinline__ void store_param(void *p, int32_t dtype, int32_t i, f
         static_cast<uint16_t *>(p)[i] = dtype == PPOW_BF16 ? Storage<PPOW_BF16>::put(v) : Storage<PPOW_F16>::put(v);
 }
 
+// ---- rows ahead of their use ------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void *src)
+{
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// The thread's own units of the next rows.  VEC: S slots in shared memory, filled by asynchronous copies; a thread reads what
+// it copied itself, so no barrier is needed and the bytes in flight cost no registers.  Scalar: registers, one row ahead.
+template <int DTYPE, bool VEC, int TPR, int U, int S> struct RowAhead;
+template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, true, TPR, U, S> {
+    using DealT = Deal<DTYPE, true>;
+    using T = typename DealT::T;
+    static constexpr size_t BYTES = (size_t)S * U * TPR * 16;       // per row group
+    uint32_t base;                                                  // this thread's first unit in slot 0
+    __device__ __forceinline__ RowAhead(void *smem, int t) : base(smem_address(smem) + t * 16) {}
+    __device__ __forceinline__ void start(int slot, const T *row, int t, int32_t units, int32_t)
+    {
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (t + k * TPR < units) copy_async<16>(base + (slot * U + k) * (TPR * 16), reinterpret_cast<const uint4 *>(row) + t + k * TPR);
+    }
+    __device__ __forceinline__ void take() {}
+    // units behind the row's end read as whatever the slot holds: callers use them only where t + k * TPR < units
+    __device__ __forceinline__ void get(int slot, int k, float (&f)[DealT::E]) const
+    {
+        uint4 w;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                     : "r"(base + (slot * U + k) * (TPR * 16)));
+        DealT::S::unpack(w, f);
+    }
+};
+template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, false, TPR, U, S> {
+    using DealT = Deal<DTYPE, false>;
+    using T = typename DealT::T;
+    static constexpr size_t BYTES = 0;
+    DealT next[U], now[U];
+    __device__ __forceinline__ RowAhead(void *, int) {}
+    __device__ __forceinline__ void start(int, const T *row, int t, int32_t units, int32_t D)
+    {
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (t + k * TPR < units) next[k].load(row, t + k * TPR, D);
+    }
+    __device__ __forceinline__ void take()
+    {
+#pragma unroll
+        for (int k = 0; k < U; ++k) now[k] = next[k];
+    }
+    __device__ __forceinline__ void get(int, int k, float (&f)[4]) const { now[k].get(f); }
+};
+// The 8-bit form of the next rows, and the scales of the thread's units.
+template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
+    using DealT = Deal<DTYPE, VEC>;
+    static constexpr int E = DealT::E;
+    static constexpr size_t BYTES = VEC ? (size_t)S * U * TPR * E : 0;
+    uint32_t base;
+    uint32_t next[VEC ? 1 : U][E / 2], now[VEC ? 1 : U][E / 2];
+    uint8_t next_scale[U], now_scale[U];
+    __device__ __forceinline__ CodesAhead(void *smem, int t) : base(smem_address(smem) + t * E) {}
+    __device__ __forceinline__ void start(int slot, const uint8_t *row, int t, int32_t units, int32_t D)
+    {
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (t + k * TPR < units) {
+                if constexpr (VEC)
+                    copy_async<E>(base + (slot * U + k) * (TPR * E), row + (size_t)(t + k * TPR) * E);
+                else
+                    DealT::load_codes(row, t + k * TPR, D, next[k]);
+            }
+    }
+    // one row ahead in registers: a byte is too small for an asynchronous copy
+    __device__ __forceinline__ void start_scales(const uint8_t *scales, int t, int32_t units)
+    {
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (t + k * TPR < units) next_scale[k] = __ldcs(scales + (t + k * TPR) / DealT::BLOCK_LANES);
+    }
+    __device__ __forceinline__ void take()
+    {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            now_scale[k] = next_scale[k];
+            if constexpr (!VEC) {
+#pragma unroll
+                for (int e = 0; e < E / 2; ++e) now[k][e] = next[k][e];
+            }
+        }
+    }
+    __device__ __forceinline__ void get(int slot, int k, float (&f)[E]) const
+    {
+        uint32_t q[E / 2];
+        if constexpr (!VEC) {
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) q[e] = now[k][e];
+        } else {
+            const uint32_t at = base + (slot * U + k) * (TPR * E);
+            uint32_t lo, hi = 0;
+            if constexpr (E == 8)
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(lo), "=r"(hi) : "r"(at));
+            else
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(lo) : "r"(at));
+            q[0] = lo & 0xffffu, q[1] = lo >> 16;
+            if constexpr (E == 8) q[2] = hi & 0xffffu, q[3] = hi >> 16;
+        }
+        const float down = scale_down(now_scale[k]);
+#pragma unroll
+        for (int e = 0; e < E / 2; ++e) {
+            const float2 v = values_of(q[e], down);
+            f[2 * e] = v.x, f[2 * e + 1] = v.y;
+        }
+    }
+};
+
 // ---- forward ----------------------------------------------------------------------------------------
 struct NormJob {
     const void *x;
@@ -250,113 +358,132 @@ struct NormJob {
     uint8_t *codes, *scales;     // null: no checkpoint
 };
 
-// TPR threads hold one row, U units each.
+// TPR threads hold one row, 32 values each (16 in the scalar deal, whose rows ahead sit in registers); below 128 threads a CTA
+// takes several rows at a time.
 template <int TPR> __host__ __device__ constexpr int norm_threads() { return TPR < 128 ? 128 : TPR; }
+template <bool VEC> __host__ __device__ constexpr int norm_values() { return VEC ? 32 : 16; }
+template <int DTYPE, bool VEC> __host__ __device__ constexpr int norm_units() { return norm_values<VEC>() / (VEC && DTYPE != PPOW_F32 ? 8 : 4); }
+// Rows in flight: about 16 to 64 KB of shared memory per CTA.
+template <int DTYPE, int TPR> __host__ __device__ constexpr int forward_slots() { return TPR <= 128 ? 4 : TPR == 256 ? 3 : 2; }
+template <int DTYPE, int TPR> __host__ __device__ constexpr int backward_slots()
+{
+    return TPR <= 128 ? 3 : TPR == 256 || DTYPE != PPOW_F32 ? 2 : 1;
+}
 
-template <int DTYPE, bool VEC, int TPR, int U>
+template <int DTYPE, bool VEC, int TPR>
 __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const NormJob job)
 {
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
-    constexpr int E = DealT::E, THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR, WARPS = TPR / 32;
-    constexpr bool HOLD = TPR <= 256;                        // weight and bias of the thread's columns stay in registers
-    __shared__ float2 part[2][WARPS];                        // per warp: mean, sum of squares about it
-    const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
+    constexpr int E = DealT::E, U = norm_units<DTYPE, VEC>(), S = forward_slots<DTYPE, TPR>();
+    constexpr int ROWS = norm_threads<TPR>() / TPR, WARPS = TPR / 32;
+    using Ahead = RowAhead<DTYPE, VEC, TPR, U, S>;
+    extern __shared__ uint4 slots[];
+    __shared__ float2 part[2][WARPS];                        // per warp: sum, sum of squares about the warp's own mean
+    __shared__ float counts[WARPS];
+    const int t = threadIdx.x % TPR, lane = threadIdx.x & 31, group = threadIdx.x / TPR;
     const int32_t D = job.D, units = DealT::units(D);
-    float w[HOLD ? U : 1][E], b[HOLD ? U : 1][E];
-    if constexpr (HOLD) {
-#pragma unroll
-        for (int k = 0; k < U; ++k)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int32_t c = DealT::column(t + k * TPR, e);
-                w[k][e] = c < D ? load_param(job.weight, job.param_dtype, c) : 0.0f;
-                b[k][e] = c < D && job.bias ? load_param(job.bias, job.param_dtype, c) : 0.0f;
-            }
-    }
-    // columns that this thread and this warp hold
-    int32_t mine = 0;
+    if (!PPOW_CHECK(units <= TPR * U, 601, nullptr)) return;
+    float w[U][E], b[U][E];                                  // weight and bias of the thread's columns
+    int32_t mine = 0;                                        // columns that this thread holds
 #pragma unroll
     for (int k = 0; k < U; ++k)
 #pragma unroll
-        for (int e = 0; e < E; ++e) mine += t + k * TPR < units && DealT::column(t + k * TPR, e) < D;
+        for (int e = 0; e < E; ++e) {
+            const int32_t c = DealT::column(t + k * TPR, e);
+            const bool has = t + k * TPR < units && c < D;
+            mine += has;
+            w[k][e] = has ? load_param(job.weight, job.param_dtype, c) : 0.0f;
+            b[k][e] = has && job.bias ? load_param(job.bias, job.param_dtype, c) : 0.0f;
+        }
     const float in_warp = (float)__reduce_add_sync(0xffffffffu, mine);
     const float inv_warp = in_warp > 0.0f ? 1.0f / in_warp : 0.0f, inv_d = 1.0f / (float)D;
-    int turn = 0;
+    if (WARPS > 1) {
+        if (lane == 0) counts[t >> 5] = in_warp;
+        __syncthreads();
+    }
 
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < job.R; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-        if (!PPOW_CHECK(units <= TPR * U, 601, nullptr)) return;
-        DealT x[U];
-        const T *src = static_cast<const T *>(job.x) + row * job.x_stride;
+    const int64_t step = (int64_t)gridDim.x * ROWS, first = (int64_t)blockIdx.x * ROWS + group;
+    const T *x = static_cast<const T *>(job.x);
+    Ahead ahead(reinterpret_cast<uint8_t *>(slots) + group * Ahead::BYTES, t);
+    constexpr int LEAD = VEC ? S - 1 : 1;                    // rows that are on their way when one is worked on
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int32_t u = t + k * TPR;
-            if (u < units)
-                x[k].load(src, u, D);
-            else
-                x[k].zero();
-        }
-        // mean of the warp's values, then squares about it: no difference of large sums
-        float sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            float f[E];
-            x[k].get(f);
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum += f[e];
-        }
-        const float m = warp_sum(sum) * inv_warp;
-        float sq = 0.0f;
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            const int32_t u = t + k * TPR;
-            float f[E];
-            x[k].get(f);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float d = u < units && DealT::has(u, e, D) ? f[e] - m : 0.0f;
-                sq = fmaf(d, d, sq);
+    for (int i = 0; i < LEAD; ++i) {
+        if (first + i * step < job.R) ahead.start(i, x + (first + i * step) * job.x_stride, t, units, D);
+        if (VEC) copy_commit();
+    }
+    int slot = 0, turn = 0;
+    for (int64_t row = first; row < job.R; row += step, turn ^= 1) {
+        ahead.take();
+        {
+            const int64_t next = row + LEAD * step;
+            const int to = slot == 0 ? S - 1 : slot - 1;     // the slot of the row before
+            if (next < job.R) ahead.start(to, x + next * job.x_stride, t, units, D);
+            if (VEC) {
+                copy_commit();
+                copy_wait<LEAD>();
             }
         }
-        sq = warp_sum(sq);
+        float f[U][E];
+        float2 sum2 = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (t + k * TPR < units) {
+                ahead.get(slot, k, f[k]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) f[k][e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < E; e += 2) sum2 = __fadd2_rn(sum2, make_float2(f[k][e], f[k][e + 1]));
+        }
+        // sum of the warp's values, then squares about their mean: no difference of large sums
+        const float sum = warp_sum(sum2.x + sum2.y), m = sum * inv_warp;
+        const float2 minus_m = make_float2(-m, -m);
+        float2 sq2 = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const float2 d = __fadd2_rn(make_float2(f[k][e], f[k][e + 1]), minus_m);
+                if constexpr (VEC) {
+                    if (t + k * TPR < units) sq2 = __ffma2_rn(d, d, sq2);
+                } else {
+                    const int32_t u = t + k * TPR;
+                    const float2 in = make_float2(DealT::has(u, e, D) ? d.x : 0.0f, DealT::has(u, e + 1, D) ? d.y : 0.0f);
+                    sq2 = __ffma2_rn(in, in, sq2);
+                }
+            }
+        const float sq = warp_sum(sq2.x + sq2.y);
         float mean = m, squares = sq;
         if (WARPS > 1) {
-            // every warp's count follows from the deal: recompute it instead of sending it
-            if (lane == 0) part[turn][t >> 5] = make_float2(m * in_warp, in_warp > 0.0f ? sq : 0.0f);
+            // squares about the row's mean: each warp's squares about its own, plus its count times the gap squared
+            if (lane == 0) part[turn][t >> 5] = make_float2(sum, sq);
             __syncthreads();
             float total = 0.0f;
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) total += part[turn][i].x;
             mean = total * inv_d;
-            // squares about the row's mean: each warp's squares about its own, plus its count times the gap squared
-            const float gap = m - mean;
-            float own = sq + in_warp * gap * gap;
-            __shared__ float spread[2][WARPS];
-            if (lane == 0) spread[turn][t >> 5] = in_warp > 0.0f ? own : 0.0f;
-            __syncthreads();
             squares = 0.0f;
 #pragma unroll
-            for (int i = 0; i < WARPS; ++i) squares += spread[turn][i];
+            for (int i = 0; i < WARPS; ++i) {
+                const float n = counts[i], gap = n > 0.0f ? part[turn][i].x / n - mean : 0.0f;
+                squares += part[turn][i].y + n * gap * gap;
+            }
         }
         const float rstd = 1.0f / sqrtf(squares * inv_d + job.eps);
+        const float2 minus_mean = make_float2(-mean, -mean), r2 = make_float2(rstd, rstd);
         T *dst = static_cast<T *>(job.y) + row * D;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             const int32_t u = t + k * TPR;
             if (u < units) {
-                float f[E], y[E];
-                x[k].get(f);
+                float y[E];
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    float we, be;
-                    if constexpr (HOLD) {
-                        we = w[k][e], be = b[k][e];
-                    } else {
-                        const int32_t c = min(DealT::column(u, e), D - 1);
-                        we = load_param(job.weight, job.param_dtype, c);
-                        be = job.bias ? load_param(job.bias, job.param_dtype, c) : 0.0f;
-                    }
-                    y[e] = fmaf((f[e] - mean) * rstd, we, be);
+                for (int e = 0; e < E; e += 2) {
+                    const float2 xh = __fmul2_rn(__fadd2_rn(make_float2(f[k][e], f[k][e + 1]), minus_mean), r2);
+                    const float2 o = __ffma2_rn(xh, make_float2(w[k][e], w[k][e + 1]), make_float2(b[k][e], b[k][e + 1]));
+                    y[e] = o.x, y[e + 1] = o.y;
                 }
                 DealT::store(dst, u, D, y);
             }
@@ -367,13 +494,10 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const
         }
         if (job.codes) {
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const int32_t u = t + k * TPR;
-                float f[E];
-                x[k].get(f);
-                pack_unit<DealT>(f, u < units, u, D, job.codes + row * D, job.scales + row * job.blocks);
-            }
+            for (int k = 0; k < U; ++k)
+                pack_unit<DealT>(f[k], t + k * TPR < units, t + k * TPR, D, job.codes + row * D, job.scales + row * job.blocks);
         }
+        slot = slot == S - 1 ? 0 : slot + 1;
     }
 }
 
@@ -391,167 +515,152 @@ struct NormGradJob {
     float *partial;                      // [CTAs][2][D]: shares of dw, then of db
 };
 
-template <int DTYPE, bool VEC, bool PACKED, int TPR, int U>
+// Two passes over a row's values, both from the thread's own copies: sums first, then dx.  The column sums of dw and db stay in
+// the registers of the thread that owns the column.
+template <int DTYPE, bool VEC, bool PACKED, int TPR>
 __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(const NormGradJob job)
 {
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
-    constexpr int E = DealT::E, THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR, WARPS = TPR / 32;
-    constexpr bool HOLD = TPR <= 256;    // the column sums and the weight stay in registers; else the sums in shared memory
-    extern __shared__ float sums[];      // !HOLD: [2][D]
+    constexpr int E = DealT::E, U = norm_units<DTYPE, VEC>(), S = backward_slots<DTYPE, TPR>();
+    constexpr int ROWS = norm_threads<TPR>() / TPR, WARPS = TPR / 32;
+    using Grads = RowAhead<DTYPE, VEC, TPR, U, S>;
+    using Inputs = std::conditional_t<PACKED, CodesAhead<DTYPE, VEC, TPR, U, S>, RowAhead<DTYPE, VEC, TPR, U, S>>;
+    extern __shared__ uint4 slots[];
     __shared__ float2 part[2][WARPS];
-    const int t = threadIdx.x % TPR, lane = threadIdx.x & 31;
+    const int t = threadIdx.x % TPR, lane = threadIdx.x & 31, group = threadIdx.x / TPR;
     const int32_t D = job.D, units = DealT::units(D);
+    if (!PPOW_CHECK(units <= TPR * U, 602, nullptr)) return;
     const float inv_d = 1.0f / (float)D;
-    float w[HOLD ? U : 1][E], dw[HOLD ? U : 1][E], db[HOLD ? U : 1][E];
+    float w[U][E];
+    float2 dw[U][E / 2], db[U][E / 2];
 #pragma unroll
-    for (int k = 0; k < (HOLD ? U : 1); ++k)
+    for (int k = 0; k < U; ++k)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const int32_t c = DealT::column(t + k * TPR, e);
-            w[k][e] = HOLD && c < D ? load_param(job.weight, job.param_dtype, c) : 0.0f;
-            dw[k][e] = db[k][e] = 0.0f;
+            w[k][e] = t + k * TPR < units && c < D ? load_param(job.weight, job.param_dtype, c) : 0.0f;
+            dw[k][e / 2] = db[k][e / 2] = make_float2(0.0f, 0.0f);
         }
-    if (!HOLD) {
-        for (int32_t i = threadIdx.x; i < 2 * D; i += THREADS) sums[i] = 0.0f;
-        __syncthreads();
-    }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < job.R; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-        if (!PPOW_CHECK(units <= TPR * U, 602, nullptr)) return;
-        DealT g[U], x[PACKED ? 1 : U];
-        float xp[PACKED ? U : 1][E];
-        const T *gsrc = static_cast<const T *>(job.grad_y) + row * job.grad_y_stride;
-        const T *xsrc = static_cast<const T *>(job.x) + row * job.x_stride;
+    const int64_t step = (int64_t)gridDim.x * ROWS, first = (int64_t)blockIdx.x * ROWS + group;
+    uint8_t *own = reinterpret_cast<uint8_t *>(slots) + group * (Grads::BYTES + Inputs::BYTES);
+    Grads grads(own, t);
+    Inputs inputs(own + Grads::BYTES, t);
+    constexpr int LEAD = VEC ? S - 1 : 1;
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    auto start = [&](int slot, int64_t row) {
+        if (row < job.R) {
+            grads.start(slot, static_cast<const T *>(job.grad_y) + row * job.grad_y_stride, t, units, D);
+            if constexpr (PACKED)
+                inputs.start(slot, job.codes + row * D, t, units, D);
+            else
+                inputs.start(slot, static_cast<const T *>(job.x) + row * job.x_stride, t, units, D);
+        }
+        if (VEC) copy_commit();
+    };
+    auto start_scalars = [&](int64_t row) {
+        if (row < job.R) {
+            next_mean = job.mean[row];
+            next_rstd = job.rstd[row];
+            if constexpr (PACKED) inputs.start_scales(job.scales + row * job.blocks, t, units);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < LEAD; ++i) start(i, first + i * step);
+    start_scalars(first);
+    int slot = 0, turn = 0;
+    for (int64_t row = first; row < job.R; row += step, turn ^= 1) {
+        grads.take();
+        inputs.take();
+        const float2 minus_mean = make_float2(-next_mean, -next_mean), r2 = make_float2(next_rstd, next_rstd);
+        const float rstd = next_rstd;
+        start(LEAD == 0 ? slot : slot == 0 ? S - 1 : slot - 1, row + LEAD * step);
+        start_scalars(row + step);
+        if (VEC) copy_wait<LEAD>();
+        float2 c1 = make_float2(0.0f, 0.0f), c2 = c1;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-            const int32_t u = t + k * TPR;
-            if (u < units) {
-                g[k].load(gsrc, u, D);
-                if (PACKED)
-                    unpack_unit<DealT>(job.codes + row * D, job.scales + row * job.blocks, u, D, xp[PACKED ? k : 0]);
-                else
-                    x[PACKED ? 0 : k].load(xsrc, u, D);
-            } else {
-                g[k].zero();
-                if (PACKED) {
+            if (t + k * TPR < units) {
+                float f[E], g[E];
+                inputs.get(slot, k, f);
+                grads.get(slot, k, g);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) xp[PACKED ? k : 0][e] = 0.0f;
-                } else {
-                    x[PACKED ? 0 : k].zero();
+                for (int e = 0; e < E; e += 2) {
+                    // columns that do not exist have g = 0 and w = 0
+                    const float2 xh = __fmul2_rn(__fadd2_rn(make_float2(f[e], f[e + 1]), minus_mean), r2);
+                    const float2 gy = make_float2(g[e], g[e + 1]), a = __fmul2_rn(gy, make_float2(w[k][e], w[k][e + 1]));
+                    c1 = __fadd2_rn(c1, a);
+                    c2 = __ffma2_rn(a, xh, c2);
+                    dw[k][e / 2] = __ffma2_rn(gy, xh, dw[k][e / 2]);
+                    db[k][e / 2] = __fadd2_rn(db[k][e / 2], gy);
                 }
             }
         }
-        const float mean = job.mean[row], rstd = job.rstd[row];
-        auto weight_at = [&](int k, int e) {
-            if constexpr (HOLD) {
-                return w[k][e];
-            } else {
-                const int32_t c = DealT::column(t + k * TPR, e);
-                return c < D ? load_param(job.weight, job.param_dtype, c) : 0.0f;
-            }
-        };
-        auto input = [&](int k, float (&f)[E]) {
-            if (PACKED) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) f[e] = xp[PACKED ? k : 0][e];
-            } else {
-                x[PACKED ? 0 : k].get(f);
-            }
-        };
-        float c1 = 0.0f, c2 = 0.0f;
-#pragma unroll
-        for (int k = 0; k < U; ++k) {
-            float f[E], gy[E];
-            input(k, f);
-            g[k].get(gy);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                // columns that do not exist have gy = 0 and w = 0
-                const float xh = (f[e] - mean) * rstd, a = gy[e] * weight_at(k, e);
-                c1 += a;
-                c2 = fmaf(a, xh, c2);
-                if constexpr (HOLD) {
-                    dw[k][e] = fmaf(gy[e], xh, dw[k][e]);
-                    db[k][e] += gy[e];
-                } else {
-                    const int32_t c = DealT::column(t + k * TPR, e);
-                    if (t + k * TPR < units && c < D) {
-                        sums[c] = fmaf(gy[e], xh, sums[c]);
-                        sums[D + c] += gy[e];
-                    }
-                }
-            }
-        }
-        c1 = warp_sum(c1);
-        c2 = warp_sum(c2);
+        float s1 = warp_sum(c1.x + c1.y), s2 = warp_sum(c2.x + c2.y);
         if (WARPS > 1) {
-            if (lane == 0) part[turn][t >> 5] = make_float2(c1, c2);
+            if (lane == 0) part[turn][t >> 5] = make_float2(s1, s2);
             __syncthreads();
-            c1 = c2 = 0.0f;
+            s1 = s2 = 0.0f;
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) {
-                c1 += part[turn][i].x;
-                c2 += part[turn][i].y;
+                s1 += part[turn][i].x;
+                s2 += part[turn][i].y;
             }
         }
-        c1 *= inv_d;
-        c2 *= inv_d;
+        s1 *= -inv_d;
+        s2 *= -inv_d;
+        const float2 m1 = make_float2(s1, s1), m2 = make_float2(s2, s2), rr = make_float2(rstd, rstd);
         T *dst = static_cast<T *>(job.grad_x) + row * D;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             const int32_t u = t + k * TPR;
             if (u < units) {
-                float f[E], gy[E], o[E];
-                input(k, f);
-                g[k].get(gy);
+                float f[E], g[E], o[E];
+                inputs.get(slot, k, f);
+                grads.get(slot, k, g);
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float xh = (f[e] - mean) * rstd;
-                    o[e] = (gy[e] * weight_at(k, e) - c1 - xh * c2) * rstd;
+                for (int e = 0; e < E; e += 2) {
+                    const float2 xh = __fmul2_rn(__fadd2_rn(make_float2(f[e], f[e + 1]), minus_mean), r2);
+                    const float2 a = __fmul2_rn(make_float2(g[e], g[e + 1]), make_float2(w[k][e], w[k][e + 1]));
+                    const float2 d = __fmul2_rn(__ffma2_rn(xh, m2, __fadd2_rn(a, m1)), rr);
+                    o[e] = d.x, o[e + 1] = d.y;
                 }
                 DealT::store(dst, u, D, o);
             }
         }
+        slot = slot == S - 1 ? 0 : slot + 1;
     }
     // this CTA's share of the column sums
     float *out = job.partial + (size_t)blockIdx.x * 2 * D;
-    if constexpr (!HOLD) {
-        __syncthreads();
-        for (int32_t i = threadIdx.x; i < 2 * D; i += THREADS) out[i] = sums[i];
-    }
-    if constexpr (HOLD && ROWS == 1) {
+    auto each_column = [&](auto &&f) {
 #pragma unroll
         for (int k = 0; k < U; ++k)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const int32_t u = t + k * TPR, c = DealT::column(u, e);
-                if (u < units && c < D) {
-                    out[c] = dw[k][e];
-                    out[D + c] = db[k][e];
-                }
+                if (u < units && c < D) f(c, e & 1 ? dw[k][e / 2].y : dw[k][e / 2].x, e & 1 ? db[k][e / 2].y : db[k][e / 2].x);
             }
-    }
-    if constexpr (ROWS > 1) {
-        // several rows at a time: the warps add their sums up one after the other
-        __shared__ float joint[2][TPR * U * E];
+    };
+    if constexpr (ROWS == 1) {
+        each_column([&](int32_t c, float sw, float sb) {
+            out[c] = sw;
+            out[D + c] = sb;
+        });
+    } else {
+        // several rows at a time: the groups add their sums up one after the other
+        __shared__ float joint[2][TPR * norm_values<VEC>()];
         for (int s = 0; s < ROWS; ++s) {
-            if (threadIdx.x / TPR == s) {
-#pragma unroll
-                for (int k = 0; k < U; ++k)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const int i = (k * E + e) * TPR + t;
-                        const float sw = (s ? joint[0][i] : 0.0f) + dw[k][e], sb = (s ? joint[1][i] : 0.0f) + db[k][e];
-                        joint[0][i] = sw;
-                        joint[1][i] = sb;
-                        const int32_t u = t + k * TPR, c = DealT::column(u, e);
-                        if (s == ROWS - 1 && u < units && c < D) {
-                            out[c] = sw;
-                            out[D + c] = sb;
-                        }
+            if (group == s)
+                each_column([&](int32_t c, float sw, float sb) {
+                    sw += s ? joint[0][c] : 0.0f;
+                    sb += s ? joint[1][c] : 0.0f;
+                    joint[0][c] = sw;
+                    joint[1][c] = sb;
+                    if (s == ROWS - 1) {
+                        out[c] = sw;
+                        out[D + c] = sb;
                     }
-            }
+                });
             __syncthreads();
         }
     }
@@ -593,6 +702,25 @@ struct PackJob {
     int32_t R, D, blocks;
 };
 
+// Chunks of 32 units, row by row; a warp takes PACK_CHUNKS neighbours.  One division per warp.
+struct ChunkWalk {
+    int64_t row;
+    int32_t chunk;
+    __device__ __forceinline__ ChunkWalk(int64_t warp, int32_t per_row)
+    {
+        const int64_t first = warp * PACK_CHUNKS;
+        row = first / per_row;
+        chunk = (int32_t)(first - row * per_row);
+    }
+    __device__ __forceinline__ void step(int32_t per_row)
+    {
+        if (++chunk == per_row) {
+            chunk = 0;
+            ++row;
+        }
+    }
+};
+
 template <int DTYPE, bool VEC>
 __global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const PackJob job)
 {
@@ -600,23 +728,22 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const PackJob job)
     using T = typename DealT::T;
     const int lane = threadIdx.x & 31;
     const int32_t units = DealT::units(job.D), per_row = (units + 31) / 32;
-    const int64_t chunks = (int64_t)job.R * per_row, first = ((int64_t)blockIdx.x * (PACK_THREADS / 32) + (threadIdx.x >> 5)) * PACK_CHUNKS;
+    ChunkWalk at((int64_t)blockIdx.x * (PACK_THREADS / 32) + (threadIdx.x >> 5), per_row);
     DealT x[PACK_CHUNKS];
+    ChunkWalk ahead = at;
 #pragma unroll
-    for (int i = 0; i < PACK_CHUNKS; ++i) {
-        const int64_t c = first + i, row = c / per_row;
-        const int32_t u = (int32_t)(c % per_row) * 32 + lane;
+    for (int i = 0; i < PACK_CHUNKS; ++i, ahead.step(per_row)) {
+        const int32_t u = ahead.chunk * 32 + lane;
         x[i].zero();
-        if (c < chunks && u < units) x[i].load(static_cast<const T *>(job.x) + row * job.x_stride, u, job.D);
+        if (ahead.row < job.R && u < units) x[i].load(static_cast<const T *>(job.x) + ahead.row * job.x_stride, u, job.D);
     }
 #pragma unroll
-    for (int i = 0; i < PACK_CHUNKS; ++i) {
-        const int64_t c = first + i, row = c / per_row;
-        const int32_t u = (int32_t)(c % per_row) * 32 + lane;
-        if (c >= chunks || !PPOW_CHECK(row < job.R, 603, nullptr)) return;
+    for (int i = 0; i < PACK_CHUNKS; ++i, at.step(per_row)) {
+        const int32_t u = at.chunk * 32 + lane;
+        if (at.row >= job.R || !PPOW_CHECK(at.chunk < per_row, 603, nullptr)) return;
         float f[DealT::E];
         x[i].get(f);
-        pack_unit<DealT>(f, u < units, u, job.D, job.codes + row * job.D, job.scales + row * job.blocks);
+        pack_unit<DealT>(f, u < units, u, job.D, job.codes + at.row * job.D, job.scales + at.row * job.blocks);
     }
 }
 
@@ -627,16 +754,29 @@ __global__ void __launch_bounds__(PACK_THREADS) unpack_kernel(const PackJob job)
     using T = typename DealT::T;
     const int lane = threadIdx.x & 31;
     const int32_t units = DealT::units(job.D), per_row = (units + 31) / 32;
-    const int64_t chunks = (int64_t)job.R * per_row, first = ((int64_t)blockIdx.x * (PACK_THREADS / 32) + (threadIdx.x >> 5)) * PACK_CHUNKS;
+    ChunkWalk at((int64_t)blockIdx.x * (PACK_THREADS / 32) + (threadIdx.x >> 5), per_row), ahead = at;
+    uint32_t q[PACK_CHUNKS][DealT::E / 2];
+    uint8_t scale[PACK_CHUNKS];
 #pragma unroll
-    for (int i = 0; i < PACK_CHUNKS; ++i) {
-        const int64_t c = first + i, row = c / per_row;
-        const int32_t u = (int32_t)(c % per_row) * 32 + lane;
-        if (c >= chunks || !PPOW_CHECK(row < job.R, 604, nullptr)) return;
+    for (int i = 0; i < PACK_CHUNKS; ++i, ahead.step(per_row)) {
+        const int32_t u = ahead.chunk * 32 + lane;
+        if (ahead.row < job.R && u < units) {
+            DealT::load_codes(job.codes + ahead.row * job.D, u, job.D, q[i]);
+            scale[i] = job.scales[ahead.row * job.blocks + u / DealT::BLOCK_LANES];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PACK_CHUNKS; ++i, at.step(per_row)) {
+        const int32_t u = at.chunk * 32 + lane;
+        if (at.row >= job.R || !PPOW_CHECK(at.chunk < per_row, 604, nullptr)) return;
         if (u < units) {
             float f[DealT::E];
-            unpack_unit<DealT>(job.codes + row * job.D, job.scales + row * job.blocks, u, job.D, f);
-            DealT::store(static_cast<T *>(job.out) + row * job.D, u, job.D, f);
+#pragma unroll
+            for (int e = 0; e < DealT::E / 2; ++e) {
+                const float2 v = values_of(q[i][e], scale_down(scale[i]));
+                f[2 * e] = v.x, f[2 * e + 1] = v.y;
+            }
+            DealT::store(static_cast<T *>(job.out) + at.row * job.D, u, job.D, f);
         }
     }
 }
@@ -685,33 +825,38 @@ int resident_ctas(Resident &known, Kernel kernel, int threads, size_t smem)
 // CTAs of the backward pass: each leaves one share of the column sums.  148 SMs x 2 to 4; a function of the sizes alone.
 constexpr int32_t SHARES_MAX = 148 * 4;
 
-template <int DTYPE, bool VEC, int TPR, int U>
+template <int DTYPE, bool VEC, int TPR>
 bool forward_launch(const NormJob &job, cudaStream_t stream)
 {
     constexpr int THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR;
+    constexpr size_t SMEM = ROWS * RowAhead<DTYPE, VEC, TPR, norm_units<DTYPE, VEC>(), forward_slots<DTYPE, TPR>()>::BYTES;
+    auto kernel = norm_forward_kernel<DTYPE, VEC, TPR>;
     static Resident known;
-    const int64_t need = ((int64_t)job.R + ROWS - 1) / ROWS, most = resident_ctas(known, norm_forward_kernel<DTYPE, VEC, TPR, U>, THREADS, 0);
+    const int64_t need = ((int64_t)job.R + ROWS - 1) / ROWS, most = resident_ctas(known, kernel, THREADS, SMEM);
     if (most < 1) return false;
-    norm_forward_kernel<DTYPE, VEC, TPR, U><<<(unsigned)(need < most ? need : most), THREADS, 0, stream>>>(job);
+    kernel<<<(unsigned)(need < most ? need : most), THREADS, SMEM, stream>>>(job);
     return cudaGetLastError() == cudaSuccess;
 }
 
+// The fewest threads that hold a row.
 template <int DTYPE, bool VEC>
 bool forward_shape(const NormJob &job, cudaStream_t stream)
 {
-    const int32_t units = VEC ? job.D / (16 / (int32_t)bytes_of(DTYPE)) : (job.D + CKPT_BLOCK - 1) / CKPT_BLOCK * 32;
-    if (units <= 32 * 4) return forward_launch<DTYPE, VEC, 32, 4>(job, stream);
-    if (units <= 128 * 4) return forward_launch<DTYPE, VEC, 128, 4>(job, stream);
-    if (units <= 256 * 4) return forward_launch<DTYPE, VEC, 256, 4>(job, stream);
-    return forward_launch<DTYPE, VEC, 1024, 4>(job, stream);
+    constexpr int HELD = norm_values<VEC>();
+    if (job.D <= 32 * HELD) return forward_launch<DTYPE, VEC, 32>(job, stream);
+    if (job.D <= 128 * HELD) return forward_launch<DTYPE, VEC, 128>(job, stream);
+    if (job.D <= 256 * HELD) return forward_launch<DTYPE, VEC, 256>(job, stream);
+    if (VEC || job.D <= 512 * HELD) return forward_launch<DTYPE, VEC, 512>(job, stream);
+    return forward_launch<DTYPE, VEC, VEC ? 512 : 1024>(job, stream);
 }
 
-template <int DTYPE, bool VEC, bool PACKED, int TPR, int U>
+template <int DTYPE, bool VEC, bool PACKED, int TPR>
 bool backward_launch(const NormGradJob &job, int32_t *shares, cudaStream_t stream)
 {
-    constexpr int THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR;
-    constexpr size_t SMEM = TPR <= 256 ? 0 : (size_t)NORM_MAX_WIDTH * 8;
-    auto kernel = norm_backward_kernel<DTYPE, VEC, PACKED, TPR, U>;
+    constexpr int THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR, U = norm_units<DTYPE, VEC>(), S = backward_slots<DTYPE, TPR>();
+    constexpr size_t ROW = RowAhead<DTYPE, VEC, TPR, U, S>::BYTES;
+    constexpr size_t SMEM = ROWS * (ROW + (PACKED ? CodesAhead<DTYPE, VEC, TPR, U, S>::BYTES : ROW));
+    auto kernel = norm_backward_kernel<DTYPE, VEC, PACKED, TPR>;
     static Resident known;
     const int64_t most = resident_ctas(known, kernel, THREADS, SMEM);
     if (most < 1) return false;
@@ -726,11 +871,12 @@ bool backward_launch(const NormGradJob &job, int32_t *shares, cudaStream_t strea
 template <int DTYPE, bool VEC, bool PACKED>
 bool backward_shape(const NormGradJob &job, int32_t *shares, cudaStream_t stream)
 {
-    const int32_t units = VEC ? job.D / (16 / (int32_t)bytes_of(DTYPE)) : (job.D + CKPT_BLOCK - 1) / CKPT_BLOCK * 32;
-    if (units <= 32 * 4) return backward_launch<DTYPE, VEC, PACKED, 32, 4>(job, shares, stream);
-    if (units <= 128 * 4) return backward_launch<DTYPE, VEC, PACKED, 128, 4>(job, shares, stream);
-    if (units <= 256 * 4) return backward_launch<DTYPE, VEC, PACKED, 256, 4>(job, shares, stream);
-    return backward_launch<DTYPE, VEC, PACKED, 1024, 4>(job, shares, stream);
+    constexpr int HELD = norm_values<VEC>();
+    if (job.D <= 32 * HELD) return backward_launch<DTYPE, VEC, PACKED, 32>(job, shares, stream);
+    if (job.D <= 128 * HELD) return backward_launch<DTYPE, VEC, PACKED, 128>(job, shares, stream);
+    if (job.D <= 256 * HELD) return backward_launch<DTYPE, VEC, PACKED, 256>(job, shares, stream);
+    if (VEC || job.D <= 512 * HELD) return backward_launch<DTYPE, VEC, PACKED, 512>(job, shares, stream);
+    return backward_launch<DTYPE, VEC, PACKED, VEC ? 512 : 1024>(job, shares, stream);
 }
 
 template <int DTYPE, bool VEC>
