@@ -121,10 +121,16 @@ template <int DTYPE> struct Deal<DTYPE, false> {
     static __device__ __forceinline__ int32_t units(int32_t D) { return (D + CKPT_BLOCK - 1) / CKPT_BLOCK * 32; }
     static __device__ __forceinline__ int32_t column(int32_t u, int e) { return (u >> 5) * CKPT_BLOCK + e * 32 + (u & 31); }
     static __device__ __forceinline__ bool has(int32_t u, int e, int32_t D) { return column(u, e) < D; }
+    static __device__ __forceinline__ bool whole(int32_t u, int32_t D) { return ((u >> 5) + 1) * CKPT_BLOCK <= D; }   // of the warp's block
     __device__ __forceinline__ void load(const T *row, int32_t u, int32_t D)
     {
+        if (whole(u, D)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) raw[e] = has(u, e, D) ? __ldcs(row + column(u, e)) : T(0);
+            for (int e = 0; e < 4; ++e) raw[e] = __ldcs(row + column(u, 0) + 32 * e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) raw[e] = has(u, e, D) ? __ldcs(row + column(u, e)) : T(0);
+        }
     }
     __device__ __forceinline__ void zero() { raw[0] = raw[1] = raw[2] = raw[3] = T(0); }
     __device__ __forceinline__ void get(float (&f)[4]) const
@@ -134,22 +140,35 @@ template <int DTYPE> struct Deal<DTYPE, false> {
     }
     static __device__ __forceinline__ void store(T *row, int32_t u, int32_t D, const float (&f)[4])
     {
+        T *to = row + column(u, 0);
+        if (whole(u, D)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (has(u, e, D)) row[column(u, e)] = S::put(f[e]);
+            for (int e = 0; e < 4; ++e) to[32 * e] = S::put(f[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (has(u, e, D)) to[32 * e] = S::put(f[e]);
+        }
     }
     static __device__ __forceinline__ void store_codes(uint8_t *row, int32_t u, int32_t D, const uint32_t (&q)[2])
     {
+        uint8_t *to = row + column(u, 0);
+        if (whole(u, D)) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (has(u, e, D)) row[column(u, e)] = (uint8_t)(q[e >> 1] >> (8 * (e & 1)));
+            for (int e = 0; e < 4; ++e) to[32 * e] = (uint8_t)(q[e >> 1] >> (8 * (e & 1)));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (has(u, e, D)) to[32 * e] = (uint8_t)(q[e >> 1] >> (8 * (e & 1)));
+        }
     }
     static __device__ __forceinline__ void load_codes(const uint8_t *row, int32_t u, int32_t D, uint32_t (&q)[2])
     {
-        q[0] = q[1] = 0;
+        uint32_t c[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (has(u, e, D)) q[e >> 1] |= (uint32_t)__ldcs(row + column(u, e)) << (8 * (e & 1));
+        for (int e = 0; e < 4; ++e) c[e] = whole(u, D) || has(u, e, D) ? __ldcs(row + column(u, 0) + 32 * e) : 0u;
+        q[0] = c[0] | (c[1] << 8);
+        q[1] = c[2] | (c[3] << 8);
     }
 };
 
@@ -169,17 +188,19 @@ __device__ __forceinline__ float finite_magnitude(float x)
     const float a = fabsf(x);
     return a < INFINITY ? a : 0.0f;
 }
-// two values; an infinity becomes NaN (the format has none), as NaN does
-__device__ __forceinline__ uint32_t codes_of(float a, float b, float up)
+__device__ __forceinline__ float nan_for_inf(float x) { return fmaf(x, 0.0f, x); }     // the format has no infinity
+// two scaled values, to nearest even; NaN stays NaN
+__device__ __forceinline__ uint32_t codes_of(float a, float b)
 {
-    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(fmaf(a, 0.0f, a) * up, fmaf(b, 0.0f, b) * up), __NV_SATFINITE, __NV_E4M3);
+    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
-__device__ __forceinline__ float2 values_of(uint32_t codes, float down)
+// two codes as float16 pairs (exact)
+__device__ __forceinline__ float2 halves_of(uint32_t codes)
 {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3);
-    const float2 f = __half22float2(__half2(h));
-    return make_float2(f.x * down, f.y * down);
+    return __half22float2(__half2(h));
 }
+__device__ __forceinline__ float2 values_of(uint32_t codes, float down) { return __fmul2_rn(halves_of(codes), make_float2(down, down)); }
 
 template <int LANES> __device__ __forceinline__ float lanes_max(float v)
 {
@@ -194,20 +215,34 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// Packs one unit per lane (the whole warp calls; `valid` lanes hold a unit).
+// Packs one unit per lane (the whole warp calls; `valid` lanes hold a unit, the others any finite values).
 template <typename DealT>
 __device__ __forceinline__ void pack_unit(const float (&f)[DealT::E], bool valid, int32_t u, int32_t D, uint8_t *codes, uint8_t *scales)
 {
     float top = 0.0f;
 #pragma unroll
-    for (int e = 0; e < DealT::E; ++e) top = fmaxf(top, finite_magnitude(f[e]));
+    for (int e = 0; e < DealT::E; ++e) top = fmaxf(top, fabsf(f[e]));      // passes NaN over
     top = lanes_max<DealT::BLOCK_LANES>(valid ? top : 0.0f);
-    if (!valid) return;
-    const uint32_t code = scale_code(top);
-    const float up = scale_up(code);
     uint32_t q[DealT::E / 2];
+    uint32_t code;
+    if (__any_sync(0xffffffffu, top == INFINITY)) {                       // the scale goes by the finite values
+        float finite = 0.0f;
 #pragma unroll
-    for (int e = 0; e < DealT::E / 2; ++e) q[e] = codes_of(f[2 * e], f[2 * e + 1], up);
+        for (int e = 0; e < DealT::E; ++e) finite = fmaxf(finite, finite_magnitude(f[e]));
+        code = scale_code(lanes_max<DealT::BLOCK_LANES>(valid ? finite : 0.0f));
+        const float up = scale_up(code);
+#pragma unroll
+        for (int e = 0; e < DealT::E / 2; ++e) q[e] = codes_of(nan_for_inf(f[2 * e]) * up, nan_for_inf(f[2 * e + 1]) * up);
+    } else {
+        code = scale_code(top);
+        const float2 up = make_float2(scale_up(code), scale_up(code));
+#pragma unroll
+        for (int e = 0; e < DealT::E / 2; ++e) {
+            const float2 v = __fmul2_rn(make_float2(f[2 * e], f[2 * e + 1]), up);
+            q[e] = codes_of(v.x, v.y);
+        }
+    }
+    if (!valid) return;
     DealT::store_codes(codes, u, D, q);
     if (u % DealT::BLOCK_LANES == 0) scales[u / DealT::BLOCK_LANES] = (uint8_t)code;
 }
@@ -263,6 +298,13 @@ template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, true, TPR, U,
                      : "r"(base + (slot * U + k) * (TPR * 16)));
         DealT::S::unpack(w, f);
     }
+    __device__ __forceinline__ void centred(int slot, int k, float2 minus_mean, float2 (&c)[DealT::E / 2]) const
+    {
+        float f[DealT::E];
+        get(slot, k, f);
+#pragma unroll
+        for (int e = 0; e < DealT::E / 2; ++e) c[e] = __fadd2_rn(make_float2(f[2 * e], f[2 * e + 1]), minus_mean);
+    }
 };
 template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, false, TPR, U, S> {
     using DealT = Deal<DTYPE, false>;
@@ -282,6 +324,13 @@ template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, false, TPR, U
         for (int k = 0; k < U; ++k) now[k] = next[k];
     }
     __device__ __forceinline__ void get(int, int k, float (&f)[4]) const { now[k].get(f); }
+    __device__ __forceinline__ void centred(int, int k, float2 minus_mean, float2 (&c)[2]) const
+    {
+        float f[4];
+        now[k].get(f);
+        c[0] = __fadd2_rn(make_float2(f[0], f[1]), minus_mean);
+        c[1] = __fadd2_rn(make_float2(f[2], f[3]), minus_mean);
+    }
 };
 // The 8-bit form of the next rows, and the scales of the thread's units.
 template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
@@ -321,7 +370,7 @@ template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
             }
         }
     }
-    __device__ __forceinline__ void get(int slot, int k, float (&f)[E]) const
+    __device__ __forceinline__ void centred(int slot, int k, float2 minus_mean, float2 (&c)[E / 2]) const
     {
         uint32_t q[E / 2];
         if constexpr (!VEC) {
@@ -337,12 +386,10 @@ template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
             q[0] = lo & 0xffffu, q[1] = lo >> 16;
             if constexpr (E == 8) q[2] = hi & 0xffffu, q[3] = hi >> 16;
         }
-        const float down = scale_down(now_scale[k]);
+        // a code times a power of two is exact: one rounding, that of the difference
+        const float2 down = make_float2(scale_down(now_scale[k]), scale_down(now_scale[k]));
 #pragma unroll
-        for (int e = 0; e < E / 2; ++e) {
-            const float2 v = values_of(q[e], down);
-            f[2 * e] = v.x, f[2 * e + 1] = v.y;
-        }
+        for (int e = 0; e < E / 2; ++e) c[e] = __ffma2_rn(halves_of(q[e]), down, minus_mean);
     }
 };
 
@@ -448,6 +495,8 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const
                 const float2 d = __fadd2_rn(make_float2(f[k][e], f[k][e + 1]), minus_m);
                 if constexpr (VEC) {
                     if (t + k * TPR < units) sq2 = __ffma2_rn(d, d, sq2);
+                } else if (DealT::whole(t + k * TPR, D)) {
+                    sq2 = __ffma2_rn(d, d, sq2);
                 } else {
                     const int32_t u = t + k * TPR;
                     const float2 in = make_float2(DealT::has(u, e, D) ? d.x : 0.0f, DealT::has(u, e + 1, D) ? d.y : 0.0f);
@@ -573,7 +622,6 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
         grads.take();
         inputs.take();
         const float2 minus_mean = make_float2(-next_mean, -next_mean), r2 = make_float2(next_rstd, next_rstd);
-        const float rstd = next_rstd;
         start(LEAD == 0 ? slot : slot == 0 ? S - 1 : slot - 1, row + LEAD * step);
         start_scalars(row + step);
         if (VEC) copy_wait<LEAD>();
@@ -581,13 +629,14 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (t + k * TPR < units) {
-                float f[E], g[E];
-                inputs.get(slot, k, f);
+                float g[E];
+                float2 xc[E / 2];
+                inputs.centred(slot, k, minus_mean, xc);
                 grads.get(slot, k, g);
 #pragma unroll
                 for (int e = 0; e < E; e += 2) {
                     // columns that do not exist have g = 0 and w = 0
-                    const float2 xh = __fmul2_rn(__fadd2_rn(make_float2(f[e], f[e + 1]), minus_mean), r2);
+                    const float2 xh = __fmul2_rn(xc[e / 2], r2);
                     const float2 gy = make_float2(g[e], g[e + 1]), a = __fmul2_rn(gy, make_float2(w[k][e], w[k][e + 1]));
                     c1 = __fadd2_rn(c1, a);
                     c2 = __ffma2_rn(a, xh, c2);
@@ -609,20 +658,21 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
         }
         s1 *= -inv_d;
         s2 *= -inv_d;
-        const float2 m1 = make_float2(s1, s1), m2 = make_float2(s2, s2), rr = make_float2(rstd, rstd);
+        const float2 m1 = make_float2(s1, s1), m2 = make_float2(s2, s2);
         T *dst = static_cast<T *>(job.grad_x) + row * D;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             const int32_t u = t + k * TPR;
             if (u < units) {
-                float f[E], g[E], o[E];
-                inputs.get(slot, k, f);
+                float g[E], o[E];
+                float2 xc[E / 2];
+                inputs.centred(slot, k, minus_mean, xc);
                 grads.get(slot, k, g);
 #pragma unroll
                 for (int e = 0; e < E; e += 2) {
-                    const float2 xh = __fmul2_rn(__fadd2_rn(make_float2(f[e], f[e + 1]), minus_mean), r2);
-                    const float2 a = __fmul2_rn(make_float2(g[e], g[e + 1]), make_float2(w[k][e], w[k][e + 1]));
-                    const float2 d = __fmul2_rn(__ffma2_rn(xh, m2, __fadd2_rn(a, m1)), rr);
+                    const float2 xh = __fmul2_rn(xc[e / 2], r2);
+                    const float2 a = __ffma2_rn(make_float2(g[e], g[e + 1]), make_float2(w[k][e], w[k][e + 1]), m1);
+                    const float2 d = __fmul2_rn(__ffma2_rn(xh, m2, a), r2);
                     o[e] = d.x, o[e + 1] = d.y;
                 }
                 DealT::store(dst, u, D, o);
