@@ -15,6 +15,7 @@
 #include "../../include/ppow.h"
 #include "ppow_checked.cuh"
 #include "ppow_device.cuh"
+#include "ppow_mma.cuh"
 
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -215,36 +216,67 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// Packs one unit per lane (the whole warp calls; `valid` lanes hold a unit, the others any finite values).
-template <typename DealT>
-__device__ __forceinline__ void pack_unit(const float (&f)[DealT::E], bool valid, int32_t u, int32_t D, uint8_t *codes, uint8_t *scales)
+// 1 / sqrt(v): the approximation and one step of Newton's method, exact to about a step of float32
+__device__ __forceinline__ float inverse_root(float v)
 {
-    float top = 0.0f;
+    const float r = rsqrtf(v), h = 0.5f * v * r;
+    return v > 0.0f && v < INFINITY ? fmaf(r, fmaf(-h, r, 0.5f), r) : r;
+}
+
+template <int U> __device__ __forceinline__ float total_of(float2 (&v)[U])
+{
 #pragma unroll
-    for (int e = 0; e < DealT::E; ++e) top = fmaxf(top, fabsf(f[e]));      // passes NaN over
-    top = lanes_max<DealT::BLOCK_LANES>(valid ? top : 0.0f);
-    uint32_t q[DealT::E / 2];
-    uint32_t code;
-    if (__any_sync(0xffffffffu, top == INFINITY)) {                       // the scale goes by the finite values
-        float finite = 0.0f;
+    for (int h = U / 2; h > 0; h >>= 1)
 #pragma unroll
-        for (int e = 0; e < DealT::E; ++e) finite = fmaxf(finite, finite_magnitude(f[e]));
-        code = scale_code(lanes_max<DealT::BLOCK_LANES>(valid ? finite : 0.0f));
-        const float up = scale_up(code);
+        for (int k = 0; k < h; ++k) v[k] = __fadd2_rn(v[k], v[k + h]);
+    return v[0].x + v[0].y;
+}
+
+// Packs N units per lane, `step` units apart (the whole warp calls; lanes with no unit bring any finite values).
+template <typename DealT, int N>
+__device__ __forceinline__ void pack_units(const float (&f)[N][DealT::E], int32_t u0, int32_t step, int32_t units, int32_t D, uint8_t *codes,
+                                           uint8_t *scales)
+{
+    constexpr int E = DealT::E, LANES = DealT::BLOCK_LANES;
+    float top[N];
+    bool infinite = false;
 #pragma unroll
-        for (int e = 0; e < DealT::E / 2; ++e) q[e] = codes_of(nan_for_inf(f[2 * e]) * up, nan_for_inf(f[2 * e + 1]) * up);
-    } else {
-        code = scale_code(top);
+    for (int k = 0; k < N; ++k) {
+        float a = 0.0f, b = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; e += 2) a = fmaxf(a, fabsf(f[k][e])), b = fmaxf(b, fabsf(f[k][e + 1]));     // pass NaN over
+        top[k] = u0 + k * step < units ? fmaxf(a, b) : 0.0f;
+    }
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], o));
+#pragma unroll
+    for (int k = 0; k < N; ++k) infinite = infinite || top[k] == INFINITY;
+    infinite = __any_sync(0xffffffffu, infinite);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int32_t u = u0 + k * step;
+        uint32_t q[E / 2], code = scale_code(top[k]);
+        if (infinite) {                                                   // the scale goes by the finite values
+            float finite = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) finite = fmaxf(finite, finite_magnitude(f[k][e]));
+            code = scale_code(lanes_max<LANES>(u < units ? finite : 0.0f));
+        }
         const float2 up = make_float2(scale_up(code), scale_up(code));
 #pragma unroll
-        for (int e = 0; e < DealT::E / 2; ++e) {
-            const float2 v = __fmul2_rn(make_float2(f[2 * e], f[2 * e + 1]), up);
+        for (int e = 0; e < E / 2; ++e) {
+            float2 v = make_float2(f[k][2 * e], f[k][2 * e + 1]);
+            if (infinite) v = make_float2(nan_for_inf(v.x), nan_for_inf(v.y));
+            v = __fmul2_rn(v, up);
             q[e] = codes_of(v.x, v.y);
         }
+        if (u < units) {
+            DealT::store_codes(codes, u, D, q);
+            if (u % LANES == 0) scales[u / LANES] = (uint8_t)code;
+        }
     }
-    if (!valid) return;
-    DealT::store_codes(codes, u, D, q);
-    if (u % DealT::BLOCK_LANES == 0) scales[u / DealT::BLOCK_LANES] = (uint8_t)code;
 }
 
 __device__ __forceinline__ float load_param(const void *p, int32_t dtype, int32_t i)
@@ -298,7 +330,7 @@ template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, true, TPR, U,
                      : "r"(base + (slot * U + k) * (TPR * 16)));
         DealT::S::unpack(w, f);
     }
-    __device__ __forceinline__ void centred(int slot, int k, float2 minus_mean, float2 (&c)[DealT::E / 2]) const
+    __device__ __forceinline__ void centred(int slot, int k, float, float2 minus_mean, float2 (&c)[DealT::E / 2]) const
     {
         float f[DealT::E];
         get(slot, k, f);
@@ -324,7 +356,7 @@ template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, false, TPR, U
         for (int k = 0; k < U; ++k) now[k] = next[k];
     }
     __device__ __forceinline__ void get(int, int k, float (&f)[4]) const { now[k].get(f); }
-    __device__ __forceinline__ void centred(int, int k, float2 minus_mean, float2 (&c)[2]) const
+    __device__ __forceinline__ void centred(int, int k, float, float2 minus_mean, float2 (&c)[2]) const
     {
         float f[4];
         now[k].get(f);
@@ -339,7 +371,6 @@ template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
     static constexpr size_t BYTES = VEC ? (size_t)S * U * TPR * E : 0;
     uint32_t base;
     uint32_t next[VEC ? 1 : U][E / 2], now[VEC ? 1 : U][E / 2];
-    uint8_t next_scale[U], now_scale[U];
     __device__ __forceinline__ CodesAhead(void *smem, int t) : base(smem_address(smem) + t * E) {}
     __device__ __forceinline__ void start(int slot, const uint8_t *row, int t, int32_t units, int32_t D)
     {
@@ -352,25 +383,14 @@ template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
                     DealT::load_codes(row, t + k * TPR, D, next[k]);
             }
     }
-    // one row ahead in registers: a byte is too small for an asynchronous copy
-    __device__ __forceinline__ void start_scales(const uint8_t *scales, int t, int32_t units)
-    {
-#pragma unroll
-        for (int k = 0; k < U; ++k)
-            if (t + k * TPR < units) next_scale[k] = __ldcs(scales + (t + k * TPR) / DealT::BLOCK_LANES);
-    }
     __device__ __forceinline__ void take()
     {
 #pragma unroll
-        for (int k = 0; k < U; ++k) {
-            now_scale[k] = next_scale[k];
-            if constexpr (!VEC) {
+        for (int k = 0; k < (VEC ? 0 : U); ++k)
 #pragma unroll
-                for (int e = 0; e < E / 2; ++e) now[k][e] = next[k][e];
-            }
-        }
+            for (int e = 0; e < E / 2; ++e) now[k][e] = next[k][e];
     }
-    __device__ __forceinline__ void centred(int slot, int k, float2 minus_mean, float2 (&c)[E / 2]) const
+    __device__ __forceinline__ void centred(int slot, int k, float scale, float2 minus_mean, float2 (&c)[E / 2]) const
     {
         uint32_t q[E / 2];
         if constexpr (!VEC) {
@@ -387,9 +407,45 @@ template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
             if constexpr (E == 8) q[2] = hi & 0xffffu, q[3] = hi >> 16;
         }
         // a code times a power of two is exact: one rounding, that of the difference
-        const float2 down = make_float2(scale_down(now_scale[k]), scale_down(now_scale[k]));
+        const float2 down = make_float2(scale, scale);
 #pragma unroll
         for (int e = 0; e < E / 2; ++e) c[e] = __ffma2_rn(halves_of(q[e]), down, minus_mean);
+    }
+};
+
+// Mean, rstd and the scales of the thread's units, for the next rows: four-byte copies into the thread's own words (loaded into
+// registers a row ahead they held the loop up: 16384 x 4096 took 28 us more).  A scale is a byte: the aligned word around it
+// is copied.
+template <typename DealT, bool PACKED, int TPR, int U, int S> struct ScalarsAhead {
+    static constexpr int WORDS = 2 + (PACKED ? U : 0);
+    static constexpr size_t BYTES = (size_t)S * WORDS * TPR * 4;
+    uint32_t base;
+    __device__ __forceinline__ ScalarsAhead(void *smem, int t) : base(smem_address(smem) + t * 4) {}
+    __device__ __forceinline__ uint32_t word(int slot, int i) const { return base + (slot * WORDS + i) * (TPR * 4); }
+    __device__ __forceinline__ void start(int slot, const float *mean, const float *rstd, const uint8_t *scales, int t, int32_t units)
+    {
+        copy_async<4>(word(slot, 0), mean);
+        copy_async<4>(word(slot, 1), rstd);
+        if constexpr (PACKED) {
+#pragma unroll
+            for (int k = 0; k < U; ++k)
+                if (t + k * TPR < units)
+                    copy_async<4>(word(slot, 2 + k), reinterpret_cast<const void *>((uintptr_t)(scales + (t + k * TPR) / DealT::BLOCK_LANES) & ~(uintptr_t)3));
+        }
+    }
+    __device__ __forceinline__ uint32_t get(int slot, int i) const
+    {
+        uint32_t w;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(word(slot, i)));
+        return w;
+    }
+    __device__ __forceinline__ float scale(int slot, int k, const uint8_t *scales, int t) const
+    {
+        if constexpr (PACKED) {
+            const uint32_t at = (uint32_t)(uintptr_t)(scales + (t + k * TPR) / DealT::BLOCK_LANES) & 3u;
+            return scale_down(__byte_perm(get(slot, 2 + k), 0, 0x4440u | at));
+        }
+        return 1.0f;
     }
 };
 
@@ -412,14 +468,16 @@ template <bool VEC> __host__ __device__ constexpr int norm_values() { return VEC
 template <int DTYPE, bool VEC> __host__ __device__ constexpr int norm_units() { return norm_values<VEC>() / (VEC && DTYPE != PPOW_F32 ? 8 : 4); }
 // Rows in flight: about 16 to 64 KB of shared memory per CTA.
 template <int DTYPE, int TPR> __host__ __device__ constexpr int forward_slots() { return TPR <= 128 ? 4 : TPR == 256 ? 3 : 2; }
-template <int DTYPE, int TPR> __host__ __device__ constexpr int backward_slots()
+template <int DTYPE, bool VEC, int TPR> __host__ __device__ constexpr int backward_slots()
 {
-    return TPR <= 128 ? 3 : TPR == 256 || DTYPE != PPOW_F32 ? 2 : 1;
+    return !VEC || DTYPE == PPOW_F32 ? (VEC && TPR > 256 ? 1 : 2) : TPR <= 128 ? 4 : 2;
 }
 
 template <int DTYPE, bool VEC, int TPR>
 __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const NormJob job)
 {
+    allow_next_kernel();
+    wait_for_previous_kernel();
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
     constexpr int E = DealT::E, U = norm_units<DTYPE, VEC>(), S = forward_slots<DTYPE, TPR>();
@@ -427,7 +485,7 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const
     using Ahead = RowAhead<DTYPE, VEC, TPR, U, S>;
     extern __shared__ uint4 slots[];
     __shared__ float2 part[2][WARPS];                        // per warp: sum, sum of squares about the warp's own mean
-    __shared__ float counts[WARPS];
+    __shared__ float2 counts[WARPS];                         // values that a warp holds, and one over that
     const int t = threadIdx.x % TPR, lane = threadIdx.x & 31, group = threadIdx.x / TPR;
     const int32_t D = job.D, units = DealT::units(D);
     if (!PPOW_CHECK(units <= TPR * U, 601, nullptr)) return;
@@ -446,7 +504,7 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const
     const float in_warp = (float)__reduce_add_sync(0xffffffffu, mine);
     const float inv_warp = in_warp > 0.0f ? 1.0f / in_warp : 0.0f, inv_d = 1.0f / (float)D;
     if (WARPS > 1) {
-        if (lane == 0) counts[t >> 5] = in_warp;
+        if (lane == 0) counts[t >> 5] = make_float2(in_warp, inv_warp);
         __syncthreads();
     }
 
@@ -472,7 +530,7 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const
             }
         }
         float f[U][E];
-        float2 sum2 = make_float2(0.0f, 0.0f);
+        float2 sum2[U];                                      // a chain of additions per unit
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (t + k * TPR < units) {
@@ -481,29 +539,32 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const
 #pragma unroll
                 for (int e = 0; e < E; ++e) f[k][e] = 0.0f;
             }
+            sum2[k] = make_float2(f[k][0], f[k][1]);
 #pragma unroll
-            for (int e = 0; e < E; e += 2) sum2 = __fadd2_rn(sum2, make_float2(f[k][e], f[k][e + 1]));
+            for (int e = 2; e < E; e += 2) sum2[k] = __fadd2_rn(sum2[k], make_float2(f[k][e], f[k][e + 1]));
         }
         // sum of the warp's values, then squares about their mean: no difference of large sums
-        const float sum = warp_sum(sum2.x + sum2.y), m = sum * inv_warp;
+        const float sum = warp_sum(total_of(sum2)), m = sum * inv_warp;
         const float2 minus_m = make_float2(-m, -m);
-        float2 sq2 = make_float2(0.0f, 0.0f);
+        float2 sq2[U];
 #pragma unroll
-        for (int k = 0; k < U; ++k)
+        for (int k = 0; k < U; ++k) {
+            sq2[k] = make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
                 const float2 d = __fadd2_rn(make_float2(f[k][e], f[k][e + 1]), minus_m);
                 if constexpr (VEC) {
-                    if (t + k * TPR < units) sq2 = __ffma2_rn(d, d, sq2);
+                    if (t + k * TPR < units) sq2[k] = __ffma2_rn(d, d, sq2[k]);
                 } else if (DealT::whole(t + k * TPR, D)) {
-                    sq2 = __ffma2_rn(d, d, sq2);
+                    sq2[k] = __ffma2_rn(d, d, sq2[k]);
                 } else {
                     const int32_t u = t + k * TPR;
                     const float2 in = make_float2(DealT::has(u, e, D) ? d.x : 0.0f, DealT::has(u, e + 1, D) ? d.y : 0.0f);
-                    sq2 = __ffma2_rn(in, in, sq2);
+                    sq2[k] = __ffma2_rn(in, in, sq2[k]);
                 }
             }
-        const float sq = warp_sum(sq2.x + sq2.y);
+        }
+        const float sq = warp_sum(total_of(sq2));
         float mean = m, squares = sq;
         if (WARPS > 1) {
             // squares about the row's mean: each warp's squares about its own, plus its count times the gap squared
@@ -516,11 +577,12 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const
             squares = 0.0f;
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) {
-                const float n = counts[i], gap = n > 0.0f ? part[turn][i].x / n - mean : 0.0f;
-                squares += part[turn][i].y + n * gap * gap;
+                const float2 n = counts[i], p = part[turn][i];
+                const float gap = fmaf(p.x, n.y, -mean);
+                squares += fmaf(n.x * gap, gap, p.y);
             }
         }
-        const float rstd = 1.0f / sqrtf(squares * inv_d + job.eps);
+        const float rstd = inverse_root(fmaf(squares, inv_d, job.eps));
         const float2 minus_mean = make_float2(-mean, -mean), r2 = make_float2(rstd, rstd);
         T *dst = static_cast<T *>(job.y) + row * D;
 #pragma unroll
@@ -542,9 +604,7 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const
             job.rstd[row] = rstd;
         }
         if (job.codes) {
-#pragma unroll
-            for (int k = 0; k < U; ++k)
-                pack_unit<DealT>(f[k], t + k * TPR < units, t + k * TPR, D, job.codes + row * D, job.scales + row * job.blocks);
+            pack_units<DealT, U>(f, t, TPR, units, D, job.codes + row * D, job.scales + row * job.blocks);
         }
         slot = slot == S - 1 ? 0 : slot + 1;
     }
@@ -569,9 +629,11 @@ struct NormGradJob {
 template <int DTYPE, bool VEC, bool PACKED, int TPR>
 __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(const NormGradJob job)
 {
+    allow_next_kernel();
+    wait_for_previous_kernel();
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
-    constexpr int E = DealT::E, U = norm_units<DTYPE, VEC>(), S = backward_slots<DTYPE, TPR>();
+    constexpr int E = DealT::E, U = norm_units<DTYPE, VEC>(), S = backward_slots<DTYPE, VEC, TPR>();
     constexpr int ROWS = norm_threads<TPR>() / TPR, WARPS = TPR / 32;
     using Grads = RowAhead<DTYPE, VEC, TPR, U, S>;
     using Inputs = std::conditional_t<PACKED, CodesAhead<DTYPE, VEC, TPR, U, S>, RowAhead<DTYPE, VEC, TPR, U, S>>;
@@ -592,11 +654,12 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
             dw[k][e / 2] = db[k][e / 2] = make_float2(0.0f, 0.0f);
         }
     const int64_t step = (int64_t)gridDim.x * ROWS, first = (int64_t)blockIdx.x * ROWS + group;
-    uint8_t *own = reinterpret_cast<uint8_t *>(slots) + group * (Grads::BYTES + Inputs::BYTES);
+    using Scalars = ScalarsAhead<DealT, PACKED, TPR, U, S>;
+    uint8_t *own = reinterpret_cast<uint8_t *>(slots) + group * (Grads::BYTES + Inputs::BYTES + Scalars::BYTES);
     Grads grads(own, t);
     Inputs inputs(own + Grads::BYTES, t);
-    constexpr int LEAD = VEC ? S - 1 : 1;
-    float next_mean = 0.0f, next_rstd = 0.0f;
+    Scalars scalars(own + Grads::BYTES + Inputs::BYTES, t);
+    constexpr int LEAD = S - 1;
     auto start = [&](int slot, int64_t row) {
         if (row < job.R) {
             grads.start(slot, static_cast<const T *>(job.grad_y) + row * job.grad_y_stride, t, units, D);
@@ -604,48 +667,45 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
                 inputs.start(slot, job.codes + row * D, t, units, D);
             else
                 inputs.start(slot, static_cast<const T *>(job.x) + row * job.x_stride, t, units, D);
+            scalars.start(slot, job.mean + row, job.rstd + row, job.scales + row * job.blocks, t, units);
         }
-        if (VEC) copy_commit();
-    };
-    auto start_scalars = [&](int64_t row) {
-        if (row < job.R) {
-            next_mean = job.mean[row];
-            next_rstd = job.rstd[row];
-            if constexpr (PACKED) inputs.start_scales(job.scales + row * job.blocks, t, units);
-        }
+        copy_commit();
     };
 #pragma unroll
     for (int i = 0; i < LEAD; ++i) start(i, first + i * step);
-    start_scalars(first);
     int slot = 0, turn = 0;
     for (int64_t row = first; row < job.R; row += step, turn ^= 1) {
         grads.take();
         inputs.take();
-        const float2 minus_mean = make_float2(-next_mean, -next_mean), r2 = make_float2(next_rstd, next_rstd);
-        start(LEAD == 0 ? slot : slot == 0 ? S - 1 : slot - 1, row + LEAD * step);
-        start_scalars(row + step);
-        if (VEC) copy_wait<LEAD>();
-        float2 c1 = make_float2(0.0f, 0.0f), c2 = c1;
+        start(slot == 0 ? S - 1 : slot - 1, row + LEAD * step);          // S == 1: the row itself
+        copy_wait<LEAD>();
+        const float mean = __uint_as_float(scalars.get(slot, 0)), rstd = __uint_as_float(scalars.get(slot, 1));
+        const float2 minus_mean = make_float2(-mean, -mean), r2 = make_float2(rstd, rstd);
+        float scale[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) scale[k] = scalars.scale(slot, k, job.scales + row * job.blocks, t);
+        float2 c1[U], c2[U];
 #pragma unroll
         for (int k = 0; k < U; ++k) {
+            c1[k] = c2[k] = make_float2(0.0f, 0.0f);
             if (t + k * TPR < units) {
                 float g[E];
                 float2 xc[E / 2];
-                inputs.centred(slot, k, minus_mean, xc);
+                inputs.centred(slot, k, scale[k], minus_mean, xc);
                 grads.get(slot, k, g);
 #pragma unroll
                 for (int e = 0; e < E; e += 2) {
                     // columns that do not exist have g = 0 and w = 0
                     const float2 xh = __fmul2_rn(xc[e / 2], r2);
                     const float2 gy = make_float2(g[e], g[e + 1]), a = __fmul2_rn(gy, make_float2(w[k][e], w[k][e + 1]));
-                    c1 = __fadd2_rn(c1, a);
-                    c2 = __ffma2_rn(a, xh, c2);
+                    c1[k] = __fadd2_rn(c1[k], a);
+                    c2[k] = __ffma2_rn(a, xh, c2[k]);
                     dw[k][e / 2] = __ffma2_rn(gy, xh, dw[k][e / 2]);
                     db[k][e / 2] = __fadd2_rn(db[k][e / 2], gy);
                 }
             }
         }
-        float s1 = warp_sum(c1.x + c1.y), s2 = warp_sum(c2.x + c2.y);
+        float s1 = warp_sum(total_of(c1)), s2 = warp_sum(total_of(c2));
         if (WARPS > 1) {
             if (lane == 0) part[turn][t >> 5] = make_float2(s1, s2);
             __syncthreads();
@@ -666,7 +726,7 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
             if (u < units) {
                 float g[E], o[E];
                 float2 xc[E / 2];
-                inputs.centred(slot, k, minus_mean, xc);
+                inputs.centred(slot, k, scale[k], minus_mean, xc);
                 grads.get(slot, k, g);
 #pragma unroll
                 for (int e = 0; e < E; e += 2) {
@@ -717,16 +777,28 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
 }
 
 // Column sums over the CTAs' shares, in a fixed order: 32 columns by 8 groups of shares per CTA.
-constexpr int JOIN_GROUPS = 8;
+constexpr int JOIN_GROUPS = 16;
 __global__ void __launch_bounds__(32 * JOIN_GROUPS) norm_join_kernel(const float *__restrict__ partial, int32_t shares, int32_t D,
                                                                      int32_t param_dtype, void *grad_weight, void *grad_bias)
 {
     __shared__ float group[JOIN_GROUPS][32];
     const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
     const int32_t c = blockIdx.x * 32 + lane;        // column of dw, then of db
+    allow_next_kernel();
+    wait_for_previous_kernel();
     float sum = 0.0f;
-    if (c < 2 * D)
-        for (int32_t s = g; s < shares; s += JOIN_GROUPS) sum += partial[(size_t)s * 2 * D + c];
+    if (c < 2 * D) {
+        const float *p = partial + c;
+        int32_t s = g;
+        for (; s + 7 * JOIN_GROUPS < shares; s += 8 * JOIN_GROUPS) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = p[(size_t)(s + i * JOIN_GROUPS) * 2 * D];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+        for (; s < shares; s += JOIN_GROUPS) sum += p[(size_t)s * 2 * D];
+    }
     group[g][lane] = sum;
     __syncthreads();
     if (g == 0 && c < 2 * D) {
@@ -774,6 +846,8 @@ struct ChunkWalk {
 template <int DTYPE, bool VEC>
 __global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const PackJob job)
 {
+    allow_next_kernel();
+    wait_for_previous_kernel();
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
     const int lane = threadIdx.x & 31;
@@ -791,15 +865,17 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const PackJob job)
     for (int i = 0; i < PACK_CHUNKS; ++i, at.step(per_row)) {
         const int32_t u = at.chunk * 32 + lane;
         if (at.row >= job.R || !PPOW_CHECK(at.chunk < per_row, 603, nullptr)) return;
-        float f[DealT::E];
-        x[i].get(f);
-        pack_unit<DealT>(f, u < units, u, job.D, job.codes + at.row * job.D, job.scales + at.row * job.blocks);
+        float f[1][DealT::E];
+        x[i].get(f[0]);
+        pack_units<DealT, 1>(f, u, 0, units, job.D, job.codes + at.row * job.D, job.scales + at.row * job.blocks);
     }
 }
 
 template <int DTYPE, bool VEC>
 __global__ void __launch_bounds__(PACK_THREADS) unpack_kernel(const PackJob job)
 {
+    allow_next_kernel();
+    wait_for_previous_kernel();
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
     const int lane = threadIdx.x & 31;
@@ -884,8 +960,7 @@ bool forward_launch(const NormJob &job, cudaStream_t stream)
     static Resident known;
     const int64_t need = ((int64_t)job.R + ROWS - 1) / ROWS, most = resident_ctas(known, kernel, THREADS, SMEM);
     if (most < 1) return false;
-    kernel<<<(unsigned)(need < most ? need : most), THREADS, SMEM, stream>>>(job);
-    return cudaGetLastError() == cudaSuccess;
+    return launch_after(kernel, (unsigned)(need < most ? need : most), THREADS, SMEM, stream, job);
 }
 
 // The fewest threads that hold a row.
@@ -896,16 +971,17 @@ bool forward_shape(const NormJob &job, cudaStream_t stream)
     if (job.D <= 32 * HELD) return forward_launch<DTYPE, VEC, 32>(job, stream);
     if (job.D <= 128 * HELD) return forward_launch<DTYPE, VEC, 128>(job, stream);
     if (job.D <= 256 * HELD) return forward_launch<DTYPE, VEC, 256>(job, stream);
-    if (VEC || job.D <= 512 * HELD) return forward_launch<DTYPE, VEC, 512>(job, stream);
-    return forward_launch<DTYPE, VEC, VEC ? 512 : 1024>(job, stream);
+    if (512 * HELD >= NORM_MAX_WIDTH || job.D <= 512 * HELD) return forward_launch<DTYPE, VEC, 512>(job, stream);
+    return forward_launch<DTYPE, VEC, 512 * HELD >= NORM_MAX_WIDTH ? 512 : 1024>(job, stream);
 }
 
 template <int DTYPE, bool VEC, bool PACKED, int TPR>
 bool backward_launch(const NormGradJob &job, int32_t *shares, cudaStream_t stream)
 {
-    constexpr int THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR, U = norm_units<DTYPE, VEC>(), S = backward_slots<DTYPE, TPR>();
+    constexpr int THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR, U = norm_units<DTYPE, VEC>(), S = backward_slots<DTYPE, VEC, TPR>();
     constexpr size_t ROW = RowAhead<DTYPE, VEC, TPR, U, S>::BYTES;
-    constexpr size_t SMEM = ROWS * (ROW + (PACKED ? CodesAhead<DTYPE, VEC, TPR, U, S>::BYTES : ROW));
+    constexpr size_t SMEM = ROWS * (ROW + (PACKED ? CodesAhead<DTYPE, VEC, TPR, U, S>::BYTES : ROW) +
+                                    ScalarsAhead<Deal<DTYPE, VEC>, PACKED, TPR, U, S>::BYTES);
     auto kernel = norm_backward_kernel<DTYPE, VEC, PACKED, TPR>;
     static Resident known;
     const int64_t most = resident_ctas(known, kernel, THREADS, SMEM);
@@ -914,8 +990,7 @@ bool backward_launch(const NormGradJob &job, int32_t *shares, cudaStream_t strea
     if (n > most) n = most;
     if (n > SHARES_MAX) n = SHARES_MAX;
     *shares = (int32_t)n;
-    kernel<<<(unsigned)n, THREADS, SMEM, stream>>>(job);
-    return cudaGetLastError() == cudaSuccess;
+    return launch_after(kernel, (unsigned)n, THREADS, SMEM, stream, job);
 }
 
 template <int DTYPE, bool VEC, bool PACKED>
@@ -925,8 +1000,8 @@ bool backward_shape(const NormGradJob &job, int32_t *shares, cudaStream_t stream
     if (job.D <= 32 * HELD) return backward_launch<DTYPE, VEC, PACKED, 32>(job, shares, stream);
     if (job.D <= 128 * HELD) return backward_launch<DTYPE, VEC, PACKED, 128>(job, shares, stream);
     if (job.D <= 256 * HELD) return backward_launch<DTYPE, VEC, PACKED, 256>(job, shares, stream);
-    if (VEC || job.D <= 512 * HELD) return backward_launch<DTYPE, VEC, PACKED, 512>(job, shares, stream);
-    return backward_launch<DTYPE, VEC, PACKED, VEC ? 512 : 1024>(job, shares, stream);
+    if (512 * HELD >= NORM_MAX_WIDTH || job.D <= 512 * HELD) return backward_launch<DTYPE, VEC, PACKED, 512>(job, shares, stream);
+    return backward_launch<DTYPE, VEC, PACKED, 512 * HELD >= NORM_MAX_WIDTH ? 512 : 1024>(job, shares, stream);
 }
 
 template <int DTYPE, bool VEC>
@@ -935,11 +1010,7 @@ bool pack_launch(const PackJob &job, bool unpack, cudaStream_t stream)
     const int32_t units = VEC ? job.D / (16 / (int32_t)bytes_of(DTYPE)) : (job.D + CKPT_BLOCK - 1) / CKPT_BLOCK * 32;
     const int64_t chunks = (int64_t)job.R * ((units + 31) / 32), per_cta = PACK_THREADS / 32 * PACK_CHUNKS;
     const unsigned grid = (unsigned)((chunks + per_cta - 1) / per_cta);
-    if (unpack)
-        unpack_kernel<DTYPE, VEC><<<grid, PACK_THREADS, 0, stream>>>(job);
-    else
-        pack_kernel<DTYPE, VEC><<<grid, PACK_THREADS, 0, stream>>>(job);
-    return cudaGetLastError() == cudaSuccess;
+    return launch_after(unpack ? unpack_kernel<DTYPE, VEC> : pack_kernel<DTYPE, VEC>, grid, PACK_THREADS, 0, stream, job);
 }
 
 #define PPOW_BY_TYPE(dtype, vec, CALL)                                                                          \
@@ -1012,9 +1083,9 @@ extern "C" ppow_status ppow_layer_norm_backward(const ppow_norm_params *params, 
     if (!PPOW_BY_TYPE(params->dtype, vec, PPOW_CALL)) return PPOW_ERR_CUDA;
 #undef PPOW_CALL
     if (grad_weight || grad_bias) {
-        norm_join_kernel<<<(unsigned)((2 * params->D + 31) / 32), 32 * JOIN_GROUPS, 0, stream>>>(job.partial, shares, params->D,
-                                                                                             params->param_dtype, grad_weight, grad_bias);
-        if (cudaGetLastError() != cudaSuccess) return PPOW_ERR_CUDA;
+        if (!launch_after(norm_join_kernel, (unsigned)((2 * params->D + 31) / 32), 32 * JOIN_GROUPS, 0, stream, job.partial, shares, params->D,
+                          params->param_dtype, grad_weight, grad_bias))
+            return PPOW_ERR_CUDA;
     }
     return PPOW_OK;
 }
