@@ -312,8 +312,9 @@ template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, true, TPR, U,
     using DealT = Deal<DTYPE, true>;
     using T = typename DealT::T;
     static constexpr size_t BYTES = (size_t)S * U * TPR * 16;       // per row group
-    uint32_t base;                                                  // this thread's first unit in slot 0
-    __device__ __forceinline__ RowAhead(void *smem, int t) : base(smem_address(smem) + t * 16) {}
+    uint8_t *own;                                                   // this thread's first unit in slot 0
+    uint32_t base;
+    __device__ __forceinline__ RowAhead(uint8_t *smem, int t) : own(smem + t * 16), base(smem_address(own)) {}
     __device__ __forceinline__ void start(int slot, const T *row, int t, int32_t units, int32_t)
     {
 #pragma unroll
@@ -324,10 +325,7 @@ template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, true, TPR, U,
     // units behind the row's end read as whatever the slot holds: callers use them only where t + k * TPR < units
     __device__ __forceinline__ void get(int slot, int k, float (&f)[DealT::E]) const
     {
-        uint4 w;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
-                     : "r"(base + (slot * U + k) * (TPR * 16)));
+        const uint4 w = *reinterpret_cast<const uint4 *>(own + (slot * U + k) * (TPR * 16));
         DealT::S::unpack(w, f);
     }
     __device__ __forceinline__ void centred(int slot, int k, float, float2 minus_mean, float2 (&c)[DealT::E / 2]) const
@@ -343,7 +341,7 @@ template <int DTYPE, int TPR, int U, int S> struct RowAhead<DTYPE, false, TPR, U
     using T = typename DealT::T;
     static constexpr size_t BYTES = 0;
     DealT next[U], now[U];
-    __device__ __forceinline__ RowAhead(void *, int) {}
+    __device__ __forceinline__ RowAhead(uint8_t *, int) {}
     __device__ __forceinline__ void start(int, const T *row, int t, int32_t units, int32_t D)
     {
 #pragma unroll
@@ -369,9 +367,10 @@ template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
     using DealT = Deal<DTYPE, VEC>;
     static constexpr int E = DealT::E;
     static constexpr size_t BYTES = VEC ? (size_t)S * U * TPR * E : 0;
+    uint8_t *own;
     uint32_t base;
     uint32_t next[VEC ? 1 : U][E / 2], now[VEC ? 1 : U][E / 2];
-    __device__ __forceinline__ CodesAhead(void *smem, int t) : base(smem_address(smem) + t * E) {}
+    __device__ __forceinline__ CodesAhead(uint8_t *smem, int t) : own(smem + t * E), base(smem_address(own)) {}
     __device__ __forceinline__ void start(int slot, const uint8_t *row, int t, int32_t units, int32_t D)
     {
 #pragma unroll
@@ -397,12 +396,14 @@ template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
 #pragma unroll
             for (int e = 0; e < E / 2; ++e) q[e] = now[k][e];
         } else {
-            const uint32_t at = base + (slot * U + k) * (TPR * E);
+            const uint32_t *at = reinterpret_cast<const uint32_t *>(own + (slot * U + k) * (TPR * E));
             uint32_t lo, hi = 0;
-            if constexpr (E == 8)
-                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(lo), "=r"(hi) : "r"(at));
-            else
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(lo) : "r"(at));
+            if constexpr (E == 8) {
+                const uint2 both = *reinterpret_cast<const uint2 *>(at);
+                lo = both.x, hi = both.y;
+            } else {
+                lo = *at;
+            }
             q[0] = lo & 0xffffu, q[1] = lo >> 16;
             if constexpr (E == 8) q[2] = hi & 0xffffu, q[3] = hi >> 16;
         }
@@ -413,37 +414,38 @@ template <int DTYPE, bool VEC, int TPR, int U, int S> struct CodesAhead {
     }
 };
 
-// Mean, rstd and the scales of the thread's units, for the next rows: four-byte copies into the thread's own words (loaded into
-// registers a row ahead they held the loop up: 16384 x 4096 took 28 us more).  A scale is a byte: the aligned word around it
-// is copied.
+// Mean, rstd and the scales of a warp's blocks, for the next rows: one four-byte copy per word and warp, each by a lane of its own
+// (loaded into registers a row ahead they held the loop up; copied by every lane for itself each copy takes 32 shared-memory
+// cycles.  16384 x 4096: 28 us more either way).  A scale is a byte: the aligned word around it is copied.
 template <typename DealT, bool PACKED, int TPR, int U, int S> struct ScalarsAhead {
-    static constexpr int WORDS = 2 + (PACKED ? U : 0);
-    static constexpr size_t BYTES = (size_t)S * WORDS * TPR * 4;
-    uint32_t base;
-    __device__ __forceinline__ ScalarsAhead(void *smem, int t) : base(smem_address(smem) + t * 4) {}
-    __device__ __forceinline__ uint32_t word(int slot, int i) const { return base + (slot * WORDS + i) * (TPR * 4); }
+    static constexpr int LANES = DealT::BLOCK_LANES, PER_UNIT = 32 / LANES;      // blocks that a warp's 32 units span
+    static constexpr int WORDS = 2 + (PACKED ? U * PER_UNIT : 0);
+    static_assert(WORDS <= 32, "one lane per word");
+    static constexpr size_t BYTES = (size_t)S * (TPR / 32) * WORDS * 4 + 16;
+    uint32_t *own;                   // the warp's words in slot 0
+    __device__ __forceinline__ ScalarsAhead(uint8_t *smem, int t) : own(reinterpret_cast<uint32_t *>(smem) + t / 32 * WORDS) {}
+    static __device__ __forceinline__ int32_t block_of(int t, int k, int j) { return ((t & ~31) + k * TPR) / LANES + j; }
+    __device__ __forceinline__ uint32_t *word(int slot, int i) const { return own + slot * (TPR / 32 * WORDS) + i; }
     __device__ __forceinline__ void start(int slot, const float *mean, const float *rstd, const uint8_t *scales, int t, int32_t units)
     {
-        copy_async<4>(word(slot, 0), mean);
-        copy_async<4>(word(slot, 1), rstd);
-        if constexpr (PACKED) {
-#pragma unroll
-            for (int k = 0; k < U; ++k)
-                if (t + k * TPR < units)
-                    copy_async<4>(word(slot, 2 + k), reinterpret_cast<const void *>((uintptr_t)(scales + (t + k * TPR) / DealT::BLOCK_LANES) & ~(uintptr_t)3));
+        const int lane = t & 31;
+        const void *src = lane == 0 ? mean : rstd;
+        bool has = lane < 2;
+        if (PACKED && lane >= 2 && lane < WORDS) {
+            const int32_t block = block_of(t, (lane - 2) / PER_UNIT, (lane - 2) % PER_UNIT);
+            has = block * LANES < units;
+            src = reinterpret_cast<const void *>((uintptr_t)(scales + block) & ~(uintptr_t)3);
         }
+        if (has) copy_async<4>(smem_address(word(slot, lane)), src);
     }
-    __device__ __forceinline__ uint32_t get(int slot, int i) const
-    {
-        uint32_t w;
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(word(slot, i)));
-        return w;
-    }
+    // after the copies have been waited for and the warp has met
+    __device__ __forceinline__ float get(int slot, int i) const { return __uint_as_float(*word(slot, i)); }
     __device__ __forceinline__ float scale(int slot, int k, const uint8_t *scales, int t) const
     {
         if constexpr (PACKED) {
-            const uint32_t at = (uint32_t)(uintptr_t)(scales + (t + k * TPR) / DealT::BLOCK_LANES) & 3u;
-            return scale_down(__byte_perm(get(slot, 2 + k), 0, 0x4440u | at));
+            const int j = (t & 31) / LANES;
+            const uint32_t at = (uint32_t)(uintptr_t)(scales + block_of(t, k, j)) & 3u;
+            return scale_down(__byte_perm(*word(slot, 2 + k * PER_UNIT + j), 0, 0x4440u | at));
         }
         return 1.0f;
     }
@@ -679,7 +681,8 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
         inputs.take();
         start(slot == 0 ? S - 1 : slot - 1, row + LEAD * step);          // S == 1: the row itself
         copy_wait<LEAD>();
-        const float mean = __uint_as_float(scalars.get(slot, 0)), rstd = __uint_as_float(scalars.get(slot, 1));
+        __syncwarp();
+        const float mean = scalars.get(slot, 0), rstd = scalars.get(slot, 1);
         const float2 minus_mean = make_float2(-mean, -mean), r2 = make_float2(rstd, rstd);
         float scale[U];
 #pragma unroll
