@@ -6,6 +6,7 @@ PyTorch is used for device memory and streams only.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -518,7 +519,7 @@ def _raw_stream(stream, dev: int) -> int:
 
 def _call(fn, where, dev: int, *args) -> None:
     """Calls the library with device ``dev`` current."""
-    if torch.cuda.current_device() == dev:
+    if torch._C._cuda_getDevice() == dev:
         st = fn(*args)
     else:
         with torch.cuda.device(dev):
@@ -527,20 +528,13 @@ def _call(fn, where, dev: int, *args) -> None:
         raise PpowError(st, where)
 
 
-class _On:
-    """Current stream ``stream`` if one is given: what is allocated inside belongs to it, so that the allocator hands it on
-    only behind the work enqueued there."""
+_PLAIN = contextlib.nullcontext()
 
-    def __init__(self, stream):
-        self.inner = None if stream is None else torch.cuda.stream(stream)
 
-    def __enter__(self):
-        if self.inner is not None:
-            self.inner.__enter__()
-
-    def __exit__(self, *exc):
-        if self.inner is not None:
-            self.inner.__exit__(*exc)
+def _on(stream):
+    """Context in which ``stream``, if one is given, is current: what is allocated inside belongs to it, so that the allocator
+    hands it on only behind the work enqueued there."""
+    return _PLAIN if stream is None else torch.cuda.stream(stream)
 
 
 def make_head_params(hidden, weight, temperature=1.0) -> ppow_head_params:
@@ -715,31 +709,43 @@ def select_windows(score, n_keep: int, want_mask: bool = False, stream=None):
     return (sel, mask) if want_mask else sel
 
 
+# The wrappers below hand the addresses of what they have just allocated straight to the library; sizes go to torch.empty as
+# plain integers, since a tuple takes it 0.8 us more.
+
+
 def _workspace(nbytes: int, dev) -> torch.Tensor:
-    return torch.empty(nbytes or 256, dtype=torch.uint8, device=dev)      # (sizes as plain integers: a tuple takes 0.8 us more)
+    return torch.empty(nbytes or 256, dtype=torch.uint8, device=dev)
 
 
 def head_logprob(hidden, weight, tokens, *, temperature=1.0, stream=None) -> dict:
     """Allocate outputs and workspace, run ppow_head_logprob; returns logp and lse, both [T] float32."""
-    params = make_head_params(hidden, weight, temperature)
-    dev = hidden.device
-    with _On(stream):
-        out = {"logp": torch.empty(params.T, dtype=torch.float32, device=dev),
-               "lse": torch.empty(params.T, dtype=torch.float32, device=dev)}
-        ws = _workspace(ppow_head_workspace_bytes(params, False), dev)
-        ppow_head_logprob(params, hidden, weight, tokens, out["logp"], out["lse"], ws, stream)
-    return out
+    params, lib, f32 = make_head_params(hidden, weight, temperature), load_library(), torch.float32
+    T, V, D, dt, device, dev = params.T, params.V, params.D, hidden.dtype, hidden.device, _index_of(hidden, "hidden")
+    h, w = _rows_arg(hidden, dt, (T, D), dev, "hidden")[0], _rows_arg(weight, dt, (V, D), dev, "weight")[0]
+    y = _arg(tokens, torch.int32, (T,), dev, "tokens")
+    with _on(stream):
+        logp, lse = torch.empty(T, dtype=f32, device=device), torch.empty(T, dtype=f32, device=device)
+        nbytes = lib.ppow_head_workspace_bytes(ctypes.byref(params), 0)
+        ws = _workspace(nbytes, device)
+    _call(lib.ppow_head_logprob, "ppow_head_logprob", dev, ctypes.byref(params), h, w, y, logp.data_ptr(), lse.data_ptr(),
+          ws.data_ptr(), nbytes, _raw_stream(stream, dev))
+    return {"logp": logp, "lse": lse}
 
 
 def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature=1.0, want_hidden=True, want_weight=True, stream=None):
     """Allocate gradients and workspace, run ppow_head_logprob_backward; returns (grad_hidden, grad_weight), None where not wanted."""
-    params = make_head_params(hidden, weight, temperature)
-    dev = hidden.device
-    with _On(stream):
-        gh = torch.empty(params.T, params.D, dtype=hidden.dtype, device=dev) if want_hidden else None
-        gw = torch.empty(params.V, params.D, dtype=hidden.dtype, device=dev) if want_weight else None
-        ws = _workspace(ppow_head_workspace_bytes(params, True), dev)
-        ppow_head_logprob_backward(params, hidden, weight, tokens, lse, grad_logp, gh, gw, ws, stream)
+    params, lib, f32 = make_head_params(hidden, weight, temperature), load_library(), torch.float32
+    T, V, D, dt, device, dev = params.T, params.V, params.D, hidden.dtype, hidden.device, _index_of(hidden, "hidden")
+    h, w = _rows_arg(hidden, dt, (T, D), dev, "hidden")[0], _rows_arg(weight, dt, (V, D), dev, "weight")[0]
+    y = _arg(tokens, torch.int32, (T,), dev, "tokens")
+    l, g = _arg(lse, f32, (T,), dev, "lse"), _arg(grad_logp, f32, (T,), dev, "grad_logp")
+    with _on(stream):
+        gh = torch.empty(T, D, dtype=dt, device=device) if want_hidden else None
+        gw = torch.empty(V, D, dtype=dt, device=device) if want_weight else None
+        nbytes = lib.ppow_head_workspace_bytes(ctypes.byref(params), 1)
+        ws = _workspace(nbytes, device)
+    _call(lib.ppow_head_logprob_backward, "ppow_head_logprob_backward", dev, ctypes.byref(params), h, w, y, l, g,
+          None if gh is None else gh.data_ptr(), None if gw is None else gw.data_ptr(), ws.data_ptr(), nbytes, _raw_stream(stream, dev))
     return gh, gw
 
 
@@ -747,14 +753,18 @@ def layer_norm(x, weight, bias=None, *, eps=1e-5, checkpoint=False, stream=None)
     """Allocate outputs and run ppow_layer_norm on ``x`` [R, D]; returns y, mean, rstd and, with ``checkpoint``, the 8-bit form of
     ``x`` as packed and scale."""
     R, D = x.shape
-    params = make_norm_params(R, D, x.dtype, weight.dtype, eps)
-    dev = x.device
-    with _On(stream):
-        out = {"y": torch.empty(R, D, dtype=x.dtype, device=dev), "mean": torch.empty(R, dtype=torch.float32, device=dev),
-               "rstd": torch.empty(R, dtype=torch.float32, device=dev)}
+    dt, pt, device, dev, f32 = x.dtype, weight.dtype, x.device, _index_of(x, "x"), torch.float32
+    params = make_norm_params(R, D, dt, pt, eps)
+    xp, xs = _rows_arg(x, dt, (R, D), dev, "x")
+    w, b = _arg(weight, pt, (D,), dev, "weight"), _arg(bias, pt, (D,), dev, "bias")
+    with _on(stream):
+        out = {"y": torch.empty(R, D, dtype=dt, device=device), "mean": torch.empty(R, dtype=f32, device=device),
+               "rstd": torch.empty(R, dtype=f32, device=device)}
         if checkpoint:
-            out.update(_alloc_packed(R, D, dev))
-        ppow_layer_norm(params, x, weight, bias, out["y"], out["mean"], out["rstd"], out.get("packed"), out.get("scale"), stream)
+            out["packed"], out["scale"] = _alloc_packed(R, D, device)
+    _call(load_library().ppow_layer_norm, "ppow_layer_norm", dev, ctypes.byref(params), xp, xs, w, b, out["y"].data_ptr(),
+          out["mean"].data_ptr(), out["rstd"].data_ptr(), out["packed"].data_ptr() if checkpoint else None,
+          out["scale"].data_ptr() if checkpoint else None, _raw_stream(stream, dev))
     return out
 
 
@@ -762,36 +772,48 @@ def layer_norm_backward(grad_y, x, weight, mean, rstd, *, want_bias=True, stream
     """Allocate gradients and workspace, run ppow_layer_norm_backward; returns (grad_x, grad_weight, grad_bias or None).
     ``x`` is the forward pass's input or the pair (packed, scale) that the forward pass left."""
     R, D = grad_y.shape
-    params = make_norm_params(R, D, grad_y.dtype, weight.dtype)
-    dev = grad_y.device
-    x, packed, scale = (None, *x) if isinstance(x, (tuple, list)) else (x, None, None)
-    with _On(stream):
-        gx = torch.empty(R, D, dtype=grad_y.dtype, device=dev)
-        gw = torch.empty(D, dtype=weight.dtype, device=dev)
-        gb = torch.empty(D, dtype=weight.dtype, device=dev) if want_bias else None
-        ws = _workspace(ppow_layer_norm_workspace_bytes(params), dev)
-        ppow_layer_norm_backward(params, grad_y, x, packed, scale, weight, mean, rstd, gx, gw, gb, ws, stream)
+    dt, pt, device, dev, f32 = grad_y.dtype, weight.dtype, grad_y.device, _index_of(grad_y, "grad_y"), torch.float32
+    params, lib = make_norm_params(R, D, dt, pt), load_library()
+    gp, gs = _rows_arg(grad_y, dt, (R, D), dev, "grad_y")
+    if isinstance(x, (tuple, list)):
+        (xp, xs), (q, s) = (None, D), _packed_args(*x, R, D, dev)
+    else:
+        (xp, xs), (q, s) = _rows_arg(x, dt, (R, D), dev, "x"), (None, None)
+    w, m, r = _arg(weight, pt, (D,), dev, "weight"), _arg(mean, f32, (R,), dev, "mean"), _arg(rstd, f32, (R,), dev, "rstd")
+    with _on(stream):
+        gx = torch.empty(R, D, dtype=dt, device=device)
+        gw = torch.empty(D, dtype=pt, device=device)
+        gb = torch.empty(D, dtype=pt, device=device) if want_bias else None
+        nbytes = lib.ppow_layer_norm_workspace_bytes(ctypes.byref(params))
+        ws = _workspace(nbytes, device)
+    _call(lib.ppow_layer_norm_backward, "ppow_layer_norm_backward", dev, ctypes.byref(params), gp, gs, xp, xs, q, s, w, m, r,
+          gx.data_ptr(), gw.data_ptr(), None if gb is None else gb.data_ptr(), ws.data_ptr(), nbytes, _raw_stream(stream, dev))
     return gx, gw, gb
 
 
-def _alloc_packed(R: int, D: int, dev) -> dict:
-    return {"packed": torch.empty(R, D, dtype=CHECKPOINT_DTYPE, device=dev),
-            "scale": torch.empty(R, -(-D // CHECKPOINT_BLOCK), dtype=torch.uint8, device=dev)}
+def _alloc_packed(R: int, D: int, device):
+    return (torch.empty(R, D, dtype=CHECKPOINT_DTYPE, device=device),
+            torch.empty(R, (D + CHECKPOINT_BLOCK - 1) // CHECKPOINT_BLOCK, dtype=torch.uint8, device=device))
 
 
 def pack_activation(x, stream=None):
     """Allocate and run ppow_pack_activation; returns (packed, scale)."""
-    dev = x.device
-    with _On(stream):
-        out = _alloc_packed(x.shape[0], x.shape[1], dev)
-        ppow_pack_activation(x, out["packed"], out["scale"], stream)
-    return out["packed"], out["scale"]
+    R, D = x.shape
+    code, dev = _storage_code(x.dtype, "x"), _index_of(x, "x")
+    xp, xs = _rows_arg(x, x.dtype, (R, D), dev, "x")
+    with _on(stream):
+        packed, scale = _alloc_packed(R, D, x.device)
+    _call(load_library().ppow_pack_activation, "ppow_pack_activation", dev, xp, xs, R, D, code, packed.data_ptr(), scale.data_ptr(),
+          _raw_stream(stream, dev))
+    return packed, scale
 
 
 def unpack_activation(packed, scale, dtype=torch.bfloat16, stream=None):
     """Allocate and run ppow_unpack_activation; returns the restored activation in ``dtype``."""
-    dev = packed.device
-    with _On(stream):
-        x = torch.empty(*packed.shape, dtype=dtype, device=dev)
-        ppow_unpack_activation(packed, scale, x, stream)
+    R, D = packed.shape
+    code, dev = _storage_code(dtype, "dtype"), _index_of(packed, "packed")
+    q, s = _packed_args(packed, scale, R, D, dev)
+    with _on(stream):
+        x = torch.empty(R, D, dtype=dtype, device=packed.device)
+    _call(load_library().ppow_unpack_activation, "ppow_unpack_activation", dev, q, s, R, D, code, x.data_ptr(), _raw_stream(stream, dev))
     return x
