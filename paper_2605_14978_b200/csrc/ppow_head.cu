@@ -123,7 +123,6 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
     __shared__ int32_t part[4][GATHER_THREADS / 32];
     __shared__ int32_t dest[GATHER_ROWS_MAX];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    allow_next_kernel();
     wait_for_previous_kernel();
     const int32_t r0 = (int32_t)min((int64_t)blockIdx.x * job.rows_per_cta, (int64_t)job.T);
     const int32_t n = min(job.rows_per_cta, job.T - r0);
@@ -643,7 +642,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     tcgen05_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(tmem_slot));
-    allow_next_kernel();
     wait_for_previous_kernel();
 
     Extent e;
@@ -780,7 +778,6 @@ __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows
     __shared__ double sums[MERGE_THREADS / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int32_t row = blockIdx.x;
-    allow_next_kernel();
     wait_for_previous_kernel();
     if (row >= rows.header->live) return;
     const float2 *p = partial + (size_t)row * parts;
@@ -826,7 +823,6 @@ template <bool BF16>
 __global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows rows, const float *__restrict__ parts, int32_t few,
                                                                      int32_t D, uint16_t *__restrict__ grad_hidden)
 {
-    allow_next_kernel();
     wait_for_previous_kernel();
     const int32_t units = D / 4, splits = rows.header->splits, live = rows.header->live;
     const size_t split_units = (size_t)(few ? few : (live + TILE - 1) / TILE * TILE) * units;

@@ -478,7 +478,6 @@ template <int DTYPE, bool VEC, int TPR> __host__ __device__ constexpr int backwa
 template <int DTYPE, bool VEC, int TPR>
 __global__ void __launch_bounds__(norm_threads<TPR>()) norm_forward_kernel(const NormJob job)
 {
-    allow_next_kernel();
     wait_for_previous_kernel();
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
@@ -631,7 +630,6 @@ struct NormGradJob {
 template <int DTYPE, bool VEC, bool PACKED, int TPR>
 __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(const NormGradJob job)
 {
-    allow_next_kernel();
     wait_for_previous_kernel();
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
@@ -787,7 +785,6 @@ __global__ void __launch_bounds__(32 * JOIN_GROUPS) norm_join_kernel(const float
     __shared__ float group[JOIN_GROUPS][32];
     const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
     const int32_t c = blockIdx.x * 32 + lane;        // column of dw, then of db
-    allow_next_kernel();
     wait_for_previous_kernel();
     float sum = 0.0f;
     if (c < 2 * D) {
@@ -849,7 +846,6 @@ struct ChunkWalk {
 template <int DTYPE, bool VEC>
 __global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const PackJob job)
 {
-    allow_next_kernel();
     wait_for_previous_kernel();
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
@@ -877,7 +873,6 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const PackJob job)
 template <int DTYPE, bool VEC>
 __global__ void __launch_bounds__(PACK_THREADS) unpack_kernel(const PackJob job)
 {
-    allow_next_kernel();
     wait_for_previous_kernel();
     using DealT = Deal<DTYPE, VEC>;
     using T = typename DealT::T;
