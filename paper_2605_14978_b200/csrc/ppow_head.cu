@@ -30,6 +30,9 @@ constexpr int BK = 64;               // products' inner step per pipeline stage:
 constexpr uint32_t A_BYTES = HALF_TILE * BK * 2;           // 16 KB
 constexpr int MMA_THREADS = 320;     // producer warp, issuing warp, eight epilogue warps
 constexpr int PAIRS = 74;            // pairs of SMs that the shares of an inner axis are planned for
+// Steps that the logits of the forward pass are summed over in Tensor Memory before the sum moves on to registers: the tensor
+// cores' additions cut off what does not fit, and over 256 steps of 16 that left lse off by 3e-6 (4096 wide); like this 5e-7.
+constexpr int SUM_STEPS = 16;
 constexpr int MAX_PAIRS = 128;       // pairs that a launch uses at most
 
 // Columns of a tile: 256, or for few tokens the tokens themselves (16, 32, 64 or 128), with W taking the 256 rows.
@@ -387,7 +390,8 @@ __device__ __forceinline__ void put_box(uint32_t box, int32_t in_tile, int half,
 // rows: tokens, columns: vocabulary
 template <int PRODUCT, bool BF16, typename R>
 __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Extent &e, const Tile &x, const RowData &own, uint32_t src,
-                                              int32_t in_tile, int half, const CUtensorMap *map_out, uint32_t box, R &&release)
+                                              int32_t in_tile, int half, const CUtensorMap *map_out, uint32_t box,
+                                              uint32_t (&w)[TILE / 64][32], R &&release)
 {
     constexpr int COLS = TILE / 2;
     const int32_t row = x.row + in_tile;                     // a live row, or for GRAD_WEIGHT an entry of the piece
@@ -397,13 +401,7 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
     if (PRODUCT == LOGITS_SUM) {
         const int32_t left = min(TILE, job.V - x.col) - first;   // columns that exist
         const int32_t at = own.token - x.col - first;            // padded rows hold a negative token
-        // all 128 columns at once: one maximum, no rescaling, and the accumulator is free before the arithmetic starts
-        uint32_t w[COLS / 32][32];
-#pragma unroll
-        for (int i = 0; i < COLS / 32; ++i) tmem_load(src + 32 * i, w[i]);
-#pragma unroll
-        for (int i = 0; i < COLS / 32; ++i) tmem_wait(w[i]);
-        release();
+        // all 128 columns at once: one maximum, no rescaling
         if (left < COLS) {
 #pragma unroll
             for (int j = 0; j < COLS; ++j)
@@ -516,6 +514,10 @@ __device__ __forceinline__ void across_lanes(float (&v)[WIDTH], Op op)
     }
 }
 
+// A warp's columns of a tile, in registers: chunks of at most 32.
+template <int N> __host__ __device__ constexpr int sum_width() { return N / 2 < 32 ? N / 2 : 32; }
+template <int N> __host__ __device__ constexpr int sum_chunks() { return N / 2 / sum_width<N>(); }
+
 // Maximum and sum of exponentials, over the tiles that a warp has seen, of column lane % 32 of a chunk of 32.
 struct RunningSum {
     float top, sum;
@@ -524,17 +526,19 @@ struct RunningSum {
 // rows: the vocabulary's entries, for GRAD_HIDDEN the width's; columns: tokens.  Sums over the rows run across the lanes.
 template <int PRODUCT, bool BF16, int N, typename R>
 __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent &e, const Tile &x, uint32_t src, int32_t in_tile, int half,
-                                             RunningSum (&run)[2], R &&release)
+                                             RunningSum (&run)[2], uint32_t (&z)[sum_chunks<N>()][sum_width<N>()], R &&release)
 {
-    constexpr int COLS = N / 2, WIDTH = COLS < 32 ? COLS : 32;
+    constexpr int COLS = N / 2, WIDTH = sum_width<N>();
     const int lane = threadIdx.x & 31;
     const int32_t row = x.row + in_tile, first = half * COLS;
     src += first;
     [[maybe_unused]] unsigned int *flags = &job.rows.header->error_flags;
     if (PRODUCT == LOGITS_SUM) {
         const bool inside = row < job.V;
-        for_chunks<COLS / WIDTH, WIDTH>(src, release, [&](int c, uint32_t (&w)[WIDTH]) {
-            if (first + c >= e.live) return;
+#pragma unroll
+        for (int c = 0; c < COLS; c += WIDTH) {
+            if (first + c >= e.live) break;
+            uint32_t (&w)[WIDTH] = z[c / WIDTH];
             float v[WIDTH], r[WIDTH];
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) r[j] = v[j] = inside ? __uint_as_float(w[j]) * job.scale : -INFINITY;
@@ -557,7 +561,7 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
                 for (int j = 0; j < WIDTH; ++j)
                     if ((hits >> j & 1u) && __shfl_sync(0xffffffffu, at, j) == lane) job.at_token[first + c + j] = __uint_as_float(w[j]);
             }
-        });
+        }
     } else if (PRODUCT == LOGITS_GRAD) {
         const bool inside = row < job.V;
         uint16_t *to = job.dz + x.index * TILE + in_tile;
@@ -596,7 +600,7 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
 
 // Persistent: one CTA per SM, pair p takes tiles p, p + pairs, ...  Warp 0 keeps the operand ring full, one thread of
 // the leader's warp 1 issues the products into one of two accumulators, warps 2..9 read the other one out.
-template <int PRODUCT, bool BF16, int N>
+template <int PRODUCT, bool BF16, int N, bool PARTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     head_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                         const __grid_constant__ CUtensorMap map_out, const ProductJob job)
@@ -689,25 +693,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
         if (rank == 0 && lane == 0) {
             uint32_t it = 0, acc = 0;
             bool ok = true;
-            for (int64_t t = pair; t < tiles && ok; t += pairs, ++acc) {
+            for (int64_t t = pair; t < tiles && ok; t += pairs) {
                 const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
-                const uint32_t b = acc & 1u, d = tmem + b * TILE;
-                ok = mbar_wait_ns(acc_empty(b), ((acc >> 1) & 1u) ^ 1u);
-                tcgen05_fence_after();
-                for (int32_t k = x.k0; k < x.k1 && ok; ++k, ++it) {
-                    const uint32_t s = it % STAGES;
-                    ok = mbar_wait_ns(full(s), (it / STAGES) & 1u);
-                    if (!ok) break;
+                for (int32_t k0 = x.k0; ok && (k0 < x.k1 || k0 == x.k0); ++acc) {
+                    const int32_t k1 = PARTS ? min(k0 + SUM_STEPS, x.k1) : x.k1;
+                    const uint32_t b = acc & 1u, d = tmem + b * TILE;
+                    ok = mbar_wait_ns(acc_empty(b), ((acc >> 1) & 1u) ^ 1u);
                     tcgen05_fence_after();
-                    const uint32_t a = smem + s * STAGE_BYTES;
-                    const uint64_t da = operand_descriptor(a, A_K, BLOCK_BYTES), db = operand_descriptor(a + A_BYTES, B_K, BLOCK_BYTES);
+                    for (int32_t k = k0; k < k1 && ok; ++k, ++it) {
+                        const uint32_t s = it % STAGES;
+                        ok = mbar_wait_ns(full(s), (it / STAGES) & 1u);
+                        if (!ok) break;
+                        tcgen05_fence_after();
+                        const uint32_t a = smem + s * STAGE_BYTES;
+                        const uint64_t da = operand_descriptor(a, A_K, BLOCK_BYTES), db = operand_descriptor(a + A_BYTES, B_K, BLOCK_BYTES);
 #pragma unroll
-                    for (int q = 0; q < BK / 16; ++q)
-                        mma_pair(d, da + (uint64_t)(q * (A_K ? 32 : 2048) >> 4), db + (uint64_t)(q * (B_K ? 32 : 2048) >> 4), INSTRUCTION,
-                                 k > x.k0 || q > 0);
-                    mma_commit_pair(empty(s));
+                        for (int q = 0; q < BK / 16; ++q)
+                            mma_pair(d, da + (uint64_t)(q * (A_K ? 32 : 2048) >> 4), db + (uint64_t)(q * (B_K ? 32 : 2048) >> 4), INSTRUCTION,
+                                     k > k0 || q > 0);
+                        mma_commit_pair(empty(s));
+                    }
+                    if (ok) mma_commit_pair(acc_full(b));
+                    if (k1 == k0) break;             // a share without steps
+                    k0 = k1;
                 }
-                if (ok) mma_commit_pair(acc_full(b));
             }
             if (!ok) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
         }
@@ -718,9 +727,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
         uint32_t acc = 0;
         bool ok = true;
         RunningSum run[2] = {{-INFINITY, 0.0f}, {-INFINITY, 0.0f}};
-        for (int64_t t = pair; t < tiles; t += pairs, ++acc) {
+        uint32_t z[sum_chunks<N>()][sum_width<N>()] = {};        // LOGITS_SUM: the warp's logits
+        for (int64_t t = pair; t < tiles && ok; t += pairs) {
             const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
-            const uint32_t b = acc & 1u;
             RowData own = {};
             if (!FEW && (PRODUCT == LOGITS_SUM || PRODUCT == LOGITS_GRAD)) {
                 own.token = job.rows.token[x.row + in_tile];
@@ -729,20 +738,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                     own.lse2 = job.rows.lse2[x.row + in_tile];
                 }
             }
-            // all four warps of a half go on or none does: they meet at barriers further down
-            ok = named_barrier_all(1 + half, 128, mbar_wait_ns(acc_full(b), (acc >> 1) & 1u));
-            if (!ok) break;
-            tcgen05_fence_after();
-            const uint32_t src = tmem + b * TILE + (quarter * 32u << 16);
-            auto release = [&] {
-                tcgen05_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(peer_addr(acc_empty(b), 0));
-            };
-            if constexpr (FEW)
-                epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half, run, release);
-            else
-                epilogue_many<PRODUCT, BF16>(job, e, x, own, src, in_tile, half, &map_out, box, release);
+            const int32_t parts = PARTS ? (x.k1 - x.k0 + SUM_STEPS - 1) / SUM_STEPS : 1;
+            for (int32_t part = 0; part < parts; ++part, ++acc) {
+                const uint32_t b = acc & 1u;
+                // all four warps of a half go on or none does: they meet at barriers further down
+                ok = named_barrier_all(1 + half, 128, mbar_wait_ns(acc_full(b), (acc >> 1) & 1u));
+                if (!ok) break;
+                tcgen05_fence_after();
+                const uint32_t src = tmem + b * TILE + (quarter * 32u << 16);
+                auto release = [&] {
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(peer_addr(acc_empty(b), 0));
+                };
+                if constexpr (PRODUCT == LOGITS_SUM) {
+                    constexpr int CHUNKS = sum_chunks<N>(), WIDTH = sum_width<N>(), ADD = WIDTH < 16 ? WIDTH : 16;
+                    const uint32_t from = src + half * (N / 2);
+                    if (!PARTS || part == 0) {
+#pragma unroll
+                        for (int i = 0; i < CHUNKS; ++i) tmem_load(from + i * WIDTH, z[i]);
+#pragma unroll
+                        for (int i = 0; i < CHUNKS; ++i) tmem_wait(z[i]);
+                    } else {
+                        // few registers are left beside the sums: 16 columns at a time, behind the products of the next steps
+#pragma unroll
+                        for (int c = 0; c < N / 2; c += ADD) {
+                            uint32_t w[ADD];
+                            tmem_load(from + c, w);
+                            tmem_wait(w);
+#pragma unroll
+                            for (int j = 0; j < ADD; ++j) {
+                                uint32_t &sum = z[(c + j) / WIDTH][(c + j) % WIDTH];
+                                sum = __float_as_uint(__uint_as_float(sum) + __uint_as_float(w[j]));
+                            }
+                        }
+                    }
+                    release();
+                    if (part + 1 < parts) continue;
+                }
+                if constexpr (FEW)
+                    epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half, run, z, release);
+                else
+                    epilogue_many<PRODUCT, BF16>(job, e, x, own, src, in_tile, half, &map_out, box, z, release);
+            }
         }
         if (FEW && PRODUCT == LOGITS_SUM) {
             constexpr int COLS = N / 2;
@@ -947,8 +985,10 @@ bool make_map(CUtensorMap *map, const void *base, bool bf16, int64_t width, int6
 constexpr int DEVICES = 64;
 template <int PRODUCT, bool BF16, int N> bool allow_smem()
 {
-    return cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)mma_smem<N>()) ==
-           cudaSuccess;
+    constexpr int BYTES = (int)mma_smem<N>();
+    return cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16, N, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) == cudaSuccess &&
+           (PRODUCT != LOGITS_SUM || cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16, N, PRODUCT == LOGITS_SUM>,
+                                                          cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) == cudaSuccess);
 }
 template <int PRODUCT, bool BF16> bool allow_smem_few()
 {
@@ -975,7 +1015,10 @@ bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap 
                   cudaStream_t stream)
 {
     const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
-    return launch_after(head_product_kernel<PRODUCT, BF16, N>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, job);
+    // one part is a kernel of its own: the loop over parts costs it a third (2048 x 128 x 128256: 106 us, with the loop 140)
+    if (PRODUCT == LOGITS_SUM && job.D > SUM_STEPS * BK)
+        return launch_after(head_product_kernel<PRODUCT, BF16, N, PRODUCT == LOGITS_SUM>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, job);
+    return launch_after(head_product_kernel<PRODUCT, BF16, N, false>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, job);
 }
 
 // `rows` and `weight`: the operand maps of the token side and of W's side.  With few tokens the two change places.  `out`: the

@@ -142,3 +142,191 @@ def test_gradient_matches_the_definition(T, V, D, dtype):
     out, gh, gw = run(h, w, tok, grad, 0.7)
     check_forward(h, w, tok, 0.7, out)
     check_backward(h, w, tok, out["lse"], grad, 0.7, gh, gw)
+
+
+# ------------------------------------------------------------------ masks, strides, ends of the ranges
+
+
+def test_masked_rows_may_hold_anything_and_get_zeros():
+    h, w, tok, grad = make(300, 1500, 200, torch.bfloat16, seed=2, masked=0.0)
+    clean = h.clone()
+    dead = torch.zeros(300, dtype=torch.bool, device=DEV)
+    dead[::3] = True
+    dead[256:290] = True
+    tok[dead] = torch.where(torch.arange(int(dead.sum()), device=DEV) % 2 == 0, -1, -2 ** 31).int()
+    h[dead] = torch.tensor([float("nan"), float("inf"), -float("inf")], device=DEV).repeat(67).to(h.dtype)[:200]
+    grad[dead] = float("nan")
+    clean[dead] = 0
+    out, gh, gw = run(h, w, tok, grad)
+    check_forward(clean, w, tok, 1.0, out)
+    grad[dead] = 1.0
+    check_backward(clean, w, tok, out["lse"], grad, 1.0, gh, gw)
+
+
+def test_rows_without_gradient_are_masked_in_the_backward_pass():
+    h, w, tok, grad = make(70, 900, 72, torch.float16, seed=3, masked=0.0)
+    out = B.head_logprob(h, w, tok)
+    grad[5:40] = 0.0
+    grad[41] = -0.0
+    clean = h.clone()
+    h[5:40] = float("nan")
+    gh, gw = B.head_logprob_backward(h, w, tok, out["lse"], grad)
+    torch.cuda.synchronize()
+    check_backward(clean, w, tok, out["lse"], grad, 1.0, gh, gw)
+
+
+@pytest.mark.parametrize("T", [1, 16, 100, 300, 1000])
+def test_all_rows_masked(T):
+    h, w, tok, grad = make(T, 600, 64, torch.bfloat16, masked=0.0)
+    tok.fill_(-1)
+    h.fill_(float("nan"))
+    out, gh, gw = run(h, w, tok, grad)
+    assert not out["logp"].any() and not out["lse"].any() and not gh.any() and not gw.any()
+
+
+def test_no_tokens():
+    h, w, tok, grad = make(4, 600, 64, torch.bfloat16)
+    out, gh, gw = run(h[:0], w, tok[:0], grad[:0])
+    assert out["logp"].shape == (0,) and gh.shape == (0, 64) and not gw.any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T", [40, 400])
+@pytest.mark.parametrize("offset,pad", [(1, 3), (8, 8), (0, 1)])
+def test_rows_of_other_strides_and_alignments(T, offset, pad, dtype):
+    h, w, tok, grad = make(T, 1000, 136, dtype, seed=4)
+    wide = torch.full((T, 136 + offset + pad), float("nan"), dtype=dtype, device=DEV)
+    hv = wide[:, offset:offset + 136]
+    hv.copy_(h)
+    ww = torch.full((1000, 136 + 24), float("nan"), dtype=dtype, device=DEV)
+    wv = ww[:, 8:144]
+    wv.copy_(w)
+    a, b = run(h, w, tok, grad), run(hv, wv, tok, grad)
+    assert torch.equal(a[0]["logp"], b[0]["logp"]) and torch.equal(a[0]["lse"], b[0]["lse"])
+    assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
+
+
+@pytest.mark.parametrize("T", [20, 500])
+def test_tokens_behind_the_vocabulary_are_reported(T):
+    h, w, tok, grad = make(T, 777, 64, torch.bfloat16, seed=5, masked=0.0)
+    tok[3], tok[11] = 777, 2 ** 31 - 1
+    p = B.make_head_params(h, w)
+    for backward in (False, True):
+        ws = B.alloc_workspace(B.ppow_head_workspace_bytes(p, backward), DEV)
+        if not backward:
+            logp, lse = torch.empty(T, device=DEV), torch.empty(T, device=DEV)
+            B.ppow_head_logprob(p, h, w, tok, logp, lse, ws)
+        else:
+            gh, gw = torch.empty_like(h), torch.empty_like(w)
+            B.ppow_head_logprob_backward(p, h, w, tok, lse, grad, gh, gw, ws)
+        assert B.ppow_read_error_flags(ws) == B.PPOW_FLAG_TOKEN_RANGE
+    check_forward(h, w, tok, 1.0, {"logp": logp, "lse": lse})
+    assert not gh[3].any() and not gh[11].any()
+    check_backward(h, w, tok, lse, grad, 1.0, gh, gw)
+    tok[3] = tok[11] = 0
+    ws.fill_(255)                                             # whatever the workspace held before
+    B.ppow_head_logprob_backward(p, h, w, tok, lse, grad, gh, gw, ws)
+    assert B.ppow_read_error_flags(ws) == 0
+
+
+@pytest.mark.parametrize("T", [90, 300])
+def test_either_gradient_alone(T):
+    h, w, tok, grad = make(T, 1100, 264, torch.bfloat16, seed=6)
+    out, gh, gw = run(h, w, tok, grad)
+    only_h = B.head_logprob_backward(h, w, tok, out["lse"], grad, want_weight=False)
+    only_w = B.head_logprob_backward(h, w, tok, out["lse"], grad, want_hidden=False)
+    torch.cuda.synchronize()
+    assert only_h[1] is None and only_w[0] is None
+    assert torch.equal(only_h[0], gh) and torch.equal(only_w[1], gw)
+
+
+def test_gradients_of_very_different_rows_in_half_precision():
+    h, w, tok, grad = make(200, 1000, 64, torch.float16, seed=7, masked=0.0)
+    grad *= torch.logspace(-9, 3, 200, device=DEV)
+    out, gh, gw = run(h, w, tok, grad)
+    check_backward(h, w, tok, out["lse"], grad, 1.0, gh, gw)
+
+
+def test_several_pieces_of_the_vocabulary():
+    # 2304 rows of dz over 128256 entries are 591 MB: two pieces, the second shorter, sums of grad_hidden carried over
+    h, w, tok, grad = make(2304, 128256, 64, torch.bfloat16, seed=8)
+    out, gh, gw = run(h, w, tok, grad)
+    check_forward(h, w, tok, 1.0, out)
+    check_backward(h, w, tok, out["lse"], grad, 1.0, gh, gw)
+
+
+def test_results_do_not_depend_on_the_run_and_nothing_behind_them_is_touched():
+    for T, dtype in ((50, torch.float16), (700, torch.bfloat16)):
+        h, w, tok, grad = make(T, 2000, 328, dtype, seed=9)
+        p = B.make_head_params(h, w, 0.9)
+        first = None
+        for fill in (0.0, float("nan")):
+            bufs = {"logp": torch.full((T + 8,), 7.0, device=DEV), "lse": torch.full((T + 8,), 7.0, device=DEV),
+                    "gh": torch.full((T + 2, 328), 7.0, device=DEV, dtype=dtype), "gw": torch.full((2002, 328), 7.0, device=DEV, dtype=dtype)}
+            ws = [B.alloc_workspace(B.ppow_head_workspace_bytes(p, b), DEV) for b in (False, True)]
+            for x in ws:
+                x.view(torch.float32)[:].fill_(fill) if x.numel() % 4 == 0 else x.fill_(255)
+            B.ppow_head_logprob(p, h, w, tok, bufs["logp"][:T], bufs["lse"][:T], ws[0])
+            B.ppow_head_logprob_backward(p, h, w, tok, bufs["lse"][:T], grad, bufs["gh"][:T], bufs["gw"][:2000], ws[1])
+            torch.cuda.synchronize()
+            assert torch.all(bufs["logp"][T:] == 7) and torch.all(bufs["lse"][T:] == 7)
+            assert torch.all(bufs["gh"][T:] == 7) and torch.all(bufs["gw"][2000:] == 7)
+            if first is not None:
+                assert all(torch.equal(first[k], bufs[k]) for k in bufs)
+            first = bufs
+
+
+def test_two_streams_at_once_and_a_stream_that_is_not_current():
+    cases = [make(T, 3001, 256, torch.bfloat16, seed=10 + T) for T in (33, 600)]
+    want = [run(*c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = []
+        for (h, w, tok, grad), s in zip(cases, streams):
+            out = B.head_logprob(h, w, tok, stream=s)
+            got.append((out, *B.head_logprob_backward(h, w, tok, out["lse"], grad, stream=s)))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a[0]["logp"], b[0]["logp"]) and torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
+
+
+@pytest.mark.parametrize("T", [60, 700])
+def test_captured_and_replayed_on_new_inputs(T):
+    h, w, tok, grad = make(T, 2500, 136, torch.bfloat16, seed=11)
+    h2, w2, tok2, grad2 = make(T, 2500, 136, torch.bfloat16, seed=12, masked=0.6)
+    want = run(h2, w2, tok2, grad2)
+    run(h, w, tok, grad)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = B.head_logprob(h, w, tok)
+        gh, gw = B.head_logprob_backward(h, w, tok, out["lse"], grad)
+    for a, b in ((h, h2), (w, w2), (tok, tok2), (grad, grad2)):
+        a.copy_(b)
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out["logp"], want[0]["logp"]) and torch.equal(gh, want[1]) and torch.equal(gw, want[2])
+
+
+@pytest.mark.parametrize("T", [12, 300])
+def test_gradient_against_differences_of_the_forward_pass(T):
+    # hidden states on a grid of 2^-6, moved by one step along u in {-1, 1}^D: exact in float16.  Along u the logits are linear,
+    # with slopes a = W u; the third derivative of lse is their third cumulant, at most (max a - min a)^3 in magnitude.
+    g = torch.Generator(device=DEV).manual_seed(13)
+    V, D, step = 300, 64, 2.0 ** -6
+    h = (torch.randint(-64, 65, (T, D), generator=g, device=DEV) * step).half()
+    w = (torch.randn((V, D), generator=g, device=DEV) * 0.1).half()
+    tok = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    grad = torch.randn(T, generator=g, device=DEV)
+    u = (torch.randint(0, 2, (T, D), generator=g, device=DEV) * 2 - 1).half()
+    logp = [B.head_logprob(h + s * step * u, w, tok)["logp"].double() for s in (1, -1)]
+    out, gh, _ = run(h, w, tok, grad)
+    got = (gh.double() * u.double()).sum(1)
+    want = grad.double() * (logp[0] - logp[1]) / (2 * step)
+    a = u.double() @ w.double().t()
+    spread = a.amax(1) - a.amin(1)
+    err = logits(h, w, 1.0)[1].amax(1) * 2 + 2.0 ** -19 + out["lse"].double().abs() * 2.0 ** -21
+    tol = grad.double().abs() * (step ** 2 / 6 * spread ** 3 + err / step)
+    dh, th, _, _ = gradient(h, w, tok, out["lse"], grad, 1.0)
+    assert torch.all((got - want).abs() <= tol + th.sum(1))

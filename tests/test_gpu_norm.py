@@ -151,3 +151,215 @@ def test_pack_and_unpack(R, D, dtype):
     value = reference_pack(x)[2]
     for t, back in backs.items():
         assert torch.equal(back, value.to(t)), t
+
+
+# ------------------------------------------------------------------ odd inputs, strides, streams
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [64, 1000, 1531, 4096])
+def test_constant_rows_large_offsets_and_zero_gradient(D, dtype):
+    x, w, b, gy = make(40, D, dtype, seed=3)
+    x[0], x[1], x[2] = 0.0, 3.0, -0.5
+    x[3:10] += 500.0                                          # a mean far above the spread
+    gy[5] = 0.0
+    out = B.layer_norm(x, w, b, eps=1e-5, checkpoint=True)
+    got = B.layer_norm_backward(gy, x, w, out["mean"], out["rstd"])
+    packed = B.layer_norm_backward(gy, (out["packed"], out["scale"]), w, out["mean"], out["rstd"])
+    torch.cuda.synchronize()
+    check_forward(x, w, b, 1e-5, out)
+    check_packed(x, out["packed"], out["scale"])
+    check_backward(gy, x.double(), w, out["mean"], out["rstd"], got, torch.float32)
+    check_backward(gy, reference_pack(x)[2], w, out["mean"], out["rstd"], packed, torch.float32)
+    assert not got[0][5].any() and torch.all(out["y"][0] == b.to(dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [64, 777, 4096, 8200])
+def test_rows_that_are_not_finite_stay_among_themselves(D, dtype):
+    x, w, b, gy = make(9, D, dtype, seed=4)
+    clean = B.layer_norm(x, w, b, checkpoint=True)
+    x[2, D // 2], x[5, 0], x[7, D - 1] = float("nan"), float("inf"), -float("inf")
+    out = B.layer_norm(x, w, b, checkpoint=True)
+    torch.cuda.synchronize()
+    bad = torch.tensor([2, 5, 7], device=DEV)
+    good = torch.tensor([0, 1, 3, 4, 6, 8], device=DEV)
+    for k in ("y", "mean", "rstd", "scale"):
+        assert torch.equal(out[k][good], clean[k][good]), k
+    assert torch.equal(out["packed"].view(torch.uint8)[good], clean["packed"].view(torch.uint8)[good])
+    assert out["y"][bad].isnan().any(1).all()
+    check_packed(x, out["packed"], out["scale"])             # the scale goes by the finite values, what is not finite is NaN
+    q, s = B.pack_activation(x)
+    torch.cuda.synchronize()
+    assert torch.equal(q.view(torch.uint8), out["packed"].view(torch.uint8)) and torch.equal(s, out["scale"])
+    gx, _, _ = B.layer_norm_backward(gy, x, w, out["mean"], out["rstd"])
+    want, _, _ = B.layer_norm_backward(gy, torch.where(x.isfinite(), x, 0), w, clean["mean"], clean["rstd"])
+    torch.cuda.synchronize()
+    assert torch.equal(gx[good], want[good])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [128, 131, 640])
+def test_edges_of_the_8_bit_format(D, dtype):
+    top = torch.finfo(dtype).max
+    rows = []
+    for k in (0, 1, 5, -3, 8):                               # borders of the scale: 448 * 2^k and its neighbours
+        for f in (1.0, 1.0 + torch.finfo(dtype).eps, 1.0 - torch.finfo(dtype).eps / 2, 0.5, 448.5 / 448):
+            rows.append(448.0 * 2.0 ** k * f)
+    rows += [top, torch.finfo(dtype).tiny, torch.finfo(dtype).smallest_normal / 4, 0.0, 2.0 ** -9, 1.0]
+    x = torch.zeros((len(rows), D), dtype=torch.float64, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(D)
+    ramp = 2.0 ** -torch.randint(0, 20, (len(rows), D), generator=g, device=DEV).double()
+    ramp *= 1 + torch.randint(0, 64, (len(rows), D), generator=g, device=DEV) / 64            # ties of the rounding among them
+    x = (ramp * torch.tensor(rows, dtype=torch.float64, device=DEV)[:, None] / 2).to(dtype)
+    x[:, D // 3] = torch.tensor(rows, dtype=torch.float64, device=DEV).to(dtype)
+    x[::2] = -x[::2]
+    q, s = B.pack_activation(x)
+    back = {t: B.unpack_activation(q, s, t) for t in TYPES}
+    torch.cuda.synchronize()
+    check_packed(x, q, s)
+    value = reference_pack(x)[2]
+    for t in TYPES:                                          # 448 * 2^8 is an infinity in float16 and comes back as NaN
+        torch.testing.assert_close(back[t], value.to(t), rtol=0, atol=0, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("R,D,offset,pad", [(30, 512, 1, 0), (30, 512, 16, 16), (5, 4096, 3, 2), (17, 1531, 0, 5), (3, 8192, 8, 8)])
+def test_rows_of_other_strides_and_alignments(R, D, offset, pad, dtype):
+    x, w, b, gy = make(R, D, dtype, seed=5)
+
+    def view(t):
+        wide = torch.full((R, D + offset + pad), float("nan"), dtype=dtype, device=DEV)
+        wide[:, offset:offset + D] = t
+        return wide[:, offset:offset + D]
+    a = B.layer_norm(x, w, b, checkpoint=True)
+    v = B.layer_norm(view(x), w, b, checkpoint=True)
+    q, s = B.pack_activation(view(x))
+    ga = B.layer_norm_backward(gy, x, w, a["mean"], a["rstd"])
+    gv = B.layer_norm_backward(view(gy), view(x), w, a["mean"], a["rstd"])
+    gp = B.layer_norm_backward(view(gy), (a["packed"], a["scale"]), w, a["mean"], a["rstd"])
+    torch.cuda.synchronize()
+    check_forward(x, w, b, 1e-5, v)
+    assert torch.equal(a["packed"].view(torch.uint8), v["packed"].view(torch.uint8)) and torch.equal(a["scale"], v["scale"])
+    assert torch.equal(q.view(torch.uint8), a["packed"].view(torch.uint8)) and torch.equal(s, a["scale"])
+    check_backward(gy, x.double(), w, a["mean"], a["rstd"], ga, torch.float32)
+    check_backward(gy, x.double(), w, a["mean"], a["rstd"], gv, torch.float32)
+    check_backward(gy, reference_pack(x)[2], w, a["mean"], a["rstd"], gp, torch.float32)
+
+
+@pytest.mark.parametrize("offset", [1, 2, 3, 5])
+def test_parameters_and_packed_bytes_at_odd_addresses(offset):
+    R, D = 6, 256
+    x, w, b, gy = make(R, D, torch.bfloat16, seed=6)
+    par = torch.zeros(2 * D + 16, device=DEV)
+    wv, bv = par[offset:offset + D], par[D + offset:2 * D + offset]
+    wv.copy_(w), bv.copy_(b)
+    buf = torch.zeros(R * D + 16, dtype=torch.uint8, device=DEV)
+    sc = torch.zeros(R * 2 + 16, dtype=torch.uint8, device=DEV)
+    qv, sv = buf[offset:offset + R * D].view(R, D).view(torch.float8_e4m3fn), sc[offset:offset + 2 * R].view(R, 2)
+    want = B.layer_norm(x, w, b, checkpoint=True)
+    out = {k: torch.empty_like(v) for k, v in want.items()}
+    p = B.make_norm_params(R, D, x.dtype, torch.float32)
+    B.ppow_layer_norm(p, x, wv, bv, out["y"], out["mean"], out["rstd"], qv, sv)
+    g1 = B.layer_norm_backward(gy, (qv, sv), wv, want["mean"], want["rstd"])
+    g2 = B.layer_norm_backward(gy, (want["packed"], want["scale"]), w, want["mean"], want["rstd"])
+    torch.cuda.synchronize()
+    check_forward(x, w, b, 1e-5, out)
+    check_packed(x, qv, sv)
+    for g in (g1, g2):
+        check_backward(gy, reference_pack(x)[2], w, want["mean"], want["rstd"], g, torch.float32)
+    assert not buf[:offset].any() and not buf[offset + R * D:].any() and not sc[:offset].any() and not sc[offset + 2 * R:].any()
+
+
+@pytest.mark.parametrize("R,D,dtype", [(700, 4096, torch.bfloat16), (4000, 72, torch.float16), (50, 1531, torch.float32)])
+def test_same_results_every_time_and_nothing_behind_them_is_touched(R, D, dtype):
+    x, w, b, gy = make(R, D, dtype, seed=7)
+    p = B.make_norm_params(R, D, dtype, torch.float32)
+    first = None
+    for fill in (0, 255):
+        o = {"y": torch.full((R + 1, D), 7.0, device=DEV, dtype=dtype), "m": torch.full((R + 4,), 7.0, device=DEV),
+             "r": torch.full((R + 4,), 7.0, device=DEV), "gx": torch.full((R + 1, D), 7.0, device=DEV, dtype=dtype),
+             "gw": torch.full((D + 4,), 7.0, device=DEV), "gb": torch.full((D + 4,), 7.0, device=DEV)}
+        ws = torch.full((B.ppow_layer_norm_workspace_bytes(p),), fill, dtype=torch.uint8, device=DEV)
+        B.ppow_layer_norm(p, x, w, b, o["y"][:R], o["m"][:R], o["r"][:R])
+        B.ppow_layer_norm_backward(p, gy, x, None, None, w, o["m"][:R], o["r"][:R], o["gx"][:R], o["gw"][:D], o["gb"][:D], ws)
+        torch.cuda.synchronize()
+        for k, n in (("y", R), ("m", R), ("r", R), ("gx", R), ("gw", D), ("gb", D)):
+            assert torch.all(o[k][n:] == 7), k
+        assert first is None or all(torch.equal(first[k], o[k]) for k in o)
+        first = o
+
+
+def test_no_rows():
+    x, w, b, gy = make(3, 200, torch.bfloat16)
+    out = B.layer_norm(x[:0], w, b, checkpoint=True)
+    assert out["y"].shape == (0, 200) and out["packed"].shape == (0, 200) and out["scale"].shape == (0, 2)
+    gx, gw, gb = B.layer_norm_backward(gy[:0], x[:0], w, out["mean"], out["rstd"])
+    torch.cuda.synchronize()
+    assert gx.shape == (0, 200) and not gw.any() and not gb.any()
+    q, s = B.pack_activation(x[:0])
+    assert B.unpack_activation(q, s).shape == (0, 200)
+
+
+def test_wider_than_supported():
+    x = torch.zeros((2, 16385), device=DEV, dtype=torch.bfloat16)
+    w = torch.zeros(16385, device=DEV)
+    with pytest.raises(B.PpowError) as e:
+        B.layer_norm(x, w)
+    assert e.value.status == B.PPOW_ERR_UNSUPPORTED
+    q, s = B.pack_activation(x)                              # a checkpoint may be wider
+    assert torch.equal(B.unpack_activation(q, s), x)
+
+
+def test_streams_and_replays():
+    x, w, b, gy = make(900, 1000, torch.bfloat16, seed=8)
+    x2, _, _, gy2 = make(900, 1000, torch.bfloat16, seed=9)
+
+    def step(x, gy, **k):
+        out = B.layer_norm(x, w, b, checkpoint=True, **k)
+        q, s = B.pack_activation(gy, **k)
+        return (out["y"], *B.layer_norm_backward(gy, (out["packed"], out["scale"]), w, out["mean"], out["rstd"], **k),
+                B.unpack_activation(q, s, **k))
+    want, want2 = step(x, gy), step(x2, gy2)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        a, c = step(x, gy, stream=s1), step(x2, gy2, stream=s2)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(a, want)) and all(torch.equal(p, q) for p, q in zip(c, want2))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(x, gy)
+    x.copy_(x2), gy.copy_(gy2)
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want2))
+
+
+@pytest.mark.parametrize("R,D", [(5, 96), (3, 1531)])
+def test_gradient_against_differences_of_the_forward_pass(R, D):
+    # float32: along a unit direction d of the row's space the loss is smooth; its third derivative times h^2/6 and the forward
+    # pass's rounding over h bound the difference.  Along x + h d, y = w (x - mean) rstd + b with sigma about 1: derivatives of
+    # 1/sigma up to order three stay below 15 for |d| = 1 and sigma >= 1/2, hence below 15 max|gy w| sqrt(D) in all.
+    x, w, b, gy = make(R, D, torch.float32, seed=10, offset=0.0)
+    x = torch.randn((R, D), device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
+    g = torch.Generator(device=DEV).manual_seed(11)
+    d = torch.randn((R, D), generator=g, device=DEV)
+    d = d / d.norm(dim=1, keepdim=True)
+    h = 2.0 ** -5
+    at = [x + s * h * d for s in (1, -1)]
+    step = (at[0].double() - at[1].double())                 # what was added after rounding
+    loss = [(B.layer_norm(t, w, b)["y"].double() * gy.double()).sum(1) for t in at]
+    out = B.layer_norm(x, w, b)
+    gx, _, _ = B.layer_norm_backward(gy, x, w, out["mean"], out["rstd"])
+    got, want = (gx.double() * step).sum(1), loss[0] - loss[1]
+    a = (gy * w).double().abs()
+    smooth = 2 * h ** 3 / 6 * 15 * a.amax(1) * D ** 0.5
+    y = out["y"].double().abs()
+    rounding = 2 * (gy.double().abs() * (256 * E * (y + b.double().abs()) + 160 * E * x.double().abs().amax(1, keepdim=True) * w.double().abs())).sum(1)
+    back = (step.abs() * (256 * E * (a + a.mean(1, keepdim=True)) * 2)).sum(1)
+    assert torch.all((got - want).abs() <= smooth + rounding + back)
+    # and not by being loose: without the two mean terms the difference is far outside
+    naive = ((gy * w).double() * out["rstd"].double()[:, None] * step).sum(1)
+    assert float((naive - want).abs().max()) > 4 * float((got - want).abs().max())
