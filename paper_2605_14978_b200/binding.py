@@ -160,8 +160,25 @@ def load_library():
     lib.ppow_status_string.argtypes = [ctypes.c_int]
     lib.ppow_version.restype = ctypes.c_int
     lib.ppow_version.argtypes = []
+    _bind_calls(lib)
     _lib = lib
     return lib
+
+
+_calls = None
+CALLED = ("ppow_head_workspace_bytes", "ppow_head_logprob", "ppow_head_logprob_backward", "ppow_layer_norm",
+          "ppow_layer_norm_workspace_bytes", "ppow_layer_norm_backward", "ppow_pack_activation", "ppow_unpack_activation")
+
+
+def _bind_calls(lib) -> None:
+    """Hand the addresses of the training-end entry points to the extension module that marshals their calls."""
+    global _calls
+    try:
+        from . import _calls as module
+    except ImportError as e:
+        raise RuntimeError("_calls.so is missing or does not load (%s): build it with `python -m paper_2605_14978_b200.build`" % e)
+    module.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in CALLED})
+    _calls = module
 
 
 def ppow_status_string(status: int) -> str:
@@ -709,8 +726,21 @@ def select_windows(score, n_keep: int, want_mask: bool = False, stream=None):
     return (sel, mask) if want_mask else sel
 
 
-# The wrappers below hand the addresses of what they have just allocated straight to the library; sizes go to torch.empty as
-# plain integers, since a tuple takes it 0.8 us more.
+# The wrappers below go through the extension module first, which marshals a call in a fifth of the time and answers None where
+# something is not as it should be, or where the call is for another stream or device: the rest of the wrapper is for those.
+# It hands the addresses of what it has just allocated straight to the library.
+
+
+def _quick():
+    if _calls is None:
+        load_library()
+    return _calls
+
+
+def _done(got, where):
+    if got[0] != PPOW_OK:
+        raise PpowError(got[0], where)
+    return got[1:]
 
 
 def _workspace(nbytes: int, dev) -> torch.Tensor:
@@ -719,6 +749,11 @@ def _workspace(nbytes: int, dev) -> torch.Tensor:
 
 def head_logprob(hidden, weight, tokens, *, temperature=1.0, stream=None) -> dict:
     """Allocate outputs and workspace, run ppow_head_logprob; returns logp and lse, both [T] float32."""
+    if stream is None:
+        got = _quick().head_logprob(hidden, weight, tokens, temperature)
+        if got is not None:
+            logp, lse = _done(got, "ppow_head_logprob")
+            return {"logp": logp, "lse": lse}
     params, lib, f32 = make_head_params(hidden, weight, temperature), load_library(), torch.float32
     T, V, D, dt, device, dev = params.T, params.V, params.D, hidden.dtype, hidden.device, _index_of(hidden, "hidden")
     h, w = _rows_arg(hidden, dt, (T, D), dev, "hidden")[0], _rows_arg(weight, dt, (V, D), dev, "weight")[0]
@@ -734,6 +769,10 @@ def head_logprob(hidden, weight, tokens, *, temperature=1.0, stream=None) -> dic
 
 def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature=1.0, want_hidden=True, want_weight=True, stream=None):
     """Allocate gradients and workspace, run ppow_head_logprob_backward; returns (grad_hidden, grad_weight), None where not wanted."""
+    if stream is None:
+        got = _quick().head_logprob_backward(hidden, weight, tokens, lse, grad_logp, temperature, want_hidden, want_weight)
+        if got is not None:
+            return _done(got, "ppow_head_logprob_backward")
     params, lib, f32 = make_head_params(hidden, weight, temperature), load_library(), torch.float32
     T, V, D, dt, device, dev = params.T, params.V, params.D, hidden.dtype, hidden.device, _index_of(hidden, "hidden")
     h, w = _rows_arg(hidden, dt, (T, D), dev, "hidden")[0], _rows_arg(weight, dt, (V, D), dev, "weight")[0]
@@ -752,6 +791,14 @@ def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature
 def layer_norm(x, weight, bias=None, *, eps=1e-5, checkpoint=False, stream=None) -> dict:
     """Allocate outputs and run ppow_layer_norm on ``x`` [R, D]; returns y, mean, rstd and, with ``checkpoint``, the 8-bit form of
     ``x`` as packed and scale."""
+    if stream is None:
+        got = _quick().layer_norm(x, weight, bias, eps, checkpoint)
+        if got is not None:
+            y, mean, rstd, packed, scale = _done(got, "ppow_layer_norm")
+            out = {"y": y, "mean": mean, "rstd": rstd}
+            if checkpoint:
+                out["packed"], out["scale"] = packed, scale
+            return out
     R, D = x.shape
     dt, pt, device, dev, f32 = x.dtype, weight.dtype, x.device, _index_of(x, "x"), torch.float32
     params = make_norm_params(R, D, dt, pt, eps)
@@ -771,6 +818,11 @@ def layer_norm(x, weight, bias=None, *, eps=1e-5, checkpoint=False, stream=None)
 def layer_norm_backward(grad_y, x, weight, mean, rstd, *, want_bias=True, stream=None):
     """Allocate gradients and workspace, run ppow_layer_norm_backward; returns (grad_x, grad_weight, grad_bias or None).
     ``x`` is the forward pass's input or the pair (packed, scale) that the forward pass left."""
+    if stream is None:
+        direct, (packed, scale) = (None, x) if isinstance(x, (tuple, list)) else (x, (None, None))
+        got = _quick().layer_norm_backward(grad_y, direct, packed, scale, weight, mean, rstd, want_bias)
+        if got is not None:
+            return _done(got, "ppow_layer_norm_backward")
     R, D = grad_y.shape
     dt, pt, device, dev, f32 = grad_y.dtype, weight.dtype, grad_y.device, _index_of(grad_y, "grad_y"), torch.float32
     params, lib = make_norm_params(R, D, dt, pt), load_library()
@@ -798,6 +850,10 @@ def _alloc_packed(R: int, D: int, device):
 
 def pack_activation(x, stream=None):
     """Allocate and run ppow_pack_activation; returns (packed, scale)."""
+    if stream is None:
+        got = _quick().pack_activation(x)
+        if got is not None:
+            return _done(got, "ppow_pack_activation")
     R, D = x.shape
     code, dev = _storage_code(x.dtype, "x"), _index_of(x, "x")
     xp, xs = _rows_arg(x, x.dtype, (R, D), dev, "x")
@@ -810,6 +866,10 @@ def pack_activation(x, stream=None):
 
 def unpack_activation(packed, scale, dtype=torch.bfloat16, stream=None):
     """Allocate and run ppow_unpack_activation; returns the restored activation in ``dtype``."""
+    if stream is None and dtype in DTYPE_CODES:
+        got = _quick().unpack_activation(packed, scale, DTYPE_CODES[dtype])
+        if got is not None:
+            return _done(got, "ppow_unpack_activation")[0]
     R, D = packed.shape
     code, dev = _storage_code(dtype, "dtype"), _index_of(packed, "packed")
     q, s = _packed_args(packed, scale, R, D, dev)

@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import glob
 import os
+import shutil
 import subprocess
 import sys
 
@@ -11,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libppow.so")
 LIB_CHECKED = os.path.join(HERE, "libppow_checked.so")   # the same sources with -DPPOW_CHECKED (bounds-checked build)
 LIB_TIMELINE = os.path.join(HERE, "libppow_timeline.so")  # ... with -DPPOW_TIMELINE (per-warp timeline of the row kernel)
+CALLS = os.path.join(HERE, "_calls.so")                 # csrc/ppow_calls.cpp: one call from Python per training-end operator
 ROOT = os.path.dirname(HERE)
 
 
@@ -29,10 +31,34 @@ def is_stale(lib: str = LIB) -> bool:
     return any(os.path.getmtime(f) > t for f in _deps())
 
 
+def build_calls(force: bool = False) -> str:
+    """Compile the extension module that marshals the training-end calls, against the torch that is installed."""
+    src = os.path.join(CSRC, "ppow_calls.cpp")
+    deps = [src, os.path.join(ROOT, "include", "ppow.h")]
+    if not force and os.path.exists(CALLS) and all(os.path.getmtime(f) <= os.path.getmtime(CALLS) for f in deps):
+        return CALLS
+    import sysconfig
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(shutil.which(os.environ.get("NVCC", "nvcc")) or "/usr/local/cuda/bin/nvcc"))
+    tmp = CALLS + ".tmp.%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+           "-I" + os.path.join(at, "include"), "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
+           "-I" + os.path.join(cuda, "include"), "-I" + sysconfig.get_path("include"), src, "-o", tmp,
+           "-L" + os.path.join(at, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + res.stderr)
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = False, timeline: bool = False) -> str:
     """Compile every .cu under csrc/ into one shared library for sm_100a.  ``checked``: the bounds-checked
     build (every kernel-computed index tested before use, failures counted and skipped, never trapped)."""
     lib = LIB_CHECKED if checked else LIB_TIMELINE if timeline else LIB
+    build_calls(force and lib == LIB)
     if not force and not is_stale(lib):
         return lib
     nvcc = os.environ.get("NVCC", "nvcc")
