@@ -48,7 +48,7 @@ template <int N> __host__ __device__ constexpr size_t mma_smem()
     return 1024 + (size_t)stage_count<N>() * stage_bytes<N>() + (N == 256 ? 2 * BOX_BYTES : 0) + 256;
 }
 
-constexpr int GATHER_THREADS = 256;
+constexpr int GATHER_THREADS = 256, EARLY = 4;
 constexpr int GATHER_ROWS_MAX = 1024, GATHER_CTAS = 1024;
 constexpr size_t HEADER_BYTES = 256;
 constexpr size_t DZ_BYTES = 512u << 20;      // a piece of dz holds at most this much
@@ -95,18 +95,20 @@ struct GatherJob {
 // Shares of the inner axis of dh: `tiles` output tiles times the shares should fill whole rounds of the pairs.  A share is
 // at least eight steps long, and each one costs a pass over its sums (2 % of a round is about what that measures).
 constexpr int32_t SPLIT_TILES = 8 * PAIRS;      // tiles x shares where there is more than one share
-__device__ __forceinline__ int32_t split_count(int32_t tiles, int32_t steps)
+__device__ __forceinline__ int32_t split_count(int32_t tiles, int32_t steps)      // one warp, a candidate per lane and turn
 {
-    int32_t best = 1;
-    float best_cost = (float)((tiles + PAIRS - 1) / PAIRS);
-    for (int32_t s = 2; s <= PAIRS && s * 8 <= steps && s * tiles <= SPLIT_TILES; ++s) {
-        const float cost = (float)((tiles * s + PAIRS - 1) / PAIRS) / (float)s * (1.0f + 0.02f * (float)min(s, 10));
+    float best_cost = INFINITY;
+    uint32_t best = 1;
+    for (int32_t s = 1 + (int32_t)(threadIdx.x & 31); s <= PAIRS; s += 32) {
+        if (s > 1 && (s * 8 > steps || s * tiles > SPLIT_TILES)) break;
+        const float cost = (float)((tiles * s + PAIRS - 1) / PAIRS) / (float)s * (1.0f + 0.02f * (float)min(s - 1, 10));
         if (cost < best_cost) {
             best_cost = cost;
-            best = s;
+            best = (uint32_t)s;
         }
     }
-    return best;
+    const uint32_t lowest = __reduce_min_sync(0xffffffffu, __float_as_uint(best_cost));        // costs are positive
+    return (int32_t)__reduce_min_sync(0xffffffffu, __float_as_uint(best_cost) == lowest ? best : ~0u);
 }
 
 // mult of a row, and for f16 the split into a factor near 2^15 and a power of two: dz of a row whose gradient is small
@@ -126,22 +128,31 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
     __shared__ int32_t part[4][GATHER_THREADS / 32];
     __shared__ int32_t dest[GATHER_ROWS_MAX];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    allow_next_kernel();
     wait_for_previous_kernel();
     const int32_t r0 = (int32_t)min((int64_t)blockIdx.x * job.rows_per_cta, (int64_t)job.T);
     const int32_t n = min(job.rows_per_cta, job.T - r0);
-    auto live = [&](int32_t i) {
-        const int32_t y = job.tokens[i];
-        if (BACKWARD) return y >= 0 && y < job.V && !(job.grad[i] == 0.0f);
-        return y >= 0;
-    };
+    // rows that start on 16-byte boundaries are on their way before it is known where they go
+    const int32_t units = job.D / 8, all = n * units;
+    uint4 early[EARLY];
+    if (job.vec) {
+#pragma unroll
+        for (int j = 0; j < EARLY; ++j) {
+            const int32_t i = tid + j * GATHER_THREADS;
+            if (i < all) early[j] = __ldg(reinterpret_cast<const uint4 *>(job.hidden + (size_t)(r0 + i / units) * job.stride) + i % units);
+        }
+    }
+    auto live = [&](int32_t y, float g) { return BACKWARD ? y >= 0 && y < job.V && !(g == 0.0f) : y >= 0; };
     int32_t before = 0, total = 0, top = -1000, range = 0;
     for (int32_t i = tid; i < job.T; i += GATHER_THREADS) {
-        const bool ok = live(i);
+        const int32_t y = job.tokens[i];
+        const float g = BACKWARD ? job.grad[i] : 1.0f;
+        const bool ok = live(y, g);
         total += ok;
         before += ok && i < r0;
-        range |= job.tokens[i] >= job.V;
+        range |= y >= job.V;
         if (SCALED && ok) {
-            const float m = row_mult(job.grad[i], job.inv_temperature);
+            const float m = row_mult(g, job.inv_temperature);
             if (isfinite(m) && m != 0.0f) top = max(top, row_exponent(m, 0));
         }
     }
@@ -170,15 +181,17 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
         out.header->error_flags = range ? (unsigned)PPOW_FLAG_TOKEN_RANGE : 0u;
         out.header->live = total;
         out.header->out_scale = SCALED ? ldexpf(1.0f, top - 15) : 1.0f;
-        if (BACKWARD) {
-            const int64_t tiles = (int64_t)(job.few ? 1 : max(1, (total + TILE - 1) / TILE)) * job.d_tiles;
-            out.header->splits = tiles > SPLIT_TILES ? 1 : split_count((int32_t)tiles, job.piece_steps);
-        }
+    }
+    if (BACKWARD && blockIdx.x == 0 && warp == 1) {
+        const int64_t tiles = (int64_t)(job.few ? 1 : max(1, (total + TILE - 1) / TILE)) * job.d_tiles;
+        const int32_t splits = tiles > SPLIT_TILES ? 1 : split_count((int32_t)tiles, job.piece_steps);
+        if (lane == 0) out.header->splits = splits;
     }
     if (warp == 0) {
         int32_t next = before;
         for (int32_t k = 0; k < n; k += 32) {
-            const bool ok = k + lane < n && live(r0 + k + lane);
+            const int32_t r = min(r0 + k + lane, job.T - 1);
+            const bool ok = k + lane < n && live(job.tokens[r], BACKWARD ? job.grad[r] : 1.0f);
             const unsigned m = __ballot_sync(0xffffffffu, ok);
             if (k + lane < n) dest[k + lane] = ok ? next + __popc(m & ((1u << lane) - 1u)) : -1;
             next += __popc(m);
@@ -209,22 +222,11 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
         }
     }
     // the rows themselves, by 16-byte units
-    const int32_t units = job.D / 8;
-    for (int32_t i = tid; i < n * units; i += GATHER_THREADS) {
+    auto put = [&](int32_t i, uint4 x) {
         const int32_t k = i / units, u = i % units, r = r0 + k, d = dest[k];
         if (d < 0) {
             if (BACKWARD && job.grad_hidden) reinterpret_cast<uint4 *>(job.grad_hidden + (size_t)r * job.D)[u] = make_uint4(0, 0, 0, 0);
-            continue;
-        }
-        const uint16_t *src = job.hidden + (size_t)r * job.stride;
-        uint4 x;
-        if (job.vec) {
-            x = __ldg(reinterpret_cast<const uint4 *>(src) + u);
-        } else {
-            uint32_t w[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) w[q] = (uint32_t)src[u * 8 + 2 * q] | ((uint32_t)src[u * 8 + 2 * q + 1] << 16);
-            x = make_uint4(w[0], w[1], w[2], w[3]);
+            return;
         }
         reinterpret_cast<uint4 *>((uint16_t *)out.rows + (size_t)d * job.D)[u] = x;
         if (SCALED) {
@@ -237,6 +239,21 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
                 w[q] = *reinterpret_cast<const uint32_t *>(&s);
             }
             reinterpret_cast<uint4 *>((uint16_t *)out.scaled + (size_t)d * job.D)[u] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    };
+    if (job.vec) {
+#pragma unroll
+        for (int j = 0; j < EARLY; ++j)
+            if (tid + j * GATHER_THREADS < all) put(tid + j * GATHER_THREADS, early[j]);
+        for (int32_t i = tid + EARLY * GATHER_THREADS; i < all; i += GATHER_THREADS)
+            put(i, __ldg(reinterpret_cast<const uint4 *>(job.hidden + (size_t)(r0 + i / units) * job.stride) + i % units));
+    } else {
+        for (int32_t i = tid; i < all; i += GATHER_THREADS) {
+            const uint16_t *src = job.hidden + (size_t)(r0 + i / units) * job.stride + i % units * 8;
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = (uint32_t)src[2 * q] | ((uint32_t)src[2 * q + 1] << 16);
+            put(i, make_uint4(w[0], w[1], w[2], w[3]));
         }
     }
     // the last tile's rows behind the live ones are zeros: they are products' operands too
