@@ -42,31 +42,18 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity)
-{
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return done != 0;
-}
-
 // Bounded wait of the matrix kernels: false once WAIT_NS have passed without the phase completing.  The longest
 // proper wait is one tile's products (well under 10 ms for the largest sizes accepted).
 constexpr uint64_t MMA_WAIT_NS = 2000000000ull;
 __device__ __forceinline__ bool mbar_wait_ns(uint32_t bar, uint32_t parity)
 {
     for (int i = 0; i < 64; ++i)
-        if (mbar_try_wait_cluster(bar, parity)) return true;
+        if (mbar_try_wait(bar, parity)) return true;
     uint64_t t0, t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
     do {
         for (int i = 0; i < 64; ++i)
-            if (mbar_try_wait_cluster(bar, parity)) return true;
+            if (mbar_try_wait(bar, parity)) return true;
         asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     } while (t - t0 < MMA_WAIT_NS);
     return false;
