@@ -296,7 +296,8 @@ ppow_status ppow_head_logprob(const ppow_head_params *params, const void *hidden
  * Gradient of sum_i grad_logp[i] * logp[i] with respect to hidden and weight:
  *     dz_i = grad_logp[i] / temperature * (onehot(y_i) - softmax(z_i))     grad_hidden = dz weight     grad_weight = dz^T hidden
  * dz is rounded to the storage type (a relative error of at most half a step per term, of the size of the operands' own
- * rounding); for PPOW_F16 each row of it is brought near 2^15 by a power of two first, which is undone after the sums.
+ * rounding); for PPOW_F16 each row of it is brought near 2^15 by a power of two first, which is undone after the sums.  What the
+ * rounding of a row's largest term, the one at its token, leaves over is added to grad_hidden in float32.
  * The sums are float32 in a fixed order: equal inputs give equal results.
  *   hidden, weight, tokens   as above.  Rows with a negative token, a token >= V (which sets PPOW_FLAG_TOKEN_RANGE) or
  *                            grad_logp == 0 are masked: their gradient is 0 and they add nothing to grad_weight.
@@ -332,7 +333,8 @@ typedef struct {
  * value is x / 2^e rounded to nearest even in e4m3 (1 sign, 4 exponent, 3 mantissa bits; no infinity).  A value that is
  * not finite becomes NaN.
  *   packed   device, [R, D] bytes, contiguous: the e4m3 codes
- *   scale    device, [R, ceil(D / 128)] bytes, contiguous: e + 127
+ *   scale    device, [R, ceil(D / 128)] bytes, contiguous: e + 127 (1 .. 247).  Read in aligned 4-byte words: up to 3 bytes on
+ *            either side of it, of the same words, are read too.
  * Restored values are code * 2^e, rounded once to the storage type (exact in float32 and, but for subnormals, in bfloat16).
  */
 

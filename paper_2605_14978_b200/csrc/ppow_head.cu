@@ -71,6 +71,7 @@ struct HeadRows {
     float *mult;           // dz = mult * (softmax - onehot)
     float *lse2;           // normaliser in log2 units
     float *row_scale;      // dh = row_scale * (dz W)
+    float *residual;       // what the rounding of dz at the token left over
     void *rows;            // [padded, D] hidden states
     void *scaled;          // f16 backward: the same times a power of two per row
 };
@@ -311,6 +312,20 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+template <bool BF16>
+__device__ __forceinline__ float2 unpack2(uint32_t w)
+{
+    if (BF16) return make_float2(bf16_lo(w), bf16_hi(w));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+}
+
+// x minus x rounded to 16 bits
+template <bool BF16>
+__device__ __forceinline__ float rounding_of(float x)
+{
+    return x - (BF16 ? __bfloat162float(__float2bfloat16_rn(x)) : __half2float(__float2half_rn(x)));
+}
+
 // What a launch works on: sizes that follow from the number of live rows.
 struct Extent {
     int32_t live, row_tiles, splits;
@@ -460,9 +475,11 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
 #pragma unroll
             for (int j = 0; j < 32; ++j) p[j] = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -lse2));
             if (at >= c && at < c + 32) {
+                float target = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (at == c + j) p[j] -= 1.0f;
+                    if (at == c + j) target = p[j] -= 1.0f;
+                if (row < e.live) job.rows.residual[row] = rounding_of<BF16>(target * mult);
             }
             if (row >= e.live || c + 32 > left) {
 #pragma unroll
@@ -592,8 +609,10 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
             for (int j = 0; j < WIDTH; ++j) {
                 const float l = __shfl_sync(0xffffffffu, lse2, j), m = __shfl_sync(0xffffffffu, mult, j);
                 float d = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -l));
-                if (__shfl_sync(0xffffffffu, token, j) == row) d -= 1.0f;
+                const bool target = __shfl_sync(0xffffffffu, token, j) == row;
+                if (target) d -= 1.0f;
                 d = inside && first + c + j < e.live ? d * m : 0.0f;
+                if (target) job.rows.residual[first + c + j] = rounding_of<BF16>(d);
                 if (PPOW_CHECK(x.index * TILE + in_tile < job.piece, 507, flags))
                     to[(size_t)(first + c + j) * job.piece] = (uint16_t)pack2<BF16>(d, 0.0f);
             }
@@ -876,7 +895,8 @@ __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows
 constexpr int FINISH_THREADS = 128;
 template <bool BF16>
 __global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows rows, const float *__restrict__ parts, int32_t few,
-                                                                     int32_t D, uint16_t *__restrict__ grad_hidden)
+                                                                     int32_t D, const uint16_t *__restrict__ weight,
+                                                                     int64_t weight_stride, uint16_t *__restrict__ grad_hidden)
 {
     wait_for_previous_kernel();
     const int32_t units = D / 4, splits = rows.header->splits, live = rows.header->live;
@@ -898,6 +918,11 @@ __global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows ro
             const float4 a = p[s * split_units];
             f.x += a.x, f.y += a.y, f.z += a.z, f.w += a.w;
         }
+        // the token's entry of dz is most of the row: what its rounding left over comes back here, in float32
+        const uint2 wy = *(reinterpret_cast<const uint2 *>(weight + (size_t)rows.token[row] * weight_stride) + u);
+        const float rest = rows.residual[row];
+        const float2 w01 = unpack2<BF16>(wy.x), w23 = unpack2<BF16>(wy.y);
+        f.x = fmaf(rest, w01.x, f.x), f.y = fmaf(rest, w01.y, f.y), f.z = fmaf(rest, w23.x, f.z), f.w = fmaf(rest, w23.y, f.w);
         const float k = rows.row_scale[row];
         reinterpret_cast<uint2 *>(grad_hidden + (size_t)rows.source[row] * D)[u] =
             make_uint2(pack2<BF16>(f.x * k, f.y * k), pack2<BF16>(f.z * k, f.w * k));
@@ -922,7 +947,7 @@ bool params_ok(const ppow_head_params *p)
 int32_t tile_columns(int32_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : TILE; }
 
 struct Layout {
-    size_t source, token, mult, lse2, row_scale, rows, scaled, partial, at_token, dz, grad_rows, total;
+    size_t source, token, mult, lse2, row_scale, residual, rows, scaled, partial, at_token, dz, grad_rows, total;
     int32_t columns, few, padded, v_tiles, d_tiles, piece, parts;
 };
 
@@ -946,6 +971,7 @@ Layout layout_of(const ppow_head_params *p, bool backward)
     L.mult = take(rows * 4);
     L.lse2 = take(rows * 4);
     L.row_scale = take(rows * 4);
+    L.residual = take(rows * 4);
     L.rows = take(rows * p->D * 2);
     if (!backward) {
         // few tokens: four warps of each CTA; there are at most as many pairs as tiles
@@ -1062,6 +1088,7 @@ HeadRows rows_of(char *ws, const Layout &L)
     r.mult = (float *)(ws + L.mult);
     r.lse2 = (float *)(ws + L.lse2);
     r.row_scale = (float *)(ws + L.row_scale);
+    r.residual = (float *)(ws + L.residual);
     r.rows = ws + L.rows;
     r.scaled = ws + L.scaled;
     return r;
@@ -1169,7 +1196,7 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     if (grad_hidden) {
         const int64_t blocks = ((int64_t)p->T * (p->D / 4) + FINISH_THREADS - 1) / FINISH_THREADS;
         if (!launch_after(head_finish_kernel<BF16>, (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16), FINISH_THREADS, 0, stream, rows,
-                          job.grad_rows, L.few, p->D, (uint16_t *)grad_hidden))
+                          job.grad_rows, L.few, p->D, (const uint16_t *)weight, p->weight_stride, (uint16_t *)grad_hidden))
             return PPOW_ERR_CUDA;
     }
     return PPOW_OK;

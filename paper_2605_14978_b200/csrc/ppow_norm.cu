@@ -421,7 +421,7 @@ template <typename DealT, bool PACKED, int TPR, int U, int S> struct ScalarsAhea
     static constexpr int LANES = DealT::BLOCK_LANES, PER_UNIT = 32 / LANES;      // blocks that a warp's 32 units span
     static constexpr int WORDS = 2 + (PACKED ? U * PER_UNIT : 0);
     static_assert(WORDS <= 32, "one lane per word");
-    static constexpr size_t BYTES = (size_t)S * (TPR / 32) * WORDS * 4 + 16;
+    static constexpr size_t BYTES = ((size_t)S * (TPR / 32) * WORDS * 4 + 15) / 16 * 16;      // what follows starts on 16 bytes again
     uint32_t *own;                   // the warp's words in slot 0
     __device__ __forceinline__ ScalarsAhead(uint8_t *smem, int t) : own(reinterpret_cast<uint32_t *>(smem) + t / 32 * WORDS) {}
     static __device__ __forceinline__ int32_t block_of(int t, int k, int j) { return ((t & ~31) + k * TPR) / LANES + j; }
