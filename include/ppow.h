@@ -275,7 +275,8 @@ typedef struct {
     float temperature;      /* > 0 */
 } ppow_head_params;
 
-/* Bytes of device scratch for these parameters (0 on invalid ones); backward != 0: for the gradient.  The gradient
+/* Bytes of device scratch for these parameters (0 on invalid ones); backward != 0: for the gradient.  The forward pass
+ * keeps 8 bytes for every 128 logits (1/32 of what 16-bit logits would take) and a copy of the live rows; the gradient
  * works on pieces of the vocabulary; its scratch holds one piece of dz (at most 512 MiB, or 256 vocabulary entries),
  * float32 sums of grad_hidden and a copy of the live rows. */
 size_t ppow_head_workspace_bytes(const ppow_head_params *params, int backward);

@@ -10,7 +10,7 @@
 //             per row; `merge` joins them in float64
 //   backward  per piece of the vocabulary: logits again, dz rounded to the operands' 16-bit type; dW of the piece, and the
 //             piece's share of dh added to float32 sums; `finish` rounds dh once
-// All three products run in one kernel template on tcgen05 (ppow_mma.cuh).
+// All products run in one kernel template on tcgen05 (ppow_mma.cuh).
 #include "../../include/ppow.h"
 #include "ppow_checked.cuh"
 #include "ppow_device.cuh"
@@ -31,7 +31,7 @@ constexpr uint32_t A_BYTES = HALF_TILE * BK * 2;           // 16 KB
 constexpr int MMA_THREADS = 320;     // producer warp, issuing warp, eight epilogue warps
 constexpr int PAIRS = 74;            // pairs of SMs that the shares of an inner axis are planned for
 // Steps that the logits of the forward pass are summed over in Tensor Memory before the sum moves on to registers: the tensor
-// cores' additions cut off what does not fit, and over 256 steps of 16 that left lse off by 3e-6 (4096 wide); like this 5e-7.
+// cores' additions cut off what does not fit, and over 256 steps of 16 that left lse off by 3e-6 (4096 wide); like this 7e-7.
 constexpr int SUM_STEPS = 16;
 constexpr int MAX_PAIRS = 128;       // pairs that a launch uses at most
 

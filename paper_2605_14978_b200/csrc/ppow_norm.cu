@@ -860,6 +860,14 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const PackJob job)
         x[i].zero();
         if (ahead.row < job.R && u < units) x[i].load(static_cast<const T *>(job.x) + ahead.row * job.x_stride, u, job.D);
     }
+    if (at.row < job.R && at.chunk + PACK_CHUNKS <= per_row && PPOW_CHECK(at.chunk >= 0, 605, nullptr)) {
+        // all in one row: their maxima go through the lanes together
+        float f[PACK_CHUNKS][DealT::E];
+#pragma unroll
+        for (int i = 0; i < PACK_CHUNKS; ++i) x[i].get(f[i]);
+        pack_units<DealT, PACK_CHUNKS>(f, at.chunk * 32 + lane, 32, units, job.D, job.codes + at.row * job.D, job.scales + at.row * job.blocks);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < PACK_CHUNKS; ++i, at.step(per_row)) {
         const int32_t u = at.chunk * 32 + lane;
