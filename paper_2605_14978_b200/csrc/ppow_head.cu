@@ -30,9 +30,6 @@ constexpr int BK = 64;               // products' inner step per pipeline stage:
 constexpr uint32_t A_BYTES = HALF_TILE * BK * 2;           // 16 KB
 constexpr int MMA_THREADS = 320;     // producer warp, issuing warp, eight epilogue warps
 constexpr int PAIRS = 74;            // pairs of SMs that the shares of an inner axis are planned for
-// Steps that the logits of the forward pass are summed over in Tensor Memory before the sum moves on to registers: the tensor
-// cores' additions cut off what does not fit, and over 256 steps of 16 that left lse off by 3e-6 (4096 wide); like this 7e-7.
-constexpr int SUM_STEPS = 16;
 constexpr int MAX_PAIRS = 128;       // pairs that a launch uses at most
 
 // Columns of a tile: 256, or for few tokens the tokens themselves (16, 32, 64 or 128), with W taking the 256 rows.
@@ -41,6 +38,10 @@ template <int N> __host__ __device__ constexpr int stage_count()
 {
     return N == 256 ? 6 : N == 128 ? 8 : N == 64 ? 10 : N == 32 ? 11 : 12;    // 192 to 204 KB
 }
+// Steps that the logits of the forward pass are summed over in Tensor Memory before the sum moves on to registers: the tensor
+// cores' additions cut off what does not fit, and over 256 products (4096 wide) that left lse off by 3e-6.  16 steps leave
+// 7e-7 and cost a large batch 3.6 % (8: 8 %); with few tokens, where a single log-probability close to 0 shows it more, 4 are free.
+template <int N> __host__ __device__ constexpr int sum_steps() { return N == 256 ? 16 : N == 128 ? 8 : 4; }
 // Tiles of 16-bit results leave through shared memory: a box of 128 rows x 64 columns for each half of the columns.
 constexpr uint32_t BOX_BYTES = HALF_TILE * 128;
 template <int N> __host__ __device__ constexpr size_t mma_smem()
@@ -428,6 +429,7 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
     constexpr int COLS = TILE / 2;
     const int32_t row = x.row + in_tile;                     // a live row, or for GRAD_WEIGHT an entry of the piece
     const int32_t first = half * COLS;                       // this warp's columns of the tile
+    [[maybe_unused]] const int lane = threadIdx.x & 31;
     src += first;
     [[maybe_unused]] unsigned int *flags = &job.rows.header->error_flags;
     if (PRODUCT == LOGITS_SUM) {
@@ -516,8 +518,33 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
         });
     } else {
         const float out_scale = job.rows.header->out_scale;
+        // With up to 32 tokens one rounding of dz is most of the error of its token's row of dW (over more tokens they average out):
+        // its remainder times the token's hidden state is added here.  Lane i looks at token i.
+        const int32_t mine = lane < e.live && e.live <= 32 ? job.rows.token[lane] - (job.v0 + row - lane) : -1;
+        const unsigned hits = __ballot_sync(0xffffffffu, mine >= 0 && mine < 32);
+        const uint16_t *states = static_cast<const uint16_t *>(BF16 ? job.rows.rows : job.rows.scaled) + x.col + first;
         const int32_t v = x.row + in_tile / HALF_TILE * HALF_TILE;       // the box's first row within the piece
         for_chunks<COLS / 32, 32>(src, release, [&](int c, uint32_t (&w)[32]) {
+            for (unsigned m = hits; m; m &= m - 1) {
+                const int i = __ffs(m) - 1;
+                if (__shfl_sync(0xffffffffu, mine, i) == lane) {
+                    const float rest = job.rows.residual[i];
+                    const uint4 *h = reinterpret_cast<const uint4 *>(states + (size_t)i * job.D + c);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (x.col + first + c + 8 * q < job.D) {
+                            const uint4 u = h[q];
+                            const uint32_t p[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 f = unpack2<BF16>(p[j]);
+                                w[8 * q + 2 * j] = __float_as_uint(fmaf(rest, f.x, __uint_as_float(w[8 * q + 2 * j])));
+                                w[8 * q + 2 * j + 1] = __float_as_uint(fmaf(rest, f.y, __uint_as_float(w[8 * q + 2 * j + 1])));
+                            }
+                        }
+                }
+                __syncwarp();
+            }
             uint32_t o[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -732,7 +759,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
             for (int64_t t = pair; t < tiles && ok; t += pairs) {
                 const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
                 for (int32_t k0 = x.k0; ok && (k0 < x.k1 || k0 == x.k0); ++acc) {
-                    const int32_t k1 = PARTS ? min(k0 + SUM_STEPS, x.k1) : x.k1;
+                    const int32_t k1 = PARTS ? min(k0 + sum_steps<N>(), x.k1) : x.k1;
                     const uint32_t b = acc & 1u, d = tmem + b * TILE;
                     ok = mbar_wait_ns(acc_empty(b), ((acc >> 1) & 1u) ^ 1u);
                     tcgen05_fence_after();
@@ -774,7 +801,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                     own.lse2 = job.rows.lse2[x.row + in_tile];
                 }
             }
-            const int32_t parts = PARTS ? (x.k1 - x.k0 + SUM_STEPS - 1) / SUM_STEPS : 1;
+            const int32_t parts = PARTS ? (x.k1 - x.k0 + sum_steps<N>() - 1) / sum_steps<N>() : 1;
             for (int32_t part = 0; part < parts; ++part, ++acc) {
                 const uint32_t b = acc & 1u;
                 // all four warps of a half go on or none does: they meet at barriers further down
@@ -1059,7 +1086,7 @@ bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap 
 {
     const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
     // one part is a kernel of its own: the loop over parts costs it a third (2048 x 128 x 128256: 106 us, with the loop 140)
-    if (PRODUCT == LOGITS_SUM && job.D > SUM_STEPS * BK)
+    if (PRODUCT == LOGITS_SUM && job.D > sum_steps<N>() * BK)
         return launch_after(head_product_kernel<PRODUCT, BF16, N, PRODUCT == LOGITS_SUM>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, job);
     return launch_after(head_product_kernel<PRODUCT, BF16, N, false>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, job);
 }

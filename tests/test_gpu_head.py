@@ -330,3 +330,31 @@ def test_gradient_against_differences_of_the_forward_pass(T):
     tol = grad.double().abs() * (step ** 2 / 6 * spread ** 3 + err / step)
     dh, th, _, _ = gradient(h, w, tok, out["lse"], grad, 1.0)
     assert torch.all((got - want).abs() <= tol + th.sum(1))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T", [1, 2, 5, 22, 32])
+def test_few_tokens_lose_no_more_than_the_rounding_of_the_results(T, dtype):
+    # One rounding of values v is off by at most half a step; uniform within it, the error's root mean square is a step / sqrt(12)
+    # = 2u / sqrt(12) = 0.577 u of the power of two below v, so of v at most.  dz is rounded too, but its largest terms are made
+    # good and the others average out: 0.62 u.  With dz rounded and left at that a call of one token is off by up to u.
+    u = U[dtype]
+    for seed in range(6):
+        h, w, tok, grad = make(T, 4001, 200, dtype, seed=30 + seed, masked=0.0)
+        out, gh, gw = run(h, w, tok, grad)
+        dh, _, dw, _ = gradient(h, w, tok, out["lse"], grad, 1.0)
+        assert float((gh.double() - dh).norm() / dh.norm()) < 0.62 * u
+        assert float((gw.double() - dw).norm() / dw.norm()) < 0.62 * u
+
+
+def test_a_single_confident_token_keeps_its_log_probability():
+    # logp close to 0 is a difference of two numbers near 20: what the sums cut off would show
+    for seed in range(8):
+        h, w, tok, _ = make(1, 1000, 4096, torch.bfloat16, seed=60 + seed, masked=0.0)
+        out = B.head_logprob(h, w, tok, temperature=0.7)
+        z = h.double() @ w.double().t() / 0.7
+        lse = torch.logsumexp(z, 1)
+        # 16 partial sums of 16 additions of 16 products, each off by at most a step 2^-23 of |z| <= 64, and their sum
+        assert float((out["lse"].double() - lse).abs()) < (16 + 16) * 2.0 ** -23 * 64
+        want = z[0, int(tok[0])] - lse[0]
+        assert float((out["logp"][0].double() - want).abs()) < 2 * (16 + 16) * 2.0 ** -23 * 64
