@@ -1,11 +1,13 @@
 """Build ``libppow.so`` (sm_100a only) in-tree with nvcc.  ``python -m paper_2605_14978_b200.build``."""
 from __future__ import annotations
 
+import concurrent.futures
 import glob
 import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -62,16 +64,23 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False, tim
     if not force and not is_stale(lib):
         return lib
     nvcc = os.environ.get("NVCC", "nvcc")
-    tmp = lib + ".tmp.%d" % os.getpid()
-    cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-o", tmp] + (["-DPPOW_CHECKED"] if checked else ["-DPPOW_TIMELINE"] if timeline else []) + sources()
-    if verbose:
-        cmd[1:1] = ["-Xptxas", "-v"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose:
-        sys.stderr.write(res.stderr)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stderr)
+    flags = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-Xcompiler", "-fPIC"]
+    flags += ["-Xptxas", "-v"] if verbose else []
+    flags += ["-DPPOW_CHECKED"] if checked else ["-DPPOW_TIMELINE"] if timeline else []
+
+    def run(cmd):
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if verbose:
+            sys.stderr.write(res.stderr)
+        if res.returncode != 0:
+            raise RuntimeError("nvcc failed:\n" + res.stderr)
+
+    with tempfile.TemporaryDirectory(prefix="ppow_build_") as objects:       # one compiler per source file, side by side
+        outs = [os.path.join(objects, os.path.basename(src) + ".o") for src in sources()]
+        with concurrent.futures.ThreadPoolExecutor(max_workers=os.cpu_count() or 1) as pool:
+            list(pool.map(lambda so: run([nvcc] + flags + ["-c", so[0], "-o", so[1]]), zip(sources(), outs)))
+        tmp = lib + ".tmp.%d" % os.getpid()
+        run([nvcc] + flags + ["-shared", "-o", tmp] + outs)
     os.replace(tmp, lib)
     return lib
 
