@@ -358,3 +358,29 @@ def test_a_single_confident_token_keeps_its_log_probability():
         assert float((out["lse"].double() - lse).abs()) < (16 + 16) * 2.0 ** -23 * 64
         want = z[0, int(tok[0])] - lse[0]
         assert float((out["logp"][0].double() - want).abs()) < 2 * (16 + 16) * 2.0 ** -23 * 64
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T", [2, 16, 31, 64, 100, 128])
+def test_few_tokens_where_they_lie_and_gathered(T, dtype):
+    # on 16-byte boundaries the forward pass reads a few rows in place, masked ones among them, whatever they hold; off them it
+    # gathers the live ones: the same numbers either way
+    h, w, tok, grad = make(T, 5000, 264, dtype, seed=90 + T, masked=0.0)
+    tok[::2] = -1
+    tok[1] = 5000 if T > 2 else tok[1]
+    clean = h.clone()
+    clean[::2] = 0
+    junk = torch.tensor([float("nan"), float("inf"), -float("inf"), 3e4], device=DEV).to(dtype)
+    h[::2] = junk.repeat(66)
+    p = B.make_head_params(h, w)
+    got = []
+    for hidden in (h, torch.nn.functional.pad(h, (1, 1))[:, 1:265]):
+        ws = B.alloc_workspace(B.ppow_head_workspace_bytes(p, False), DEV)
+        ws.fill_(255)
+        logp, lse = torch.full((T + 4,), 7.0, device=DEV), torch.full((T + 4,), 7.0, device=DEV)
+        B.ppow_head_logprob(p, hidden, w, tok, logp[:T], lse[:T], ws)
+        assert B.ppow_read_error_flags(ws) == (B.PPOW_FLAG_TOKEN_RANGE if T > 2 else 0)
+        check_forward(clean, w, tok, 1.0, {"logp": logp[:T], "lse": lse[:T]})
+        assert torch.all(logp[T:] == 7) and torch.all(lse[T:] == 7)
+        got.append((logp, lse))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
