@@ -891,6 +891,7 @@ __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows
     __shared__ double sums[MERGE_THREADS / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int32_t row = blockIdx.x;
+    allow_next_kernel();
     wait_for_previous_kernel();
     if (row >= rows.header->live) return;
     const int32_t r = rows.source ? rows.source[row] : row, y = rows.token[row];
@@ -941,6 +942,7 @@ __global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows ro
                                                                      int32_t D, const uint16_t *__restrict__ weight,
                                                                      int64_t weight_stride, uint16_t *__restrict__ grad_hidden)
 {
+    allow_next_kernel();
     wait_for_previous_kernel();
     const int32_t units = D / 4, splits = rows.header->splits, live = rows.header->live;
     const size_t split_units = (size_t)(few ? few : (live + TILE - 1) / TILE * TILE) * units;
