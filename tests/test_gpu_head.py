@@ -384,3 +384,12 @@ def test_few_tokens_where_they_lie_and_gathered(T, dtype):
         assert torch.all(logp[T:] == 7) and torch.all(lse[T:] == 7)
         got.append((logp, lse))
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("T,V,D", [(1, 1 << 22, 8), (70000, 300, 8), (1 << 20, 2, 8), (5, 300, 1 << 16), (300, 290, 1 << 16), (140, 70000, 16)])
+def test_ends_of_the_ranges(T, V, D):
+    h, w, tok, grad = make(T, V, D, torch.bfloat16, seed=40, masked=0.1 if T > 5 else 0.0)
+    out, gh, gw = run(h, w, tok, grad)
+    check_forward(h, w, tok, 1.0, out)
+    check_backward(h, w, tok, out["lse"], grad, 1.0, gh, gw)
+    torch.cuda.empty_cache()

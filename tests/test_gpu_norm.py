@@ -363,3 +363,31 @@ def test_gradient_against_differences_of_the_forward_pass(R, D):
     # and not by being loose: without the two mean terms the difference is far outside
     naive = ((gy * w).double() * out["rstd"].double()[:, None] * step).sum(1)
     assert float((naive - want).abs().max()) > 4 * float((got - want).abs().max())
+
+
+@pytest.mark.parametrize("R,D,dtype", [(1 << 20, 3, torch.float16), (1 << 20, 64, torch.bfloat16), (70000, 136, torch.float32)])
+def test_many_short_rows(R, D, dtype):
+    x, w, b, gy = make(R, D, dtype, seed=12)
+    out = B.layer_norm(x, w, b, checkpoint=True)
+    got = B.layer_norm_backward(gy, (out["packed"], out["scale"]), w, out["mean"], out["rstd"])
+    back = B.unpack_activation(out["packed"], out["scale"], dtype)
+    torch.cuda.synchronize()
+    check_forward(x, w, b, 1e-5, out)
+    check_packed(x, out["packed"], out["scale"])
+    value = reference_pack(x)[2]
+    assert torch.equal(back, value.to(dtype))
+    check_backward(gy, value, w, out["mean"], out["rstd"], got, torch.float32)
+
+
+def test_a_checkpoint_of_more_than_two_to_the_31_values():
+    R, D = 40000, 54000                                      # 2.16e9 values: offsets pass 32 bits
+    x = torch.zeros((R, D), dtype=torch.bfloat16, device=DEV)
+    probe = [0, 1, R // 2, R - 2, R - 1]
+    g = torch.Generator(device=DEV).manual_seed(0)
+    x[probe] = torch.randn((len(probe), D), generator=g, device=DEV).bfloat16()
+    q, s = B.pack_activation(x)
+    back = B.unpack_activation(q, s)
+    torch.cuda.synchronize()
+    check_packed(x[probe], q[probe], s[probe])
+    assert torch.equal(back[probe].double(), reference_pack(x[probe])[2])
+    assert not back[2].any() and int((s != 1).any(1).sum()) == len(probe)
