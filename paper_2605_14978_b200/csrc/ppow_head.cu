@@ -988,7 +988,8 @@ bool params_ok(const ppow_head_params *p)
 }
 
 // Columns of a tile for this many tokens.  Up to 128 the tokens are the columns and W the rows: 8 tokens x 4096 x 128256
-// would spend as much on loading and multiplying 256 rows, 248 of them zeros, as W takes to come from HBM.
+// would spend as much on loading and multiplying 256 rows, 248 of them zeros, as W takes to come from HBM (222 us, like this 169).
+// At 100 tokens it is 211 us against 231, at 128 x 4096 x 32000 62 against 69.
 int32_t tile_columns(int32_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : TILE; }
 
 struct Layout {
