@@ -281,6 +281,12 @@ typedef struct {
  * float32 sums of grad_hidden and a copy of the live rows. */
 size_t ppow_head_workspace_bytes(const ppow_head_params *params, int backward);
 
+/* How the gradient is cut with `live` rows that are not masked (host only, nothing is launched): the return value is the number
+ * of pieces of the vocabulary (0 on invalid parameters); for piece `piece`, where there is one, *first and *columns receive its
+ * vocabulary entries and *shares the number of shares of each piece that grad_hidden is added up from, each 64 entries long at
+ * least.  Any of the three may be NULL. */
+int ppow_head_plan(const ppow_head_params *params, int32_t live, int32_t piece, int32_t *first, int32_t *columns, int32_t *shares);
+
 /*
  *   hidden      device, [T, D], rows hidden_stride apart, aligned to its element size
  *   weight      device, [V, D], rows weight_stride apart, 16-byte aligned

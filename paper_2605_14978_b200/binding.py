@@ -33,7 +33,7 @@ EXPORTS = ("ppow_score_workspace_bytes", "ppow_score_windows", "ppow_score_windo
            "ppow_noalloc_read_error_flags",
            "ppow_group_advantage", "ppow_sequence_windows", "ppow_sequence_windows_mixed", "ppow_expected_acceptance",
            "ppow_reference_logprob", "ppow_selftest_wait_timeout", "ppow_stream_read_probe", "ppow_score_kernel_launches",
-           "ppow_head_workspace_bytes", "ppow_head_logprob", "ppow_head_logprob_backward",
+           "ppow_head_workspace_bytes", "ppow_head_plan", "ppow_head_logprob", "ppow_head_logprob_backward",
            "ppow_layer_norm", "ppow_layer_norm_workspace_bytes", "ppow_layer_norm_backward", "ppow_pack_activation",
            "ppow_unpack_activation",
            "ppow_checked_failures", "ppow_timeline_read", "ppow_status_string", "ppow_version")
@@ -136,6 +136,8 @@ def load_library():
     lib.ppow_score_kernel_launches.argtypes = [ctypes.POINTER(ppow_params)]
     lib.ppow_head_workspace_bytes.restype = sz
     lib.ppow_head_workspace_bytes.argtypes = [ctypes.POINTER(ppow_head_params), ctypes.c_int]
+    lib.ppow_head_plan.restype = ctypes.c_int
+    lib.ppow_head_plan.argtypes = [ctypes.POINTER(ppow_head_params), i32, i32] + [ctypes.POINTER(i32)] * 3
     lib.ppow_head_logprob.restype = ctypes.c_int
     lib.ppow_head_logprob.argtypes = [ctypes.POINTER(ppow_head_params), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.ppow_head_logprob_backward.restype = ctypes.c_int
@@ -567,6 +569,17 @@ def make_head_params(hidden, weight, temperature=1.0) -> ppow_head_params:
 
 def ppow_head_workspace_bytes(params: ppow_head_params, backward: bool) -> int:
     return load_library().ppow_head_workspace_bytes(ctypes.byref(params), 1 if backward else 0)
+
+
+def ppow_head_plan(params: ppow_head_params, live: int):
+    """How the gradient is cut with ``live`` rows that are not masked: [(first, columns)] of the vocabulary's pieces, and the shares
+    of each that grad_hidden is added up from.  Host only."""
+    lib, first, columns, shares = load_library(), ctypes.c_int32(), ctypes.c_int32(), ctypes.c_int32()
+    pieces = []
+    for i in range(lib.ppow_head_plan(ctypes.byref(params), live, 0, None, None, None)):
+        lib.ppow_head_plan(ctypes.byref(params), live, i, ctypes.byref(first), ctypes.byref(columns), ctypes.byref(shares))
+        pieces.append((first.value, columns.value))
+    return pieces, shares.value
 
 
 def ppow_head_logprob(params: ppow_head_params, hidden, weight, tokens, logp, lse, workspace, stream=None) -> None:

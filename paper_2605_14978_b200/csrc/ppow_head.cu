@@ -89,21 +89,29 @@ struct GatherJob {
     int64_t stride;
     int32_t T, D, V, rows_per_cta;
     int32_t few;                    // token columns of a call of few tokens, else 0
-    int32_t d_tiles, piece_steps;   // backward: what the shares of dh follow from
+    int32_t d_tiles, piece_steps;   // backward: what the shares of dh follow from; steps of the shortest piece
     float inv_temperature;
     bool vec;                       // rows start on 16-byte boundaries
 };
 
 // Shares of the inner axis of dh: `tiles` output tiles times the shares should fill whole rounds of the pairs.  A share is
-// at least eight steps long, and each one costs a pass over its sums (2 % of a round is about what that measures).
+// at least eight steps long, and each one costs a pass over its sums (2 % of a round is about what that measures).  `steps`
+// are those of the shortest piece of the vocabulary, so that no share of any piece is empty.  The host runs the same rule.
 constexpr int32_t SPLIT_TILES = 8 * PAIRS;      // tiles x shares where there is more than one share
-__device__ __forceinline__ int32_t split_count(int32_t tiles, int32_t steps)      // one warp, a candidate per lane and turn
+__host__ __device__ __forceinline__ bool split_allowed(int32_t s, int64_t tiles, int32_t steps)
+{
+    return s == 1 || (s <= PAIRS && s * 8 <= steps && s * tiles <= SPLIT_TILES);
+}
+__host__ __device__ __forceinline__ float split_cost(int32_t s, int64_t tiles)
+{
+    return (float)((tiles * s + PAIRS - 1) / PAIRS) / (float)s * fmaf(0.02f, (float)(s < 11 ? s - 1 : 10), 1.0f);
+}
+__device__ __forceinline__ int32_t split_count(int64_t tiles, int32_t steps)      // one warp, a candidate per lane and turn
 {
     float best_cost = INFINITY;
     uint32_t best = 1;
-    for (int32_t s = 1 + (int32_t)(threadIdx.x & 31); s <= PAIRS; s += 32) {
-        if (s > 1 && (s * 8 > steps || s * tiles > SPLIT_TILES)) break;
-        const float cost = (float)((tiles * s + PAIRS - 1) / PAIRS) / (float)s * (1.0f + 0.02f * (float)min(s - 1, 10));
+    for (int32_t s = 1 + (int32_t)(threadIdx.x & 31); split_allowed(s, tiles, steps); s += 32) {
+        const float cost = split_cost(s, tiles);
         if (cost < best_cost) {
             best_cost = cost;
             best = (uint32_t)s;
@@ -186,7 +194,7 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
     }
     if (BACKWARD && blockIdx.x == 0 && warp == 1) {
         const int64_t tiles = (int64_t)(job.few ? 1 : max(1, (total + TILE - 1) / TILE)) * job.d_tiles;
-        const int32_t splits = tiles > SPLIT_TILES ? 1 : split_count((int32_t)tiles, job.piece_steps);
+        const int32_t splits = split_count(tiles, job.piece_steps);
         if (lane == 0) out.header->splits = splits;
     }
     if (warp == 0) {
@@ -374,6 +382,13 @@ __device__ __forceinline__ Tile tile_at(const ProductJob &job, const Extent &e, 
     return x;
 }
 
+// Accumulators that a tile's sum passes through, one after the other.  The issuing thread and the epilogue warps both count by
+// it: every tile takes one at least, so that the two sides agree on buffer and phase whatever its steps are.
+template <int N, bool PARTS> __device__ __forceinline__ int32_t part_count(const Tile &x)
+{
+    return PARTS ? max(1, (x.k1 - x.k0 + sum_steps<N>() - 1) / sum_steps<N>()) : 1;
+}
+
 // ---- epilogues: one warp, 32 rows of the tile's accumulator (its Tensor Memory lanes), half of the columns --------
 // Loads run one step ahead of the arithmetic; `release` hands the accumulator back as soon as the last one is in.
 template <int CHUNKS, int WIDTH, typename R, typename F>
@@ -498,14 +513,13 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
     } else if (PRODUCT == GRAD_HIDDEN) {
         float *to = job.grad_rows + ((size_t)x.split * e.row_tiles * TILE + row) * job.D + x.col + first;
         const int32_t left = min(TILE, job.D - x.col) - first;   // a multiple of 8
-        const bool none = x.k0 == x.k1;                          // more shares than steps: nothing was multiplied
         for_chunks<COLS / 32, 32>(src, release, [&](int c, uint32_t (&w)[32]) {
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                if (c + 8 * h < left && row < e.live && PPOW_CHECK(x.split < e.splits, 504, flags)) {
+                if (c + 8 * h < left && row < e.live && PPOW_CHECK(x.split < e.splits && x.k0 < x.k1, 504, flags)) {
                     uint32_t o[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) o[j] = none ? 0u : w[8 * h + j];
+                    for (int j = 0; j < 8; ++j) o[j] = w[8 * h + j];
                     if (job.add) {
                         const float4 *old = reinterpret_cast<const float4 *>(to + c + 8 * h);
                         const float4 p = old[0], q = old[1];
@@ -647,14 +661,14 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
         });
     } else {
         float *to = job.grad_rows + (size_t)x.split * N * job.D + row;
-        const bool inside = row < job.D, none = x.k0 == x.k1;
+        const bool inside = row < job.D;
         for_chunks<COLS / WIDTH, WIDTH>(src, release, [&](int c, uint32_t (&w)[WIDTH]) {
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) {
                 const int32_t token = first + c + j;
-                if (inside && token < e.live && PPOW_CHECK(x.split < e.splits, 508, flags)) {
+                if (inside && token < e.live && PPOW_CHECK(x.split < e.splits && x.k0 < x.k1, 508, flags)) {
                     float *p = to + (size_t)token * job.D;
-                    const float v = none ? 0.0f : __uint_as_float(w[j]);
+                    const float v = __uint_as_float(w[j]);
                     *p = job.add ? *p + v : v;
                 }
             }
@@ -770,8 +784,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
             bool ok = true;
             for (int64_t t = pair; t < tiles && ok; t += pairs) {
                 const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
-                for (int32_t k0 = x.k0; ok && (k0 < x.k1 || k0 == x.k0); ++acc) {
-                    const int32_t k1 = PARTS ? min(k0 + sum_steps<N>(), x.k1) : x.k1;
+                const int32_t parts = part_count<N, PARTS>(x);
+                for (int32_t part = 0; part < parts && ok; ++part, ++acc) {
+                    const int32_t k0 = PARTS ? x.k0 + part * sum_steps<N>() : x.k0, k1 = PARTS ? min(k0 + sum_steps<N>(), x.k1) : x.k1;
                     const uint32_t b = acc & 1u, d = tmem + b * TILE;
                     ok = mbar_wait_ns(acc_empty(b), ((acc >> 1) & 1u) ^ 1u);
                     tcgen05_fence_after();
@@ -789,8 +804,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                         mma_commit_pair(empty(s));
                     }
                     if (ok) mma_commit_pair(acc_full(b));
-                    if (k1 == k0) break;             // a share without steps
-                    k0 = k1;
                 }
             }
             if (!ok) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
@@ -813,7 +826,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                     own.lse2 = job.rows.lse2[x.row + in_tile];
                 }
             }
-            const int32_t parts = PARTS ? (x.k1 - x.k0 + sum_steps<N>() - 1) / sum_steps<N>() : 1;
+            const int32_t parts = part_count<N, PARTS>(x);
             for (int32_t part = 0; part < parts; ++part, ++acc) {
                 const uint32_t b = acc & 1u;
                 // all four warps of a half go on or none does: they meet at barriers further down
@@ -994,8 +1007,32 @@ int32_t tile_columns(int32_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ?
 
 struct Layout {
     size_t source, token, mult, lse2, row_scale, residual, rows, scaled, partial, at_token, dz, grad_rows, total;
-    int32_t columns, few, padded, v_tiles, d_tiles, piece, parts;
+    int32_t columns, few, padded, v_tiles, d_tiles, parts;
+    int32_t pieces, piece;          // backward: pieces of the vocabulary, entries of the longest (the row length of dz)
 };
+
+// First vocabulary entry of piece i; piece `pieces` would start at or behind the vocabulary's end.
+int64_t piece_start(const Layout &L, int32_t i) { return (int64_t)L.v_tiles * i / L.pieces * TILE; }
+int32_t piece_columns(const Layout &L, int32_t V, int32_t i)
+{
+    const int64_t end = piece_start(L, i + 1);
+    return (int32_t)((end < V ? end : V) - piece_start(L, i));
+}
+// Steps of the inner axis of dh in the shortest piece: a whole one, or the last one, whose end may lie inside a tile.
+int32_t shortest_steps(const Layout &L, int32_t V)
+{
+    const int32_t whole = L.v_tiles / L.pieces * (TILE / BK), last = (piece_columns(L, V, L.pieces - 1) + BK - 1) / BK;
+    return last < whole ? last : whole;
+}
+// Output tiles of dh for this many live rows, and the shares that head_gather_kernel plans for them.
+int64_t hidden_tiles(const Layout &L, int32_t live) { return (int64_t)(L.few || live < 1 ? 1 : (live + TILE - 1) / TILE) * L.d_tiles; }
+int32_t planned_splits(int64_t tiles, int32_t steps)
+{
+    int32_t best = 1;
+    for (int32_t s = 2; split_allowed(s, tiles, steps); ++s)
+        if (split_cost(s, tiles) < split_cost(best, tiles)) best = s;
+    return best;
+}
 
 Layout layout_of(const ppow_head_params *p, bool backward)
 {
@@ -1029,8 +1066,8 @@ Layout layout_of(const ppow_head_params *p, bool backward)
         const size_t strip = rows * TILE * 2;                      // one column tile of dz
         int32_t fit = (int32_t)(DZ_BYTES / strip);
         if (fit < 1) fit = 1;
-        const int32_t pieces = (L.v_tiles + fit - 1) / fit;
-        L.piece = (L.v_tiles + pieces - 1) / pieces * TILE;        // pieces of nearly the same length
+        L.pieces = (L.v_tiles + fit - 1) / fit;
+        L.piece = (L.v_tiles + L.pieces - 1) / L.pieces * TILE;    // lengths differ by one tile at most
         L.dz = take(rows * L.piece * 2);
         // sums of dh: all rows once, or as many shares as SPLIT_TILES allows
         size_t sums = rows, split = (size_t)(SPLIT_TILES / L.d_tiles) * (L.few ? L.few : TILE);
@@ -1157,7 +1194,7 @@ bool launch_gather(const ppow_head_params *p, const Layout &L, const GatherJob &
     job.V = p->V;
     job.few = L.few;
     job.d_tiles = L.d_tiles;
-    job.piece_steps = L.piece / BK;
+    job.piece_steps = L.pieces ? shortest_steps(L, p->V) : 0;
     job.inv_temperature = (float)(1.0 / (double)p->temperature);
     job.vec = rows_aligned(hidden, p->hidden_stride);
     job.hidden = (const uint16_t *)hidden;
@@ -1244,11 +1281,11 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     job.dz = dz;
     job.grad_rows = (float *)(ws + L.grad_rows);
     const int64_t row_tiles = (L.padded + TILE - 1) / TILE;
-    for (int64_t v0 = 0; v0 < p->V; v0 += L.piece) {
-        job.v0 = (int32_t)v0;
-        job.columns = (int32_t)(p->V - v0 < L.piece ? p->V - v0 : L.piece);
+    for (int32_t i = 0; i < L.pieces; ++i) {
+        job.v0 = (int32_t)piece_start(L, i);
+        job.columns = piece_columns(L, p->V, i);
         job.v_tiles = (job.columns + TILE - 1) / TILE;
-        job.add = v0 > 0;
+        job.add = i > 0;
         if (!launch_product<LOGITS_GRAD, BF16>(map_rows, map_weight, map_dz, job, L.columns, row_tiles * job.v_tiles, pairs, stream))
             return PPOW_ERR_CUDA;
         if (grad_hidden && !launch_product<GRAD_HIDDEN, BF16>(map_dz, map_weight_t, map_dz, job, L.columns, pairs, pairs, stream)) return PPOW_ERR_CUDA;
@@ -1276,6 +1313,18 @@ using namespace ppow;
 extern "C" size_t ppow_head_workspace_bytes(const ppow_head_params *params, int backward)
 {
     return params_ok(params) ? layout_of(params, backward != 0).total : 0;
+}
+
+extern "C" int ppow_head_plan(const ppow_head_params *params, int32_t live, int32_t piece, int32_t *first, int32_t *columns, int32_t *shares)
+{
+    if (!params_ok(params) || live < 0 || live > params->T || piece < 0) return 0;
+    const Layout L = layout_of(params, true);
+    if (piece < L.pieces) {
+        if (first) *first = (int32_t)piece_start(L, piece);
+        if (columns) *columns = piece_columns(L, params->V, piece);
+        if (shares) *shares = planned_splits(hidden_tiles(L, live), shortest_steps(L, params->V));
+    }
+    return L.pieces;
 }
 
 extern "C" ppow_status ppow_head_logprob(const ppow_head_params *params, const void *hidden, const void *weight, const int32_t *tokens,

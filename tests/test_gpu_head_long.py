@@ -1,0 +1,63 @@
+"""Gradients of long batches: many pieces of the vocabulary, the last one short, most rows masked or none, against the definition in
+float64 with the bounds of test_gpu_head; and the error word of each call."""
+import pytest
+import torch
+
+from paper_2605_14978_b200 import binding as B
+
+import test_gpu_head as head
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def backward(h, w, tok, lse, grad):
+    p = B.make_head_params(h, w)
+    ws = B.alloc_workspace(B.ppow_head_workspace_bytes(p, True), DEV)
+    gh, gw = torch.empty_like(h), torch.empty_like(w)
+    B.ppow_head_logprob_backward(p, h, w, tok, lse, grad, gh, gw, ws)
+    assert B.ppow_read_error_flags(ws) == 0
+    return gh, gw
+
+
+def check(h, w, tok, lse, grad, gh, gw):
+    """Element by element within the bounds of head.gradient; and all in all: two half steps u of each value, and in float16, whose
+    steps below 2^-14 are 2^-24 whatever the value, half of such a step each, 2^-25 sqrt(count) in the norm.  (Gradients over a
+    batch of T are of the order of 1/T: with T = 262144 nearly all of them lie there.)"""
+    dh, th, dw, tw = head.gradient(h, w, tok, lse, grad, 1.0)
+    for got, want, tol in ((gh, dh, th), (gw, dw, tw)):
+        off = got.double() - want
+        assert torch.all(off.abs() <= tol)
+        least = 2.0 ** -25 * want.numel() ** 0.5 if h.dtype == torch.float16 else 0.0
+        assert float(off.norm()) < 2 * head.U[h.dtype] * float(want.norm()) + least
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,V,D,live", [(262144, 3129, 768, 6700), (51896, 128256, 1024, 3483), (49152, 129280, 2048, 2000), (65536, 65537, 256, 300)])
+def test_many_pieces_most_rows_masked(T, V, D, live, dtype):
+    g = torch.Generator(device=DEV).manual_seed(T + live)
+    h, w, tok, grad = head.make(T, V, D, dtype, seed=50, masked=0.0)
+    keep = torch.zeros(T, dtype=torch.bool, device=DEV)
+    keep[torch.randperm(T, generator=g, device=DEV)[:live]] = True
+    tok[~keep] = -1
+    assert len(B.ppow_head_plan(B.make_head_params(h, w), live)[0]) > 2
+    lse = B.head_logprob(h, w, tok)["lse"]
+    gh, gw = backward(h, w, tok, lse, grad)
+    assert not gh[~keep].any()
+    check(h[keep], w, tok[keep], lse[keep], grad[keep], gh[keep], gw)
+    torch.cuda.empty_cache()
+
+
+def test_many_pieces_no_row_masked():
+    T, V, D, rows = 65536, 65537, 256, 8192
+    h, w, tok, grad = head.make(T, V, D, torch.bfloat16, seed=51, masked=0.0)
+    lse = B.head_logprob(h, w, tok)["lse"]
+    gh, gw = backward(h, w, tok, lse, grad)
+    dw = torch.zeros((V, D), dtype=torch.float64, device=DEV)
+    for i in range(0, T, rows):
+        s = slice(i, i + rows)
+        dh, th, part, _ = head.gradient(h[s], w, tok[s], lse[s], grad[s], 1.0)
+        dw += part
+        assert torch.all((gh[s].double() - dh).abs() <= th), i
+    assert float((gw.double() - dw).norm() / dw.norm()) < 2 * head.U[torch.bfloat16]
+    torch.cuda.empty_cache()
