@@ -304,8 +304,7 @@ ppow_status ppow_head_logprob(const ppow_head_params *params, const void *hidden
  *     dz_i = grad_logp[i] / temperature * (onehot(y_i) - softmax(z_i))     grad_hidden = dz weight     grad_weight = dz^T hidden
  * dz is rounded to the storage type (a relative error of at most half a step per term, of the size of the operands' own
  * rounding); for PPOW_F16 each row of it is brought near 2^15 by a power of two first, which is undone after the sums.  What the
- * rounding of a row's largest term, the one at its token, leaves over is added to grad_hidden in float32, and with up to 32
- * rows that are not masked to grad_weight too.
+ * rounding of a row's largest term, the one at its token, leaves over is added to grad_hidden and grad_weight in float32.
  * The sums are float32 in a fixed order: equal inputs give equal results.
  *   hidden, weight, tokens   as above.  Rows with a negative token, a token >= V (which sets PPOW_FLAG_TOKEN_RANGE) or
  *                            grad_logp == 0 are masked: their gradient is 0 and they add nothing to grad_weight.

@@ -4,8 +4,9 @@
 //   dz_v = g/T ([v = y] - exp(z_v - lse)),   dh = dz W,   dW = dz^T h      (g: the gradient that arrives at logp).
 //
 // Steps of a call:
-//   gather    live rows of `hidden` are copied, in order, to the front of a workspace array (masked rows are skipped, so
-//             whatever they hold touches nothing and costs nothing; rows of any stride and alignment become tiles)
+//   gather    live rows of `hidden` are copied to the front of a workspace array, in order, for dW in the order of their tokens
+//             (masked rows may hold anything and cost no products, but the shares of a call's work are planned for all of its rows;
+//             rows of any stride and alignment become tiles)
 //   forward   logits by tiles of 256 tokens x 256 vocabulary entries; each tile leaves a maximum and a sum of exponentials
 //             per row; `merge` joins them in float64
 //   backward  per piece of the vocabulary: logits again, dz rounded to the operands' 16-bit type; dW of the piece, and the
@@ -64,6 +65,11 @@ struct HeadHeader {
     int32_t splits;        // shares of the inner axis of dh
 };
 
+// The live rows, from `first` to before `end`, whose tokens lie in one tile of the vocabulary (both 0: none).
+struct TokenRows {
+    int32_t first, end;
+};
+
 // Arrays of the workspace, all indexed by live row.
 struct HeadRows {
     HeadHeader *header;
@@ -73,11 +79,87 @@ struct HeadRows {
     float *lse2;           // normaliser in log2 units
     float *row_scale;      // dh = row_scale * (dz W)
     float *residual;       // what the rounding of dz at the token left over
+    TokenRows *rows_of;    // backward, per tile of the vocabulary
     void *rows;            // [padded, D] hidden states
     void *scaled;          // f16 backward: the same times a power of two per row
 };
 
 __device__ __forceinline__ void fault(HeadHeader *h, unsigned int bit) { atomicOr(&h->error_flags, bit); }
+
+// ---- the order of the gradient's rows ----------------------------------------------------------------
+// By token, and with the same token as they come: what dW needs of the rows of an entry then lies side by side, and neither
+// depends on the order in which threads get there.  A row's place is the number of live rows with a smaller token, or with the same
+// one and a smaller index.  Up to ORDER_COUNTED tokens every gather CTA counts that for its rows over all tokens; that is T^2
+// comparisons, so behind it four small kernels make lists of each token's rows, in any order, in which a row then counts its
+// predecessors.  (Whole gradients of T x 64 x 1000: 73 us counted at T = 4096, 75 by lists; 131 and 118 at 8192.)
+constexpr int32_t ORDER_COUNTED = 4096;
+struct RowOrder {
+    int32_t *count, *first;         // per vocabulary entry: live rows, and the place of the first
+    int32_t *slot;                  // per row: its place in the token's list
+    int32_t *list;                  // rows, by token
+};
+__device__ __forceinline__ bool grad_live(int32_t y, float g, int32_t V) { return y >= 0 && y < V && !(g == 0.0f); }
+
+constexpr int ORDER_THREADS = 256;
+__global__ void __launch_bounds__(ORDER_THREADS) head_order_clear_kernel(RowOrder order, int32_t V)
+{
+    allow_next_kernel();
+    wait_for_previous_kernel();
+    for (int32_t v = blockIdx.x * ORDER_THREADS + threadIdx.x; v < V; v += gridDim.x * ORDER_THREADS) order.count[v] = 0;
+}
+__global__ void __launch_bounds__(ORDER_THREADS) head_order_count_kernel(RowOrder order, const int32_t *tokens, const float *grad, int32_t T, int32_t V)
+{
+    allow_next_kernel();
+    wait_for_previous_kernel();
+    for (int32_t r = blockIdx.x * ORDER_THREADS + threadIdx.x; r < T; r += gridDim.x * ORDER_THREADS)
+        if (grad_live(tokens[r], grad[r], V)) order.slot[r] = atomicAdd(order.count + tokens[r], 1);
+}
+// A CTA takes `share` entries, a multiple of its threads; it adds up all counts before them itself instead of waiting for its neighbour.
+constexpr int SCAN_THREADS = 512;
+__global__ void __launch_bounds__(SCAN_THREADS) head_order_scan_kernel(RowOrder order, int32_t V, int32_t share)
+{
+    __shared__ int32_t sums[SCAN_THREADS / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    allow_next_kernel();
+    wait_for_previous_kernel();
+    const int32_t begin = blockIdx.x * share, end = min(begin + share, V);
+    int32_t carry = 0;
+#pragma unroll 8
+    for (int32_t v = tid; v < begin; v += SCAN_THREADS) carry += order.count[v];
+    carry = __reduce_add_sync(0xffffffffu, carry);
+    if (lane == 0) sums[warp] = carry;
+    __syncthreads();
+    carry = 0;
+#pragma unroll
+    for (int i = 0; i < SCAN_THREADS / 32; ++i) carry += sums[i];
+    for (int32_t v0 = begin; v0 < end; v0 += SCAN_THREADS) {
+        const int32_t v = v0 + tid, own = v < end ? order.count[v] : 0;
+        int32_t upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        __syncthreads();
+        if (lane == 31) sums[warp] = upto;
+        __syncthreads();
+        int32_t before = 0, all = 0;
+#pragma unroll
+        for (int i = 0; i < SCAN_THREADS / 32; ++i) {
+            before += i < warp ? sums[i] : 0;
+            all += sums[i];
+        }
+        if (v < end) order.first[v] = carry + before + upto - own;
+        carry += all;
+    }
+}
+__global__ void __launch_bounds__(ORDER_THREADS) head_order_list_kernel(RowOrder order, const int32_t *tokens, const float *grad, int32_t T, int32_t V)
+{
+    allow_next_kernel();
+    wait_for_previous_kernel();
+    for (int32_t r = blockIdx.x * ORDER_THREADS + threadIdx.x; r < T; r += gridDim.x * ORDER_THREADS)
+        if (grad_live(tokens[r], grad[r], V)) order.list[order.first[tokens[r]] + order.slot[r]] = r;
+}
 
 // ---- gather -----------------------------------------------------------------------------------------
 struct GatherJob {
@@ -89,6 +171,8 @@ struct GatherJob {
     int64_t stride;
     int32_t T, D, V, rows_per_cta;
     int32_t few;                    // token columns of a call of few tokens, else 0
+    bool by_token;                  // backward: rows in the order of their tokens, for dW
+    RowOrder order;                 // of many tokens; null: counted here
     int32_t d_tiles, piece_steps;   // backward: what the shares of dh follow from; steps of the shortest piece
     float inv_temperature;
     bool vec;                       // rows start on 16-byte boundaries
@@ -135,10 +219,10 @@ __device__ __forceinline__ int row_exponent(float mult, int top)
 template <bool BACKWARD, bool SCALED>
 __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob job, HeadRows out)
 {
-    __shared__ int32_t part[4][GATHER_THREADS / 32];
+    constexpr int COUNTED = ORDER_COUNTED / GATHER_CTAS;         // rows of a CTA that counts their places
+    __shared__ int32_t part[4 + COUNTED][GATHER_THREADS / 32];
     __shared__ int32_t dest[GATHER_ROWS_MAX];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    allow_next_kernel();
     wait_for_previous_kernel();
     const int32_t r0 = (int32_t)min((int64_t)blockIdx.x * job.rows_per_cta, (int64_t)job.T);
     const int32_t n = min(job.rows_per_cta, job.T - r0);
@@ -152,7 +236,14 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
             if (i < all) early[j] = __ldg(reinterpret_cast<const uint4 *>(job.hidden + (size_t)(r0 + i / units) * job.stride) + i % units);
         }
     }
-    auto live = [&](int32_t y, float g) { return BACKWARD ? y >= 0 && y < job.V && !(g == 0.0f) : y >= 0; };
+    if (BACKWARD)
+        for (int32_t i = blockIdx.x * GATHER_THREADS + tid; i < (job.V + TILE - 1) / TILE; i += gridDim.x * GATHER_THREADS)
+            out.rows_of[i] = {0, 0};
+    auto live = [&](int32_t y, float g) { return BACKWARD ? grad_live(y, g, job.V) : y >= 0; };
+    const bool counts = BACKWARD && job.by_token && !job.order.count;
+    int32_t own[COUNTED], less[COUNTED] = {};                    // the CTA's rows' tokens, -1: masked; live rows in front of them
+#pragma unroll
+    for (int k = 0; k < COUNTED; ++k) own[k] = counts && k < n && live(job.tokens[r0 + k], job.grad[r0 + k]) ? job.tokens[r0 + k] : -1;
     int32_t before = 0, total = 0, top = -1000, range = 0;
     for (int32_t i = tid; i < job.T; i += GATHER_THREADS) {
         const int32_t y = job.tokens[i];
@@ -160,6 +251,10 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
         const bool ok = live(y, g);
         total += ok;
         before += ok && i < r0;
+        if (counts) {
+#pragma unroll
+            for (int k = 0; k < COUNTED; ++k) less[k] += ok && y < own[k] + (i < r0 + k ? 1 : 0);
+        }
         range |= y >= job.V;
         if (SCALED && ok) {
             const float m = row_mult(g, job.inv_temperature);
@@ -175,6 +270,13 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
         part[1][warp] = total;
         part[2][warp] = top;
         part[3][warp] = range;
+    }
+    if (counts) {
+#pragma unroll
+        for (int k = 0; k < COUNTED; ++k) {
+            less[k] = __reduce_add_sync(0xffffffffu, less[k]);
+            if (lane == 0) part[4 + k][warp] = less[k];
+        }
     }
     __syncthreads();
     before = total = range = 0;
@@ -197,7 +299,28 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
         const int32_t splits = split_count(tiles, job.piece_steps);
         if (lane == 0) out.header->splits = splits;
     }
-    if (warp == 0) {
+    if (BACKWARD && job.by_token && !counts) {
+        for (int32_t k = warp; k < n; k += GATHER_THREADS / 32) {
+            const int32_t r = r0 + k, y = job.tokens[r];
+            int32_t place = -1;
+            if (live(y, job.grad[r])) {
+                const int32_t first = job.order.first[y], rows = job.order.count[y];
+                int32_t less = 0;
+                for (int32_t i = lane; i < rows; i += 32) less += job.order.list[first + i] < r;
+                place = first + __reduce_add_sync(0xffffffffu, less);
+            }
+            if (lane == 0) dest[k] = place;
+        }
+    } else if (counts) {
+#pragma unroll
+        for (int k = 0; k < COUNTED; ++k)
+            if (tid == 0 && k < n) {
+                int32_t place = 0;
+#pragma unroll
+                for (int w = 0; w < GATHER_THREADS / 32; ++w) place += part[4 + k][w];
+                dest[k] = own[k] < 0 ? -1 : place;
+            }
+    } else if (warp == 0) {
         int32_t next = before;
         for (int32_t k = 0; k < n; k += 32) {
             const int32_t r = min(r0 + k + lane, job.T - 1);
@@ -209,6 +332,7 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
     }
     __syncthreads();
 
+    allow_next_kernel();
     // per row: what the products need to know of it
     for (int32_t k = tid; k < n; k += GATHER_THREADS) {
         const int32_t r = r0 + k, d = dest[k];
@@ -216,7 +340,7 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
             if (!BACKWARD) job.logp_out[r] = job.lse_out[r] = 0.0f;
             continue;
         }
-        if (!PPOW_CHECK(d < total && d <= r, 501, nullptr)) continue;
+        if (!PPOW_CHECK(d < total && (BACKWARD || d <= r), 501, nullptr)) continue;
         out.source[d] = r;
         out.token[d] = job.tokens[r];
         if (BACKWARD) {
@@ -436,6 +560,14 @@ __device__ __forceinline__ void put_box(uint32_t box, int32_t in_tile, int half,
     }
 }
 
+// The gradient's rows lie in the order of their tokens: those at either end of a tile's rows say so.
+__device__ __forceinline__ void note_token(const ProductJob &job, const Extent &e, int32_t token, int32_t row)
+{
+    const int32_t before = row > 0 ? job.rows.token[row - 1] : -1, behind = row + 1 < e.live ? job.rows.token[row + 1] : -1;
+    if (before < token / TILE * TILE) job.rows.rows_of[token / TILE].first = row;
+    if (behind < 0 || behind / TILE > token / TILE) job.rows.rows_of[token / TILE].end = row + 1;
+}
+
 // rows: tokens, columns: vocabulary
 template <int PRODUCT, bool BF16, typename R>
 __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Extent &e, const Tile &x, const RowData &own, uint32_t src,
@@ -488,6 +620,7 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
         const int32_t left = min(TILE, job.V - x.col) - first;
         const int32_t at = own.token - x.col - first;
         const float mult = own.mult, lse2 = own.lse2;
+        if (at >= 0 && at < COLS && row < e.live) note_token(job, e, own.token, row);
         for_chunks<COLS / 32, 32>(src, release, [&](int c, uint32_t (&w)[32]) {
             float p[32];
 #pragma unroll
@@ -533,33 +666,8 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
         });
     } else {
         const float out_scale = job.rows.header->out_scale;
-        // With up to 32 tokens one rounding of dz is most of the error of its token's row of dW (over more tokens they average out):
-        // its remainder times the token's hidden state is added here.  Lane i looks at token i.
-        const int32_t mine = lane < e.live && e.live <= 32 ? job.rows.token[lane] - (job.v0 + row - lane) : -1;
-        const unsigned hits = __ballot_sync(0xffffffffu, mine >= 0 && mine < 32);
-        const uint16_t *states = static_cast<const uint16_t *>(BF16 ? job.rows.rows : job.rows.scaled) + x.col + first;
         const int32_t v = x.row + in_tile / HALF_TILE * HALF_TILE;       // the box's first row within the piece
         for_chunks<COLS / 32, 32>(src, release, [&](int c, uint32_t (&w)[32]) {
-            for (unsigned m = hits; m; m &= m - 1) {
-                const int i = __ffs(m) - 1;
-                if (__shfl_sync(0xffffffffu, mine, i) == lane) {
-                    const float rest = job.rows.residual[i];
-                    const uint4 *h = reinterpret_cast<const uint4 *>(states + (size_t)i * job.D + c);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (x.col + first + c + 8 * q < job.D) {
-                            const uint4 u = h[q];
-                            const uint32_t p[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float2 f = unpack2<BF16>(p[j]);
-                                w[8 * q + 2 * j] = __float_as_uint(fmaf(rest, f.x, __uint_as_float(w[8 * q + 2 * j])));
-                                w[8 * q + 2 * j + 1] = __float_as_uint(fmaf(rest, f.y, __uint_as_float(w[8 * q + 2 * j + 1])));
-                            }
-                        }
-                }
-                __syncwarp();
-            }
             uint32_t o[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -647,6 +755,7 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
             const bool live = lane < WIDTH && mine < e.live;
             const float lse2 = live ? job.rows.lse2[mine] : 0.0f, mult = live ? job.rows.mult[mine] : 0.0f;
             const int32_t token = live ? job.rows.token[mine] : -1;
+            if (token >= row - lane && token < row - lane + 32) note_token(job, e, token, mine);
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) {
                 const float l = __shfl_sync(0xffffffffu, lse2, j), m = __shfl_sync(0xffffffffu, mult, j);
@@ -676,12 +785,57 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
     }
 }
 
+// ---- remainders ---------------------------------------------------------------------------------------
+// dz at its token is most of the row of dW that it falls into, and rounded alone it is off by as much as the result's own rounding
+// (4096 x 4096 x 128256 bf16: 0.0023 of dW, 0.0017 without that error).  What the rounding left over is added as further steps of the
+// tile's sum: the tile's rows lie side by side, and for 64 of them the operand in dz's place is zero but for one entry each, their
+// remainders.  The producer warp writes it into the stage, where TMA brings the rows' hidden states beside it, in slices of the 16
+// rows that one instruction multiplies: a tile has few rows more often than not (552 tokens x 776 x 68450: 236 us with whole steps,
+// 230 like this, 217 without remainders; 4096 x 4096 x 128256: no difference).
+constexpr uint32_t SLICE_BYTES = 16 * 128;
+__device__ __forceinline__ uint32_t remainder_slices(int32_t rows) { return (uint32_t)(rows + 15) / 16; }
+template <bool REMAINDERS>
+__device__ __forceinline__ TokenRows tile_rows(const ProductJob &job, int64_t tiles, int64_t t, int64_t other)     // of tile t, if there is one
+{
+    if (!REMAINDERS) return {0, 0};
+    const int2 r = *reinterpret_cast<const int2 *>(job.rows.rows_of + job.v0 / TILE + (int32_t)(t < tiles ? t : other) / job.d_tiles);
+    return {r.x, r.y};
+}
+// `slices` slices of the half tile from vocabulary entry `base` on, rows by 128 entries, row `from` of the tile's in row `skip`, laid
+// out as TMA would: blocks of 64 entries, a row 128 bytes, its 16-byte unit u at u ^ (row & 7).
+template <bool BF16>
+__device__ __forceinline__ void put_remainders(const ProductJob &job, uint32_t a, TokenRows rows, int32_t from, int32_t skip, uint32_t slices,
+                                               int32_t base)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    int32_t row = from + (int32_t)lane;
+    const int32_t end = min(rows.end, from + BK);
+    int32_t token = row < end ? job.rows.token[row] : -1;
+    float rest = row < end ? job.rows.residual[row] : 0.0f;
+#pragma unroll 4
+    for (uint32_t i = lane; i < slices * (SLICE_BYTES / 16); i += 32) {
+        store_shared16(a + 16 * i, 0u, 0u, 0u, 0u);
+        store_shared16(a + BK * 128 + 16 * i, 0u, 0u, 0u, 0u);
+    }
+    __syncwarp();
+#pragma unroll 1
+    while (row < end) {
+        const uint32_t k = skip + row - from, m = (uint32_t)(token - base);
+        if (m < HALF_TILE && PPOW_CHECK(k < BK, 510, nullptr))
+            store_shared2(a + m / 64 * (BK * 128) + k * 128 + ((m % 64 / 8 ^ (k & 7)) << 4) + m % 8 * 2, pack2<BF16>(rest, 0.0f));
+        row += 32;
+        if (row < end) token = job.rows.token[row], rest = job.rows.residual[row];
+    }
+    fence_for_copy_engine();
+    __syncwarp();
+}
+
 // Persistent: one CTA per SM, pair p takes tiles p, p + pairs, ...  Warp 0 keeps the operand ring full, one thread of
 // the leader's warp 1 issues the products into one of two accumulators, warps 2..9 read the other one out.
 template <int PRODUCT, bool BF16, int N, bool PARTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     head_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                        const __grid_constant__ CUtensorMap map_out, const ProductJob job)
+                        const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_rest, const ProductJob job)
 {
     constexpr bool FEW = N < TILE;
     constexpr bool A_K = FEW ? PRODUCT != GRAD_HIDDEN : PRODUCT != GRAD_WEIGHT;     // the inner axis is contiguous in A
@@ -689,6 +843,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     constexpr uint32_t INSTRUCTION = mma_instruction(BF16, A_K, B_K, TILE, N);
     constexpr uint32_t BLOCK_BYTES = BK * 128;                                      // 64 wide x BK rows
     constexpr uint32_t STAGES = stage_count<N>(), STAGE_BYTES = stage_bytes<N>();
+    constexpr bool REMAINDERS = PRODUCT == GRAD_WEIGHT;                             // steps behind the product's own
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -708,7 +863,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
         prefetch_tensor_map(&map_a);
         prefetch_tensor_map(&map_b);
         for (uint32_t s = 0; s < STAGES; ++s) {
-            mbar_init(full(s), 1);
+            mbar_init(full(s), REMAINDERS ? 2 : 1);
             mbar_init(empty(s), 1);
         }
         for (uint32_t b = 0; b < 2; ++b) {
@@ -745,19 +900,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     const int64_t tiles = tile_count<PRODUCT>(job, e);
 
     if (warp == 0) {
-        if (lane == 0) {
+        if (lane == 0 || REMAINDERS) {
             uint32_t it = 0;
             bool ok = true;
+            [[maybe_unused]] TokenRows rows = tile_rows<REMAINDERS>(job, tiles, pair, pair);
             for (int64_t t = pair; t < tiles && ok; t += pairs) {
                 const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
-                for (int32_t k = x.k0; k < x.k1 && ok; ++k, ++it) {
-                    const uint32_t s = it % STAGES, phase = (it / STAGES) & 1u;
+                const int32_t n = x.col + (int32_t)rank * (N / 2);
+                [[maybe_unused]] const TokenRows next = tile_rows<REMAINDERS>(job, tiles, t + pairs, t);
+                uint32_t step = it;
+                for (int32_t k = x.k0; k < x.k1 && ok && lane == 0; ++k, ++step) {
+                    const uint32_t s = step % STAGES, phase = (step / STAGES) & 1u;
                     ok = mbar_wait_ns(empty(s), phase ^ 1u);
                     if (!ok) break;
-                    if (rank == 0) mbar_arrive_expect_tx(full(s), 2 * STAGE_BYTES);
                     const uint32_t bar = peer_addr(full(s), 0);
+                    if (rank == 0)
+                        mbar_arrive_expect_tx(full(s), 2 * STAGE_BYTES);
+                    else if (REMAINDERS)
+                        mbar_arrive_cluster(bar);
                     const uint32_t a = smem + s * STAGE_BYTES, b = a + A_BYTES;
-                    const int32_t m = x.row + (int32_t)rank * HALF_TILE, n = x.col + (int32_t)rank * (N / 2);
+                    const int32_t m = x.row + (int32_t)rank * HALF_TILE;
                     // the vocabulary is the inner axis of dh: its coordinate in W starts at the piece
                     const int32_t k_weight = k * BK + (PRODUCT == GRAD_HIDDEN ? job.v0 : 0);
                     if (A_K) {
@@ -773,10 +935,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                         tma_load_pair(b + BLOCK_BYTES, &map_b, n + 64, k_weight, bar);
                     }
                 }
+                it += x.k1 - x.k0;
+                if constexpr (REMAINDERS) {
+                    ok = __shfl_sync(0xffffffffu, ok, 0);
+                    for (int32_t row = rows.first; row < rows.end && ok; row += BK, ++it) {
+                        const uint32_t s = it % STAGES, a = smem + s * STAGE_BYTES, b = a + A_BYTES;
+                        // the hidden states read end with the last row tile at the latest: behind it the workspace holds anything
+                        const int32_t box_row = min(row, e.row_tiles * TILE - BK), skip = row - box_row;
+                        const uint32_t slices = remainder_slices(skip + min(BK, rows.end - row)), bar = peer_addr(full(s), 0);
+                        if (lane == 0) {
+                            ok = mbar_wait_ns(empty(s), ((it / STAGES) & 1u) ^ 1u);
+#pragma unroll 1
+                            for (uint32_t q = 0; q < slices && ok; ++q) {
+                                tma_load_pair(b + q * SLICE_BYTES, &map_rest, n, box_row + 16 * q, bar);
+                                tma_load_pair(b + BLOCK_BYTES + q * SLICE_BYTES, &map_rest, n + 64, box_row + 16 * q, bar);
+                            }
+                        }
+                        ok = __shfl_sync(0xffffffffu, ok, 0);
+                        if (!ok) break;
+                        put_remainders<BF16>(job, a, rows, row, skip, slices, job.v0 + x.row + (int32_t)rank * HALF_TILE);
+                        if (lane == 0) {
+                            if (rank == 0)
+                                mbar_arrive_expect_tx(full(s), slices * (2 * 2 * SLICE_BYTES));
+                            else
+                                mbar_arrive_release_cluster(bar);
+                        }
+                    }
+                    rows = next;
+                }
             }
             // the leader's last commits land on this CTA's barriers: stay until they have
-            for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it && ok; ++j) ok = mbar_wait_ns(empty(j % STAGES), (j / STAGES) & 1u);
-            if (!ok) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
+            if (lane == 0) {
+                for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it && ok; ++j) ok = mbar_wait_ns(empty(j % STAGES), (j / STAGES) & 1u);
+                if (!ok) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
+            }
         }
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
@@ -785,6 +977,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
             for (int64_t t = pair; t < tiles && ok; t += pairs) {
                 const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
                 const int32_t parts = part_count<N, PARTS>(x);
+                [[maybe_unused]] const TokenRows rows = tile_rows<REMAINDERS>(job, tiles, t, t);
                 for (int32_t part = 0; part < parts && ok; ++part, ++acc) {
                     const int32_t k0 = PARTS ? x.k0 + part * sum_steps<N>() : x.k0, k1 = PARTS ? min(k0 + sum_steps<N>(), x.k1) : x.k1;
                     const uint32_t b = acc & 1u, d = tmem + b * TILE;
@@ -802,6 +995,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                             mma_pair(d, da + (uint64_t)(q * (A_K ? 32 : 2048) >> 4), db + (uint64_t)(q * (B_K ? 32 : 2048) >> 4), INSTRUCTION,
                                      k > k0 || q > 0);
                         mma_commit_pair(empty(s));
+                    }
+                    if constexpr (REMAINDERS) {
+                        for (int32_t row = rows.first; row < rows.end && ok; row += BK, ++it) {
+                            const uint32_t s = it % STAGES;
+                            // the other CTA's half was written by its threads
+                            ok = mbar_wait_ns(full(s), (it / STAGES) & 1u) && mbar_acquire_cluster(full(s), (it / STAGES) & 1u);
+                            if (!ok) break;
+                            tcgen05_fence_after();
+                            const uint32_t a = smem + s * STAGE_BYTES;
+                            const uint64_t da = operand_descriptor(a, A_K, BLOCK_BYTES), db = operand_descriptor(a + A_BYTES, B_K, BLOCK_BYTES);
+                            const int32_t skip = row - min(row, e.row_tiles * TILE - BK);
+                            const uint32_t slices = remainder_slices(skip + min(BK, rows.end - row));
+#pragma unroll 1
+                            for (uint32_t q = 0; q < slices; ++q)
+                                mma_pair(d, da + (uint64_t)(q * SLICE_BYTES >> 4), db + (uint64_t)(q * SLICE_BYTES >> 4), INSTRUCTION, true);
+                            mma_commit_pair(empty(s));
+                        }
                     }
                     if (ok) mma_commit_pair(acc_full(b));
                 }
@@ -1006,7 +1216,7 @@ bool params_ok(const ppow_head_params *p)
 int32_t tile_columns(int32_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : TILE; }
 
 struct Layout {
-    size_t source, token, mult, lse2, row_scale, residual, rows, scaled, partial, at_token, dz, grad_rows, total;
+    size_t source, token, mult, lse2, row_scale, residual, rows_of, rows, scaled, partial, at_token, dz, grad_rows, order, total;
     int32_t columns, few, padded, v_tiles, d_tiles, parts;
     int32_t pieces, piece;          // backward: pieces of the vocabulary, entries of the longest (the row length of dz)
 };
@@ -1062,6 +1272,7 @@ Layout layout_of(const ppow_head_params *p, bool backward)
         L.partial = take(rows * L.parts * sizeof(float2));
         L.at_token = take(rows * 4);
     } else {
+        if (p->T > ORDER_COUNTED) L.order = take(((size_t)p->V * 2 + rows * 2) * 4);
         if (p->dtype == PPOW_F16) L.scaled = take(rows * p->D * 2);
         const size_t strip = rows * TILE * 2;                      // one column tile of dz
         int32_t fit = (int32_t)(DZ_BYTES / strip);
@@ -1073,6 +1284,7 @@ Layout layout_of(const ppow_head_params *p, bool backward)
         size_t sums = rows, split = (size_t)(SPLIT_TILES / L.d_tiles) * (L.few ? L.few : TILE);
         if (split > sums) sums = split;
         L.grad_rows = take(sums * p->D * 4);
+        L.rows_of = take((size_t)L.v_tiles * sizeof(TokenRows));
     }
     L.total = off;
     return L;
@@ -1137,14 +1349,14 @@ template <bool BF16> int pair_count()
 }
 
 template <int PRODUCT, bool BF16, int N>
-bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const ProductJob &job, int64_t most_tiles, int pairs,
-                  cudaStream_t stream)
+bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const CUtensorMap &rest, const ProductJob &job,
+                  int64_t most_tiles, int pairs, cudaStream_t stream)
 {
     const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
     // one part is a kernel of its own: the loop over parts costs it a third (2048 x 128 x 128256: 106 us, with the loop 140)
     if (PRODUCT == LOGITS_SUM && job.D > sum_steps<N>() * BK)
-        return launch_after(head_product_kernel<PRODUCT, BF16, N, PRODUCT == LOGITS_SUM>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, job);
-    return launch_after(head_product_kernel<PRODUCT, BF16, N, false>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, job);
+        return launch_after(head_product_kernel<PRODUCT, BF16, N, PRODUCT == LOGITS_SUM>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, rest, job);
+    return launch_after(head_product_kernel<PRODUCT, BF16, N, false>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, rest, job);
 }
 
 // `rows` and `weight`: the operand maps of the token side and of W's side.  With few tokens the two change places.  `out`: the
@@ -1154,12 +1366,12 @@ bool launch_product(const CUtensorMap &rows, const CUtensorMap &weight, const CU
                     int64_t most_tiles, int pairs, cudaStream_t stream)
 {
     switch (columns) {
-    case 16: return launch_tiles<PRODUCT, BF16, 16>(weight, rows, out, job, most_tiles, pairs, stream);
-    case 32: return launch_tiles<PRODUCT, BF16, 32>(weight, rows, out, job, most_tiles, pairs, stream);
-    case 64: return launch_tiles<PRODUCT, BF16, 64>(weight, rows, out, job, most_tiles, pairs, stream);
-    case 128: return launch_tiles<PRODUCT, BF16, 128>(weight, rows, out, job, most_tiles, pairs, stream);
+    case 16: return launch_tiles<PRODUCT, BF16, 16>(weight, rows, out, out, job, most_tiles, pairs, stream);
+    case 32: return launch_tiles<PRODUCT, BF16, 32>(weight, rows, out, out, job, most_tiles, pairs, stream);
+    case 64: return launch_tiles<PRODUCT, BF16, 64>(weight, rows, out, out, job, most_tiles, pairs, stream);
+    case 128: return launch_tiles<PRODUCT, BF16, 128>(weight, rows, out, out, job, most_tiles, pairs, stream);
     }
-    return launch_tiles<PRODUCT, BF16, TILE>(rows, weight, out, job, most_tiles, pairs, stream);
+    return launch_tiles<PRODUCT, BF16, TILE>(rows, weight, out, out, job, most_tiles, pairs, stream);
 }
 
 // Rows on 16-byte boundaries, within the strides that a tensor map can hold.
@@ -1178,6 +1390,7 @@ HeadRows rows_of(char *ws, const Layout &L)
     r.lse2 = (float *)(ws + L.lse2);
     r.row_scale = (float *)(ws + L.row_scale);
     r.residual = (float *)(ws + L.residual);
+    r.rows_of = (TokenRows *)(ws + L.rows_of);
     r.rows = ws + L.rows;
     r.scaled = ws + L.scaled;
     return r;
@@ -1255,13 +1468,14 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     const Layout L = layout_of(p, true);
     const HeadRows rows = rows_of(ws, L);
     uint16_t *dz = (uint16_t *)(ws + L.dz);
-    CUtensorMap map_rows, map_rows_t, map_weight, map_weight_t, map_dz, map_dz_t, map_grad;
+    CUtensorMap map_rows, map_rows_t, map_weight, map_weight_t, map_dz, map_dz_t, map_grad, map_rest;
     if (!make_map(&map_rows, rows.rows, BF16, p->D, L.padded, p->D, L.columns / 2) ||
         !make_map(&map_rows_t, BF16 ? rows.rows : rows.scaled, BF16, p->D, L.padded, p->D, BK) ||
         !make_map(&map_weight, weight, BF16, p->D, p->V, p->weight_stride, HALF_TILE) ||
         !make_map(&map_weight_t, weight, BF16, p->D, p->V, p->weight_stride, BK) ||
         !make_map(&map_dz, dz, BF16, L.piece, L.padded, L.piece, L.columns / 2) || !make_map(&map_dz_t, dz, BF16, L.piece, L.padded, L.piece, BK) ||
-        (grad_weight && !make_map(&map_grad, grad_weight, BF16, p->D, p->V, p->D, HALF_TILE)))
+        (grad_weight && (!make_map(&map_grad, grad_weight, BF16, p->D, p->V, p->D, HALF_TILE) ||
+                         !make_map(&map_rest, BF16 ? rows.rows : rows.scaled, BF16, p->D, L.padded, p->D, 16))))
         return PPOW_ERR_CUDA;
     const int pairs = pair_count<BF16>();
     if (pairs < 1) return PPOW_ERR_CUDA;
@@ -1270,6 +1484,20 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     g.lse = lse;
     g.grad = grad_logp;
     g.grad_hidden = (uint16_t *)grad_hidden;
+    g.by_token = grad_weight != nullptr;
+    if (L.order && grad_weight) {
+        g.order.count = (int32_t *)(ws + L.order);
+        g.order.first = g.order.count + p->V;
+        g.order.slot = g.order.first + p->V;
+        g.order.list = g.order.slot + L.padded;
+        const int32_t most = 148 * 8, share = (p->V / 148 / SCAN_THREADS + 1) * SCAN_THREADS;
+        auto grid = [&](int32_t n) { return (unsigned)((n - 1) / ORDER_THREADS + 1 < most ? (n - 1) / ORDER_THREADS + 1 : most); };
+        if (!launch_after(head_order_clear_kernel, grid(p->V), ORDER_THREADS, 0, stream, g.order, p->V) ||
+            !launch_after(head_order_count_kernel, grid(p->T), ORDER_THREADS, 0, stream, g.order, tokens, grad_logp, p->T, p->V) ||
+            !launch_after(head_order_scan_kernel, (unsigned)((p->V + share - 1) / share), SCAN_THREADS, 0, stream, g.order, p->V, share) ||
+            !launch_after(head_order_list_kernel, grid(p->T), ORDER_THREADS, 0, stream, g.order, tokens, grad_logp, p->T, p->V))
+            return PPOW_ERR_CUDA;
+    }
     if (!launch_gather<true, !BF16>(p, L, g, rows, hidden, stream)) return PPOW_ERR_CUDA;
     ProductJob job = {};
     job.rows = rows;
@@ -1289,7 +1517,7 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
         if (!launch_product<LOGITS_GRAD, BF16>(map_rows, map_weight, map_dz, job, L.columns, row_tiles * job.v_tiles, pairs, stream))
             return PPOW_ERR_CUDA;
         if (grad_hidden && !launch_product<GRAD_HIDDEN, BF16>(map_dz, map_weight_t, map_dz, job, L.columns, pairs, pairs, stream)) return PPOW_ERR_CUDA;
-        if (grad_weight && !launch_tiles<GRAD_WEIGHT, BF16, TILE>(map_dz_t, map_rows_t, map_grad, job, (int64_t)job.v_tiles * L.d_tiles, pairs, stream))
+        if (grad_weight && !launch_tiles<GRAD_WEIGHT, BF16, TILE>(map_dz_t, map_rows_t, map_grad, map_rest, job, (int64_t)job.v_tiles * L.d_tiles, pairs, stream))
             return PPOW_ERR_CUDA;
     }
     if (grad_hidden) {

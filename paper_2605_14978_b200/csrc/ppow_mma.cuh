@@ -42,8 +42,27 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
-// Bounded wait of the matrix kernels: false once WAIT_NS have passed without the phase completing.  The longest
-// proper wait is one tile's products (well under 10 ms for the largest sizes accepted).
+// One that does: what this thread knows of is visible in the other CTA to the thread that finds the phase complete and then calls
+// mbar_acquire_cluster (true at once: the phase is complete).
+__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_acquire_cluster(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+
+// Bounded wait of the matrix kernels: false once MMA_WAIT_NS have passed without the phase completing.  The longest
+// proper wait is one tile's products (under 50 ms for the largest sizes accepted).
 constexpr uint64_t MMA_WAIT_NS = 2000000000ull;
 __device__ __forceinline__ bool mbar_wait_ns(uint32_t bar, uint32_t parity)
 {
@@ -237,6 +256,11 @@ __device__ __forceinline__ bool named_barrier_all(uint32_t id, uint32_t threads,
 __device__ __forceinline__ void store_shared16(uint32_t dst, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+__device__ __forceinline__ void store_shared2(uint32_t dst, uint32_t low)
+{
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(dst), "h"((uint16_t)low) : "memory");
 }
 
 // ---- 32-byte stores ----
