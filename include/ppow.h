@@ -263,7 +263,8 @@ ppow_status ppow_reference_logprob(const ppow_params *params, const void *ref_ta
  * clipped objective, Sec. 4.1, and of the supervised loss, App. C.2), without keeping the logits:
  *     z = hidden weight^T / temperature        lse = log sum_v exp(z_v)        logp = z_y - lse
  * The cross entropy of a token is -logp.  Products are of the storage type with float32 sums; maximum, sum and
- * logarithm are float32 per 256 vocabulary entries and float64 across them.
+ * logarithm are float32 per 128 vocabulary entries and float64 across them.  The token's own product is summed in float64
+ * (float32 within 8 products), so that logp and 1 - exp(logp) keep their relative accuracy where logp is close to 0.
  */
 typedef struct {
     int32_t T;              /* tokens, 0 .. 2^20 */

@@ -78,6 +78,7 @@ struct HeadRows {
     float *mult;           // dz = mult * (softmax - onehot)
     float *lse2;           // normaliser in log2 units
     float *row_scale;      // dh = row_scale * (dz W)
+    float *target;         // p - 1 at the token
     float *residual;       // what the rounding of dz at the token left over
     TokenRows *rows_of;    // backward, per tile of the vocabulary
     void *rows;            // [padded, D] hidden states
@@ -85,6 +86,56 @@ struct HeadRows {
 };
 
 __device__ __forceinline__ void fault(HeadHeader *h, unsigned int bit) { atomicOr(&h->error_flags, bit); }
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if (BF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+template <bool BF16>
+__device__ __forceinline__ float2 unpack2(uint32_t w)
+{
+    if (BF16) return make_float2(bf16_lo(w), bf16_hi(w));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+}
+
+// x minus x rounded to 16 bits
+template <bool BF16>
+__device__ __forceinline__ float rounding_of(float x)
+{
+    return x - (BF16 ? __bfloat162float(__float2bfloat16_rn(x)) : __half2float(__float2half_rn(x)));
+}
+
+// ---- the token's own product ---------------------------------------------------------------------------
+// 1 - p of a token that the drafter is nearly sure of is a small difference, and log p close to 0 too: an error d of the token's
+// logit appears in them as d / (1 - p).  Tensor cores cut sums off towards zero, and over a product whose terms have one sign that
+// adds up (4096 wide, logits near 14: 1e-4, of the gradient of a token with p = 0.9995 a third to all).  So the token's logit is
+// computed apart: float32 over the 8 products of a unit, float64 from there on.  The calling lane's share: units first, first + step, ...
+template <bool BF16>
+__device__ __forceinline__ double token_product(const uint16_t *h, const uint16_t *w, int32_t units, int32_t first, int32_t step)
+{
+    double sum = 0.0;
+#pragma unroll 4
+    for (int32_t u = first; u < units; u += step) {
+        const uint4 a = *(reinterpret_cast<const uint4 *>(h) + u), b = *(reinterpret_cast<const uint4 *>(w) + u);
+        const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = unpack2<BF16>(x[i]), q = unpack2<BF16>(y[i]);
+            s = fmaf(p.x, q.x, s);
+            s = fmaf(p.y, q.y, s);
+        }
+        sum += (double)s;
+    }
+    return sum;
+}
 
 // ---- the order of the gradient's rows ----------------------------------------------------------------
 // By token, and with the same token as they come: what dW needs of the rows of an entry then lies side by side, and neither
@@ -174,6 +225,9 @@ struct GatherJob {
     bool by_token;                  // backward: rows in the order of their tokens, for dW
     RowOrder order;                 // of many tokens; null: counted here
     int32_t d_tiles, piece_steps;   // backward: what the shares of dh follow from; steps of the shortest piece
+    const uint16_t *weight;         // backward
+    int64_t weight_stride;
+    double exact_inv_temperature;
     float inv_temperature;
     bool vec;                       // rows start on 16-byte boundaries
 };
@@ -390,6 +444,34 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
             put(i, make_uint4(w[0], w[1], w[2], w[3]));
         }
     }
+    if (BACKWARD) {
+        // p - 1 at the token; of a few rows by all warps together, else a warp per row
+        __shared__ double shares[COUNTED][GATHER_THREADS / 32];
+        const bool together = n <= COUNTED;
+        __syncthreads();
+        for (int32_t k = together ? 0 : warp; k < n; k += together ? 1 : GATHER_THREADS / 32) {
+            const int32_t d = dest[k];
+            if (d < 0) continue;
+            const int32_t r = r0 + k;
+            const double z = warp_sum_f64(token_product<!SCALED>((const uint16_t *)out.rows + (size_t)d * job.D,
+                                                                 job.weight + (size_t)job.tokens[r] * job.weight_stride, units,
+                                                                 together ? tid : lane, together ? GATHER_THREADS : 32));
+            if (lane != 0) continue;
+            if (together)
+                shares[k][warp] = z;
+            else
+                out.target[d] = expm1f((float)(z * job.exact_inv_temperature - (double)job.lse[r]));
+        }
+        if (together) {
+            __syncthreads();
+            if (tid < n && dest[tid] >= 0) {
+                double z = 0.0;
+#pragma unroll
+                for (int w = 0; w < GATHER_THREADS / 32; ++w) z += shares[tid][w];
+                out.target[dest[tid]] = expm1f((float)(z * job.exact_inv_temperature - (double)job.lse[r0 + tid]));
+            }
+        }
+    }
     // the last tile's rows behind the live ones are zeros: they are products' operands too
     const int32_t padded = job.few ? job.few : max(TILE, (total + TILE - 1) / TILE * TILE);
     for (int32_t p = total + blockIdx.x; p < padded; p += gridDim.x) {
@@ -423,8 +505,7 @@ struct ProductJob {
     int32_t direct;         // LOGITS_SUM, few tokens: that many tokens, read where they lie (0: gathered)
     bool add;               // GRAD_HIDDEN: add to what the pieces before left
     int32_t parts;          // LOGITS_SUM: entries of `partial` per row
-    float2 *partial;        // LOGITS_SUM: [live row][parts] maximum, sum (log2 units)
-    float *at_token;        // LOGITS_SUM: the token's product, per live row
+    float2 *partial;        // LOGITS_SUM: [live row][parts] maximum, sum (log2 units), without the token
     uint16_t *dz;           // [padded rows][piece]
     float *grad_rows;       // GRAD_HIDDEN: [splits][padded live rows][D]
 };
@@ -434,31 +515,6 @@ struct Tile {
     int32_t k0, k1;         // inner steps of BK
     int32_t index, split;   // tile along the vocabulary or the width; share of the inner axis
 };
-
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack2(float a, float b)
-{
-    if (BF16) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-        return *reinterpret_cast<const uint32_t *>(&h);
-    }
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-
-template <bool BF16>
-__device__ __forceinline__ float2 unpack2(uint32_t w)
-{
-    if (BF16) return make_float2(bf16_lo(w), bf16_hi(w));
-    return __half22float2(*reinterpret_cast<const __half2 *>(&w));
-}
-
-// x minus x rounded to 16 bits
-template <bool BF16>
-__device__ __forceinline__ float rounding_of(float x)
-{
-    return x - (BF16 ? __bfloat162float(__float2bfloat16_rn(x)) : __half2float(__float2half_rn(x)));
-}
 
 // What a launch works on: sizes that follow from the number of live rows.
 struct Extent {
@@ -534,7 +590,7 @@ __device__ __forceinline__ void for_chunks(uint32_t src, R &&release, F &&f)
 // What a row's epilogue needs of its token, loaded before the tile is waited for.
 struct RowData {
     int32_t token;
-    float mult, lse2;
+    float mult, lse2, target;
 };
 
 // 32 columns (from column c of the half's 128) of the calling thread's row into the half's box, in the 128-byte swizzle: the
@@ -583,11 +639,11 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
     if (PRODUCT == LOGITS_SUM) {
         const int32_t left = min(TILE, job.V - x.col) - first;   // columns that exist
         const int32_t at = own.token - x.col - first;            // padded rows hold a negative token
-        // all 128 columns at once: one maximum, no rescaling
-        if (left < COLS) {
+        // all 128 columns at once: one maximum, no rescaling; the token's term comes from elsewhere
+        if (left < COLS || (at >= 0 && at < COLS)) {
 #pragma unroll
             for (int j = 0; j < COLS; ++j)
-                if (j >= left) w[j / 32][j % 32] = 0xff800000u;
+                if (j >= left || j == at) w[j / 32][j % 32] = 0xff800000u;
         }
         float hi[4];
 #pragma unroll
@@ -604,18 +660,10 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
             add[(j >> 1) & 3] = __fadd2_rn(add[(j >> 1) & 3], make_float2(ex2_approx(a.x), ex2_approx(a.y)));
         }
         const float2 s01 = __fadd2_rn(add[0], add[1]), s23 = __fadd2_rn(add[2], add[3]);
-        // a half that lies behind the vocabulary's end has no terms
-        const float sum = left > 0 ? (s01.x + s01.y) + (s23.x + s23.y) : 0.0f;
-        float mine = 0.0f;
-        if (at >= 0 && at < COLS) {
-#pragma unroll
-            for (int j = 0; j < COLS; ++j)
-                if (at == j) mine = __uint_as_float(w[j / 32][j % 32]);
-        }
-        if (row < e.live && PPOW_CHECK(2 * x.index + half < job.parts, 502, flags)) {
+        // a half may have no terms: behind the vocabulary's end, or but for the token
+        const float sum = most > -INFINITY ? (s01.x + s01.y) + (s23.x + s23.y) : 0.0f;
+        if (row < e.live && PPOW_CHECK(2 * x.index + half < job.parts, 502, flags))
             job.partial[(size_t)row * job.parts + 2 * x.index + half] = make_float2(top, sum);
-            if (at >= 0 && at < min(left, COLS)) job.at_token[row] = mine;
-        }
     } else if (PRODUCT == LOGITS_GRAD) {
         const int32_t left = min(TILE, job.V - x.col) - first;
         const int32_t at = own.token - x.col - first;
@@ -626,11 +674,10 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
 #pragma unroll
             for (int j = 0; j < 32; ++j) p[j] = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -lse2));
             if (at >= c && at < c + 32) {
-                float target = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (at == c + j) target = p[j] -= 1.0f;
-                if (row < e.live) job.rows.residual[row] = rounding_of<BF16>(target * mult);
+                    if (at == c + j) p[j] = own.target;
+                if (row < e.live) job.rows.residual[row] = rounding_of<BF16>(own.target * mult);
             }
             if (row >= e.live || c + 32 > left) {
 #pragma unroll
@@ -710,7 +757,8 @@ struct RunningSum {
 // rows: the vocabulary's entries, for GRAD_HIDDEN the width's; columns: tokens.  Sums over the rows run across the lanes.
 template <int PRODUCT, bool BF16, int N, typename R>
 __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent &e, const Tile &x, uint32_t src, int32_t in_tile, int half,
-                                             RunningSum (&run)[2], uint32_t (&z)[sum_chunks<N>()][sum_width<N>()], R &&release)
+                                             RunningSum (&run)[2], const int32_t (&token)[2], uint32_t (&z)[sum_chunks<N>()][sum_width<N>()],
+                                             R &&release)
 {
     constexpr int COLS = N / 2, WIDTH = sum_width<N>();
     const int lane = threadIdx.x & 31;
@@ -723,6 +771,14 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
         for (int c = 0; c < COLS; c += WIDTH) {
             if (first + c >= e.live) break;
             uint32_t (&w)[WIDTH] = z[c / WIDTH];
+            // the term of a token that lies in this warp's 32 rows, if any does, comes from elsewhere
+            const int32_t at = token[c / 32] - (row - lane);
+            const unsigned hits = __ballot_sync(0xffffffffu, at >= 0 && at < 32);
+            if (hits) {
+#pragma unroll
+                for (int j = 0; j < WIDTH; ++j)
+                    if ((hits >> j & 1u) && __shfl_sync(0xffffffffu, at, j) == lane) w[j] = 0xff800000u;
+            }
             float v[WIDTH], r[WIDTH];
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) r[j] = v[j] = inside ? __uint_as_float(w[j]) * job.scale : -INFINITY;
@@ -737,14 +793,6 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
             across_lanes<WIDTH>(r, [](float a, float b) { return a + b; });
             seen.sum = top > -INFINITY ? fmaf(seen.sum, ex2_approx(seen.top - top), r[0]) : 0.0f;
             seen.top = top;
-            // the product of a token that lies in this warp's 32 rows, if any does
-            const int32_t mine = first + c + lane, at = lane < WIDTH && mine < e.live ? job.rows.token[mine] - (row - lane) : -1;
-            const unsigned hits = __ballot_sync(0xffffffffu, at >= 0 && at < 32);
-            if (hits) {
-#pragma unroll
-                for (int j = 0; j < WIDTH; ++j)
-                    if ((hits >> j & 1u) && __shfl_sync(0xffffffffu, at, j) == lane) job.at_token[first + c + j] = __uint_as_float(w[j]);
-            }
         }
     } else if (PRODUCT == LOGITS_GRAD) {
         const bool inside = row < job.V;
@@ -761,7 +809,7 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
                 const float l = __shfl_sync(0xffffffffu, lse2, j), m = __shfl_sync(0xffffffffu, mult, j);
                 float d = ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -l));
                 const bool target = __shfl_sync(0xffffffffu, token, j) == row;
-                if (target) d -= 1.0f;
+                if (target) d = job.rows.target[first + c + j];
                 d = inside && first + c + j < e.live ? d * m : 0.0f;
                 if (target) job.rows.residual[first + c + j] = rounding_of<BF16>(d);
                 if (PPOW_CHECK(x.index * TILE + in_tile < job.piece, 507, flags))
@@ -1025,6 +1073,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
         uint32_t acc = 0;
         bool ok = true;
         RunningSum run[2] = {{-INFINITY, 0.0f}, {-INFINITY, 0.0f}};
+        int32_t token[2] = {-1, -1};                             // LOGITS_SUM, few tokens: those of columns lane % 32 of the chunks
+        if (FEW && PRODUCT == LOGITS_SUM) {
+#pragma unroll
+            for (int c = 0; c < N / 2; c += 32)
+                if (c + lane < N / 2 && half * (N / 2) + c + lane < e.live) token[c / 32] = max(job.rows.token[half * (N / 2) + c + lane], -1);
+        }
         uint32_t z[sum_chunks<N>()][sum_width<N>()] = {};        // LOGITS_SUM: the warp's logits
         for (int64_t t = pair; t < tiles && ok; t += pairs) {
             const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
@@ -1034,6 +1088,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                 if (PRODUCT == LOGITS_GRAD) {
                     own.mult = job.rows.mult[x.row + in_tile];
                     own.lse2 = job.rows.lse2[x.row + in_tile];
+                    own.target = job.rows.target[x.row + in_tile];
                 }
             }
             const int32_t parts = part_count<N, PARTS>(x);
@@ -1075,7 +1130,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                     if (part + 1 < parts) continue;
                 }
                 if constexpr (FEW)
-                    epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half, run, z, release);
+                    epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half, run, token, z, release);
                 else
                     epilogue_many<PRODUCT, BF16>(job, e, x, own, src, in_tile, half, &map_out, box, z, release);
             }
@@ -1105,24 +1160,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
 
 // ---- merge: one CTA per row ----------------------------------------------------------------------
 constexpr int MERGE_THREADS = 128;
-__global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows, const float2 *__restrict__ partial,
-                                                                   const float *__restrict__ at_token, int32_t parts, int32_t V,
-                                                                   float scale, float *__restrict__ logp, float *__restrict__ lse)
+struct MergeJob {
+    HeadRows rows;
+    const float2 *partial;
+    const uint16_t *hidden, *weight;      // hidden: by live row
+    int64_t hidden_stride, weight_stride;
+    int32_t parts, V, D;
+    double exact_scale;                   // log2(e) / temperature
+    float *logp, *lse;
+};
+template <bool BF16>
+__global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(const MergeJob job)
 {
     constexpr int HELD = 16;                             // entries per thread that are read once; more are read twice
     __shared__ float tops[MERGE_THREADS / 32];
-    __shared__ double sums[MERGE_THREADS / 32];
+    __shared__ double sums[MERGE_THREADS / 32], products[MERGE_THREADS / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int32_t row = blockIdx.x;
+    const int32_t row = blockIdx.x, parts = job.parts;
+    const HeadRows &rows = job.rows;
     allow_next_kernel();
     wait_for_previous_kernel();
     if (row >= rows.header->live) return;
     const int32_t r = rows.source ? rows.source[row] : row, y = rows.token[row];
     if (y < 0) {                                         // tokens that were not gathered: the masked ones are among them
-        if (tid == 0) logp[r] = lse[r] = 0.0f;
+        if (tid == 0) job.logp[r] = job.lse[r] = 0.0f;
         return;
     }
-    const float2 *p = partial + (size_t)row * parts;
+    const float2 *p = job.partial + (size_t)row * parts;
     float2 held[HELD];
     float top = -INFINITY;
 #pragma unroll
@@ -1134,27 +1198,44 @@ __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(HeadRows rows
     for (int i = 0; i < HELD; ++i) top = fmaxf(top, held[i].x);
 #pragma unroll 8
     for (int32_t k = tid + HELD * MERGE_THREADS; k < parts; k += MERGE_THREADS) top = fmaxf(top, p[k].x);
+    const double product = y < job.V ? token_product<BF16>(job.hidden + (size_t)row * job.hidden_stride, job.weight + (size_t)y * job.weight_stride,
+                                                           job.D / 8, tid, MERGE_THREADS)
+                                     : 0.0;
     top = warp_max(top);
     if (lane == 0) tops[warp] = top;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < MERGE_THREADS / 32; ++i) top = fmaxf(top, tops[i]);
-    double sum = 0.0;
+    double sum = 0.0, z2 = warp_sum_f64(product);
 #pragma unroll
     for (int i = 0; i < HELD; ++i) sum += (double)(held[i].y * ex2_approx(held[i].x - top));
 #pragma unroll 8
     for (int32_t k = tid + HELD * MERGE_THREADS; k < parts; k += MERGE_THREADS) sum += (double)(p[k].y * ex2_approx(p[k].x - top));
     sum = warp_sum_f64(sum);
-    if (lane == 0) sums[warp] = sum;
+    if (lane == 0) {
+        sums[warp] = sum;
+        products[warp] = z2;
+    }
     __syncthreads();
     if (tid == 0) {
-        sum = 0.0;
+        sum = z2 = 0.0;
 #pragma unroll
-        for (int i = 0; i < MERGE_THREADS / 32; ++i) sum += sums[i];
-        const double lse2 = (double)top + log2(sum);
+        for (int i = 0; i < MERGE_THREADS / 32; ++i) {
+            sum += sums[i];
+            z2 += products[i];
+        }
         const double ln2 = 0.69314718055994530942;
-        lse[r] = (float)(lse2 * ln2);
-        logp[r] = y < V ? (float)(((double)at_token[row] * (double)scale - lse2) * ln2) : -INFINITY;
+        z2 *= job.exact_scale;
+        if (y >= job.V) {                                // no such token: the sums are whole without it
+            job.lse[r] = (float)(((double)top + log2(sum)) * ln2);
+            job.logp[r] = -INFINITY;
+        } else {
+            // the others' share against the token's: log p = -log(1 + others / token), exact for p near 1 too
+            const double ratio2 = (double)top + log2(sum) - z2;
+            const double nats = ratio2 < 60.0 ? log1p(exp2(ratio2)) : ratio2 * ln2;
+            job.logp[r] = (float)-nats;
+            job.lse[r] = (float)(z2 * ln2 + nats);
+        }
     }
 }
 
@@ -1216,7 +1297,7 @@ bool params_ok(const ppow_head_params *p)
 int32_t tile_columns(int32_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : TILE; }
 
 struct Layout {
-    size_t source, token, mult, lse2, row_scale, residual, rows_of, rows, scaled, partial, at_token, dz, grad_rows, order, total;
+    size_t source, token, mult, lse2, row_scale, target, residual, rows_of, rows, scaled, partial, dz, grad_rows, order, total;
     int32_t columns, few, padded, v_tiles, d_tiles, parts;
     int32_t pieces, piece;          // backward: pieces of the vocabulary, entries of the longest (the row length of dz)
 };
@@ -1264,13 +1345,13 @@ Layout layout_of(const ppow_head_params *p, bool backward)
     L.mult = take(rows * 4);
     L.lse2 = take(rows * 4);
     L.row_scale = take(rows * 4);
+    L.target = take(rows * 4);
     L.residual = take(rows * 4);
     L.rows = take(rows * p->D * 2);
     if (!backward) {
         // few tokens: four warps of each CTA; there are at most as many pairs as tiles
         L.parts = L.few ? 8 * (L.v_tiles < MAX_PAIRS ? L.v_tiles : MAX_PAIRS) : 2 * L.v_tiles;
         L.partial = take(rows * L.parts * sizeof(float2));
-        L.at_token = take(rows * 4);
     } else {
         if (p->T > ORDER_COUNTED) L.order = take(((size_t)p->V * 2 + rows * 2) * 4);
         if (p->dtype == PPOW_F16) L.scaled = take(rows * p->D * 2);
@@ -1389,6 +1470,7 @@ HeadRows rows_of(char *ws, const Layout &L)
     r.mult = (float *)(ws + L.mult);
     r.lse2 = (float *)(ws + L.lse2);
     r.row_scale = (float *)(ws + L.row_scale);
+    r.target = (float *)(ws + L.target);
     r.residual = (float *)(ws + L.residual);
     r.rows_of = (TokenRows *)(ws + L.rows_of);
     r.rows = ws + L.rows;
@@ -1408,7 +1490,8 @@ bool launch_gather(const ppow_head_params *p, const Layout &L, const GatherJob &
     job.few = L.few;
     job.d_tiles = L.d_tiles;
     job.piece_steps = L.pieces ? shortest_steps(L, p->V) : 0;
-    job.inv_temperature = (float)(1.0 / (double)p->temperature);
+    job.exact_inv_temperature = 1.0 / (double)p->temperature;
+    job.inv_temperature = (float)job.exact_inv_temperature;
     job.vec = rows_aligned(hidden, p->hidden_stride);
     job.hidden = (const uint16_t *)hidden;
     // a row per CTA, more where that would be over a thousand CTAs: each of them looks at all tokens
@@ -1453,12 +1536,22 @@ ppow_status forward(const ppow_head_params *p, const void *hidden, const void *w
     job.d_tiles = L.d_tiles;
     job.parts = L.few ? 8 * (L.v_tiles < pairs ? L.v_tiles : pairs) : L.parts;
     job.partial = (float2 *)(ws + L.partial);
-    job.at_token = (float *)(ws + L.at_token);
     const int64_t tiles = (int64_t)((L.padded + TILE - 1) / TILE) * L.v_tiles;
     if (!launch_product<LOGITS_SUM, BF16>(map_rows, map_weight, map_rows, job, L.columns, tiles, pairs, stream)) return PPOW_ERR_CUDA;
-    return launch_after(head_merge_kernel, (unsigned)p->T, MERGE_THREADS, 0, stream, rows, job.partial, job.at_token, job.parts, p->V, job.scale, logp, lse)
-               ? PPOW_OK
-               : PPOW_ERR_CUDA;
+    MergeJob merge = {};
+    merge.rows = rows;
+    merge.partial = job.partial;
+    merge.hidden = (const uint16_t *)(direct ? hidden : rows.rows);
+    merge.hidden_stride = direct ? p->hidden_stride : p->D;
+    merge.weight = (const uint16_t *)weight;
+    merge.weight_stride = p->weight_stride;
+    merge.parts = job.parts;
+    merge.V = p->V;
+    merge.D = p->D;
+    merge.exact_scale = 1.4426950408889634074 / (double)p->temperature;
+    merge.logp = logp;
+    merge.lse = lse;
+    return launch_after(head_merge_kernel<BF16>, (unsigned)p->T, MERGE_THREADS, 0, stream, merge) ? PPOW_OK : PPOW_ERR_CUDA;
 }
 
 template <bool BF16>
@@ -1485,6 +1578,8 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     g.grad = grad_logp;
     g.grad_hidden = (uint16_t *)grad_hidden;
     g.by_token = grad_weight != nullptr;
+    g.weight = (const uint16_t *)weight;
+    g.weight_stride = p->weight_stride;
     if (L.order && grad_weight) {
         g.order.count = (int32_t *)(ws + L.order);
         g.order.first = g.order.count + p->V;
