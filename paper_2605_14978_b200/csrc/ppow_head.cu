@@ -39,10 +39,22 @@ template <int N> __host__ __device__ constexpr int stage_count()
 {
     return N == 256 ? 6 : N == 128 ? 8 : N == 64 ? 10 : N == 32 ? 11 : 12;    // 192 to 204 KB
 }
-// Steps that the logits of the forward pass are summed over in Tensor Memory before the sum moves on to registers: the tensor
-// cores' additions cut off what does not fit, and over 256 products (4096 wide) that left lse off by 3e-6.  16 steps leave
-// 7e-7 and cost a large batch 3.6 % (8: 8 %); with few tokens, where a single log-probability close to 0 shows it more, 4 are free.
-template <int N> __host__ __device__ constexpr int sum_steps() { return N == 256 ? 16 : N == 128 ? 8 : 4; }
+enum Product {
+    LOGITS_SUM,   // rows x W^T: maximum and sum of exponentials per row and tile
+    LOGITS_GRAD,  // rows x W^T: dz of a piece of the vocabulary
+    GRAD_HIDDEN,  // dz x W: the piece's share of dh
+    GRAD_WEIGHT   // dz^T x rows: dW of the piece
+};
+
+// Steps that a product is summed over in Tensor Memory before the sum moves on to registers: the tensor cores' additions cut off
+// what does not fit.  Logits of the forward pass: over 256 products (4096 wide) that left lse off by 3e-6; 16 steps leave 7e-7 and
+// cost a large batch 3.6 % (8: 8 %), with few tokens 4 are free.  dW: its sum runs over the tokens, and where its terms have one sign
+// (every softmax's has, so the states' mean is enough) each 65536 of them took 4e-4 off it, of 2^20 0.7 %; with parts of 8192 tokens
+// it is under 1e-4.  (Gradient of 262144 x 1024 x 4096: 12.5 ms either way.)
+template <int PRODUCT, int N> __host__ __device__ constexpr int sum_steps()
+{
+    return PRODUCT == GRAD_WEIGHT ? 128 : N == 256 ? 16 : N == 128 ? 8 : 4;
+}
 // Tiles of 16-bit results leave through shared memory: a box of 128 rows x 64 columns for each half of the columns.
 constexpr uint32_t BOX_BYTES = HALF_TILE * 128;
 template <int N> __host__ __device__ constexpr size_t mma_smem()
@@ -54,6 +66,7 @@ constexpr int GATHER_THREADS = 256, EARLY = 4;
 constexpr int GATHER_ROWS_MAX = 1024, GATHER_CTAS = 1024;
 constexpr size_t HEADER_BYTES = 256;
 constexpr size_t DZ_BYTES = 512u << 20;      // a piece of dz holds at most this much
+constexpr int32_t PIECE_TILES = 1024;        // and this many vocabulary tiles: dh is summed over a piece (see sum_steps)
 constexpr int32_t MAX_TOKENS = 1 << 20, MAX_VOCAB = 1 << 22, MAX_WIDTH = 1 << 16;
 
 // First bytes of the workspace; error_flags sits where ppow_read_error_flags looks for it.
@@ -488,17 +501,11 @@ __global__ void __launch_bounds__(GATHER_THREADS) head_gather_kernel(GatherJob j
 }
 
 // ---- the products -----------------------------------------------------------------------------------
-enum Product {
-    LOGITS_SUM,   // rows x W^T: maximum and sum of exponentials per row and tile
-    LOGITS_GRAD,  // rows x W^T: dz of a piece of the vocabulary
-    GRAD_HIDDEN,  // dz x W: the piece's share of dh
-    GRAD_WEIGHT   // dz^T x rows: dW of the piece
-};
-
 struct ProductJob {
     HeadRows rows;
     float scale;            // log2(e) / temperature
     int32_t D, V;
+    int32_t tokens;         // GRAD_WEIGHT: rows at most, masked ones with them
     int32_t v0, columns;    // the piece: vocabulary entries v0 .. v0 + columns - 1
     int32_t v_tiles, d_tiles;
     int32_t piece;          // row length of dz
@@ -564,9 +571,9 @@ __device__ __forceinline__ Tile tile_at(const ProductJob &job, const Extent &e, 
 
 // Accumulators that a tile's sum passes through, one after the other.  The issuing thread and the epilogue warps both count by
 // it: every tile takes one at least, so that the two sides agree on buffer and phase whatever its steps are.
-template <int N, bool PARTS> __device__ __forceinline__ int32_t part_count(const Tile &x)
+template <int PRODUCT, int N, bool PARTS> __device__ __forceinline__ int32_t part_count(const Tile &x)
 {
-    return PARTS ? max(1, (x.k1 - x.k0 + sum_steps<N>() - 1) / sum_steps<N>()) : 1;
+    return PARTS ? max(1, (x.k1 - x.k0 + sum_steps<PRODUCT, N>() - 1) / sum_steps<PRODUCT, N>()) : 1;
 }
 
 // ---- epilogues: one warp, 32 rows of the tile's accumulator (its Tensor Memory lanes), half of the columns --------
@@ -625,7 +632,7 @@ __device__ __forceinline__ void note_token(const ProductJob &job, const Extent &
 }
 
 // rows: tokens, columns: vocabulary
-template <int PRODUCT, bool BF16, typename R>
+template <int PRODUCT, bool BF16, bool PARTS, typename R>
 __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Extent &e, const Tile &x, const RowData &own, uint32_t src,
                                               int32_t in_tile, int half, const CUtensorMap *map_out, uint32_t box,
                                               uint32_t (&w)[TILE / 64][32], R &&release)
@@ -714,13 +721,19 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
     } else {
         const float out_scale = job.rows.header->out_scale;
         const int32_t v = x.row + in_tile / HALF_TILE * HALF_TILE;       // the box's first row within the piece
-        for_chunks<COLS / 32, 32>(src, release, [&](int c, uint32_t (&w)[32]) {
+        auto store = [&](int c, uint32_t (&w)[32]) {
             uint32_t o[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 o[j] = pack2<BF16>(__uint_as_float(w[2 * j]) * out_scale, __uint_as_float(w[2 * j + 1]) * out_scale);
             put_box(box, in_tile, half, c, o, map_out, x.col + first, job.v0 + v, x.col + first + (c & 64) < job.D && v < job.columns);
-        });
+        };
+        if constexpr (PARTS) {
+#pragma unroll
+            for (int c = 0; c < COLS; c += 32) store(c, w[c / 32]);
+        } else {
+            for_chunks<COLS / 32, 32>(src, release, store);
+        }
     }
 }
 
@@ -1024,10 +1037,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
             bool ok = true;
             for (int64_t t = pair; t < tiles && ok; t += pairs) {
                 const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
-                const int32_t parts = part_count<N, PARTS>(x);
+                const int32_t parts = part_count<PRODUCT, N, PARTS>(x);
                 [[maybe_unused]] const TokenRows rows = tile_rows<REMAINDERS>(job, tiles, t, t);
                 for (int32_t part = 0; part < parts && ok; ++part, ++acc) {
-                    const int32_t k0 = PARTS ? x.k0 + part * sum_steps<N>() : x.k0, k1 = PARTS ? min(k0 + sum_steps<N>(), x.k1) : x.k1;
+                    const int32_t k0 = PARTS ? x.k0 + part * sum_steps<PRODUCT, N>() : x.k0, k1 = PARTS ? min(k0 + sum_steps<PRODUCT, N>(), x.k1) : x.k1;
                     const uint32_t b = acc & 1u, d = tmem + b * TILE;
                     ok = mbar_wait_ns(acc_empty(b), ((acc >> 1) & 1u) ^ 1u);
                     tcgen05_fence_after();
@@ -1045,7 +1058,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                         mma_commit_pair(empty(s));
                     }
                     if constexpr (REMAINDERS) {
-                        for (int32_t row = rows.first; row < rows.end && ok; row += BK, ++it) {
+                        for (int32_t row = part + 1 < parts ? rows.end : rows.first; row < rows.end && ok; row += BK, ++it) {
                             const uint32_t s = it % STAGES;
                             // the other CTA's half was written by its threads
                             ok = mbar_wait_ns(full(s), (it / STAGES) & 1u) && mbar_acquire_cluster(full(s), (it / STAGES) & 1u);
@@ -1079,7 +1092,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
             for (int c = 0; c < N / 2; c += 32)
                 if (c + lane < N / 2 && half * (N / 2) + c + lane < e.live) token[c / 32] = max(job.rows.token[half * (N / 2) + c + lane], -1);
         }
-        uint32_t z[sum_chunks<N>()][sum_width<N>()] = {};        // LOGITS_SUM: the warp's logits
+        uint32_t z[sum_chunks<N>()][sum_width<N>()] = {};        // LOGITS_SUM, GRAD_WEIGHT in parts: the warp's columns
         for (int64_t t = pair; t < tiles && ok; t += pairs) {
             const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
             RowData own = {};
@@ -1091,7 +1104,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                     own.target = job.rows.target[x.row + in_tile];
                 }
             }
-            const int32_t parts = part_count<N, PARTS>(x);
+            const int32_t parts = part_count<PRODUCT, N, PARTS>(x);
             for (int32_t part = 0; part < parts; ++part, ++acc) {
                 const uint32_t b = acc & 1u;
                 // all four warps of a half go on or none does: they meet at barriers further down
@@ -1104,7 +1117,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(peer_addr(acc_empty(b), 0));
                 };
-                if constexpr (PRODUCT == LOGITS_SUM) {
+                if constexpr (PRODUCT == LOGITS_SUM || (PRODUCT == GRAD_WEIGHT && PARTS)) {
                     constexpr int CHUNKS = sum_chunks<N>(), WIDTH = sum_width<N>(), ADD = WIDTH < 16 ? WIDTH : 16;
                     const uint32_t from = src + half * (N / 2);
                     if (!PARTS || part == 0) {
@@ -1132,7 +1145,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                 if constexpr (FEW)
                     epilogue_few<PRODUCT, BF16, N>(job, e, x, src, in_tile, half, run, token, z, release);
                 else
-                    epilogue_many<PRODUCT, BF16>(job, e, x, own, src, in_tile, half, &map_out, box, z, release);
+                    epilogue_many<PRODUCT, BF16, PARTS>(job, e, x, own, src, in_tile, half, &map_out, box, z, release);
             }
         }
         if (FEW && PRODUCT == LOGITS_SUM) {
@@ -1358,6 +1371,7 @@ Layout layout_of(const ppow_head_params *p, bool backward)
         const size_t strip = rows * TILE * 2;                      // one column tile of dz
         int32_t fit = (int32_t)(DZ_BYTES / strip);
         if (fit < 1) fit = 1;
+        if (fit > PIECE_TILES) fit = PIECE_TILES;
         L.pieces = (L.v_tiles + fit - 1) / fit;
         L.piece = (L.v_tiles + L.pieces - 1) / L.pieces * TILE;    // lengths differ by one tile at most
         L.dz = take(rows * L.piece * 2);
@@ -1402,12 +1416,13 @@ bool make_map(CUtensorMap *map, const void *base, bool bf16, int64_t width, int6
 
 // Pairs of SMs of the current device, asked once per device; the kernels' shared-memory limit is raised at the same time.
 constexpr int DEVICES = 64;
+template <int PRODUCT> constexpr bool in_parts() { return PRODUCT == LOGITS_SUM || PRODUCT == GRAD_WEIGHT; }
 template <int PRODUCT, bool BF16, int N> bool allow_smem()
 {
     constexpr int BYTES = (int)mma_smem<N>();
     return cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16, N, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) == cudaSuccess &&
-           (PRODUCT != LOGITS_SUM || cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16, N, PRODUCT == LOGITS_SUM>,
-                                                          cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) == cudaSuccess);
+           (!in_parts<PRODUCT>() || cudaFuncSetAttribute(head_product_kernel<PRODUCT, BF16, N, in_parts<PRODUCT>()>,
+                                                         cudaFuncAttributeMaxDynamicSharedMemorySize, BYTES) == cudaSuccess);
 }
 template <int PRODUCT, bool BF16> bool allow_smem_few()
 {
@@ -1434,9 +1449,9 @@ bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap 
                   int64_t most_tiles, int pairs, cudaStream_t stream)
 {
     const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
-    // one part is a kernel of its own: the loop over parts costs it a third (2048 x 128 x 128256: 106 us, with the loop 140)
-    if (PRODUCT == LOGITS_SUM && job.D > sum_steps<N>() * BK)
-        return launch_after(head_product_kernel<PRODUCT, BF16, N, PRODUCT == LOGITS_SUM>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, rest, job);
+    // one part is a kernel of its own: the loop over parts costs the forward pass a third (2048 x 128 x 128256: 106 us, with it 140)
+    if (in_parts<PRODUCT>() && (PRODUCT == LOGITS_SUM ? job.D : job.tokens) > sum_steps<PRODUCT, N>() * BK)
+        return launch_after(head_product_kernel<PRODUCT, BF16, N, in_parts<PRODUCT>()>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, rest, job);
     return launch_after(head_product_kernel<PRODUCT, BF16, N, false>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, rest, job);
 }
 
@@ -1601,6 +1616,7 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     job.V = p->V;
     job.d_tiles = L.d_tiles;
     job.piece = L.piece;
+    job.tokens = p->T;
     job.dz = dz;
     job.grad_rows = (float *)(ws + L.grad_rows);
     const int64_t row_tiles = (L.padded + TILE - 1) / TILE;

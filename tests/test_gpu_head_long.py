@@ -61,3 +61,30 @@ def test_many_pieces_no_row_masked():
         assert torch.all((gh[s].double() - dh).abs() <= th), i
     assert float((gw.double() - dw).norm() / dw.norm()) < 2 * head.U[torch.bfloat16]
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T", [8192, 8193, 65536, 262144])
+def test_sums_over_many_tokens_whose_terms_have_one_sign(T, dtype):
+    # Hidden states with a mean of 1, a loss of equal weights: every entry's softmax pulls its row of dW the same way.  Besides the
+    # roundings of the result and of dz (see test_gpu_head_rounding) the tensor cores cut off what does not fit: in a sum of 8192 tokens
+    # 513 times, at most two steps 2^-23 of its magnitude each, 1.3e-4 of sum |dz| |h|.
+    V, D, rows = 300, 64, 8192
+    g = torch.Generator(device=DEV).manual_seed(T)
+    w = (torch.randn((V, D), generator=g, device=DEV) * 0.1).to(dtype)
+    h = (1 + 0.2 * torch.randn((T, D), generator=g, device=DEV)).to(dtype)
+    tok = torch.randint(0, V // 2, (T,), generator=g, device=DEV, dtype=torch.int32)
+    grad = torch.full((T,), -1.0 / 64, device=DEV)
+    lse = B.head_logprob(h, w, tok)["lse"]
+    _, gw = backward(h, w, tok, lse, grad)
+    want, size, others = torch.zeros((3, V, D), dtype=torch.float64, device=DEV)
+    for i in range(0, T, rows):
+        x, y = h[i:i + rows].double(), tok[i:i + rows].long()[:, None]
+        q = torch.exp(x @ w.double().t() - lse[i:i + rows].double()[:, None])
+        dz = (q - torch.zeros_like(q).scatter(1, y, 1.0)) / 64
+        want += dz.t() @ x
+        size += dz.abs().t() @ x.abs()
+        others += dz.scatter(1, y, 0.0).square().t() @ x.square()
+    own = (want.to(dtype).double() - want).square().sum()
+    most = 1.05 * (own + head.U[dtype] ** 2 / 3 * others.sum()).sqrt() + 1.3e-4 * size.norm()
+    assert float((gw.double() - want).norm()) <= float(most)
