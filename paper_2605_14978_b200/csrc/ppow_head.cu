@@ -792,16 +792,16 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
                 for (int j = 0; j < WIDTH; ++j)
                     if ((hits >> j & 1u) && __shfl_sync(0xffffffffu, at, j) == lane) w[j] = 0xff800000u;
             }
-            float v[WIDTH], r[WIDTH];
+            float r[WIDTH];
 #pragma unroll
-            for (int j = 0; j < WIDTH; ++j) r[j] = v[j] = inside ? __uint_as_float(w[j]) * job.scale : -INFINITY;
+            for (int j = 0; j < WIDTH; ++j) r[j] = inside ? __uint_as_float(w[j]) : -INFINITY;
             across_lanes<WIDTH>(r, [](float a, float b) { return fmaxf(a, b); });
             RunningSum &seen = run[c / 32];
-            const float top = fmaxf(seen.top, r[0]);         // of column lane % WIDTH
+            const float top = fmaxf(seen.top, r[0] * job.scale);     // of column lane % WIDTH; rounded, and taken as it is from here on
 #pragma unroll
             for (int j = 0; j < WIDTH; ++j) {
                 const float hi = __shfl_sync(0xffffffffu, top, j);
-                r[j] = inside ? ex2_approx(v[j] - hi) : 0.0f;
+                r[j] = inside ? ex2_approx(fmaf(__uint_as_float(w[j]), job.scale, -hi)) : 0.0f;
             }
             across_lanes<WIDTH>(r, [](float a, float b) { return a + b; });
             seen.sum = top > -INFINITY ? fmaf(seen.sum, ex2_approx(seen.top - top), r[0]) : 0.0f;
@@ -1179,7 +1179,7 @@ struct MergeJob {
     const uint16_t *hidden, *weight;      // hidden: by live row
     int64_t hidden_stride, weight_stride;
     int32_t parts, V, D;
-    double exact_scale;                   // log2(e) / temperature
+    double exact_scale, rescale;          // log2(e) / temperature; that over the float32 value that the sums were taken with
     float *logp, *lse;
 };
 template <bool BF16>
@@ -1239,12 +1239,14 @@ __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(const MergeJo
         }
         const double ln2 = 0.69314718055994530942;
         z2 *= job.exact_scale;
+        // the sums' reference was scaled by a rounded number: 6e-8 of a logit of 60 would be in the result undamped
+        const double others2 = (double)top * job.rescale + log2(sum);
         if (y >= job.V) {                                // no such token: the sums are whole without it
-            job.lse[r] = (float)(((double)top + log2(sum)) * ln2);
+            job.lse[r] = (float)(others2 * ln2);
             job.logp[r] = -INFINITY;
         } else {
             // the others' share against the token's: log p = -log(1 + others / token), exact for p near 1 too
-            const double ratio2 = (double)top + log2(sum) - z2;
+            const double ratio2 = others2 - z2;
             const double nats = ratio2 < 60.0 ? log1p(exp2(ratio2)) : ratio2 * ln2;
             job.logp[r] = (float)-nats;
             job.lse[r] = (float)(z2 * ln2 + nats);
@@ -1564,6 +1566,7 @@ ppow_status forward(const ppow_head_params *p, const void *hidden, const void *w
     merge.V = p->V;
     merge.D = p->D;
     merge.exact_scale = 1.4426950408889634074 / (double)p->temperature;
+    merge.rescale = merge.exact_scale / (double)job.scale;
     merge.logp = logp;
     merge.lse = lse;
     return launch_after(head_merge_kernel<BF16>, (unsigned)p->T, MERGE_THREADS, 0, stream, merge) ? PPOW_OK : PPOW_ERR_CUDA;
