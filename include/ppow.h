@@ -313,7 +313,8 @@ ppow_status ppow_head_logprob(const ppow_head_params *params, const void *hidden
  *   grad_logp    device, [T] float32
  *   grad_hidden  device, [T, D] of the storage type, contiguous, 16-byte aligned, or NULL
  *   grad_weight  device, [V, D] of the storage type, contiguous, 16-byte aligned, or NULL (a frozen head).  At least one
- *                of the two is required.  T == 0 sets grad_weight to 0.
+ *                of the two is required, but with T == 0, which sets grad_weight to 0 where there is one (grad_hidden is empty
+ *                then, and an empty array may well be at NULL).
  *   workspace    device, >= ppow_head_workspace_bytes(params, 1), 256-byte aligned
  */
 ppow_status ppow_head_logprob_backward(const ppow_head_params *params, const void *hidden, const void *weight,

@@ -1688,13 +1688,13 @@ extern "C" ppow_status ppow_head_logprob_backward(const ppow_head_params *params
                                                   void *grad_weight, void *workspace, size_t workspace_bytes, void *cuda_stream)
 {
     if (!params_ok(params)) return PPOW_ERR_INVALID_ARG;
-    if ((!grad_hidden && !grad_weight) || (uintptr_t)grad_hidden % 16 || (uintptr_t)grad_weight % 16) return PPOW_ERR_INVALID_ARG;
+    if ((uintptr_t)grad_hidden % 16 || (uintptr_t)grad_weight % 16) return PPOW_ERR_INVALID_ARG;
     if (params->T == 0) {
         if (grad_weight && cudaMemsetAsync(grad_weight, 0, (size_t)params->V * params->D * 2, (cudaStream_t)cuda_stream) != cudaSuccess)
             return PPOW_ERR_CUDA;
         return PPOW_OK;
     }
-    if (!hidden || !weight || !tokens || !lse || !grad_logp) return PPOW_ERR_INVALID_ARG;
+    if ((!grad_hidden && !grad_weight) || !hidden || !weight || !tokens || !lse || !grad_logp) return PPOW_ERR_INVALID_ARG;
     if ((uintptr_t)hidden % 2 || (uintptr_t)weight % 16 || (uintptr_t)tokens % 4 || (uintptr_t)lse % 4 || (uintptr_t)grad_logp % 4)
         return PPOW_ERR_INVALID_ARG;
     if (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < layout_of(params, true).total) return PPOW_ERR_WORKSPACE;
