@@ -295,7 +295,8 @@ int ppow_head_plan(const ppow_head_params *params, int32_t live, int32_t piece, 
  *               anything) and logp = lse = 0.  A token >= V gets logp = -inf and sets PPOW_FLAG_TOKEN_RANGE.
  *   logp, lse   device, [T] float32
  *   workspace   device, >= ppow_head_workspace_bytes(params, 0), 256-byte aligned; ppow_read_error_flags works on it
- * Rows that are not masked must hold finite values.  The error flag PPOW_FLAG_DEVICE_TIMEOUT as for ppow_score_windows.
+ * Rows that are not masked must hold finite values.  The error flag PPOW_FLAG_DEVICE_TIMEOUT as for ppow_score_windows; with it set,
+ * logp and lse of the rows that are not masked are NaN.
  */
 ppow_status ppow_head_logprob(const ppow_head_params *params, const void *hidden, const void *weight, const int32_t *tokens,
                               float *logp, float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream);
@@ -315,7 +316,8 @@ ppow_status ppow_head_logprob(const ppow_head_params *params, const void *hidden
  *   grad_weight  device, [V, D] of the storage type, contiguous, 16-byte aligned, or NULL (a frozen head).  At least one
  *                of the two is required, but with T == 0, which sets grad_weight to 0 where there is one (grad_hidden is empty
  *                then, and an empty array may well be at NULL).
- *   workspace    device, >= ppow_head_workspace_bytes(params, 1), 256-byte aligned
+ *   workspace    device, >= ppow_head_workspace_bytes(params, 1), 256-byte aligned; ppow_read_error_flags works on it.  With
+ *                PPOW_FLAG_DEVICE_TIMEOUT set grad_hidden is NaN and grad_weight is not to be used.
  */
 ppow_status ppow_head_logprob_backward(const ppow_head_params *params, const void *hidden, const void *weight,
                                        const int32_t *tokens, const float *lse, const float *grad_logp,

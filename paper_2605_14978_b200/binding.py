@@ -760,13 +760,15 @@ def _workspace(nbytes: int, dev) -> torch.Tensor:
     return torch.empty(nbytes or 256, dtype=torch.uint8, device=dev)
 
 
-def head_logprob(hidden, weight, tokens, *, temperature=1.0, stream=None) -> dict:
-    """Allocate outputs and workspace, run ppow_head_logprob; returns logp and lse, both [T] float32."""
+def head_logprob(hidden, weight, tokens, *, temperature=1.0, want_workspace=False, stream=None) -> dict:
+    """Allocate outputs and workspace, run ppow_head_logprob; returns logp and lse, both [T] float32.  With ``want_workspace`` also
+    ``_workspace``, whose error word ppow_read_error_flags reads (tokens behind the vocabulary, a device wait that ran out); it is not
+    kept otherwise, because it holds 8 bytes for every 128 logits and a copy of the rows."""
     if stream is None:
-        got = _quick().head_logprob(hidden, weight, tokens, temperature)
+        got = _quick().head_logprob(hidden, weight, tokens, temperature, want_workspace)
         if got is not None:
-            logp, lse = _done(got, "ppow_head_logprob")
-            return {"logp": logp, "lse": lse}
+            logp, lse, ws = _done(got, "ppow_head_logprob")
+            return {"logp": logp, "lse": lse, "_workspace": ws} if want_workspace else {"logp": logp, "lse": lse}
     params, lib, f32 = make_head_params(hidden, weight, temperature), load_library(), torch.float32
     T, V, D, dt, device, dev = params.T, params.V, params.D, hidden.dtype, hidden.device, _index_of(hidden, "hidden")
     h, w = _rows_arg(hidden, dt, (T, D), dev, "hidden")[0], _rows_arg(weight, dt, (V, D), dev, "weight")[0]
@@ -777,15 +779,17 @@ def head_logprob(hidden, weight, tokens, *, temperature=1.0, stream=None) -> dic
         ws = _workspace(nbytes, device)
     _call(lib.ppow_head_logprob, "ppow_head_logprob", dev, ctypes.byref(params), h, w, y, logp.data_ptr(), lse.data_ptr(),
           ws.data_ptr(), nbytes, _raw_stream(stream, dev))
-    return {"logp": logp, "lse": lse}
+    return {"logp": logp, "lse": lse, "_workspace": ws} if want_workspace else {"logp": logp, "lse": lse}
 
 
-def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature=1.0, want_hidden=True, want_weight=True, stream=None):
-    """Allocate gradients and workspace, run ppow_head_logprob_backward; returns (grad_hidden, grad_weight), None where not wanted."""
+def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature=1.0, want_hidden=True, want_weight=True,
+                          want_workspace=False, stream=None):
+    """Allocate gradients and workspace, run ppow_head_logprob_backward; returns (grad_hidden, grad_weight), None where not wanted.
+    With ``want_workspace`` the workspace is returned as a third, for ppow_read_error_flags (it holds up to 512 MiB and more)."""
     if stream is None:
-        got = _quick().head_logprob_backward(hidden, weight, tokens, lse, grad_logp, temperature, want_hidden, want_weight)
+        got = _quick().head_logprob_backward(hidden, weight, tokens, lse, grad_logp, temperature, want_hidden, want_weight, want_workspace)
         if got is not None:
-            return _done(got, "ppow_head_logprob_backward")
+            return _done(got, "ppow_head_logprob_backward")[:3 if want_workspace else 2]
     params, lib, f32 = make_head_params(hidden, weight, temperature), load_library(), torch.float32
     T, V, D, dt, device, dev = params.T, params.V, params.D, hidden.dtype, hidden.device, _index_of(hidden, "hidden")
     h, w = _rows_arg(hidden, dt, (T, D), dev, "hidden")[0], _rows_arg(weight, dt, (V, D), dev, "weight")[0]
@@ -798,7 +802,7 @@ def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature
         ws = _workspace(nbytes, device)
     _call(lib.ppow_head_logprob_backward, "ppow_head_logprob_backward", dev, ctypes.byref(params), h, w, y, l, g,
           None if gh is None else gh.data_ptr(), None if gw is None else gw.data_ptr(), ws.data_ptr(), nbytes, _raw_stream(stream, dev))
-    return gh, gw
+    return (gh, gw, ws) if want_workspace else (gh, gw)
 
 
 def layer_norm(x, weight, bias=None, *, eps=1e-5, checkpoint=False, stream=None) -> dict:

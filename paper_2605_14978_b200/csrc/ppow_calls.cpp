@@ -97,7 +97,7 @@ bool head_params(ppow_head_params &p, const at::Tensor &hidden, const at::Tensor
 }
 
 // Each returns (status, outputs...), or None where the Python path is to be taken.
-py::object head_logprob(const at::Tensor &hidden, const at::Tensor &weight, const at::Tensor &tokens, double temperature)
+py::object head_logprob(const at::Tensor &hidden, const at::Tensor &weight, const at::Tensor &tokens, double temperature, bool want_workspace)
 {
     const Place at(hidden);
     ppow_head_params p;
@@ -107,11 +107,11 @@ py::object head_logprob(const at::Tensor &hidden, const at::Tensor &weight, cons
     const at::Tensor ws = at.scratch(bytes);
     const ppow_status st = lib.head_logprob(&p, hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr<int32_t>(), logp.data_ptr<float>(),
                                             lse.data_ptr<float>(), ws.data_ptr(), bytes, at.stream);
-    return py::make_tuple(status_of(st), to_python(logp), to_python(lse));
+    return py::make_tuple(status_of(st), to_python(logp), to_python(lse), to_python(want_workspace ? ws : at::Tensor()));
 }
 
 py::object head_logprob_backward(const at::Tensor &hidden, const at::Tensor &weight, const at::Tensor &tokens, const at::Tensor &lse,
-                                 const at::Tensor &grad_logp, double temperature, bool want_hidden, bool want_weight)
+                                 const at::Tensor &grad_logp, double temperature, bool want_hidden, bool want_weight, bool want_workspace)
 {
     const Place at(hidden);
     ppow_head_params p;
@@ -125,7 +125,7 @@ py::object head_logprob_backward(const at::Tensor &hidden, const at::Tensor &wei
     const ppow_status st = lib.head_logprob_backward(&p, hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr<int32_t>(),
                                                      lse.data_ptr<float>(), grad_logp.data_ptr<float>(), want_hidden ? gh.data_ptr() : nullptr,
                                                      want_weight ? gw.data_ptr() : nullptr, ws.data_ptr(), bytes, at.stream);
-    return py::make_tuple(status_of(st), to_python(gh), to_python(gw));
+    return py::make_tuple(status_of(st), to_python(gh), to_python(gw), to_python(want_workspace ? ws : at::Tensor()));
 }
 
 bool norm_params(ppow_norm_params &p, const at::Tensor &rows, const at::Tensor &weight, double eps, const Place &at)

@@ -99,6 +99,8 @@ struct HeadRows {
 };
 
 __device__ __forceinline__ void fault(HeadHeader *h, unsigned int bit) { atomicOr(&h->error_flags, bit); }
+// A kernel of this call gave a wait up: its results are not there, and what is made of them is NaN.
+__device__ __forceinline__ bool gave_up(const HeadHeader *h) { return h->error_flags & PPOW_FLAG_DEVICE_TIMEOUT; }
 
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float a, float b)
@@ -719,7 +721,7 @@ __device__ __forceinline__ void epilogue_many(const ProductJob &job, const Exten
             }
         });
     } else {
-        const float out_scale = job.rows.header->out_scale;
+        const float out_scale = gave_up(job.rows.header) ? NAN : job.rows.header->out_scale;
         const int32_t v = x.row + in_tile / HALF_TILE * HALF_TILE;       // the box's first row within the piece
         auto store = [&](int c, uint32_t (&w)[32]) {
             uint32_t o[16];
@@ -1239,6 +1241,7 @@ __global__ void __launch_bounds__(MERGE_THREADS) head_merge_kernel(const MergeJo
         }
         const double ln2 = 0.69314718055994530942;
         z2 *= job.exact_scale;
+        if (gave_up(rows.header)) sum = NAN;
         // the sums' reference was scaled by a rounded number: 6e-8 of a logit of 60 would be in the result undamped
         const double others2 = (double)top * job.rescale + log2(sum);
         if (y >= job.V) {                                // no such token: the sums are whole without it
@@ -1266,6 +1269,7 @@ __global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows ro
     const int32_t units = D / 4, splits = rows.header->splits, live = rows.header->live;
     const size_t split_units = (size_t)(few ? few : (live + TILE - 1) / TILE * TILE) * units;
     const int64_t all = (int64_t)live * units;
+    const bool lost = gave_up(rows.header);
     for (int64_t i = (int64_t)blockIdx.x * FINISH_THREADS + threadIdx.x; i < all; i += (int64_t)gridDim.x * FINISH_THREADS) {
         const int32_t row = (int32_t)(i / units), u = (int32_t)(i % units);
         const float4 *p = reinterpret_cast<const float4 *>(parts) + i;
@@ -1287,7 +1291,7 @@ __global__ void __launch_bounds__(FINISH_THREADS) head_finish_kernel(HeadRows ro
         const float rest = rows.residual[row];
         const float2 w01 = unpack2<BF16>(wy.x), w23 = unpack2<BF16>(wy.y);
         f.x = fmaf(rest, w01.x, f.x), f.y = fmaf(rest, w01.y, f.y), f.z = fmaf(rest, w23.x, f.z), f.w = fmaf(rest, w23.y, f.w);
-        const float k = rows.row_scale[row];
+        const float k = lost ? NAN : rows.row_scale[row];
         reinterpret_cast<uint2 *>(grad_hidden + (size_t)rows.source[row] * D)[u] =
             make_uint2(pack2<BF16>(f.x * k, f.y * k), pack2<BF16>(f.z * k, f.w * k));
     }
@@ -1643,6 +1647,13 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     return PPOW_OK;
 }
 
+// Without tokens nothing is launched that would; a workspace is not needed then.
+ppow_status clear_header(void *workspace, size_t bytes, cudaStream_t stream)
+{
+    if (!workspace || bytes < sizeof(HeadHeader)) return PPOW_OK;
+    return cudaMemsetAsync(workspace, 0, sizeof(HeadHeader), stream) == cudaSuccess ? PPOW_OK : PPOW_ERR_CUDA;
+}
+
 }  // namespace
 }  // namespace ppow
 
@@ -1673,7 +1684,7 @@ extern "C" ppow_status ppow_head_logprob(const ppow_head_params *params, const v
                                          float *logp, float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream)
 {
     if (!params_ok(params)) return PPOW_ERR_INVALID_ARG;
-    if (params->T == 0) return PPOW_OK;
+    if (params->T == 0) return clear_header(workspace, workspace_bytes, (cudaStream_t)cuda_stream);
     if (!hidden || !weight || !tokens || !logp || !lse) return PPOW_ERR_INVALID_ARG;
     if ((uintptr_t)hidden % 2 || (uintptr_t)weight % 16 || (uintptr_t)tokens % 4 || (uintptr_t)logp % 4 || (uintptr_t)lse % 4)
         return PPOW_ERR_INVALID_ARG;
@@ -1692,7 +1703,7 @@ extern "C" ppow_status ppow_head_logprob_backward(const ppow_head_params *params
     if (params->T == 0) {
         if (grad_weight && cudaMemsetAsync(grad_weight, 0, (size_t)params->V * params->D * 2, (cudaStream_t)cuda_stream) != cudaSuccess)
             return PPOW_ERR_CUDA;
-        return PPOW_OK;
+        return clear_header(workspace, workspace_bytes, (cudaStream_t)cuda_stream);
     }
     if ((!grad_hidden && !grad_weight) || !hidden || !weight || !tokens || !lse || !grad_logp) return PPOW_ERR_INVALID_ARG;
     if ((uintptr_t)hidden % 2 || (uintptr_t)weight % 16 || (uintptr_t)tokens % 4 || (uintptr_t)lse % 4 || (uintptr_t)grad_logp % 4)
