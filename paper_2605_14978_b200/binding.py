@@ -9,6 +9,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import warnings
 from typing import Optional
 
 import torch
@@ -167,19 +168,31 @@ def load_library():
     return lib
 
 
+class _NoCalls:
+    """In the place of the extension module where that does not load: every call goes the wrappers' Python way."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
 _calls = None
 CALLED = ("ppow_head_workspace_bytes", "ppow_head_logprob", "ppow_head_logprob_backward", "ppow_layer_norm",
           "ppow_layer_norm_workspace_bytes", "ppow_layer_norm_backward", "ppow_pack_activation", "ppow_unpack_activation")
 
 
 def _bind_calls(lib) -> None:
-    """Hand the addresses of the training-end entry points to the extension module that marshals their calls."""
+    """Hand the addresses of the training-end entry points to the extension module that marshals their calls.  A module that is
+    missing or was built against another torch costs those calls 5 to 15 us each and nothing else."""
     global _calls
     try:
         from . import _calls as module
+        if module.torch_version != torch.__version__:
+            raise ImportError("built against torch %s, this is %s" % (module.torch_version, torch.__version__))
+        module.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in CALLED})
     except ImportError as e:
-        raise RuntimeError("_calls.so is missing or does not load (%s): build it with `python -m paper_2605_14978_b200.build`" % e)
-    module.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in CALLED})
+        warnings.warn("_calls.so does not load (%s): training-end calls are marshalled in Python, which is slower; build it with "
+                      "`python -m paper_2605_14978_b200.build`" % e, RuntimeWarning, stacklevel=3)
+        module = _NoCalls()
     _calls = module
 
 

@@ -8,6 +8,7 @@ import shutil
 import subprocess
 import sys
 import tempfile
+import threading
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -33,21 +34,34 @@ def is_stale(lib: str = LIB) -> bool:
     return any(os.path.getmtime(f) > t for f in _deps())
 
 
+def _torch_mark() -> str:
+    """What _calls.so carries to say which torch it was built against."""
+    import torch
+    return "ppow_calls for torch " + torch.__version__
+
+
+def calls_are_stale() -> bool:
+    """Missing, older than its sources, or built against another torch than the installed one."""
+    deps = [os.path.join(CSRC, "ppow_calls.cpp"), os.path.join(ROOT, "include", "ppow.h")]
+    if not os.path.exists(CALLS) or any(os.path.getmtime(f) > os.path.getmtime(CALLS) for f in deps):
+        return True
+    with open(CALLS, "rb") as f:
+        return _torch_mark().encode() + b"\0" not in f.read()
+
+
 def build_calls(force: bool = False) -> str:
     """Compile the extension module that marshals the training-end calls, against the torch that is installed."""
-    src = os.path.join(CSRC, "ppow_calls.cpp")
-    deps = [src, os.path.join(ROOT, "include", "ppow.h")]
-    if not force and os.path.exists(CALLS) and all(os.path.getmtime(f) <= os.path.getmtime(CALLS) for f in deps):
+    if not force and not calls_are_stale():
         return CALLS
     import sysconfig
     import torch
     at = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(shutil.which(os.environ.get("NVCC", "nvcc")) or "/usr/local/cuda/bin/nvcc"))
-    tmp = CALLS + ".tmp.%d" % os.getpid()
+    tmp = CALLS + ".tmp.%d.%d" % (os.getpid(), threading.get_ident())
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
-           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), '-DPPOW_TORCH_MARK="%s"' % _torch_mark(),
            "-I" + os.path.join(at, "include"), "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
-           "-I" + os.path.join(cuda, "include"), "-I" + sysconfig.get_path("include"), src, "-o", tmp,
+           "-I" + os.path.join(cuda, "include"), "-I" + sysconfig.get_path("include"), os.path.join(CSRC, "ppow_calls.cpp"), "-o", tmp,
            "-L" + os.path.join(at, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
@@ -60,9 +74,13 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False, tim
     """Compile every .cu under csrc/ into one shared library for sm_100a.  ``checked``: the bounds-checked
     build (every kernel-computed index tested before use, failures counted and skipped, never trapped)."""
     lib = LIB_CHECKED if checked else LIB_TIMELINE if timeline else LIB
-    build_calls(force and lib == LIB)
-    if not force and not is_stale(lib):
-        return lib
+    if force or is_stale(lib):
+        _build_library(lib, verbose, checked, timeline)
+    build_calls(force and lib == LIB)        # behind the library, which does without it
+    return lib
+
+
+def _build_library(lib: str, verbose: bool, checked: bool, timeline: bool) -> None:
     nvcc = os.environ.get("NVCC", "nvcc")
     flags = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-Xcompiler", "-fPIC"]
     flags += ["-Xptxas", "-v"] if verbose else []
@@ -82,7 +100,6 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False, tim
         tmp = lib + ".tmp.%d" % os.getpid()
         run([nvcc] + flags + ["-shared", "-o", tmp] + outs)
     os.replace(tmp, lib)
-    return lib
 
 
 if __name__ == "__main__":

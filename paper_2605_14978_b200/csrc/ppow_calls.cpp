@@ -12,6 +12,8 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/utils/pybind.h>
 
+#include <string>
+
 #include "../../include/ppow.h"
 
 namespace py = pybind11;
@@ -218,6 +220,8 @@ template <typename... Args> auto guarded(py::object (*f)(Args...))
 
 PYBIND11_MODULE(_calls, m)
 {
+    const std::string mark = PPOW_TORCH_MARK;        // "ppow_calls for torch <version>"
+    m.attr("torch_version") = mark.substr(mark.rfind(' ') + 1);
     m.def("bind", &bind);
     m.def("head_logprob", guarded(&head_logprob));
     m.def("head_logprob_backward", guarded(&head_logprob_backward));
