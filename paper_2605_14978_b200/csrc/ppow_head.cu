@@ -47,13 +47,19 @@ enum Product {
 };
 
 // Steps that a product is summed over in Tensor Memory before the sum moves on to registers: the tensor cores' additions cut off
-// what does not fit.  Logits of the forward pass: over 256 products (4096 wide) that left lse off by 3e-6; 16 steps leave 7e-7 and
-// cost a large batch 3.6 % (8: 8 %), with few tokens 4 are free.  dW: its sum runs over the tokens, and where its terms have one sign
-// (every softmax's has, so the states' mean is enough) each 65536 of them took 4e-4 off it, of 2^20 0.7 %; with parts of 8192 tokens
-// it is under 1e-4.  (Gradient of 262144 x 1024 x 4096: 12.5 ms either way.)
-template <int PRODUCT, int N> __host__ __device__ constexpr int sum_steps()
+// what does not fit, and logp and lse show it (with 16 steps 1.4e-6 of logp in bf16, twice that in f16; with 4 a quarter).
+//   Logits of the forward pass: up to 1024 wide half of the steps, then a third, 4 to 16; few tokens 8 at most, or 4.  That keeps
+//   logp about as exact as a float32 product has it: 300 tokens x 1024 in bf16 at T = 0.7 1.2e-6 (in one sum 2.1e-6, by a float32
+//   product 0.8e-6), and costs 2048 x 1024 x 32000 112 -> 119 us, x 2048 214 -> 220; 4096 wide it is 16 steps, 3.6 % (8: 8 %).
+//   dW: its sum runs over the tokens, and where its terms have one sign (every softmax's has, so the states' mean is enough) each
+//   65536 of them took 4e-4 off it, of 2^20 0.7 %; with parts of 8192 tokens it is under 1e-4.  (Gradient of 262144 x 1024 x 4096:
+//   12.5 ms either way.)
+constexpr int32_t WEIGHT_PART_STEPS = 128;
+inline int32_t logit_part_steps(int32_t width, int32_t columns)
 {
-    return PRODUCT == GRAD_WEIGHT ? 128 : N == 256 ? 16 : N == 128 ? 8 : 4;
+    const int32_t steps = (width + BK - 1) / BK, share = steps <= 16 ? (steps + 1) / 2 : (steps + 2) / 3;
+    const int32_t most = columns == 256 ? 16 : columns == 128 ? 8 : 4;
+    return share < 4 ? 4 : share < most ? share : most;
 }
 // Tiles of 16-bit results leave through shared memory: a box of 128 rows x 64 columns for each half of the columns.
 constexpr uint32_t BOX_BYTES = HALF_TILE * 128;
@@ -66,7 +72,7 @@ constexpr int GATHER_THREADS = 256, EARLY = 4;
 constexpr int GATHER_ROWS_MAX = 1024, GATHER_CTAS = 1024;
 constexpr size_t HEADER_BYTES = 256;
 constexpr size_t DZ_BYTES = 512u << 20;      // a piece of dz holds at most this much
-constexpr int32_t PIECE_TILES = 1024;        // and this many vocabulary tiles: dh is summed over a piece (see sum_steps)
+constexpr int32_t PIECE_TILES = 1024;        // and this many vocabulary tiles: dh is summed over a piece (see below)
 constexpr int32_t MAX_TOKENS = 1 << 20, MAX_VOCAB = 1 << 22, MAX_WIDTH = 1 << 16;
 
 // First bytes of the workspace; error_flags sits where ppow_read_error_flags looks for it.
@@ -508,6 +514,7 @@ struct ProductJob {
     float scale;            // log2(e) / temperature
     int32_t D, V;
     int32_t tokens;         // GRAD_WEIGHT: rows at most, masked ones with them
+    int32_t part_steps;     // LOGITS_SUM, GRAD_WEIGHT: steps of a part of the sum
     int32_t v0, columns;    // the piece: vocabulary entries v0 .. v0 + columns - 1
     int32_t v_tiles, d_tiles;
     int32_t piece;          // row length of dz
@@ -573,9 +580,9 @@ __device__ __forceinline__ Tile tile_at(const ProductJob &job, const Extent &e, 
 
 // Accumulators that a tile's sum passes through, one after the other.  The issuing thread and the epilogue warps both count by
 // it: every tile takes one at least, so that the two sides agree on buffer and phase whatever its steps are.
-template <int PRODUCT, int N, bool PARTS> __device__ __forceinline__ int32_t part_count(const Tile &x)
+template <bool PARTS> __device__ __forceinline__ int32_t part_count(const ProductJob &job, const Tile &x)
 {
-    return PARTS ? max(1, (x.k1 - x.k0 + sum_steps<PRODUCT, N>() - 1) / sum_steps<PRODUCT, N>()) : 1;
+    return PARTS ? max(1, (x.k1 - x.k0 + job.part_steps - 1) / job.part_steps) : 1;
 }
 
 // ---- epilogues: one warp, 32 rows of the tile's accumulator (its Tensor Memory lanes), half of the columns --------
@@ -1039,10 +1046,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
             bool ok = true;
             for (int64_t t = pair; t < tiles && ok; t += pairs) {
                 const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
-                const int32_t parts = part_count<PRODUCT, N, PARTS>(x);
+                const int32_t parts = part_count<PARTS>(job, x);
                 [[maybe_unused]] const TokenRows rows = tile_rows<REMAINDERS>(job, tiles, t, t);
                 for (int32_t part = 0; part < parts && ok; ++part, ++acc) {
-                    const int32_t k0 = PARTS ? x.k0 + part * sum_steps<PRODUCT, N>() : x.k0, k1 = PARTS ? min(k0 + sum_steps<PRODUCT, N>(), x.k1) : x.k1;
+                    const int32_t k0 = PARTS ? x.k0 + part * job.part_steps : x.k0, k1 = PARTS ? min(k0 + job.part_steps, x.k1) : x.k1;
                     const uint32_t b = acc & 1u, d = tmem + b * TILE;
                     ok = mbar_wait_ns(acc_empty(b), ((acc >> 1) & 1u) ^ 1u);
                     tcgen05_fence_after();
@@ -1106,7 +1113,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                     own.target = job.rows.target[x.row + in_tile];
                 }
             }
-            const int32_t parts = part_count<PRODUCT, N, PARTS>(x);
+            const int32_t parts = part_count<PARTS>(job, x);
             for (int32_t part = 0; part < parts; ++part, ++acc) {
                 const uint32_t b = acc & 1u;
                 // all four warps of a half go on or none does: they meet at barriers further down
@@ -1456,7 +1463,7 @@ bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap 
 {
     const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
     // one part is a kernel of its own: the loop over parts costs the forward pass a third (2048 x 128 x 128256: 106 us, with it 140)
-    if (in_parts<PRODUCT>() && (PRODUCT == LOGITS_SUM ? job.D : job.tokens) > sum_steps<PRODUCT, N>() * BK)
+    if (in_parts<PRODUCT>() && (PRODUCT == LOGITS_SUM ? job.D : job.tokens) > job.part_steps * BK)
         return launch_after(head_product_kernel<PRODUCT, BF16, N, in_parts<PRODUCT>()>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, rest, job);
     return launch_after(head_product_kernel<PRODUCT, BF16, N, false>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, rest, job);
 }
@@ -1553,6 +1560,7 @@ ppow_status forward(const ppow_head_params *p, const void *hidden, const void *w
     job.D = p->D;
     job.V = job.columns = p->V;
     job.direct = direct ? p->T : 0;
+    job.part_steps = logit_part_steps(p->D, L.columns);
     job.v_tiles = L.v_tiles;
     job.d_tiles = L.d_tiles;
     job.parts = L.few ? 8 * (L.v_tiles < pairs ? L.v_tiles : pairs) : L.parts;
@@ -1624,6 +1632,7 @@ ppow_status backward(const ppow_head_params *p, const void *hidden, const void *
     job.d_tiles = L.d_tiles;
     job.piece = L.piece;
     job.tokens = p->T;
+    job.part_steps = WEIGHT_PART_STEPS;
     job.dz = dz;
     job.grad_rows = (float *)(ws + L.grad_rows);
     const int64_t row_tiles = (L.padded + TILE - 1) / TILE;
