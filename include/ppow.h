@@ -307,7 +307,7 @@ ppow_status ppow_head_logprob(const ppow_head_params *params, const void *hidden
  * dz is rounded to the storage type (a relative error of at most half a step per term, of the size of the operands' own
  * rounding); for PPOW_F16 each row of it is brought near 2^15 by a power of two first, which is undone after the sums.  What the
  * rounding of a row's largest term, the one at its token, leaves over is added to grad_hidden and grad_weight in float32.
- * The sums are float32 in a fixed order: equal inputs give equal results.
+ * The sums are float32 in an order that follows from the inputs and the device: equal inputs give equal results on it.
  *   hidden, weight, tokens   as above.  Rows with a negative token, a token >= V (which sets PPOW_FLAG_TOKEN_RANGE) or
  *                            grad_logp == 0 are masked: their gradient is 0 and they add nothing to grad_weight.
  *   lse          device, [T] float32, as written by ppow_head_logprob (not read at masked rows)
@@ -328,7 +328,7 @@ ppow_status ppow_head_logprob_backward(const ppow_head_params *params, const voi
  * Layer normalisation of the drafter's hidden states in front of its head, and its gradient:
  *     y = (x - mean) * rstd * weight + bias         rstd = 1 / sqrt(var + eps), var the population variance of the row
  * and 8-bit checkpoints of activations, so that what the backward pass needs of the forward pass takes half the memory.
- * Statistics and sums are float32; sums over rows are added up in a fixed order.
+ * Statistics and sums are float32; sums over rows are added up in an order that is fixed for a device and a build of the library.
  */
 typedef struct {
     int32_t R;              /* rows, 0 .. 2^28 */

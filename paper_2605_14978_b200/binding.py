@@ -752,7 +752,9 @@ def select_windows(score, n_keep: int, want_mask: bool = False, stream=None):
     return (sel, mask) if want_mask else sel
 
 
-# The wrappers below go through the extension module first, which marshals a call in a fifth of the time and answers None where
+# The wrappers below are plain calls outside autograd: what they return is detached, whatever their inputs require, and each gradient
+# has a call of its own.
+# They go through the extension module first, which marshals a call in a fifth of the time and answers None where
 # something is not as it should be, or where the call is for another stream or device: the rest of the wrapper is for those.
 # It hands the addresses of what it has just allocated straight to the library.
 
@@ -774,7 +776,8 @@ def _workspace(nbytes: int, dev) -> torch.Tensor:
 
 
 def head_logprob(hidden, weight, tokens, *, temperature=1.0, want_workspace=False, stream=None) -> dict:
-    """Allocate outputs and workspace, run ppow_head_logprob; returns logp and lse, both [T] float32.  With ``want_workspace`` also
+    """Allocate outputs and workspace, run ppow_head_logprob; returns logp and lse, both [T] float32, outside autograd (the gradient is
+    head_logprob_backward's).  With ``want_workspace`` also
     ``_workspace``, whose error word ppow_read_error_flags reads (tokens behind the vocabulary, a device wait that ran out); it is not
     kept otherwise, because it holds 8 bytes for every 128 logits and a copy of the rows."""
     if stream is None:
@@ -820,7 +823,7 @@ def head_logprob_backward(hidden, weight, tokens, lse, grad_logp, *, temperature
 
 def layer_norm(x, weight, bias=None, *, eps=1e-5, checkpoint=False, stream=None) -> dict:
     """Allocate outputs and run ppow_layer_norm on ``x`` [R, D]; returns y, mean, rstd and, with ``checkpoint``, the 8-bit form of
-    ``x`` as packed and scale."""
+    ``x`` as packed and scale, all outside autograd (the gradient is layer_norm_backward's)."""
     if stream is None:
         got = _quick().layer_norm(x, weight, bias, eps, checkpoint)
         if got is not None:
@@ -879,7 +882,7 @@ def _alloc_packed(R: int, D: int, device):
 
 
 def pack_activation(x, stream=None):
-    """Allocate and run ppow_pack_activation; returns (packed, scale)."""
+    """Allocate and run ppow_pack_activation; returns (packed, scale), outside autograd."""
     if stream is None:
         got = _quick().pack_activation(x)
         if got is not None:
@@ -895,7 +898,7 @@ def pack_activation(x, stream=None):
 
 
 def unpack_activation(packed, scale, dtype=torch.bfloat16, stream=None):
-    """Allocate and run ppow_unpack_activation; returns the restored activation in ``dtype``."""
+    """Allocate and run ppow_unpack_activation; returns the restored activation in ``dtype``, outside autograd."""
     if stream is None and dtype in DTYPE_CODES:
         got = _quick().unpack_activation(packed, scale, DTYPE_CODES[dtype])
         if got is not None:

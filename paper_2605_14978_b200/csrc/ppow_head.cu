@@ -29,7 +29,7 @@ constexpr int TILE = 256;            // rows and columns of an output tile (a pa
 constexpr int HALF_TILE = 128;       // rows of A that one CTA holds
 constexpr int BK = 64;               // products' inner step per pipeline stage: one 128-byte swizzle row
 constexpr uint32_t A_BYTES = HALF_TILE * BK * 2;           // 16 KB
-constexpr int MMA_THREADS = 320;     // producer warp, issuing warp, eight epilogue warps
+constexpr int MMA_THREADS = 320;     // producer warp, issuing warp, eight epilogue warps; for dW one more, for the remainders
 constexpr int PAIRS = 74;            // pairs of SMs that the shares of an inner axis are planned for
 constexpr int MAX_PAIRS = 128;       // pairs that a launch uses at most
 
@@ -65,7 +65,7 @@ inline int32_t logit_part_steps(int32_t width, int32_t columns)
 constexpr uint32_t BOX_BYTES = HALF_TILE * 128;
 template <int N> __host__ __device__ constexpr size_t mma_smem()
 {
-    return 1024 + (size_t)stage_count<N>() * stage_bytes<N>() + (N == 256 ? 2 * BOX_BYTES : 0) + 256;
+    return 1024 + (size_t)stage_count<N>() * stage_bytes<N>() + (N == 256 ? 2 * BOX_BYTES : 0) + 512;
 }
 
 constexpr int GATHER_THREADS = 256, EARLY = 4;
@@ -859,11 +859,22 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
 // dz at its token is most of the row of dW that it falls into, and rounded alone it is off by as much as the result's own rounding
 // (4096 x 4096 x 128256 bf16: 0.0023 of dW, 0.0017 without that error).  What the rounding left over is added as further steps of the
 // tile's sum: the tile's rows lie side by side, and for 64 of them the operand in dz's place is zero but for one entry each, their
-// remainders.  The producer warp writes it into the stage, where TMA brings the rows' hidden states beside it, in slices of the 16
+// remainders.  A warp of its own writes it into the stage (done by the producer warp it held the copies up, and the tensor pipe was 79 %
+// active at 2048 x 4096 x 32000, not 95), where TMA brings the rows' hidden states beside it, in slices of the 16
 // rows that one instruction multiplies: a tile has few rows more often than not (552 tokens x 776 x 68450: 236 us with whole steps,
 // 230 like this, 217 without remainders; 4096 x 4096 x 128256: no difference).
 constexpr uint32_t SLICE_BYTES = 16 * 128;
-__device__ __forceinline__ uint32_t remainder_slices(int32_t rows) { return (uint32_t)(rows + 15) / 16; }
+// A step takes the 64 rows from `row` on, of those of the tile.  The hidden states read with them end with the last row tile at the
+// latest, because behind it the workspace holds anything: `row` is row `skip` of what is read.
+struct RemainderStep {
+    int32_t box_row, skip;
+    uint32_t slices;
+};
+__device__ __forceinline__ RemainderStep remainder_step(const Extent &e, TokenRows rows, int32_t row)
+{
+    const int32_t box_row = min(row, e.row_tiles * TILE - BK);
+    return {box_row, row - box_row, (uint32_t)(row - box_row + min(BK, rows.end - row) + 15) / 16};
+}
 template <bool REMAINDERS>
 __device__ __forceinline__ TokenRows tile_rows(const ProductJob &job, int64_t tiles, int64_t t, int64_t other)     // of tile t, if there is one
 {
@@ -871,30 +882,37 @@ __device__ __forceinline__ TokenRows tile_rows(const ProductJob &job, int64_t ti
     const int2 r = *reinterpret_cast<const int2 *>(job.rows.rows_of + job.v0 / TILE + (int32_t)(t < tiles ? t : other) / job.d_tiles);
     return {r.x, r.y};
 }
-// `slices` slices of the half tile from vocabulary entry `base` on, rows by 128 entries, row `from` of the tile's in row `skip`, laid
-// out as TMA would: blocks of 64 entries, a row 128 bytes, its 16-byte unit u at u ^ (row & 7).
-template <bool BF16>
-__device__ __forceinline__ void put_remainders(const ProductJob &job, uint32_t a, TokenRows rows, int32_t from, int32_t skip, uint32_t slices,
-                                               int32_t base)
+struct RemainderRows {
+    int32_t token[BK / 32];          // of rows `from` + lane + 32 i, negative: none
+    float rest[BK / 32];
+};
+__device__ __forceinline__ RemainderRows remainder_rows(const ProductJob &job, TokenRows rows, int32_t from)
+{
+    RemainderRows r;
+#pragma unroll
+    for (int i = 0; i < BK / 32; ++i) {
+        const int32_t row = from + 32 * i + (int32_t)(threadIdx.x & 31);
+        r.token[i] = row < rows.end ? job.rows.token[row] : -1;
+        r.rest[i] = row < rows.end ? job.rows.residual[row] : 0.0f;
+    }
+    return r;
+}
+// A step's slices of the half tile from vocabulary entry `base` on, rows by 128 entries, laid out as TMA would: blocks of 64 entries, a
+// row 128 bytes, its 16-byte unit u at u ^ (row & 7).
+template <bool BF16> __device__ __forceinline__ void put_remainders(uint32_t a, const RemainderRows &r, const RemainderStep &step, int32_t base)
 {
     const uint32_t lane = threadIdx.x & 31;
-    int32_t row = from + (int32_t)lane;
-    const int32_t end = min(rows.end, from + BK);
-    int32_t token = row < end ? job.rows.token[row] : -1;
-    float rest = row < end ? job.rows.residual[row] : 0.0f;
 #pragma unroll 4
-    for (uint32_t i = lane; i < slices * (SLICE_BYTES / 16); i += 32) {
+    for (uint32_t i = lane; i < step.slices * (SLICE_BYTES / 16); i += 32) {
         store_shared16(a + 16 * i, 0u, 0u, 0u, 0u);
         store_shared16(a + BK * 128 + 16 * i, 0u, 0u, 0u, 0u);
     }
     __syncwarp();
-#pragma unroll 1
-    while (row < end) {
-        const uint32_t k = skip + row - from, m = (uint32_t)(token - base);
-        if (m < HALF_TILE && PPOW_CHECK(k < BK, 510, nullptr))
-            store_shared2(a + m / 64 * (BK * 128) + k * 128 + ((m % 64 / 8 ^ (k & 7)) << 4) + m % 8 * 2, pack2<BF16>(rest, 0.0f));
-        row += 32;
-        if (row < end) token = job.rows.token[row], rest = job.rows.residual[row];
+#pragma unroll
+    for (int i = 0; i < BK / 32; ++i) {
+        const uint32_t k = step.skip + 32 * i + lane, m = (uint32_t)(r.token[i] - base);
+        if (r.token[i] >= 0 && m < HALF_TILE && PPOW_CHECK(k < BK, 510, nullptr))
+            store_shared2(a + m / 64 * (BK * 128) + k * 128 + ((m % 64 / 8 ^ (k & 7)) << 4) + m % 8 * 2, pack2<BF16>(r.rest[i], 0.0f));
     }
     fence_for_copy_engine();
     __syncwarp();
@@ -902,8 +920,9 @@ __device__ __forceinline__ void put_remainders(const ProductJob &job, uint32_t a
 
 // Persistent: one CTA per SM, pair p takes tiles p, p + pairs, ...  Warp 0 keeps the operand ring full, one thread of
 // the leader's warp 1 issues the products into one of two accumulators, warps 2..9 read the other one out.
+template <int PRODUCT> __host__ __device__ constexpr int mma_threads() { return MMA_THREADS + (PRODUCT == GRAD_WEIGHT ? 32 : 0); }
 template <int PRODUCT, bool BF16, int N, bool PARTS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(mma_threads<PRODUCT>(), 1)
     head_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                         const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_rest, const ProductJob job)
 {
@@ -922,6 +941,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     auto empty = [&](uint32_t s) { return bars + 8 * (STAGES + s); };
     auto acc_full = [&](uint32_t b) { return bars + 8 * (2 * STAGES + b); };
     auto acc_empty = [&](uint32_t b) { return bars + 8 * (2 * STAGES + 2 + b); };   // the leader's count, for both CTAs
+    // Steps of remainders: the producer warp, which passes every step of the ring, says that the step's stage is free; the leader's
+    // count of both CTAs says that the remainders are written.  The producer is no more steps ahead of the products than the ring has
+    // stages, so of more barriers than that, taken by turns, none completes a second time before the first has been waited for.
+    constexpr uint32_t TURNS = 8;
+    static_assert(STAGES < TURNS || !REMAINDERS, "a barrier must not complete twice before it is waited for");
+    [[maybe_unused]] auto free_stage = [&](uint32_t step) { return bars + 8 * (2 * STAGES + 5 + step % TURNS); };
+    [[maybe_unused]] auto written = [&](uint32_t step) { return bars + 8 * (2 * STAGES + 5 + TURNS + step % TURNS); };
     const uint32_t tmem_slot = bars + 8 * (2 * STAGES + 4);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -933,13 +959,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
         prefetch_tensor_map(&map_a);
         prefetch_tensor_map(&map_b);
         for (uint32_t s = 0; s < STAGES; ++s) {
-            mbar_init(full(s), REMAINDERS ? 2 : 1);
+            mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
         for (uint32_t b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
             mbar_init(acc_empty(b), 16);     // eight epilogue warps of each CTA
         }
+        if (REMAINDERS)
+            for (uint32_t i = 0; i < TURNS; ++i) {
+                mbar_init(free_stage(i), 1);
+                mbar_init(written(i), 2);
+            }
         mbar_init_fence();
     }
     if (warp == 1) tmem_alloc_pair(tmem_slot);
@@ -970,24 +1001,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
     const int64_t tiles = tile_count<PRODUCT>(job, e);
 
     if (warp == 0) {
-        if (lane == 0 || REMAINDERS) {
+        if (lane == 0) {
             uint32_t it = 0;
+            [[maybe_unused]] uint32_t step = 0;              // of remainders
             bool ok = true;
             [[maybe_unused]] TokenRows rows = tile_rows<REMAINDERS>(job, tiles, pair, pair);
             for (int64_t t = pair; t < tiles && ok; t += pairs) {
                 const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
                 const int32_t n = x.col + (int32_t)rank * (N / 2);
                 [[maybe_unused]] const TokenRows next = tile_rows<REMAINDERS>(job, tiles, t + pairs, t);
-                uint32_t step = it;
-                for (int32_t k = x.k0; k < x.k1 && ok && lane == 0; ++k, ++step) {
-                    const uint32_t s = step % STAGES, phase = (step / STAGES) & 1u;
+                for (int32_t k = x.k0; k < x.k1 && ok; ++k, ++it) {
+                    const uint32_t s = it % STAGES, phase = (it / STAGES) & 1u;
                     ok = mbar_wait_ns(empty(s), phase ^ 1u);
                     if (!ok) break;
+                    if (rank == 0) mbar_arrive_expect_tx(full(s), 2 * STAGE_BYTES);
                     const uint32_t bar = peer_addr(full(s), 0);
-                    if (rank == 0)
-                        mbar_arrive_expect_tx(full(s), 2 * STAGE_BYTES);
-                    else if (REMAINDERS)
-                        mbar_arrive_cluster(bar);
                     const uint32_t a = smem + s * STAGE_BYTES, b = a + A_BYTES;
                     const int32_t m = x.row + (int32_t)rank * HALF_TILE;
                     // the vocabulary is the inner axis of dh: its coordinate in W starts at the piece
@@ -1005,44 +1033,58 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                         tma_load_pair(b + BLOCK_BYTES, &map_b, n + 64, k_weight, bar);
                     }
                 }
-                it += x.k1 - x.k0;
                 if constexpr (REMAINDERS) {
-                    ok = __shfl_sync(0xffffffffu, ok, 0);
-                    for (int32_t row = rows.first; row < rows.end && ok; row += BK, ++it) {
-                        const uint32_t s = it % STAGES, a = smem + s * STAGE_BYTES, b = a + A_BYTES;
-                        // the hidden states read end with the last row tile at the latest: behind it the workspace holds anything
-                        const int32_t box_row = min(row, e.row_tiles * TILE - BK), skip = row - box_row;
-                        const uint32_t slices = remainder_slices(skip + min(BK, rows.end - row)), bar = peer_addr(full(s), 0);
-                        if (lane == 0) {
-                            ok = mbar_wait_ns(empty(s), ((it / STAGES) & 1u) ^ 1u);
-#pragma unroll 1
-                            for (uint32_t q = 0; q < slices && ok; ++q) {
-                                tma_load_pair(b + q * SLICE_BYTES, &map_rest, n, box_row + 16 * q, bar);
-                                tma_load_pair(b + BLOCK_BYTES + q * SLICE_BYTES, &map_rest, n + 64, box_row + 16 * q, bar);
-                            }
-                        }
-                        ok = __shfl_sync(0xffffffffu, ok, 0);
+                    for (int32_t row = rows.first; row < rows.end && ok; row += BK, ++it, ++step) {
+                        const uint32_t s = it % STAGES, b = smem + s * STAGE_BYTES + A_BYTES;
+                        ok = mbar_wait_ns(empty(s), ((it / STAGES) & 1u) ^ 1u);
                         if (!ok) break;
-                        put_remainders<BF16>(job, a, rows, row, skip, slices, job.v0 + x.row + (int32_t)rank * HALF_TILE);
-                        if (lane == 0) {
-                            if (rank == 0)
-                                mbar_arrive_expect_tx(full(s), slices * (2 * 2 * SLICE_BYTES));
-                            else
-                                mbar_arrive_release_cluster(bar);
+                        mbar_arrive(free_stage(step));
+                        const RemainderStep r = remainder_step(e, rows, row);
+                        if (rank == 0) mbar_arrive_expect_tx(full(s), r.slices * (2 * 2 * SLICE_BYTES));
+                        const uint32_t bar = peer_addr(full(s), 0);
+#pragma unroll 1
+                        for (uint32_t q = 0; q < r.slices; ++q) {
+                            tma_load_pair(b + q * SLICE_BYTES, &map_rest, n, r.box_row + 16 * q, bar);
+                            tma_load_pair(b + BLOCK_BYTES + q * SLICE_BYTES, &map_rest, n + 64, r.box_row + 16 * q, bar);
                         }
                     }
                     rows = next;
                 }
             }
             // the leader's last commits land on this CTA's barriers: stay until they have
-            if (lane == 0) {
-                for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it && ok; ++j) ok = mbar_wait_ns(empty(j % STAGES), (j / STAGES) & 1u);
-                if (!ok) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
+            for (uint32_t j = it > STAGES ? it - STAGES : 0; j < it && ok; ++j) ok = mbar_wait_ns(empty(j % STAGES), (j / STAGES) & 1u);
+            if (!ok) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
+        }
+    } else if (REMAINDERS && warp == MMA_THREADS / 32) {
+        if constexpr (REMAINDERS) {
+            uint32_t it = 0, step = 0;
+            bool ok = true;
+            TokenRows rows = tile_rows<REMAINDERS>(job, tiles, pair, pair);
+            RemainderRows ahead = remainder_rows(job, rows, rows.first);
+            for (int64_t t = pair; t < tiles && ok; t += pairs) {
+                const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
+                const TokenRows next = tile_rows<REMAINDERS>(job, tiles, t + pairs, t);
+                it += x.k1 - x.k0;
+                for (int32_t row = rows.first; row < rows.end && ok; row += BK, ++it, ++step) {
+                    const uint32_t s = it % STAGES;
+                    const RemainderRows here = ahead;
+                    if (row + BK < rows.end) ahead = remainder_rows(job, rows, row + BK);
+                    if (lane == 0) ok = mbar_wait_ns(free_stage(step), (step / TURNS) & 1u);
+                    ok = __shfl_sync(0xffffffffu, ok, 0);
+                    __syncwarp();
+                    if (!ok) break;
+                    put_remainders<BF16>(smem + s * STAGE_BYTES, here, remainder_step(e, rows, row), job.v0 + x.row + (int32_t)rank * HALF_TILE);
+                    if (lane == 0) mbar_arrive_release_cluster(peer_addr(written(step), 0));
+                }
+                rows = next;
+                ahead = remainder_rows(job, rows, rows.first);
             }
+            if (!ok && lane == 0) fault(header, PPOW_FLAG_DEVICE_TIMEOUT);
         }
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
             uint32_t it = 0, acc = 0;
+            [[maybe_unused]] uint32_t step = 0;              // of remainders
             bool ok = true;
             for (int64_t t = pair; t < tiles && ok; t += pairs) {
                 const Tile x = tile_at<PRODUCT, FEW>(job, e, t);
@@ -1067,16 +1109,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMA_THREADS, 1)
                         mma_commit_pair(empty(s));
                     }
                     if constexpr (REMAINDERS) {
-                        for (int32_t row = part + 1 < parts ? rows.end : rows.first; row < rows.end && ok; row += BK, ++it) {
+                        for (int32_t row = part + 1 < parts ? rows.end : rows.first; row < rows.end && ok; row += BK, ++it, ++step) {
                             const uint32_t s = it % STAGES;
-                            // the other CTA's half was written by its threads
-                            ok = mbar_wait_ns(full(s), (it / STAGES) & 1u) && mbar_acquire_cluster(full(s), (it / STAGES) & 1u);
+                            ok = mbar_wait_ns(full(s), (it / STAGES) & 1u) && mbar_wait_ns(written(step), (step / TURNS) & 1u) &&
+                                 mbar_acquire_cluster(written(step), (step / TURNS) & 1u);
                             if (!ok) break;
                             tcgen05_fence_after();
                             const uint32_t a = smem + s * STAGE_BYTES;
                             const uint64_t da = operand_descriptor(a, A_K, BLOCK_BYTES), db = operand_descriptor(a + A_BYTES, B_K, BLOCK_BYTES);
-                            const int32_t skip = row - min(row, e.row_tiles * TILE - BK);
-                            const uint32_t slices = remainder_slices(skip + min(BK, rows.end - row));
+                            const uint32_t slices = remainder_step(e, rows, row).slices;
 #pragma unroll 1
                             for (uint32_t q = 0; q < slices; ++q)
                                 mma_pair(d, da + (uint64_t)(q * SLICE_BYTES >> 4), db + (uint64_t)(q * SLICE_BYTES >> 4), INSTRUCTION, true);
@@ -1464,8 +1505,8 @@ bool launch_tiles(const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap 
     const int n = (int)(most_tiles < pairs ? most_tiles : pairs);
     // one part is a kernel of its own: the loop over parts costs the forward pass a third (2048 x 128 x 128256: 106 us, with it 140)
     if (in_parts<PRODUCT>() && (PRODUCT == LOGITS_SUM ? job.D : job.tokens) > job.part_steps * BK)
-        return launch_after(head_product_kernel<PRODUCT, BF16, N, in_parts<PRODUCT>()>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, rest, job);
-    return launch_after(head_product_kernel<PRODUCT, BF16, N, false>, 2 * n, MMA_THREADS, mma_smem<N>(), stream, a, b, out, rest, job);
+        return launch_after(head_product_kernel<PRODUCT, BF16, N, in_parts<PRODUCT>()>, 2 * n, mma_threads<PRODUCT>(), mma_smem<N>(), stream, a, b, out, rest, job);
+    return launch_after(head_product_kernel<PRODUCT, BF16, N, false>, 2 * n, mma_threads<PRODUCT>(), mma_smem<N>(), stream, a, b, out, rest, job);
 }
 
 // `rows` and `weight`: the operand maps of the token side and of W's side.  With few tokens the two change places.  `out`: the

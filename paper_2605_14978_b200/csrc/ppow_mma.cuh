@@ -35,6 +35,9 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t smem, uint32_t rank)
     return r;
 }
 
+// An arrival on a barrier of this CTA.
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
 // An arrival that orders no memory: a release at cluster scope would wait for the warp's outstanding global stores each time
 // (2 of 11 cycles per instruction of a logit epilogue), and what is handed over here is Tensor Memory, by tcgen05 fences.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)

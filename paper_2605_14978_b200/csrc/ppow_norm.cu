@@ -9,9 +9,9 @@
 // values are x / 2^e rounded to nearest even in e4m3.  A power of two costs at most one bit of range against max/448 and
 // makes the division exact, so each value is rounded once and any implementation gives the same bits.
 //
-// All of it is bound by memory: one row at a time is held in registers by one warp or one CTA, read once; the sums over
-// rows (dw, db) stay in registers of the thread that owns the column, are written once per CTA and added up in a fixed
-// order by a second kernel.
+// Bound by memory, the backward pass by what a warp has to wait for between two passes over a row: one row at a time is held in
+// registers by one warp or one CTA, read once; the sums over rows (dw, db) stay in registers of the thread that owns the column,
+// are written once per CTA and added up by a second kernel in an order that is fixed for a device and build.
 #include "../../include/ppow.h"
 #include "ppow_checked.cuh"
 #include "ppow_device.cuh"
@@ -777,7 +777,7 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
     }
 }
 
-// Column sums over the CTAs' shares, in a fixed order: 32 columns by 8 groups of shares per CTA.
+// Column sums over the CTAs' shares, in a fixed order: 32 columns by JOIN_GROUPS groups of shares per CTA.
 constexpr int JOIN_GROUPS = 16;
 __global__ void __launch_bounds__(32 * JOIN_GROUPS) norm_join_kernel(const float *__restrict__ partial, int32_t shares, int32_t D,
                                                                      int32_t param_dtype, void *grad_weight, void *grad_bias)
@@ -954,7 +954,8 @@ int resident_ctas(Resident &known, Kernel kernel, int threads, size_t smem)
     return n;
 }
 
-// CTAs of the backward pass: each leaves one share of the column sums.  148 SMs x 2 to 4; a function of the sizes alone.
+// CTAs of the backward pass: each leaves one share of the column sums.  148 SMs x 2 to 4, and no more than the device keeps resident:
+// the order of the sums is fixed for a device and a build of the kernel, not across them.
 constexpr int32_t SHARES_MAX = 148 * 4;
 
 template <int DTYPE, bool VEC, int TPR>
