@@ -163,7 +163,7 @@ __device__ __forceinline__ double token_product(const uint16_t *h, const uint16_
 // depends on the order in which threads get there.  A row's place is the number of live rows with a smaller token, or with the same
 // one and a smaller index.  Up to ORDER_COUNTED tokens every gather CTA counts that for its rows over all tokens; that is T^2
 // comparisons, so behind it four small kernels make lists of each token's rows, in any order, in which a row then counts its
-// predecessors.  (Whole gradients of T x 64 x 1000: 73 us counted at T = 4096, 75 by lists; 131 and 118 at 8192.)
+// predecessors.  (Whole gradients of T x 64 x 1000 by lists: 1.5 us more at T = 4096, 12 us less at 8192.)
 constexpr int32_t ORDER_COUNTED = 4096;
 struct RowOrder {
     int32_t *count, *first;         // per vocabulary entry: live rows, and the place of the first
@@ -282,6 +282,8 @@ __device__ __forceinline__ int32_t split_count(int64_t tiles, int32_t steps)    
 
 // mult of a row, and for f16 the split into a factor near 2^15 and a power of two: dz of a row whose gradient is small
 // would fall below f16's smallest values.
+// (The states that dW multiplies are brought down by the row's power against the largest's instead: a row 2^14 and more below the
+// largest loses bits of its share of dW, which is as far below the largest rows' shares.)
 __device__ __forceinline__ float row_mult(float g, float inv_temperature) { return -g * inv_temperature; }
 __device__ __forceinline__ int row_exponent(float mult, int top)
 {
@@ -861,8 +863,8 @@ __device__ __forceinline__ void epilogue_few(const ProductJob &job, const Extent
 // tile's sum: the tile's rows lie side by side, and for 64 of them the operand in dz's place is zero but for one entry each, their
 // remainders.  A warp of its own writes it into the stage (done by the producer warp it held the copies up, and the tensor pipe was 79 %
 // active at 2048 x 4096 x 32000, not 95), where TMA brings the rows' hidden states beside it, in slices of the 16
-// rows that one instruction multiplies: a tile has few rows more often than not (552 tokens x 776 x 68450: 236 us with whole steps,
-// 230 like this, 217 without remainders; 4096 x 4096 x 128256: no difference).
+// rows that one instruction multiplies, since a tile has few rows more often than not (552 tokens x 776 x 68450: 6 us less than by
+// whole steps; 222 us in all, without remainders 217).
 constexpr uint32_t SLICE_BYTES = 16 * 128;
 // A step takes the 64 rows from `row` on, of those of the tile.  The hidden states read with them end with the last row tile at the
 // latest, because behind it the workspace holds anything: `row` is row `skip` of what is read.
