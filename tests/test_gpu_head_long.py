@@ -88,3 +88,36 @@ def test_sums_over_many_tokens_whose_terms_have_one_sign(T, dtype):
     own = (want.to(dtype).double() - want).square().sum()
     most = 1.05 * (own + head.U[dtype] ** 2 / 3 * others.sum()).sqrt() + 1.3e-4 * size.norm()
     assert float((gw.double() - want).norm()) <= float(most)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,V", [(6000, 3000), (9000, 40)])
+def test_rows_ordered_by_lists_give_the_same_every_time(T, V, dtype):
+    # above 4096 tokens the rows' order comes from lists that threads fill in any order: either gradient alone, eager and captured,
+    # on two streams at once, always the same bits
+    h, w, tok, grad = head.make(T, V, 136, dtype, seed=52, masked=0.3)
+    lse = B.head_logprob(h, w, tok)["lse"]
+    gh, gw = backward(h, w, tok, lse, grad)
+    check(h, w, tok, lse, grad, gh, gw)
+    assert torch.equal(B.head_logprob_backward(h, w, tok, lse, grad, want_weight=False)[0], gh)
+    assert torch.equal(B.head_logprob_backward(h, w, tok, lse, grad, want_hidden=False)[1], gw)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [B.head_logprob_backward(h, w, tok, lse, grad, stream=streams[i % 2]) for i in range(4)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, gh) and torch.equal(b, gw) for a, b in got)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a, b = B.head_logprob_backward(h, w, tok, lse, grad)
+    other = head.make(T, V, 136, dtype, seed=53, masked=0.6)
+    want = B.head_logprob_backward(other[0], other[1], other[2], lse, other[3])
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(a, gh) and torch.equal(b, gw)
+    for x, y in zip((h, w, tok, grad), other):
+        x.copy_(y)
+    graph.replay()
+    torch.cuda.synchronize()
+    # bit by bit: lse is the first inputs', and a p far above 1 is infinite in float16
+    assert torch.equal(a.view(torch.int16), want[0].view(torch.int16)) and torch.equal(b.view(torch.int16), want[1].view(torch.int16))
