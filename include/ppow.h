@@ -385,6 +385,97 @@ ppow_status ppow_pack_activation(const void *x, int64_t x_stride, int32_t R, int
 ppow_status ppow_unpack_activation(const uint8_t *packed, const uint8_t *scale, int32_t R, int32_t D, int32_t dtype,
                                    void *x, void *cuda_stream);
 
+/*
+ * Root-mean-square norm with the residual's addition, and its gradient (an addition of this library; the paper has no counterpart):
+ *     s = x + residual, rounded to the storage type (s = x without a residual)
+ *     rstd = 1 / sqrt(mean(s^2) + eps)        y = s * rstd * weight
+ * Sizes, types and limits as for ppow_layer_norm (no bias).  Sums are float32: rows of magnitudes above 1e19 overflow.
+ *   x               device, [R, D] of params->dtype, rows x_stride elements apart
+ *   residual        the same, rows residual_stride apart, or NULL; then sum is NULL too, else required
+ *   sum             device, [R, D], contiguous: s.  May be x or residual itself where that is contiguous
+ *   y               device, [R, D], contiguous, or NULL where y_packed is given
+ *   rstd            device, [R] float32
+ *   y_packed, y_scale   8-bit form of y, taken from its float32 values, or both NULL
+ *   packed, scale       8-bit form of s, for the gradient, or both NULL
+ * Apart from sum, outputs must not overlap inputs or one another.  No workspace.
+ */
+ppow_status ppow_rms_norm(const ppow_norm_params *params, const void *x, int64_t x_stride,
+                          const void *residual, int64_t residual_stride, const void *weight,
+                          void *sum, void *y, float *rstd, uint8_t *y_packed, uint8_t *y_scale,
+                          uint8_t *packed, uint8_t *scale, void *cuda_stream);
+
+/* Bytes of device scratch of the gradient (0 on parameters it refuses). */
+size_t ppow_rms_norm_workspace_bytes(const ppow_norm_params *params);
+
+/*
+ * Gradient, with a = grad_y * weight and xh = s * rstd:
+ *     grad_x = rstd * (a - xh * mean(a * xh)) + grad_sum         grad_weight = sum_rows grad_y * xh
+ * grad_x is the gradient of x and of the residual alike.
+ *   grad_y          device, [R, D] of params->dtype, rows grad_y_stride elements apart
+ *   grad_sum        what reaches s past the norm, the same with grad_sum_stride, or NULL for nothing
+ *   x, x_stride     s (what the forward pass normalised), or NULL: then packed and scale hold its 8-bit form
+ *   rstd            device, [R] float32, as written by ppow_rms_norm
+ *   grad_x          device, [R, D], contiguous
+ *   grad_weight     device, [D] of params->param_dtype, or NULL.  R == 0 sets it to 0.
+ *   workspace       device, >= ppow_rms_norm_workspace_bytes(params), 256-byte aligned
+ */
+ppow_status ppow_rms_norm_backward(const ppow_norm_params *params, const void *grad_y, int64_t grad_y_stride,
+                                   const void *grad_sum, int64_t grad_sum_stride, const void *x, int64_t x_stride,
+                                   const uint8_t *packed, const uint8_t *scale, const void *weight, const float *rstd,
+                                   void *grad_x, void *grad_weight, void *workspace, size_t workspace_bytes,
+                                   void *cuda_stream);
+
+/* Bytes of device scratch of ppow_clip_gradients for n tensors (0 on an n it refuses). */
+size_t ppow_clip_workspace_bytes(int32_t n);
+
+/*
+ * Global norm of the gradients of a step and clipping (an addition of this library; the paper has no counterpart):
+ *     norm = sqrt(sum over all tensors of g^2)      out = g * min(1, max_norm / norm), rounded to g's type
+ * A norm that is NaN makes every gradient NaN; an infinite one makes them 0 but for what was infinite, which becomes NaN.  The
+ * sum is float64 from 32 squares on, in an order that goes by the tensors' sizes and alignment alone.
+ *   n               tensors, 0 .. 65536
+ *   grads           host, [n] device addresses, each aligned to its element size; dense tensors of any shape.  A tensor may be
+ *                   listed more than once where out is not the gradients themselves: it counts every time
+ *   out             host, [n] device addresses, or NULL for the norm alone.  out[i] may be grads[i]; other than that no
+ *                   output may overlap a gradient or another output (PPOW_ERR_INVALID_ARG)
+ *   sizes, dtypes   host, [n]: elements (0 is allowed, 2^40 in all at most) and ppow_dtype of each
+ *   max_norm        >= 0, finite; ignored where out is NULL
+ *   norm            device, one float32
+ *   workspace       device, >= ppow_clip_workspace_bytes(n), 256-byte aligned
+ * The host arrays are read before the call returns.  In place, gradients within max_norm are not written.
+ */
+ppow_status ppow_clip_gradients(int32_t n, const void *const *grads, void *const *out, const int64_t *sizes,
+                                const int32_t *dtypes, double max_norm, float *norm,
+                                void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * Tokens drawn from logits with given uniforms (the drafter's rollout, Alg. 1; temperatures of Sec. 5.1).  With a row's tokens
+ * in descending order of their logits z_i, equal ones by index, w_i = exp((z_i - z_1) / temperature) and C_n the sum of the
+ * first n weights:
+ *     n_k = min(top_k, number of logits above -inf)         n_p = least n <= n_k with C_n >= top_p * C_(n_k)
+ *     n_m = number of i with w_i >= min_p                   n   = min(n_k, n_p, n_m)
+ *     token = the first in that order with C_j > u * C_n        logp = (z_token - z_1) / temperature - ln C_n
+ * so logp is that of the distribution the token was drawn from.  Masses are 64-bit: tokens are those of the definition, whichever
+ * way a row is cut, and repeat.
+ *   logits      device, [R, V], rows logits_stride elements apart, aligned to the element size.  -inf forbids a token.  A row of
+ *               nothing else gives token -1, logp -inf, kept 0; a row with a NaN or +inf gives token -1, logp NaN, kept 0
+ *   uniforms    device, [R] float32 in [0, 1); others count as the nearest in it, NaN as 0
+ *   tokens      device, [R] int32        logp   device, [R] float32        kept   device, [R] int32 or NULL: n
+ * 16-bit logits of magnitudes below 2048 (float16) or 4096 (bfloat16) take one pass over memory; float32 and others take several.
+ * No workspace.
+ */
+typedef struct {
+    int32_t R, V;               /* rows, 0 .. 2^27; vocabulary, >= 1, more than 2^22 is PPOW_ERR_UNSUPPORTED */
+    int32_t dtype;              /* ppow_dtype of the logits */
+    int32_t top_k;              /* 0: off */
+    int64_t logits_stride;      /* >= V */
+    double temperature;         /* 1e-300 .. 1e300 */
+    double top_p;               /* (0, 1]; 1: off */
+    double min_p;               /* [0, 1]; 0: off */
+} ppow_sample_params;
+ppow_status ppow_sample_tokens(const ppow_sample_params *params, const void *logits, const float *uniforms,
+                               int32_t *tokens, float *logp, int32_t *kept, void *cuda_stream);
+
 /* Copies the error word that the last ppow_score_windows call on `workspace` left behind into
  * *flags_host (PPOW_FLAG_* bits) and synchronises `cuda_stream` to do so.  Returns
  * PPOW_ERR_DEVICE_TIMEOUT if that bit is set, PPOW_ERR_CUDA on a CUDA failure, else PPOW_OK. */

@@ -36,7 +36,8 @@ EXPORTS = ("ppow_score_workspace_bytes", "ppow_score_windows", "ppow_score_windo
            "ppow_reference_logprob", "ppow_selftest_wait_timeout", "ppow_stream_read_probe", "ppow_score_kernel_launches",
            "ppow_head_workspace_bytes", "ppow_head_plan", "ppow_head_logprob", "ppow_head_logprob_backward",
            "ppow_layer_norm", "ppow_layer_norm_workspace_bytes", "ppow_layer_norm_backward", "ppow_pack_activation",
-           "ppow_unpack_activation",
+           "ppow_unpack_activation", "ppow_rms_norm", "ppow_rms_norm_workspace_bytes", "ppow_rms_norm_backward",
+           "ppow_clip_workspace_bytes", "ppow_clip_gradients", "ppow_sample_tokens",
            "ppow_checked_failures", "ppow_timeline_read", "ppow_status_string", "ppow_version")
 
 POSITION_OUTPUTS = {"accept_flag": torch.uint8, "kl": torch.float32, "conf": torch.float32, "crit": torch.float32,
@@ -73,6 +74,11 @@ class ppow_head_params(ctypes.Structure):
 class ppow_norm_params(ctypes.Structure):
     _fields_ = [("R", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32),
                 ("eps", ctypes.c_float)]
+
+
+class ppow_sample_params(ctypes.Structure):
+    _fields_ = [("R", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32), ("top_k", ctypes.c_int32),
+                ("logits_stride", ctypes.c_int64), ("temperature", ctypes.c_double), ("top_p", ctypes.c_double), ("min_p", ctypes.c_double)]
 
 
 class PpowError(RuntimeError):
@@ -155,6 +161,18 @@ def load_library():
     lib.ppow_pack_activation.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp]
     lib.ppow_unpack_activation.restype = ctypes.c_int
     lib.ppow_unpack_activation.argtypes = [vp, vp, i32, i32, i32, vp, vp]
+    lib.ppow_rms_norm.restype = ctypes.c_int
+    lib.ppow_rms_norm.argtypes = [ctypes.POINTER(ppow_norm_params), vp, i64, vp, i64] + [vp] * 9
+    lib.ppow_rms_norm_workspace_bytes.restype = sz
+    lib.ppow_rms_norm_workspace_bytes.argtypes = [ctypes.POINTER(ppow_norm_params)]
+    lib.ppow_rms_norm_backward.restype = ctypes.c_int
+    lib.ppow_rms_norm_backward.argtypes = [ctypes.POINTER(ppow_norm_params), vp, i64, vp, i64, vp, i64] + [vp] * 7 + [sz, vp]
+    lib.ppow_clip_workspace_bytes.restype = sz
+    lib.ppow_clip_workspace_bytes.argtypes = [i32]
+    lib.ppow_clip_gradients.restype = ctypes.c_int
+    lib.ppow_clip_gradients.argtypes = [i32, vp, vp, vp, vp, ctypes.c_double, vp, vp, sz, vp]
+    lib.ppow_sample_tokens.restype = ctypes.c_int
+    lib.ppow_sample_tokens.argtypes = [ctypes.POINTER(ppow_sample_params)] + [vp] * 6
     lib.ppow_checked_failures.restype = ctypes.c_int
     lib.ppow_checked_failures.argtypes = [ctypes.POINTER(ctypes.c_uint32), ctypes.POINTER(ctypes.c_uint32)]
     lib.ppow_timeline_read.restype = ctypes.c_int
@@ -177,7 +195,8 @@ class _NoCalls:
 
 _calls = None
 CALLED = ("ppow_head_workspace_bytes", "ppow_head_logprob", "ppow_head_logprob_backward", "ppow_layer_norm",
-          "ppow_layer_norm_workspace_bytes", "ppow_layer_norm_backward", "ppow_pack_activation", "ppow_unpack_activation")
+          "ppow_layer_norm_workspace_bytes", "ppow_layer_norm_backward", "ppow_pack_activation", "ppow_unpack_activation", "ppow_rms_norm",
+          "ppow_rms_norm_workspace_bytes", "ppow_rms_norm_backward", "ppow_clip_workspace_bytes", "ppow_clip_gradients", "ppow_sample_tokens")
 
 
 def _bind_calls(lib) -> None:
@@ -682,6 +701,91 @@ def ppow_unpack_activation(packed, scale, x, stream=None) -> None:
           _arg(x, x.dtype, (R, D), dev, "x"), _raw_stream(stream, dev))
 
 
+def _maybe_rows_arg(t: Optional[torch.Tensor], dtype, shape, dev: int, name):
+    """_rows_arg, or no address and the plain stride where there is no tensor."""
+    return (None, shape[1]) if t is None else _rows_arg(t, dtype, shape, dev, name)
+
+
+def ppow_rms_norm(params: ppow_norm_params, x, residual, weight, sum, y, rstd, y_packed=None, y_scale=None, packed=None, scale=None,
+                  stream=None) -> None:
+    """Enqueue the forward pass on ``x`` [R, D], to which ``residual`` is added if it is not None; then ``sum`` receives the sum."""
+    R, D, dt, pt, dev = params.R, params.D, LOGIT_DTYPES[params.dtype], LOGIT_DTYPES[params.param_dtype], _index_of(x, "x")
+    _call(load_library().ppow_rms_norm, "ppow_rms_norm", dev, ctypes.byref(params), *_rows_arg(x, dt, (R, D), dev, "x"),
+          *_maybe_rows_arg(residual, dt, (R, D), dev, "residual"), _arg(weight, pt, (D,), dev, "weight"), _arg(sum, dt, (R, D), dev, "sum"),
+          _arg(y, dt, (R, D), dev, "y"), _arg(rstd, torch.float32, (R,), dev, "rstd"), *_packed_args(y_packed, y_scale, R, D, dev),
+          *_packed_args(packed, scale, R, D, dev), _raw_stream(stream, dev))
+
+
+def ppow_rms_norm_workspace_bytes(params: ppow_norm_params) -> int:
+    return load_library().ppow_rms_norm_workspace_bytes(ctypes.byref(params))
+
+
+def ppow_rms_norm_backward(params: ppow_norm_params, grad_y, grad_sum, x, packed, scale, weight, rstd, grad_x, grad_weight, workspace,
+                           stream=None) -> None:
+    """Enqueue the gradient; what the forward pass normalised is either ``x`` or, where that is None, ``packed`` and ``scale``."""
+    R, D, dt, pt, dev = params.R, params.D, LOGIT_DTYPES[params.dtype], LOGIT_DTYPES[params.param_dtype], _index_of(grad_y, "grad_y")
+    _call(load_library().ppow_rms_norm_backward, "ppow_rms_norm_backward", dev, ctypes.byref(params),
+          *_rows_arg(grad_y, dt, (R, D), dev, "grad_y"), *_maybe_rows_arg(grad_sum, dt, (R, D), dev, "grad_sum"),
+          *_maybe_rows_arg(x, dt, (R, D), dev, "x"), *_packed_args(packed, scale, R, D, dev), _arg(weight, pt, (D,), dev, "weight"),
+          _arg(rstd, torch.float32, (R,), dev, "rstd"), _arg(grad_x, dt, (R, D), dev, "grad_x"), _arg(grad_weight, pt, (D,), dev, "grad_weight"),
+          *_workspace_arg(workspace, dev), _raw_stream(stream, dev))
+
+
+def ppow_clip_workspace_bytes(n: int) -> int:
+    return load_library().ppow_clip_workspace_bytes(n)
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether the elements fill their stretch of memory, in any order of the dimensions."""
+    want = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != want:
+            return t.numel() == 0
+        want *= size
+    return True
+
+
+def ppow_clip_gradients(grads, out, max_norm: float, norm, workspace, stream=None) -> None:
+    """Enqueue the global norm of ``grads`` (a sequence of tensors) into ``norm`` (one float32) and, unless ``out`` is None, the clipped
+    gradients into the tensors of ``out``, which may be ``grads``."""
+    dev, n = _index_of(norm, "norm"), len(grads)
+    if out is not None and len(out) != n:
+        raise ValueError("out must have as many tensors as grads")
+    for i, t in enumerate(grads):
+        if t.dtype not in DTYPE_CODES or t.get_device() != dev or not _dense(t):
+            raise ValueError("grads[%d] must be a dense float32, bfloat16 or float16 tensor on cuda:%d, got %s, %s, strides %s on %s" % (
+                i, dev, t.dtype, tuple(t.shape), t.stride(), t.device))
+        if out is not None:
+            o = out[i]
+            if o.dtype is not t.dtype or o.shape != t.shape or o.get_device() != dev or (t.numel() > 1 and any(
+                    a != b for a, b, s in zip(o.stride(), t.stride(), t.shape) if s > 1)):
+                raise ValueError("out[%d] must be like its gradient: %s, %s, strides %s on cuda:%d" % (i, t.dtype, tuple(t.shape), t.stride(), dev))
+    ptrs, i64s, i32s = ctypes.c_void_p * n, ctypes.c_int64 * n, ctypes.c_int32 * n
+    _call(load_library().ppow_clip_gradients, "ppow_clip_gradients", dev, n, ptrs(*[t.data_ptr() for t in grads]),
+          None if out is None else ptrs(*[t.data_ptr() for t in out]), i64s(*[t.numel() for t in grads]),
+          i32s(*[DTYPE_CODES[t.dtype] for t in grads]), float(max_norm), _arg(norm, torch.float32, norm.shape, dev, "norm"),
+          *_workspace_arg(workspace, dev), _raw_stream(stream, dev))
+
+
+def make_sample_params(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) -> ppow_sample_params:
+    """Sizes, type and row stride of a draw, from its logits [R, V], and the filters."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be 2-D")
+    R, V = logits.shape
+    top_k = max(-1, min(int(top_k), 2 ** 31 - 1))            # what is out of range stays so
+    return ppow_sample_params(min(R, 2 ** 31 - 1), min(V, 2 ** 31 - 1), _storage_code(logits.dtype, "logits"), top_k, logits.stride(0) if R > 1 else V, float(temperature),
+                              float(top_p), float(min_p))
+
+
+def ppow_sample_tokens(params: ppow_sample_params, logits, uniforms, tokens, logp, kept=None, stream=None) -> None:
+    """Enqueue the draw of one token for each row of ``logits`` [R, V]; ``kept`` may be None."""
+    R, V, dt, dev = params.R, params.V, LOGIT_DTYPES[params.dtype], _index_of(logits, "logits")
+    x, params.logits_stride = _rows_arg(logits, dt, (R, V), dev, "logits")
+    _call(load_library().ppow_sample_tokens, "ppow_sample_tokens", dev, ctypes.byref(params), x,
+          _arg(uniforms, torch.float32, (R,), dev, "uniforms"), _arg(tokens, torch.int32, (R,), dev, "tokens"),
+          _arg(logp, torch.float32, (R,), dev, "logp"), _arg(kept, torch.int32, (R,), dev, "kept"), _raw_stream(stream, dev))
+
+
 def _host_ptr(t: Optional[torch.Tensor], dtype=None, name="tensor"):
     if t is None:
         return None
@@ -910,3 +1014,112 @@ def unpack_activation(packed, scale, dtype=torch.bfloat16, stream=None):
         x = torch.empty(R, D, dtype=dtype, device=packed.device)
     _call(load_library().ppow_unpack_activation, "ppow_unpack_activation", dev, q, s, R, D, code, x.data_ptr(), _raw_stream(stream, dev))
     return x
+
+
+def rms_norm(x, weight, residual=None, *, eps=1e-6, checkpoint=False, packed_output=False, stream=None) -> dict:
+    """Allocate outputs and run ppow_rms_norm on ``x`` [R, D]; returns y and rstd, with ``residual`` also sum = x + residual (what was
+    normalised), with ``checkpoint`` the 8-bit form of that as packed and scale; with ``packed_output`` y_packed and y_scale in the
+    place of y.  All outside autograd (the gradient is rms_norm_backward's)."""
+    if stream is None:
+        got = _quick().rms_norm(x, weight, residual, eps, checkpoint, packed_output)
+        if got is not None:
+            got = _done(got, "ppow_rms_norm")
+            return {k: t for k, t in zip(("sum", "y", "rstd", "y_packed", "y_scale", "packed", "scale"), got) if t is not None}
+    R, D = x.shape
+    dt, pt, device, dev = x.dtype, weight.dtype, x.device, _index_of(x, "x")
+    params = make_norm_params(R, D, dt, pt, eps)
+    xp, xs = _rows_arg(x, dt, (R, D), dev, "x")
+    rp, rs = _maybe_rows_arg(residual, dt, (R, D), dev, "residual")
+    w, out = _arg(weight, pt, (D,), dev, "weight"), {}
+    with _on(stream):
+        if residual is not None:
+            out["sum"] = torch.empty(R, D, dtype=dt, device=device)
+        if packed_output:
+            out["y_packed"], out["y_scale"] = _alloc_packed(R, D, device)
+        else:
+            out["y"] = torch.empty(R, D, dtype=dt, device=device)
+        out["rstd"] = torch.empty(R, dtype=torch.float32, device=device)
+        if checkpoint:
+            out["packed"], out["scale"] = _alloc_packed(R, D, device)
+    at = {k: t.data_ptr() for k, t in out.items()}
+    _call(load_library().ppow_rms_norm, "ppow_rms_norm", dev, ctypes.byref(params), xp, xs, rp, rs, w, at.get("sum"), at.get("y"), at["rstd"],
+          at.get("y_packed"), at.get("y_scale"), at.get("packed"), at.get("scale"), _raw_stream(stream, dev))
+    return out
+
+
+def rms_norm_backward(grad_y, x, weight, rstd, *, grad_sum=None, stream=None):
+    """Allocate gradients and workspace, run ppow_rms_norm_backward; returns (grad_x, grad_weight).  ``x`` is what the forward pass
+    normalised (its sum, where it had a residual) or the pair (packed, scale) that it left; ``grad_sum`` is what reaches that sum past
+    the norm.  grad_x is the gradient of the forward pass's x and residual alike."""
+    if stream is None:
+        direct, (packed, scale) = (None, x) if isinstance(x, (tuple, list)) else (x, (None, None))
+        got = _quick().rms_norm_backward(grad_y, direct, packed, scale, weight, rstd, grad_sum)
+        if got is not None:
+            return _done(got, "ppow_rms_norm_backward")
+    R, D = grad_y.shape
+    dt, pt, device, dev = grad_y.dtype, weight.dtype, grad_y.device, _index_of(grad_y, "grad_y")
+    params, lib = make_norm_params(R, D, dt, pt), load_library()
+    gp, gs = _rows_arg(grad_y, dt, (R, D), dev, "grad_y")
+    sp, ss = _maybe_rows_arg(grad_sum, dt, (R, D), dev, "grad_sum")
+    if isinstance(x, (tuple, list)):
+        (xp, xs), (q, s) = (None, D), _packed_args(*x, R, D, dev)
+    else:
+        (xp, xs), (q, s) = _rows_arg(x, dt, (R, D), dev, "x"), (None, None)
+    w, r = _arg(weight, pt, (D,), dev, "weight"), _arg(rstd, torch.float32, (R,), dev, "rstd")
+    with _on(stream):
+        gx, gw = torch.empty(R, D, dtype=dt, device=device), torch.empty(D, dtype=pt, device=device)
+        nbytes = lib.ppow_rms_norm_workspace_bytes(ctypes.byref(params))
+        ws = _workspace(nbytes, device)
+    _call(lib.ppow_rms_norm_backward, "ppow_rms_norm_backward", dev, ctypes.byref(params), gp, gs, sp, ss, xp, xs, q, s, w, r, gx.data_ptr(),
+          gw.data_ptr(), ws.data_ptr(), nbytes, _raw_stream(stream, dev))
+    return gx, gw
+
+
+def clip_gradients(grads, max_norm, *, out=None, stream=None):
+    """Scale the gradients ``grads`` (a sequence of CUDA tensors of one device, dense, of any shapes and float types) by
+    min(1, max_norm / norm), norm the square root of the sum of all their squares: in place, or into the tensors of ``out``, which have
+    the gradients' shapes, types and strides.  Returns norm, a float32 tensor without dimensions; nothing waits for it."""
+    return _clip(grads, grads if out is None else out, max_norm, stream)
+
+
+def gradient_norm(grads, *, stream=None):
+    """The norm that clip_gradients goes by, alone."""
+    return _clip(grads, None, 0.0, stream)
+
+
+def _clip(grads, out, max_norm, stream):
+    grads = list(grads)
+    out = None if out is None else list(out)
+    if not grads:
+        raise ValueError("grads must hold at least one tensor")
+    if stream is None:
+        got = _quick().clip_gradients(grads, out, max_norm)
+        if got is not None:
+            return _done(got, "ppow_clip_gradients")[0]
+    device = grads[0].device
+    _index_of(grads[0], "grads[0]")
+    with _on(stream):
+        norm = torch.empty((), dtype=torch.float32, device=device)
+        ws = _workspace(ppow_clip_workspace_bytes(len(grads)), device)
+    ppow_clip_gradients(grads, out, max_norm, norm, ws, stream)
+    return norm
+
+
+def sample_tokens(logits, uniforms, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=None) -> dict:
+    """Allocate outputs and run ppow_sample_tokens on ``logits`` [R, V] and ``uniforms`` [R]; returns tokens (int32), logp (of the
+    distribution that was drawn from, after temperature and filters) and kept (how many tokens the filters left)."""
+    if stream is None:
+        got = _quick().sample_tokens(logits, uniforms, temperature, top_k, top_p, min_p)
+        if got is not None:
+            tokens, logp, kept = _done(got, "ppow_sample_tokens")
+            return {"tokens": tokens, "logp": logp, "kept": kept}
+    params, device, dev = make_sample_params(logits, temperature, top_k, top_p, min_p), logits.device, _index_of(logits, "logits")
+    R, V = logits.shape
+    x = _rows_arg(logits, logits.dtype, (R, V), dev, "logits")[0]
+    u = _arg(uniforms, torch.float32, (R,), dev, "uniforms")
+    with _on(stream):
+        out = {"tokens": torch.empty(R, dtype=torch.int32, device=device), "logp": torch.empty(R, dtype=torch.float32, device=device),
+               "kept": torch.empty(R, dtype=torch.int32, device=device)}
+    _call(load_library().ppow_sample_tokens, "ppow_sample_tokens", dev, ctypes.byref(params), x, u, out["tokens"].data_ptr(),
+          out["logp"].data_ptr(), out["kept"].data_ptr(), _raw_stream(stream, dev))
+    return out

@@ -13,6 +13,7 @@
 #include <torch/csrc/utils/pybind.h>
 
 #include <string>
+#include <vector>
 
 #include "../../include/ppow.h"
 
@@ -29,6 +30,12 @@ struct Library {
     decltype(&ppow_layer_norm_backward) layer_norm_backward = nullptr;
     decltype(&ppow_pack_activation) pack_activation = nullptr;
     decltype(&ppow_unpack_activation) unpack_activation = nullptr;
+    decltype(&ppow_rms_norm) rms_norm = nullptr;
+    decltype(&ppow_rms_norm_workspace_bytes) rms_norm_workspace_bytes = nullptr;
+    decltype(&ppow_rms_norm_backward) rms_norm_backward = nullptr;
+    decltype(&ppow_clip_workspace_bytes) clip_workspace_bytes = nullptr;
+    decltype(&ppow_clip_gradients) clip_gradients = nullptr;
+    decltype(&ppow_sample_tokens) sample_tokens = nullptr;
 } lib;
 
 void bind(const py::dict &addresses)
@@ -42,6 +49,12 @@ void bind(const py::dict &addresses)
     set("ppow_layer_norm_backward", lib.layer_norm_backward);
     set("ppow_pack_activation", lib.pack_activation);
     set("ppow_unpack_activation", lib.unpack_activation);
+    set("ppow_rms_norm", lib.rms_norm);
+    set("ppow_rms_norm_workspace_bytes", lib.rms_norm_workspace_bytes);
+    set("ppow_rms_norm_backward", lib.rms_norm_backward);
+    set("ppow_clip_workspace_bytes", lib.clip_workspace_bytes);
+    set("ppow_clip_gradients", lib.clip_gradients);
+    set("ppow_sample_tokens", lib.sample_tokens);
 }
 
 int code_of(at::ScalarType t)
@@ -204,6 +217,99 @@ py::object unpack_activation(const at::Tensor &packed, const at::Tensor &scale, 
     return py::make_tuple(status_of(st), to_python(x));
 }
 
+py::object rms_norm(const at::Tensor &x, const at::Tensor &weight, const c10::optional<at::Tensor> &residual, double eps, bool checkpoint,
+                    bool packed_output)
+{
+    const Place at(x);
+    ppow_norm_params p;
+    if (!norm_params(p, x, weight, eps, at) || (residual && !rows_ok(*residual, p.R, p.D, x.scalar_type(), at.dev))) return py::none();
+    at::Tensor sum, y, y_packed, y_scale, packed, scale;
+    if (residual) sum = at.empty({p.R, p.D}, x.scalar_type());
+    if (packed_output) {
+        y_packed = at.empty({p.R, p.D}, at::kFloat8_e4m3fn);
+        y_scale = at.empty({p.R, (p.D + 127) / 128}, at::kByte);
+    } else {
+        y = at.empty({p.R, p.D}, x.scalar_type());
+    }
+    const at::Tensor rstd = at.empty({p.R}, at::kFloat);
+    if (checkpoint) {
+        packed = at.empty({p.R, p.D}, at::kFloat8_e4m3fn);
+        scale = at.empty({p.R, (p.D + 127) / 128}, at::kByte);
+    }
+    const ppow_status st = lib.rms_norm(
+        &p, x.data_ptr(), row_stride(x), residual ? residual->data_ptr() : nullptr, residual ? row_stride(*residual) : p.D, weight.data_ptr(),
+        residual ? sum.data_ptr() : nullptr, packed_output ? nullptr : y.data_ptr(), rstd.data_ptr<float>(),
+        packed_output ? (uint8_t *)y_packed.data_ptr() : nullptr, packed_output ? y_scale.data_ptr<uint8_t>() : nullptr,
+        checkpoint ? (uint8_t *)packed.data_ptr() : nullptr, checkpoint ? scale.data_ptr<uint8_t>() : nullptr, at.stream);
+    return py::make_tuple(status_of(st), to_python(sum), to_python(y), to_python(rstd), to_python(y_packed), to_python(y_scale), to_python(packed),
+                          to_python(scale));
+}
+
+py::object rms_norm_backward(const at::Tensor &grad_y, const c10::optional<at::Tensor> &x, const c10::optional<at::Tensor> &packed,
+                             const c10::optional<at::Tensor> &scale, const at::Tensor &weight, const at::Tensor &rstd,
+                             const c10::optional<at::Tensor> &grad_sum)
+{
+    const Place at(grad_y);
+    ppow_norm_params p;
+    if (!norm_params(p, grad_y, weight, 1e-5, at) || !vector_ok(rstd, p.R, at::kFloat, at.dev) ||
+        (grad_sum && !rows_ok(*grad_sum, p.R, p.D, grad_y.scalar_type(), at.dev)))
+        return py::none();
+    if (x ? !rows_ok(*x, p.R, p.D, grad_y.scalar_type(), at.dev) : !packed || !scale || !packed_ok(*packed, *scale, p.R, p.D, at.dev))
+        return py::none();
+    const at::Tensor gx = at.empty({p.R, p.D}, grad_y.scalar_type()), gw = at.empty({p.D}, weight.scalar_type());
+    const size_t bytes = lib.rms_norm_workspace_bytes(&p);
+    const at::Tensor ws = at.scratch(bytes);
+    const ppow_status st = lib.rms_norm_backward(
+        &p, grad_y.data_ptr(), row_stride(grad_y), grad_sum ? grad_sum->data_ptr() : nullptr, grad_sum ? row_stride(*grad_sum) : p.D,
+        x ? x->data_ptr() : nullptr, x ? row_stride(*x) : p.D, x ? nullptr : (const uint8_t *)packed->data_ptr(),
+        x ? nullptr : scale->data_ptr<uint8_t>(), weight.data_ptr(), rstd.data_ptr<float>(), gx.data_ptr(), gw.data_ptr(), ws.data_ptr(), bytes,
+        at.stream);
+    return py::make_tuple(status_of(st), to_python(gx), to_python(gw));
+}
+
+py::object clip_gradients(const std::vector<at::Tensor> &grads, const c10::optional<std::vector<at::Tensor>> &out, double max_norm)
+{
+    if (grads.empty() || grads.size() > 65536 || (out && out->size() != grads.size())) return py::none();
+    const Place at(grads[0]);
+    if (!at.here) return py::none();
+    const size_t n = grads.size();
+    std::vector<const void *> from(n);
+    std::vector<void *> to(n);
+    std::vector<int64_t> sizes(n);
+    std::vector<int32_t> dtypes(n);
+    for (size_t i = 0; i < n; ++i) {
+        const at::Tensor &g = grads[i];
+        if (!on_device(g, at.dev) || (dtypes[i] = code_of(g.scalar_type())) < 0 || !g.is_non_overlapping_and_dense()) return py::none();
+        from[i] = g.data_ptr();
+        sizes[i] = g.numel();
+        if (out) {
+            const at::Tensor &o = (*out)[i];
+            if (!on_device(o, at.dev) || o.scalar_type() != g.scalar_type() || o.sizes() != g.sizes() || o.strides() != g.strides())
+                return py::none();
+            to[i] = o.data_ptr();
+        }
+    }
+    const at::Tensor norm = at.empty({}, at::kFloat);
+    const size_t bytes = lib.clip_workspace_bytes((int32_t)n);
+    const at::Tensor ws = at.scratch(bytes);
+    const ppow_status st = lib.clip_gradients((int32_t)n, from.data(), out ? to.data() : nullptr, sizes.data(), dtypes.data(), max_norm,
+                                              norm.data_ptr<float>(), ws.data_ptr(), bytes, at.stream);
+    return py::make_tuple(status_of(st), to_python(norm));
+}
+
+py::object sample_tokens(const at::Tensor &logits, const at::Tensor &uniforms, double temperature, int64_t top_k, double top_p, double min_p)
+{
+    const Place at(logits);
+    if (!at.here || logits.dim() != 2 || code_of(logits.scalar_type()) < 0 || top_k < INT32_MIN || top_k > INT32_MAX) return py::none();
+    const int64_t R = logits.size(0), V = logits.size(1);
+    if (!fits(R) || !fits(V) || !rows_ok(logits, R, V, logits.scalar_type(), at.dev) || !vector_ok(uniforms, R, at::kFloat, at.dev)) return py::none();
+    const ppow_sample_params p = {(int32_t)R, (int32_t)V, code_of(logits.scalar_type()), (int32_t)top_k, row_stride(logits), temperature, top_p, min_p};
+    const at::Tensor tokens = at.empty({R}, at::kInt), logp = at.empty({R}, at::kFloat), kept = at.empty({R}, at::kInt);
+    const ppow_status st = lib.sample_tokens(&p, logits.data_ptr(), uniforms.data_ptr<float>(), tokens.data_ptr<int32_t>(), logp.data_ptr<float>(),
+                                             kept.data_ptr<int32_t>(), at.stream);
+    return py::make_tuple(status_of(st), to_python(tokens), to_python(logp), to_python(kept));
+}
+
 // Out of memory is the Python path's to report: its allocations raise torch's own exception.
 template <typename... Args> auto guarded(py::object (*f)(Args...))
 {
@@ -229,4 +335,8 @@ PYBIND11_MODULE(_calls, m)
     m.def("layer_norm_backward", guarded(&layer_norm_backward));
     m.def("pack_activation", guarded(&pack_activation));
     m.def("unpack_activation", guarded(&unpack_activation));
+    m.def("rms_norm", guarded(&rms_norm));
+    m.def("rms_norm_backward", guarded(&rms_norm_backward));
+    m.def("clip_gradients", guarded(&clip_gradients));
+    m.def("sample_tokens", guarded(&sample_tokens));
 }

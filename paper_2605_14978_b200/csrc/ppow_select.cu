@@ -203,6 +203,9 @@ int read_check_counters_score(unsigned int *f, unsigned int *s);
 int read_check_counters_train(unsigned int *f, unsigned int *s);
 int read_check_counters_head(unsigned int *f, unsigned int *s);
 int read_check_counters_norm(unsigned int *f, unsigned int *s);
+int read_check_counters_rms(unsigned int *f, unsigned int *s);
+int read_check_counters_sample(unsigned int *f, unsigned int *s);
+int read_check_counters_clip(unsigned int *f, unsigned int *s);
 }
 #endif
 
@@ -213,7 +216,8 @@ extern "C" ppow_status ppow_checked_failures(uint32_t *failures_host, uint32_t *
     unsigned int f = 0, s = 0;
     if (cudaDeviceSynchronize() != cudaSuccess) return PPOW_ERR_CUDA;
     if (read_check_counters(&f, &s) || read_check_counters_score(&f, &s) || read_check_counters_train(&f, &s) ||
-        read_check_counters_head(&f, &s) || read_check_counters_norm(&f, &s))
+        read_check_counters_head(&f, &s) || read_check_counters_norm(&f, &s) || read_check_counters_rms(&f, &s) ||
+        read_check_counters_sample(&f, &s) || read_check_counters_clip(&f, &s))
         return PPOW_ERR_CUDA;
     *failures_host = f;
     if (first_site_host) *first_site_host = s;
