@@ -11,28 +11,33 @@
 //
 //   16-bit logits   A row holds at most 65536 different numbers: one pass counts them, by integer additions in shared memory, and all the
 //                   rest is arithmetic on a few thousand (number, count) pairs.  Bound by those additions (one warp's 32 fall on the 32
-//                   banks at random, 3.5 cycles) where the row's bytes take 2.2 of the same cycles.
+//                   banks at random, about 4 cycles) where the row's bytes take 2.7 of the same cycles.
+//   few logits      Up to 2048 above -inf are sorted in shared memory, and their masses added up in that order.
 //   float32         A row holds any numbers, so they go into 2048 bins of equal depth below the maximum, each with its count and its mass in
-//                   64-bit fixed point relative to the bin's top (integers again).  A border is followed into its bin by further passes
-//                   over the keys, 2048 to one, until a bin holds one number.  16-bit rows that the counting does not fit (logits
-//                   of 2048 and more, more than 65535 equal ones) go the same way.
+//                   fixed point relative to the bin's top (integers again).  The few hundred elements of the bin that holds a border
+//                   are sorted; a bin of more (many equal ones) is followed by further passes over the keys, 2048 to one, until one holds one number.
+//                   16-bit rows that the counting does not fit (logits of 2048 and more, more than 65535 equal ones) go the same way.
 //
 // A cluster of CTAs shares a row, each with a contiguous piece of it: one CTA when there are rows enough, up to eight for a few.
 #include "ppow_checked.cuh"
 #include "ppow_rows.cuh"
 
+#include <algorithm>
 #include <cooperative_groups.h>
 
 namespace ppow {
 namespace cg = cooperative_groups;
 
-constexpr int SAMPLE_THREADS = 512, SAMPLE_WARPS = SAMPLE_THREADS / 32, SAMPLE_CTAS = 8;
+constexpr int SAMPLE_CTAS = 8, WARPS_MOST = 16;
 constexpr int32_t SAMPLE_MAX_VOCAB = 1 << 22;
-constexpr int CHUNK = 256;               // bins whose counts and masses are summed up together
-constexpr int CHUNKS_MOST = 256;
-constexpr int SEARCH_BINS = 2048, SEARCH_CHUNK = 32, SEARCH_CHUNKS = SEARCH_BINS / SEARCH_CHUNK;
+constexpr int GROUP = 128;               // numbers of one sign whose counts and masses are summed up together: four to a lane
+constexpr int SEARCH_GROUP = 32;         // the same of the bins of a search
+constexpr int LIST = 2048;               // as many elements are sorted, or as there are bins if that is fewer
 constexpr double SEARCH_NATS = 64.0;     // what lies deeper than this below the maximum has no mass: 2^22 exp(-64) is 1e-21
-constexpr double MASS_ONE = 2199023255552.0;        // 2^41: a weight of 1; the 2^22 weights of a bin stay below 2^64
+// A mass in fixed point, 2^39 to 1, is added up in three limbs of 13 bits, so that 2^19 elements to a CTA fit words of 32.
+constexpr int LIMBS = 3, LIMB_BITS = 13;
+constexpr double MASS_ONE = 549755813888.0;
+constexpr int32_t PIECE_MOST = 1 << 19;
 
 struct SampleJob {
     const void *logits;
@@ -46,28 +51,51 @@ struct SampleJob {
 };
 
 // ---- formats ----------------------------------------------------------------------------------------
-// Counting: keys (bits in the order of the numbers) from BASE on, BINS of them, hold every |z| < LIMIT.  ZERO, the bin of +0, is even
-// and not a chunk's first, so that -0, the bin before it, can be added to it within the chunk.
+// Counting: a word for each of WORDS neighbouring magnitudes (by their bits) from LOW on; positive numbers in the low half, negative ones
+// in the high half, so that neighbours lie in different banks.
+//   bfloat16   64 exponents, 2^-51 <= |z| < 2^13.  A magnitude's word is its low 13 bits, whatever LOW is.  Zeros are counted apart.
+//   float16    all magnitudes below 2^11; a magnitude's word is the magnitude.  -0 is added to +0 afterwards.
 template <int DTYPE> struct Counted;
 template <> struct Counted<PPOW_BF16> {
-    static constexpr uint32_t LOWEST = 0x007fu, HIGHEST = 0xff80u, NEG_INF = 0xff80u;   // keys of -inf, +inf; bits of -inf
-    static constexpr uint32_t ZERO = 139 * 128, BINS = 2 * ZERO, BASE = 0x8000u - ZERO;
-    static constexpr double LIMIT = 4096.0;
+    static constexpr uint32_t INF = 0x7f80u, LOW = 76 * 128, WORDS = 64 * 128, MASK = WORDS - 1;
+    static constexpr int THREADS = 256, CTAS = 4;            // of a block; blocks on an SM
+    static constexpr double LIMIT = 8192.0;
+    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b) { return max_bf16x2(a, b); }     // NaN is passed over
+    static __device__ __forceinline__ uint32_t equal(uint32_t a, uint32_t b)
+    {
+        return __heq2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    }
 };
 template <> struct Counted<PPOW_F16> {
-    static constexpr uint32_t LOWEST = 0x03ffu, HIGHEST = 0xfc00u, NEG_INF = 0xfc00u;
-    static constexpr uint32_t ZERO = 26 * 1024 + 128, BINS = 2 * ZERO, BASE = 0x8000u - ZERO;
+    static constexpr uint32_t INF = 0x7c00u, LOW = 0, WORDS = 26 * 1024, MASK = 0x7fffu;
+    static constexpr int THREADS = 512, CTAS = 2;
     static constexpr double LIMIT = 2048.0;
+    static __device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b)
+    {
+        const __half2 m = __hmax2(UnitF16::h2(a), UnitF16::h2(b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+    static __device__ __forceinline__ uint32_t equal(uint32_t a, uint32_t b) { return __heq2_mask(UnitF16::h2(a), UnitF16::h2(b)); }
 };
-static_assert(Counted<PPOW_BF16>::BINS % CHUNK == 0 && Counted<PPOW_F16>::BINS % CHUNK == 0, "whole chunks");
-static_assert(Counted<PPOW_BF16>::ZERO % CHUNK != 0 && Counted<PPOW_F16>::ZERO % CHUNK != 0, "-0 beside +0");
-static_assert(Counted<PPOW_F16>::BINS / CHUNK <= CHUNKS_MOST, "chunks");
-
-template <int DTYPE> __device__ __forceinline__ float number_of(uint32_t bin)
-{
-    const uint32_t key = bin + Counted<DTYPE>::BASE;
-    return Storage<DTYPE>::get((uint16_t)(key & 0x8000u ? key ^ 0x8000u : ~key));
-}
+// Groups of one sign, by rising magnitude; positive ones first, then the zeros (where they are counted apart), then negative ones.
+template <int DTYPE> struct Groups {
+    using F = Counted<DTYPE>;
+    static constexpr int SIDE = F::WORDS / GROUP, ZERO = SIDE, ALL = 2 * SIDE + 1;
+    static_assert(F::WORDS % GROUP == 0 && F::LOW % GROUP == 0, "whole groups");
+    static __device__ __forceinline__ bool negative(int group) { return group > ZERO; }
+    static __device__ __forceinline__ int side(int group) { return group > ZERO ? group - ZERO - 1 : group; }
+    // first word of a group of either sign
+    static __device__ __forceinline__ int word(int side) { return (int)(((uint32_t)side * GROUP + F::LOW) & F::MASK); }
+    // the i-th group in descending order
+    static __device__ __forceinline__ int at(int i) { return i < SIDE ? SIDE - 1 - i : i; }
+    // the i-th number of a group, by rising magnitude
+    static __device__ __forceinline__ float number(int group, int i)
+    {
+        return group == ZERO ? 0.0f : Storage<DTYPE>::get((uint16_t)(F::LOW + side(group) * GROUP + i + (negative(group) ? 0x8000 : 0)));
+    }
+};
+constexpr int GROUPS_MOST = Groups<PPOW_F16>::ALL;
+static_assert(GROUPS_MOST >= Groups<PPOW_BF16>::ALL && GROUPS_MOST >= LIST / SEARCH_GROUP, "groups");
 
 // Order-preserving key of a float32 (-0 is +0), and back.
 __device__ __forceinline__ uint32_t key_of(float z)
@@ -105,7 +133,7 @@ template <int DTYPE> struct Piece {
                 if (2 < lo || 2 >= hi) w.z = 0xff800000u;
                 if (3 < lo || 3 >= hi) w.w = 0xff800000u;
             } else {
-                mask_halves(w, lo, hi, Counted<DTYPE>::NEG_INF);
+                mask_halves(w, lo, hi, 0x8000u | Counted<DTYPE>::INF);
             }
         }
         return w;
@@ -132,19 +160,26 @@ struct Target {
     }
 };
 
-// The item of 0 .. n-1 (n <= 256, descending) that holds the border; the last one that is not empty if rounding leaves it to
-// none.  get(item, count, mass).  The whole warp calls, every lane has the result.
-template <typename Get> __device__ Place warp_find(int n, const Target &target, const Place &before, Get &&get)
+// The item of 0 .. n-1 (n <= 32 PER, descending) that holds the border; the last one that counts if rounding leaves it to none.
+// get(item): count and mass.  The whole warp calls, every lane has the result.
+struct Part {
+    uint32_t count;
+    double mass;
+};
+template <int PER, typename Get> __device__ __forceinline__ Place warp_find(int n, const Target &target, const Place &before, Get &&get)
 {
-    constexpr int PER = CHUNKS_MOST / 32;
     const int lane = threadIdx.x & 31;
     uint32_t c[PER], count = 0;
     double m[PER], mass = 0.0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        c[i] = 0;
-        m[i] = 0.0;
-        if (lane * PER + i < n) get(lane * PER + i, c[i], m[i]);
+        const bool in = lane * PER + i < n;
+        const Part part = get(in ? lane * PER + i : 0);
+        c[i] = in ? part.count : 0;
+        m[i] = in ? part.mass : 0.0;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
         count += c[i];
         mass += m[i];
     }
@@ -176,48 +211,51 @@ template <typename Get> __device__ Place warp_find(int n, const Target &target, 
         from = who ? 31 - __clz(who) : 0;
         found = last;
     }
-    return {__shfl_sync(0xffffffffu, found.item, from), __shfl_sync(0xffffffffu, found.count, from), __shfl_sync(0xffffffffu, found.mass, from)};
+    return {max(__shfl_sync(0xffffffffu, found.item, from), 0), __shfl_sync(0xffffffffu, found.count, from), __shfl_sync(0xffffffffu, found.mass, from)};
 }
 
-// A number, how many elements have it, what lies before them, and which of them is meant.
-struct Number {
+// An element: its number, its place in the order, the mass up to and with it.  Where its token is not known, it is the rank-th (from 0) of
+// the `have` elements with that number, by index.
+struct Element {
     float value;
-    uint32_t have, before, rank;         // rank: 0 .. have - 1
-    double weight, mass;                 // of one element; of those before
-    __device__ __forceinline__ uint32_t n() const { return before + rank + 1; }
-    __device__ __forceinline__ double total() const { return mass + (rank + 1) * weight; }
-    __device__ __forceinline__ void choose(const Target &target)
-    {
-        if (target.kind == Border::Count) {
-            rank = min(target.count - before, have) - 1;
-            return;
-        }
-        // the quotient is right to a small part of 1, but for weights below 1e-13 of the mass, which no border can tell apart
-        const double q = floor((target.mass - mass) / weight);
-        rank = q >= (double)have ? have - 1 : q > 0.0 ? (uint32_t)q : 0;
-        if (rank > 0 && target.met(0, mass + rank * weight)) --rank;
-        if (rank < have - 1 && !target.met(0, mass + (rank + 1) * weight)) ++rank;
-    }
-};
-
-struct SampleShared {
-    uint32_t chunk_count[CHUNKS_MOST], chunk_within[CHUNKS_MOST];       // elements; those within min_p
-    double chunk_mass[CHUNKS_MOST];
-    int32_t chunk_top[CHUNKS_MOST];          // highest bin that is not empty
-    uint32_t none, low, flags;               // -inf; below the counted range; SAMPLE_*
-    uint32_t warp_count[2][SAMPLE_WARPS];
-    uint32_t here;                           // elements of the drawn number in this piece
-    // search
-    uint32_t max_key, low_key, high_key, within;
-    // results of warp 0
-    Number drawn;
     uint32_t n;
     double total;
+    int32_t token;           // -1: not known
+    uint32_t rank, have;
+};
+
+// Which of `have` equal elements of this weight, behind `before`, the border falls on.
+__device__ __forceinline__ Element choose(const Target &target, const Place &before, float value, uint32_t have, double weight)
+{
+    uint32_t rank;
+    if (target.kind == Border::Count) {
+        rank = min(target.count - before.count, have) - 1;
+    } else {
+        // the quotient is right to a small part of 1, but for weights below 1e-13 of the mass, which no border can tell apart
+        const double q = floor((target.mass - before.mass) / weight);
+        rank = q >= (double)have ? have - 1 : q > 0.0 ? (uint32_t)q : 0;
+        if (rank > 0 && target.met(0, before.mass + rank * weight)) --rank;
+        if (rank < have - 1 && !target.met(0, before.mass + (rank + 1) * weight)) ++rank;
+    }
+    return {value, before.count + rank + 1, before.mass + (rank + 1) * weight, -1, rank, have};
+}
+
+struct SampleShared {
+    uint32_t group_count[GROUPS_MOST];
+    double group_mass[GROUPS_MOST];
+    double warp_mass[WARPS_MOST];
+    uint32_t warp_count[2][WARPS_MOST];
+    uint32_t none, low, zeros;               // -inf; below the counted range; zeros that are counted apart
+    uint32_t flags, within, top;             // SAMPLE_*; within min_p; key of the maximum
+    uint32_t here;                           // elements of the drawn number in this piece
+    uint32_t low_key, high_key, listed;
+    int32_t first;
+    Element drawn;
     Place place;
 };
 enum : uint32_t { SAMPLE_BAD = 1, SAMPLE_ODD = 2 };      // NaN or +inf; a row that counting does not fit
 
-template <typename Cluster> __device__ __forceinline__ void meet(const Cluster &cluster, int ctas)
+__device__ __forceinline__ void meet(const cg::cluster_group &cluster, int ctas)
 {
     if (ctas == 1)
         __syncthreads();
@@ -225,54 +263,73 @@ template <typename Cluster> __device__ __forceinline__ void meet(const Cluster &
         cluster.sync();
 }
 
-// The whole distribution of a row from find(target), which gives the number that holds a border: what is kept, and the draw.
-// F: elements above -inf, of which `massive` carry the mass `all`.  One warp.
+// The whole distribution of a row from find(target), which gives the element on a border: what is kept, and the draw.
+// F: elements above -inf, of which `massive` carry the mass `all`.
 template <typename Find>
-__device__ void decide(const SampleJob &job, float u, uint32_t F, uint32_t massive, double all, uint32_t within, Find &&find, Number &drawn,
-                       uint32_t &n, double &total)
+__device__ __forceinline__ void decide(const SampleJob &job, float u, uint32_t F, uint32_t massive, double all, uint32_t within, Find &&find,
+                                       Element &drawn, uint32_t &n, double &total)
 {
     n = job.top_k > 0 && (uint32_t)job.top_k < F ? (uint32_t)job.top_k : F;
-    total = n < massive ? find(Target{Border::Count, n, 0.0}).total() : all;
-    if (job.top_p < 1.0) {
-        const Number border = find(Target{Border::MassFrom, 0, job.top_p * total});
-        if (border.n() < n) n = border.n(), total = border.total();
+    total = all;
+    u = fminf(fmaxf(u, 0.0f), 0x1.fffffep-1f);               // NaN is 0
+    // one copy of the code of `find` for all borders: it is long, and each row runs through it once
+#pragma unroll 1
+    for (int step = 0; step < 5; ++step) {
+        Target target = {Border::Count, n, 0.0};
+        if (step == 0) {
+            if (n >= massive) continue;
+        } else if (step == 1) {
+            if (!(job.top_p < 1.0)) continue;
+            target = {Border::MassFrom, 0, job.top_p * total};
+        } else if (step == 2) {
+            if (!(job.min_p > 0.0 && within < n)) continue;
+            target.count = n = within;
+        } else if (step == 3) {
+            target = {Border::MassAbove, 0, (double)u * total};
+        } else if (drawn.n <= n) {
+            continue;
+        }
+        const Element e = find(target);
+        if (step >= 3)
+            drawn = e;
+        else if (step != 1 || e.n < n)
+            n = e.n, total = e.total;
     }
-    if (job.min_p > 0.0 && within < n) {
-        n = within;
-        total = find(Target{Border::Count, n, 0.0}).total();
-    }
-    const double at = fminf(fmaxf(u, 0.0f), 0x1.fffffep-1f);        // NaN is 0
-    drawn = find(Target{Border::MassAbove, 0, at * total});
-    if (drawn.n() > n) drawn = find(Target{Border::Count, n, 0.0});
 }
 
-// The index of the rank-th element of this piece that `matches` accepts; searched in rounds, each warp a stretch of neighbouring units.
-template <int DTYPE, typename Matches>
+// The index of the rank-th element of this piece that `matches` accepts, searched in rounds: each warp a stretch of neighbouring units, the
+// next round's on their way while this one's are counted.  matches: a bit for each of a unit's elements, that of element e at
+// e / 2 + 16 (e % 2) where there are eight, at e where there are four.
+template <int THREADS, int DTYPE, typename Matches>
 __device__ void locate(const Piece<DTYPE> &piece, uint32_t rank, SampleShared &sh, int32_t *token, Matches &&matches)
 {
-    using S = Storage<DTYPE>;
-    constexpr int E = S::PER_UNIT, DEEP = 4;
+    constexpr int DEEP = 4;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t seen = 0;
     int turn = 0;
-    for (int32_t base = piece.begin; base < piece.end; base += SAMPLE_THREADS * DEEP, turn ^= 1) {
-        uint32_t bits[DEEP], mine = 0;
+    uint4 next[DEEP];
+    auto fetch = [&](int32_t base) {
 #pragma unroll
         for (int q = 0; q < DEEP; ++q) {
             const int32_t u = base + (warp * DEEP + q) * 32 + lane;
-            bits[q] = 0;
-            if (u < piece.end) bits[q] = matches(piece.load(u));
-            mine += __popc(bits[q]);
+            if (u < piece.end) next[q] = piece.load(u);
         }
+    };
+    fetch(piece.begin);
+    for (int32_t base = piece.begin; base < piece.end; base += THREADS * DEEP, turn ^= 1) {
+        uint32_t bits[DEEP], mine = 0;
+#pragma unroll
+        for (int q = 0; q < DEEP; ++q) {
+            bits[q] = base + (warp * DEEP + q) * 32 + lane < piece.end ? matches(next[q]) : 0u;
+        }
+        fetch(base + THREADS * DEEP);
+        if (bits[0] | bits[1] | bits[2] | bits[3]) mine = __popc(bits[0]) + __popc(bits[1]) + __popc(bits[2]) + __popc(bits[3]);
         mine = __reduce_add_sync(0xffffffffu, mine);
         if (lane == 0) sh.warp_count[turn][warp] = mine;
         __syncthreads();
-        uint32_t before = seen;
-        for (int i = 0; i < SAMPLE_WARPS; ++i) {
-            const uint32_t c = sh.warp_count[turn][i];
-            if (i < warp) before += c;
-            seen += c;
-        }
+        const uint32_t c = lane < (THREADS / 32) ? sh.warp_count[turn][lane] : 0u;
+        uint32_t before = seen + __reduce_add_sync(0xffffffffu, lane < warp ? c : 0u);
+        seen += __reduce_add_sync(0xffffffffu, c);
         if (before <= rank && rank < before + mine) {
 #pragma unroll
             for (int q = 0; q < DEEP; ++q) {
@@ -282,25 +339,123 @@ __device__ void locate(const Piece<DTYPE> &piece, uint32_t rank, SampleShared &s
                     const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
                     if (lane >= o) upto += v;
                 }
-                const uint32_t from = before + upto - __popc(bits[q]);
-                if (from <= rank && rank < before + upto)
-                    *token = piece.token(base + (warp * DEEP + q) * 32 + lane, (int)__fns(bits[q], 0, (int)(rank - from) + 1));
+                uint32_t from = before + upto - __popc(bits[q]);
+#pragma unroll
+                for (int e = 0; e < Piece<DTYPE>::E; ++e)
+                    if (bits[q] >> (Piece<DTYPE>::E == 8 ? e / 2 + e % 2 * 16 : e) & 1) {
+                        if (from == rank) *token = piece.token(base + (warp * DEEP + q) * 32 + lane, e);
+                        ++from;
+                    }
                 before += __shfl_sync(0xffffffffu, upto, 31);
             }
         }
         if (seen > rank) return;             // the same for the whole CTA
     }
-    static_assert(E <= 8, "a bit for each element");
+}
+
+// ---- a sorted list ----------------------------------------------------------------------------------
+// key << 32 | ~index: descending is by number, equal ones by index.
+__device__ __forceinline__ unsigned long long list_entry(float z, int32_t token) { return (unsigned long long)key_of(z) << 32 | (uint32_t)~token; }
+__device__ __forceinline__ float list_value(unsigned long long e) { return float_of((uint32_t)(e >> 32)); }
+__device__ __forceinline__ int32_t list_token(unsigned long long e) { return (int32_t)~(uint32_t)e; }
+
+// Sorts list[0 .. n) in descending order, n <= LIST, in place; a network over the next power of two.  Exchanges over up to 32 places stay within
+// a warp's 64 entries.
+template <int THREADS> __device__ void sort_list(unsigned long long *list, int n)
+{
+    int size = 64;
+    while (size < n) size <<= 1;
+    for (int i = n + (int)threadIdx.x; i < size; i += THREADS) list[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= size; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            for (int t = threadIdx.x; t < size / 2; t += THREADS) {
+                const int lo = ((t & ~(j - 1)) << 1) | (t & (j - 1)), hi = lo | j;
+                const unsigned long long a = list[lo], b = list[hi];
+                if ((a < b) == ((lo & k) == 0)) list[lo] = b, list[hi] = a;
+            }
+            if (j > 32 || (j == 1 && k >= 64))
+                __syncthreads();
+            else
+                __syncwarp();
+        }
+}
+
+// mass[i]: of list[0 .. i], behind `before`.  up(z): the weight of a number.
+template <int THREADS, typename Weight> __device__ void add_up_list(const unsigned long long *list, double *mass, int n, double before, SampleShared &sh, Weight &&weight)
+{
+    constexpr int PER = LIST / THREADS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    double m[PER], sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int at = threadIdx.x * PER + i;
+        m[i] = 0.0;
+        if (at < n) m[i] = weight(list_value(list[at]));
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += m[i];
+    double upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) sh.warp_mass[warp] = upto;
+    upto = __shfl_up_sync(0xffffffffu, upto, 1);
+    if (lane == 0) upto = 0.0;
+    __syncthreads();
+    for (int i = 0; i < warp; ++i) before += sh.warp_mass[i];
+    before += upto;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int at = threadIdx.x * PER + i;
+        before += m[i];
+        if (at < n) mass[at] = before;
+    }
+    __syncthreads();
+}
+
+// The element of a sorted list on the border; the last one if there is none.  The whole CTA calls.
+template <int THREADS> __device__ Element find_in_list(const unsigned long long *list, const double *mass, int n, uint32_t before, const Target &target, SampleShared &sh)
+{
+    if (threadIdx.x == 0) sh.first = n - 1;
+    __syncthreads();
+    int at = n - 1;
+    for (int i = threadIdx.x; i < n; i += THREADS)
+        if (target.met(before + i + 1, mass[i])) {
+            at = i;
+            break;
+        }
+    at = __reduce_min_sync(0xffffffffu, at);
+    if ((threadIdx.x & 31) == 0) atomicMin(&sh.first, at);
+    __syncthreads();
+    at = sh.first;
+    __syncthreads();
+    return {list_value(list[at]), before + at + 1, mass[at], list_token(list[at]), 0, 1};
 }
 
 // ---- search: any row --------------------------------------------------------------------------------
-struct SearchBins {
-    uint32_t count[SEARCH_BINS], low[SEARCH_BINS], high[SEARCH_BINS];       // of this CTA; mass in fixed point
-    uint32_t all_count[SEARCH_BINS];                                        // of the cluster
+template <int SEARCH_BINS> struct SearchBins {
+    union {
+        struct {                                             // of this CTA
+            uint32_t count[SEARCH_BINS], limb[LIMBS][SEARCH_BINS];
+        };
+        struct {
+            unsigned long long list[SEARCH_BINS];
+            union {
+                double mass[SEARCH_BINS];
+                unsigned long long own[SEARCH_BINS];                // this CTA's part of the list, before it is put together
+            };
+        };
+    };
+    uint32_t all_count[SEARCH_BINS];                         // of the cluster
     double all_mass[SEARCH_BINS];
 };
 
-template <int DTYPE> struct Search {
+template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
+    static constexpr int SEARCH_GROUPS = SEARCH_BINS / SEARCH_GROUP, MOST = SEARCH_BINS < LIST ? SEARCH_BINS : LIST;
+    using Bins = SearchBins<SEARCH_BINS>;
     using S = Storage<DTYPE>;
     static constexpr int E = S::PER_UNIT;
     const SampleJob &job;
@@ -308,61 +463,80 @@ template <int DTYPE> struct Search {
     const cg::cluster_group &cluster;
     int rank, ctas;
     SampleShared &sh;
-    SearchBins &bins;
+    Bins &bins;
     double top, scale, per_nat;              // maximum; bins per logit; 1 / temperature
+    bool depths;                             // whether all_count and all_mass hold the depth bins
 
+    template <typename T> __device__ __forceinline__ T *of(T *p, int r) const { return ctas == 1 ? p : cluster.map_shared_rank(p, r); }
+    // f(z, token) for every logit of the piece; those around the row are -inf
     template <typename F> __device__ __forceinline__ void each(F &&f) const
     {
-        for (int32_t u = piece.begin + (int32_t)threadIdx.x; u < piece.end; u += SAMPLE_THREADS) {
-            float z[E];
-            S::unpack(piece.load(u), z);
+        constexpr int DEEP = 2;
+        for (int32_t u0 = piece.begin + (int32_t)threadIdx.x; u0 < piece.end; u0 += THREADS * DEEP) {
+            uint4 w[DEEP];
 #pragma unroll
-            for (int e = 0; e < E; ++e) f(z[e]);
+            for (int q = 0; q < DEEP; ++q)
+                if (u0 + q * THREADS < piece.end) w[q] = piece.load(u0 + q * THREADS);
+#pragma unroll
+            for (int q = 0; q < DEEP; ++q)
+                if (u0 + q * THREADS < piece.end) {
+                    float z[E];
+                    S::unpack(w[q], z);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) f(z[e], piece.token(u0 + q * THREADS, e));
+                }
         }
     }
     __device__ __forceinline__ int depth_bin(double d) const { return (int)fmin(d * scale, (double)(SEARCH_BINS - 1)); }
-    __device__ __forceinline__ double weight(double d) const { return exp(-d * per_nat); }
+    __device__ __forceinline__ double weight(float z) const { return exp(((double)z - top) * per_nat); }
 
     __device__ void clear()
     {
-        for (int i = threadIdx.x; i < SEARCH_BINS; i += SAMPLE_THREADS) bins.count[i] = bins.low[i] = bins.high[i] = 0;
+        uint32_t *words = bins.count;
+        for (int i = threadIdx.x; i < (1 + LIMBS) * SEARCH_BINS; i += THREADS) words[i] = 0;
         __syncthreads();
     }
-    // mass relative to the top of a depth bin, 2^41 to the whole
+    // one more element, its mass relative to the top of its depth bin
     __device__ __forceinline__ void add(int item, double d, double bin_top)
     {
-        const unsigned long long w = __double2ull_rn(exp((bin_top - d) * per_nat) * MASS_ONE);
         if (!PPOW_CHECK(item >= 0 && item < SEARCH_BINS, 801, nullptr)) return;
+        const unsigned long long w = __double2ull_rn(exp((bin_top - d) * per_nat) * MASS_ONE);
         atomicAdd(&bins.count[item], 1u);
-        const uint32_t lo = (uint32_t)w, old = atomicAdd(&bins.low[item], lo);
-        const uint32_t hi = (uint32_t)(w >> 32) + (old + lo < old ? 1u : 0u);
-        if (hi) atomicAdd(&bins.high[item], hi);
+#pragma unroll
+        for (int i = 0; i < LIMBS; ++i) {
+            const uint32_t limb = (uint32_t)(w >> (i * LIMB_BITS)) & (i == LIMBS - 1 ? 0xffffffffu : (1u << LIMB_BITS) - 1);
+            atomicAdd(&bins.limb[i][item], limb);
+        }
     }
-    // Sums up the CTAs' bins, each CTA a share of them for all, and the chunks.  unit(item): what a mass of 1 in this bin stands for.
+    // Sums up the CTAs' bins, each CTA a share of them for all, and the groups.  unit(item): what a mass of 1 in this bin stands for.
     template <typename Unit> __device__ void join(Unit &&unit)
     {
         meet(cluster, ctas);
-        for (int i = rank * SAMPLE_THREADS + (int)threadIdx.x; i < SEARCH_BINS; i += ctas * SAMPLE_THREADS) {
+        for (int i = rank * THREADS + (int)threadIdx.x; i < SEARCH_BINS; i += ctas * THREADS) {
             uint32_t count = 0;
-            unsigned long long mass = 0;
+            unsigned long long limbs[LIMBS] = {};
             for (int r = 0; r < ctas; ++r) {
-                const SearchBins *b = ctas == 1 ? &bins : cluster.map_shared_rank(&bins, r);
+                const Bins *b = of(&bins, r);
                 count += b->count[i];
-                mass += b->low[i] + ((unsigned long long)b->high[i] << 32);
+#pragma unroll
+                for (int l = 0; l < LIMBS; ++l) limbs[l] += b->limb[l][i];
             }
+            unsigned long long mass = 0;
+#pragma unroll
+            for (int l = 0; l < LIMBS; ++l) mass += limbs[l] << (l * LIMB_BITS);
             const double m = count ? (double)mass * (1.0 / MASS_ONE) * unit(i) : 0.0;
             for (int r = 0; r < ctas; ++r) {
-                SearchBins *b = ctas == 1 ? &bins : cluster.map_shared_rank(&bins, r);
+                Bins *b = of(&bins, r);
                 b->all_count[i] = count;
                 b->all_mass[i] = m;
             }
         }
         meet(cluster, ctas);
-        for (int c = threadIdx.x >> 5; c < SEARCH_CHUNKS; c += SAMPLE_WARPS) {
-            const int i = c * SEARCH_CHUNK + (threadIdx.x & 31);
+        for (int c = threadIdx.x >> 5; c < SEARCH_GROUPS; c += (THREADS / 32)) {
+            const int i = c * SEARCH_GROUP + (threadIdx.x & 31);
             const uint32_t count = __reduce_add_sync(0xffffffffu, bins.all_count[i]);
             const double mass = warp_sum_f64(bins.all_mass[i]);
-            if ((threadIdx.x & 31) == 0) sh.chunk_count[c] = count, sh.chunk_mass[c] = mass;
+            if ((threadIdx.x & 31) == 0) sh.group_count[c] = count, sh.group_mass[c] = mass;
         }
         __syncthreads();
     }
@@ -370,12 +544,10 @@ template <int DTYPE> struct Search {
     __device__ Place find_bin(const Target &target, const Place &before)
     {
         if (threadIdx.x < 32) {
-            Place p = warp_find(SEARCH_CHUNKS, target, before, [&](int i, uint32_t &c, double &m) { c = sh.chunk_count[i], m = sh.chunk_mass[i]; });
-            const int chunk = p.item < 0 ? 0 : p.item;
-            p = warp_find(SEARCH_CHUNK, target, p, [&](int i, uint32_t &c, double &m) {
-                c = bins.all_count[chunk * SEARCH_CHUNK + i], m = bins.all_mass[chunk * SEARCH_CHUNK + i];
-            });
-            p.item = chunk * SEARCH_CHUNK + (p.item < 0 ? 0 : p.item);
+            Place p = warp_find<SEARCH_GROUPS / 32>(SEARCH_GROUPS, target, before, [&](int i) { return Part{sh.group_count[i], sh.group_mass[i]}; });
+            const int first = p.item * SEARCH_GROUP;
+            p = warp_find<1>(SEARCH_GROUP, target, p, [&](int i) { return Part{bins.all_count[first + i], bins.all_mass[first + i]}; });
+            p.item += first;
             if (threadIdx.x == 0) sh.place = p;
         }
         __syncthreads();
@@ -385,8 +557,9 @@ template <int DTYPE> struct Search {
     }
     __device__ void fill_depths()
     {
+        if (depths) return;
         clear();
-        each([&](float z) {
+        each([&](float z, int32_t) {
             if (z == -INFINITY) return;
             const double d = top - (double)z;
             const int b = depth_bin(d);
@@ -396,39 +569,77 @@ template <int DTYPE> struct Search {
                 atomicAdd(&bins.count[b], 1u);               // too deep for any mass
         });
         join([&](int i) { return exp(-(i / scale) * per_nat); });
+        depths = true;
     }
-    // The number that holds the border; the whole CTA, and the whole cluster in step.
-    __device__ Number find(const Target &target)
+    // The elements that `takes` accepts, MOST at most, sorted, in every CTA of the cluster, with the masses up to each behind `before`.
+    template <typename Takes> __device__ int make_list(double before, Takes &&takes)
+    {
+        if (threadIdx.x == 0) sh.listed = 0;
+        __syncthreads();
+        each([&](float z, int32_t token) {
+            if (z == -INFINITY || !takes(z)) return;
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (PPOW_CHECK(at < MOST, 803, nullptr)) (ctas == 1 ? bins.list : bins.own)[at] = list_entry(z, token);
+        });
+        meet(cluster, ctas);
+        int n = 0;
+        if (ctas > 1) {
+            int first = 0;
+            for (int r = 0; r < ctas; ++r) {
+                const int c = (int)*of(&sh.listed, r);
+                if (r < rank) first += c;
+                n += c;
+            }
+            const int mine = (int)sh.listed;
+            for (int r = 0; r < ctas; ++r) {
+                unsigned long long *list = of(bins.list, r);
+                for (int i = threadIdx.x; i < mine; i += THREADS)
+                    if (PPOW_CHECK(first + i < MOST, 804, nullptr)) list[first + i] = bins.own[i];
+            }
+            cluster.sync();
+        } else {
+            n = (int)sh.listed;
+        }
+        sort_list<THREADS>(bins.list, n);
+        add_up_list<THREADS>(bins.list, bins.mass, n, before, sh, [&](float z) { return weight(z); });
+        return n;
+    }
+    // The element on the border; the whole CTA, and the whole cluster in step.
+    __device__ Element find(const Target &target)
     {
         fill_depths();
         Place p = find_bin(target, Place{0, 0, 0.0});
         const int bin = p.item;
+        if (bins.all_count[bin] <= MOST) {
+            const int n = make_list(p.mass, [&](float z) { return depth_bin(top - (double)z) == bin; });
+            return find_in_list<THREADS>(bins.list, bins.mass, n, p.count, target, sh);
+        }
         const bool massless = bin == SEARCH_BINS - 1;
         const double bin_top = bin / scale, unit = massless ? 0.0 : exp(-bin_top * per_nat);
         // keys in the bin
+        depths = false;
         if (threadIdx.x == 0) sh.low_key = 0xffffffffu, sh.high_key = 0;
         meet(cluster, ctas);
         uint32_t lo = 0xffffffffu, hi = 0;
-        each([&](float z) {
+        each([&](float z, int32_t) {
             if (z == -INFINITY || depth_bin(top - (double)z) != bin) return;
             const uint32_t k = key_of(z);
             lo = min(lo, k), hi = max(hi, k);
         });
         lo = __reduce_min_sync(0xffffffffu, lo), hi = __reduce_max_sync(0xffffffffu, hi);
-        if ((threadIdx.x & 31) == 0) {
+        if ((threadIdx.x & 31) == 0)
             for (int r = 0; r < ctas; ++r) {
-                SampleShared *s = ctas == 1 ? &sh : cluster.map_shared_rank(&sh, r);
+                SampleShared *s = of(&sh, r);
                 atomicMin(&s->low_key, lo);
                 atomicMax(&s->high_key, hi);
             }
-        }
         meet(cluster, ctas);
         lo = sh.low_key, hi = sh.high_key;
         int shift = 0;
         while (((hi - lo) >> shift) >= SEARCH_BINS) ++shift;
         for (;;) {
             clear();
-            each([&](float z) {
+            each([&](float z, int32_t) {
                 if (z == -INFINITY) return;
                 const uint32_t k = key_of(z);
                 if (k < lo || k > hi) return;
@@ -445,40 +656,33 @@ template <int DTYPE> struct Search {
             if (shift == 0) break;
             const uint32_t width = (1u << shift) - 1;
             lo = hi - lo > width ? hi - width : lo;
-            shift = shift > 11 ? shift - 11 : 0;
+            shift = 0;
+            while (((hi - lo) >> shift) >= SEARCH_BINS) ++shift;
         }
-        Number found;
-        found.value = float_of(hi);
-        found.have = bins.all_count[p.item];
-        found.before = p.count;
-        found.mass = p.mass;
-        found.weight = massless ? 0.0 : weight(top - (double)found.value);
-        if (massless)
-            found.rank = target.kind == Border::Count ? min(target.count - p.count, found.have) - 1 : 0;
-        else
-            found.choose(target);
+        const float value = float_of(hi);
+        const uint32_t have = bins.all_count[p.item];
         __syncthreads();
-        return found;
+        if (massless && target.kind != Border::Count) return {value, p.count + 1, p.mass, -1, 0, have};
+        return choose(target, p, value, have, massless ? 0.0 : weight(value));
     }
     __device__ void run(int64_t row)
     {
-        if (threadIdx.x == 0) sh.max_key = sh.none = sh.flags = sh.within = 0;
+        if (threadIdx.x == 0) sh.top = sh.none = sh.flags = sh.within = 0;
         meet(cluster, ctas);
         uint32_t most = 0, none = 0, bad = 0;
-        each([&](float z) {
+        each([&](float z, int32_t) {
             bad |= !(z < INFINITY);
             none += z == -INFINITY;
             most = max(most, key_of(z));
         });
         most = __reduce_max_sync(0xffffffffu, most), none = __reduce_add_sync(0xffffffffu, none), bad = __reduce_or_sync(0xffffffffu, bad);
-        if ((threadIdx.x & 31) == 0) {
+        if ((threadIdx.x & 31) == 0)
             for (int r = 0; r < ctas; ++r) {
-                SampleShared *s = ctas == 1 ? &sh : cluster.map_shared_rank(&sh, r);
-                atomicMax(&s->max_key, most);
+                SampleShared *s = of(&sh, r);
+                atomicMax(&s->top, most);
                 atomicAdd(&s->none, none);
                 if (bad) atomicOr(&s->flags, (uint32_t)SAMPLE_BAD);
             }
-        }
         meet(cluster, ctas);
         const uint32_t F = (uint32_t)piece.units * E - sh.none;
         const bool lead = rank == 0 && threadIdx.x == 0;
@@ -490,38 +694,54 @@ template <int DTYPE> struct Search {
             }
             return;
         }
-        top = (double)float_of(sh.max_key);
+        top = (double)float_of(sh.top);
         per_nat = 1.0 / job.temperature;
         scale = (SEARCH_BINS - 1) / (SEARCH_NATS * job.temperature);
-        if (job.min_p > 0.0) {
-            uint32_t within = 0;
-            each([&](float z) { within += z > -INFINITY && weight(top - (double)z) >= job.min_p; });
-            within = __reduce_add_sync(0xffffffffu, within);
-            if ((threadIdx.x & 31) == 0)
-                for (int r = 0; r < ctas; ++r) atomicAdd(&(ctas == 1 ? &sh : cluster.map_shared_rank(&sh, r))->within, within);
-        }
-        fill_depths();
-        uint32_t massive = F - bins.all_count[SEARCH_BINS - 1];
-        double all = 0.0;
-        for (int c = 0; c < SEARCH_CHUNKS; ++c) all += sh.chunk_mass[c];
-        const uint32_t within = sh.within;
-        __syncthreads();
-        Number drawn;
+        depths = false;
+        Element drawn;
         uint32_t n;
         double total;
-        decide(job, job.uniforms[row], F, massive, all, within, [&](const Target &t) { return find(t); }, drawn, n, total);
+        if (F <= MOST) {
+            const int listed = make_list(0.0, [&](float) { return true; });
+            uint32_t within = 0;
+            if (job.min_p > 0.0) {
+                for (int i = threadIdx.x; i < listed; i += THREADS) within += weight(list_value(bins.list[i])) >= job.min_p;
+                within = __reduce_add_sync(0xffffffffu, within);
+                if ((threadIdx.x & 31) == 0) atomicAdd(&sh.within, within);
+                __syncthreads();
+                within = sh.within;
+            }
+            decide(job, job.uniforms[row], F, F, bins.mass[listed - 1], within,
+                   [&](const Target &t) { return find_in_list<THREADS>(bins.list, bins.mass, listed, 0, t, sh); }, drawn, n, total);
+        } else {
+            if (job.min_p > 0.0) {
+                uint32_t within = 0;
+                each([&](float z, int32_t) { within += z > -INFINITY && weight(z) >= job.min_p; });
+                within = __reduce_add_sync(0xffffffffu, within);
+                if ((threadIdx.x & 31) == 0)
+                    for (int r = 0; r < ctas; ++r) atomicAdd(&of(&sh, r)->within, within);
+            }
+            fill_depths();                   // all threads of the row meet in it
+            const uint32_t massive = F - bins.all_count[SEARCH_BINS - 1], within = sh.within;
+            double all = 0.0;
+            for (int c = 0; c < SEARCH_GROUPS; ++c) all += sh.group_mass[c];
+            __syncthreads();
+            decide(job, job.uniforms[row], F, massive, all, within, [&](const Target &t) { return find(t); }, drawn, n, total);
+        }
         if (lead) {
             job.logp[row] = (float)(((double)drawn.value - top) * per_nat - log(total));
             if (job.kept) job.kept[row] = (int32_t)n;
+            if (drawn.token >= 0) job.tokens[row] = drawn.token;
         }
-        // which piece holds it
+        if (drawn.token >= 0) return;
+        // one of many equal ones: which piece holds it, and where
         const uint32_t key = key_of(drawn.value);
         auto matches = [&](const uint4 &w) {
             float z[E];
             S::unpack(w, z);
             uint32_t bits = 0;
 #pragma unroll
-            for (int e = 0; e < E; ++e) bits |= (z[e] > -INFINITY && key_of(z[e]) == key) ? 1u << e : 0u;
+            for (int e = 0; e < E; ++e) bits |= (z[e] > -INFINITY && key_of(z[e]) == key) ? 1u << (E == 8 ? e / 2 + e % 2 * 16 : e) : 0u;
             return bits;
         };
         uint32_t skip = 0, have = 0xffffffffu;
@@ -529,71 +749,99 @@ template <int DTYPE> struct Search {
             if (threadIdx.x == 0) sh.here = 0;
             __syncthreads();
             uint32_t mine = 0;
-            for (int32_t u = piece.begin + (int32_t)threadIdx.x; u < piece.end; u += SAMPLE_THREADS) mine += __popc(matches(piece.load(u)));
+            for (int32_t u = piece.begin + (int32_t)threadIdx.x; u < piece.end; u += THREADS) mine += __popc(matches(piece.load(u)));
             mine = __reduce_add_sync(0xffffffffu, mine);
             if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&sh.here, mine);
             cluster.sync();
-            for (int r = 0; r < rank; ++r) skip += cluster.map_shared_rank(&sh, r)->here;
+            for (int r = 0; r < rank; ++r) skip += of(&sh, r)->here;
             have = sh.here;
         }
-        if (drawn.rank >= skip && drawn.rank - skip < have) locate(piece, drawn.rank - skip, sh, job.tokens + row, matches);
+        if (drawn.rank >= skip && drawn.rank - skip < have) locate<THREADS>(piece, drawn.rank - skip, sh, job.tokens + row, matches);
     }
 };
 
-template <int DTYPE>
+template <int DTYPE, int THREADS, int SEARCH_BINS>
 __device__ __noinline__ void search_row(const SampleJob &job, int64_t row, int rank, int ctas, SampleShared &sh, void *smem)
 {
     const Piece<DTYPE> piece(job, row, rank, ctas);
     const cg::cluster_group cluster = cg::this_cluster();
-    Search<DTYPE> s{job, piece, cluster, rank, ctas, sh, *static_cast<SearchBins *>(smem), 0.0, 0.0, 0.0};
+    Search<DTYPE, THREADS, SEARCH_BINS> s{job, piece, cluster, rank, ctas, sh, *static_cast<SearchBins<SEARCH_BINS> *>(smem), 0.0, 0.0, 0.0, false};
     s.run(row);
 }
 
-__global__ void __launch_bounds__(SAMPLE_THREADS) sample_search_kernel(const SampleJob job)
+template <int DTYPE, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_search_kernel(const SampleJob job)
 {
     wait_for_previous_kernel();
     extern __shared__ uint4 sample_smem[];
     __shared__ SampleShared sh;
     const cg::cluster_group cluster = cg::this_cluster();
     const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    search_row<PPOW_F32>(job, blockIdx.x / ctas, rank, ctas, sh, sample_smem);
+    search_row<DTYPE, THREADS, LIST>(job, blockIdx.x / ctas, rank, ctas, sh, sample_smem);
     if (ctas > 1) cluster.sync();            // no CTA leaves while another still reads its shared memory
 }
 
 // ---- counting: 16-bit rows --------------------------------------------------------------------------
 template <int DTYPE> struct Count {
     using F = Counted<DTYPE>;
-    static constexpr int CHUNKS = F::BINS / CHUNK;
-    uint32_t *words;         // two bins each
+    static constexpr uint32_t NEG_INF = 0x8000u | F::INF;
+    // what of (magnitude - LOW) is beyond WORDS: its bits in either half (bfloat16), or the top bit of a sum (float16)
+    static constexpr uint32_t OFFSET = DTYPE == PPOW_BF16 ? 0u - F::LOW * 0x10001u : (0x8000u - F::WORDS) * 0x10001u;
+    static constexpr uint32_t BEYOND = DTYPE == PPOW_BF16 ? (0xffffu - F::MASK) * 0x10001u : 0x80008000u;
+    static constexpr bool ZEROS = F::LOW > 0;                // counted apart
+    char *words;
+    uint32_t none = 0, low = 0, zeros = 0, flags = 0, most = NEG_INF * 0x10001u;
 
-    __device__ __forceinline__ void add(uint32_t key, uint32_t &none, uint32_t &low, uint32_t &flags)
+    // 1 in the low half for a positive number, in the high half for a negative one: copies of the sign in two bytes, and 1.
+    template <int SELECT> static __device__ __forceinline__ uint32_t one(uint32_t w)
     {
-        const uint32_t bin = key - F::BASE;
-        if (bin < F::BINS) {
-            atomicAdd(&words[bin >> 1], 1u << ((bin & 1) * 16));
-        } else if (key == F::LOWEST) {
-            ++none;
-        } else if (key < F::LOWEST || key >= F::HIGHEST) {
-            flags |= SAMPLE_BAD;
-        } else if (key < F::BASE) {
-            ++low;
+        uint32_t signs;
+        asm("prmt.b32 %0, %1, 0, %2;" : "=r"(signs) : "r"(w), "n"(SELECT));
+        return signs + 1u;
+    }
+    __device__ __forceinline__ void low_half(uint32_t w) { atomicAdd(reinterpret_cast<uint32_t *>(words + (w << 2 & F::MASK << 2)), one<0x4499>(w)); }
+    __device__ __forceinline__ void high_half(uint32_t w) { atomicAdd(reinterpret_cast<uint32_t *>(words + (w >> 14 & F::MASK << 2)), one<0x44bb>(w)); }
+    // Not zero if a half may be beyond the counted range (a borrow from the low half can only add to what it says of the high one).
+    static __device__ __forceinline__ uint32_t beyond(uint32_t w) { return ((w & 0x7fff7fffu) + OFFSET) & BEYOND; }
+
+    // Eight logits.  Bound by the integer units (4 operations a logit) and the additions in shared memory: nothing is looked at one by one
+    // where all eight are in range.
+    __device__ __forceinline__ void add(const uint4 &w)
+    {
+        most = F::most(most, F::most(F::most(w.x, w.y), F::most(w.z, w.w)));
+        if ((beyond(w.x) | beyond(w.y) | beyond(w.z) | beyond(w.w)) == 0) {
+            low_half(w.x), high_half(w.x), low_half(w.y), high_half(w.y);
+            low_half(w.z), high_half(w.z), low_half(w.w), high_half(w.w);
         } else {
-            flags |= SAMPLE_ODD;
+            for (const uint32_t v : {w.x, w.y, w.z, w.w}) {
+                if (in_range(v & 0x7fffu)) low_half(v); else beyond_one(v & 0xffffu);
+                if (in_range(v >> 16 & 0x7fffu)) high_half(v); else beyond_one(v >> 16);
+            }
         }
     }
-    __device__ __forceinline__ void add_word(uint32_t w, uint32_t &none, uint32_t &low, uint32_t &flags)
+    static __device__ __forceinline__ bool in_range(uint32_t magnitude) { return magnitude - F::LOW < F::WORDS; }
+    __device__ __forceinline__ void beyond_one(uint32_t bits)
     {
-        const uint32_t sign = w & 0x80008000u, keys = w ^ (sign - (sign >> 15)) ^ 0x80008000u;
-        add(keys & 0xffffu, none, low, flags);
-        add(keys >> 16, none, low, flags);
+        const uint32_t magnitude = bits & 0x7fffu;
+        none += bits == NEG_INF;
+        zeros += magnitude == 0;
+        if (bits != NEG_INF && magnitude != 0) {
+            if (magnitude >= F::INF)
+                flags |= SAMPLE_BAD;
+            else if (bits & 0x8000u && magnitude > F::WORDS)
+                ++low;
+            else
+                flags |= SAMPLE_ODD;
+        }
     }
 };
 
 template <int DTYPE>
-__global__ void __launch_bounds__(SAMPLE_THREADS) sample_count_kernel(const SampleJob job)
+__global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS) sample_count_kernel(const SampleJob job)
 {
     using F = Counted<DTYPE>;
-    using C = Count<DTYPE>;
+    constexpr int THREADS = F::THREADS;
+    using G = Groups<DTYPE>;
     extern __shared__ uint4 sample_smem[];
     __shared__ SampleShared sh;
     wait_for_previous_kernel();
@@ -602,221 +850,212 @@ __global__ void __launch_bounds__(SAMPLE_THREADS) sample_count_kernel(const Samp
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = blockIdx.x / ctas;
     const Piece<DTYPE> piece(job, row, rank, ctas);
-    C bins{reinterpret_cast<uint32_t *>(sample_smem)};
-    for (int i = threadIdx.x; i < (int)F::BINS / 8; i += SAMPLE_THREADS) sample_smem[i] = make_uint4(0, 0, 0, 0);
-    if (threadIdx.x == 0) sh.none = sh.low = sh.flags = 0;
-    __syncthreads();
+    auto of = [&](auto *p, int r) { return ctas == 1 ? p : cluster.map_shared_rank(p, r); };
+    constexpr int DEEP = 4;
+    uint4 w[DEEP];
+    auto fetch = [&](int32_t u0) {
+#pragma unroll
+        for (int q = 0; q < DEEP; ++q)
+            if (u0 + q * THREADS < piece.end) w[q] = piece.load(u0 + q * THREADS);
+    };
+    fetch(piece.begin + (int32_t)threadIdx.x);
+    for (int i = threadIdx.x; i < (int)F::WORDS / 4; i += THREADS) sample_smem[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < G::ALL; i += THREADS) sh.group_count[i] = 0, sh.group_mass[i] = 0.0;
+    if (threadIdx.x == 0) sh.none = sh.low = sh.zeros = sh.flags = sh.within = sh.top = 0;
+    meet(cluster, ctas);                     // the others write into these
     {
-        uint32_t none = 0, low = 0, flags = 0;
-        constexpr int DEEP = 4;
-        for (int32_t u0 = piece.begin + (int32_t)threadIdx.x; u0 < piece.end; u0 += SAMPLE_THREADS * DEEP) {
-            uint4 w[DEEP];
+        Count<DTYPE> count{reinterpret_cast<char *>(sample_smem)};
+        for (int32_t u0 = piece.begin + (int32_t)threadIdx.x; u0 < piece.end; u0 += THREADS * DEEP) {
+            uint4 now[DEEP];
+#pragma unroll
+            for (int q = 0; q < DEEP; ++q) now[q] = w[q];
+            fetch(u0 + THREADS * DEEP);
 #pragma unroll
             for (int q = 0; q < DEEP; ++q)
-                if (u0 + q * SAMPLE_THREADS < piece.end) w[q] = piece.load(u0 + q * SAMPLE_THREADS);
+                if (u0 + q * THREADS < piece.end) count.add(now[q]);
+        }
+        const uint32_t none = __reduce_add_sync(0xffffffffu, count.none), low = __reduce_add_sync(0xffffffffu, count.low),
+                       zeros = __reduce_add_sync(0xffffffffu, count.zeros), flags = __reduce_or_sync(0xffffffffu, count.flags);
+        const uint32_t top = __reduce_max_sync(0xffffffffu, max(key_of(Storage<DTYPE>::get((uint16_t)count.most)),
+                                                                key_of(Storage<DTYPE>::get((uint16_t)(count.most >> 16)))));
+        if (lane == 0)
+            for (int r = 0; r < ctas; ++r) {
+                SampleShared *s = of(&sh, r);
+                if (none) atomicAdd(&s->none, none);
+                if (low) atomicAdd(&s->low, low);
+                if (zeros) atomicAdd(&s->zeros, zeros);
+                if (flags) atomicOr(&s->flags, flags);
+                atomicMax(&s->top, top);
+            }
+    }
+    meet(cluster, ctas);
+    const double per_nat = 1.0 / job.temperature, top = (double)float_of(sh.top);
+    const uint32_t none = sh.none, low = sh.low;
+    {
+        // Each CTA adds up a share of the groups for all, in its own words: the other CTAs read none of those.
+        const int from = G::SIDE * rank / ctas, to = G::SIDE * (rank + 1) / ctas;
+        uint32_t over = 0, within = 0;
+        for (int g = from + warp; g < to; g += THREADS / 32) {
+            const int at = G::word(g) / 4 + lane;
+            const uint4 own = sample_smem[at];
+            if (ctas == 1 && !__any_sync(0xffffffffu, own.x | own.y | own.z | own.w)) continue;
+            uint32_t b[2][4] = {{own.x & 0xffffu, own.y & 0xffffu, own.z & 0xffffu, own.w & 0xffffu}, {own.x >> 16, own.y >> 16, own.z >> 16, own.w >> 16}};
+            for (int r = 1; r < ctas; ++r) {
+                const uint4 o = cluster.map_shared_rank(sample_smem, rank + r < ctas ? rank + r : rank + r - ctas)[at];
+                b[0][0] += o.x & 0xffffu, b[0][1] += o.y & 0xffffu, b[0][2] += o.z & 0xffffu, b[0][3] += o.w & 0xffffu;
+                b[1][0] += o.x >> 16, b[1][1] += o.y >> 16, b[1][2] += o.z >> 16, b[1][3] += o.w >> 16;
+            }
+            if (!Count<DTYPE>::ZEROS && at == 0) b[0][0] += b[1][0], b[1][0] = 0;        // -0 is +0
+            if (ctas > 1 || (!Count<DTYPE>::ZEROS && g == 0)) {
+                sample_smem[at] = make_uint4(b[0][0] | b[1][0] << 16, b[0][1] | b[1][1] << 16, b[0][2] | b[1][2] << 16, b[0][3] | b[1][3] << 16);
+                over |= b[0][0] | b[0][1] | b[0][2] | b[0][3] | b[1][0] | b[1][1] | b[1][2] | b[1][3];
+            }
 #pragma unroll
-            for (int q = 0; q < DEEP; ++q)
-                if (u0 + q * SAMPLE_THREADS < piece.end) {
-                    bins.add_word(w[q].x, none, low, flags);
-                    bins.add_word(w[q].y, none, low, flags);
-                    bins.add_word(w[q].z, none, low, flags);
-                    bins.add_word(w[q].w, none, low, flags);
+            for (int side = 0; side < 2; ++side) {
+                const uint32_t have = b[side][0] + b[side][1] + b[side][2] + b[side][3];
+                if (!__any_sync(0xffffffffu, have != 0)) continue;
+                const int group = side ? G::ZERO + 1 + g : g;
+                double mass = 0.0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const double e = exp(((double)G::number(group, lane * 4 + i) - top) * per_nat);
+                    mass += b[side][i] ? b[side][i] * e : 0.0;   // beyond the maximum e may overflow, with nothing to count
+                    within += e >= job.min_p ? b[side][i] : 0u;
                 }
+                mass = warp_sum_f64(mass);
+                const uint32_t counted = __reduce_add_sync(0xffffffffu, have);
+                for (int r = lane; r < ctas; r += 32) {
+                    SampleShared *s = of(&sh, r);
+                    s->group_count[group] = counted;
+                    s->group_mass[group] = mass;
+                }
+            }
         }
-        none = __reduce_add_sync(0xffffffffu, none), low = __reduce_add_sync(0xffffffffu, low), flags = __reduce_or_sync(0xffffffffu, flags);
-        if (lane == 0) {
-            if (none) atomicAdd(&sh.none, none);
-            if (low) atomicAdd(&sh.low, low);
-            if (flags) atomicOr(&sh.flags, flags);
+        if (Count<DTYPE>::ZEROS && threadIdx.x == 0 && sh.zeros > 0) {       // every CTA for itself
+            const double e = exp(-top * per_nat);
+            sh.group_count[G::ZERO] = sh.zeros;
+            sh.group_mass[G::ZERO] = sh.zeros * e;
+            if (rank == 0 && e >= job.min_p) within += sh.zeros;
         }
+        within = __reduce_add_sync(0xffffffffu, within);
+        over = __reduce_or_sync(0xffffffffu, over) >> 16;
+        if (lane == 0)
+            for (int r = 0; r < ctas; ++r) {
+                if (within) atomicAdd(&of(&sh, r)->within, within);
+                if (over) atomicOr(&of(&sh, r)->flags, (uint32_t)SAMPLE_ODD);
+            }
     }
     meet(cluster, ctas);
-    // Each CTA adds up a share of the chunks for all, in its own bins: the other CTAs read none of those.
-    const int from = C::CHUNKS * rank / ctas, to = C::CHUNKS * (rank + 1) / ctas;
-    for (int c = from + warp; c < to; c += SAMPLE_WARPS) {
-        const int at = c * (CHUNK / 8) + lane;
-        uint4 w = sample_smem[at];
-        uint32_t b[8] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16, w.z & 0xffffu, w.z >> 16, w.w & 0xffffu, w.w >> 16};
-        for (int r = 1; r < ctas; ++r) {
-            const uint4 o = cluster.map_shared_rank(sample_smem, (rank + r) % ctas)[at];
-            b[0] += o.x & 0xffffu, b[1] += o.x >> 16, b[2] += o.y & 0xffffu, b[3] += o.y >> 16;
-            b[4] += o.z & 0xffffu, b[5] += o.z >> 16, b[6] += o.w & 0xffffu, b[7] += o.w >> 16;
-        }
-        if (c == (int)F::ZERO / CHUNK) {                     // -0 to +0
-            constexpr int LANE = F::ZERO % CHUNK / 8, SLOT = F::ZERO % 8;
-            static_assert(SLOT == 0, "+0 is the first of its lane's bins, -0 the last of the lane before");
-            const uint32_t minus = __shfl_sync(0xffffffffu, b[7], LANE - 1);
-            if (lane == LANE) b[0] += minus;
-            if (lane == LANE - 1) b[7] = 0;
-        }
-        uint32_t count = 0, over = 0;
-        int32_t top = -1;
+    auto owner = [&](int side) {             // the CTA that added this group up
+        int r = 0;
+        while (G::SIDE * (r + 1) / ctas <= side) ++r;
+        return r;
+    };
+    if (warp == 0) {
+        constexpr int PER = (G::ALL + 31) / 32;
+        uint32_t counted = 0, flags = sh.flags;
+        double all = 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            count += b[i];
-            over |= b[i] >> 16;
-            if (b[i]) top = c * CHUNK + lane * 8 + i;
+        for (int i = 0; i < PER; ++i) {
+            const int g = lane + 32 * i;
+            if (g < G::ALL) counted += sh.group_count[g], all += sh.group_mass[g];
         }
-        if (__any_sync(0xffffffffu, over != 0) && lane == 0) atomicOr(&sh.flags, (uint32_t)SAMPLE_ODD);
-        if (ctas > 1 || c == (int)F::ZERO / CHUNK)
-            sample_smem[at] = make_uint4(b[0] | (b[1] << 16), b[2] | (b[3] << 16), b[4] | (b[5] << 16), b[6] | (b[7] << 16));
-        count = __reduce_add_sync(0xffffffffu, count);
-        top = __reduce_max_sync(0xffffffffu, top);
-        for (int r = lane; r < ctas; r += 32) {
-            SampleShared *s = ctas == 1 ? &sh : cluster.map_shared_rank(&sh, r);
-            s->chunk_count[c] = count;
-            s->chunk_top[c] = top;
+        counted = __reduce_add_sync(0xffffffffu, counted);
+        all = warp_sum_f64(all);
+        // a count that ran over left a sum that is short; numbers below the counted range have to be too deep for any mass
+        if (counted + none + low != (uint32_t)piece.units * 8) flags |= SAMPLE_ODD;
+        if (low > 0) {
+            const double deep = (top + F::LIMIT) * per_nat;
+            if (counted == 0 || deep < SEARCH_NATS || (job.min_p > 0.0 && exp(-deep) >= job.min_p)) flags |= SAMPLE_ODD;
         }
-    }
-    meet(cluster, ctas);
-    uint32_t none = 0, low = 0, flags = 0, counted = 0;
-    int32_t top_bin = -1;
-    for (int r = 0; r < ctas; ++r) {
-        const SampleShared *s = ctas == 1 ? &sh : cluster.map_shared_rank(&sh, r);
-        none += s->none, low += s->low, flags |= s->flags;
-    }
-    for (int c = lane; c < C::CHUNKS; c += 32) counted += sh.chunk_count[c], top_bin = max(top_bin, sh.chunk_top[c]);
-    counted = __reduce_add_sync(0xffffffffu, counted);
-    top_bin = __reduce_max_sync(0xffffffffu, top_bin);
-    const double top = top_bin < 0 ? 0.0 : (double)number_of<DTYPE>((uint32_t)top_bin), per_nat = 1.0 / job.temperature;
-    // a count that ran over left a sum that is short; numbers below the counted range have to be too deep for any mass
-    if (counted + none + low != (uint32_t)piece.units * 8) flags |= SAMPLE_ODD;
-    if (low > 0) {
-        const double deep = (top + F::LIMIT) * per_nat;
-        if (top_bin < 0 || deep < SEARCH_NATS || (job.min_p > 0.0 && exp(-deep) >= job.min_p)) flags |= SAMPLE_ODD;
-    }
-    if (flags || counted == 0) {                             // the same for all CTAs of the row
-        if (flags & SAMPLE_BAD || (flags == 0 && counted == 0)) {
-            if (rank == 0 && threadIdx.x == 0) {
+        if (flags == 0 && counted > 0) {
+            auto find = [&](const Target &target) {
+                Place p = warp_find<PER>(G::ALL, target, Place{0, 0, 0.0}, [&](int i) { return Part{sh.group_count[G::at(i)], sh.group_mass[G::at(i)]}; });
+                const int group = G::at(p.item);
+                if (group == G::ZERO) return choose(target, p, 0.0f, sh.zeros, exp(-top * per_nat));
+                const uint32_t *counts = reinterpret_cast<const uint32_t *>(of(&sample_smem[0], owner(G::side(group)))) + G::word(G::side(group));
+                auto place = [&](int i) { return G::negative(group) ? i : GROUP - 1 - i; };
+                auto count_at = [&](int i) { return G::negative(group) ? counts[place(i)] >> 16 : counts[place(i)] & 0xffffu; };
+                auto weight_at = [&](int i) { return exp(((double)G::number(group, place(i)) - top) * per_nat); };
+                p = warp_find<GROUP / 32>(GROUP, target, p, [&](int i) {
+                    const uint32_t c = count_at(i);
+                    const double e = weight_at(i);
+                    return Part{c, c ? c * e : 0.0};         // beyond the maximum e may overflow
+                });
+                return choose(target, p, G::number(group, place(p.item)), count_at(p.item), weight_at(p.item));
+            };
+            Element drawn;
+            uint32_t n;
+            double total;
+            decide(job, job.uniforms[row], counted + low, counted, all, sh.within, find, drawn, n, total);
+            if (lane == 0) {
+                if (rank == 0) {
+                    job.logp[row] = (float)(((double)drawn.value - top) * per_nat - log(total));
+                    if (job.kept) job.kept[row] = (int32_t)n;
+                }
+                sh.drawn = drawn;
+            }
+        } else if (lane == 0) {
+            if (rank == 0 && (flags & SAMPLE_BAD || flags == 0)) {
                 job.tokens[row] = -1;
                 job.logp[row] = flags ? NAN : -INFINITY;
                 if (job.kept) job.kept[row] = 0;
             }
-            meet(cluster, ctas);
-        } else {
-            meet(cluster, ctas);             // everybody has read what the search writes over
-            search_row<DTYPE>(job, row, rank, ctas, sh, sample_smem);
+            sh.drawn.n = 0;
+            sh.drawn.rank = flags;
+        }
+    }
+    __syncthreads();
+    const Element drawn = sh.drawn;
+    if (drawn.n == 0) {                      // the same for all CTAs of the row
+        const bool odd = drawn.rank == SAMPLE_ODD;
+        meet(cluster, ctas);                 // everybody has read what the search writes over
+        if (odd) {
+            search_row<DTYPE, THREADS, 1024>(job, row, rank, ctas, sh, sample_smem);
             meet(cluster, ctas);
         }
         return;
     }
-    for (int c = from + warp; c < to; c += SAMPLE_WARPS) {
-        if (sh.chunk_count[c] == 0) continue;
-        const uint4 w = sample_smem[c * (CHUNK / 8) + lane];
-        const uint32_t b[8] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16, w.z & 0xffffu, w.z >> 16, w.w & 0xffffu, w.w >> 16};
-        double mass = 0.0;
-        uint32_t within = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (b[i]) {
-                const double e = exp(((double)number_of<DTYPE>((uint32_t)(c * CHUNK + lane * 8 + i)) - top) * per_nat);
-                mass += b[i] * e;
-                if (e >= job.min_p) within += b[i];
-            }
-        mass = warp_sum_f64(mass);
-        within = __reduce_add_sync(0xffffffffu, within);
-        for (int r = lane; r < ctas; r += 32) {
-            SampleShared *s = ctas == 1 ? &sh : cluster.map_shared_rank(&sh, r);
-            s->chunk_mass[c] = mass;
-            s->chunk_within[c] = within;
-        }
-    }
-    meet(cluster, ctas);
-    if (warp == 0) {
-        uint32_t within = 0;
-        double all = 0.0;
-        for (int c = lane; c < C::CHUNKS; c += 32)
-            if (sh.chunk_count[c]) within += sh.chunk_within[c], all += sh.chunk_mass[c];
-        within = __reduce_add_sync(0xffffffffu, within);
-        all = warp_sum_f64(all);
-        auto owner = [&](int chunk) {        // the CTA that added this chunk up
-            int r = 0;
-            while (C::CHUNKS * (r + 1) / ctas <= chunk) ++r;
-            return r;
-        };
-        auto find = [&](const Target &target) {
-            Place p = warp_find(C::CHUNKS, target, Place{0, 0, 0.0}, [&](int i, uint32_t &c, double &m) {
-                const int chunk = C::CHUNKS - 1 - i;
-                c = sh.chunk_count[chunk];
-                m = c ? sh.chunk_mass[chunk] : 0.0;
-            });
-            const int chunk = C::CHUNKS - 1 - max(p.item, 0);
-            const uint4 *remote = ctas == 1 ? sample_smem : cluster.map_shared_rank(sample_smem, owner(chunk));
-            const uint16_t *counts = reinterpret_cast<const uint16_t *>(remote + chunk * (CHUNK / 8));
-            auto weight = [&](int bin) { return exp(((double)number_of<DTYPE>((uint32_t)bin) - top) * per_nat); };
-            p = warp_find(CHUNK, target, p, [&](int i, uint32_t &c, double &m) {
-                c = counts[CHUNK - 1 - i];
-                m = c ? c * weight(chunk * CHUNK + CHUNK - 1 - i) : 0.0;
-            });
-            const int item = CHUNK - 1 - max(p.item, 0);
-            Number found;
-            found.value = number_of<DTYPE>((uint32_t)(chunk * CHUNK + item));
-            found.have = counts[item];
-            found.before = p.count;
-            found.mass = p.mass;
-            found.weight = weight(chunk * CHUNK + item);
-            found.choose(target);
-            return found;
-        };
-        Number drawn;
-        uint32_t n;
-        double total;
-        decide(job, job.uniforms[row], counted + low, counted, all, within, find, drawn, n, total);
-        if (lane == 0) {
-            if (rank == 0) {
-                job.logp[row] = (float)(((double)drawn.value - top) * per_nat - log(total));
-                if (job.kept) job.kept[row] = (int32_t)n;
-            }
-            sh.drawn = drawn;
-        }
-    }
-    __syncthreads();
-    const Number drawn = sh.drawn;
-    // bits to look for; the zeros are one number
-    const uint32_t bits = drawn.value == 0.0f ? 0u : Storage<DTYPE>::put(drawn.value);
-    const uint32_t mask = bits ? 0xffffu : 0x7fffu, both = bits * 0x10001u, masks = mask * 0x10001u;
+    const uint32_t bits = Storage<DTYPE>::put(drawn.value), both = bits * 0x10001u;
+    auto matches = [&](const uint4 &w) {     // equality of numbers: the zeros are one
+        return (F::equal(w.x, both) & 0x00010001u) | (F::equal(w.y, both) & 0x00020002u) | (F::equal(w.z, both) & 0x00040004u) |
+               (F::equal(w.w, both) & 0x00080008u);
+    };
     uint32_t skip = 0, have = drawn.have;
-    if (ctas > 1) {
-        // how many of them each piece holds: the other CTAs' bins still tell; the owner's own are what is left of the sum
-        const uint32_t key = bits & 0x8000u ? 0xffffu - bits : bits | 0x8000u, bin = key - F::BASE;
-        const int chunk = (int)bin / CHUNK;
-        int owner = 0;
-        while (C::CHUNKS * (owner + 1) / ctas <= chunk) ++owner;
-        uint32_t others = 0, mine = 0, before = 0;
+    if (ctas > 1 && Count<DTYPE>::ZEROS && drawn.value == 0.0f) {
+        uint32_t mine = 0;                   // zeros have no word: counted here
+        for (int32_t u = piece.begin + (int32_t)threadIdx.x; u < piece.end; u += THREADS) mine += __popc(matches(piece.load(u)));
+        mine = __reduce_add_sync(0xffffffffu, mine);
+        if (threadIdx.x == 0) sh.here = 0;
+        __syncthreads();
+        if (lane == 0 && mine) atomicAdd(&sh.here, mine);
+        cluster.sync();
+        for (int r = 0; r < rank; ++r) skip += cluster.map_shared_rank(&sh, r)->here;
+        have = sh.here;
+    } else if (ctas > 1) {
+        // how many of them each piece holds: the other CTAs' words still tell; the owner's own are what is left of the sum
+        const uint32_t magnitude = bits & 0x7fffu;
+        const int own = owner((int)(magnitude - F::LOW) / GROUP);
+        uint32_t others = 0, mine = 0;
         for (int r = 0; r < ctas; ++r) {
-            if (r == owner) continue;
-            const uint16_t *counts = reinterpret_cast<const uint16_t *>(cluster.map_shared_rank(sample_smem, r));
-            const uint32_t c = counts[bin] + (bin == F::ZERO ? counts[bin - 1] : 0u);
+            if (r == own) continue;
+            const uint32_t word = reinterpret_cast<const uint32_t *>(cluster.map_shared_rank(&sample_smem[0], r))[magnitude & F::MASK];
+            const uint32_t c = magnitude == 0 ? (word & 0xffffu) + (word >> 16) : bits & 0x8000u ? word >> 16 : word & 0xffffu;
             others += c;
-            if (r < rank) before += c;
+            if (r < rank) skip += c;
             if (r == rank) mine = c;
         }
-        if (owner == rank) mine = drawn.have - others;
-        if (owner < rank) before += drawn.have - others;
-        skip = before;
-        have = mine;
+        if (own < rank) skip += drawn.have - others;
+        have = own == rank ? drawn.have - others : mine;
     }
-    if (drawn.rank >= skip && drawn.rank - skip < have)
-        locate(piece, drawn.rank - skip, sh, job.tokens + row, [&](const uint4 &w) {
-            const uint32_t x = (w.x & masks) ^ both, y = (w.y & masks) ^ both, z = (w.z & masks) ^ both, v = (w.w & masks) ^ both;
-            uint32_t m = 0;
-            m |= (x & 0xffffu) ? 0u : 1u;
-            m |= (x >> 16) ? 0u : 2u;
-            m |= (y & 0xffffu) ? 0u : 4u;
-            m |= (y >> 16) ? 0u : 8u;
-            m |= (z & 0xffffu) ? 0u : 16u;
-            m |= (z >> 16) ? 0u : 32u;
-            m |= (v & 0xffffu) ? 0u : 64u;
-            m |= (v >> 16) ? 0u : 128u;
-            return m;
-        });
+    if (drawn.rank >= skip && drawn.rank - skip < have) locate<THREADS>(piece, drawn.rank - skip, sh, job.tokens + row, matches);
     if (ctas > 1) cluster.sync();            // no CTA leaves while another still reads its shared memory
 }
 
 // ---- host side --------------------------------------------------------------------------------------
 namespace {
 
-template <auto kernel>
+template <auto kernel, int THREADS>
 bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     static std::atomic<bool> ready[DEVICES];
@@ -826,12 +1065,12 @@ bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units,
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
         ready[dev].store(true, std::memory_order_relaxed);
     }
-    // As many CTAs to a row as keep the device's places filled, each with 512 units or more.
+    // As many CTAs to a row as keep the device's places filled, each with 512 units or more; and no more than PIECE_MOST logits to one.
     int ctas = 1;
-    while (ctas < SAMPLE_CTAS && (int64_t)job.R * ctas * 2 <= 148 * per_sm && units / (ctas * 2) >= 512) ctas *= 2;
+    while (ctas < SAMPLE_CTAS && (((int64_t)job.R * ctas * 2 <= 148 * per_sm && units / (ctas * 2) >= 512) || job.V > (int64_t)PIECE_MOST * ctas)) ctas *= 2;
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3((unsigned)(job.R * ctas));
-    config.blockDim = dim3(SAMPLE_THREADS);
+    config.blockDim = dim3(THREADS);
     config.dynamicSmemBytes = smem;
     config.stream = stream;
     cudaLaunchAttribute attributes[2];
@@ -843,6 +1082,19 @@ bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units,
     config.attrs = attributes;
     config.numAttrs = 2;
     return cudaLaunchKernelEx(&config, kernel, job) == cudaSuccess;
+}
+
+template <int DTYPE> bool launch_search(const SampleJob &job, int32_t units, cudaStream_t stream)
+{
+    constexpr int THREADS = 512;
+    return sample_launch<sample_search_kernel<DTYPE, THREADS>, THREADS>(sizeof(SearchBins<LIST>), 1024 / THREADS, job, units, stream);
+}
+// A row that counting does not fit is searched in the same shared memory, with half the bins.
+template <int DTYPE> bool launch_count(const SampleJob &job, int32_t units, cudaStream_t stream)
+{
+    using F = Counted<DTYPE>;
+    static_assert(sizeof(SearchBins<1024>) <= F::WORDS * 4, "room for a search");
+    return sample_launch<sample_count_kernel<DTYPE>, F::THREADS>(F::WORDS * 4, F::CTAS, job, units, stream);
 }
 
 }  // namespace
@@ -872,8 +1124,12 @@ extern "C" ppow_status ppow_sample_tokens(const ppow_sample_params *params, cons
                            params->top_p, params->min_p,         tokens,   logp,      kept};
     const int32_t units = (int32_t)((params->V * (int64_t)es + 15) / 16);
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    const bool ok = params->dtype == PPOW_F32    ? sample_launch<sample_search_kernel>(sizeof(SearchBins), 4, job, units, stream)
-                    : params->dtype == PPOW_BF16 ? sample_launch<sample_count_kernel<PPOW_BF16>>(Counted<PPOW_BF16>::BINS * 2, 2, job, units, stream)
-                                                 : sample_launch<sample_count_kernel<PPOW_F16>>(Counted<PPOW_F16>::BINS * 2, 2, job, units, stream);
+    bool ok = false;
+    if (params->dtype == PPOW_F32)
+        ok = launch_search<PPOW_F32>(job, units, stream);
+    else if (params->dtype == PPOW_BF16)
+        ok = params->V <= LIST ? launch_search<PPOW_BF16>(job, units, stream) : launch_count<PPOW_BF16>(job, units, stream);
+    else
+        ok = params->V <= LIST ? launch_search<PPOW_F16>(job, units, stream) : launch_count<PPOW_F16>(job, units, stream);
     return ok ? PPOW_OK : PPOW_ERR_CUDA;
 }
