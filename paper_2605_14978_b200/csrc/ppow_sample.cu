@@ -82,6 +82,7 @@ template <int DTYPE> struct Groups {
     using F = Counted<DTYPE>;
     static constexpr int SIDE = F::WORDS / GROUP, ZERO = SIDE, ALL = 2 * SIDE + 1;
     static_assert(F::WORDS % GROUP == 0 && F::LOW % GROUP == 0, "whole groups");
+    static_assert(SIDE % SAMPLE_CTAS == 0, "equal shares");
     static __device__ __forceinline__ bool negative(int group) { return group > ZERO; }
     static __device__ __forceinline__ int side(int group) { return group > ZERO ? group - ZERO - 1 : group; }
     // first word of a group of either sign
@@ -142,77 +143,87 @@ template <int DTYPE> struct Piece {
 };
 
 // ---- borders ----------------------------------------------------------------------------------------
-enum class Border { Count, MassFrom, MassAbove };    // the first place where the count, or the mass, reaches `target`; the mass passes it
-
 struct Place {
     int item;
     uint32_t count;          // elements before it
     double mass;             // and their mass
 };
 
+// The first place where the count reaches `count`, the mass reaches `from` and passes `above`: one of the three is asked for, the
+// others hold everywhere (no branches: each row runs through this in one warp).
 struct Target {
-    Border kind;
     uint32_t count;
-    double mass;
-    __device__ __forceinline__ bool met(uint32_t c, double m) const
-    {
-        return kind == Border::Count ? c >= count : kind == Border::MassFrom ? m >= mass : m > mass;
-    }
+    double from, above;
+    static __device__ __forceinline__ Target at_count(uint32_t n) { return {n, -INFINITY, -INFINITY}; }
+    static __device__ __forceinline__ Target mass_from(double m) { return {0, m, -INFINITY}; }
+    static __device__ __forceinline__ Target mass_above(double m) { return {0, -INFINITY, m}; }
+    __device__ __forceinline__ bool by_count() const { return count > 0; }
+    __device__ __forceinline__ bool met(uint32_t c, double m) const { return (c >= count) & (m >= from) & (m > above); }
 };
 
-// The item of 0 .. n-1 (n <= 32 PER, descending) that holds the border; the last one that counts if rounding leaves it to none.
-// get(item): count and mass.  The whole warp calls, every lane has the result.
+// What lies up to each of the items 0 .. n-1 (n <= 32 PER, descending), PER neighbours to a lane, and the item that holds a border.  The
+// whole warp calls, every lane has the result.
 struct Part {
     uint32_t count;
     double mass;
 };
-template <int PER, typename Get> __device__ __forceinline__ Place warp_find(int n, const Target &target, const Place &before, Get &&get)
-{
-    const int lane = threadIdx.x & 31;
-    uint32_t c[PER], count = 0;
-    double m[PER], mass = 0.0;
+template <int PER> struct Scan {
+    uint32_t count[PER + 1];         // before the lane's first item; up to and with each
+    double mass[PER + 1];
+
+    // get(item): count and mass of one
+    template <typename Get> __device__ __forceinline__ Scan(int n, const Place &before, Get &&get)
+    {
+        const int lane = threadIdx.x & 31;
+        count[0] = 0;
+        mass[0] = 0.0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const bool in = lane * PER + i < n;
-        const Part part = get(in ? lane * PER + i : 0);
-        c[i] = in ? part.count : 0;
-        m[i] = in ? part.mass : 0.0;
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        count += c[i];
-        mass += m[i];
-    }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t c2 = __shfl_up_sync(0xffffffffu, count, o);
-        const double m2 = __shfl_up_sync(0xffffffffu, mass, o);
-        if (lane >= o) count += c2, mass += m2;
-    }
-    count = __shfl_up_sync(0xffffffffu, count, 1);
-    mass = __shfl_up_sync(0xffffffffu, mass, 1);
-    if (lane == 0) count = 0, mass = 0.0;
-    count += before.count;
-    mass += before.mass;
-    Place found = {-1, 0, 0.0}, last = {-1, 0, 0.0};
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if (target.kind == Border::Count ? c[i] > 0 : m[i] > 0.0) {
-            last = {lane * PER + i, count, mass};
-            if (found.item < 0 && target.met(count + c[i], mass + m[i])) found = last;
+        for (int i = 0; i < PER; ++i) {
+            Part part = {0, 0.0};
+            if (lane * PER + i < n) part = get(lane * PER + i);
+            count[i + 1] = count[i] + part.count;
+            mass[i + 1] = mass[i] + part.mass;
         }
-        count += c[i];
-        mass += m[i];
+        uint32_t c = count[PER];
+        double m = mass[PER];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t c2 = __shfl_up_sync(0xffffffffu, c, o);
+            const double m2 = __shfl_up_sync(0xffffffffu, m, o);
+            if (lane >= o) c += c2, m += m2;
+        }
+        c = __shfl_up_sync(0xffffffffu, c, 1);
+        m = __shfl_up_sync(0xffffffffu, m, 1);
+        c = before.count + (lane ? c : 0);
+        m = before.mass + (lane ? m : 0.0);
+#pragma unroll
+        for (int i = 0; i <= PER; ++i) {
+            count[i] += c;
+            mass[i] += m;
+        }
     }
-    uint32_t who = __ballot_sync(0xffffffffu, found.item >= 0);
-    int from = __ffs(who) - 1;
-    if (who == 0) {
-        who = __ballot_sync(0xffffffffu, last.item >= 0);
-        from = who ? 31 - __clz(who) : 0;
-        found = last;
+    __device__ __forceinline__ Part all() const { return {__shfl_sync(0xffffffffu, count[PER], 31), __shfl_sync(0xffffffffu, mass[PER], 31)}; }
+    // The last item that adds something, if rounding leaves the border to none.
+    __device__ __forceinline__ Place find(Target target) const
+    {
+        const int lane = threadIdx.x & 31;
+        for (int again = 0;; ++again) {
+            Place p = {-1, 0, 0.0};
+#pragma unroll
+            for (int i = PER - 1; i >= 0; --i) {
+                const bool here = target.met(count[i + 1], mass[i + 1]);
+                p = {here ? lane * PER + i : p.item, here ? count[i] : p.count, here ? mass[i] : p.mass};
+            }
+            const uint32_t who = __ballot_sync(0xffffffffu, p.item >= 0);
+            if (who || again) {
+                const int from = who ? __ffs(who) - 1 : 31;
+                return {max(__shfl_sync(0xffffffffu, p.item, from), 0), __shfl_sync(0xffffffffu, p.count, from), __shfl_sync(0xffffffffu, p.mass, from)};
+            }
+            const Part sum = all();
+            target = target.by_count() ? Target::at_count(sum.count) : Target::mass_from(sum.mass);
+        }
     }
-    return {max(__shfl_sync(0xffffffffu, found.item, from), 0), __shfl_sync(0xffffffffu, found.count, from), __shfl_sync(0xffffffffu, found.mass, from)};
-}
+};
 
 // An element: its number, its place in the order, the mass up to and with it.  Where its token is not known, it is the rank-th (from 0) of
 // the `have` elements with that number, by index.
@@ -228,11 +239,11 @@ struct Element {
 __device__ __forceinline__ Element choose(const Target &target, const Place &before, float value, uint32_t have, double weight)
 {
     uint32_t rank;
-    if (target.kind == Border::Count) {
+    if (target.by_count()) {
         rank = min(target.count - before.count, have) - 1;
     } else {
         // the quotient is right to a small part of 1, but for weights below 1e-13 of the mass, which no border can tell apart
-        const double q = floor((target.mass - before.mass) / weight);
+        const double q = floor((fmax(target.from, target.above) - before.mass) / weight);
         rank = q >= (double)have ? have - 1 : q > 0.0 ? (uint32_t)q : 0;
         if (rank > 0 && target.met(0, before.mass + rank * weight)) --rank;
         if (rank < have - 1 && !target.met(0, before.mass + (rank + 1) * weight)) ++rank;
@@ -275,17 +286,18 @@ __device__ __forceinline__ void decide(const SampleJob &job, float u, uint32_t F
     // one copy of the code of `find` for all borders: it is long, and each row runs through it once
 #pragma unroll 1
     for (int step = 0; step < 5; ++step) {
-        Target target = {Border::Count, n, 0.0};
+        Target target = Target::at_count(n);
         if (step == 0) {
             if (n >= massive) continue;
         } else if (step == 1) {
             if (!(job.top_p < 1.0)) continue;
-            target = {Border::MassFrom, 0, job.top_p * total};
+            target = Target::mass_from(job.top_p * total);
         } else if (step == 2) {
             if (!(job.min_p > 0.0 && within < n)) continue;
-            target.count = n = within;
+            n = within;
+            target = Target::at_count(n);
         } else if (step == 3) {
-            target = {Border::MassAbove, 0, (double)u * total};
+            target = Target::mass_above((double)u * total);
         } else if (drawn.n <= n) {
             continue;
         }
@@ -298,12 +310,13 @@ __device__ __forceinline__ void decide(const SampleJob &job, float u, uint32_t F
 }
 
 // The index of the rank-th element of this piece that `matches` accepts, searched in rounds: each warp a stretch of neighbouring units, the
-// next round's on their way while this one's are counted.  matches: a bit for each of a unit's elements, that of element e at
-// e / 2 + 16 (e % 2) where there are eight, at e where there are four.
+// next round's on their way while this one's are counted.  matches: a byte with a bit for each of a unit's elements, that of element e at
+// e / 2 + 4 (e % 2) where there are eight, at e where there are four.  Out of line: inlined, it takes registers from the rest (4096 x
+// 128256: 442 us, inlined 487).
 template <int THREADS, int DTYPE, typename Matches>
-__device__ void locate(const Piece<DTYPE> &piece, uint32_t rank, SampleShared &sh, int32_t *token, Matches &&matches)
+__device__ __noinline__ void locate(const Piece<DTYPE> piece, uint32_t rank, SampleShared &sh, int32_t *token, const Matches matches)
 {
-    constexpr int DEEP = 4;
+    constexpr int DEEP = 4;                  // 8: 13 % slower, what is read behind the token costs more than the rounds
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t seen = 0;
     int turn = 0;
@@ -317,32 +330,30 @@ __device__ void locate(const Piece<DTYPE> &piece, uint32_t rank, SampleShared &s
     };
     fetch(piece.begin);
     for (int32_t base = piece.begin; base < piece.end; base += THREADS * DEEP, turn ^= 1) {
-        uint32_t bits[DEEP], mine = 0;
+        uint32_t bits = 0;
 #pragma unroll
-        for (int q = 0; q < DEEP; ++q) {
-            bits[q] = base + (warp * DEEP + q) * 32 + lane < piece.end ? matches(next[q]) : 0u;
-        }
+        for (int q = 0; q < DEEP; ++q)
+            if (base + (warp * DEEP + q) * 32 + lane < piece.end) bits |= matches(next[q]) << (q * 8);
         fetch(base + THREADS * DEEP);
-        if (bits[0] | bits[1] | bits[2] | bits[3]) mine = __popc(bits[0]) + __popc(bits[1]) + __popc(bits[2]) + __popc(bits[3]);
-        mine = __reduce_add_sync(0xffffffffu, mine);
+        const uint32_t mine = __reduce_add_sync(0xffffffffu, __popc(bits));
         if (lane == 0) sh.warp_count[turn][warp] = mine;
         __syncthreads();
         const uint32_t c = lane < (THREADS / 32) ? sh.warp_count[turn][lane] : 0u;
         uint32_t before = seen + __reduce_add_sync(0xffffffffu, lane < warp ? c : 0u);
         seen += __reduce_add_sync(0xffffffffu, c);
         if (before <= rank && rank < before + mine) {
-#pragma unroll
             for (int q = 0; q < DEEP; ++q) {
-                uint32_t upto = __popc(bits[q]);
+                const uint32_t m = bits >> (q * 8) & 0xffu;
+                uint32_t upto = __popc(m);
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
                     const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
                     if (lane >= o) upto += v;
                 }
-                uint32_t from = before + upto - __popc(bits[q]);
+                uint32_t from = before + upto - __popc(m);
 #pragma unroll
                 for (int e = 0; e < Piece<DTYPE>::E; ++e)
-                    if (bits[q] >> (Piece<DTYPE>::E == 8 ? e / 2 + e % 2 * 16 : e) & 1) {
+                    if (m >> (Piece<DTYPE>::E == 8 ? e / 2 + e % 2 * 4 : e) & 1) {
                         if (from == rank) *token = piece.token(base + (warp * DEEP + q) * 32 + lane, e);
                         ++from;
                     }
@@ -352,6 +363,31 @@ __device__ void locate(const Piece<DTYPE> &piece, uint32_t rank, SampleShared &s
         if (seen > rank) return;             // the same for the whole CTA
     }
 }
+
+// Elements with the bits of one float32 key; elements of 16-bit units equal to a number (the zeros are one).
+template <int DTYPE> struct HasKey {
+    uint32_t key;
+    __device__ __forceinline__ uint32_t operator()(const uint4 &w) const
+    {
+        constexpr int E = Storage<DTYPE>::PER_UNIT;
+        float z[E];
+        Storage<DTYPE>::unpack(w, z);
+        uint32_t bits = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) bits |= (z[e] > -INFINITY && key_of(z[e]) == key) ? 1u << (E == 8 ? e / 2 + e % 2 * 4 : e) : 0u;
+        return bits;
+    }
+};
+template <int DTYPE> struct Equals {
+    uint32_t both;           // the number, twice
+    __device__ __forceinline__ uint32_t operator()(const uint4 &w) const
+    {
+        using F = Counted<DTYPE>;
+        const uint32_t m = (F::equal(w.x, both) & 0x00010001u) | (F::equal(w.y, both) & 0x00020002u) | (F::equal(w.z, both) & 0x00040004u) |
+                           (F::equal(w.w, both) & 0x00080008u);
+        return (m | m >> 12) & 0xffu;
+    }
+};
 
 // ---- a sorted list ----------------------------------------------------------------------------------
 // key << 32 | ~index: descending is by number, equal ones by index.
@@ -544,9 +580,11 @@ template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
     __device__ Place find_bin(const Target &target, const Place &before)
     {
         if (threadIdx.x < 32) {
-            Place p = warp_find<SEARCH_GROUPS / 32>(SEARCH_GROUPS, target, before, [&](int i) { return Part{sh.group_count[i], sh.group_mass[i]}; });
+            const Scan<SEARCH_GROUPS / 32> groups(SEARCH_GROUPS, before, [&](int i) { return Part{sh.group_count[i], sh.group_mass[i]}; });
+            Place p = groups.find(target);
             const int first = p.item * SEARCH_GROUP;
-            p = warp_find<1>(SEARCH_GROUP, target, p, [&](int i) { return Part{bins.all_count[first + i], bins.all_mass[first + i]}; });
+            const Scan<1> in_group(SEARCH_GROUP, p, [&](int i) { return Part{bins.all_count[first + i], bins.all_mass[first + i]}; });
+            p = in_group.find(target);
             p.item += first;
             if (threadIdx.x == 0) sh.place = p;
         }
@@ -662,7 +700,7 @@ template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
         const float value = float_of(hi);
         const uint32_t have = bins.all_count[p.item];
         __syncthreads();
-        if (massless && target.kind != Border::Count) return {value, p.count + 1, p.mass, -1, 0, have};
+        if (massless && !target.by_count()) return {value, p.count + 1, p.mass, -1, 0, have};
         return choose(target, p, value, have, massless ? 0.0 : weight(value));
     }
     __device__ void run(int64_t row)
@@ -735,15 +773,7 @@ template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
         }
         if (drawn.token >= 0) return;
         // one of many equal ones: which piece holds it, and where
-        const uint32_t key = key_of(drawn.value);
-        auto matches = [&](const uint4 &w) {
-            float z[E];
-            S::unpack(w, z);
-            uint32_t bits = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) bits |= (z[e] > -INFINITY && key_of(z[e]) == key) ? 1u << (E == 8 ? e / 2 + e % 2 * 16 : e) : 0u;
-            return bits;
-        };
+        const HasKey<DTYPE> matches{key_of(drawn.value)};
         uint32_t skip = 0, have = 0xffffffffu;
         if (ctas > 1) {
             if (threadIdx.x == 0) sh.here = 0;
@@ -804,37 +834,192 @@ template <int DTYPE> struct Count {
     // Not zero if a half may be beyond the counted range (a borrow from the low half can only add to what it says of the high one).
     static __device__ __forceinline__ uint32_t beyond(uint32_t w) { return ((w & 0x7fff7fffu) + OFFSET) & BEYOND; }
 
-    // Eight logits.  Bound by the integer units (4 operations a logit) and the additions in shared memory: nothing is looked at one by one
-    // where all eight are in range.
+    // Eight logits; the whole warp calls.   Bound by the integer units (4 operations a logit) and the additions in shared memory: nothing
+    // is looked at one by one where all are in range, or in range and -inf (one way for the warp: both would cost the sum).
     __device__ __forceinline__ void add(const uint4 &w)
     {
         most = F::most(most, F::most(F::most(w.x, w.y), F::most(w.z, w.w)));
-        if ((beyond(w.x) | beyond(w.y) | beyond(w.z) | beyond(w.w)) == 0) {
-            low_half(w.x), high_half(w.x), low_half(w.y), high_half(w.y);
-            low_half(w.z), high_half(w.z), low_half(w.w), high_half(w.w);
-        } else {
-            for (const uint32_t v : {w.x, w.y, w.z, w.w}) {
-                if (in_range(v & 0x7fffu)) low_half(v); else beyond_one(v & 0xffffu);
-                if (in_range(v >> 16 & 0x7fffu)) high_half(v); else beyond_one(v >> 16);
+        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+        uint32_t out[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = beyond(words[i]);
+        if (!__any_sync(0xffffffffu, out[0] | out[1] | out[2] | out[3])) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) low_half(words[i]), high_half(words[i]);
+            return;
+        }
+        uint32_t odd = 0, count = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t masked = F::equal(words[i], NEG_INF * 0x10001u);
+            odd |= out[i] & ~masked;
+            count += masked & 0x10001u;
+            if (!(out[i] & 0xffffu)) low_half(words[i]);
+            if (!(out[i] >> 16)) high_half(words[i]);
+        }
+        none += (count & 0xffffu) + (count >> 16);
+        if (odd) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                beyond_one(words[i] & 0xffffu, !(out[i] & 0xffffu));
+                beyond_one(words[i] >> 16, !(out[i] >> 16));
             }
         }
     }
-    static __device__ __forceinline__ bool in_range(uint32_t magnitude) { return magnitude - F::LOW < F::WORDS; }
-    __device__ __forceinline__ void beyond_one(uint32_t bits)
+    // What has not been counted, or taken for beyond the range on account of its neighbour; -inf was counted already.
+    __device__ __forceinline__ void beyond_one(uint32_t bits, bool counted)
     {
         const uint32_t magnitude = bits & 0x7fffu;
-        none += bits == NEG_INF;
-        zeros += magnitude == 0;
-        if (bits != NEG_INF && magnitude != 0) {
-            if (magnitude >= F::INF)
-                flags |= SAMPLE_BAD;
-            else if (bits & 0x8000u && magnitude > F::WORDS)
-                ++low;
-            else
-                flags |= SAMPLE_ODD;
-        }
+        if (counted || bits == NEG_INF) return;
+        if (magnitude - F::LOW < F::WORDS)
+            low_half(bits);
+        else if (magnitude == 0)
+            ++zeros;
+        else if (magnitude >= F::INF)
+            flags |= SAMPLE_BAD;
+        else if (bits & 0x8000u && magnitude > F::WORDS)
+            ++low;
+        else
+            flags |= SAMPLE_ODD;
     }
 };
+
+// The groups' counts and masses: each CTA adds up a share of the groups for all, in its own words (the others read none of those).
+template <int DTYPE>
+__device__ __forceinline__ void sum_groups(const SampleJob &job, int rank, int ctas, SampleShared &sh, uint4 *words)
+{
+    using F = Counted<DTYPE>;
+    using G = Groups<DTYPE>;
+    constexpr int THREADS = F::THREADS;
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto of = [&](auto *p, int r) { return ctas == 1 ? p : cluster.map_shared_rank(p, r); };
+    const double per_nat = 1.0 / job.temperature, top = (double)float_of(sh.top);
+    const int from = G::SIDE / ctas * rank, to = G::SIDE / ctas * (rank + 1);
+    uint32_t over = 0, within = 0;
+    for (int g = from + warp; g < to; g += THREADS / 32) {
+        const int at = G::word(g) / 4 + lane;
+        const uint4 own = words[at];
+        if (ctas == 1 && !__any_sync(0xffffffffu, own.x | own.y | own.z | own.w)) continue;
+        uint32_t b[2][4] = {{own.x & 0xffffu, own.y & 0xffffu, own.z & 0xffffu, own.w & 0xffffu}, {own.x >> 16, own.y >> 16, own.z >> 16, own.w >> 16}};
+        uint4 others[SAMPLE_CTAS];       // all on their way at once
+#pragma unroll
+        for (int r = 1; r < SAMPLE_CTAS; ++r)
+            if (r < ctas) others[r] = cluster.map_shared_rank(words, rank + r < ctas ? rank + r : rank + r - ctas)[at];
+#pragma unroll
+        for (int r = 1; r < SAMPLE_CTAS; ++r) {
+            if (r >= ctas) break;
+            const uint4 o = others[r];
+            b[0][0] += o.x & 0xffffu, b[0][1] += o.y & 0xffffu, b[0][2] += o.z & 0xffffu, b[0][3] += o.w & 0xffffu;
+            b[1][0] += o.x >> 16, b[1][1] += o.y >> 16, b[1][2] += o.z >> 16, b[1][3] += o.w >> 16;
+        }
+        if (!Count<DTYPE>::ZEROS && at == 0) b[0][0] += b[1][0], b[1][0] = 0;        // -0 is +0
+        if (ctas > 1 || (!Count<DTYPE>::ZEROS && g == 0)) {
+            words[at] = make_uint4(b[0][0] | b[1][0] << 16, b[0][1] | b[1][1] << 16, b[0][2] | b[1][2] << 16, b[0][3] | b[1][3] << 16);
+            over |= b[0][0] | b[0][1] | b[0][2] | b[0][3] | b[1][0] | b[1][1] | b[1][2] | b[1][3];
+        }
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const uint32_t have = b[side][0] + b[side][1] + b[side][2] + b[side][3];
+            if (!__any_sync(0xffffffffu, have != 0)) continue;
+            const int group = side ? G::ZERO + 1 + g : g;
+            double mass = 0.0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const double e = exp(((double)G::number(group, lane * 4 + i) - top) * per_nat);
+                mass += b[side][i] ? b[side][i] * e : 0.0;   // beyond the maximum e may overflow, with nothing to count
+                within += e >= job.min_p ? b[side][i] : 0u;
+            }
+            mass = warp_sum_f64(mass);
+            const uint32_t counted = __reduce_add_sync(0xffffffffu, have);
+            for (int r = lane; r < ctas; r += 32) {
+                SampleShared *s = of(&sh, r);
+                s->group_count[group] = counted;
+                s->group_mass[group] = mass;
+            }
+        }
+    }
+    if (Count<DTYPE>::ZEROS && threadIdx.x == 0 && sh.zeros > 0) {       // every CTA for itself
+        const double e = exp(-top * per_nat);
+        sh.group_count[G::ZERO] = sh.zeros;
+        sh.group_mass[G::ZERO] = sh.zeros * e;
+        if (rank == 0 && e >= job.min_p) within += sh.zeros;
+    }
+    within = __reduce_add_sync(0xffffffffu, within);
+    over = __reduce_or_sync(0xffffffffu, over) >> 16;
+    if (lane == 0)
+        for (int r = 0; r < ctas; ++r) {
+            if (within) atomicAdd(&of(&sh, r)->within, within);
+            if (over) atomicOr(&of(&sh, r)->flags, (uint32_t)SAMPLE_ODD);
+        }
+}
+
+// What is kept of a row, and the draw, from the groups' counts and masses; sh.drawn.n is 0 where there is none (rank: the flags). One warp.
+template <int DTYPE>
+__device__ __forceinline__ void decide_counted(const SampleJob &job, int64_t row, uint32_t logits, int rank, int ctas, SampleShared &sh, const uint4 *own)
+{
+    using F = Counted<DTYPE>;
+    using G = Groups<DTYPE>;
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int lane = threadIdx.x & 31;
+    const double per_nat = 1.0 / job.temperature, top = (double)float_of(sh.top);
+    constexpr int PER = (G::ALL + 31) / 32;
+    const Scan<PER> groups(G::ALL, Place{0, 0, 0.0}, [&](int i) { return Part{sh.group_count[G::at(i)], sh.group_mass[G::at(i)]}; });
+    const Part all = groups.all();
+    uint32_t flags = sh.flags;
+    const uint32_t low = sh.low;
+    // a count that ran over left a sum that is short; numbers below the counted range have to be too deep for any mass
+    if (all.count + sh.none + low != logits) flags |= SAMPLE_ODD;
+    if (low > 0) {
+        const double deep = (top + F::LIMIT) * per_nat;
+        if (all.count == 0 || deep < SEARCH_NATS || (job.min_p > 0.0 && exp(-deep) >= job.min_p)) flags |= SAMPLE_ODD;
+    }
+    if (flags || all.count == 0) {
+        if (lane == 0) {
+            if (rank == 0 && (flags & SAMPLE_BAD || flags == 0)) {
+                job.tokens[row] = -1;
+                job.logp[row] = flags ? NAN : -INFINITY;
+                if (job.kept) job.kept[row] = 0;
+            }
+            sh.drawn.n = 0;
+            sh.drawn.rank = flags;
+        }
+        return;
+    }
+    auto find = [&](const Target &target) {
+        Place p = groups.find(target);
+        const int group = G::at(p.item);
+        if (group == G::ZERO) return choose(target, p, 0.0f, sh.zeros, exp(-top * per_nat));
+        // four words a lane, of the group's numbers in descending order, from the CTA that added this group up
+        const bool negative = G::negative(group);
+        const int owner = G::side(group) / (G::SIDE / ctas), at = G::word(G::side(group)) / 4 + (negative ? lane : 31 - lane);
+        const uint4 words = ctas == 1 ? own[at] : cluster.map_shared_rank(own, owner)[at];
+        const uint32_t half = negative ? 16 : 0;
+        const uint32_t have[4] = {(negative ? words.x : words.w) >> half & 0xffffu, (negative ? words.y : words.z) >> half & 0xffffu,
+                                  (negative ? words.z : words.y) >> half & 0xffffu, (negative ? words.w : words.x) >> half & 0xffffu};
+        auto number = [&](int i) { return G::number(group, negative ? i : GROUP - 1 - i); };
+        auto weight = [&](int i) { return exp(((double)number(i) - top) * per_nat); };
+        const Scan<GROUP / 32> numbers(GROUP, p, [&](int i) {
+            const uint32_t c = have[i % 4];
+            const double e = weight(i);
+            return Part{c, c ? c * e : 0.0};                 // beyond the maximum e may overflow
+        });
+        p = numbers.find(target);
+        const uint32_t mine = p.item % 4 == 0 ? have[0] : p.item % 4 == 1 ? have[1] : p.item % 4 == 2 ? have[2] : have[3];
+        return choose(target, p, number(p.item), __shfl_sync(0xffffffffu, mine, p.item / 4), weight(p.item));
+    };
+    Element drawn;
+    uint32_t n;
+    double total;
+    decide(job, job.uniforms[row], all.count + low, all.count, all.mass, sh.within, find, drawn, n, total);
+    if (lane == 0) {
+        if (rank == 0) {
+            job.logp[row] = (float)(((double)drawn.value - top) * per_nat - log(total));
+            if (job.kept) job.kept[row] = (int32_t)n;
+        }
+        sh.drawn = drawn;
+    }
+}
 
 template <int DTYPE>
 __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS) sample_count_kernel(const SampleJob job)
@@ -853,10 +1038,13 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
     auto of = [&](auto *p, int r) { return ctas == 1 ? p : cluster.map_shared_rank(p, r); };
     constexpr int DEEP = 4;
     uint4 w[DEEP];
-    auto fetch = [&](int32_t u0) {
+    auto fetch = [&](int32_t u0) {           // behind the piece's end, -inf
 #pragma unroll
-        for (int q = 0; q < DEEP; ++q)
+        for (int q = 0; q < DEEP; ++q) {
+            constexpr uint32_t BEHIND = Count<DTYPE>::NEG_INF * 0x10001u;
+            w[q] = make_uint4(BEHIND, BEHIND, BEHIND, BEHIND);
             if (u0 + q * THREADS < piece.end) w[q] = piece.load(u0 + q * THREADS);
+        }
     };
     fetch(piece.begin + (int32_t)threadIdx.x);
     for (int i = threadIdx.x; i < (int)F::WORDS / 4; i += THREADS) sample_smem[i] = make_uint4(0, 0, 0, 0);
@@ -865,16 +1053,19 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
     meet(cluster, ctas);                     // the others write into these
     {
         Count<DTYPE> count{reinterpret_cast<char *>(sample_smem)};
-        for (int32_t u0 = piece.begin + (int32_t)threadIdx.x; u0 < piece.end; u0 += THREADS * DEEP) {
+        for (int32_t u0 = piece.begin + (int32_t)threadIdx.x; u0 - lane < piece.end; u0 += THREADS * DEEP) {
             uint4 now[DEEP];
 #pragma unroll
             for (int q = 0; q < DEEP; ++q) now[q] = w[q];
             fetch(u0 + THREADS * DEEP);
 #pragma unroll
             for (int q = 0; q < DEEP; ++q)
-                if (u0 + q * THREADS < piece.end) count.add(now[q]);
+                if (u0 - lane + q * THREADS < piece.end) count.add(now[q]);
         }
-        const uint32_t none = __reduce_add_sync(0xffffffffu, count.none), low = __reduce_add_sync(0xffffffffu, count.low),
+        // without what fetch() put behind the piece
+        const int32_t length = piece.end - piece.begin, behind = (32 - length % 32) % 32;
+        const bool last = warp == (int)((uint32_t)(length / 32) % (THREADS / 32));       // the warp whose units the end divides
+        const uint32_t none = __reduce_add_sync(0xffffffffu, count.none) - (last ? behind * 8u : 0u), low = __reduce_add_sync(0xffffffffu, count.low),
                        zeros = __reduce_add_sync(0xffffffffu, count.zeros), flags = __reduce_or_sync(0xffffffffu, count.flags);
         const uint32_t top = __reduce_max_sync(0xffffffffu, max(key_of(Storage<DTYPE>::get((uint16_t)count.most)),
                                                                 key_of(Storage<DTYPE>::get((uint16_t)(count.most >> 16)))));
@@ -889,122 +1080,9 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
             }
     }
     meet(cluster, ctas);
-    const double per_nat = 1.0 / job.temperature, top = (double)float_of(sh.top);
-    const uint32_t none = sh.none, low = sh.low;
-    {
-        // Each CTA adds up a share of the groups for all, in its own words: the other CTAs read none of those.
-        const int from = G::SIDE * rank / ctas, to = G::SIDE * (rank + 1) / ctas;
-        uint32_t over = 0, within = 0;
-        for (int g = from + warp; g < to; g += THREADS / 32) {
-            const int at = G::word(g) / 4 + lane;
-            const uint4 own = sample_smem[at];
-            if (ctas == 1 && !__any_sync(0xffffffffu, own.x | own.y | own.z | own.w)) continue;
-            uint32_t b[2][4] = {{own.x & 0xffffu, own.y & 0xffffu, own.z & 0xffffu, own.w & 0xffffu}, {own.x >> 16, own.y >> 16, own.z >> 16, own.w >> 16}};
-            for (int r = 1; r < ctas; ++r) {
-                const uint4 o = cluster.map_shared_rank(sample_smem, rank + r < ctas ? rank + r : rank + r - ctas)[at];
-                b[0][0] += o.x & 0xffffu, b[0][1] += o.y & 0xffffu, b[0][2] += o.z & 0xffffu, b[0][3] += o.w & 0xffffu;
-                b[1][0] += o.x >> 16, b[1][1] += o.y >> 16, b[1][2] += o.z >> 16, b[1][3] += o.w >> 16;
-            }
-            if (!Count<DTYPE>::ZEROS && at == 0) b[0][0] += b[1][0], b[1][0] = 0;        // -0 is +0
-            if (ctas > 1 || (!Count<DTYPE>::ZEROS && g == 0)) {
-                sample_smem[at] = make_uint4(b[0][0] | b[1][0] << 16, b[0][1] | b[1][1] << 16, b[0][2] | b[1][2] << 16, b[0][3] | b[1][3] << 16);
-                over |= b[0][0] | b[0][1] | b[0][2] | b[0][3] | b[1][0] | b[1][1] | b[1][2] | b[1][3];
-            }
-#pragma unroll
-            for (int side = 0; side < 2; ++side) {
-                const uint32_t have = b[side][0] + b[side][1] + b[side][2] + b[side][3];
-                if (!__any_sync(0xffffffffu, have != 0)) continue;
-                const int group = side ? G::ZERO + 1 + g : g;
-                double mass = 0.0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const double e = exp(((double)G::number(group, lane * 4 + i) - top) * per_nat);
-                    mass += b[side][i] ? b[side][i] * e : 0.0;   // beyond the maximum e may overflow, with nothing to count
-                    within += e >= job.min_p ? b[side][i] : 0u;
-                }
-                mass = warp_sum_f64(mass);
-                const uint32_t counted = __reduce_add_sync(0xffffffffu, have);
-                for (int r = lane; r < ctas; r += 32) {
-                    SampleShared *s = of(&sh, r);
-                    s->group_count[group] = counted;
-                    s->group_mass[group] = mass;
-                }
-            }
-        }
-        if (Count<DTYPE>::ZEROS && threadIdx.x == 0 && sh.zeros > 0) {       // every CTA for itself
-            const double e = exp(-top * per_nat);
-            sh.group_count[G::ZERO] = sh.zeros;
-            sh.group_mass[G::ZERO] = sh.zeros * e;
-            if (rank == 0 && e >= job.min_p) within += sh.zeros;
-        }
-        within = __reduce_add_sync(0xffffffffu, within);
-        over = __reduce_or_sync(0xffffffffu, over) >> 16;
-        if (lane == 0)
-            for (int r = 0; r < ctas; ++r) {
-                if (within) atomicAdd(&of(&sh, r)->within, within);
-                if (over) atomicOr(&of(&sh, r)->flags, (uint32_t)SAMPLE_ODD);
-            }
-    }
+    sum_groups<DTYPE>(job, rank, ctas, sh, sample_smem);
     meet(cluster, ctas);
-    auto owner = [&](int side) {             // the CTA that added this group up
-        int r = 0;
-        while (G::SIDE * (r + 1) / ctas <= side) ++r;
-        return r;
-    };
-    if (warp == 0) {
-        constexpr int PER = (G::ALL + 31) / 32;
-        uint32_t counted = 0, flags = sh.flags;
-        double all = 0.0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int g = lane + 32 * i;
-            if (g < G::ALL) counted += sh.group_count[g], all += sh.group_mass[g];
-        }
-        counted = __reduce_add_sync(0xffffffffu, counted);
-        all = warp_sum_f64(all);
-        // a count that ran over left a sum that is short; numbers below the counted range have to be too deep for any mass
-        if (counted + none + low != (uint32_t)piece.units * 8) flags |= SAMPLE_ODD;
-        if (low > 0) {
-            const double deep = (top + F::LIMIT) * per_nat;
-            if (counted == 0 || deep < SEARCH_NATS || (job.min_p > 0.0 && exp(-deep) >= job.min_p)) flags |= SAMPLE_ODD;
-        }
-        if (flags == 0 && counted > 0) {
-            auto find = [&](const Target &target) {
-                Place p = warp_find<PER>(G::ALL, target, Place{0, 0, 0.0}, [&](int i) { return Part{sh.group_count[G::at(i)], sh.group_mass[G::at(i)]}; });
-                const int group = G::at(p.item);
-                if (group == G::ZERO) return choose(target, p, 0.0f, sh.zeros, exp(-top * per_nat));
-                const uint32_t *counts = reinterpret_cast<const uint32_t *>(of(&sample_smem[0], owner(G::side(group)))) + G::word(G::side(group));
-                auto place = [&](int i) { return G::negative(group) ? i : GROUP - 1 - i; };
-                auto count_at = [&](int i) { return G::negative(group) ? counts[place(i)] >> 16 : counts[place(i)] & 0xffffu; };
-                auto weight_at = [&](int i) { return exp(((double)G::number(group, place(i)) - top) * per_nat); };
-                p = warp_find<GROUP / 32>(GROUP, target, p, [&](int i) {
-                    const uint32_t c = count_at(i);
-                    const double e = weight_at(i);
-                    return Part{c, c ? c * e : 0.0};         // beyond the maximum e may overflow
-                });
-                return choose(target, p, G::number(group, place(p.item)), count_at(p.item), weight_at(p.item));
-            };
-            Element drawn;
-            uint32_t n;
-            double total;
-            decide(job, job.uniforms[row], counted + low, counted, all, sh.within, find, drawn, n, total);
-            if (lane == 0) {
-                if (rank == 0) {
-                    job.logp[row] = (float)(((double)drawn.value - top) * per_nat - log(total));
-                    if (job.kept) job.kept[row] = (int32_t)n;
-                }
-                sh.drawn = drawn;
-            }
-        } else if (lane == 0) {
-            if (rank == 0 && (flags & SAMPLE_BAD || flags == 0)) {
-                job.tokens[row] = -1;
-                job.logp[row] = flags ? NAN : -INFINITY;
-                if (job.kept) job.kept[row] = 0;
-            }
-            sh.drawn.n = 0;
-            sh.drawn.rank = flags;
-        }
-    }
+    if (warp == 0) decide_counted<DTYPE>(job, row, (uint32_t)piece.units * 8, rank, ctas, sh, sample_smem);
     __syncthreads();
     const Element drawn = sh.drawn;
     if (drawn.n == 0) {                      // the same for all CTAs of the row
@@ -1016,11 +1094,8 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
         }
         return;
     }
-    const uint32_t bits = Storage<DTYPE>::put(drawn.value), both = bits * 0x10001u;
-    auto matches = [&](const uint4 &w) {     // equality of numbers: the zeros are one
-        return (F::equal(w.x, both) & 0x00010001u) | (F::equal(w.y, both) & 0x00020002u) | (F::equal(w.z, both) & 0x00040004u) |
-               (F::equal(w.w, both) & 0x00080008u);
-    };
+    const uint32_t bits = Storage<DTYPE>::put(drawn.value);
+    const Equals<DTYPE> matches{bits * 0x10001u};
     uint32_t skip = 0, have = drawn.have;
     if (ctas > 1 && Count<DTYPE>::ZEROS && drawn.value == 0.0f) {
         uint32_t mine = 0;                   // zeros have no word: counted here
@@ -1035,18 +1110,16 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
     } else if (ctas > 1) {
         // how many of them each piece holds: the other CTAs' words still tell; the owner's own are what is left of the sum
         const uint32_t magnitude = bits & 0x7fffu;
-        const int own = owner((int)(magnitude - F::LOW) / GROUP);
-        uint32_t others = 0, mine = 0;
-        for (int r = 0; r < ctas; ++r) {
-            if (r == own) continue;
-            const uint32_t word = reinterpret_cast<const uint32_t *>(cluster.map_shared_rank(&sample_smem[0], r))[magnitude & F::MASK];
-            const uint32_t c = magnitude == 0 ? (word & 0xffffu) + (word >> 16) : bits & 0x8000u ? word >> 16 : word & 0xffffu;
-            others += c;
-            if (r < rank) skip += c;
-            if (r == rank) mine = c;
+        const int own = (int)(magnitude - F::LOW) / GROUP / (G::SIDE / ctas);      // the CTA that added this group up
+        uint32_t c = 0;
+        if (lane < ctas && lane != own) {
+            const uint32_t word = reinterpret_cast<const uint32_t *>(cluster.map_shared_rank(&sample_smem[0], lane))[magnitude & F::MASK];
+            c = magnitude == 0 ? (word & 0xffffu) + (word >> 16) : bits & 0x8000u ? word >> 16 : word & 0xffffu;
         }
-        if (own < rank) skip += drawn.have - others;
-        have = own == rank ? drawn.have - others : mine;
+        const uint32_t others = __reduce_add_sync(0xffffffffu, c);
+        if (lane == own) c = drawn.have - others;
+        skip = __reduce_add_sync(0xffffffffu, lane < rank ? c : 0u);
+        have = __shfl_sync(0xffffffffu, c, rank);
     }
     if (drawn.rank >= skip && drawn.rank - skip < have) locate<THREADS>(piece, drawn.rank - skip, sh, job.tokens + row, matches);
     if (ctas > 1) cluster.sync();            // no CTA leaves while another still reads its shared memory
