@@ -469,7 +469,7 @@ typedef struct {
     int32_t dtype;              /* ppow_dtype of the logits */
     int32_t top_k;              /* 0: off */
     int64_t logits_stride;      /* >= V */
-    double temperature;         /* 1e-300 .. 1e300 */
+    double temperature;         /* 1e-30 .. 1e30 */
     double top_p;               /* (0, 1]; 1: off */
     double min_p;               /* [0, 1]; 0: off */
 } ppow_sample_params;

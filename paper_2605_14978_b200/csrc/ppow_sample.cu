@@ -12,11 +12,11 @@
 //   16-bit logits   A row holds at most 65536 different numbers: one pass counts them, by integer additions in shared memory, and all the
 //                   rest is arithmetic on a few thousand (number, count) pairs.  Bound by those additions (one warp's 32 fall on the 32
 //                   banks at random, about 4 cycles) where the row's bytes take 2.7 of the same cycles.
-//   few logits      Up to 2048 above -inf are sorted in shared memory, and their masses added up in that order.
 //   float32         A row holds any numbers, so they go into 2048 bins of equal depth below the maximum, each with its count and its mass in
 //                   fixed point relative to the bin's top (integers again).  The few hundred elements of the bin that holds a border
-//                   are sorted; a bin of more (many equal ones) is followed by further passes over the keys, 2048 to one, until one holds one number.
-//                   16-bit rows that the counting does not fit (logits of 2048 and more, more than 65535 equal ones) go the same way.
+//                   are listed, and dealt out over the keys in it until a part holds one element or one number; a bin of more than
+//                   2048 (many equal ones) in passes over the row.  Short rows are listed whole, of any type.  16-bit rows that the
+//                   counting does not fit (logits of 2048 and more, more than 65535 equal ones) go the same way.
 //
 // A cluster of CTAs shares a row, each with a contiguous piece of it: one CTA when there are rows enough, up to eight for a few.
 #include "ppow_checked.cuh"
@@ -32,11 +32,12 @@ constexpr int SAMPLE_CTAS = 8, WARPS_MOST = 16;
 constexpr int32_t SAMPLE_MAX_VOCAB = 1 << 22;
 constexpr int GROUP = 128;               // numbers of one sign whose counts and masses are summed up together: four to a lane
 constexpr int SEARCH_GROUP = 32;         // the same of the bins of a search
-constexpr int LIST = 2048;               // as many elements are sorted, or as there are bins if that is fewer
-constexpr double SEARCH_NATS = 64.0;     // what lies deeper than this below the maximum has no mass: 2^22 exp(-64) is 1e-21
-// A mass in fixed point, 2^39 to 1, is added up in three limbs of 13 bits, so that 2^19 elements to a CTA fit words of 32.
+constexpr int SEARCH_BINS = 2048;
+constexpr double SEARCH_NATS = 56.0;     // what lies deeper than this below the maximum has no mass: 2^22 exp(-56) is 2e-18
+constexpr uint32_t LOWEST_FINITE = 0x00800000u;     // key of the lowest float32 above -inf
+// A mass in fixed point, 2^38 to 1, is added up in three limbs of 13 bits, so that 2^19 elements to a CTA fit words of 32.
 constexpr int LIMBS = 3, LIMB_BITS = 13;
-constexpr double MASS_ONE = 549755813888.0;
+constexpr double MASS_ONE = 274877906944.0;
 constexpr int32_t PIECE_MOST = 1 << 19;
 
 struct SampleJob {
@@ -96,7 +97,7 @@ template <int DTYPE> struct Groups {
     }
 };
 constexpr int GROUPS_MOST = Groups<PPOW_F16>::ALL;
-static_assert(GROUPS_MOST >= Groups<PPOW_BF16>::ALL && GROUPS_MOST >= LIST / SEARCH_GROUP, "groups");
+static_assert(GROUPS_MOST >= Groups<PPOW_BF16>::ALL && GROUPS_MOST >= SEARCH_BINS / SEARCH_GROUP, "groups");
 
 // Order-preserving key of a float32 (-0 is +0), and back.
 __device__ __forceinline__ uint32_t key_of(float z)
@@ -254,13 +255,12 @@ __device__ __forceinline__ Element choose(const Target &target, const Place &bef
 struct SampleShared {
     uint32_t group_count[GROUPS_MOST];
     double group_mass[GROUPS_MOST];
-    double warp_mass[WARPS_MOST];
     uint32_t warp_count[2][WARPS_MOST];
     uint32_t none, low, zeros;               // -inf; below the counted range; zeros that are counted apart
     uint32_t flags, within, top;             // SAMPLE_*; within min_p; key of the maximum
     uint32_t here;                           // elements of the drawn number in this piece
-    uint32_t low_key, high_key, listed;
-    int32_t first;
+    uint32_t listed, only_key;
+    int32_t only_token;
     Element drawn;
     Place place;
 };
@@ -389,124 +389,51 @@ template <int DTYPE> struct Equals {
     }
 };
 
-// ---- a sorted list ----------------------------------------------------------------------------------
-// key << 32 | ~index: descending is by number, equal ones by index.
-__device__ __forceinline__ unsigned long long list_entry(float z, int32_t token) { return (unsigned long long)key_of(z) << 32 | (uint32_t)~token; }
-__device__ __forceinline__ float list_value(unsigned long long e) { return float_of((uint32_t)(e >> 32)); }
-__device__ __forceinline__ int32_t list_token(unsigned long long e) { return (int32_t)~(uint32_t)e; }
-
-// Sorts list[0 .. n) in descending order, n <= LIST, in place; a network over the next power of two.  Exchanges over up to 32 places stay within
-// a warp's 64 entries.
-template <int THREADS> __device__ void sort_list(unsigned long long *list, int n)
-{
-    int size = 64;
-    while (size < n) size <<= 1;
-    for (int i = n + (int)threadIdx.x; i < size; i += THREADS) list[i] = 0;
-    __syncthreads();
-    for (int k = 2; k <= size; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int t = threadIdx.x; t < size / 2; t += THREADS) {
-                const int lo = ((t & ~(j - 1)) << 1) | (t & (j - 1)), hi = lo | j;
-                const unsigned long long a = list[lo], b = list[hi];
-                if ((a < b) == ((lo & k) == 0)) list[lo] = b, list[hi] = a;
-            }
-            if (j > 32 || (j == 1 && k >= 64))
-                __syncthreads();
-            else
-                __syncwarp();
-        }
-}
-
-// mass[i]: of list[0 .. i], behind `before`.  up(z): the weight of a number.
-template <int THREADS, typename Weight> __device__ void add_up_list(const unsigned long long *list, double *mass, int n, double before, SampleShared &sh, Weight &&weight)
-{
-    constexpr int PER = LIST / THREADS;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    double m[PER], sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int at = threadIdx.x * PER + i;
-        m[i] = 0.0;
-        if (at < n) m[i] = weight(list_value(list[at]));
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) sum += m[i];
-    double upto = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const double v = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += v;
-    }
-    if (lane == 31) sh.warp_mass[warp] = upto;
-    upto = __shfl_up_sync(0xffffffffu, upto, 1);
-    if (lane == 0) upto = 0.0;
-    __syncthreads();
-    for (int i = 0; i < warp; ++i) before += sh.warp_mass[i];
-    before += upto;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int at = threadIdx.x * PER + i;
-        before += m[i];
-        if (at < n) mass[at] = before;
-    }
-    __syncthreads();
-}
-
-// The element of a sorted list on the border; the last one if there is none.  The whole CTA calls.
-template <int THREADS> __device__ Element find_in_list(const unsigned long long *list, const double *mass, int n, uint32_t before, const Target &target, SampleShared &sh)
-{
-    if (threadIdx.x == 0) sh.first = n - 1;
-    __syncthreads();
-    int at = n - 1;
-    for (int i = threadIdx.x; i < n; i += THREADS)
-        if (target.met(before + i + 1, mass[i])) {
-            at = i;
-            break;
-        }
-    at = __reduce_min_sync(0xffffffffu, at);
-    if ((threadIdx.x & 31) == 0) atomicMin(&sh.first, at);
-    __syncthreads();
-    at = sh.first;
-    __syncthreads();
-    return {list_value(list[at]), before + at + 1, mass[at], list_token(list[at]), 0, 1};
-}
-
 // ---- search: any row --------------------------------------------------------------------------------
-template <int SEARCH_BINS> struct SearchBins {
+// Counts and masses of bins, the masses in fixed point as limbs: of this CTA, and of the cluster.
+template <int BINS> struct BinCounts {
+    uint32_t count[BINS], limb[LIMBS][BINS];
+};
+template <int BINS> struct BinTotals {
+    uint32_t count[BINS];
+    double mass[BINS];
+};
+template <int BINS> struct SearchBins {
+    static constexpr int SUB = BINS / 4, LIST = BINS;        // parts of a bin; elements that are listed
     union {
-        struct {                                             // of this CTA
-            uint32_t count[SEARCH_BINS], limb[LIMBS][SEARCH_BINS];
-        };
+        BinCounts<BINS> depth;
         struct {
-            unsigned long long list[SEARCH_BINS];
-            union {
-                double mass[SEARCH_BINS];
-                unsigned long long own[SEARCH_BINS];                // this CTA's part of the list, before it is put together
-            };
+            BinCounts<SUB> sub;
+            unsigned long long list[LIST];                   // of this piece: key << 32 | token
         };
     };
-    uint32_t all_count[SEARCH_BINS];                         // of the cluster
-    double all_mass[SEARCH_BINS];
+    BinTotals<BINS> depths;
+    BinTotals<SUB> subs;
 };
 
-template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
-    static constexpr int SEARCH_GROUPS = SEARCH_BINS / SEARCH_GROUP, MOST = SEARCH_BINS < LIST ? SEARCH_BINS : LIST;
-    using Bins = SearchBins<SEARCH_BINS>;
+template <int DTYPE, int THREADS, int BINS> struct Search {
     using S = Storage<DTYPE>;
-    static constexpr int E = S::PER_UNIT;
+    using Bins = SearchBins<BINS>;
+    static constexpr int E = S::PER_UNIT, SUB = Bins::SUB;
+    static constexpr double STEP = SEARCH_NATS / (BINS - 1);         // depth of a bin, nats
     const SampleJob &job;
     const Piece<DTYPE> &piece;
     const cg::cluster_group &cluster;
     int rank, ctas;
     SampleShared &sh;
     Bins &bins;
-    double top, scale, per_nat;              // maximum; bins per logit; 1 / temperature
-    bool depths;                             // whether all_count and all_mass hold the depth bins
+    double top, per_nat;                     // maximum; 1 / temperature
+    float top32, scale;                      // the same maximum; bins per logit
+    int listed;                              // the elements looked at: those of the list, so many, or, < 0, all of the piece
 
     template <typename T> __device__ __forceinline__ T *of(T *p, int r) const { return ctas == 1 ? p : cluster.map_shared_rank(p, r); }
-    // f(z, token) for every logit of the piece; those around the row are -inf
+    // f(z, token) for every logit; those around the row are -inf
     template <typename F> __device__ __forceinline__ void each(F &&f) const
     {
+        if (listed >= 0) {
+            for (int i = threadIdx.x; i < listed; i += THREADS) f(float_of((uint32_t)(bins.list[i] >> 32)), (int32_t)(uint32_t)bins.list[i]);
+            return;
+        }
         constexpr int DEEP = 2;
         for (int32_t u0 = piece.begin + (int32_t)threadIdx.x; u0 < piece.end; u0 += THREADS * DEEP) {
             uint4 w[DEEP];
@@ -523,36 +450,55 @@ template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
                 }
         }
     }
-    __device__ __forceinline__ int depth_bin(double d) const { return (int)fmin(d * scale, (double)(SEARCH_BINS - 1)); }
     __device__ __forceinline__ double weight(float z) const { return exp(((double)z - top) * per_nat); }
-
-    __device__ void clear()
+    // In float32, whose differences and products keep the order: a bin is a stretch of numbers.  Its rounding moves a border by 1e-5 nats.
+    __device__ __forceinline__ int depth_bin(float z) const { return (int)fminf((top32 - z) * scale, (float)(BINS - 1)); }
+    // Key of the lowest number that is in `bin` or above it.
+    __device__ uint32_t lowest_key(int bin) const
     {
-        uint32_t *words = bins.count;
-        for (int i = threadIdx.x; i < (1 + LIMBS) * SEARCH_BINS; i += THREADS) words[i] = 0;
+        uint32_t lo = LOWEST_FINITE, hi = key_of(top32);
+        while (lo < hi) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (depth_bin(float_of(mid)) <= bin) hi = mid; else lo = mid + 1;
+        }
+        return lo;
+    }
+    // One more element; its mass relative to the top of its depth bin, by the series of exp (the argument lies in -STEP .. 1e-5, the
+    // term left out below 1e-15).  Adding 2^52 leaves the rounded mass in the low bits.
+    template <int N> __device__ __forceinline__ void add(BinCounts<N> &to, int item, float z, int bin)
+    {
+        if (!PPOW_CHECK(item >= 0 && item < N, 801, nullptr)) return;
+        const double depth = __hiloint2double(0x43300000, bin) - 4503599627370496.0;
+        const double x = fma(depth, STEP, ((double)z - top) * per_nat);
+        double w = fma(x, 1.0 / 5040.0, 1.0 / 720.0);
+        w = fma(x, w, 1.0 / 120.0);
+        w = fma(x, w, 1.0 / 24.0);
+        w = fma(x, w, 1.0 / 6.0);
+        w = fma(x, w, 0.5);
+        w = fma(x, w, 1.0);
+        w = fma(x, w, 1.0);
+        w = fma(w, MASS_ONE, 4503599627370496.0);
+        const uint32_t lo = (uint32_t)__double2loint(w), hi = (uint32_t)__double2hiint(w) & 0xfffffu;
+        static_assert(LIMBS == 3 && LIMB_BITS == 13, "limbs");
+        atomicAdd(&to.count[item], 1u);
+        atomicAdd(&to.limb[0][item], lo & 0x1fffu);
+        atomicAdd(&to.limb[1][item], lo >> 13 & 0x1fffu);
+        atomicAdd(&to.limb[2][item], lo >> 26 | hi << 6);
+    }
+    template <int N> __device__ void clear(BinCounts<N> &counts)
+    {
+        for (int i = threadIdx.x; i < (1 + LIMBS) * N; i += THREADS) counts.count[i] = 0;        // the limbs lie behind
         __syncthreads();
     }
-    // one more element, its mass relative to the top of its depth bin
-    __device__ __forceinline__ void add(int item, double d, double bin_top)
-    {
-        if (!PPOW_CHECK(item >= 0 && item < SEARCH_BINS, 801, nullptr)) return;
-        const unsigned long long w = __double2ull_rn(exp((bin_top - d) * per_nat) * MASS_ONE);
-        atomicAdd(&bins.count[item], 1u);
-#pragma unroll
-        for (int i = 0; i < LIMBS; ++i) {
-            const uint32_t limb = (uint32_t)(w >> (i * LIMB_BITS)) & (i == LIMBS - 1 ? 0xffffffffu : (1u << LIMB_BITS) - 1);
-            atomicAdd(&bins.limb[i][item], limb);
-        }
-    }
     // Sums up the CTAs' bins, each CTA a share of them for all, and the groups.  unit(item): what a mass of 1 in this bin stands for.
-    template <typename Unit> __device__ void join(Unit &&unit)
+    template <int N, typename Unit> __device__ void join(BinCounts<N> &counts, BinTotals<N> &totals, Unit &&unit)
     {
         meet(cluster, ctas);
-        for (int i = rank * THREADS + (int)threadIdx.x; i < SEARCH_BINS; i += ctas * THREADS) {
+        for (int i = rank * THREADS + (int)threadIdx.x; i < N; i += ctas * THREADS) {
             uint32_t count = 0;
             unsigned long long limbs[LIMBS] = {};
             for (int r = 0; r < ctas; ++r) {
-                const Bins *b = of(&bins, r);
+                const BinCounts<N> *b = of(&counts, r);
                 count += b->count[i];
 #pragma unroll
                 for (int l = 0; l < LIMBS; ++l) limbs[l] += b->limb[l][i];
@@ -560,30 +506,31 @@ template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
             unsigned long long mass = 0;
 #pragma unroll
             for (int l = 0; l < LIMBS; ++l) mass += limbs[l] << (l * LIMB_BITS);
-            const double m = count ? (double)mass * (1.0 / MASS_ONE) * unit(i) : 0.0;
+            const double m = mass ? (double)mass * (1.0 / MASS_ONE) * unit(i) : 0.0;
             for (int r = 0; r < ctas; ++r) {
-                Bins *b = of(&bins, r);
-                b->all_count[i] = count;
-                b->all_mass[i] = m;
+                BinTotals<N> *t = of(&totals, r);
+                t->count[i] = count;
+                t->mass[i] = m;
             }
         }
         meet(cluster, ctas);
-        for (int c = threadIdx.x >> 5; c < SEARCH_GROUPS; c += (THREADS / 32)) {
+    }
+    // The bin that holds the border; all threads have the result.
+    template <int N> __device__ Place find_bin(const BinTotals<N> &totals, const Target &target, const Place &before)
+    {
+        constexpr int GROUPS = N / SEARCH_GROUP, PER = (GROUPS + 31) / 32;
+        for (int c = threadIdx.x >> 5; c < GROUPS; c += THREADS / 32) {
             const int i = c * SEARCH_GROUP + (threadIdx.x & 31);
-            const uint32_t count = __reduce_add_sync(0xffffffffu, bins.all_count[i]);
-            const double mass = warp_sum_f64(bins.all_mass[i]);
+            const uint32_t count = __reduce_add_sync(0xffffffffu, totals.count[i]);
+            const double mass = warp_sum_f64(totals.mass[i]);
             if ((threadIdx.x & 31) == 0) sh.group_count[c] = count, sh.group_mass[c] = mass;
         }
         __syncthreads();
-    }
-    // The bin that holds the border; all threads have the result.
-    __device__ Place find_bin(const Target &target, const Place &before)
-    {
         if (threadIdx.x < 32) {
-            const Scan<SEARCH_GROUPS / 32> groups(SEARCH_GROUPS, before, [&](int i) { return Part{sh.group_count[i], sh.group_mass[i]}; });
+            const Scan<PER> groups(GROUPS, before, [&](int i) { return Part{sh.group_count[i], sh.group_mass[i]}; });
             Place p = groups.find(target);
             const int first = p.item * SEARCH_GROUP;
-            const Scan<1> in_group(SEARCH_GROUP, p, [&](int i) { return Part{bins.all_count[first + i], bins.all_mass[first + i]}; });
+            const Scan<1> in_group(SEARCH_GROUP, p, [&](int i) { return Part{totals.count[first + i], totals.mass[first + i]}; });
             p = in_group.find(target);
             p.item += first;
             if (threadIdx.x == 0) sh.place = p;
@@ -593,113 +540,63 @@ template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
         __syncthreads();
         return p;
     }
-    __device__ void fill_depths()
-    {
-        if (depths) return;
-        clear();
-        each([&](float z, int32_t) {
-            if (z == -INFINITY) return;
-            const double d = top - (double)z;
-            const int b = depth_bin(d);
-            if (b < SEARCH_BINS - 1)
-                add(b, d, b / scale);
-            else
-                atomicAdd(&bins.count[b], 1u);               // too deep for any mass
-        });
-        join([&](int i) { return exp(-(i / scale) * per_nat); });
-        depths = true;
-    }
-    // The elements that `takes` accepts, MOST at most, sorted, in every CTA of the cluster, with the masses up to each behind `before`.
-    template <typename Takes> __device__ int make_list(double before, Takes &&takes)
+    // Lists this piece's elements with keys in lo .. hi, Bins::LIST at most.
+    __device__ void make_list(uint32_t lo, uint32_t hi)
     {
         if (threadIdx.x == 0) sh.listed = 0;
         __syncthreads();
         each([&](float z, int32_t token) {
-            if (z == -INFINITY || !takes(z)) return;
-            const uint32_t at = atomicAdd(&sh.listed, 1u);
-            if (PPOW_CHECK(at < MOST, 803, nullptr)) (ctas == 1 ? bins.list : bins.own)[at] = list_entry(z, token);
-        });
-        meet(cluster, ctas);
-        int n = 0;
-        if (ctas > 1) {
-            int first = 0;
-            for (int r = 0; r < ctas; ++r) {
-                const int c = (int)*of(&sh.listed, r);
-                if (r < rank) first += c;
-                n += c;
-            }
-            const int mine = (int)sh.listed;
-            for (int r = 0; r < ctas; ++r) {
-                unsigned long long *list = of(bins.list, r);
-                for (int i = threadIdx.x; i < mine; i += THREADS)
-                    if (PPOW_CHECK(first + i < MOST, 804, nullptr)) list[first + i] = bins.own[i];
-            }
-            cluster.sync();
-        } else {
-            n = (int)sh.listed;
-        }
-        sort_list<THREADS>(bins.list, n);
-        add_up_list<THREADS>(bins.list, bins.mass, n, before, sh, [&](float z) { return weight(z); });
-        return n;
-    }
-    // The element on the border; the whole CTA, and the whole cluster in step.
-    __device__ Element find(const Target &target)
-    {
-        fill_depths();
-        Place p = find_bin(target, Place{0, 0, 0.0});
-        const int bin = p.item;
-        if (bins.all_count[bin] <= MOST) {
-            const int n = make_list(p.mass, [&](float z) { return depth_bin(top - (double)z) == bin; });
-            return find_in_list<THREADS>(bins.list, bins.mass, n, p.count, target, sh);
-        }
-        const bool massless = bin == SEARCH_BINS - 1;
-        const double bin_top = bin / scale, unit = massless ? 0.0 : exp(-bin_top * per_nat);
-        // keys in the bin
-        depths = false;
-        if (threadIdx.x == 0) sh.low_key = 0xffffffffu, sh.high_key = 0;
-        meet(cluster, ctas);
-        uint32_t lo = 0xffffffffu, hi = 0;
-        each([&](float z, int32_t) {
-            if (z == -INFINITY || depth_bin(top - (double)z) != bin) return;
             const uint32_t k = key_of(z);
-            lo = min(lo, k), hi = max(hi, k);
+            if (k < lo || k > hi) return;
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (PPOW_CHECK(at < Bins::LIST, 803, nullptr)) bins.list[at] = (unsigned long long)k << 32 | (uint32_t)token;
         });
-        lo = __reduce_min_sync(0xffffffffu, lo), hi = __reduce_max_sync(0xffffffffu, hi);
-        if ((threadIdx.x & 31) == 0)
-            for (int r = 0; r < ctas; ++r) {
-                SampleShared *s = of(&sh, r);
-                atomicMin(&s->low_key, lo);
-                atomicMax(&s->high_key, hi);
-            }
-        meet(cluster, ctas);
-        lo = sh.low_key, hi = sh.high_key;
-        int shift = 0;
-        while (((hi - lo) >> shift) >= SEARCH_BINS) ++shift;
+        __syncthreads();
+        listed = (int)sh.listed;
+    }
+    // The element on the border; the whole CTA, and the whole cluster in step.  The list, if there is one, is left.
+    __device__ Element find(const Target &target, bool whole)
+    {
+        if (!whole) listed = -1;
+        Place p = find_bin(bins.depths, target, Place{0, 0, 0.0});
+        const int bin = p.item;
+        const bool massless = bin == BINS - 1;
+        const double unit = massless ? 0.0 : exp(-bin * STEP);
+        uint32_t lo = lowest_key(bin), hi = bin == 0 ? key_of(top32) : lowest_key(bin - 1) - 1;
+        if (!whole && bins.depths.count[bin] <= Bins::LIST) make_list(lo, hi);
         for (;;) {
-            clear();
+            int shift = 0;
+            while (((hi - lo) >> shift) >= SUB) ++shift;
+            clear(bins.sub);
             each([&](float z, int32_t) {
-                if (z == -INFINITY) return;
                 const uint32_t k = key_of(z);
                 if (k < lo || k > hi) return;
                 const int item = (int)((hi - k) >> shift);
-                if (massless) {
-                    if (PPOW_CHECK(item < SEARCH_BINS, 802, nullptr)) atomicAdd(&bins.count[item], 1u);
-                } else {
-                    add(item, top - (double)z, bin_top);
-                }
+                if (!massless)
+                    add(bins.sub, item, z, bin);
+                else if (PPOW_CHECK(item < SUB, 802, nullptr))
+                    atomicAdd(&bins.sub.count[item], 1u);
             });
-            join([&](int) { return unit; });
-            p = find_bin(target, p);
+            join(bins.sub, bins.subs, [&](int) { return unit; });
+            p = find_bin(bins.subs, target, p);
             hi -= (uint32_t)p.item << shift;
-            if (shift == 0) break;
             const uint32_t width = (1u << shift) - 1;
             lo = hi - lo > width ? hi - width : lo;
-            shift = 0;
-            while (((hi - lo) >> shift) >= SEARCH_BINS) ++shift;
+            if (shift == 0 || bins.subs.count[p.item] == 1) break;
+        }
+        const uint32_t have = bins.subs.count[p.item];
+        if (lo < hi) {                       // one element: which?
+            meet(cluster, ctas);
+            each([&](float z, int32_t token) {
+                const uint32_t k = key_of(z);
+                if (k < lo || k > hi) return;
+                for (int r = 0; r < ctas; ++r) of(&sh, r)->only_key = k, of(&sh, r)->only_token = token;
+            });
+            meet(cluster, ctas);
+            const float value = float_of(sh.only_key);
+            return {value, p.count + 1, p.mass + (massless ? 0.0 : weight(value)), sh.only_token, 0, 1};
         }
         const float value = float_of(hi);
-        const uint32_t have = bins.all_count[p.item];
-        __syncthreads();
         if (massless && !target.by_count()) return {value, p.count + 1, p.mass, -1, 0, have};
         return choose(target, p, value, have, massless ? 0.0 : weight(value));
     }
@@ -707,17 +604,19 @@ template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
     {
         if (threadIdx.x == 0) sh.top = sh.none = sh.flags = sh.within = 0;
         meet(cluster, ctas);
-        uint32_t most = 0, none = 0, bad = 0;
+        float most = -INFINITY;
+        uint32_t none = 0, bad = 0;
         each([&](float z, int32_t) {
             bad |= !(z < INFINITY);
             none += z == -INFINITY;
-            most = max(most, key_of(z));
+            most = fmaxf(most, z);
         });
-        most = __reduce_max_sync(0xffffffffu, most), none = __reduce_add_sync(0xffffffffu, none), bad = __reduce_or_sync(0xffffffffu, bad);
+        const uint32_t key = __reduce_max_sync(0xffffffffu, key_of(most));
+        none = __reduce_add_sync(0xffffffffu, none), bad = __reduce_or_sync(0xffffffffu, bad);
         if ((threadIdx.x & 31) == 0)
             for (int r = 0; r < ctas; ++r) {
                 SampleShared *s = of(&sh, r);
-                atomicMax(&s->top, most);
+                atomicMax(&s->top, key);
                 atomicAdd(&s->none, none);
                 if (bad) atomicOr(&s->flags, (uint32_t)SAMPLE_BAD);
             }
@@ -732,70 +631,83 @@ template <int DTYPE, int THREADS, int SEARCH_BINS> struct Search {
             }
             return;
         }
-        top = (double)float_of(sh.top);
+        top32 = float_of(sh.top);
+        top = (double)top32;
         per_nat = 1.0 / job.temperature;
-        scale = (SEARCH_BINS - 1) / (SEARCH_NATS * job.temperature);
-        depths = false;
+        scale = (float)((BINS - 1) / (SEARCH_NATS * job.temperature));
+        uint32_t floor_key = LOWEST_FINITE;  // of the lowest number within min_p
+        if (job.min_p > 0.0) {
+            uint32_t hi = sh.top;
+            while (floor_key < hi) {
+                const uint32_t mid = floor_key + (hi - floor_key) / 2;
+                if (weight(float_of(mid)) >= job.min_p) hi = mid; else floor_key = mid + 1;
+            }
+        }
+        clear(bins.depth);
+        uint32_t within = 0;
+        each([&](float z, int32_t) {
+            if (z == -INFINITY) return;
+            within += key_of(z) >= floor_key;
+            const int b = depth_bin(z);
+            if (b < BINS - 1)
+                add(bins.depth, b, z, b);
+            else
+                atomicAdd(&bins.depth.count[b], 1u);         // too deep for any mass
+        });
+        within = __reduce_add_sync(0xffffffffu, within);
+        if ((threadIdx.x & 31) == 0)
+            for (int r = 0; r < ctas; ++r) atomicAdd(&of(&sh, r)->within, within);
+        join(bins.depth, bins.depths, [&](int i) { return i < BINS - 1 ? exp(-i * STEP) : 0.0; });
+        const bool whole = F <= Bins::LIST;  // then the list holds the row once and for all
+        if (whole) make_list(LOWEST_FINITE, 0xffffffffu);
+        double all = 0.0;
+        for (int i = threadIdx.x & 31; i < BINS; i += 32) all += bins.depths.mass[i];
+        all = warp_sum_f64(all);
         Element drawn;
         uint32_t n;
         double total;
-        if (F <= MOST) {
-            const int listed = make_list(0.0, [&](float) { return true; });
-            uint32_t within = 0;
-            if (job.min_p > 0.0) {
-                for (int i = threadIdx.x; i < listed; i += THREADS) within += weight(list_value(bins.list[i])) >= job.min_p;
-                within = __reduce_add_sync(0xffffffffu, within);
-                if ((threadIdx.x & 31) == 0) atomicAdd(&sh.within, within);
-                __syncthreads();
-                within = sh.within;
-            }
-            decide(job, job.uniforms[row], F, F, bins.mass[listed - 1], within,
-                   [&](const Target &t) { return find_in_list<THREADS>(bins.list, bins.mass, listed, 0, t, sh); }, drawn, n, total);
-        } else {
-            if (job.min_p > 0.0) {
-                uint32_t within = 0;
-                each([&](float z, int32_t) { within += z > -INFINITY && weight(z) >= job.min_p; });
-                within = __reduce_add_sync(0xffffffffu, within);
-                if ((threadIdx.x & 31) == 0)
-                    for (int r = 0; r < ctas; ++r) atomicAdd(&of(&sh, r)->within, within);
-            }
-            fill_depths();                   // all threads of the row meet in it
-            const uint32_t massive = F - bins.all_count[SEARCH_BINS - 1], within = sh.within;
-            double all = 0.0;
-            for (int c = 0; c < SEARCH_GROUPS; ++c) all += sh.group_mass[c];
-            __syncthreads();
-            decide(job, job.uniforms[row], F, massive, all, within, [&](const Target &t) { return find(t); }, drawn, n, total);
-        }
+        decide(job, job.uniforms[row], F, F - bins.depths.count[BINS - 1], all, sh.within, [&](const Target &t) { return find(t, whole); }, drawn, n,
+               total);
         if (lead) {
             job.logp[row] = (float)(((double)drawn.value - top) * per_nat - log(total));
             if (job.kept) job.kept[row] = (int32_t)n;
             if (drawn.token >= 0) job.tokens[row] = drawn.token;
         }
         if (drawn.token >= 0) return;
-        // one of many equal ones: which piece holds it, and where
-        const HasKey<DTYPE> matches{key_of(drawn.value)};
-        uint32_t skip = 0, have = 0xffffffffu;
+        // one of several equal ones: which piece holds it, and where
+        const uint32_t drawn_key = key_of(drawn.value);
+        uint32_t skip = 0, have = drawn.have;
         if (ctas > 1) {
             if (threadIdx.x == 0) sh.here = 0;
             __syncthreads();
             uint32_t mine = 0;
-            for (int32_t u = piece.begin + (int32_t)threadIdx.x; u < piece.end; u += THREADS) mine += __popc(matches(piece.load(u)));
+            each([&](float z, int32_t) { mine += key_of(z) == drawn_key; });
             mine = __reduce_add_sync(0xffffffffu, mine);
             if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&sh.here, mine);
             cluster.sync();
             for (int r = 0; r < rank; ++r) skip += of(&sh, r)->here;
             have = sh.here;
         }
-        if (drawn.rank >= skip && drawn.rank - skip < have) locate<THREADS>(piece, drawn.rank - skip, sh, job.tokens + row, matches);
+        if (drawn.rank < skip || drawn.rank - skip >= have) return;
+        if (listed < 0) {
+            locate<THREADS>(piece, drawn.rank - skip, sh, job.tokens + row, HasKey<DTYPE>{drawn_key});
+            return;
+        }
+        each([&](float z, int32_t token) {
+            if (key_of(z) != drawn_key) return;
+            uint32_t before = 0;
+            for (int i = 0; i < listed; ++i) before += (uint32_t)(bins.list[i] >> 32) == drawn_key && (int32_t)(uint32_t)bins.list[i] < token;
+            if (before == drawn.rank - skip) job.tokens[row] = token;
+        });
     }
 };
 
-template <int DTYPE, int THREADS, int SEARCH_BINS>
+template <int DTYPE, int THREADS, int BINS>
 __device__ __noinline__ void search_row(const SampleJob &job, int64_t row, int rank, int ctas, SampleShared &sh, void *smem)
 {
     const Piece<DTYPE> piece(job, row, rank, ctas);
     const cg::cluster_group cluster = cg::this_cluster();
-    Search<DTYPE, THREADS, SEARCH_BINS> s{job, piece, cluster, rank, ctas, sh, *static_cast<SearchBins<SEARCH_BINS> *>(smem), 0.0, 0.0, 0.0, false};
+    Search<DTYPE, THREADS, BINS> s{job, piece, cluster, rank, ctas, sh, *static_cast<SearchBins<BINS> *>(smem), 0.0, 0.0, 0.0f, 0.0f, -1};
     s.run(row);
 }
 
@@ -807,7 +719,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_search_kernel(
     __shared__ SampleShared sh;
     const cg::cluster_group cluster = cg::this_cluster();
     const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    search_row<DTYPE, THREADS, LIST>(job, blockIdx.x / ctas, rank, ctas, sh, sample_smem);
+    search_row<DTYPE, THREADS, SEARCH_BINS>(job, blockIdx.x / ctas, rank, ctas, sh, sample_smem);
     if (ctas > 1) cluster.sync();            // no CTA leaves while another still reads its shared memory
 }
 
@@ -1129,7 +1041,7 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
 namespace {
 
 template <auto kernel, int THREADS>
-bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units, cudaStream_t stream)
+bool sample_launch(size_t smem, int per_sm, int passes, const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     static std::atomic<bool> ready[DEVICES];
     int dev = 0;
@@ -1138,9 +1050,13 @@ bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units,
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
         ready[dev].store(true, std::memory_order_relaxed);
     }
-    // As many CTAs to a row as keep the device's places filled, each with 512 units or more; and no more than PIECE_MOST logits to one.
+    // As many CTAs to a row as keep the device's places filled, each with 512 units or more; where a row is passed over several times, so
+    // many that the rows in work stay in the L2 cache; and no more than PIECE_MOST logits to one.
     int ctas = 1;
-    while (ctas < SAMPLE_CTAS && (((int64_t)job.R * ctas * 2 <= 148 * per_sm && units / (ctas * 2) >= 512) || job.V > (int64_t)PIECE_MOST * ctas)) ctas *= 2;
+    while (ctas < SAMPLE_CTAS && job.V > (int64_t)PIECE_MOST * ctas) ctas *= 2;
+    while (ctas < SAMPLE_CTAS && units / (ctas * 2) >= 512 &&
+           ((int64_t)job.R * ctas * 2 <= 148 * per_sm || (passes > 2 && (int64_t)units * 16 * (148 * per_sm / ctas) > 48 << 20)))
+        ctas *= 2;
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3((unsigned)(job.R * ctas));
     config.blockDim = dim3(THREADS);
@@ -1160,14 +1076,14 @@ bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units,
 template <int DTYPE> bool launch_search(const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     constexpr int THREADS = 512;
-    return sample_launch<sample_search_kernel<DTYPE, THREADS>, THREADS>(sizeof(SearchBins<LIST>), 1024 / THREADS, job, units, stream);
+    return sample_launch<sample_search_kernel<DTYPE, THREADS>, THREADS>(sizeof(SearchBins<SEARCH_BINS>), 1024 / THREADS, 4, job, units, stream);
 }
 // A row that counting does not fit is searched in the same shared memory, with half the bins.
 template <int DTYPE> bool launch_count(const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     using F = Counted<DTYPE>;
     static_assert(sizeof(SearchBins<1024>) <= F::WORDS * 4, "room for a search");
-    return sample_launch<sample_count_kernel<DTYPE>, F::THREADS>(F::WORDS * 4, F::CTAS, job, units, stream);
+    return sample_launch<sample_count_kernel<DTYPE>, F::THREADS>(F::WORDS * 4, F::CTAS, 2, job, units, stream);
 }
 
 }  // namespace
@@ -1184,7 +1100,7 @@ extern "C" ppow_status ppow_sample_tokens(const ppow_sample_params *params, cons
 {
     if (!params || params->R < 0 || params->R > (1 << 27) || params->V < 1 || !dtype_ok(params->dtype) || !stride_ok(params->logits_stride, params->V))
         return PPOW_ERR_INVALID_ARG;
-    if (!(params->temperature >= 1e-300 && params->temperature <= 1e300) || params->top_k < 0 || !(params->top_p > 0.0 && params->top_p <= 1.0) ||
+    if (!(params->temperature >= 1e-30 && params->temperature <= 1e30) || params->top_k < 0 || !(params->top_p > 0.0 && params->top_p <= 1.0) ||
         !(params->min_p >= 0.0 && params->min_p <= 1.0))
         return PPOW_ERR_INVALID_ARG;
     if (params->V > SAMPLE_MAX_VOCAB) return PPOW_ERR_UNSUPPORTED;
@@ -1201,8 +1117,8 @@ extern "C" ppow_status ppow_sample_tokens(const ppow_sample_params *params, cons
     if (params->dtype == PPOW_F32)
         ok = launch_search<PPOW_F32>(job, units, stream);
     else if (params->dtype == PPOW_BF16)
-        ok = params->V <= LIST ? launch_search<PPOW_BF16>(job, units, stream) : launch_count<PPOW_BF16>(job, units, stream);
+        ok = params->V <= SEARCH_BINS ? launch_search<PPOW_BF16>(job, units, stream) : launch_count<PPOW_BF16>(job, units, stream);
     else
-        ok = params->V <= LIST ? launch_search<PPOW_F16>(job, units, stream) : launch_count<PPOW_F16>(job, units, stream);
+        ok = params->V <= SEARCH_BINS ? launch_search<PPOW_F16>(job, units, stream) : launch_count<PPOW_F16>(job, units, stream);
     return ok ? PPOW_OK : PPOW_ERR_CUDA;
 }
