@@ -97,7 +97,7 @@ template <int DTYPE> struct Groups {
     }
 };
 constexpr int GROUPS_MOST = Groups<PPOW_F16>::ALL;
-static_assert(GROUPS_MOST >= Groups<PPOW_BF16>::ALL && GROUPS_MOST >= SEARCH_BINS / SEARCH_GROUP, "groups");
+static_assert(GROUPS_MOST >= Groups<PPOW_BF16>::ALL && GROUPS_MOST >= SEARCH_BINS / SEARCH_GROUP * 5 / 4, "groups");
 
 // Order-preserving key of a float32 (-0 is +0), and back.
 __device__ __forceinline__ uint32_t key_of(float z)
@@ -434,34 +434,35 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
             for (int i = threadIdx.x; i < listed; i += THREADS) f(float_of((uint32_t)(bins.list[i] >> 32)), (int32_t)(uint32_t)bins.list[i]);
             return;
         }
-        constexpr int DEEP = 2;
-        for (int32_t u0 = piece.begin + (int32_t)threadIdx.x; u0 < piece.end; u0 += THREADS * DEEP) {
-            uint4 w[DEEP];
+        // one unit at a time: more of them in flight make the code longer and the kernel slower (4: 592 us, 1: 527, 512 x 152064)
+        for (int32_t u = piece.begin + (int32_t)threadIdx.x; u < piece.end; u += THREADS) {
+            float z[E];
+            S::unpack(piece.load(u), z);
 #pragma unroll
-            for (int q = 0; q < DEEP; ++q)
-                if (u0 + q * THREADS < piece.end) w[q] = piece.load(u0 + q * THREADS);
-#pragma unroll
-            for (int q = 0; q < DEEP; ++q)
-                if (u0 + q * THREADS < piece.end) {
-                    float z[E];
-                    S::unpack(w[q], z);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) f(z[e], piece.token(u0 + q * THREADS, e));
-                }
+            for (int e = 0; e < E; ++e) f(z[e], piece.token(u, e));
         }
     }
     __device__ __forceinline__ double weight(float z) const { return exp(((double)z - top) * per_nat); }
     // In float32, whose differences and products keep the order: a bin is a stretch of numbers.  Its rounding moves a border by 1e-5 nats.
     __device__ __forceinline__ int depth_bin(float z) const { return (int)fminf((top32 - z) * scale, (float)(BINS - 1)); }
-    // Key of the lowest number that is in `bin` or above it.
-    __device__ uint32_t lowest_key(int bin) const
+    // The lowest key in lo .. hi whose number `accepts`, which all above it are and hi's is: 32 places at a time, by each warp for itself.
+    template <typename Accepts> __device__ uint32_t lowest_key(uint32_t lo, uint32_t hi, Accepts &&accepts) const
     {
-        uint32_t lo = LOWEST_FINITE, hi = key_of(top32);
+        const uint32_t lane = threadIdx.x & 31;
         while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (depth_bin(float_of(mid)) <= bin) hi = mid; else lo = mid + 1;
+            const uint32_t step = (hi - lo) / 32 + 1, at = lo + lane * step;     // lane 0 is lo
+            const uint32_t yes = __ballot_sync(0xffffffffu, at < hi ? accepts(float_of(at)) : true);
+            const int first = __ffs(yes) - 1;                // 0: lo itself; none (step 1 and 32 places): hi
+            if (first == 0) return lo;
+            const uint32_t last_no = lo + (uint32_t)(first < 0 ? 31 : first - 1) * step, first_yes = first < 0 ? hi : lo + (uint32_t)first * step;
+            lo = last_no + 1, hi = min(first_yes, hi);
         }
         return lo;
+    }
+    // of a number in `bin` or above it
+    __device__ uint32_t lowest_of(int bin) const
+    {
+        return lowest_key(LOWEST_FINITE, key_of(top32), [&](float z) { return depth_bin(z) <= bin; });
     }
     // One more element; its mass relative to the top of its depth bin, by the series of exp (the argument lies in -STEP .. 1e-5, the
     // term left out below 1e-15).  Adding 2^52 leaves the rounded mass in the low bits.
@@ -515,24 +516,28 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         }
         meet(cluster, ctas);
     }
-    // The bin that holds the border; all threads have the result.
-    template <int N> __device__ Place find_bin(const BinTotals<N> &totals, const Target &target, const Place &before)
+    // The groups' sums, from `first` on in sh.
+    template <int N> __device__ void sum_bins(const BinTotals<N> &totals, int first)
     {
-        constexpr int GROUPS = N / SEARCH_GROUP, PER = (GROUPS + 31) / 32;
-        for (int c = threadIdx.x >> 5; c < GROUPS; c += THREADS / 32) {
+        for (int c = threadIdx.x >> 5; c < N / SEARCH_GROUP; c += THREADS / 32) {
             const int i = c * SEARCH_GROUP + (threadIdx.x & 31);
             const uint32_t count = __reduce_add_sync(0xffffffffu, totals.count[i]);
             const double mass = warp_sum_f64(totals.mass[i]);
-            if ((threadIdx.x & 31) == 0) sh.group_count[c] = count, sh.group_mass[c] = mass;
+            if ((threadIdx.x & 31) == 0) sh.group_count[first + c] = count, sh.group_mass[first + c] = mass;
         }
         __syncthreads();
+    }
+    // The bin that holds the border; all threads have the result.
+    template <int N> __device__ Place find_bin(const BinTotals<N> &totals, int first, const Target &target, const Place &before)
+    {
+        constexpr int GROUPS = N / SEARCH_GROUP, PER = (GROUPS + 31) / 32;
         if (threadIdx.x < 32) {
-            const Scan<PER> groups(GROUPS, before, [&](int i) { return Part{sh.group_count[i], sh.group_mass[i]}; });
+            const Scan<PER> groups(GROUPS, before, [&](int i) { return Part{sh.group_count[first + i], sh.group_mass[first + i]}; });
             Place p = groups.find(target);
-            const int first = p.item * SEARCH_GROUP;
-            const Scan<1> in_group(SEARCH_GROUP, p, [&](int i) { return Part{totals.count[first + i], totals.mass[first + i]}; });
+            const int start = p.item * SEARCH_GROUP;
+            const Scan<1> in_group(SEARCH_GROUP, p, [&](int i) { return Part{totals.count[start + i], totals.mass[start + i]}; });
             p = in_group.find(target);
-            p.item += first;
+            p.item += start;
             if (threadIdx.x == 0) sh.place = p;
         }
         __syncthreads();
@@ -540,16 +545,16 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         __syncthreads();
         return p;
     }
-    // Lists this piece's elements with keys in lo .. hi, Bins::LIST at most.
+    // Lists the piece's elements with keys in lo .. hi, Bins::LIST at most.
     __device__ void make_list(uint32_t lo, uint32_t hi)
     {
         if (threadIdx.x == 0) sh.listed = 0;
         __syncthreads();
+        const float low = float_of(lo), high = float_of(hi);
         each([&](float z, int32_t token) {
-            const uint32_t k = key_of(z);
-            if (k < lo || k > hi) return;
+            if (!(z >= low && z <= high)) return;
             const uint32_t at = atomicAdd(&sh.listed, 1u);
-            if (PPOW_CHECK(at < Bins::LIST, 803, nullptr)) bins.list[at] = (unsigned long long)k << 32 | (uint32_t)token;
+            if (PPOW_CHECK(at < Bins::LIST, 803, nullptr)) bins.list[at] = (unsigned long long)key_of(z) << 32 | (uint32_t)token;
         });
         __syncthreads();
         listed = (int)sh.listed;
@@ -558,11 +563,11 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
     __device__ Element find(const Target &target, bool whole)
     {
         if (!whole) listed = -1;
-        Place p = find_bin(bins.depths, target, Place{0, 0, 0.0});
+        Place p = find_bin(bins.depths, 0, target, Place{0, 0, 0.0});
         const int bin = p.item;
         const bool massless = bin == BINS - 1;
         const double unit = massless ? 0.0 : exp(-bin * STEP);
-        uint32_t lo = lowest_key(bin), hi = bin == 0 ? key_of(top32) : lowest_key(bin - 1) - 1;
+        uint32_t lo = lowest_of(bin), hi = bin == 0 ? key_of(top32) : lowest_of(bin - 1) - 1;
         if (!whole && bins.depths.count[bin] <= Bins::LIST) make_list(lo, hi);
         for (;;) {
             int shift = 0;
@@ -578,7 +583,8 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
                     atomicAdd(&bins.sub.count[item], 1u);
             });
             join(bins.sub, bins.subs, [&](int) { return unit; });
-            p = find_bin(bins.subs, target, p);
+            sum_bins(bins.subs, BINS / SEARCH_GROUP);
+            p = find_bin(bins.subs, BINS / SEARCH_GROUP, target, p);
             hi -= (uint32_t)p.item << shift;
             const uint32_t width = (1u << shift) - 1;
             lo = hi - lo > width ? hi - width : lo;
@@ -636,18 +642,13 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         per_nat = 1.0 / job.temperature;
         scale = (float)((BINS - 1) / (SEARCH_NATS * job.temperature));
         uint32_t floor_key = LOWEST_FINITE;  // of the lowest number within min_p
-        if (job.min_p > 0.0) {
-            uint32_t hi = sh.top;
-            while (floor_key < hi) {
-                const uint32_t mid = floor_key + (hi - floor_key) / 2;
-                if (weight(float_of(mid)) >= job.min_p) hi = mid; else floor_key = mid + 1;
-            }
-        }
+        if (job.min_p > 0.0) floor_key = lowest_key(LOWEST_FINITE, sh.top, [&](float z) { return weight(z) >= job.min_p; });
+        const float floor = float_of(floor_key);
         clear(bins.depth);
         uint32_t within = 0;
         each([&](float z, int32_t) {
             if (z == -INFINITY) return;
-            within += key_of(z) >= floor_key;
+            within += z >= floor;
             const int b = depth_bin(z);
             if (b < BINS - 1)
                 add(bins.depth, b, z, b);
@@ -659,9 +660,10 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
             for (int r = 0; r < ctas; ++r) atomicAdd(&of(&sh, r)->within, within);
         join(bins.depth, bins.depths, [&](int i) { return i < BINS - 1 ? exp(-i * STEP) : 0.0; });
         const bool whole = F <= Bins::LIST;  // then the list holds the row once and for all
-        if (whole) make_list(LOWEST_FINITE, 0xffffffffu);
+        if (whole) make_list(LOWEST_FINITE, sh.top);
+        sum_bins(bins.depths, 0);
         double all = 0.0;
-        for (int i = threadIdx.x & 31; i < BINS; i += 32) all += bins.depths.mass[i];
+        for (int i = threadIdx.x & 31; i < BINS / SEARCH_GROUP; i += 32) all += sh.group_mass[i];
         all = warp_sum_f64(all);
         Element drawn;
         uint32_t n;
@@ -948,7 +950,7 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
     const int64_t row = blockIdx.x / ctas;
     const Piece<DTYPE> piece(job, row, rank, ctas);
     auto of = [&](auto *p, int r) { return ctas == 1 ? p : cluster.map_shared_rank(p, r); };
-    constexpr int DEEP = 4;
+    constexpr int DEEP = 2;
     uint4 w[DEEP];
     auto fetch = [&](int32_t u0) {           // behind the piece's end, -inf
 #pragma unroll
@@ -1041,7 +1043,7 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
 namespace {
 
 template <auto kernel, int THREADS>
-bool sample_launch(size_t smem, int per_sm, int passes, const SampleJob &job, int32_t units, cudaStream_t stream)
+bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     static std::atomic<bool> ready[DEVICES];
     int dev = 0;
@@ -1050,13 +1052,11 @@ bool sample_launch(size_t smem, int per_sm, int passes, const SampleJob &job, in
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
         ready[dev].store(true, std::memory_order_relaxed);
     }
-    // As many CTAs to a row as keep the device's places filled, each with 512 units or more; where a row is passed over several times, so
-    // many that the rows in work stay in the L2 cache; and no more than PIECE_MOST logits to one.
+    // As many CTAs to a row as keep the device's places filled, each with 512 units or more; and no more than PIECE_MOST logits to one.  (A
+    // float32 row is passed over four times: shared by four CTAs the rows in work would stay in the L2 cache, but each pass ends in
+    // meetings.  512 x 152064: 717 us against 590.)
     int ctas = 1;
-    while (ctas < SAMPLE_CTAS && job.V > (int64_t)PIECE_MOST * ctas) ctas *= 2;
-    while (ctas < SAMPLE_CTAS && units / (ctas * 2) >= 512 &&
-           ((int64_t)job.R * ctas * 2 <= 148 * per_sm || (passes > 2 && (int64_t)units * 16 * (148 * per_sm / ctas) > 48 << 20)))
-        ctas *= 2;
+    while (ctas < SAMPLE_CTAS && (((int64_t)job.R * ctas * 2 <= 148 * per_sm && units / (ctas * 2) >= 512) || job.V > (int64_t)PIECE_MOST * ctas)) ctas *= 2;
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3((unsigned)(job.R * ctas));
     config.blockDim = dim3(THREADS);
@@ -1076,14 +1076,14 @@ bool sample_launch(size_t smem, int per_sm, int passes, const SampleJob &job, in
 template <int DTYPE> bool launch_search(const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     constexpr int THREADS = 512;
-    return sample_launch<sample_search_kernel<DTYPE, THREADS>, THREADS>(sizeof(SearchBins<SEARCH_BINS>), 1024 / THREADS, 4, job, units, stream);
+    return sample_launch<sample_search_kernel<DTYPE, THREADS>, THREADS>(sizeof(SearchBins<SEARCH_BINS>), 1024 / THREADS, job, units, stream);
 }
 // A row that counting does not fit is searched in the same shared memory, with half the bins.
 template <int DTYPE> bool launch_count(const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     using F = Counted<DTYPE>;
     static_assert(sizeof(SearchBins<1024>) <= F::WORDS * 4, "room for a search");
-    return sample_launch<sample_count_kernel<DTYPE>, F::THREADS>(F::WORDS * 4, F::CTAS, 2, job, units, stream);
+    return sample_launch<sample_count_kernel<DTYPE>, F::THREADS>(F::WORDS * 4, F::CTAS, job, units, stream);
 }
 
 }  // namespace
