@@ -10,6 +10,7 @@
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <string>
@@ -267,32 +268,48 @@ py::object rms_norm_backward(const at::Tensor &grad_y, const c10::optional<at::T
     return py::make_tuple(status_of(st), to_python(gx), to_python(gw));
 }
 
-py::object clip_gradients(const std::vector<at::Tensor> &grads, const c10::optional<std::vector<at::Tensor>> &out, double max_norm)
+// The tensors of a list, without a reference each: the list holds them.  False if something else is in it.
+bool tensors_of(const py::list &list, std::vector<const at::Tensor *> &tensors)
 {
-    if (grads.empty() || grads.size() > 65536 || (out && out->size() != grads.size())) return py::none();
-    const Place at(grads[0]);
+    const size_t n = list.size();
+    tensors.resize(n);
+    for (size_t i = 0; i < n; ++i) {
+        PyObject *item = PyList_GET_ITEM(list.ptr(), (Py_ssize_t)i);
+        if (!THPVariable_Check(item)) return false;
+        tensors[i] = &THPVariable_Unpack(item);
+    }
+    return true;
+}
+
+py::object clip_gradients(const py::list &grad_list, const py::object &out_list, double max_norm)
+{
+    std::vector<const at::Tensor *> grads, out;
+    const size_t n = grad_list.size();
+    if (n == 0 || n > 65536 || !tensors_of(grad_list, grads)) return py::none();
+    if (!out_list.is_none() && (!py::isinstance<py::list>(out_list) || !tensors_of(py::reinterpret_borrow<py::list>(out_list), out) || out.size() != n))
+        return py::none();
+    const bool write = !out_list.is_none();
+    const Place at(*grads[0]);
     if (!at.here) return py::none();
-    const size_t n = grads.size();
     std::vector<const void *> from(n);
-    std::vector<void *> to(n);
+    std::vector<void *> to(write ? n : 0);
     std::vector<int64_t> sizes(n);
     std::vector<int32_t> dtypes(n);
     for (size_t i = 0; i < n; ++i) {
-        const at::Tensor &g = grads[i];
+        const at::Tensor &g = *grads[i];
         if (!on_device(g, at.dev) || (dtypes[i] = code_of(g.scalar_type())) < 0 || !g.is_non_overlapping_and_dense()) return py::none();
         from[i] = g.data_ptr();
         sizes[i] = g.numel();
-        if (out) {
-            const at::Tensor &o = (*out)[i];
-            if (!on_device(o, at.dev) || o.scalar_type() != g.scalar_type() || o.sizes() != g.sizes() || o.strides() != g.strides())
-                return py::none();
-            to[i] = o.data_ptr();
-        }
+        if (!write) continue;
+        const at::Tensor &o = *out[i];
+        if (&o != &g && (!on_device(o, at.dev) || o.scalar_type() != g.scalar_type() || o.sizes() != g.sizes() || o.strides() != g.strides()))
+            return py::none();
+        to[i] = o.data_ptr();
     }
     const at::Tensor norm = at.empty({}, at::kFloat);
     const size_t bytes = lib.clip_workspace_bytes((int32_t)n);
     const at::Tensor ws = at.scratch(bytes);
-    const ppow_status st = lib.clip_gradients((int32_t)n, from.data(), out ? to.data() : nullptr, sizes.data(), dtypes.data(), max_norm,
+    const ppow_status st = lib.clip_gradients((int32_t)n, from.data(), write ? to.data() : nullptr, sizes.data(), dtypes.data(), max_norm,
                                               norm.data_ptr<float>(), ws.data_ptr(), bytes, at.stream);
     return py::make_tuple(status_of(st), to_python(norm));
 }

@@ -27,7 +27,8 @@ struct ClipEntry {
     void *out;
     int64_t size;            // elements
 };
-// Tensors of a launch: a short table for the common case, and a long one just below the limit of kernel arguments (32764 bytes).
+// Tensors of a launch.  Three sizes of table, for it is copied at every launch; the longest is just below the limit of kernel arguments
+// (32764 bytes).
 template <int N> struct ClipTable {
     static constexpr int MOST = N;
     ClipEntry at[N];
@@ -36,6 +37,7 @@ template <int N> struct ClipTable {
     int32_t n, chunks;
 };
 using ShortTable = ClipTable<48>;
+using MiddleTable = ClipTable<256>;
 using LongTable = ClipTable<1024>;
 static_assert(sizeof(LongTable) + 64 <= 32764, "kernel arguments");
 
@@ -370,8 +372,9 @@ extern "C" ppow_status ppow_clip_gradients(int32_t n, const void *const *grads, 
     }
     double *shares = static_cast<double *>(workspace);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    return (n <= ShortTable::MOST ? clip_launch<ShortTable>(n, grads, out, sizes, dtypes, max_norm, in_place, norm, shares, stream)
-                                  : clip_launch<LongTable>(n, grads, out, sizes, dtypes, max_norm, in_place, norm, shares, stream))
+    return (n <= ShortTable::MOST    ? clip_launch<ShortTable>(n, grads, out, sizes, dtypes, max_norm, in_place, norm, shares, stream)
+            : n <= MiddleTable::MOST ? clip_launch<MiddleTable>(n, grads, out, sizes, dtypes, max_norm, in_place, norm, shares, stream)
+                                     : clip_launch<LongTable>(n, grads, out, sizes, dtypes, max_norm, in_place, norm, shares, stream))
                ? PPOW_OK
                : PPOW_ERR_CUDA;
 }
