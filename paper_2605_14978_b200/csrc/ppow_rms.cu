@@ -15,12 +15,18 @@
 
 namespace ppow {
 
-// Slots of rows in flight per CTA: as many as keep two or more CTAs on an SM, up to four.  `bytes`: of one row in all its streams,
-// times the rows that a CTA takes at a time.
-__host__ __device__ constexpr int rms_slots(size_t bytes, int threads)
+// Slots of rows in flight per CTA.  `bytes`: of one row in all its streams, times the rows that a CTA takes at a time.
+//   many streams (x and residual; gradient, input and residual's gradient): one slot, the other CTAs' rows fill the wait.  16384 x 4096
+//   bf16: forward 84 us with one slot, 95 with three; backward 91 with one, 99 with two
+//   otherwise two at least, and what 40 KB hold.  8192 x 8192 bf16 without a residual: forward 44 us with two, 60 with one; backward 74 and 85
+// Rows of a warp take more slots (16384 x 1024: 21.2 us with four, 22.4 with one), so do the widest (4096 x 16384: 42.6 us with three, 46.5
+// with two); float32 rows, twice as long, what 56 KB hold.
+template <int DTYPE, int TPR> __host__ __device__ constexpr int rms_slots(size_t bytes, bool many_streams)
 {
-    const size_t room = threads <= 256 ? 56 * 1024 : 112 * 1024;
-    return room / bytes >= 4 ? 4 : room / bytes >= 1 ? (int)(room / bytes) : 1;
+    if (DTYPE == PPOW_F32 || TPR == 32) return 56 * 1024 / bytes >= 4 ? 4 : 56 * 1024 / bytes >= 1 ? (int)(56 * 1024 / bytes) : 1;
+    if (many_streams) return 1;
+    if (TPR == 512) return 112 * 1024 / bytes >= 3 ? 3 : 1;
+    return 40 * 1024 / bytes >= 4 ? 4 : 40 * 1024 / bytes >= 2 ? (int)(40 * 1024 / bytes) : bytes <= 56 * 1024 ? 2 : 1;
 }
 
 // ---- forward ----------------------------------------------------------------------------------------
@@ -42,7 +48,7 @@ struct RmsJob {
 template <int DTYPE, bool VEC, bool RES, int TPR> struct RmsForward {
     using DealT = Deal<DTYPE, VEC>;
     static constexpr int U = norm_units<DTYPE, VEC>(), THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR;
-    static constexpr int S = rms_slots((size_t)(RES ? 2 : 1) * U * THREADS * 16, THREADS);
+    static constexpr int S = rms_slots<DTYPE, TPR>((size_t)(RES ? 2 : 1) * U * THREADS * 16, RES);
     using Ahead = RowAhead<DTYPE, VEC, TPR, U, S>;
     static constexpr size_t SMEM = ROWS * (RES ? 2 : 1) * Ahead::BYTES;
 };
@@ -170,7 +176,7 @@ template <int DTYPE, bool VEC, bool PACKED, bool RES, int TPR> struct RmsBackwar
     using DealT = Deal<DTYPE, VEC>;
     static constexpr int U = norm_units<DTYPE, VEC>(), THREADS = norm_threads<TPR>(), ROWS = THREADS / TPR;
     static constexpr size_t UNIT = (RES ? 32 : 16) + (PACKED ? DealT::E : 16);       // bytes of a unit in all streams
-    static constexpr int S = VEC ? rms_slots(UNIT * U * THREADS, THREADS) : 2;
+    static constexpr int S = VEC ? rms_slots<DTYPE, TPR>(UNIT * U * THREADS, RES && !PACKED) : 1;      // the scalar deal's rows sit in registers
     using Grads = RowAhead<DTYPE, VEC, TPR, U, S>;
     using Inputs = std::conditional_t<PACKED, CodesAhead<DTYPE, VEC, TPR, U, S>, RowAhead<DTYPE, VEC, TPR, U, S>>;
     using Scalars = ScalarsAhead<DealT, PACKED, TPR, U, S>;
@@ -178,9 +184,13 @@ template <int DTYPE, bool VEC, bool PACKED, bool RES, int TPR> struct RmsBackwar
     static constexpr size_t SMEM = ROWS * ROW;
 };
 
+// Blocks on an SM that registers have to leave room for.  Left to itself the compiler gives the scalar deal of an 8-bit input so many (for
+// addresses of single bytes) that few warps are left: 8192 x 4095 with a residual 240 us, with two blocks 136.
+template <bool VEC, bool PACKED, int TPR> __host__ __device__ constexpr int rms_blocks() { return VEC || !PACKED || TPR >= 512 ? 1 : TPR <= 128 ? 4 : 2; }
+
 // Two passes over a row's values, both from the thread's own copies: sums first, then dx.
 template <int DTYPE, bool VEC, bool PACKED, bool RES, int TPR>
-__global__ void __launch_bounds__(norm_threads<TPR>()) rms_backward_kernel(const RmsGradJob job)
+__global__ void __launch_bounds__(norm_threads<TPR>(), rms_blocks<VEC, PACKED, TPR>()) rms_backward_kernel(const RmsGradJob job)
 {
     wait_for_previous_kernel();
     using Shape = RmsBackward<DTYPE, VEC, PACKED, RES, TPR>;
@@ -229,10 +239,10 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) rms_backward_kernel(const
     int slot = 0, turn = 0;
     const float2 zero = make_float2(0.0f, 0.0f);
     for (int64_t row = first; row < job.R; row += step, turn ^= 1) {
+        start(slot == 0 ? S - 1 : slot - 1, row + LEAD * step);          // S == 1: the row itself
         grads.take();
         inputs.take();
         if constexpr (RES) more.take();
-        start(slot == 0 ? S - 1 : slot - 1, row + LEAD * step);          // S == 1: the row itself
         copy_wait<LEAD>();
         __syncwarp();
         const float rstd = scalars.get(slot, 1);
