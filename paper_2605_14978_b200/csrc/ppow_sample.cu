@@ -15,7 +15,7 @@
 //   float32         A row holds any numbers, so they go into 2048 bins of equal depth below the maximum, each with its count and its mass in
 //                   fixed point relative to the bin's top (integers again).  The few hundred elements of the bin that holds a border
 //                   are listed, and dealt out over the keys in it until a part holds one element or one number; a bin of more than
-//                   2048 (many equal ones) in passes over the row.  Short rows are listed whole, of any type.  16-bit rows that the
+//                   2048 (many equal ones) in passes over the row.  Short rows are listed whole.  16-bit rows that the
 //                   counting does not fit (logits of 2048 and more, more than 65535 equal ones) go the same way.
 //
 // A cluster of CTAs shares a row, each with a contiguous piece of it: one CTA when there are rows enough, up to eight for a few.
@@ -705,7 +705,7 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
 };
 
 template <int DTYPE, int THREADS, int BINS>
-__device__ __noinline__ void search_row(const SampleJob &job, int64_t row, int rank, int ctas, SampleShared &sh, void *smem)
+__device__ __forceinline__ void search_row(const SampleJob &job, int64_t row, int rank, int ctas, SampleShared &sh, void *smem)
 {
     const Piece<DTYPE> piece(job, row, rank, ctas);
     const cg::cluster_group cluster = cg::this_cluster();
@@ -713,7 +713,7 @@ __device__ __noinline__ void search_row(const SampleJob &job, int64_t row, int r
     s.run(row);
 }
 
-template <int DTYPE, int THREADS>
+template <int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_search_kernel(const SampleJob job)
 {
     wait_for_previous_kernel();
@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_search_kernel(
     __shared__ SampleShared sh;
     const cg::cluster_group cluster = cg::this_cluster();
     const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    search_row<DTYPE, THREADS, SEARCH_BINS>(job, blockIdx.x / ctas, rank, ctas, sh, sample_smem);
+    search_row<PPOW_F32, THREADS, SEARCH_BINS>(job, blockIdx.x / ctas, rank, ctas, sh, sample_smem);
     if (ctas > 1) cluster.sync();            // no CTA leaves while another still reads its shared memory
 }
 
@@ -935,6 +935,14 @@ __device__ __forceinline__ void decide_counted(const SampleJob &job, int64_t row
     }
 }
 
+// A row that counting does not fit, in the same shared memory with half the bins.  Rare, and out of line: registers are the others'.
+template <int DTYPE, int THREADS>
+__device__ __noinline__ void search_odd_row(const SampleJob &job, int64_t row, int rank, int ctas, SampleShared &sh, void *smem)
+{
+    static_assert(sizeof(SearchBins<1024>) <= Counted<DTYPE>::WORDS * 4, "room for a search");
+    search_row<DTYPE, THREADS, 1024>(job, row, rank, ctas, sh, smem);
+}
+
 template <int DTYPE>
 __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS) sample_count_kernel(const SampleJob job)
 {
@@ -1003,7 +1011,7 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
         const bool odd = drawn.rank == SAMPLE_ODD;
         meet(cluster, ctas);                 // everybody has read what the search writes over
         if (odd) {
-            search_row<DTYPE, THREADS, 1024>(job, row, rank, ctas, sh, sample_smem);
+            search_odd_row<DTYPE, THREADS>(job, row, rank, ctas, sh, sample_smem);
             meet(cluster, ctas);
         }
         return;
@@ -1073,16 +1081,14 @@ bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units,
     return cudaLaunchKernelEx(&config, kernel, job) == cudaSuccess;
 }
 
-template <int DTYPE> bool launch_search(const SampleJob &job, int32_t units, cudaStream_t stream)
+bool launch_search(const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     constexpr int THREADS = 512;
-    return sample_launch<sample_search_kernel<DTYPE, THREADS>, THREADS>(sizeof(SearchBins<SEARCH_BINS>), 1024 / THREADS, job, units, stream);
+    return sample_launch<sample_search_kernel<THREADS>, THREADS>(sizeof(SearchBins<SEARCH_BINS>), 1024 / THREADS, job, units, stream);
 }
-// A row that counting does not fit is searched in the same shared memory, with half the bins.
 template <int DTYPE> bool launch_count(const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     using F = Counted<DTYPE>;
-    static_assert(sizeof(SearchBins<1024>) <= F::WORDS * 4, "room for a search");
     return sample_launch<sample_count_kernel<DTYPE>, F::THREADS>(F::WORDS * 4, F::CTAS, job, units, stream);
 }
 
@@ -1113,12 +1119,8 @@ extern "C" ppow_status ppow_sample_tokens(const ppow_sample_params *params, cons
                            params->top_p, params->min_p,         tokens,   logp,      kept};
     const int32_t units = (int32_t)((params->V * (int64_t)es + 15) / 16);
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    bool ok = false;
-    if (params->dtype == PPOW_F32)
-        ok = launch_search<PPOW_F32>(job, units, stream);
-    else if (params->dtype == PPOW_BF16)
-        ok = params->V <= SEARCH_BINS ? launch_search<PPOW_BF16>(job, units, stream) : launch_count<PPOW_BF16>(job, units, stream);
-    else
-        ok = params->V <= SEARCH_BINS ? launch_search<PPOW_F16>(job, units, stream) : launch_count<PPOW_F16>(job, units, stream);
+    const bool ok = params->dtype == PPOW_F32    ? launch_search(job, units, stream)
+                    : params->dtype == PPOW_BF16 ? launch_count<PPOW_BF16>(job, units, stream)
+                                                 : launch_count<PPOW_F16>(job, units, stream);
     return ok ? PPOW_OK : PPOW_ERR_CUDA;
 }
