@@ -1197,7 +1197,7 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
 namespace {
 
 template <auto kernel, int THREADS>
-bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units, cudaStream_t stream)
+bool sample_launch(size_t smem, const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     static std::atomic<bool> ready[DEVICES];
     int dev = 0;
@@ -1206,11 +1206,12 @@ bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units,
         if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return false;
         ready[dev].store(true, std::memory_order_relaxed);
     }
-    // As many CTAs to a row as keep the device's places filled, each with 512 units or more; and no more than PIECE_MOST logits to one.  (A
-    // float32 row is passed over four times: shared by four CTAs the rows in work would stay in the L2 cache, but each pass ends in
-    // meetings.  512 x 152064: 717 us against 590.)
+    // Few rows are shared out, until 768 threads to an SM have work, each CTA with 1024 units or more: what a CTA does besides reading
+    // its piece costs as much as 2000 units.  74 x 128256 bf16: 31 us with 296 CTAs, 35 with 148, 47 with 592; f16: 37 with 148, 61 with
+    // 296; f32: 92 and 121.  And no more than PIECE_MOST logits to a CTA.  (A float32 row is passed over four times: shared by four CTAs
+    // the rows in work would stay in the L2 cache, but each pass ends in meetings.  512 x 152064: 717 us against 590.)
     int ctas = 1;
-    while (ctas < SAMPLE_CTAS && (((int64_t)job.R * ctas * 2 <= 148 * per_sm && units / (ctas * 2) >= 512) || job.V > (int64_t)PIECE_MOST * ctas)) ctas *= 2;
+    while (ctas < SAMPLE_CTAS && (((int64_t)job.R * ctas * 2 * THREADS <= 148 * 768 && units / (ctas * 2) >= 1024) || job.V > (int64_t)PIECE_MOST * ctas)) ctas *= 2;
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3((unsigned)(job.R * ctas));
     config.blockDim = dim3(THREADS);
@@ -1230,7 +1231,7 @@ bool sample_launch(size_t smem, int per_sm, const SampleJob &job, int32_t units,
 bool launch_search(const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     constexpr int THREADS = 512;
-    return sample_launch<sample_search_kernel<THREADS>, THREADS>(sizeof(SearchBins<SEARCH_BINS>), 1024 / THREADS, job, units, stream);
+    return sample_launch<sample_search_kernel<THREADS>, THREADS>(sizeof(SearchBins<SEARCH_BINS>), job, units, stream);
 }
 template <int PER> bool launch_sort(const SampleJob &job, cudaStream_t stream)
 {
@@ -1239,7 +1240,7 @@ template <int PER> bool launch_sort(const SampleJob &job, cudaStream_t stream)
 template <int DTYPE> bool launch_count(const SampleJob &job, int32_t units, cudaStream_t stream)
 {
     using F = Counted<DTYPE>;
-    return sample_launch<sample_count_kernel<DTYPE>, F::THREADS>(F::WORDS * 4, F::CTAS, job, units, stream);
+    return sample_launch<sample_count_kernel<DTYPE>, F::THREADS>(F::WORDS * 4, job, units, stream);
 }
 
 }  // namespace
