@@ -240,8 +240,9 @@ struct Element {
 // Which of `have` equal elements of this weight, behind `before`, the border falls on.
 __device__ __forceinline__ Element choose(const Target &target, const Place &before, float value, uint32_t have, double weight)
 {
-    uint32_t rank;
-    if (target.by_count()) {
+    uint32_t rank = 0;
+    if (have == 1) {
+    } else if (target.by_count()) {
         rank = min(target.count - before.count, have) - 1;
     } else {
         // the quotient is right to a small part of 1, but for weights below 1e-13 of the mass, which no border can tell apart
@@ -944,6 +945,23 @@ template <int DTYPE> struct Count {
     }
 };
 
+// Weights of the four numbers of a group from `first` on, by rising magnitude.  A group lies within one power of two, so they are a step apart: one
+// exp for the largest and one for the step, unless the step is more than a nat.
+template <int DTYPE> __device__ __forceinline__ void weights_of(int group, int first, double top, double per_nat, double (&w)[4])
+{
+    using G = Groups<DTYPE>;
+    const double z0 = (double)G::number(group, first), z3 = (double)G::number(group, first + 3), step = fabs(z3 - z0) * (1.0 / 3.0) * per_nat;
+    if (step > 1.0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = exp(((double)G::number(group, first + i) - top) * per_nat);
+        return;
+    }
+    const double r = exp(-step), e = exp((fmax(z0, z3) - top) * per_nat), r2 = r * r;
+    const double down[4] = {e, e * r, e * r2, e * (r2 * r)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = G::negative(group) ? down[i] : down[3 - i];
+}
+
 // The groups' counts and masses: each CTA adds up a share of the groups for all, in its own words (the others read none of those).
 template <int DTYPE>
 __device__ __forceinline__ void sum_groups(const SampleJob &job, int rank, int ctas, SampleShared &sh, uint4 *words)
@@ -983,12 +1001,12 @@ __device__ __forceinline__ void sum_groups(const SampleJob &job, int rank, int c
             const uint32_t have = b[side][0] + b[side][1] + b[side][2] + b[side][3];
             if (!__any_sync(0xffffffffu, have != 0)) continue;
             const int group = side ? G::ZERO + 1 + g : g;
-            double mass = 0.0;
+            double mass = 0.0, weights[4];
+            weights_of<DTYPE>(group, lane * 4, top, per_nat, weights);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const double e = exp(((double)G::number(group, lane * 4 + i) - top) * per_nat);
-                mass += b[side][i] ? b[side][i] * e : 0.0;   // beyond the maximum e may overflow, with nothing to count
-                within += e >= job.min_p ? b[side][i] : 0u;
+                mass += b[side][i] ? b[side][i] * weights[i] : 0.0;      // beyond the maximum a weight may overflow, with nothing to count
+                within += weights[i] >= job.min_p || G::number(group, lane * 4 + i) == (float)top ? b[side][i] : 0u;
             }
             mass = warp_sum_f64(mass);
             const uint32_t counted = __reduce_add_sync(0xffffffffu, have);
@@ -1016,7 +1034,7 @@ __device__ __forceinline__ void sum_groups(const SampleJob &job, int rank, int c
 
 // What is kept of a row, and the draw, from the groups' counts and masses; sh.drawn.n is 0 where there is none (rank: the flags). One warp.
 template <int DTYPE>
-__device__ __forceinline__ void decide_counted(const SampleJob &job, int64_t row, uint32_t logits, int rank, int ctas, SampleShared &sh, const uint4 *own)
+__device__ __forceinline__ void decide_counted(const SampleJob &job, int64_t row, float uniform, uint32_t logits, int rank, int ctas, SampleShared &sh, const uint4 *own)
 {
     using F = Counted<DTYPE>;
     using G = Groups<DTYPE>;
@@ -1058,20 +1076,25 @@ __device__ __forceinline__ void decide_counted(const SampleJob &job, int64_t row
         const uint32_t have[4] = {(negative ? words.x : words.w) >> half & 0xffffu, (negative ? words.y : words.z) >> half & 0xffffu,
                                   (negative ? words.z : words.y) >> half & 0xffffu, (negative ? words.w : words.x) >> half & 0xffffu};
         auto number = [&](int i) { return G::number(group, negative ? i : GROUP - 1 - i); };
-        auto weight = [&](int i) { return exp(((double)number(i) - top) * per_nat); };
+        double rising[4];
+        weights_of<DTYPE>(group, negative ? lane * 4 : GROUP - 4 - lane * 4, top, per_nat, rising);
+        const double falling[4] = {negative ? rising[0] : rising[3], negative ? rising[1] : rising[2], negative ? rising[2] : rising[1],
+                                   negative ? rising[3] : rising[0]};
         const Scan<GROUP / 32> numbers(GROUP, p, [&](int i) {
             const uint32_t c = have[i % 4];
-            const double e = weight(i);
-            return Part{c, c ? c * e : 0.0};                 // beyond the maximum e may overflow
+            return Part{c, c ? c * falling[i % 4] : 0.0};      // beyond the maximum a weight may overflow
         });
         p = numbers.find(target);
-        const uint32_t mine = p.item % 4 == 0 ? have[0] : p.item % 4 == 1 ? have[1] : p.item % 4 == 2 ? have[2] : have[3];
-        return choose(target, p, number(p.item), __shfl_sync(0xffffffffu, mine, p.item / 4), weight(p.item));
+        const int at_lane = p.item / 4, slot = p.item % 4;
+        const uint32_t mine = slot == 0 ? have[0] : slot == 1 ? have[1] : slot == 2 ? have[2] : have[3];
+        const double weight = slot == 0 ? falling[0] : slot == 1 ? falling[1] : slot == 2 ? falling[2] : falling[3];
+        // the weight that the masses were added up from: a border on a multiple of it stays there
+        return choose(target, p, number(p.item), __shfl_sync(0xffffffffu, mine, at_lane), __shfl_sync(0xffffffffu, weight, at_lane));
     };
     Element drawn;
     uint32_t n;
     double total;
-    decide(job, job.uniforms[row], all.count + low, all.count, all.mass, sh.within, find, drawn, n, total);
+    decide(job, uniform, all.count + low, all.count, all.mass, sh.within, find, drawn, n, total);
     if (lane == 0) {
         if (rank == 0) {
             job.logp[row] = (float)(((double)drawn.value - top) * per_nat - log(total));
@@ -1103,6 +1126,7 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = blockIdx.x / ctas;
     const Piece<DTYPE> piece(job, row, rank, ctas);
+    const float uniform = job.uniforms[row];                 // on its way early
     auto of = [&](auto *p, int r) { return ctas == 1 ? p : cluster.map_shared_rank(p, r); };
     constexpr int DEEP = 2;
     uint4 w[DEEP];
@@ -1150,7 +1174,7 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
     meet(cluster, ctas);
     sum_groups<DTYPE>(job, rank, ctas, sh, sample_smem);
     meet(cluster, ctas);
-    if (warp == 0) decide_counted<DTYPE>(job, row, (uint32_t)piece.units * 8, rank, ctas, sh, sample_smem);
+    if (warp == 0) decide_counted<DTYPE>(job, row, uniform, (uint32_t)piece.units * 8, rank, ctas, sh, sample_smem);
     __syncthreads();
     const Element drawn = sh.drawn;
     if (drawn.n == 0) {                      // the same for all CTAs of the row
