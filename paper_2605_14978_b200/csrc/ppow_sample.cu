@@ -461,10 +461,14 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         }
         return lo;
     }
-    // of a number in `bin` or above it
+    // Of a number in `bin` or above it, sought around where the bin ends but for rounding.
     __device__ uint32_t lowest_of(int bin) const
     {
-        return lowest_key(LOWEST_FINITE, key_of(top32), [&](float z) { return depth_bin(z) <= bin; });
+        auto accepts = [&](float z) { return depth_bin(z) <= bin; };
+        const float end = top32 - (float)(bin + 1) / scale, about = 1e-6f * (fabsf(top32) + fabsf(end));
+        const uint32_t lo = max(key_of(end - about), LOWEST_FINITE), hi = min(key_of(end + about), key_of(top32));
+        const bool inside = lo < hi && !accepts(float_of(lo)) && accepts(float_of(hi));
+        return lowest_key(inside ? lo + 1 : LOWEST_FINITE, inside ? hi : key_of(top32), accepts);
     }
     // One more element; its mass relative to the top of its depth bin, by the series of exp (the argument lies in -STEP .. 1e-5, the
     // term left out below 1e-15).  Adding 2^52 leaves the rounded mass in the low bits.
