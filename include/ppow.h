@@ -461,7 +461,8 @@ ppow_status ppow_clip_gradients(int32_t n, const void *const *grads, void *const
  *               nothing else gives token -1, logp -inf, kept 0; a row with a NaN or +inf gives token -1, logp NaN, kept 0
  *   uniforms    device, [R] float32 in [0, 1); others count as the nearest in it, NaN as 0
  *   tokens      device, [R] int32        logp   device, [R] float32        kept   device, [R] int32 or NULL: n
- * 16-bit logits of magnitudes below 2048 (float16) or 4096 (bfloat16) take one pass over memory; float32 and others take several.
+ * 16-bit logits of magnitudes below 2048 (float16), or 0 and 2^-51 up to 8192 (bfloat16), or far below the largest, take one pass over memory
+ * and another over half of the row; float32 and other rows take several.
  * No workspace.
  */
 typedef struct {

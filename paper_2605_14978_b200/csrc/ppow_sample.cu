@@ -11,13 +11,13 @@
 //
 //   16-bit logits   A row holds at most 65536 different numbers: one pass counts them, by integer additions in shared memory, and all the
 //                   rest is arithmetic on a few thousand (number, count) pairs.  Bound by those additions (one warp's 32 fall on the 32
-//                   banks at random, about 4 cycles) where the row's bytes take 2.7 of the same cycles.
+//                   banks at random, 3 cycles) where the row's bytes take 2.7 of the same cycles.
 //   short float32   Up to 2048 are sorted, and their masses added up in that order.
 //   float32         A row holds any numbers, so they go into 2048 bins of equal depth below the maximum, each with its count and its mass in
 //                   fixed point relative to the bin's top (integers again).  The few hundred elements of the bin that holds a border
 //                   are listed, and dealt out over the keys in it until a part holds one element or one number; a bin of more than
-//                   2048 (many equal ones) in passes over the row.  16-bit rows that the
-//                   counting does not fit (logits of 2048 and more, more than 65535 equal ones) go the same way.
+//                   2048 (many equal ones) in passes over the row.  16-bit rows that the counting does not fit (very large or
+//                   very small logits, more than 65535 equal ones) go the same way.
 //
 // A cluster of CTAs shares a row, each with a contiguous piece of it: one CTA when there are rows enough, up to eight for a few.
 #include "ppow_checked.cuh"
@@ -942,7 +942,7 @@ template <int DTYPE> struct Count {
             ++zeros;
         else if (magnitude >= F::INF)
             flags |= SAMPLE_BAD;
-        else if (bits & 0x8000u && magnitude > F::WORDS)
+        else if (bits & 0x8000u && magnitude >= F::LOW + F::WORDS)
             ++low;
         else
             flags |= SAMPLE_ODD;

@@ -148,6 +148,19 @@ def test_rows_that_counting_does_not_fit(R, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tiny", [2.0 ** -50, 2.0 ** -51, 2.0 ** -52, 1e-17, 2.0 ** -63, 2.0 ** -64, 1e-30, 1e-39, 2.0 ** -24])
+def test_logits_next_to_zero(tiny, dtype):
+    # few logits near zero decide a row of otherwise deep ones, and order among themselves by sign and magnitude
+    z, u = make(8, 3000, dtype, seed=13)
+    z = (z - 30.0).to(dtype)
+    for i in range(8):
+        near = torch.tensor([tiny, -tiny, 0.0, -0.0, 2 * tiny, -3 * tiny, -0.5, 0.25][: i + 1], dtype=torch.float64, device=DEV)
+        z[i, 17 * (i + 1):17 * (i + 1) + 7 * near.numel():7] = near.to(dtype)
+    for k in (dict(), dict(top_k=3), dict(top_p=0.6), dict(min_p=0.9), dict(temperature=0.1, top_p=0.9)):
+        check(z, u, B.sample_tokens(z, u, **k), **k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_uniforms_at_the_ends_and_outside(dtype):
     z, _ = make(12, 3001, dtype, seed=5)
     u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 2.0 ** -149, 0.5, 1.0, 2.0, -1.0, math.nan, INF, -INF, -0.0, 2.0 ** -30], device=DEV)
