@@ -62,7 +62,7 @@ def build_calls(force: bool = False) -> str:
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), '-DPPOW_TORCH_MARK="%s"' % _torch_mark(),
            "-I" + os.path.join(at, "include"), "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
            "-I" + os.path.join(cuda, "include"), "-I" + sysconfig.get_path("include"), os.path.join(CSRC, "ppow_calls.cpp"), "-o", tmp,
-           "-L" + os.path.join(at, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+           "-L" + os.path.join(at, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cuda", "-ltorch_cpu", "-ltorch_python"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("g++ failed:\n" + res.stderr)

@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -92,8 +93,12 @@ struct Place {
     {
         if (here) stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
     }
-    at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type) const { return at::empty(sizes, options.dtype(type)); }
-    at::Tensor scratch(size_t bytes) const { return at::empty({(int64_t)(bytes ? bytes : 256)}, options.dtype(at::kByte)); }
+    // without the dispatcher, which the type and device would only lead back here (3 tensors: 0.9 us less)
+    at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type) const
+    {
+        return at::detail::empty_cuda(sizes, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)dev), c10::nullopt);
+    }
+    at::Tensor scratch(size_t bytes) const { return empty({(int64_t)(bytes ? bytes : 256)}, at::kByte); }
 };
 
 py::object status_of(ppow_status st) { return py::int_((int)st); }

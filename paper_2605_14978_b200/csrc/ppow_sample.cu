@@ -950,7 +950,7 @@ template <int DTYPE> struct Count {
 };
 
 // Weights of the four numbers of a group from `first` on, by rising magnitude.  A group lies within one power of two, so they are a step apart: one
-// exp for the largest and one for the step, unless the step is more than a nat.
+// exp for the largest and one for the step, unless the step is more than a nat.  That of the maximum is 1.
 template <int DTYPE> __device__ __forceinline__ void weights_of(int group, int first, double top, double per_nat, double (&w)[4])
 {
     using G = Groups<DTYPE>;
@@ -963,7 +963,7 @@ template <int DTYPE> __device__ __forceinline__ void weights_of(int group, int f
     const double r = exp(-step), e = exp((fmax(z0, z3) - top) * per_nat), r2 = r * r;
     const double down[4] = {e, e * r, e * r2, e * (r2 * r)};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = G::negative(group) ? down[i] : down[3 - i];
+    for (int i = 0; i < 4; ++i) w[i] = (double)G::number(group, first + i) == top ? 1.0 : G::negative(group) ? down[i] : down[3 - i];
 }
 
 // The groups' counts and masses: each CTA adds up a share of the groups for all, in its own words (the others read none of those).
@@ -1010,7 +1010,7 @@ __device__ __forceinline__ void sum_groups(const SampleJob &job, int rank, int c
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 mass += b[side][i] ? b[side][i] * weights[i] : 0.0;      // beyond the maximum a weight may overflow, with nothing to count
-                within += weights[i] >= job.min_p || G::number(group, lane * 4 + i) == (float)top ? b[side][i] : 0u;
+                within += weights[i] >= job.min_p ? b[side][i] : 0u;
             }
             mass = warp_sum_f64(mass);
             const uint32_t counted = __reduce_add_sync(0xffffffffu, have);
