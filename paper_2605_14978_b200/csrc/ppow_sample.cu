@@ -311,39 +311,38 @@ __device__ __forceinline__ void decide(const SampleJob &job, float u, uint32_t F
     }
 }
 
-// The index of the rank-th element of this piece that `matches` accepts, searched in rounds: each warp a stretch of neighbouring units, the
-// next round's on their way while this one's are counted.  matches: a byte with a bit for each of a unit's elements, that of element e at
-// e / 2 + 4 (e % 2) where there are eight, at e where there are four.  Out of line: inlined, it takes registers from the rest (4096 x
-// 128256: 442 us, inlined 487).
+// The index of an element of this piece that `matches` accepts and `behind` others follow, searched from the end, where the pass over the row
+// was last and the L2 cache still holds most, in rounds: each warp a stretch of neighbouring units, the next round's on their way while
+// this one's are counted.  matches: a byte with a bit for each of a unit's elements, that of element e at e / 2 + 4 (e % 2) where there are
+// eight, at e where there are four.  Out of line: inlined, it takes registers from the rest (4096 x 128256: 442 us, inlined 487).
 template <int THREADS, int DTYPE, typename Matches>
-__device__ __noinline__ void locate(const Piece<DTYPE> piece, uint32_t rank, SampleShared &sh, int32_t *token, const Matches matches)
+__device__ __noinline__ void locate(const Piece<DTYPE> piece, uint32_t behind, SampleShared &sh, int32_t *token, const Matches matches)
 {
-    constexpr int DEEP = 4;                  // 8: 13 % slower, what is read behind the token costs more than the rounds
+    constexpr int DEEP = 4;                  // 8: 13 % slower, what is read beyond the token costs more than the rounds
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t seen = 0;
     int turn = 0;
     uint4 next[DEEP];
+    auto unit = [&](int32_t base, int q) { return base - (warp * DEEP + q) * 32 - lane; };
     auto fetch = [&](int32_t base) {
 #pragma unroll
-        for (int q = 0; q < DEEP; ++q) {
-            const int32_t u = base + (warp * DEEP + q) * 32 + lane;
-            if (u < piece.end) next[q] = piece.load(u);
-        }
+        for (int q = 0; q < DEEP; ++q)
+            if (unit(base, q) >= piece.begin) next[q] = piece.load(unit(base, q));
     };
-    fetch(piece.begin);
-    for (int32_t base = piece.begin; base < piece.end; base += THREADS * DEEP, turn ^= 1) {
+    fetch(piece.end - 1);
+    for (int32_t base = piece.end - 1; base >= piece.begin; base -= THREADS * DEEP, turn ^= 1) {
         uint32_t bits = 0;
 #pragma unroll
         for (int q = 0; q < DEEP; ++q)
-            if (base + (warp * DEEP + q) * 32 + lane < piece.end) bits |= matches(next[q]) << (q * 8);
-        fetch(base + THREADS * DEEP);
+            if (unit(base, q) >= piece.begin) bits |= matches(next[q]) << (q * 8);
+        fetch(base - THREADS * DEEP);
         const uint32_t mine = __reduce_add_sync(0xffffffffu, __popc(bits));
         if (lane == 0) sh.warp_count[turn][warp] = mine;
         __syncthreads();
         const uint32_t c = lane < (THREADS / 32) ? sh.warp_count[turn][lane] : 0u;
         uint32_t before = seen + __reduce_add_sync(0xffffffffu, lane < warp ? c : 0u);
         seen += __reduce_add_sync(0xffffffffu, c);
-        if (before <= rank && rank < before + mine) {
+        if (before <= behind && behind < before + mine) {
             for (int q = 0; q < DEEP; ++q) {
                 const uint32_t m = bits >> (q * 8) & 0xffu;
                 uint32_t upto = __popc(m);
@@ -354,15 +353,15 @@ __device__ __noinline__ void locate(const Piece<DTYPE> piece, uint32_t rank, Sam
                 }
                 uint32_t from = before + upto - __popc(m);
 #pragma unroll
-                for (int e = 0; e < Piece<DTYPE>::E; ++e)
+                for (int e = Piece<DTYPE>::E - 1; e >= 0; --e)
                     if (m >> (Piece<DTYPE>::E == 8 ? e / 2 + e % 2 * 4 : e) & 1) {
-                        if (from == rank) *token = piece.token(base + (warp * DEEP + q) * 32 + lane, e);
+                        if (from == behind) *token = piece.token(unit(base, q), e);
                         ++from;
                     }
                 before += __shfl_sync(0xffffffffu, upto, 31);
             }
         }
-        if (seen > rank) return;             // the same for the whole CTA
+        if (seen > behind) return;           // the same for the whole CTA
     }
 }
 
@@ -698,7 +697,7 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         }
         if (drawn.rank < skip || drawn.rank - skip >= have) return;
         if (listed < 0) {
-            locate<THREADS>(piece, drawn.rank - skip, sh, job.tokens + row, HasKey<DTYPE>{drawn_key});
+            locate<THREADS>(piece, have - 1 - (drawn.rank - skip), sh, job.tokens + row, HasKey<DTYPE>{drawn_key});
             return;
         }
         each([&](float z, int32_t token) {
@@ -1217,7 +1216,7 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
         skip = __reduce_add_sync(0xffffffffu, lane < rank ? c : 0u);
         have = __shfl_sync(0xffffffffu, c, rank);
     }
-    if (drawn.rank >= skip && drawn.rank - skip < have) locate<THREADS>(piece, drawn.rank - skip, sh, job.tokens + row, matches);
+    if (drawn.rank >= skip && drawn.rank - skip < have) locate<THREADS>(piece, have - 1 - (drawn.rank - skip), sh, job.tokens + row, matches);
     if (ctas > 1) cluster.sync();            // no CTA leaves while another still reads its shared memory
 }
 
