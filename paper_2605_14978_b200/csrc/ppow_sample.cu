@@ -314,7 +314,8 @@ __device__ __forceinline__ void decide(const SampleJob &job, float u, uint32_t F
 // The index of an element of this piece that `matches` accepts and `behind` others follow, searched from the end, where the pass over the row
 // was last and the L2 cache still holds most, in rounds: each warp a stretch of neighbouring units, the next round's on their way while
 // this one's are counted.  matches: a byte with a bit for each of a unit's elements, that of element e at e / 2 + 4 (e % 2) where there are
-// eight, at e where there are four.  Out of line: inlined, it takes registers from the rest (4096 x 128256: 442 us, inlined 487).
+// eight, at e where there are four.  Out of line: inlined, it takes registers from the rest (4096 x 128256: 10 % slower).  From
+// the row's start the same took 438 us, so 432.
 template <int THREADS, int DTYPE, typename Matches>
 __device__ __noinline__ void locate(const Piece<DTYPE> piece, uint32_t behind, SampleShared &sh, int32_t *token, const Matches matches)
 {
