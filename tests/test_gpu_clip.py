@@ -111,6 +111,19 @@ def test_magnitudes_whose_squares_float32_does_not_hold(dtype, scale):
     check(grads, 0.01 * norm, got, out)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_norm", [1e-5, 1e-20, 1e-30, 1e-37, 1e-42])
+def test_factors_that_float32_does_not_hold(max_norm, dtype):
+    # the factor lies far below 2^-126, the clipped gradients are ordinary numbers (of the last two, small ones)
+    g = torch.Generator(device=DEV).manual_seed(8)
+    grads = [(torch.randn((n,), generator=g, device=DEV).double() * 1e35).to(dtype) for n in (5, 70000, 999)]
+    grads.append((torch.randn((5000,), generator=g, device=DEV).double() * 1e-3).to(dtype))          # nothing is left of these
+    out = [torch.empty_like(t) for t in grads]
+    got = B.clip_gradients(grads, max_norm, out=out)
+    torch.cuda.synchronize()
+    check(grads, max_norm, got, out)
+
+
 def test_zeros_infinities_and_nan():
     grads = [torch.zeros(1000, device=DEV, dtype=torch.bfloat16), torch.zeros(3, device=DEV)]
     assert float(B.clip_gradients(grads, 0.0)) == 0.0 and not grads[0].any()
