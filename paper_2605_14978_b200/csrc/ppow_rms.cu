@@ -276,6 +276,8 @@ __global__ void __launch_bounds__(norm_threads<TPR>(), rms_blocks<VEC, PACKED, T
             s2 = 0.0f;
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) s2 += part[turn][i];
+        } else {
+            __syncwarp();                                    // the next row's start writes over scalars that all lanes have read by now
         }
         s2 *= -inv_d;
         const float2 m2 = make_float2(s2, s2);
