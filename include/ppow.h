@@ -440,7 +440,8 @@ size_t ppow_clip_workspace_bytes(int32_t n);
  *                   output may overlap a gradient or another output (PPOW_ERR_INVALID_ARG)
  *   sizes, dtypes   host, [n]: elements (0 is allowed, 2^40 in all at most) and ppow_dtype of each
  *   max_norm        >= 0, finite; ignored where out is NULL
- *   norm            device, one float32
+ *   norm            device, one float32 that lies in no gradient, output or workspace; infinite where float32 does not hold it (the
+ *                   factor still goes by the 64-bit one)
  *   workspace       device, >= ppow_clip_workspace_bytes(n), 256-byte aligned
  * The host arrays are read before the call returns.  In place, gradients within max_norm are not written.
  */
