@@ -614,7 +614,9 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
     }
     __device__ void run(int64_t row)
     {
+        const bool lead = rank == 0 && threadIdx.x == 0;
         if (threadIdx.x == 0) sh.top = sh.none = sh.flags = sh.within = 0;
+        if (lead) job.tokens[row] = -1;      // never left unwritten, even if the row changes between its readings
         meet(cluster, ctas);
         float most = -INFINITY;
         uint32_t none = 0, bad = 0;
@@ -634,10 +636,8 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
             }
         meet(cluster, ctas);
         const uint32_t F = (uint32_t)piece.units * E - sh.none;
-        const bool lead = rank == 0 && threadIdx.x == 0;
         if (sh.flags & SAMPLE_BAD || F == 0) {
             if (lead) {
-                job.tokens[row] = -1;
                 job.logp[row] = F == 0 && !(sh.flags & SAMPLE_BAD) ? -INFINITY : NAN;
                 if (job.kept) job.kept[row] = 0;
             }
@@ -880,9 +880,6 @@ template <int PER> __global__ void __launch_bounds__(SORT_THREADS) sample_sort_k
 template <int DTYPE> struct Count {
     using F = Counted<DTYPE>;
     static constexpr uint32_t NEG_INF = 0x8000u | F::INF;
-    // what of (magnitude - LOW) is beyond WORDS: its bits in either half (bfloat16), or the top bit of a sum (float16)
-    static constexpr uint32_t OFFSET = DTYPE == PPOW_BF16 ? 0u - F::LOW * 0x10001u : (0x8000u - F::WORDS) * 0x10001u;
-    static constexpr uint32_t BEYOND = DTYPE == PPOW_BF16 ? (0xffffu - F::MASK) * 0x10001u : 0x80008000u;
     static constexpr bool ZEROS = F::LOW > 0;                // counted apart
     char *words;
     uint32_t none = 0, low = 0, zeros = 0, flags = 0, most = NEG_INF * 0x10001u;
@@ -896,8 +893,16 @@ template <int DTYPE> struct Count {
     }
     __device__ __forceinline__ void low_half(uint32_t w) { atomicAdd(reinterpret_cast<uint32_t *>(words + (w << 2 & F::MASK << 2)), one<0x4499>(w)); }
     __device__ __forceinline__ void high_half(uint32_t w) { atomicAdd(reinterpret_cast<uint32_t *>(words + (w >> 14 & F::MASK << 2)), one<0x44bb>(w)); }
-    // Not zero if a half may be beyond the counted range (a borrow from the low half can only add to what it says of the high one).
-    static __device__ __forceinline__ uint32_t beyond(uint32_t w) { return ((w & 0x7fff7fffu) + OFFSET) & BEYOND; }
+    // Not zero in the halves that are beyond the counted range.  Nothing goes from one half to the other: above its magnitude a half has a 1,
+    // which the difference with LOW leaves (its bits past WORDS are those of a borrow, or of what is too large), and a sum with
+    // 2^15 - WORDS reaches 2^15 and stays below 2^16.
+    static __device__ __forceinline__ uint32_t beyond(uint32_t w)
+    {
+        if constexpr (F::LOW > 0)
+            return (((w | 0x80008000u) - F::LOW * 0x10001u) ^ 0x80008000u) & (0xffffu - F::MASK) * 0x10001u;
+        else
+            return ((w & 0x7fff7fffu) + (0x8000u - F::WORDS) * 0x10001u) & 0x80008000u;
+    }
 
     // Eight logits; the whole warp calls.   Bound by the integer units (4 operations a logit) and the additions in shared memory: nothing
     // is looked at one by one where all are in range, or in range and -inf (one way for the warp: both would cost the sum).
@@ -931,14 +936,12 @@ template <int DTYPE> struct Count {
             }
         }
     }
-    // What has not been counted, or taken for beyond the range on account of its neighbour; -inf was counted already.
+    // What has not been counted; -inf was counted already.
     __device__ __forceinline__ void beyond_one(uint32_t bits, bool counted)
     {
         const uint32_t magnitude = bits & 0x7fffu;
         if (counted || bits == NEG_INF) return;
-        if (magnitude - F::LOW < F::WORDS)
-            low_half(bits);
-        else if (magnitude == 0)
+        if (magnitude == 0)
             ++zeros;
         else if (magnitude >= F::INF)
             flags |= SAMPLE_BAD;
@@ -1059,7 +1062,6 @@ __device__ __forceinline__ void decide_counted(const SampleJob &job, int64_t row
     if (flags || all.count == 0) {
         if (lane == 0) {
             if (rank == 0 && (flags & SAMPLE_BAD || flags == 0)) {
-                job.tokens[row] = -1;
                 job.logp[row] = flags ? NAN : -INFINITY;
                 if (job.kept) job.kept[row] = 0;
             }
@@ -1146,6 +1148,7 @@ __global__ void __launch_bounds__(Counted<DTYPE>::THREADS, Counted<DTYPE>::CTAS)
     for (int i = threadIdx.x; i < (int)F::WORDS / 4; i += THREADS) sample_smem[i] = make_uint4(0, 0, 0, 0);
     for (int i = threadIdx.x; i < G::ALL; i += THREADS) sh.group_count[i] = 0, sh.group_mass[i] = 0.0;
     if (threadIdx.x == 0) sh.none = sh.low = sh.zeros = sh.flags = sh.within = sh.top = 0;
+    if (rank == 0 && threadIdx.x == 0) job.tokens[row] = -1;     // never left unwritten, even if the row changes between its two readings
     meet(cluster, ctas);                     // the others write into these
     {
         Count<DTYPE> count{reinterpret_cast<char *>(sample_smem)};
