@@ -456,8 +456,8 @@ ppow_status ppow_clip_gradients(int32_t n, const void *const *grads, void *const
  *     n_k = min(top_k, number of logits above -inf)         n_p = least n <= n_k with C_n >= top_p * C_(n_k)
  *     n_m = number of i with w_i >= min_p                   n   = min(n_k, n_p, n_m)
  *     token = the first in that order with C_j > u * C_n        logp = (z_token - z_1) / temperature - ln C_n
- * so logp is that of the distribution the token was drawn from.  Masses are 64-bit: tokens are those of the definition, whichever
- * way a row is cut, and repeat.
+ * so logp is that of the distribution the token was drawn from.  Weights are right to 1e-13 of themselves and their sums lose no more, so
+ * tokens are those of the definition but where u lies within 1e-13 of a border; they are the same whichever way a row is cut, and repeat.
  *   logits      device, [R, V], rows logits_stride elements apart, aligned to the element size.  -inf forbids a token.  A row of
  *               nothing else gives token -1, logp -inf, kept 0; a row with a NaN or +inf gives token -1, logp NaN, kept 0
  *   uniforms    device, [R] float32 in [0, 1); others count as the nearest in it, NaN as 0

@@ -7,14 +7,15 @@
 //   n   = min(n_k, n_p, n_m);    token = first j with C_j > u C_n;    logp = (z_j - z_max) / T - ln C_n
 //
 // A draw lies next to one of up to a million borders, so the masses have to be right to far more digits than float32 holds if the token
-// is to be the definition's, and the same whichever way the row is cut.  All masses are float64, and none depends on an order:
+// is to be the definition's, and the same whichever way the row is cut.  All masses are float64, or integers of which each weight has 43 bits
+// and more (right to 1e-13 of it), and none depends on an order:
 //
 //   16-bit logits   A row holds at most 65536 different numbers: one pass counts them, by integer additions in shared memory, and all the
 //                   rest is arithmetic on a few thousand (number, count) pairs.  Bound by those additions (one warp's 32 fall on the 32
 //                   banks at random, 3 cycles) where the row's bytes take 2.7 of the same cycles.
 //   short float32   Up to 2048 are sorted, and their masses added up in that order.
-//   float32         A row holds any numbers, so they go into 2048 bins of equal depth below the maximum, each with its count and its mass in
-//                   fixed point relative to the bin's top (integers again).  The few hundred elements of the bin that holds a border
+//   float32         A row holds any numbers, so they go into 2048 bins of equal depth below the maximum, each with its count and what its
+//                   mass falls short of the count, in fixed point relative to the bin's top (integers again).  The few hundred elements of the bin that holds a border
 //                   are listed, and dealt out over the keys in it until a part holds one element or one number; a bin of more than
 //                   2048 (many equal ones) in passes over the row.  16-bit rows that the counting does not fit (very large or
 //                   very small logits, more than 65535 equal ones) go the same way.
@@ -36,9 +37,9 @@ constexpr int SEARCH_GROUP = 32;         // the same of the bins of a search
 constexpr int SEARCH_BINS = 2048;
 constexpr double SEARCH_NATS = 56.0;     // what lies deeper than this below the maximum has no mass: 2^22 exp(-56) is 2e-18
 constexpr uint32_t LOWEST_FINITE = 0x00800000u;     // key of the lowest float32 above -inf
-// A mass in fixed point, 2^38 to 1, is added up in three limbs of 13 bits, so that 2^19 elements to a CTA fit words of 32.
+// What weights fall short of a bin's top is added up in fixed point, in three limbs of 13 bits, so that 2^19 elements to a CTA fit words of 32.
 constexpr int LIMBS = 3, LIMB_BITS = 13;
-constexpr double MASS_ONE = 274877906944.0;
+constexpr double LIMBS_HOLD = 549755813888.0;        // 2^39
 constexpr int32_t PIECE_MOST = 1 << 19;
 
 struct SampleJob {
@@ -392,7 +393,7 @@ template <int DTYPE> struct Equals {
 };
 
 // ---- search: any row --------------------------------------------------------------------------------
-// Counts and masses of bins, the masses in fixed point as limbs: of this CTA, and of the cluster.
+// Counts of bins and what their masses fall short of them, in fixed point as limbs, of this CTA; counts and masses of the cluster.
 template <int BINS> struct BinCounts {
     uint32_t count[BINS], limb[LIMBS][BINS];
 };
@@ -418,6 +419,11 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
     using Bins = SearchBins<BINS>;
     static constexpr int E = S::PER_UNIT, SUB = Bins::SUB;
     static constexpr double STEP = SEARCH_NATS / (BINS - 1);         // depth of a bin, nats
+    // A weight lies between exp(-STEP) and 1 of its bin's top, so only the small rest to 1 is held, 2^44 (2^43 of wider bins) to 1: off by
+    // 2^-45 (2^-44) of the bin's top, and not at all at the maximum.  SLACK keeps it above 0 where the rounding of depth_bin puts a number
+    // into the bin below its own, by up to 1e-5.
+    static constexpr double SLACK = 0x1p-15, UNIT = (STEP + 2 * SLACK) * 0x1p44 < LIMBS_HOLD ? 0x1p44 : 0x1p43;
+    static_assert((STEP + 2 * SLACK) * UNIT < LIMBS_HOLD, "limbs");
     const SampleJob &job;
     const Piece<DTYPE> &piece;
     const cg::cluster_group &cluster;
@@ -470,11 +476,10 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         const bool inside = lo < hi && !accepts(float_of(lo)) && accepts(float_of(hi));
         return lowest_key(inside ? lo + 1 : LOWEST_FINITE, inside ? hi : key_of(top32), accepts);
     }
-    // One more element; its mass relative to the top of its depth bin, by the series of exp (the argument lies in -STEP .. 1e-5, the
-    // term left out below 1e-15).  Adding 2^52 leaves the rounded mass in the low bits.
-    template <int N> __device__ __forceinline__ void add(BinCounts<N> &to, int item, float z, int bin)
+    // UNIT times what z's weight falls short of the top of its depth bin, rounded, and SLACK, above 2^52: the low bits are the integer.  By the
+    // series of exp(x) - 1 (x lies in -STEP .. 1e-5 but for rounding; the term left out is below 1e-17, in wider bins below 3e-15).
+    __device__ __forceinline__ double rest_of(float z, int bin) const
     {
-        if (!PPOW_CHECK(item >= 0 && item < N, 801, nullptr)) return;
         const double depth = __hiloint2double(0x43300000, bin) - 4503599627370496.0;
         const double x = fma(depth, STEP, ((double)z - top) * per_nat);
         double w = fma(x, 1.0 / 5040.0, 1.0 / 720.0);
@@ -483,8 +488,18 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         w = fma(x, w, 1.0 / 6.0);
         w = fma(x, w, 0.5);
         w = fma(x, w, 1.0);
-        w = fma(x, w, 1.0);
-        w = fma(w, MASS_ONE, 4503599627370496.0);
+        return fma(x * w, -UNIT, 4503599627370496.0 + SLACK * UNIT);
+    }
+    // z's weight as the masses are added up from it; top_weight: that of the bin's top
+    __device__ __forceinline__ double weight_in(float z, int bin, double top_weight) const
+    {
+        return (1.0 - (rest_of(z, bin) - (4503599627370496.0 + SLACK * UNIT)) * (1.0 / UNIT)) * top_weight;
+    }
+    // One more element.
+    template <int N> __device__ __forceinline__ void add(BinCounts<N> &to, int item, float z, int bin)
+    {
+        if (!PPOW_CHECK(item >= 0 && item < N, 801, nullptr)) return;
+        const double w = rest_of(z, bin);
         const uint32_t lo = (uint32_t)__double2loint(w), hi = (uint32_t)__double2hiint(w) & 0xfffffu;
         static_assert(LIMBS == 3 && LIMB_BITS == 13, "limbs");
         atomicAdd(&to.count[item], 1u);
@@ -497,8 +512,8 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         for (int i = threadIdx.x; i < (1 + LIMBS) * N; i += THREADS) counts.count[i] = 0;        // the limbs lie behind
         __syncthreads();
     }
-    // Sums up the CTAs' bins, each CTA a share of them for all, and the groups.  unit(item): what a mass of 1 in this bin stands for.
-    template <int N, typename Unit> __device__ void join(BinCounts<N> &counts, BinTotals<N> &totals, Unit &&unit)
+    // Sums up the CTAs' bins, each CTA a share of them for all, and the groups.  top_weight(item): that of the bin's top.
+    template <int N, typename TopWeight> __device__ void join(BinCounts<N> &counts, BinTotals<N> &totals, TopWeight &&top_weight)
     {
         meet(cluster, ctas);
         for (int i = rank * THREADS + (int)threadIdx.x; i < N; i += ctas * THREADS) {
@@ -510,10 +525,10 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
 #pragma unroll
                 for (int l = 0; l < LIMBS; ++l) limbs[l] += b->limb[l][i];
             }
-            unsigned long long mass = 0;
+            long long rest = -(long long)count * (long long)(SLACK * UNIT);
 #pragma unroll
-            for (int l = 0; l < LIMBS; ++l) mass += limbs[l] << (l * LIMB_BITS);
-            const double m = mass ? (double)mass * (1.0 / MASS_ONE) * unit(i) : 0.0;
+            for (int l = 0; l < LIMBS; ++l) rest += (long long)(limbs[l] << (l * LIMB_BITS));
+            const double m = count ? ((double)count - (double)rest * (1.0 / UNIT)) * top_weight(i) : 0.0;
             for (int r = 0; r < ctas; ++r) {
                 BinTotals<N> *t = of(&totals, r);
                 t->count[i] = count;
@@ -572,7 +587,7 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         Place p = find_bin(bins.depths, 0, target, Place{0, 0, 0.0});
         const int bin = p.item;
         const bool massless = bin == BINS - 1;
-        const double unit = massless ? 0.0 : exp(-bin * STEP);
+        const double top_weight = massless ? 0.0 : exp(-bin * STEP);
         uint32_t lo = lowest_of(bin), hi = bin == 0 ? key_of(top32) : lowest_of(bin - 1) - 1;
         if (!whole && bins.depths.count[bin] <= Bins::LIST) make_list(lo, hi);
         for (;;) {
@@ -588,7 +603,7 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
                 else if (PPOW_CHECK(item < SUB, 802, nullptr))
                     atomicAdd(&bins.sub.count[item], 1u);
             });
-            join(bins.sub, bins.subs, [&](int) { return unit; });
+            join(bins.sub, bins.subs, [&](int) { return top_weight; });
             sum_bins(bins.subs, BINS / SEARCH_GROUP);
             p = find_bin(bins.subs, BINS / SEARCH_GROUP, target, p);
             hi -= (uint32_t)p.item << shift;
@@ -606,11 +621,12 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
             });
             meet(cluster, ctas);
             const float value = float_of(sh.only_key);
-            return {value, p.count + 1, p.mass + (massless ? 0.0 : weight(value)), sh.only_token, 0, 1};
+            return {value, p.count + 1, p.mass + (massless ? 0.0 : weight_in(value, bin, top_weight)), sh.only_token, 0, 1};
         }
         const float value = float_of(hi);
         if (massless && !target.by_count()) return {value, p.count + 1, p.mass, -1, 0, have};
-        return choose(target, p, value, have, massless ? 0.0 : weight(value));
+        // the weight that the masses were added up from: a border on a multiple of it stays there
+        return choose(target, p, value, have, massless ? 0.0 : weight_in(value, bin, top_weight));
     }
     __device__ void run(int64_t row)
     {
