@@ -9,6 +9,8 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <ATen/record_function.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -93,9 +95,18 @@ struct Place {
     {
         if (here) stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
     }
-    // without the dispatcher, which the type and device would only lead back here (3 tensors: 0.9 us less)
+    // Whether somebody is to see, or fill, what is allocated: dispatch modes and other changes of this thread's dispatch keys, observers of
+    // operators (the profiler), deterministic algorithms, which fill memory.
+    static bool watched()
+    {
+        const c10::impl::LocalDispatchKeySet keys = c10::impl::tls_local_dispatch_key_set();
+        return keys.included_ != c10::default_included_set || keys.excluded_ != c10::default_excluded_set || at::hasCallbacks() ||
+               at::globalContext().deterministicAlgorithms();
+    }
+    // Unwatched, without the dispatcher, which the type and device would only lead back here (3 tensors: 0.9 us less).
     at::Tensor empty(at::IntArrayRef sizes, at::ScalarType type) const
     {
+        if (watched()) return at::empty(sizes, options.dtype(type));
         return at::detail::empty_cuda(sizes, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)dev), c10::nullopt);
     }
     at::Tensor scratch(size_t bytes) const { return empty({(int64_t)(bytes ? bytes : 256)}, at::kByte); }
