@@ -765,6 +765,8 @@ def ppow_clip_gradients(grads, out, max_norm: float, norm, workspace, stream=Non
           None if out is None else ptrs(*[t.data_ptr() for t in out]), i64s(*[t.numel() for t in grads]),
           i32s(*[DTYPE_CODES[t.dtype] for t in grads]), float(max_norm), _arg(norm, torch.float32, norm.shape, dev, "norm"),
           *_workspace_arg(workspace, dev), _raw_stream(stream, dev))
+    if out is not None:
+        torch.autograd.graph.increment_version([t for t in out if not t.is_inference()])
 
 
 def make_sample_params(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) -> ppow_sample_params:
@@ -1078,7 +1080,8 @@ def rms_norm_backward(grad_y, x, weight, rstd, *, grad_sum=None, stream=None):
 def clip_gradients(grads, max_norm, *, out=None, stream=None):
     """Scale the gradients ``grads`` (a sequence of CUDA tensors of one device, dense, of any shapes and float types) by
     min(1, max_norm / norm), norm the square root of the sum of all their squares: in place, or into the tensors of ``out``, which have
-    the gradients' shapes, types and strides.  Returns norm, a float32 tensor without dimensions; nothing waits for it."""
+    the gradients' shapes, types and strides.  Returns norm, a float32 tensor without dimensions; nothing waits for it.  To autograd the
+    tensors written are modified in place: a backward pass that saved one raises."""
     return _clip(grads, grads if out is None else out, max_norm, stream)
 
 

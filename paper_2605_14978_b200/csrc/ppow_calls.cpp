@@ -327,6 +327,9 @@ py::object clip_gradients(const py::list &grad_list, const py::object &out_list,
     const at::Tensor ws = at.scratch(bytes);
     const ppow_status st = lib.clip_gradients((int32_t)n, from.data(), write ? to.data() : nullptr, sizes.data(), dtypes.data(), max_norm,
                                               norm.data_ptr<float>(), ws.data_ptr(), bytes, at.stream);
+    if (st == PPOW_OK)
+        for (const at::Tensor *t : out)                      // for autograd, modified in place (inference tensors keep no version)
+            if (!t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
     return py::make_tuple(status_of(st), to_python(norm));
 }
 
