@@ -297,6 +297,11 @@ bool tensors_of(const py::list &list, std::vector<const at::Tensor *> &tensors)
     return true;
 }
 
+bool alike(const c10::TensorImpl *a, const c10::TensorImpl *b)
+{
+    return a->key_set() == b->key_set() && a->dtype() == b->dtype() && a->device() == b->device();
+}
+
 py::object clip_gradients(const py::list &grad_list, const py::object &out_list, double max_norm)
 {
     std::vector<const at::Tensor *> grads, out;
@@ -311,16 +316,24 @@ py::object clip_gradients(const py::list &grad_list, const py::object &out_list,
     std::vector<void *> to(write ? n : 0);
     std::vector<int64_t> sizes(n);
     std::vector<int32_t> dtypes(n);
+    // tensors with the dispatch keys, the device and the type of one that was looked at are like it
+    const c10::TensorImpl *like = nullptr;
+    int32_t like_code = -1;
     for (size_t i = 0; i < n; ++i) {
         const at::Tensor &g = *grads[i];
-        if (!on_device(g, at.dev) || (dtypes[i] = code_of(g.scalar_type())) < 0 || !g.is_non_overlapping_and_dense()) return py::none();
-        from[i] = g.data_ptr();
+        const c10::TensorImpl *impl = g.unsafeGetTensorImpl();
+        if (!like || !alike(impl, like)) {
+            if (!on_device(g, at.dev) || (like_code = code_of(g.scalar_type())) < 0) return py::none();
+            like = impl;
+        }
+        if (!g.is_non_overlapping_and_dense()) return py::none();
+        dtypes[i] = like_code;
+        from[i] = g.const_data_ptr();
         sizes[i] = g.numel();
         if (!write) continue;
         const at::Tensor &o = *out[i];
-        if (&o != &g && (!on_device(o, at.dev) || o.scalar_type() != g.scalar_type() || o.sizes() != g.sizes() || o.strides() != g.strides()))
-            return py::none();
-        to[i] = o.data_ptr();
+        if (&o != &g && (!o.defined() || !alike(o.unsafeGetTensorImpl(), like) || o.sizes() != g.sizes() || o.strides() != g.strides())) return py::none();
+        to[i] = o.mutable_data_ptr();
     }
     const at::Tensor norm = at.empty({}, at::kFloat);
     const size_t bytes = lib.clip_workspace_bytes((int32_t)n);
