@@ -206,7 +206,8 @@ template <int PER> struct Scan {
         }
     }
     __device__ __forceinline__ Part all() const { return {__shfl_sync(0xffffffffu, count[PER], 31), __shfl_sync(0xffffffffu, mass[PER], 31)}; }
-    // The last item that adds something, if rounding leaves the border to none.
+    // Only items with elements: the lanes' sums are rounded in orders of their own, so behind the last element one may be the first to reach
+    // a mass next to the whole.  If rounding leaves the border to none, the last item that adds some mass, or an element.
     __device__ __forceinline__ Place find(Target target) const
     {
         const int lane = threadIdx.x & 31;
@@ -214,16 +215,16 @@ template <int PER> struct Scan {
             Place p = {-1, 0, 0.0};
 #pragma unroll
             for (int i = PER - 1; i >= 0; --i) {
-                const bool here = target.met(count[i + 1], mass[i + 1]);
+                const bool here = count[i + 1] > count[i] && target.met(count[i + 1], mass[i + 1]);
                 p = {here ? lane * PER + i : p.item, here ? count[i] : p.count, here ? mass[i] : p.mass};
             }
             const uint32_t who = __ballot_sync(0xffffffffu, p.item >= 0);
-            if (who || again) {
+            if (who || again == 2) {
                 const int from = who ? __ffs(who) - 1 : 31;
                 return {max(__shfl_sync(0xffffffffu, p.item, from), 0), __shfl_sync(0xffffffffu, p.count, from), __shfl_sync(0xffffffffu, p.mass, from)};
             }
             const Part sum = all();
-            target = target.by_count() ? Target::at_count(sum.count) : Target::mass_from(sum.mass);
+            target = target.by_count() || again ? Target::at_count(sum.count) : Target::mass_from(sum.mass);
         }
     }
 };
@@ -242,7 +243,7 @@ struct Element {
 __device__ __forceinline__ Element choose(const Target &target, const Place &before, float value, uint32_t have, double weight)
 {
     uint32_t rank = 0;
-    if (have == 1) {
+    if (have <= 1) {
     } else if (target.by_count()) {
         rank = min(target.count - before.count, have) - 1;
     } else {
@@ -555,6 +556,7 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         if (threadIdx.x < 32) {
             const Scan<PER> groups(GROUPS, before, [&](int i) { return Part{sh.group_count[first + i], sh.group_mass[first + i]}; });
             Place p = groups.find(target);
+            if (!PPOW_CHECK(p.item < GROUPS, 804, nullptr)) p.item = 0;
             const int start = p.item * SEARCH_GROUP;
             const Scan<1> in_group(SEARCH_GROUP, p, [&](int i) { return Part{totals.count[start + i], totals.mass[start + i]}; });
             p = in_group.find(target);
@@ -1088,6 +1090,7 @@ __device__ __forceinline__ void decide_counted(const SampleJob &job, int64_t row
     }
     auto find = [&](const Target &target) {
         Place p = groups.find(target);
+        if (!PPOW_CHECK(p.item < G::ALL, 805, nullptr)) p.item = 0;
         const int group = G::at(p.item);
         if (group == G::ZERO) return choose(target, p, 0.0f, sh.zeros, exp(-top * per_nat));
         // four words a lane, of the group's numbers in descending order, from the CTA that added this group up
