@@ -277,6 +277,8 @@ __global__ void __launch_bounds__(norm_threads<TPR>()) norm_backward_kernel(cons
                 s1 += part[turn][i].x;
                 s2 += part[turn][i].y;
             }
+        } else {
+            __syncwarp();                                    // the next row's start writes over scalars that all lanes have read by now
         }
         s1 *= -inv_d;
         s2 *= -inv_d;
