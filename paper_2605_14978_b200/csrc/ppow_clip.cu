@@ -6,8 +6,9 @@
 // takes each run from its end, so that it starts with what the first pass read last and the L2 cache still holds.  The table of
 // tensors travels as a kernel argument: no copy to the device, and a captured graph holds it.
 //
-// Squares are added in float32, 16 to 32 to a chain, and from there in float64.  Chains whose sum lies outside the range where float32
-// squares are good (overflow, or below 2^-96, where squares of 2^-63 and less have lost bits) are added again in float64.
+// A thread's squares of a chunk, 64 of 16-bit types or 32 of float32, are added in float32, as four chains of 16 or 8 that are then joined,
+// and from there on in float64.  In float64 from the start, where their float32 sum lies outside the range in which float32 squares
+// are good (overflow, or below 2^-96, where squares of 2^-63 and less have lost bits).  The norm is right to 10 half steps of float32.
 #include "ppow_checked.cuh"
 #include "ppow_rows.cuh"
 
@@ -169,7 +170,7 @@ __global__ void __launch_bounds__(CLIP_THREADS, 4) clip_norm_kernel(const __grid
 // A factor as a power of two and the rest.  Below 2^-100 float32 has no bits for it, or soon not, and the product may still be an ordinary
 // number (1e35 clipped to 1e-5): the power of two takes 2^-100 of the exponent away.  The first product is exact, or so small that
 // nothing is left after the second.  Loops of their own for the two, the rare one a unit at a time: with both products in one loop all calls
-// pay (743 M bf16: 717 us, so 705), and with more than 128 registers one CTA is left on an SM (791 us).
+// pay (743 M bf16: 717 us, so 709), and with more than 128 registers one CTA is left on an SM (791 us).
 struct ClipFactor {
     float power = 1.0f, rest = 1.0f;
     __device__ __forceinline__ bool small() const { return power != 1.0f; }

@@ -316,8 +316,8 @@ __device__ __forceinline__ void decide(const SampleJob &job, float u, uint32_t F
 // The index of an element of this piece that `matches` accepts and `behind` others follow, searched from the end, where the pass over the row
 // was last and the L2 cache still holds most, in rounds: each warp a stretch of neighbouring units, the next round's on their way while
 // this one's are counted.  matches: a byte with a bit for each of a unit's elements, that of element e at e / 2 + 4 (e % 2) where there are
-// eight, at e where there are four.  Out of line: inlined, it takes registers from the rest (4096 x 128256: 10 % slower).  From
-// the row's start the same took 438 us, so 432.
+// eight, at e where there are four.  Out of line: inlined, it takes registers from the rest (4096 x 128256 bf16: 471 us, so 420).
+// From the row's start the same takes 428 us.
 template <int THREADS, int DTYPE, typename Matches>
 __device__ __noinline__ void locate(const Piece<DTYPE> piece, uint32_t behind, SampleShared &sh, int32_t *token, const Matches matches)
 {
@@ -443,7 +443,7 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
             for (int i = threadIdx.x; i < listed; i += THREADS) f(float_of((uint32_t)(bins.list[i] >> 32)), (int32_t)(uint32_t)bins.list[i]);
             return;
         }
-        // one unit at a time: more of them in flight make the code longer and the kernel slower (4: 592 us, 1: 527, 512 x 152064)
+        // one unit at a time: more of them in flight make the code longer and the kernel slower (4: 535 us, 1: 507, 512 x 152064)
         for (int32_t u = piece.begin + (int32_t)threadIdx.x; u < piece.end; u += THREADS) {
             float z[E];
             S::unpack(piece.load(u), z);
@@ -752,7 +752,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_search_kernel(
 // ---- sorting: short float32 rows --------------------------------------------------------------------
 // A row of up to SORT_THREADS * PER logits, sorted in registers: thread t holds the elements PER t .. of the order.  An entry is key << 32 | ~index,
 // so that descending entries are descending numbers, equal ones by index; 0 is none.  Exchanges within PER places stay in a thread, within
-// 32 PER in a warp, and only the rest goes through shared memory (256 x 1000: 23 us by a search, 9 us so).
+// 32 PER in a warp, and only the rest goes through shared memory (256 x 1000: 21 us by a search, 10 us so).
 constexpr int SORT_THREADS = 256, SORT_WARPS = SORT_THREADS / 32;
 
 template <int PER> __device__ __forceinline__ void sort_entries(unsigned long long (&v)[PER], unsigned long long *exchange)
@@ -1257,9 +1257,9 @@ bool sample_launch(size_t smem, const SampleJob &job, int32_t units, cudaStream_
         ready[dev].store(true, std::memory_order_relaxed);
     }
     // Few rows are shared out, until 768 threads to an SM have work, each CTA with 1024 units or more: what a CTA does besides reading
-    // its piece costs as much as 2000 units.  74 x 128256 bf16: 31 us with 296 CTAs, 35 with 148, 47 with 592; f16: 37 with 148, 61 with
-    // 296; f32: 92 and 121.  And no more than PIECE_MOST logits to a CTA.  (A float32 row is passed over four times: shared by four CTAs
-    // the rows in work would stay in the L2 cache, but each pass ends in meetings.  512 x 152064: 717 us against 590.)
+    // its piece costs as much as 2000 units.  74 x 128256: bf16 25 us with 296 CTAs, 28 with 148, 38 with 592; f16 29 with 148, 50 with
+    // 296; f32 68 with 148, 109 with 74, 87 with 296.  And no more than PIECE_MOST logits to a CTA.  (A float32 row is passed over four times:
+    // shared by four CTAs the rows in work would stay in the L2 cache, but each pass ends in meetings.  512 x 152064: 561 us against 507.)
     int ctas = 1;
     while (ctas < SAMPLE_CTAS && (((int64_t)job.R * ctas * 2 * THREADS <= 148 * 768 && units / (ctas * 2) >= 1024) || job.V > (int64_t)PIECE_MOST * ctas)) ctas *= 2;
     cudaLaunchConfig_t config = {};
