@@ -577,10 +577,11 @@ template <int DTYPE, int THREADS, int BINS> struct Search {
         each([&](float z, int32_t token) {
             if (!(z >= low && z <= high)) return;
             const uint32_t at = atomicAdd(&sh.listed, 1u);
-            if (PPOW_CHECK(at < Bins::LIST, 803, nullptr)) bins.list[at] = (unsigned long long)key_of(z) << 32 | (uint32_t)token;
+            // they were counted, but in another reading: a row that changes meanwhile must not write past the list
+            if (PPOW_CHECK(at < Bins::LIST, 803, nullptr) && at < Bins::LIST) bins.list[at] = (unsigned long long)key_of(z) << 32 | (uint32_t)token;
         });
         __syncthreads();
-        listed = (int)sh.listed;
+        listed = min((int)sh.listed, (int)Bins::LIST);
     }
     // The element on the border; the whole CTA, and the whole cluster in step.  The list, if there is one, is left.
     __device__ Element find(const Target &target, bool whole)
