@@ -328,12 +328,12 @@ py::object clip_gradients(const py::list &grad_list, const py::object &out_list,
         }
         if (!g.is_non_overlapping_and_dense()) return py::none();
         dtypes[i] = like_code;
-        from[i] = g.const_data_ptr();
+        from[i] = g.data_ptr();                              // in place it has to be the address that is written
         sizes[i] = g.numel();
         if (!write) continue;
         const at::Tensor &o = *out[i];
         if (&o != &g && (!o.defined() || !alike(o.unsafeGetTensorImpl(), like) || o.sizes() != g.sizes() || o.strides() != g.strides())) return py::none();
-        to[i] = o.mutable_data_ptr();
+        to[i] = o.data_ptr();
     }
     const at::Tensor norm = at.empty({}, at::kFloat);
     const size_t bytes = lib.clip_workspace_bytes((int32_t)n);
